@@ -285,6 +285,128 @@ evo_status evo_redundancy_map(const float* trace, int32_t T, int32_t U, int32_t 
 evo_status evo_guided_schedules(const float* d, int32_t U, int32_t T, int32_t K, float eps, int32_t gamma,
                                 const uint64_t* rnd, int32_t P, uint8_t* S, void* stream);
 
+/* Unit caches in 8 bits: Eq. 1 for policies that run their own units (other
+ * widths, layers or architectures than evo_denoise serves).  A unit's cache of N
+ * samples is codes [N][H][E] (e4m3, a byte each) and scales [N][H][E/32]: one
+ * power of two for every 32 values, 2^k with the least integer k >= -126 for
+ * which the group's largest magnitude is at most 448 * 2^k, held as the byte
+ * k + 127 (255: the group holds a NaN or an infinity and reads back as NaN).  A
+ * code is value * 2^-k rounded to nearest even, so a cached value is off by at
+ * most 2^-4 of itself, or 2^(k-10) below 2^(k-6).
+ *
+ * evo_cache_write refreshes a unit: for every sample n with refresh[n] != 0 (all,
+ * if refresh is NULL) the codes and scales of r[n] are stored and y[n] = x[n] +
+ * r[n]; for the others the cache stays as it is and y[n] = x[n].
+ *   r       device [N][H][E] of `dtype` (EVO_DTYPE_*)
+ *   refresh device [N] uint8 or NULL
+ *   x, y    device [N][H][E] fp32: the residual stream before and after; y may be
+ *           x; both NULL: only the cache is written
+ * evo_cache_add reuses a run of U skipped units: y[n] = x[n] + the cached values
+ * of every unit u with reuse[u][n] != 0 (all, if reuse is NULL), added in unit
+ * order in fp32.
+ *   codes   device [U][N][H][E], scales device [U][N][H][E/32]
+ *   reuse   device [U][N] uint8 or NULL
+ * E is a multiple of 32, N * H * E at most 2^33.  N = 0 or H = 0 launches nothing;
+ * U = 0 copies x.  x and y are the same buffer or do not overlap; fp32 and bf16
+ * buffers start on 16 bytes, codes on 8 (EVO_ERR_ARG otherwise).  Asynchronous on
+ * the stream; every buffer belongs to the current device. */
+evo_status evo_cache_write(const void* r, int32_t dtype, const uint8_t* refresh, int32_t N, int32_t H, int32_t E,
+                           const float* x, float* y, uint8_t* codes, uint8_t* scales, void* stream);
+evo_status evo_cache_add(const uint8_t* codes, const uint8_t* scales, const uint8_t* reuse, int32_t U, int32_t N,
+                         int32_t H, int32_t E, const float* x, float* y, void* stream);
+
+/* Paged memory: keys and values of tokens that a policy keeps (observations,
+ * past actions), appended as they come in and read by the attention of each
+ * chunk of new tokens.  It is what evo_denoise's memory of 1 + n_obs tokens is for
+ * a policy whose memory is long, grows, or is shared by candidates.
+ *
+ * The memory of sequence n (of n_seq) is the tokens 0 .. lens[n]-1; token i lies
+ * in page table[n][i / page_tokens] at slot i % page_tokens.  Sequences may share
+ * pages.  A call's new tokens ("rows") stand one sequence after the other:
+ * sequence n has the rows starts[n] .. starts[n+1]-1, possibly none; rows before
+ * starts[0] or behind starts[n_seq] are left as they are.  starts NULL: n_seq
+ * chunks of equal length.  lens counts a sequence's new tokens as part of its
+ * memory wherever they are (evo_memory_append, causal attention): row j of m is
+ * token lens[n] - m + j.
+ *
+ * dtype is the type of the rows (queries, keys, values, outputs); format is how
+ * pages hold keys and values: the same type, or EVO_CACHE_E4M3, e4m3 codes with a
+ * scale byte per token and head in k_scales / v_scales (the format of the unit
+ * caches, the group being the head's row).
+ *
+ * A page entry outside 0 .. n_pages-1, a length outside 0 .. max_pages *
+ * page_tokens or above max_len, starts that fall or count more than the call's
+ * rows or max_new, and a rotation position outside the table make EVO_ERR_CORRUPT in
+ * *status (device memory, zeroed by the caller; NULL: not reported).  Nothing out
+ * of bounds is read or written for them; evo_memory_append stores no such token
+ * and leaves its q_out row, and evo_memory_attend's rows of such a sequence are unspecified. */
+enum { EVO_CACHE_F32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_E4M3 = 2 };
+typedef struct evo_memory {
+  int32_t dtype;            /* EVO_DTYPE_* of the rows */
+  int32_t format;           /* EVO_CACHE_* of the pages: E4M3, or the one that matches dtype */
+  int32_t n_head;           /* query heads, a multiple of n_kv_head */
+  int32_t n_kv_head;        /* key/value heads; query head h reads key/value head h * n_kv_head / n_head */
+  int32_t head_dim;         /* 64 or 128 */
+  int32_t page_tokens;      /* 16, 32, 64 or 128 */
+  int32_t n_pages;          /* pages of the pool */
+  int32_t max_pages;        /* columns of the table; max_pages * page_tokens < 2^31 */
+  int32_t n_seq;
+  int32_t pad_;
+  void *k_pages, *v_pages;  /* device [n_pages][n_kv_head][page_tokens][head_dim], start on 16 bytes */
+  uint8_t *k_scales, *v_scales;   /* device [n_pages][n_kv_head][page_tokens]; NULL unless E4M3 */
+  const int32_t* table;     /* device [n_seq][max_pages] */
+  const int32_t* lens;      /* device [n_seq] */
+  const int32_t* starts;    /* device [n_seq + 1] or NULL */
+  int32_t* status;          /* device [1] or NULL */
+} evo_memory;
+
+/* Cosines and sines of positions 0 .. n_pos-1 for evo_memory_append, computed in
+ * double precision: out (host) [n_pos][head_dim] = cos(p w_i) | sin(p w_i), i <
+ * head_dim / 2, w_i = base^(-2i / head_dim).  base > 0. */
+evo_status evo_rotation_table(int32_t n_pos, int32_t head_dim, double base, float* out);
+
+/* Append the call's rows to their memories.  Queries and keys get, per head, an
+ * RMS norm x / sqrt(mean(x^2) + eps) * gain where their gain is given, and a
+ * rotation of the pairs (i, i + head_dim/2) by their position where `rotation` is;
+ * keys and values go to their pages, queries to q_out.  fp32 inside, one rounding.
+ *   q, k, v  device [rows][heads][head_dim], ld* elements between rows (so that they
+ *            may be column ranges of one projection).  q NULL: only keys and values
+ *            are appended; k and v NULL: only queries are made
+ *   q_out    device [rows][n_head][head_dim], ldo between rows; may be q
+ *   q_gain, k_gain  device [head_dim] fp32 or NULL (no norm)
+ *   rotation device [n_pos][head_dim] fp32 (evo_rotation_table) or NULL
+ *   pos0     device [n_seq] or NULL (zero): position of a memory's token 0, so that a
+ *            memory whose oldest pages were dropped keeps its positions
+ * Buffers start on 16 bytes and row strides are multiples of 16 bytes, at least
+ * a row (EVO_ERR_ARG).  Two rows of a call must not be the same token of the same
+ * page (sequences that share their last page are not appended to in one call).
+ * Asynchronous on the stream. */
+evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k, const void* v, int64_t ldq,
+                             int64_t ldk, int64_t ldv, int32_t rows, const float* q_gain, const float* k_gain,
+                             float eps, const float* rotation, int32_t n_pos, const int32_t* pos0, void* q_out,
+                             int64_t ldo, void* stream);
+
+/* Attention of the call's rows over their memories:
+ *   out = softmax over the keys i that a row sees of (scale <q, k_i>) times v_i
+ * causal = 0: every row sees the whole memory, 0 .. lens[n]-1; causal = 1: row j of
+ * m sees tokens up to its own, lens[n] - m + j.  window > 0: only the last `window`
+ * of those.  A row that sees no key is zero; what a masked token holds (a NaN,
+ * too) reaches no row that does not see it.
+ *   q, out  device [rows][n_head][head_dim], ldq / ldo elements between rows; start
+ *           on 16 bytes, strides multiples of 16 bytes.  They must not overlap
+ *   max_new, max_len  at least the largest chunk and memory of the call: they size the
+ *           launch, nothing else depends on them
+ *   scratch device, evo_memory_scratch_bytes(mem, rows, max_new, max_len) bytes,
+ *           16-byte aligned, caller-owned; need not be cleared.  Calls that overlap on
+ *           the GPU need their own
+ * Scores, softmax statistics and sums are fp32.  With bf16 rows the weights
+ * 2^(s - max) are rounded to bf16 before their product with the values.
+ * Deterministic; asynchronous on the stream. */
+size_t evo_memory_scratch_bytes(const evo_memory* mem, int32_t rows, int32_t max_new, int32_t max_len);
+evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
+                             int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,
+                             void* scratch, void* stream);
+
 /* Schedule search (Sec. 3.2 genetic algorithm, Sec. 3.3 redundancy-guided
  * initialisation and target-conditioned early stopping, Eq. 8 and 9).  Host
  * code; fitness comes from the caller:

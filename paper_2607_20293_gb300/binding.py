@@ -40,6 +40,13 @@ class SearchConfig(ctypes.Structure):
                 ("delta_acc", ctypes.c_double), ("seed", ctypes.c_uint64)]
 
 
+class MemoryView(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("dtype", "format", "n_head", "n_kv_head", "head_dim", "page_tokens",
+                                               "n_pages", "max_pages", "n_seq", "pad_")]
+                + [(f, ctypes.c_void_p) for f in ("k_pages", "v_pages", "k_scales", "v_scales", "table", "lens",
+                                                  "starts", "status")])
+
+
 class SearchResult(ctypes.Structure):
     _fields_ = [("best_fitness", ctypes.c_double), ("generations", ctypes.c_int32), ("evaluations", ctypes.c_int32),
                 ("formal_evaluations", ctypes.c_int32), ("memo_hits", ctypes.c_int32),
@@ -79,6 +86,7 @@ def load(debug: bool = False) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     cfgp = ctypes.POINTER(EvoConfig)
+    memp = ctypes.POINTER(MemoryView)
     sig = {
         "evo_weight_count": (SZ, [cfgp]),
         "evo_create": (I32, [P, SZ, cfgp, I32, ctypes.POINTER(P)]),
@@ -104,6 +112,12 @@ def load(debug: bool = False) -> ctypes.CDLL:
         "evo_redundancy_scratch_bytes": (SZ, [I32, I32, I32, I32, I32]),
         "evo_redundancy_map": (I32, [P, I32, I32, I32, I32, I32, P, P, P]),
         "evo_guided_schedules": (I32, [P, I32, I32, I32, ctypes.c_float, I32, P, I32, P, P]),
+        "evo_cache_write": (I32, [P, I32, P, I32, I32, I32, P, P, P, P, P]),
+        "evo_cache_add": (I32, [P, P, P, I32, I32, I32, I32, P, P, P]),
+        "evo_rotation_table": (I32, [I32, I32, ctypes.c_double, P]),
+        "evo_memory_append": (I32, [memp, P, P, P, I64, I64, I64, I32, P, P, ctypes.c_float, P, I32, P, P, I64, P]),
+        "evo_memory_scratch_bytes": (SZ, [memp, I32, I32, I32]),
+        "evo_memory_attend": (I32, [memp, P, I64, I32, I32, I32, ctypes.c_float, I32, I32, P, I64, P, P]),
         "evo_status_string": (ctypes.c_char_p, [I32]),
     }
     for name, (res, args) in sig.items():
@@ -352,6 +366,200 @@ def guided_schedules(d, K: int, rnd, eps: float = 0.05, gamma: int = 2, stream=N
     _check(load().evo_guided_schedules(_ptr(d), U, T, K, float(eps), int(gamma), _ptr(rnd), P, _ptr(S),
                                        _stream(stream)), "evo_guided_schedules")
     return S
+
+
+CACHE_FORMATS = {"fp32": 0, "bf16": 1, "e4m3": 2}
+UNIT_GROUP = 32          # values of a unit's cache that share a scale
+
+
+def _need(t, what: str, dtype, shape=None, device=None):
+    """A contiguous tensor of this type (and shape, and device), or ValueError."""
+    if str(t.dtype) != dtype and str(t.dtype) not in dtype:
+        raise ValueError(f"{what}: type {t.dtype}, expected {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: must be contiguous")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what}: on {t.device}, expected {device}")
+    return t.data_ptr()
+
+
+def _current(device):
+    """Check that `device` is the current CUDA device: the library launches there."""
+    import torch
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {device}, the call runs on the current CUDA device")
+
+
+_F32, _U8, _I32 = "torch.float32", "torch.uint8", "torch.int32"
+_DTYPE_OF = {"torch.float32": 0, "torch.bfloat16": 1}
+
+
+def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
+    """evo_cache_write: the residual r [N][H][E] (fp32 or bf16) to the unit's 8-bit
+    cache (codes [N][H][E], scales [N][H][E/32], uint8) for the samples whose
+    refresh [N] (uint8) is not zero, or all.  Returns y = x + r for those samples
+    and x for the others (in `out`, which may be x), or None without x."""
+    N, H, E = r.shape
+    dev = r.device
+    _current(dev)
+    rp = _need(r, "r", tuple(_DTYPE_OF))
+    cp = _need(codes, "codes", _U8, (N, H, E), dev)
+    sp = _need(scales, "scales", _U8, (N, H, E // UNIT_GROUP), dev)
+    gp = None if refresh is None else _need(refresh, "refresh", _U8, (N,), dev)
+    xp = yp = None
+    if x is not None:
+        xp = _need(x, "x", _F32, r.shape, dev)
+        if out is None:
+            import torch
+            out = torch.empty_like(x)
+        yp = _need(out, "out", _F32, r.shape, dev)
+    elif out is not None:
+        raise ValueError("out without x")
+    _check(load().evo_cache_write(rp, _DTYPE_OF[str(r.dtype)], gp, N, H, E, xp, yp, cp, sp, _stream(stream)),
+           "evo_cache_write")
+    return out
+
+
+def cache_add(codes, scales, x, reuse=None, out=None, stream=None):
+    """evo_cache_add: x [N][H][E] (fp32) plus the cached values of a run of units
+    (codes [U][N][H][E], scales [U][N][H][E/32]) where reuse [U][N] is not zero, or
+    of all; in `out` (which may be x) or a new tensor."""
+    import torch
+    U, N, H, E = codes.shape
+    dev = x.device
+    _current(dev)
+    cp = _need(codes, "codes", _U8, None, dev)
+    sp = _need(scales, "scales", _U8, (U, N, H, E // UNIT_GROUP), dev)
+    gp = None if reuse is None else _need(reuse, "reuse", _U8, (U, N), dev)
+    xp = _need(x, "x", _F32, (N, H, E), dev)
+    if out is None:
+        out = torch.empty_like(x)
+    yp = _need(out, "out", _F32, (N, H, E), dev)
+    _check(load().evo_cache_add(cp, sp, gp, U, N, H, E, xp, yp, _stream(stream)), "evo_cache_add")
+    return out
+
+
+def rotation_table(n_pos: int, head_dim: int, base: float = 10000.0) -> np.ndarray:
+    """Cosines and sines [n_pos][head_dim] of positions 0 .. n_pos-1 (evo_rotation_table), float32 on the host."""
+    out = np.empty((n_pos, head_dim), dtype=np.float32)
+    _check(load().evo_rotation_table(n_pos, head_dim, float(base), out.ctypes.data), "evo_rotation_table")
+    return out
+
+
+class Memory:
+    """A paged memory (evo_memory) over caller-owned CUDA tensors.
+
+    k_pages, v_pages  [n_pages][n_kv_head][page_tokens][head_dim]: of `dtype`, or uint8
+                      e4m3 codes with k_scales, v_scales [n_pages][n_kv_head][page_tokens]
+    table [n_seq][max_pages], lens [n_seq], starts [n_seq + 1] or None (equal chunks),
+    status [1] or None: int32.  The tensors are kept; their contents may change between calls.
+    """
+
+    def __init__(self, k_pages, v_pages, table, lens, n_head: int, k_scales=None, v_scales=None, starts=None,
+                 status=None, dtype: str = "bf16"):
+        self._lib = load()
+        dev = self.device = k_pages.device
+        e4m3 = k_pages.dtype.itemsize == 1
+        self.torch_dtype = "torch.float32" if dtype == "fp32" else "torch.bfloat16"
+        n_pages, n_kv, page, dim = k_pages.shape
+        n_seq, cols = table.shape
+        kind = _U8 if e4m3 else self.torch_dtype
+        if e4m3 != (k_scales is not None) or e4m3 != (v_scales is not None):
+            raise ValueError("scales belong to pages of 8-bit codes")
+        v = MemoryView(DTYPES[dtype], CACHE_FORMATS["e4m3" if e4m3 else dtype], n_head, n_kv, dim, page, n_pages, cols,
+                       n_seq, 0)
+        v.k_pages = _need(k_pages, "k_pages", kind)
+        v.v_pages = _need(v_pages, "v_pages", kind, k_pages.shape, dev)
+        if e4m3:
+            v.k_scales = _need(k_scales, "k_scales", _U8, k_pages.shape[:3], dev)
+            v.v_scales = _need(v_scales, "v_scales", _U8, k_pages.shape[:3], dev)
+        v.table = _need(table, "table", _I32, None, dev)
+        v.lens = _need(lens, "lens", _I32, (n_seq,), dev)
+        v.starts = None if starts is None else _need(starts, "starts", _I32, (n_seq + 1,), dev)
+        v.status = None if status is None else _need(status, "status", _I32, (1,), dev)
+        self.view, self._ref = v, ctypes.byref(v)
+        self.n_head, self.n_kv_head, self.head_dim, self.n_seq = n_head, n_kv, dim, n_seq
+        self.max_len = cols * page
+        self.uniform = starts is None
+        self.tensors = (k_pages, v_pages, table, lens, k_scales, v_scales, starts, status)
+
+    def _rows(self, t, what: str, heads: int, rows=None):
+        """(pointer, elements between rows) of [rows][heads][head_dim], heads of a row contiguous."""
+        if str(t.dtype) != self.torch_dtype or t.device != self.device:
+            raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {self.torch_dtype} on {self.device}")
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or rows not in (None, t.shape[0]):
+            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected ({rows or 'rows'}, {heads}, {self.head_dim})")
+        ld, between, within = t.stride()
+        if within != 1 or (heads > 1 and between != self.head_dim):
+            raise ValueError(f"{what}: the heads of a row must be contiguous")
+        return t.data_ptr(), ld if t.shape[0] > 1 else heads * self.head_dim
+
+    def _vector(self, t, what: str, shape, kind=_F32):
+        return None if t is None else _need(t, what, kind, shape, self.device)
+
+    def append(self, q, k, v, q_gain=None, k_gain=None, eps: float = 1e-6, rotation=None, pos0=None, out=None,
+               max_new=None, stream=None):
+        """evo_memory_append: keys and values [rows][n_kv_head][head_dim] to their pages, and the
+        normed and rotated queries [rows][n_head][head_dim] (in `out`, which may be q, or a new
+        tensor).  q may be None (returns None), or k and v.  max_new is not needed here."""
+        import torch
+        _current(self.device)
+        if q is None and k is None:
+            raise ValueError("neither queries nor keys")
+        rows = (k if q is None else q).shape[0]
+        qp = kp = vp = op = None
+        ldq = ldk = ldv = ldo = 0
+        if q is not None:
+            qp, ldq = self._rows(q, "q", self.n_head, rows)
+            if out is None:
+                out = torch.empty((rows, self.n_head, self.head_dim), dtype=q.dtype, device=q.device)
+            op, ldo = self._rows(out, "out", self.n_head, rows)
+        if k is not None or v is not None:
+            if k is None or v is None:
+                raise ValueError("keys and values come together")
+            kp, ldk = self._rows(k, "k", self.n_kv_head, rows)
+            vp, ldv = self._rows(v, "v", self.n_kv_head, rows)
+        n_pos = 0 if rotation is None else rotation.shape[0]
+        _check(self._lib.evo_memory_append(
+            self._ref, qp, kp, vp, ldq, ldk, ldv, rows, self._vector(q_gain, "q_gain", (self.head_dim,)),
+            self._vector(k_gain, "k_gain", (self.head_dim,)), eps,
+            self._vector(rotation, "rotation", (n_pos, self.head_dim)), n_pos,
+            self._vector(pos0, "pos0", (self.n_seq,), _I32), op, ldo, _stream(stream)), "evo_memory_append")
+        return out if q is not None else None
+
+    def attend(self, q, scale=None, causal: bool = True, window: int = 0, max_new=None, max_len=None, out=None,
+               stream=None):
+        """evo_memory_attend: attention of q [rows][n_head][head_dim] over the memories, in `out` or
+        a new tensor (rows of no sequence are left as they are: unset in a new tensor).  scale
+        None: head_dim ** -0.5.  max_new, max_len: bounds on the chunks and memories (None: the
+        rows, or their equal share, and what the table can hold)."""
+        import torch
+        _current(self.device)
+        rows = q.shape[0]
+        qp, ldq = self._rows(q, "q", self.n_head)
+        if out is None:
+            out = torch.empty((rows, self.n_head, self.head_dim), dtype=q.dtype, device=q.device)
+        op, ldo = self._rows(out, "out", self.n_head, rows)
+        if rows == 0:
+            return out
+        if max_new is None:
+            max_new = rows // max(1, self.n_seq) if self.uniform else rows
+        if max_len is None:
+            max_len = self.max_len
+        if scale is None:
+            scale = self.head_dim ** -0.5
+        nb = self._lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
+        scratch = None
+        if nb:
+            scratch = torch.empty(nb, dtype=torch.uint8, device=self.device)
+            if stream is not None:                  # not reused before that stream's work is done
+                scratch.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+        _check(self._lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, scale, int(causal), window, op,
+                                           ldo, scratch.data_ptr() if nb else None, _stream(stream)),
+               "evo_memory_attend")
+        return out
 
 
 def search(n_units: int, n_steps: int, budget: int, quick, formal=None, d_map=None, block_wise: bool = False,

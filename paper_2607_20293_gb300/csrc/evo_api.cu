@@ -137,12 +137,12 @@ int guards_check(const GuardList& list) {
   return 0;
 }
 
+// CUDA runtime error of the most recent failed call on this thread
+thread_local int g_last_cuda_error = 0;
+
 }  // namespace evo
 
 namespace {
-
-// CUDA runtime error of the most recent failed call on this thread
-thread_local int g_last_cuda_error = 0;
 
 #define EVO_CUDA(x)                                   \
   do {                                                \

@@ -1,0 +1,264 @@
+// Attention over a paged memory: the fp32 kernel, the join of split memories
+// and the choice among the kernels.
+//
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(s_j - max s),  s_j = scale log2(e) <q, k_j>
+//
+// over the keys j that the row sees, in one pass with a running maximum and sum
+// (a row that sees none is zero).  A memory split over several blocks leaves each
+// piece's maximum, sum and unnormalised values, which a second kernel joins.
+//
+// fp32 kernel: a block of 256 threads takes BM = 16 RM rows and 64 keys at a
+// time; the thread at (ty, tx) of a 16 x 16 grid computes RM rows x 4 keys of the
+// scores and RM rows x D/16 columns of the output, all products in fp32.
+#include <algorithm>
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "evo_attend.cuh"
+#include "evo_quant.cuh"
+
+namespace evo {
+namespace {
+
+constexpr int BN = 64, THREADS = 256;
+
+template <int D, int RM>
+struct Smem {
+  static constexpr int BM = 16 * RM;
+  float q[BM][D];
+  float k[BN][D + 4];           // rows 4 banks apart: 8 rows' float4 in a phase do not collide
+  float v[BN][D];
+  float p[BM][BN + 4];
+};
+
+template <typename T>
+__device__ __forceinline__ float4 load4f(const T* p);
+template <>
+__device__ __forceinline__ float4 load4f<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <>
+__device__ __forceinline__ float4 load4f<__nv_bfloat16>(const __nv_bfloat16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+
+// 4 values of a key's or value's row in the memory's format
+template <typename T, int FORMAT>
+__device__ __forceinline__ float4 memory4(const void* pages, const uint8_t* scales, long long at, int D, int d) {
+  if constexpr (FORMAT == EVO_CACHE_E4M3) {
+    const float4 c = codes4(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(pages) + at * D + d));
+    const float f = scale_value(scales[at]);
+    return make_float4(c.x * f, c.y * f, c.z * f, c.w * f);
+  } else {
+    return load4f<T>(static_cast<const T*>(pages) + at * D + d);
+  }
+}
+
+__device__ __forceinline__ float dot4(float4 a, float4 b, float c) {
+  return fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, c))));
+}
+
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+template <typename T, int D, int FORMAT, int RM>
+__global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  Smem<D, RM>& sm = *reinterpret_cast<Smem<D, RM>*>(raw);
+  constexpr int BM = 16 * RM, DC = D / 16;
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  const Tile t = tile_of_block(a);
+  const int rows = t.count * a.group, r0 = t.tile * BM;
+  if (r0 >= rows) return;
+  const int last = min(r0 + BM, rows) - 1;
+  const Range all = piece_of(a, t, seen_by_tile(a, t, r0 / a.group, last / a.group), BN);
+
+  for (int i = tid; i < BM * D / 4; i += THREADS) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4, R = r0 + r;
+    float4 x = {};
+    if (R < rows)
+      x = load4f<T>(static_cast<const T*>(a.q) + (t.first + R / a.group) * a.ldq +
+                    (long long)(t.kv_head * a.group + R % a.group) * D + d);
+    *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
+  }
+  Range seen[RM];
+  float mx[RM], sum[RM], o[RM][DC];
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
+    const int R = r0 + ty * RM + i;
+    seen[i] = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
+    mx[i] = -INFINITY;
+    sum[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < DC; ++c) o[i][c] = 0.f;
+  }
+  for (int k0 = all.lo / BN * BN; k0 < all.hi; k0 += BN) {
+    __syncthreads();
+    for (int i = tid; i < BN * D / 4; i += THREADS) {
+      const int r = i / (D / 4), d = i % (D / 4) * 4, key = k0 + r;
+      float4 k = {}, v = {};
+      if (key >= all.lo && key < all.hi) {
+        const int page = seq_page(a.m, t.n, key / a.m.page_tokens);
+        const long long at =
+            ((long long)page * a.m.n_kv_head + t.kv_head) * a.m.page_tokens + key % a.m.page_tokens;
+        k = memory4<T, FORMAT>(a.m.k_pages, a.m.k_scales, at, D, d);
+        v = memory4<T, FORMAT>(a.m.v_pages, a.m.v_scales, at, D, d);
+      }
+      *reinterpret_cast<float4*>(&sm.k[r][d]) = k;
+      *reinterpret_cast<float4*>(&sm.v[r][d]) = v;
+    }
+    __syncthreads();
+    float s[RM][4] = {};
+    for (int d = 0; d < D; d += 4) {
+      float4 q[RM];
+#pragma unroll
+      for (int i = 0; i < RM; ++i) q[i] = *reinterpret_cast<const float4*>(&sm.q[ty * RM + i][d]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 k = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+#pragma unroll
+        for (int i = 0; i < RM; ++i) s[i][j] = dot4(q[i], k, s[i][j]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = k0 + tx + 16 * j;
+        s[i][j] = key >= max(seen[i].lo, all.lo) && key < min(seen[i].hi, all.hi) ? s[i][j] * a.scale_log2 : -INFINITY;
+        top = fmaxf(top, s[i][j]);
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+      const float now = fmaxf(mx[i], top), base = now == -INFINITY ? 0.f : now;
+      const float keep = exp2f(mx[i] - base);
+      mx[i] = now;
+      float add = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = exp2f(s[i][j] - base);
+        add += p;
+        sm.p[ty * RM + i][tx + 16 * j] = p;
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) add += __shfl_xor_sync(0xffffffffu, add, w);
+      sum[i] = sum[i] * keep + add;
+#pragma unroll
+      for (int c = 0; c < DC; ++c) o[i][c] *= keep;
+    }
+    __syncwarp();               // a row's weights come from its own half warp
+    for (int j = 0; j < BN; ++j) {
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        const float p = sm.p[ty * RM + i][j];
+        // a key that the row does not see adds nothing, whatever its value holds
+        if (p != 0.f) {
+#pragma unroll
+          for (int c = 0; c < DC; ++c) o[i][c] = fmaf(p, sm.v[j][tx + 16 * c], o[i][c]);
+        }
+      }
+    }
+    __syncwarp();
+  }
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
+    const int R = r0 + ty * RM + i;
+    if (R >= rows) continue;
+    const int row = t.first + R / a.group, head = t.kv_head * a.group + R % a.group;
+    if (a.splits == 1) {
+      const float f = sum[i] == 0.f ? 0.f : 1.f / sum[i];
+      T* dst = static_cast<T*>(a.out) + row * a.ldo + (long long)head * D;
+#pragma unroll
+      for (int c = 0; c < DC; ++c) put(dst + tx + 16 * c, o[i][c] * f);
+    } else {
+      const long long at = part_index(a, t.split, row, head);
+#pragma unroll
+      for (int c = 0; c < DC; ++c) a.part[at * D + tx + 16 * c] = o[i][c];
+      if (tx == 0) a.ml[at] = make_float2(mx[i], sum[i]);
+    }
+  }
+}
+
+// joins the pieces: a (row, head) per D / 4 lanes
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int LANES = D / 4;
+  const long long i = ((long long)blockIdx.x * THREADS + threadIdx.x) / LANES;
+  const int d = threadIdx.x % LANES * 4;
+  const int row = (int)(i / a.m.n_head), head = (int)(i % a.m.n_head);
+  if (row >= a.rows) return;
+  if (a.m.starts && (row < a.m.starts[0] || row >= a.m.starts[a.m.n_seq])) return;
+  float top = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.ml[part_index(a, s, row, head)].x);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  float4 o = {};
+  for (int s = 0; s < a.splits; ++s) {
+    const long long at = part_index(a, s, row, head);
+    const float2 ml = a.ml[at];
+    const float f = exp2f(ml.x - base);
+    const float4 p = *reinterpret_cast<const float4*>(a.part + at * D + d);
+    sum = fmaf(ml.y, f, sum);
+    o = make_float4(fmaf(p.x, f, o.x), fmaf(p.y, f, o.y), fmaf(p.z, f, o.z), fmaf(p.w, f, o.w));
+  }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  T* dst = static_cast<T*>(a.out) + row * a.ldo + (long long)head * D + d;
+  put(dst, o.x * f);
+  put(dst + 1, o.y * f);
+  put(dst + 2, o.z * f);
+  put(dst + 3, o.w * f);
+}
+
+template <typename T, int D, int FORMAT, int RM>
+cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
+  const auto k = attend_kernel<T, D, FORMAT, RM>;
+  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D, RM>));
+  if (e != cudaSuccess) return e;
+  k<<<grid, THREADS, sizeof(Smem<D, RM>), st>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_as(const AttendArgs& a, int kernel, cudaStream_t st) {
+  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
+  const bool e4m3 = a.m.format == EVO_CACHE_E4M3;
+  cudaError_t e;
+  if (kernel == 1)
+    e = e4m3 ? launch_tiles<T, D, EVO_CACHE_E4M3, 1>(a, grid, st) : launch_tiles<T, D, EVO_CACHE_F32, 1>(a, grid, st);
+  else
+    e = e4m3 ? launch_tiles<T, D, EVO_CACHE_E4M3, 4>(a, grid, st) : launch_tiles<T, D, EVO_CACHE_F32, 4>(a, grid, st);
+  if (e != cudaSuccess || a.splits == 1) return e;
+  const long long threads = (long long)a.rows * a.m.n_head * (D / 4);
+  join_kernel<T, D><<<(unsigned)((threads + THREADS - 1) / THREADS), THREADS, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) {
+  AttendPlan p;
+  const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
+  p.kernel = all <= 16 ? 1 : 4;
+  const int bm = 16 * p.kernel;
+  p.tiles = (int)((all + bm - 1) / bm);
+  const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
+  const long long most = std::max(1, max_len / (4 * BN));
+  p.splits = (int)std::max(1ll, std::min({most, 304 / blocks, 64ll}));
+  p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
+  return p;
+}
+
+cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st) {
+  a.tiles = p.tiles;
+  a.splits = p.splits;
+  a.part = static_cast<float*>(scratch);
+  a.ml = reinterpret_cast<float2*>(a.part + (size_t)p.splits * a.rows * a.m.n_head * a.m.head_dim);
+  if (a.m.dtype == EVO_DTYPE_F32)
+    return a.m.head_dim == 64 ? launch_as<float, 64>(a, p.kernel, st) : launch_as<float, 128>(a, p.kernel, st);
+  return a.m.head_dim == 64 ? launch_as<__nv_bfloat16, 64>(a, p.kernel, st)
+                            : launch_as<__nv_bfloat16, 128>(a, p.kernel, st);
+}
+
+}  // namespace evo
