@@ -32,26 +32,15 @@ struct Smem {
   float p[BM][BN + 4];
 };
 
-template <typename T>
-__device__ __forceinline__ float4 load4f(const T* p);
-template <>
-__device__ __forceinline__ float4 load4f<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <>
-__device__ __forceinline__ float4 load4f<__nv_bfloat16>(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
-}
-
 // 4 values of a key's or value's row in the memory's format
-template <typename T, int FORMAT>
+template <int FORMAT>
 __device__ __forceinline__ float4 memory4(const void* pages, const uint8_t* scales, long long at, int D, int d) {
   if constexpr (FORMAT == EVO_CACHE_E4M3) {
     const float4 c = codes4(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(pages) + at * D + d));
     const float f = scale_value(scales[at]);
     return make_float4(c.x * f, c.y * f, c.z * f, c.w * f);
   } else {
-    return load4f<T>(static_cast<const T*>(pages) + at * D + d);
+    return *reinterpret_cast<const float4*>(static_cast<const float*>(pages) + at * D + d);
   }
 }
 
@@ -62,7 +51,7 @@ __device__ __forceinline__ float dot4(float4 a, float4 b, float c) {
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-template <typename T, int D, int FORMAT, int RM>
+template <int D, int FORMAT, int RM>
 __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(16) uint8_t raw[];
   Smem<D, RM>& sm = *reinterpret_cast<Smem<D, RM>*>(raw);
@@ -78,8 +67,8 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
     const int r = i / (D / 4), d = i % (D / 4) * 4, R = r0 + r;
     float4 x = {};
     if (R < rows)
-      x = load4f<T>(static_cast<const T*>(a.q) + (t.first + R / a.group) * a.ldq +
-                    (long long)(t.kv_head * a.group + R % a.group) * D + d);
+      x = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (t.first + R / a.group) * a.ldq +
+                                           (long long)(t.kv_head * a.group + R % a.group) * D + d);
     *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
   }
   Range seen[RM];
@@ -102,8 +91,8 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
         const int page = seq_page(a.m, t.n, key / a.m.page_tokens);
         const long long at =
             ((long long)page * a.m.n_kv_head + t.kv_head) * a.m.page_tokens + key % a.m.page_tokens;
-        k = memory4<T, FORMAT>(a.m.k_pages, a.m.k_scales, at, D, d);
-        v = memory4<T, FORMAT>(a.m.v_pages, a.m.v_scales, at, D, d);
+        k = memory4<FORMAT>(a.m.k_pages, a.m.k_scales, at, D, d);
+        v = memory4<FORMAT>(a.m.v_pages, a.m.v_scales, at, D, d);
       }
       *reinterpret_cast<float4*>(&sm.k[r][d]) = k;
       *reinterpret_cast<float4*>(&sm.v[r][d]) = v;
@@ -169,9 +158,9 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
     const int row = t.first + R / a.group, head = t.kv_head * a.group + R % a.group;
     if (a.splits == 1) {
       const float f = sum[i] == 0.f ? 0.f : 1.f / sum[i];
-      T* dst = static_cast<T*>(a.out) + row * a.ldo + (long long)head * D;
+      float* dst = static_cast<float*>(a.out) + row * a.ldo + (long long)head * D;
 #pragma unroll
-      for (int c = 0; c < DC; ++c) put(dst + tx + 16 * c, o[i][c] * f);
+      for (int c = 0; c < DC; ++c) dst[tx + 16 * c] = o[i][c] * f;
     } else {
       const long long at = part_index(a, t.split, row, head);
 #pragma unroll
@@ -211,25 +200,25 @@ __global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ A
   put(dst + 3, o.w * f);
 }
 
-template <typename T, int D, int FORMAT, int RM>
+template <int D, int FORMAT, int RM>
 cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
-  const auto k = attend_kernel<T, D, FORMAT, RM>;
+  const auto k = attend_kernel<D, FORMAT, RM>;
   const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D, RM>));
   if (e != cudaSuccess) return e;
   k<<<grid, THREADS, sizeof(Smem<D, RM>), st>>>(a);
   return cudaGetLastError();
 }
 
-template <typename T, int D>
-cudaError_t launch_as(const AttendArgs& a, int kernel, cudaStream_t st) {
+template <int D>
+cudaError_t launch_f32(const AttendArgs& a, bool wide, cudaStream_t st) {
   const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
   const bool e4m3 = a.m.format == EVO_CACHE_E4M3;
-  cudaError_t e;
-  if (kernel == 1)
-    e = e4m3 ? launch_tiles<T, D, EVO_CACHE_E4M3, 1>(a, grid, st) : launch_tiles<T, D, EVO_CACHE_F32, 1>(a, grid, st);
-  else
-    e = e4m3 ? launch_tiles<T, D, EVO_CACHE_E4M3, 4>(a, grid, st) : launch_tiles<T, D, EVO_CACHE_F32, 4>(a, grid, st);
-  if (e != cudaSuccess || a.splits == 1) return e;
+  if (wide) return e4m3 ? launch_tiles<D, EVO_CACHE_E4M3, 4>(a, grid, st) : launch_tiles<D, EVO_CACHE_F32, 4>(a, grid, st);
+  return e4m3 ? launch_tiles<D, EVO_CACHE_E4M3, 1>(a, grid, st) : launch_tiles<D, EVO_CACHE_F32, 1>(a, grid, st);
+}
+
+template <typename T, int D>
+cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   const long long threads = (long long)a.rows * a.m.n_head * (D / 4);
   join_kernel<T, D><<<(unsigned)((threads + THREADS - 1) / THREADS), THREADS, 0, st>>>(a);
   return cudaGetLastError();
@@ -240,12 +229,13 @@ cudaError_t launch_as(const AttendArgs& a, int kernel, cudaStream_t st) {
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) {
   AttendPlan p;
   const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
-  p.kernel = all <= 16 ? 1 : 4;
-  const int bm = 16 * p.kernel;
+  const bool f32 = m.dtype == EVO_DTYPE_F32;
+  p.kernel = f32 ? (all <= 16 ? ATTEND_F32_16 : ATTEND_F32_64) : (all <= 16 ? ATTEND_ROWS_16 : ATTEND_ROWS_32);
+  const int bm = p.kernel == ATTEND_F32_64 ? 64 : p.kernel == ATTEND_ROWS_32 ? 32 : 16;
   p.tiles = (int)((all + bm - 1) / bm);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
-  const long long most = std::max(1, max_len / (4 * BN));
-  p.splits = (int)std::max(1ll, std::min({most, 304 / blocks, 64ll}));
+  const long long most = std::max(1, max_len / 256);
+  p.splits = (int)std::max(1ll, std::min({most, (f32 ? 304 : 1216) / blocks, 64ll}));
   p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
   return p;
 }
@@ -255,10 +245,21 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
   a.splits = p.splits;
   a.part = static_cast<float*>(scratch);
   a.ml = reinterpret_cast<float2*>(a.part + (size_t)p.splits * a.rows * a.m.n_head * a.m.head_dim);
-  if (a.m.dtype == EVO_DTYPE_F32)
-    return a.m.head_dim == 64 ? launch_as<float, 64>(a, p.kernel, st) : launch_as<float, 128>(a, p.kernel, st);
-  return a.m.head_dim == 64 ? launch_as<__nv_bfloat16, 64>(a, p.kernel, st)
-                            : launch_as<__nv_bfloat16, 128>(a, p.kernel, st);
+  const bool d64 = a.m.head_dim == 64;
+  cudaError_t e = cudaSuccess;
+  switch (p.kernel) {
+    case ATTEND_F32_16:
+    case ATTEND_F32_64: {
+      const bool wide = p.kernel == ATTEND_F32_64;
+      e = d64 ? launch_f32<64>(a, wide, st) : launch_f32<128>(a, wide, st);
+      break;
+    }
+    case ATTEND_ROWS_16: e = launch_attend_rows(a, 1, st); break;
+    case ATTEND_ROWS_32: e = launch_attend_rows(a, 2, st); break;
+  }
+  if (e != cudaSuccess || a.splits == 1) return e;
+  if (a.m.dtype == EVO_DTYPE_F32) return d64 ? launch_join<float, 64>(a, st) : launch_join<float, 128>(a, st);
+  return d64 ? launch_join<__nv_bfloat16, 64>(a, st) : launch_join<__nv_bfloat16, 128>(a, st);
 }
 
 }  // namespace evo

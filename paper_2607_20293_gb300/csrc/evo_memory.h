@@ -46,12 +46,15 @@ struct AttendArgs {
   float* part;                    // [splits][rows][n_head][head_dim]: unnormalised sums of a piece
   float2* ml;                     // [splits][rows][n_head]: its maximum (base 2) and sum
 };
-// how a call is cut up: fills tiles and splits, returns the scratch bytes
+// which kernel takes a call, and how it is cut up
+enum AttendKernel { ATTEND_F32_16, ATTEND_F32_64, ATTEND_ROWS_16, ATTEND_ROWS_32 };   // rows of a tile
 struct AttendPlan {
-  int kernel, tiles, splits;
+  AttendKernel kernel;
+  int tiles, splits;
   size_t scratch;
 };
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len);
+cudaError_t launch_attend_rows(const AttendArgs& a, int mt, cudaStream_t st);   // evo_attend_rows.cu: tiles of 16 mt rows
 cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st);
 
 // ---------------------------------------------------------------- device helpers
