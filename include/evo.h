@@ -353,7 +353,7 @@ typedef struct evo_memory {
   int32_t n_seq;
   int32_t pad_;
   void *k_pages, *v_pages;  /* device [n_pages][n_kv_head][page_tokens][head_dim], start on 16 bytes */
-  uint8_t *k_scales, *v_scales;   /* device [n_pages][n_kv_head][page_tokens]; NULL unless E4M3 */
+  uint8_t *k_scales, *v_scales;   /* device [n_pages][n_kv_head][page_tokens], start on 16 bytes; NULL unless E4M3 */
   const int32_t* table;     /* device [n_seq][max_pages] */
   const int32_t* lens;      /* device [n_seq] */
   const int32_t* starts;    /* device [n_seq + 1] or NULL */

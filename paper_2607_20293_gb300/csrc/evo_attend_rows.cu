@@ -1,24 +1,30 @@
 // Attention over a paged memory for few rows a key/value head (single tokens,
 // short action chunks): bf16 rows, bf16 or 8-bit pages.
 //
-// Such a call reads every key and value once for at most 16 MT rows, so DRAM
+// Such a call reads every key and value once for at most 8 NR rows, so DRAM
 // bounds it as long as the tensor cores and the conversion of codes keep up:
 // mma.sync (1,024 multiply-adds a cycle and SM, a quarter of what tcgen05 has)
-// needs 32 of the 174 cycles that 16 bf16 keys and values of 64 take to arrive,
-// without padding 16 rows to tcgen05's 128.
+// takes 16 of the 174 cycles in which 16 bf16 keys and values of 64 arrive for 8
+// rows, without padding them to tcgen05's 128.
+//
+// Both products have the memory as their first operand, so that a tile is 16 keys
+// (or dimensions) by 8 rows, and 8 rows cost half of what 16 do:
+//   S^T = K Q^T  (keys x rows),  O^T = V^T P^T  (dimensions x rows)
+// P^T leaves the first product as keys x rows and enters the second as its
+// transpose's fragment: one movmatrix for 8 keys.
 //
 // A block is 4 warps on one tile of rows and one piece of the memory.  Each warp
-// takes every 4th run of 16 NB keys by itself (no barrier until the end), loads
-// keys and values from global memory straight into the fragments of
-// mma.m16n8k16, and keeps its own running maximum and sums; the warps' results
-// are joined through shared memory.  Neither operand goes through shared memory,
-// because the contraction's index may be permuted at will:
-//   scores: lane (g, c) = (lane / 4, lane % 4) holds key g's values at 16 bytes
-//           contiguous per step; the queries' fragments use the same permutation;
-//   output: the four keys of a lane's fragment are 4c .. 4c+3 and its column g
-//           stands for 8 (or 16) contiguous dimensions, one n-tile each.
-// Loads are issued for the next run as soon as the registers of this one are
-// used: keys after the scores, values after the output.
+// takes every 4th run of RUN keys by itself: it brings the run's keys, values and
+// scale bytes to its own ring in shared memory by tiled bulk copies, STAGES - 1 runs
+// ahead, so that no barrier of the block is met until the end (loads straight to
+// registers, one run ahead, reached 2.8 TB/s on 64 sequences of 4,096-8,192 8-bit
+// keys).  Fragments are read with 16-byte loads, because a contraction's index may
+// be permuted at will: lane (g, c) = (lane / 4, lane % 4) holds 16 contiguous bytes
+// of key g, the queries' fragments use the same permutation, and row g of an output
+// tile stands for one of the 8 or 16 contiguous dimensions that the lane read of
+// values 2c, 2c+1, 2c+8 and 2c+9: with the copies' 128-byte swizzle the 8 lanes of a
+// phase meet 8 different chunks.  Every warp keeps its own running maximum and
+// sums; they are joined through shared memory at the end.
 //
 // The running maximum is lazy: the sums are rescaled only when a score passes
 // the row's reference by 2^8, so the common run has one vote instead of
@@ -26,31 +32,52 @@
 // most 2^8, which the 16-bit operand holds with the same relative rounding.
 //
 // 8-bit pages: codes become fp16 exactly (one conversion for two).  A key's scale
-// multiplies its column of the scores in fp32; queries are brought to fp16 by an
-// exact power of two per row.  A value's scale 2^k is added to the exponent of its
-// weights, 2^(s + k - m'), with a reference m' of its own, so that the fp16
-// operand stays in range for any mixture of scales; the sum of weights uses
-// 2^(s - m).  The weights' rounding is fp16's (2^-12 of each) there, bf16's (2^-9)
-// with bf16 pages.
+// multiplies its row of S^T in fp32; queries are brought to fp16 by an exact power of
+// two per row.  A value's scale 2^k is added to the exponent of its weights,
+// 2^(s + k - m'), with a reference m' of its own, so that the fp16 operand stays in
+// range for any mixture of scales; the sum of weights uses 2^(s - m).  The weights'
+// rounding is fp16's (2^-11 of each) there, bf16's (2^-8) with bf16 pages.
 //
-// Masks are looked at only in runs of 16 keys that some row does not see whole.
-// There, keys outside the piece give zero values, and a value that is not finite
-// is taken out of the product (0 * NaN would reach rows that do not see it) and
-// put back at the end for the rows that see it.
+// Masks are looked at only in runs that some row does not see whole.  There, keys
+// outside the piece give zero values, and a value that is not finite is taken out
+// of the product (0 * NaN would reach rows that do not see it) and put back at the
+// end for the rows that see it.
+#include <algorithm>
 #include <cstdint>
 #include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
 #include "evo_attend.cuh"
 #include "evo_quant.cuh"
+#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
-constexpr float LAZY = 8.f;                       // log2 of how far a weight may pass 1
+constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
+constexpr float NO_NUMBER = __builtin_nanf("");
 
+template <int D, bool E4M3, int NR>
+struct Cfg {
+  static constexpr int ROW = D * (E4M3 ? 1 : 2);   // bytes of a key or value
+  static constexpr int BOX = ROW < 128 ? ROW : 128;   // bytes of a row that one copy brings (the swizzle's width)
+  static constexpr int RUN = ROW == 64 ? 32 : 16;
+  static constexpr int NB = RUN / 16;
+  static constexpr int KP = ROW / 64;              // 16-byte pieces of a key a lane holds (4 lanes a key)
+  static constexpr int VP = ROW < 128 ? 1 : ROW / 128;   // 16-byte (or one 8-byte) pieces of a value (8 lanes a value)
+  static constexpr int TILE = RUN * ROW;           // bytes of a run's keys
+  static constexpr int STAGE = 2 * TILE;
+  static constexpr int STAGES = STAGE > 4096 ? 3 : 4;
+  static constexpr int JOIN = 8 * NR * (D + 4) * 4;
+  static constexpr int RING = (STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN + 1023) / 1024 * 1024;   // a warp's bytes
+  static constexpr bool QS = NR == 4 && D == 128;  // queries stay in shared memory: their fragments take 64 registers
+  static constexpr int QB = QS ? NR * (D / 16) * 256 : 0;
+  static constexpr int SCALES = E4M3 ? WARPS * STAGES * 2 * RUN : 0;
+  static constexpr int SMEM = 1024 + WARPS * RING + QB + SCALES;
+};
+
+// ---------------------------------------------------------------- PTX wrappers
 __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool half) {
   if (half)
     asm volatile(
@@ -65,14 +92,18 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
+// the transpose of an 8 x 8 matrix of 16-bit values, two of a row in a lane
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 // two codes (low 16 bits of c) to two fp16
 __device__ __forceinline__ uint32_t half2_of(uint32_t c) {
   uint32_t h;
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
   return h;
 }
-
 __device__ __forceinline__ uint32_t pack(float a, float b, bool half) {
   uint32_t r;
   if (half)
@@ -80,6 +111,46 @@ __device__ __forceinline__ uint32_t pack(float a, float b, bool half) {
   else
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t p) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t p) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t p) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p));
+  return v;
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
+          "r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+// a bounded wait: false if the copies did not arrive
+__device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
+  for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
+    if (tc::mbar_test(bar, parity)) return true;
+  return false;
+}
+
+// byte offset of 16-byte chunk `chunk` of row r in a tile of ROWS rows (boxes of at most 128 bytes, one behind the other)
+template <int ROW, int ROWS>
+__device__ __forceinline__ int chunk_at(int r, int chunk) {
+  if constexpr (ROW == 64) return r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4);
+  return (chunk >> 3) * (ROWS * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
 }
 
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w, bool* bad) {
@@ -90,389 +161,392 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w, bool* bad) {
   return w & keep;
 }
 
-// how many keys beyond the loads of a run its registers hold, per format
-template <int D, bool E4M3>
-struct Frag {
-  static constexpr int ROW = D * (E4M3 ? 1 : 2);   // bytes of a key or value
-  static constexpr int KP = ROW / 64;              // 16-byte pieces of a key a lane holds (4 lanes a key)
-  static constexpr int VB = ROW / 8;               // bytes of a value a lane holds (8 lanes a value)
-  static constexpr int VP = VB == 8 ? 1 : VB / 16; // 16-byte (or one 8-byte) pieces of them
-};
-
-template <int D, bool E4M3, int MT, int NB>
-__global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ AttendArgs a) {
-  using F = Frag<D, E4M3>;
-  constexpr int RUN = 16 * NB, NT = D / 8, KS = D / 16, LD = D + 4;
-  extern __shared__ __align__(16) float joined[];            // [WARPS][16 MT][LD], then the warps' maxima and sums
-  float2* const stat = reinterpret_cast<float2*>(joined + WARPS * 16 * MT * LD);   // [WARPS][16 MT]
-  float* const vmax = reinterpret_cast<float*>(stat + WARPS * 16 * MT);            // [WARPS][16 MT], 8-bit pages
+template <int D, bool E4M3, int NR>
+__global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ AttendArgs a,
+                                                       const __grid_constant__ CUtensorMap kmap,
+                                                       const __grid_constant__ CUtensorMap vmap) {
+  using C = Cfg<D, E4M3, NR>;
+  constexpr int RUN = C::RUN, NB = C::NB, KS = D / 16, DT = D / 16, LD = D + 4, STAGES = C::STAGES, ROWS = 8 * NR;
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t full[WARPS][STAGES];
+  __shared__ float2 stat[WARPS][ROWS];                       // the warps' maxima and sums
+  __shared__ float vmax[E4M3 ? WARPS : 1][ROWS];
   __shared__ int poison;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
+  uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
+  const uint32_t ring = tc::su32(mem) + warp * C::RING;
+  const uint32_t qsm = tc::su32(mem) + WARPS * C::RING;
+  const uint32_t ssm = qsm + C::QB + warp * (STAGES * 2 * RUN);
   const Tile t = tile_of_block(a);
-  const int rows = t.count * a.group, r0 = t.tile * 16 * MT;
+  const int rows = t.count * a.group, r0 = t.tile * ROWS;
   if (r0 >= rows) return;
-  const int last = min(r0 + 16 * MT, rows) - 1;
+  const int last = min(r0 + ROWS, rows) - 1;
   const Range first_row = seen_by(a, t, r0 / a.group), last_row = seen_by(a, t, last / a.group);
   const Range all = piece_of(a, t, {first_row.lo, last_row.hi}, RUN);
   // keys that every row of the tile sees, of this piece
   const int whole_lo = max(last_row.lo, all.lo), whole_hi = min(first_row.hi, all.hi);
-  if (tid == 0) poison = 0;
+  if (tid == 0) {
+    poison = 0;
+    for (int i = 0; i < WARPS * STAGES; ++i) tc::mbar_init1(&full[0][i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   __syncthreads();
 
-  // queries: fragments in the keys' permutation
-  uint32_t q[MT][KS][4];
-  float rf[MT][2];
+  // copies of a run: box rows each, lane i the i-th; its page is looked up a run ahead
+  const int box = min(a.m.page_tokens, RUN), shift = 31 - __clz(a.m.page_tokens), step = WARPS * RUN;
+  const int page_rows = a.m.n_kv_head * a.m.page_tokens, head_row = t.kv_head * a.m.page_tokens;
+  auto page_at = [&](int k0) {
+    const int kb = k0 + lane * box;
+    return lane * box < RUN && kb + box > all.lo && kb < all.hi ? seq_page(a.m, t.n, kb >> shift) : -1;
+  };
+  auto issue = [&](int k0, int page, int stage) {
+    const uint32_t bar = tc::su32(&full[warp][stage]);
+    const int copies = __popc(__ballot_sync(0xffffffffu, page >= 0));
+    if (lane == 0) tc::mbar_expect_tx(&full[warp][stage], copies * box * (2 * C::ROW + (E4M3 ? 2 : 0)));
+    __syncwarp();
+    if (page >= 0) {
+      const int at = page * page_rows + head_row + ((k0 + lane * box) & (a.m.page_tokens - 1));
+      const uint32_t dst = ring + stage * C::STAGE + lane * box * C::BOX;
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int R = r0 + mt * 16 + hf * 8 + g;
-      const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (long long)(t.first + R / a.group) * a.ldq +
-                                 (long long)(t.kv_head * a.group + R % a.group) * D;
-      rf[mt][hf] = a.scale_log2;
+      for (int x = 0; x < C::ROW / C::BOX; ++x) {
+        tile_load(dst + x * RUN * C::BOX, &kmap, x * 64, at, bar);
+        tile_load(dst + C::TILE + x * RUN * C::BOX, &vmap, x * 64, at, bar);
+      }
       if constexpr (E4M3) {
-        uint4 u[D / 32];                                     // values 64 h + 16 c .. + 15
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          u[i] = R < rows ? *reinterpret_cast<const uint4*>(src + 64 * (i / 2) + 16 * c + 8 * (i % 2)) : make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-        }
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^(14 - e) for a largest magnitude in [2^e, 2^(e+1)), within fp32's exponents
-        const int e = (int)(top >> 7);                       // e + 127
-        const int up = top == 0 || e == 255 ? 0 : min(max(141 - e, -126), 126);
-        const float f = __int_as_float((up + 127) << 23);
-        rf[mt][hf] = a.scale_log2 * __int_as_float((127 - up) << 23);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const uint4 v = u[ks / 2];
-          const uint32_t lo = ks % 2 ? v.z : v.x, hi = ks % 2 ? v.w : v.y;
-          q[mt][ks][hf] = pack(__uint_as_float(lo << 16) * f, __uint_as_float(lo & 0xffff0000u) * f, true);
-          q[mt][ks][2 + hf] = pack(__uint_as_float(hi << 16) * f, __uint_as_float(hi & 0xffff0000u) * f, true);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {                   // values 32 i + 8 c .. + 7: two steps
-          const uint4 u = R < rows ? *reinterpret_cast<const uint4*>(src + 32 * i + 8 * c) : make_uint4(0, 0, 0, 0);
-          q[mt][2 * i][hf] = u.x;
-          q[mt][2 * i][2 + hf] = u.y;
-          q[mt][2 * i + 1][hf] = u.z;
-          q[mt][2 * i + 1][2 + hf] = u.w;
-        }
+        bulk_load(ssm + stage * 2 * RUN + lane * box, a.m.k_scales + at, box, bar);
+        bulk_load(ssm + stage * 2 * RUN + RUN + lane * box, a.m.v_scales + at, box, bar);
       }
     }
+  };
+  int k0 = all.lo / RUN * RUN + warp * RUN;
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (k0 + i * step < all.hi) issue(k0 + i * step, page_at(k0 + i * step), i);
+  int ahead = page_at(k0 + (STAGES - 1) * step);
 
-  float o[MT][NT][4], sum[MT][2], top[MT][2], vtop[MT][2];
+  // queries: fragments in the keys' permutation; row 8 nr + g
+  uint32_t q[C::QS ? 1 : NR][C::QS ? 1 : KS][2];
+  float rf[NR][2];                                           // factor of rows 2 c, 2 c + 1 from a product to base-2 scores
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
+  for (int nr = 0; nr < NR; ++nr) {
+    const int R = r0 + 8 * nr + g;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (long long)(t.first + R / a.group) * a.ldq +
+                               (long long)(t.kv_head * a.group + R % a.group) * D;
+    uint4 u[D / 32];                                         // 8 values each, in the order of the steps
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int i = 0; i < D / 32; ++i)
+      u[i] = R < rows ? *reinterpret_cast<const uint4*>(src + (E4M3 ? 64 * (i / 2) + 16 * c + 8 * (i % 2) : 32 * i + 8 * c))
+                      : make_uint4(0, 0, 0, 0);
+    float f = a.scale_log2;
+    if constexpr (E4M3) {
+      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[mt][j][i] = 0.f;
+      for (int i = 0; i < D / 32; ++i) {
+        const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) sum[mt][hf] = 0.f, top[mt][hf] = vtop[mt][hf] = -INFINITY;
+        for (int j = 0; j < 4; ++j) top = max(top, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // 2^(14 - e) for a largest magnitude in [2^e, 2^(e+1)), within fp32's exponents
+      const int e = (int)(top >> 7);                         // e + 127
+      const int up = top == 0 || e == 255 ? 0 : min(max(141 - e, -126), 126);
+      const float s2 = __int_as_float((up + 127) << 23);
+      f *= __int_as_float((127 - up) << 23);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&u[i]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = pack(__uint_as_float(w[j] << 16) * s2, __uint_as_float(w[j] & 0xffff0000u) * s2, true);
+      }
+    }
+    rf[nr][0] = __shfl_sync(0xffffffffu, f, 8 * c);
+    rf[nr][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const uint32_t b0 = ks % 2 ? u[ks / 2].z : u[ks / 2].x, b1 = ks % 2 ? u[ks / 2].w : u[ks / 2].y;
+      if constexpr (C::QS) {
+        if (warp == 0)
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(qsm + ((nr * KS + ks) * 32 + lane) * 8), "r"(b0), "r"(b1) : "memory");
+      } else {
+        q[nr][ks][0] = b0;
+        q[nr][ks][1] = b1;
+      }
+    }
+  }
+  if constexpr (C::QS) __syncthreads();
+
+  float o[NR][DT][4], sum[NR][2], top[NR][2], vtop[NR][2];   // o: dimensions g, g + 8 x rows 2 c, 2 c + 1 of a tile
+#pragma unroll
+  for (int nr = 0; nr < NR; ++nr) {
+#pragma unroll
+    for (int j = 0; j < DT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[nr][j][i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) sum[nr][e] = 0.f, top[nr][e] = vtop[nr][e] = -INFINITY;
   }
 
-  uint4 kr[NB][2][F::KP];                                    // keys 4 (g / 2) + 2 i + g % 2 of the 16, i = 0, 1
-  uint4 vr[NB][4][F::VP];                                    // values 4 c + i of the 16
-  uint32_t kscale[NB], vscale[NB];                           // scale bytes of keys 4 c .. 4 c + 3
-  const long long head_rows = a.m.page_tokens, page_rows = (long long)a.m.n_kv_head * a.m.page_tokens;
-  const int shift = 31 - __clz(a.m.page_tokens), mask = a.m.page_tokens - 1;
-
-  // row of the pool at which 16 keys from k0 start, or -1 if none of them is in the piece
-  auto locate = [&](int k0) -> long long {
-    if (k0 + 16 <= all.lo || k0 >= all.hi) return -1;
-    return seq_page(a.m, t.n, k0 >> shift) * page_rows + t.kv_head * head_rows + (k0 & mask);
-  };
-  auto load_keys = [&](int b, long long at) {
-    if (at >= 0) {
-      const uint8_t* p = static_cast<const uint8_t*>(a.m.k_pages) + at * F::ROW;
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int h = 0; h < F::KP; ++h)
-          kr[b][i][h] = *reinterpret_cast<const uint4*>(p + (4 * (g / 2) + 2 * i + g % 2) * F::ROW + 64 * h + 16 * c);
-      if constexpr (E4M3) kscale[b] = *reinterpret_cast<const uint32_t*>(a.m.k_scales + at + 4 * c);
-    }
-  };
-  auto load_values = [&](int b, long long at) {
-    if (at >= 0) {
-      const uint8_t* p = static_cast<const uint8_t*>(a.m.v_pages) + at * F::ROW;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < F::VP; ++h) {
-          const uint8_t* s = p + (4 * c + i) * F::ROW + (F::VB == 8 ? 8 * g : 128 * h + 16 * g);
-          if constexpr (F::VB == 8) {
-            const uint2 u = *reinterpret_cast<const uint2*>(s);
-            vr[b][i][h] = make_uint4(u.x, u.y, 0, 0);
-          } else {
-            vr[b][i][h] = *reinterpret_cast<const uint4*>(s);
-          }
-        }
-      if constexpr (E4M3) vscale[b] = *reinterpret_cast<const uint32_t*>(a.m.v_scales + at + 4 * c);
-    }
-  };
-
-  const int step = WARPS * RUN;
-  int k0 = all.lo / RUN * RUN + warp * RUN;
-  long long here[NB], next[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) here[b] = locate(k0 + 16 * b), next[b] = locate(k0 + step + 16 * b);
-#pragma unroll
-  for (int b = 0; b < NB; ++b) load_keys(b, here[b]);
-#pragma unroll
-  for (int b = 0; b < NB; ++b) load_values(b, here[b]);
-
+  int stage = 0;
+  uint32_t phase = 0;
+  bool dead = false;
   for (; k0 < all.hi; k0 += step) {
-    long long after[NB];
+    if (k0 + (STAGES - 1) * step < all.hi) {
+      issue(k0 + (STAGES - 1) * step, ahead, stage == 0 ? STAGES - 1 : stage - 1);
+      ahead = page_at(k0 + STAGES * step);
+    }
+    if (!__all_sync(0xffffffffu, wait_full(tc::su32(&full[warp][stage]), phase))) {
+      dead = true;
+      break;
+    }
+    const uint32_t kt = ring + stage * C::STAGE, vt = kt + C::TILE, sc = ssm + stage * 2 * RUN;
+    // s[nr][b]: keys g, g + 8 of the b-th 16 x rows 2 c, 2 c + 1
+    float s[NR][NB][4];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) after[b] = locate(k0 + 2 * step + 16 * b);
-    float s[MT][NB][2][4];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < 4; ++e) s[nr][b][e] = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[mt][b][i][e] = 0.f;
+    for (int h = 0; h < C::KP; ++h) {
+      uint4 kr[NB][2];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i) kr[b][i] = lds128(kt + chunk_at<C::ROW, RUN>(16 * b + 8 * i + g, 4 * h + c));
 #pragma unroll
-        for (int h = 0; h < F::KP; ++h) {
-          const uint32_t w[4] = {kr[b][i][h].x, kr[b][i][h].y, kr[b][i][h].z, kr[b][i][h].w};
-          if constexpr (E4M3) {                              // 4 codes a step
+      for (int j = 0; j < (E4M3 ? 4 : 2); ++j) {             // steps of 4 values a lane
+        const int ks = (E4M3 ? 4 : 2) * h + j;
+        uint32_t qf[NR][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t b0 = half2_of(w[j]), b1 = half2_of(w[j] >> 16);
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt) mma16(s[mt][b][i], q[mt][4 * h + j], b0, b1, true);
-            }
-          } else {                                           // 4 values in two words a step
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt) mma16(s[mt][b][i], q[mt][2 * h + j], w[2 * j], w[2 * j + 1], false);
+        for (int nr = 0; nr < NR; ++nr) {
+          if constexpr (C::QS) {
+            const uint2 u = lds64(qsm + ((nr * KS + ks) * 32 + lane) * 8);
+            qf[nr][0] = u.x, qf[nr][1] = u.y;
+          } else {
+            qf[nr][0] = q[nr][ks][0], qf[nr][1] = q[nr][ks][1];
           }
         }
-    // scores in base 2; column 2 c + e of n-tile i is key 4 c + 2 i + e
-    float ks[NB][4], vs[NB][4];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (E4M3) {
-          // a value that is no number makes the key's score one: the rows that see it, and no
-          // other, then hold NaN
-          const uint32_t v = (vscale[b] >> (8 * j)) & 255u;
-          ks[b][j] = scale_value(v == SCALE_NAN ? SCALE_NAN : (kscale[b] >> (8 * j)) & 255u);
-          vs[b][j] = v == SCALE_NAN ? 0.f : (float)((int)v - 127);
-        }
-      }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) load_keys(b, next[b]);
-
-    bool raise = false;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int kb = k0 + 16 * b;
-      const bool whole = kb >= whole_lo && kb + 16 <= whole_hi;
-      bool drop[4] = {};                                     // values of this lane's keys that must not be multiplied
-      if (!whole) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) drop[j] = kb + 4 * c + j < all.lo || kb + 4 * c + j >= all.hi;
-      }
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          Range see = {0, 0};
-          if (!whole) {
-            const int R = r0 + mt * 16 + hf * 8 + g;
-            if (R < rows) see = seen_by(a, t, R / a.group);
-            see = {max(see.lo, all.lo), min(see.hi, all.hi)};
+        for (int b = 0; b < NB; ++b) {
+          const uint32_t w0[4] = {kr[b][0].x, kr[b][0].y, kr[b][0].z, kr[b][0].w};
+          const uint32_t w1[4] = {kr[b][1].x, kr[b][1].y, kr[b][1].z, kr[b][1].w};
+          uint32_t f[4];
+          if constexpr (E4M3) {
+            f[0] = half2_of(w0[j]), f[1] = half2_of(w1[j]), f[2] = half2_of(w0[j] >> 16), f[3] = half2_of(w1[j] >> 16);
+          } else {
+            f[0] = w0[2 * j % 4], f[1] = w1[2 * j % 4], f[2] = w0[(2 * j + 1) % 4], f[3] = w1[(2 * j + 1) % 4];
           }
-          float m = -INFINITY, mv = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float& x = s[mt][b][j / 2][2 * hf + j % 2];
-            if constexpr (E4M3) x *= ks[b][j];
-            x *= rf[mt][hf];
-            if (!whole) {
-              const int key = kb + 4 * c + j;
-              if (key < see.lo || key >= see.hi) x = -INFINITY;
-            }
-            m = fmaxf(m, x);
-            if constexpr (E4M3) mv = fmaxf(mv, x + vs[b][j]);
-          }
-          raise |= m > top[mt][hf] + LAZY;
-          if constexpr (E4M3) raise |= mv > vtop[mt][hf] + LAZY;
+          for (int nr = 0; nr < NR; ++nr) mma16(s[nr][b], f, qf[nr][0], qf[nr][1], E4M3);
         }
-      if constexpr (E4M3) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) drop[j] |= ks[b][j] != ks[b][j];
-        if (__any_sync(0xffffffffu, drop[0] | drop[1] | drop[2] | drop[3])) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int h = 0; h < F::VP; ++h)
-              if (drop[j]) vr[b][j][h] = make_uint4(0, 0, 0, 0);
-        }
-      } else if (!whole) {
-        bool bad = false;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int h = 0; h < F::VP; ++h) {
-            uint4& u = vr[b][j][h];
-            if (drop[j]) u = make_uint4(0, 0, 0, 0);
-            u = make_uint4(finite_halves(u.x, &bad), finite_halves(u.y, &bad), finite_halves(u.z, &bad),
-                           finite_halves(u.w, &bad));
-          }
-        if (bad) poison = 1;
       }
     }
-    if (__any_sync(0xffffffffu, raise)) {
+    // base-2 scores; a value's scale as an exponent
+    float vs[NB][2];
+    bool odd = k0 < whole_lo || k0 + RUN > whole_hi;         // some row does not see the whole run
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          float m = top[mt][hf], mv = vtop[mt][hf];
+      for (int i = 0; i < 2; ++i) {
+        float ks = 1.f;
+        if constexpr (E4M3) {
+          const uint32_t kb = lds8(sc + 16 * b + 8 * i + g), vb = lds8(sc + RUN + 16 * b + 8 * i + g);
+          ks = __uint_as_float(kb << 23);
+          vs[b][i] = __uint_as_float(0x4b000000u | vb) - 8388735.f;   // vb - 127
+          // a key or value that is no number makes the key's scores none: the rows that see it,
+          // and no other, then hold NaN
+          if (kb == SCALE_NAN || vb == SCALE_NAN) odd = true, ks = NO_NUMBER, vs[b][i] = 0.f;
+        }
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr) {
+          float2 x = make_float2(s[nr][b][2 * i], s[nr][b][2 * i + 1]);
+          if constexpr (E4M3) x = mul2(x, make_float2(ks, ks));
+          x = mul2(x, make_float2(rf[nr][0], rf[nr][1]));
+          s[nr][b][2 * i] = x.x, s[nr][b][2 * i + 1] = x.y;
+        }
+      }
+    odd = __any_sync(0xffffffffu, odd);
+    if (odd) {
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int R = r0 + 8 * nr + 2 * c + e;
+          const Range see = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
+          const int lo = max(see.lo, all.lo), hi = min(see.hi, all.hi);
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float x = s[mt][b][j / 2][2 * hf + j % 2];
-              m = fmaxf(m, x);
-              if constexpr (E4M3) mv = fmaxf(mv, x + vs[b][j]);
+            for (int i = 0; i < 2; ++i) {
+              const int key = k0 + 16 * b + 8 * i + g;
+              if (key < lo || key >= hi) s[nr][b][2 * i + e] = -INFINITY;
             }
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-          m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-          if constexpr (E4M3) {
-            mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, 1));
-            mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, 2));
-          } else {
-            mv = m;
-          }
-          const float f = ex2_approx(top[mt][hf] - (m == -INFINITY ? 0.f : m));
-          const float fv = E4M3 ? ex2_approx(vtop[mt][hf] - (mv == -INFINITY ? 0.f : mv)) : f;
-          top[mt][hf] = m;
-          vtop[mt][hf] = mv;
-          sum[mt][hf] *= f;
-#pragma unroll
-          for (int j = 0; j < NT; ++j) o[mt][j][2 * hf] *= fv, o[mt][j][2 * hf + 1] *= fv;
         }
     }
-    uint32_t p[MT][NB][4];
+    bool raise = false;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const float m = top[mt][hf] == -INFINITY ? 0.f : top[mt][hf];
-        const float mv = vtop[mt][hf] == -INFINITY ? 0.f : vtop[mt][hf];
+      for (int e = 0; e < 2; ++e) {
+        float m = -INFINITY, mv = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float w[4];
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float x = s[mt][b][j / 2][2 * hf + j % 2];
-            w[j] = ex2_approx(x - m);
-            sum[mt][hf] += w[j];
-            if constexpr (E4M3) w[j] = ex2_approx(x + (vs[b][j] - mv));
+          for (int i = 0; i < 2; ++i) {
+            m = fmaxf(m, s[nr][b][2 * i + e]);
+            if constexpr (E4M3) mv = fmaxf(mv, s[nr][b][2 * i + e] + vs[b][i]);
           }
-          p[mt][b][hf] = pack(w[0], w[1], E4M3);
-          p[mt][b][2 + hf] = pack(w[2], w[3], E4M3);
-        }
+        raise |= m > top[nr][e] + LAZY;
+        if constexpr (E4M3) raise |= mv > vtop[nr][e] + LAZY;
       }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float m = top[nr][e], mv = vtop[nr][e];
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              m = fmaxf(m, s[nr][b][2 * i + e]);
+              if constexpr (E4M3) mv = fmaxf(mv, s[nr][b][2 * i + e] + vs[b][i]);
+            }
+#pragma unroll
+          for (int x = 4; x < 32; x *= 2) {
+            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+            if constexpr (E4M3) mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+          }
+          if constexpr (!E4M3) mv = m;
+          const float f = ex2_approx(top[nr][e] - (m == -INFINITY ? 0.f : m));
+          const float fv = E4M3 ? ex2_approx(vtop[nr][e] - (mv == -INFINITY ? 0.f : mv)) : f;
+          top[nr][e] = m;
+          vtop[nr][e] = mv;
+          sum[nr][e] *= f;
+#pragma unroll
+          for (int j = 0; j < DT; ++j) o[nr][j][e] *= fv, o[nr][j][2 + e] *= fv;
+        }
+    }
+    // weights, and their transposes as the second product's fragments
+    uint32_t p[NR][NB][2];
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr) {
+      const float m0 = top[nr][0] == -INFINITY ? 0.f : top[nr][0], m1 = top[nr][1] == -INFINITY ? 0.f : top[nr][1];
+      const float v0 = vtop[nr][0] == -INFINITY ? 0.f : vtop[nr][0], v1 = vtop[nr][1] == -INFINITY ? 0.f : vtop[nr][1];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float x0 = s[nr][b][2 * i], x1 = s[nr][b][2 * i + 1];
+          float w0 = ex2_approx(x0 - m0), w1 = ex2_approx(x1 - m1);
+          sum[nr][0] += w0, sum[nr][1] += w1;
+          if constexpr (E4M3) w0 = ex2_approx(x0 + (vs[b][i] - v0)), w1 = ex2_approx(x1 + (vs[b][i] - v1));
+          p[nr][b][i] = transposed(pack(w0, w1, E4M3));
+        }
+    }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int h = 0; h < F::VP; ++h) {
-        const uint32_t w[4][4] = {{vr[b][0][h].x, vr[b][0][h].y, vr[b][0][h].z, vr[b][0][h].w},
-                                  {vr[b][1][h].x, vr[b][1][h].y, vr[b][1][h].z, vr[b][1][h].w},
-                                  {vr[b][2][h].x, vr[b][2][h].y, vr[b][2][h].z, vr[b][2][h].w},
-                                  {vr[b][3][h].x, vr[b][3][h].y, vr[b][3][h].z, vr[b][3][h].w}};
+      for (int h = 0; h < C::VP; ++h) {
+        uint32_t w[4][4];                                    // values 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 16 * b + 8 * (i / 2) + 2 * c + i % 2;
+          if constexpr (C::ROW == 64) {
+            const uint2 u = lds64(vt + chunk_at<64, RUN>(r, g / 2) + 8 * (g % 2));
+            w[i][0] = u.x, w[i][1] = u.y, w[i][2] = w[i][3] = 0;
+          } else {
+            const uint4 u = lds128(vt + chunk_at<C::ROW, RUN>(r, 8 * h + g));
+            w[i][0] = u.x, w[i][1] = u.y, w[i][2] = u.z, w[i][3] = u.w;
+          }
+        }
+        if (odd) {
+          bool bad = false;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = 16 * b + 8 * (i / 2) + 2 * c + i % 2, key = k0 + r;
+            bool drop = key < all.lo || key >= all.hi;
+            if constexpr (E4M3) drop |= lds8(sc + RUN + r) == SCALE_NAN || lds8(sc + r) == SCALE_NAN;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              if (drop) w[i][x] = 0;
+              if constexpr (!E4M3) w[i][x] = finite_halves(w[i][x], &bad);
+            }
+          }
+          if (!E4M3 && bad) poison = 1;
+        }
         if constexpr (E4M3) {
 #pragma unroll
-          for (int x = 0; x < (F::VB == 8 ? 2 : 4); ++x)     // 4 dimensions of each word
+          for (int x = 0; x < (C::ROW == 64 ? 2 : 4); ++x)   // 4 dimensions a word: two tiles
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               const uint32_t a01 = __byte_perm(w[0][x], w[1][x], y ? 0x7362 : 0x5140);
               const uint32_t a23 = __byte_perm(w[2][x], w[3][x], y ? 0x7362 : 0x5140);
+              const uint32_t f[4] = {half2_of(a01), half2_of(a01 >> 16), half2_of(a23), half2_of(a23 >> 16)};
 #pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                const uint32_t b0 = half2_of(a01 >> (16 * z)), b1 = half2_of(a23 >> (16 * z));
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) mma16(o[mt][4 * x + 2 * y + z], p[mt][b], b0, b1, true);
-              }
+              for (int nr = 0; nr < NR; ++nr) mma16(o[nr][2 * x + y], f, p[nr][b][0], p[nr][b][1], true);
             }
         } else {
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
+          for (int x = 0; x < 4; ++x) {                      // 2 dimensions a word: a tile
+            const uint32_t f[4] = {__byte_perm(w[0][x], w[1][x], 0x5410), __byte_perm(w[0][x], w[1][x], 0x7632),
+                                   __byte_perm(w[2][x], w[3][x], 0x5410), __byte_perm(w[2][x], w[3][x], 0x7632)};
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const uint32_t b0 = __byte_perm(w[0][x], w[1][x], y ? 0x7632 : 0x5410);
-              const uint32_t b1 = __byte_perm(w[2][x], w[3][x], y ? 0x7632 : 0x5410);
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt) mma16(o[mt][8 * h + 2 * x + y], p[mt][b], b0, b1, false);
-            }
+            for (int nr = 0; nr < NR; ++nr) mma16(o[nr][4 * h + x], f, p[nr][b][0], p[nr][b][1], false);
+          }
         }
       }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      load_values(b, next[b]);
-      next[b] = after[b];
-    }
+    __syncwarp();                                            // every lane has read the stage
+    if (++stage == STAGES) stage = 0, phase ^= 1;
+  }
+  if (__syncthreads_or(dead)) {                              // a copy did not arrive: nothing more is asked for
+    if (tid == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
+    const long long t0 = clock64();
+    while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);   // those in flight land before the block ends
+    return;
   }
 
-  // this warp's sums to shared memory: n-tile j, column n is dimension
-  // 8-bit: D/8 n + j; bf16: 64 (j / 8) + 8 n + j % 8
+  // this warp's sums to its part of the ring: [row][dimension]; tile j holds, in its rows g and
+  // g + 8, dimensions D/8 g + 2 j and the next (8-bit), 64 (j / 4) + 8 g + 2 (j % 4) and the next (bf16)
+  float* const mine = reinterpret_cast<float*>(mem + warp * C::RING);
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+  for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      float l = sum[mt][hf];
-      l += __shfl_xor_sync(0xffffffffu, l, 1);
-      l += __shfl_xor_sync(0xffffffffu, l, 2);
-      const int r = mt * 16 + hf * 8 + g;
-      float* dst = joined + (warp * 16 * MT + r) * LD;
+    for (int e = 0; e < 2; ++e) {
+      float l = sum[nr][e];
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int x = 4; x < 32; x *= 2) l += __shfl_xor_sync(0xffffffffu, l, x);
+      const int r = 8 * nr + 2 * c + e;
 #pragma unroll
-        for (int j = 0; j < NT; j += 4) {
-          const int d = E4M3 ? D / 8 * (2 * c + e) + j : 64 * (j / 8) + 8 * (2 * c + e) + j % 8;
-          *reinterpret_cast<float4*>(dst + d) = make_float4(o[mt][j][2 * hf + e], o[mt][j + 1][2 * hf + e],
-                                                            o[mt][j + 2][2 * hf + e], o[mt][j + 3][2 * hf + e]);
-        }
-      if (c == 0) {
-        stat[warp * 16 * MT + r] = make_float2(top[mt][hf], l);
-        if constexpr (E4M3) vmax[warp * 16 * MT + r] = vtop[mt][hf];
+      for (int j = 0; j < DT; ++j) {
+        const int d = E4M3 ? D / 8 * g + 2 * j : 64 * (j / 4) + 8 * g + 2 * (j % 4);
+        *reinterpret_cast<float2*>(mine + r * LD + d) = make_float2(o[nr][j][e], o[nr][j][2 + e]);
+      }
+      if (g == 0) {
+        stat[warp][r] = make_float2(top[nr][e], l);
+        if constexpr (E4M3) vmax[warp][r] = vtop[nr][e];
       }
     }
   __syncthreads();
-  for (int i = tid; i < 16 * MT * D / 4; i += THREADS) {
+  for (int i = tid; i < ROWS * D / 4; i += THREADS) {
     const int r = i / (D / 4), d = i % (D / 4) * 4, R = r0 + r;
-    if (R >= rows) continue;
+    if (R >= rows) break;
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w) m = fmaxf(m, stat[w * 16 * MT + r].x);
-    const float base = m == -INFINITY ? 0.f : m;
+    for (int w = 0; w < WARPS; ++w) m = fmaxf(m, stat[w][r].x);
+    const float ref = m == -INFINITY ? 0.f : m;
     float l = 0.f;
     float4 x = {};
 #pragma unroll
     for (int w = 0; w < WARPS; ++w) {
-      const float2 ml = stat[w * 16 * MT + r];
-      const float4 y = *reinterpret_cast<const float4*>(joined + (w * 16 * MT + r) * LD + d);
-      const float f = ex2_approx(ml.x - base);
+      const float2 ml = stat[w][r];
+      const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(mem + w * C::RING) + r * LD + d);
+      const float f = ex2_approx(ml.x - ref);
       // 8-bit pages: the sums stand in units of 2^m'
-      const float fv = E4M3 ? (ml.x == -INFINITY ? 0.f : ex2_approx(vmax[w * 16 * MT + r] - base)) : f;
+      const float fv = E4M3 ? (ml.x == -INFINITY ? 0.f : ex2_approx(vmax[E4M3 ? w : 0][r] - ref)) : f;
       l = fmaf(ml.y, f, l);
       x = make_float4(fmaf(y.x, fv, x.x), fmaf(y.y, fv, x.y), fmaf(y.z, fv, x.z), fmaf(y.w, fv, x.w));
     }
@@ -480,12 +554,13 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
       // values that are not finite, of the runs where they were taken out, for the rows that see them
       const Range see = seen_by(a, t, R / a.group);
       for (int k = max(see.lo, all.lo); k < min(see.hi, all.hi); ++k) {
-        const int kb = k & ~15;
-        if (kb >= whole_lo && kb + 16 <= whole_hi) {
-          k = kb + 15;
+        const int run = k / RUN * RUN;
+        if (run >= whole_lo && run + RUN <= whole_hi) {
+          k = run + RUN - 1;
           continue;
         }
-        const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.m.v_pages) + (locate(kb) + (k - kb)) * D + d;
+        const long long at = (long long)seq_page(a.m, t.n, k >> shift) * page_rows + head_row + (k & (a.m.page_tokens - 1));
+        const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.m.v_pages) + at * D + d;
         const float y[4] = {__bfloat162float(v[0]), __bfloat162float(v[1]), __bfloat162float(v[2]), __bfloat162float(v[3])};
         if (!isfinite(y[0])) x.x += y[0];
         if (!isfinite(y[1])) x.y += y[1];
@@ -506,27 +581,31 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
   }
 }
 
-template <int D, bool E4M3, int MT, int NB>
-cudaError_t launch_as(const AttendArgs& a, unsigned grid, cudaStream_t st) {
-  const auto k = rows_kernel<D, E4M3, MT, NB>;
-  constexpr int smem = WARPS * 16 * MT * (D + 4) * 4 + WARPS * 16 * MT * 12;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+template <int D, bool E4M3, int NR>
+cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
+  using C = Cfg<D, E4M3, NR>;
+  const auto k = rows_kernel<D, E4M3, NR>;
+  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
-  k<<<grid, THREADS, smem, st>>>(a);
+  CUtensorMap km, vm;
+  const int box = std::min(a.m.page_tokens, C::RUN);
+  if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
+  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
+  k<<<grid, THREADS, C::SMEM, st>>>(a, km, vm);
   return cudaGetLastError();
+}
+
+template <int NR>
+cudaError_t launch_rows(const AttendArgs& a, cudaStream_t st) {
+  const bool e = a.m.format == EVO_CACHE_E4M3;
+  if (a.m.head_dim == 64) return e ? launch_as<64, true, NR>(a, st) : launch_as<64, false, NR>(a, st);
+  return e ? launch_as<128, true, NR>(a, st) : launch_as<128, false, NR>(a, st);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_rows(const AttendArgs& a, int mt, cudaStream_t st) {
-  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
-  const bool e = a.m.format == EVO_CACHE_E4M3;
-  if (a.m.head_dim == 64) {
-    if (mt == 1) return e ? launch_as<64, true, 1, 2>(a, grid, st) : launch_as<64, false, 1, 1>(a, grid, st);
-    return e ? launch_as<64, true, 2, 2>(a, grid, st) : launch_as<64, false, 2, 1>(a, grid, st);
-  }
-  if (mt == 1) return e ? launch_as<128, true, 1, 1>(a, grid, st) : launch_as<128, false, 1, 1>(a, grid, st);
-  return e ? launch_as<128, true, 2, 1>(a, grid, st) : launch_as<128, false, 2, 1>(a, grid, st);
+cudaError_t launch_attend_rows(const AttendArgs& a, int tile_rows, cudaStream_t st) {
+  return tile_rows == 8 ? launch_rows<1>(a, st) : tile_rows == 16 ? launch_rows<2>(a, st) : launch_rows<4>(a, st);
 }
 
 }  // namespace evo

@@ -9,6 +9,35 @@
 
 using namespace evo;
 
+namespace evo {
+
+bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    cudaDriverEntryPointQueryResult q;
+    void* p = nullptr;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return (Encode) nullptr;
+    return reinterpret_cast<Encode>(p);
+  }();
+  if (!encode) return false;
+  const bool codes = m.format == EVO_CACHE_E4M3;
+  const cuuint64_t row = (cuuint64_t)m.head_dim * (codes ? 1 : 2);
+  const cuuint64_t dims[2] = {(cuuint64_t)m.head_dim, (cuuint64_t)m.n_pages * m.n_kv_head * m.page_tokens};
+  const cuuint64_t strides[1] = {row};
+  const cuuint32_t width = (cuuint32_t)(row < 128 ? row : 128);
+  const cuuint32_t box[2] = {codes ? width : width / 2, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return encode(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pages),
+                dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace evo
+
 namespace {
 
 #define EVO_CUDA(x)                       \
@@ -57,6 +86,7 @@ evo_status memory_ok(const evo_memory* m) {
   if (!aligned(m->k_pages, 16) || !aligned(m->v_pages, 16)) return EVO_ERR_ARG;
   const bool scales = m->format == EVO_CACHE_E4M3;
   if ((m->k_scales != nullptr) != scales || (m->v_scales != nullptr) != scales) return EVO_ERR_ARG;
+  if (!aligned(m->k_scales, 16) || !aligned(m->v_scales, 16)) return EVO_ERR_ARG;
   return EVO_OK;
 }
 

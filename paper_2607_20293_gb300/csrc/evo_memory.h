@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "evo.h"
@@ -47,15 +48,19 @@ struct AttendArgs {
   float2* ml;                     // [splits][rows][n_head]: its maximum (base 2) and sum
 };
 // which kernel takes a call, and how it is cut up
-enum AttendKernel { ATTEND_F32_16, ATTEND_F32_64, ATTEND_ROWS_16, ATTEND_ROWS_32 };   // rows of a tile
+enum AttendKernel { ATTEND_F32, ATTEND_ROWS };
 struct AttendPlan {
   AttendKernel kernel;
-  int tiles, splits;
+  int tile_rows, tiles, splits;
   size_t scratch;
 };
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len);
-cudaError_t launch_attend_rows(const AttendArgs& a, int mt, cudaStream_t st);   // evo_attend_rows.cu: tiles of 16 mt rows
+cudaError_t launch_attend_rows(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_attend_rows.cu
 cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st);
+
+// tensor map of a pool of pages: its rows (a token of a head each) in boxes of
+// box_rows rows x 128 bytes (64 where a row has no more), swizzled by the box's width
+bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows);
 
 // ---------------------------------------------------------------- device helpers
 
