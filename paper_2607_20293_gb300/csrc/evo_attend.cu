@@ -230,13 +230,14 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   AttendPlan p;
   const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
   const bool f32 = m.dtype == EVO_DTYPE_F32;
-  p.kernel = f32 ? ATTEND_F32 : ATTEND_ROWS;
-  p.tile_rows = f32 ? (all <= 16 ? 16 : 64) : (all <= 8 ? 8 : all <= 16 ? 16 : 32);
+  const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && all > 32;
+  p.kernel = f32 ? ATTEND_F32 : tiles ? ATTEND_TILES : ATTEND_ROWS;
+  p.tile_rows = f32 ? (all <= 16 ? 16 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
-  const long long most = std::max(1, max_len / 256);
-  const long long target = f32 ? 304 : blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
-  p.splits = (int)std::max(1ll, std::min({most, (target + blocks / 2) / blocks, 64ll}));
+  const long long most = std::max(1, max_len / (tiles ? 512 : 256));
+  const long long target = f32 ? 304 : tiles ? 152 : blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
+  p.splits = (int)std::max(1ll, std::min({most, tiles ? target / blocks : (target + blocks / 2) / blocks, 64ll}));
   p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
   return p;
 }
@@ -250,8 +251,10 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
   cudaError_t e = cudaSuccess;
   if (p.kernel == ATTEND_F32)
     e = d64 ? launch_f32<64>(a, p.tile_rows == 64, st) : launch_f32<128>(a, p.tile_rows == 64, st);
-  else
+  else if (p.kernel == ATTEND_ROWS)
     e = launch_attend_rows(a, p.tile_rows, st);
+  else
+    e = launch_attend_tiles(a, st);
   if (e != cudaSuccess || a.splits == 1) return e;
   if (a.m.dtype == EVO_DTYPE_F32) return d64 ? launch_join<float, 64>(a, st) : launch_join<float, 128>(a, st);
   return d64 ? launch_join<__nv_bfloat16, 64>(a, st) : launch_join<__nv_bfloat16, 128>(a, st);
