@@ -43,7 +43,7 @@ namespace evo {
 namespace {
 
 constexpr int BM = 128, BN = 128;
-constexpr int THREADS = 320;
+constexpr int THREADS = 384;                       // warps 10 and 11 only complete the third warpgroup
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
 constexpr int BLOCK64 = BN * 128;                  // bytes of 128 rows of 64 bf16
 
@@ -103,6 +103,11 @@ __device__ __forceinline__ void tmem_wait_ld(float (&v)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// registers of a warpgroup: 8 softmax warps of 232 and 4 of 40 are the 12 warps of 168 of the launch
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 __device__ __forceinline__ void bar_softmax() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // descriptor of V as the operand whose contiguous index is N: 64 dimensions by 8 keys
@@ -186,6 +191,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
 
+  if (warp >= 8) {
+  fewer_registers<40>();
   if (warp == 9) {
     // ------------------------------------------------------------ copies
     const int box = a.m.page_tokens, shift = 31 - __clz(box);
@@ -268,7 +275,9 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         if (i + 2 < n) scores(i & 1, i + 2, true);
       }
     }
+  }
   } else {
+    more_registers<232>();
     // ------------------------------------------------------------ softmax: stream x, a row a thread
     const int x = warp / 4, r = tid % BM, R = r0 + (pair ? tid : r);
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
@@ -277,7 +286,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     see = {max(see.lo, all.lo), min(see.hi, all.hi)};
     const int from = pair ? 0 : x, by = pair ? 1 : 2;
     float top = -INFINITY;
-    float2 sum2 = make_float2(0.f, 0.f);
+    float2 sums[4] = {};
     bool ok = true;
     int it = 0;
     for (int i = from; i < n; i += by, ++it) {
@@ -321,16 +330,21 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
           tc::fence_async_smem();
         }
       }
-      float m = v[0];
+      float mx[8];                                 // chains of their own: the latency of one is 128 steps
 #pragma unroll
-      for (int j = 1; j < BN; ++j) m = fmaxf(m, v[j]);
-      m *= sc;
+      for (int j = 0; j < 8; ++j) mx[j] = fmaxf(v[j], v[8 + j]);
+#pragma unroll
+      for (int j = 16; j < BN; j += 16)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], fmaxf(v[j + e], v[j + 8 + e]));
+      const float m = sc * fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
       const bool raise = m > top + LAZY;
       if (__any_sync(0xffffffffu, raise)) {
         const float now = raise ? m : top;
         const float f = ex2_approx(top - (now == -INFINITY ? 0.f : now));
         top = now;
-        sum2 = make_float2(sum2.x * f, sum2.y * f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sums[j] = make_float2(sums[j].x * f, sums[j].y * f);
         if (it > 0) {                              // the products before this block are done: s_full came behind them
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
@@ -351,7 +365,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           const float2 w = exp2_of(fma2(make_float2(v[64 * h + 2 * j], v[64 * h + 2 * j + 1]), sc2, ref2));
-          sum2 = add2(sum2, w);
+          sums[j % 4] = add2(sums[j % 4], w);
           p[j] = pack(w);
         }
         tmem_st32(s_at + 32 * h, p);
@@ -360,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       tc::tc_fence_before();
       tc::mbar_arrive1(&sh.p_full[x]);
     }
-    float l = sum2.x + sum2.y;
+    float l = ((sums[0].x + sums[0].y) + (sums[1].x + sums[1].y)) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
     if (ok && it > 0) ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], 0));
     tc::tc_fence_after();
     bool mine = R < rows, scaled = false;
