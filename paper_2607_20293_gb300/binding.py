@@ -372,28 +372,37 @@ CACHE_FORMATS = {"fp32": 0, "bf16": 1, "e4m3": 2}
 UNIT_GROUP = 32          # values of a unit's cache that share a scale
 
 
-def _need(t, what: str, dtype, shape=None, device=None):
-    """A contiguous tensor of this type (and shape, and device), or ValueError."""
-    if str(t.dtype) != dtype and str(t.dtype) not in dtype:
-        raise ValueError(f"{what}: type {t.dtype}, expected {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{what}: must be contiguous")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what}: on {t.device}, expected {device}")
+_torch = None
+
+
+def _load_torch():
+    global _torch
+    import torch
+    _torch = torch
+    return torch
+
+
+def _misfit(t, what: str, dtype, shape, device) -> ValueError:
+    return ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, contiguous: {t.is_contiguous()}; expected a "
+                      f"contiguous {dtype} {tuple(shape)} on {device}")
+
+
+def _need(t, what: str, dtype, shape, device):
+    """Address of a contiguous tensor of this type and shape on this device, or ValueError."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise _misfit(t, what, dtype, shape, device)
     return t.data_ptr()
 
 
-def _current(device):
-    """Check that `device` is the current CUDA device: the library launches there."""
-    import torch
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
+def _launch_stream(device, stream):
+    """The stream's handle (None: the current one); the tensors' device has to be the current one,
+    because the library launches there."""
+    index = device.index
+    if device.type != "cuda" or index != _torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the call runs on the current CUDA device")
-
-
-_F32, _U8, _I32 = "torch.float32", "torch.uint8", "torch.int32"
-_DTYPE_OF = {"torch.float32": 0, "torch.bfloat16": 1}
+    if stream is None:
+        return _torch._C._cuda_getCurrentRawStream(index)
+    return stream if isinstance(stream, int) else stream.cuda_stream
 
 
 def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
@@ -401,24 +410,26 @@ def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
     cache (codes [N][H][E], scales [N][H][E/32], uint8) for the samples whose
     refresh [N] (uint8) is not zero, or all.  Returns y = x + r for those samples
     and x for the others (in `out`, which may be x), or None without x."""
-    N, H, E = r.shape
-    dev = r.device
-    _current(dev)
-    rp = _need(r, "r", tuple(_DTYPE_OF))
-    cp = _need(codes, "codes", _U8, (N, H, E), dev)
-    sp = _need(scales, "scales", _U8, (N, H, E // UNIT_GROUP), dev)
-    gp = None if refresh is None else _need(refresh, "refresh", _U8, (N,), dev)
+    torch = _torch or _load_torch()
+    dev, dtype, u8, shape = r.device, r.dtype, torch.uint8, r.shape
+    st = _launch_stream(dev, stream)
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise _misfit(r, "r", "float32 or bfloat16", shape, dev)
+    N, H, E = shape
     xp = yp = None
     if x is not None:
-        xp = _need(x, "x", _F32, r.shape, dev)
+        xp = _need(x, "x", torch.float32, shape, dev)
         if out is None:
-            import torch
             out = torch.empty_like(x)
-        yp = _need(out, "out", _F32, r.shape, dev)
+        yp = _need(out, "out", torch.float32, shape, dev)
     elif out is not None:
         raise ValueError("out without x")
-    _check(load().evo_cache_write(rp, _DTYPE_OF[str(r.dtype)], gp, N, H, E, xp, yp, cp, sp, _stream(stream)),
-           "evo_cache_write")
+    rc = load().evo_cache_write(_need(r, "r", dtype, shape, dev), 0 if dtype is torch.float32 else 1,
+                                None if refresh is None else _need(refresh, "refresh", u8, (N,), dev), N, H, E, xp, yp,
+                                _need(codes, "codes", u8, shape, dev),
+                                _need(scales, "scales", u8, (N, H, E // UNIT_GROUP), dev), st)
+    if rc:
+        _check(rc, "evo_cache_write")
     return out
 
 
@@ -426,18 +437,19 @@ def cache_add(codes, scales, x, reuse=None, out=None, stream=None):
     """evo_cache_add: x [N][H][E] (fp32) plus the cached values of a run of units
     (codes [U][N][H][E], scales [U][N][H][E/32]) where reuse [U][N] is not zero, or
     of all; in `out` (which may be x) or a new tensor."""
-    import torch
-    U, N, H, E = codes.shape
-    dev = x.device
-    _current(dev)
-    cp = _need(codes, "codes", _U8, None, dev)
-    sp = _need(scales, "scales", _U8, (U, N, H, E // UNIT_GROUP), dev)
-    gp = None if reuse is None else _need(reuse, "reuse", _U8, (U, N), dev)
-    xp = _need(x, "x", _F32, (N, H, E), dev)
+    torch = _torch or _load_torch()
+    dev, u8, shape = x.device, torch.uint8, x.shape
+    st = _launch_stream(dev, stream)
+    N, H, E = shape
+    U = codes.shape[0]
     if out is None:
         out = torch.empty_like(x)
-    yp = _need(out, "out", _F32, (N, H, E), dev)
-    _check(load().evo_cache_add(cp, sp, gp, U, N, H, E, xp, yp, _stream(stream)), "evo_cache_add")
+    rc = load().evo_cache_add(_need(codes, "codes", u8, (U, N, H, E), dev),
+                              _need(scales, "scales", u8, (U, N, H, E // UNIT_GROUP), dev),
+                              None if reuse is None else _need(reuse, "reuse", u8, (U, N), dev), U, N, H, E,
+                              _need(x, "x", torch.float32, shape, dev), _need(out, "out", torch.float32, shape, dev), st)
+    if rc:
+        _check(rc, "evo_cache_add")
     return out
 
 
@@ -459,74 +471,80 @@ class Memory:
 
     def __init__(self, k_pages, v_pages, table, lens, n_head: int, k_scales=None, v_scales=None, starts=None,
                  status=None, dtype: str = "bf16"):
+        torch = _torch or _load_torch()
         self._lib = load()
         dev = self.device = k_pages.device
         e4m3 = k_pages.dtype.itemsize == 1
-        self.torch_dtype = "torch.float32" if dtype == "fp32" else "torch.bfloat16"
+        self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16
         n_pages, n_kv, page, dim = k_pages.shape
         n_seq, cols = table.shape
-        kind = _U8 if e4m3 else self.torch_dtype
+        kind, shape, u8, i32 = torch.uint8 if e4m3 else self.dtype, k_pages.shape, torch.uint8, torch.int32
         if e4m3 != (k_scales is not None) or e4m3 != (v_scales is not None):
             raise ValueError("scales belong to pages of 8-bit codes")
         v = MemoryView(DTYPES[dtype], CACHE_FORMATS["e4m3" if e4m3 else dtype], n_head, n_kv, dim, page, n_pages, cols,
                        n_seq, 0)
-        v.k_pages = _need(k_pages, "k_pages", kind)
-        v.v_pages = _need(v_pages, "v_pages", kind, k_pages.shape, dev)
+        v.k_pages = _need(k_pages, "k_pages", kind, shape, dev)
+        v.v_pages = _need(v_pages, "v_pages", kind, shape, dev)
         if e4m3:
-            v.k_scales = _need(k_scales, "k_scales", _U8, k_pages.shape[:3], dev)
-            v.v_scales = _need(v_scales, "v_scales", _U8, k_pages.shape[:3], dev)
-        v.table = _need(table, "table", _I32, None, dev)
-        v.lens = _need(lens, "lens", _I32, (n_seq,), dev)
-        v.starts = None if starts is None else _need(starts, "starts", _I32, (n_seq + 1,), dev)
-        v.status = None if status is None else _need(status, "status", _I32, (1,), dev)
+            v.k_scales = _need(k_scales, "k_scales", u8, shape[:3], dev)
+            v.v_scales = _need(v_scales, "v_scales", u8, shape[:3], dev)
+        v.table = _need(table, "table", i32, (n_seq, cols), dev)
+        v.lens = _need(lens, "lens", i32, (n_seq,), dev)
+        v.starts = None if starts is None else _need(starts, "starts", i32, (n_seq + 1,), dev)
+        v.status = None if status is None else _need(status, "status", i32, (1,), dev)
         self.view, self._ref = v, ctypes.byref(v)
         self.n_head, self.n_kv_head, self.head_dim, self.n_seq = n_head, n_kv, dim, n_seq
         self.max_len = cols * page
         self.uniform = starts is None
+        self._scratch = {}                          # bytes of scratch by (rows, max_new, max_len)
         self.tensors = (k_pages, v_pages, table, lens, k_scales, v_scales, starts, status)
 
-    def _rows(self, t, what: str, heads: int, rows=None):
-        """(pointer, elements between rows) of [rows][heads][head_dim], heads of a row contiguous."""
-        if str(t.dtype) != self.torch_dtype or t.device != self.device:
-            raise ValueError(f"{what}: {t.dtype} on {t.device}, expected {self.torch_dtype} on {self.device}")
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or rows not in (None, t.shape[0]):
-            raise ValueError(f"{what}: shape {tuple(t.shape)}, expected ({rows or 'rows'}, {heads}, {self.head_dim})")
-        ld, between, within = t.stride()
-        if within != 1 or (heads > 1 and between != self.head_dim):
-            raise ValueError(f"{what}: the heads of a row must be contiguous")
-        return t.data_ptr(), ld if t.shape[0] > 1 else heads * self.head_dim
-
-    def _vector(self, t, what: str, shape, kind=_F32):
-        return None if t is None else _need(t, what, kind, shape, self.device)
+    def _rows(self, t, what: str, rows: int, heads: int):
+        """(address, elements between rows) of [rows][heads][head_dim], heads of a row contiguous."""
+        dim = self.head_dim
+        ld, between, within = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if (t.dtype is not self.dtype or t.device != self.device or t.shape != (rows, heads, dim) or within != 1
+                or (between != dim and heads > 1)):
+            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; expected {self.dtype} "
+                             f"({rows}, {heads}, {dim}) on {self.device}, the heads of a row contiguous")
+        return t.data_ptr(), ld if rows > 1 else heads * dim
 
     def append(self, q, k, v, q_gain=None, k_gain=None, eps: float = 1e-6, rotation=None, pos0=None, out=None,
                max_new=None, stream=None):
         """evo_memory_append: keys and values [rows][n_kv_head][head_dim] to their pages, and the
         normed and rotated queries [rows][n_head][head_dim] (in `out`, which may be q, or a new
         tensor).  q may be None (returns None), or k and v.  max_new is not needed here."""
-        import torch
-        _current(self.device)
+        torch = _torch or _load_torch()
+        dev, dim = self.device, self.head_dim
+        st = _launch_stream(dev, stream)
         if q is None and k is None:
             raise ValueError("neither queries nor keys")
+        if (k is None) != (v is None):
+            raise ValueError("keys and values come together")
         rows = (k if q is None else q).shape[0]
-        qp = kp = vp = op = None
-        ldq = ldk = ldv = ldo = 0
+        qp = kp = vp = op = gq = gk = rot = at0 = None
+        ldq = ldk = ldv = ldo = n_pos = 0
         if q is not None:
-            qp, ldq = self._rows(q, "q", self.n_head, rows)
+            qp, ldq = self._rows(q, "q", rows, self.n_head)
             if out is None:
-                out = torch.empty((rows, self.n_head, self.head_dim), dtype=q.dtype, device=q.device)
-            op, ldo = self._rows(out, "out", self.n_head, rows)
-        if k is not None or v is not None:
-            if k is None or v is None:
-                raise ValueError("keys and values come together")
-            kp, ldk = self._rows(k, "k", self.n_kv_head, rows)
-            vp, ldv = self._rows(v, "v", self.n_kv_head, rows)
-        n_pos = 0 if rotation is None else rotation.shape[0]
-        _check(self._lib.evo_memory_append(
-            self._ref, qp, kp, vp, ldq, ldk, ldv, rows, self._vector(q_gain, "q_gain", (self.head_dim,)),
-            self._vector(k_gain, "k_gain", (self.head_dim,)), eps,
-            self._vector(rotation, "rotation", (n_pos, self.head_dim)), n_pos,
-            self._vector(pos0, "pos0", (self.n_seq,), _I32), op, ldo, _stream(stream)), "evo_memory_append")
+                out = torch.empty((rows, self.n_head, dim), dtype=self.dtype, device=dev)
+            op, ldo = self._rows(out, "out", rows, self.n_head)
+        if k is not None:
+            kp, ldk = self._rows(k, "k", rows, self.n_kv_head)
+            vp, ldv = self._rows(v, "v", rows, self.n_kv_head)
+        if q_gain is not None:
+            gq = _need(q_gain, "q_gain", torch.float32, (dim,), dev)
+        if k_gain is not None:
+            gk = _need(k_gain, "k_gain", torch.float32, (dim,), dev)
+        if rotation is not None:
+            n_pos = rotation.shape[0]
+            rot = _need(rotation, "rotation", torch.float32, (n_pos, dim), dev)
+        if pos0 is not None:
+            at0 = _need(pos0, "pos0", torch.int32, (self.n_seq,), dev)
+        rc = self._lib.evo_memory_append(self._ref, qp, kp, vp, ldq, ldk, ldv, rows, gq, gk, eps, rot, n_pos, at0, op,
+                                         ldo, st)
+        if rc:
+            _check(rc, "evo_memory_append")
         return out if q is not None else None
 
     def attend(self, q, scale=None, causal: bool = True, window: int = 0, max_new=None, max_len=None, out=None,
@@ -535,30 +553,33 @@ class Memory:
         a new tensor (rows of no sequence are left as they are: unset in a new tensor).  scale
         None: head_dim ** -0.5.  max_new, max_len: bounds on the chunks and memories (None: the
         rows, or their equal share, and what the table can hold)."""
-        import torch
-        _current(self.device)
+        torch = _torch or _load_torch()
+        dev, heads, dim = self.device, self.n_head, self.head_dim
+        st = _launch_stream(dev, stream)
         rows = q.shape[0]
-        qp, ldq = self._rows(q, "q", self.n_head)
+        qp, ldq = self._rows(q, "q", rows, heads)
         if out is None:
-            out = torch.empty((rows, self.n_head, self.head_dim), dtype=q.dtype, device=q.device)
-        op, ldo = self._rows(out, "out", self.n_head, rows)
+            out = torch.empty((rows, heads, dim), dtype=self.dtype, device=dev)
+        op, ldo = self._rows(out, "out", rows, heads)
         if rows == 0:
             return out
         if max_new is None:
             max_new = rows // max(1, self.n_seq) if self.uniform else rows
         if max_len is None:
             max_len = self.max_len
-        if scale is None:
-            scale = self.head_dim ** -0.5
-        nb = self._lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
-        scratch = None
+        nb = self._scratch.get((rows, max_new, max_len))
+        if nb is None:
+            nb = self._scratch[rows, max_new, max_len] = self._lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
+        sp = None
         if nb:
-            scratch = torch.empty(nb, dtype=torch.uint8, device=self.device)
+            scratch = torch.empty(nb, dtype=torch.uint8, device=dev)
+            sp = scratch.data_ptr()
             if stream is not None:                  # not reused before that stream's work is done
                 scratch.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-        _check(self._lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, scale, int(causal), window, op,
-                                           ldo, scratch.data_ptr() if nb else None, _stream(stream)),
-               "evo_memory_attend")
+        rc = self._lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, dim ** -0.5 if scale is None else scale,
+                                         causal, window, op, ldo, sp, st)
+        if rc:
+            _check(rc, "evo_memory_attend")
         return out
 
 

@@ -18,6 +18,7 @@
 // spread a row's heads over several warps.
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -28,10 +29,14 @@ namespace evo {
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int BATCH = 4;                            // head groups whose loads a warp has in flight
 
 __device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
+// four values as they are in memory
+template <typename T>
+using Raw = typename std::conditional<sizeof(T) == 4, float4, uint2>::type;
+__device__ __forceinline__ float4 values(float4 u) { return u; }
+__device__ __forceinline__ float4 values(uint2 u) {
   return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                      __uint_as_float(u.y & 0xffff0000u));
 }
@@ -99,18 +104,29 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
   }
   const int nq = a.q ? m.n_head : 0, nk = stores ? m.n_kv_head : 0, heads = nq + 2 * nk;
   const int slot = pos % m.page_tokens;
-  for (int h0 = part * HEADS; h0 < heads; h0 += parts * HEADS) {
-    const int h = h0 + lane / LH;
-    const bool on = h < heads;
-    const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2;            // query, key, value
-    const int hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
-    float4 x = {}, y = {};
-    if (on) {
+  for (int h0 = part * HEADS; h0 < heads; h0 += parts * HEADS * BATCH) {
+  Raw<T> raw[BATCH][2];                                           // a batch of heads' loads in flight at once
+#pragma unroll
+  for (int i = 0; i < BATCH; ++i) {
+    const int h = h0 + i * parts * HEADS + lane / LH;
+    if (h < heads) {
+      const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2;          // query, key, value
+      const int hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
       const T* src = static_cast<const T*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
                      row * (kind == 0 ? a.ldq : kind == 1 ? a.ldk : a.ldv) + (long long)hh * D + 4 * l;
-      x = load4(src);
-      y = load4(src + D / 2);
+      raw[i][0] = *reinterpret_cast<const Raw<T>*>(src);
+      raw[i][1] = *reinterpret_cast<const Raw<T>*>(src + D / 2);
     }
+  }
+#pragma unroll
+  for (int i = 0; i < BATCH; ++i) {
+    if (h0 + i * parts * HEADS >= heads) break;                   // the same for the whole warp
+    const int h = h0 + i * parts * HEADS + lane / LH;
+    const bool on = h < heads;
+    const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2;
+    const int hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
+    float4 x = {}, y = {};
+    if (on) x = values(raw[i][0]), y = values(raw[i][1]);
     const float* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
     float ss = dot4(x) + dot4(y);
 #pragma unroll
@@ -151,6 +167,7 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
       store4(dst, x);
       store4(dst + D / 2, y);
     }
+  }
   }
 }
 

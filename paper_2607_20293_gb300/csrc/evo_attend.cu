@@ -17,6 +17,7 @@
 
 #include "evo_attend.cuh"
 #include "evo_quant.cuh"
+#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
@@ -50,6 +51,15 @@ __device__ __forceinline__ float dot4(float4 a, float4 b, float c) {
 
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+// (top, sum, o) joined with another piece's
+__device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 ml, float4 p) {
+  const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
+  const float f = exp2f(top - base), g = exp2f(ml.x - base);
+  top = now;
+  sum = sum * f + ml.y * g;
+  o = make_float4(o.x * f + p.x * g, o.y * f + p.y * g, o.z * f + p.z * g, o.w * f + p.w * g);
+}
 
 template <int D, int FORMAT, int RM>
 __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
@@ -170,28 +180,48 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
   }
 }
 
-// joins the pieces: a (row, head) per D / 4 lanes
+// joins the pieces: D / 4 lanes a (row, head), or several such groups that share its
+// pieces (groups > 1: few outputs of many pieces would else wait out one load after the other)
 template <typename T, int D>
-__global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendArgs a) {
-  constexpr int LANES = D / 4;
-  const long long i = ((long long)blockIdx.x * THREADS + threadIdx.x) / LANES;
-  const int d = threadIdx.x % LANES * 4;
+__global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendArgs a, int groups) {
+  constexpr int LANES = D / 4, AT_ONCE = THREADS / LANES, BATCH = 4;
+  __shared__ float4 os[AT_ONCE][LANES];
+  __shared__ float2 mls[AT_ONCE];
+  const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES, d = lane * 4, group = slot % groups;
+  const long long i = (long long)blockIdx.x * (AT_ONCE / groups) + slot / groups;
   const int row = (int)(i / a.m.n_head), head = (int)(i % a.m.n_head);
-  if (row >= a.rows) return;
-  if (a.m.starts && (row < a.m.starts[0] || row >= a.m.starts[a.m.n_seq])) return;
-  float top = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.ml[part_index(a, s, row, head)].x);
-  const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+  tc::pdl_wait();
+  bool on = row < a.rows;
+  if (on && a.m.starts) on = row >= a.m.starts[0] && row < a.m.starts[a.m.n_seq];
+  float top = -INFINITY, sum = 0.f;
   float4 o = {};
-  for (int s = 0; s < a.splits; ++s) {
-    const long long at = part_index(a, s, row, head);
-    const float2 ml = a.ml[at];
-    const float f = exp2f(ml.x - base);
-    const float4 p = *reinterpret_cast<const float4*>(a.part + at * D + d);
-    sum = fmaf(ml.y, f, sum);
-    o = make_float4(fmaf(p.x, f, o.x), fmaf(p.y, f, o.y), fmaf(p.z, f, o.z), fmaf(p.w, f, o.w));
+  if (on)
+    for (int s0 = group; s0 < a.splits; s0 += groups * BATCH) {
+      float2 ml[BATCH];
+      float4 p[BATCH];
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) {
+        const int s = s0 + j * groups;
+        ml[j] = make_float2(-INFINITY, 0.f);
+        p[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s < a.splits) {
+          const long long at = part_index(a, s, row, head);
+          ml[j] = a.ml[at];
+          p[j] = *reinterpret_cast<const float4*>(a.part + at * D + d);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < BATCH; ++j) join(top, sum, o, ml[j], p[j]);
+    }
+  if (groups > 1) {
+    os[slot][lane] = o;
+    if (lane == 0) mls[slot] = make_float2(top, sum);
+    __syncthreads();
+    if (group == 0)
+      for (int g = 1; g < groups; ++g) join(top, sum, o, mls[slot + g], os[slot + g][lane]);
+    on = on && group == 0;
   }
+  if (!on) return;
   const float f = sum == 0.f ? 0.f : 1.f / sum;
   T* dst = static_cast<T*>(a.out) + row * a.ldo + (long long)head * D + d;
   put(dst, o.x * f);
@@ -219,9 +249,20 @@ cudaError_t launch_f32(const AttendArgs& a, bool wide, cudaStream_t st) {
 
 template <typename T, int D>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
-  const long long threads = (long long)a.rows * a.m.n_head * (D / 4);
-  join_kernel<T, D><<<(unsigned)((threads + THREADS - 1) / THREADS), THREADS, 0, st>>>(a);
-  return cudaGetLastError();
+  constexpr int AT_ONCE = THREADS / (D / 4);
+  const long long outputs = (long long)a.rows * a.m.n_head;
+  int groups = 1;                                  // 16 pieces a group, while the GPU has threads to spare
+  while (groups < AT_ONCE && groups * 16 < a.splits && outputs * groups < 152 * 8 * AT_ONCE) groups *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = (unsigned)((outputs * groups + AT_ONCE - 1) / AT_ONCE);
+  cfg.blockDim = THREADS;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];                       // the launch overlaps the pieces' end; the kernel waits for it
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, join_kernel<T, D>, a, groups);
 }
 
 }  // namespace
@@ -235,7 +276,7 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   p.tile_rows = f32 ? (all <= 16 ? 16 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
-  const long long most = std::max(1, max_len / (tiles ? 512 : 256));
+  const long long most = std::max(1, max_len / (tiles ? 512 : f32 ? 64 : 256));
   const long long target = f32 ? 304 : tiles ? 152 : blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
   p.splits = (int)std::max(1ll, std::min({most, tiles ? target / blocks : (target + blocks / 2) / blocks, 64ll}));
   p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);

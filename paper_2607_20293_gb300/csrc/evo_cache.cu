@@ -19,6 +19,7 @@ namespace evo {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int BATCH = 6;                            // units whose loads a thread has in flight
 
 template <typename T>
 struct Eight;
@@ -85,15 +86,28 @@ __global__ void __launch_bounds__(THREADS) cache_add_kernel(const uint8_t* codes
   const long long at = 8ll * i;
   float4 s[2];
   Eight<float>::load(x + at, s);
-  for (int u = 0; u < U; ++u) {
-    if (reuse && reuse[(long long)u * N + n] == 0) continue;
-    const long long v = (long long)u * total + i;
-    const uint2 c = *reinterpret_cast<const uint2*>(codes + 8 * v);
-    const float f = scale_value(scales[v >> 2]);
-    const float4 a = codes4(c.x), b = codes4(c.y);
-    // a product by a power of two is exact: the fused form rounds as the sum does
-    s[0] = make_float4(fmaf(a.x, f, s[0].x), fmaf(a.y, f, s[0].y), fmaf(a.z, f, s[0].z), fmaf(a.w, f, s[0].w));
-    s[1] = make_float4(fmaf(b.x, f, s[1].x), fmaf(b.y, f, s[1].y), fmaf(b.z, f, s[1].z), fmaf(b.w, f, s[1].w));
+  for (int u0 = 0; u0 < U; u0 += BATCH) {          // a batch of units' loads in flight at once
+    uint2 c[BATCH];
+    uint32_t f[BATCH];
+    bool on[BATCH];
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j) on[j] = u0 + j < U && (!reuse || reuse[(long long)(u0 + j) * N + n] != 0);
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j)
+      if (on[j]) {
+        const long long v = (long long)(u0 + j) * total + i;
+        c[j] = *reinterpret_cast<const uint2*>(codes + 8 * v);
+        f[j] = scales[v >> 2];
+      }
+#pragma unroll
+    for (int j = 0; j < BATCH; ++j)
+      if (on[j]) {
+        const float k = scale_value(f[j]);
+        const float4 a = codes4(c[j].x), b = codes4(c[j].y);
+        // a product by a power of two is exact: the fused form rounds as the sum does
+        s[0] = make_float4(fmaf(a.x, k, s[0].x), fmaf(a.y, k, s[0].y), fmaf(a.z, k, s[0].z), fmaf(a.w, k, s[0].w));
+        s[1] = make_float4(fmaf(b.x, k, s[1].x), fmaf(b.y, k, s[1].y), fmaf(b.z, k, s[1].z), fmaf(b.w, k, s[1].w));
+      }
   }
   reinterpret_cast<float4*>(y + at)[0] = s[0];
   reinterpret_cast<float4*>(y + at)[1] = s[1];

@@ -148,13 +148,8 @@ def test_binding_checks_tensors(B):
         with pytest.raises(ValueError):
             B.Memory(**args)
     q = torch.zeros(6, 4, 64, dtype=torch.bfloat16)
-    with pytest.raises(ValueError):
-        m._rows(q[:, :3], "q", 4)
-    with pytest.raises(ValueError):
-        m._rows(q.float(), "q", 4)
-    with pytest.raises(ValueError):
-        m._rows(q.transpose(0, 1), "q", 6)
+    for bad in (q[:, :3], q.float(), q.transpose(0, 1), q[:5], q[..., :32], q[0], q.transpose(1, 2)):
+        with pytest.raises(ValueError):
+            m._rows(bad, "q", 6, 4)
     fused = torch.zeros(6, 8 * 64, dtype=torch.bfloat16)
-    assert m._rows(fused[:, 128:384].unflatten(1, (4, 64)), "q", 4) == (fused.data_ptr() + 256, 512)
-    with pytest.raises(ValueError):              # not on the current CUDA device
-        B._current(pages.device)
+    assert m._rows(fused[:, 128:384].unflatten(1, (4, 64)), "q", 6, 4) == (fused.data_ptr() + 256, 512)
