@@ -9,13 +9,17 @@
 //             byte for the head's row (evo_quant.cuh)
 //
 // One rounding per output: everything between the load and the store is fp32.
-// A warp takes a row (a token).  D / 8 lanes hold one head, each the 4 values at
-// 4l and the 4 at D/2 + 4l: both halves of every rotated pair are in one lane, so
+// A warp takes a row (a token).  D / 16 lanes hold one head, each the 8 values at
+// 8l and the 8 at D/2 + 8l: both halves of every rotated pair are in one lane, so
 // the rotation needs no exchange, and the norm and the largest magnitude are
-// shuffles over those lanes.  The row's cosines and sines stay in registers for
-// all its heads.  The work is bound by DRAM for long chunks and by the chain
-// starts -> length -> table -> page for single tokens; short calls therefore
-// spread a row's heads over several warps.
+// shuffles over those lanes.
+//
+// The work is bound by DRAM for long chunks and by the chain starts -> length ->
+// table -> page for single tokens.  Calls of few rows spread a row's heads over
+// several warps (64 tokens of 24 heads of 64: 6.2 us).  Calls of many rows copy whole
+// rows to shared memory by bulk copies, issued before the chain is walked, and walk it
+// for all rows of a warp at once: 11,700 rows of 24 heads of 128 take 29.0 us (4.75
+// TB/s), against 32.7 with loads to registers and one chain a row.
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>
@@ -24,174 +28,344 @@
 
 #include "evo_memory.h"
 #include "evo_quant.cuh"
+#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int BATCH = 4;                            // head groups whose loads a warp has in flight
+constexpr int RING_WARPS = 4, RING_THREADS = 32 * RING_WARPS;
+constexpr int STAGES = 1;                           // rows a warp holds: 20 warps a SM with one each are ahead of 16 with two (30.1 us)
+constexpr int RING_BLOCKS = 5;                      // blocks a SM
+constexpr int BATCH = 2;                            // head groups whose loads a warp has in flight
 
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-// four values as they are in memory
+// eight values of a row as they are in memory, and as four pairs of fp32
 template <typename T>
-using Raw = typename std::conditional<sizeof(T) == 4, float4, uint2>::type;
-__device__ __forceinline__ float4 values(float4 u) { return u; }
-__device__ __forceinline__ float4 values(uint2 u) {
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
+struct Raw {
+  uint4 u[sizeof(T) / 2];
+};
+__device__ __forceinline__ void values(const Raw<float>& r, float2 (&v)[4]) {
+  v[0] = make_float2(__uint_as_float(r.u[0].x), __uint_as_float(r.u[0].y));
+  v[1] = make_float2(__uint_as_float(r.u[0].z), __uint_as_float(r.u[0].w));
+  v[2] = make_float2(__uint_as_float(r.u[1].x), __uint_as_float(r.u[1].y));
+  v[3] = make_float2(__uint_as_float(r.u[1].z), __uint_as_float(r.u[1].w));
 }
-__device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+__device__ __forceinline__ void values(const Raw<__nv_bfloat16>& r, float2 (&v)[4]) {
+  const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ float dot4(float4 a) { return (a.x * a.x + a.y * a.y) + (a.z * a.z + a.w * a.w); }
-
-// the sequence that row belongs to: the last n with starts[n] <= row, found 32
-// entries a step by the whole warp (two dependent loads for up to 1,024 sequences)
-__device__ __forceinline__ int seq_of_row(const int* starts, int n_seq, int row, int lane) {
-  int lo = 0, hi = n_seq;                             // starts[lo] <= row, starts[hi] > row
-  while (hi - lo > 1) {
-    const int step = (hi - lo + 31) / 32;
-    const int at = lo + (lane + 1) * step;
-    const unsigned past = __ballot_sync(0xffffffffu, at >= hi || starts[min(at, n_seq)] > row);
-    const int k = past ? __ffs(past) - 1 : 32;        // the first probe past the row
-    const int from = lo + k * step;
-    hi = min(hi, from + step);
-    lo = from;
+__device__ __forceinline__ void store8(float* p, const float2 (&v)[4]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float2 (&v)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[i].x, v[i].y);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
   }
-  return lo;
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// packed arithmetic that keeps subnormals
+__device__ __forceinline__ float2 mul_pair(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n"
+      " mul.rn.f32x2 rd, ra, rb;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
+      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
 }
 
-template <typename T, int D, int FORMAT>
-__global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__ AppendArgs a, int parts) {
-  constexpr int LH = D / 8, HEADS = 32 / LH;          // lanes a head, heads a warp takes at once
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(tc::su32(dst)),
+               "l"(src), "r"(bytes), "r"(tc::su32(bar))
+               : "memory");
+}
+// a bounded wait: false if the copies did not arrive
+__device__ __forceinline__ bool arrived(uint64_t* bar, uint32_t parity) {
+  for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
+    if (tc::mbar_test(tc::su32(bar), parity)) return true;
+  return false;
+}
+
+enum { QUERY, KEY, VALUE };
+
+// 8 + 8 values of a head (columns 8 l and D/2 + 8 l): norm, rotation and store
+struct Lane {
+  float2 c[4], s[4];              // cosines and sines of the row
+  float2 g0[4], g1[4];            // gain
+};
+__device__ __forceinline__ void load_pairs(const float* p, float2 (&v)[4]) {
+  Raw<float> r;
+  r.u[0] = reinterpret_cast<const uint4*>(p)[0];
+  r.u[1] = reinterpret_cast<const uint4*>(p)[1];
+  values(r, v);
+}
+
+template <typename T, int D, int FORMAT, int KIND>
+__device__ __forceinline__ void put_head(const AppendArgs& a, const Lane& t, const Raw<T>& r0, const Raw<T>& r1, bool norm,
+                                         bool turn, bool on, long long at, int row, int head, int l) {
+  constexpr int LH = D / 16;
+  float2 x[4], y[4];
+  values(r0, x);
+  values(r1, y);
+  if (KIND != VALUE && norm) {
+    float2 ss = mul_pair(x[0], x[0]), sy = mul_pair(y[0], y[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) ss = fma_pair(x[i], x[i], ss), sy = fma_pair(y[i], y[i], sy);
+    float sum = (ss.x + ss.y) + (sy.x + sy.y);
+#pragma unroll
+    for (int o = LH / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float f = rsqrtf(sum * (1.0f / D) + a.eps);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = mul_pair(mul_pair(x[i], make_float2(f, f)), t.g0[i]);
+      y[i] = mul_pair(mul_pair(y[i], make_float2(f, f)), t.g1[i]);
+    }
+  }
+  if (KIND != VALUE && turn) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 u = x[i], s = t.s[i];
+      x[i] = fma_pair(y[i], make_float2(-s.x, -s.y), mul_pair(u, t.c[i]));
+      y[i] = fma_pair(u, s, mul_pair(y[i], t.c[i]));
+    }
+  }
+  if constexpr (KIND == QUERY) {
+    T* dst = static_cast<T*>(a.q_out) + row * a.ldo + head * D + 8 * l;
+    if (on) store8(dst, x), store8(dst + D / 2, y);
+  } else if constexpr (FORMAT == EVO_CACHE_E4M3) {
+    uint32_t b = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b = amax_bits(amax_bits(amax_bits(amax_bits(b, x[i].x), x[i].y), y[i].x), y[i].y);
+    const uint32_t byte = scale_byte(group_umax<LH>(b));
+    uint8_t* dst = static_cast<uint8_t*>(KIND == KEY ? a.m.k_pages : a.m.v_pages) + at * D + 8 * l;
+    if (on) {
+      *reinterpret_cast<uint2*>(dst) = make_uint2(quantise4(make_float4(x[0].x, x[0].y, x[1].x, x[1].y), byte),
+                                                  quantise4(make_float4(x[2].x, x[2].y, x[3].x, x[3].y), byte));
+      *reinterpret_cast<uint2*>(dst + D / 2) = make_uint2(quantise4(make_float4(y[0].x, y[0].y, y[1].x, y[1].y), byte),
+                                                          quantise4(make_float4(y[2].x, y[2].y, y[3].x, y[3].y), byte));
+      if (l == 0) (KIND == KEY ? a.m.k_scales : a.m.v_scales)[at] = (uint8_t)byte;
+    }
+  } else {
+    T* dst = static_cast<T*>(KIND == KEY ? a.m.k_pages : a.m.v_pages) + at * D + 8 * l;
+    if (on) store8(dst, x), store8(dst + D / 2, y);
+  }
+}
+
+// heads [0, n) of one kind: a warp takes HEADS of them at once, every parts-th such group
+// from `first` on, the loads of BATCH groups in flight
+template <typename T, int D, int FORMAT, int KIND>
+__device__ __forceinline__ void put_heads(const AppendArgs& a, Lane& t, const T* from, const float* gain, int n, int first,
+                                          int parts, long long at0, int row, int lane) {
+  constexpr int LH = D / 16, HEADS = 32 / LH;
+  const int l = lane % LH, hl = lane / LH;
+  const bool norm = KIND != VALUE && gain, turn = KIND != VALUE && a.rotation;
+  if (first * HEADS >= n) return;
+  if (norm) load_pairs(gain + 8 * l, t.g0), load_pairs(gain + D / 2 + 8 * l, t.g1);
+  const T* src = from + 8 * l;
+  for (int g0 = first; g0 * HEADS < n; g0 += parts * BATCH) {
+    Raw<T> r[BATCH][2] = {};
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int h = (g0 + i * parts) * HEADS + hl;
+      if (h < n) {
+#pragma unroll
+        for (int e = 0; e < (int)sizeof(T) / 2; ++e) {
+          r[i][0].u[e] = reinterpret_cast<const uint4*>(src + h * D)[e];
+          r[i][1].u[e] = reinterpret_cast<const uint4*>(src + h * D + D / 2)[e];
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const int h = (g0 + i * parts) * HEADS + hl;
+      if ((g0 + i * parts) * HEADS >= n) break;      // the same for the whole warp
+      put_head<T, D, FORMAT, KIND>(a, t, r[i][0], r[i][1], norm, turn, h < n, at0 + (long long)h * a.m.page_tokens, row, h, l);
+    }
+  }
+}
+
+// where a row belongs
+struct Place {
+  int turn;                       // position for the rotation, or -1: the row is not touched
+  int page, slot;
+};
+
+// the place of this lane's row; reports what it cannot place
+__device__ __forceinline__ Place place_of(const AppendArgs& a, int row) {
   const evo_memory& m = a.m;
-  const int lane = threadIdx.x & 31, l = lane % LH;
-  const long long w = (long long)blockIdx.x * WARPS + (threadIdx.x >> 5);
-  const int row = (int)(w / parts), part = (int)(w % parts);
-  if (row >= a.rows) return;
+  Place p{-1, 0, 0};
+  if (row >= a.rows) return p;
   int n;
   if (m.starts) {
-    if (row < m.starts[0] || row >= m.starts[m.n_seq]) return;    // behind the last sequence
-    n = seq_of_row(m.starts, m.n_seq, row, lane);
+    if (row < m.starts[0] || row >= m.starts[m.n_seq]) return p;  // behind the last sequence
+    int lo = 0, hi = m.n_seq;                                     // starts[lo] <= row < starts[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (m.starts[mid] <= row) lo = mid;
+      else hi = mid;
+    }
+    n = lo;
   } else {
     n = row / (a.rows / m.n_seq);
   }
   const SeqRows s = seq_rows(m, n, a.rows, a.rows);
-  if (row < s.first || row >= s.first + s.count) return;          // malformed starts
+  if (row < s.first || row >= s.first + s.count) return p;        // malformed starts
   const int pos = m.lens[n] - s.count + (row - s.first);
-  const int turn = pos + (a.pos0 ? a.pos0[n] : 0);
-  const int pi = pos / m.page_tokens;
-  const bool stores = a.k != nullptr;
-  if (pos < 0 || pi >= m.max_pages || (a.rotation && (turn < 0 || turn >= a.n_pos))) {
+  const int turn = a.rotation ? pos + (a.pos0 ? a.pos0[n] : 0) : 0;
+  const int pi = pos >> (31 - __clz(m.page_tokens));
+  if (pos < 0 || pi >= m.max_pages || turn < 0 || (a.rotation && turn >= a.n_pos)) {
     memory_fault(m);
-    return;
+    return p;
   }
-  int page = 0;
-  if (stores) {
-    page = m.table[(long long)n * m.max_pages + pi];
-    if ((unsigned)page >= (unsigned)m.n_pages) {
+  if (a.k) {
+    p.page = m.table[(long long)n * m.max_pages + pi];
+    if ((unsigned)p.page >= (unsigned)m.n_pages) {
       memory_fault(m);
-      return;
+      return p;
     }
   }
-  float4 c, sn;
+  p.turn = turn;
+  p.slot = pos & (m.page_tokens - 1);
+  return p;
+}
+
+// a row's heads, from wherever its queries, keys and values lie: groups of HEADS heads of one
+// kind, of which this warp takes part, part + parts, ...
+template <typename T, int D, int FORMAT>
+__device__ __forceinline__ void put_row(const AppendArgs& a, const T* q, const T* k, const T* v, const float* rotation, int part,
+                                        int parts, long long at, int row, int lane) {
+  constexpr int HEADS = 512 / D;
+  Lane t;
   if (a.rotation) {
-    const float* t = a.rotation + (long long)turn * D + 4 * l;
-    c = load4(t);
-    sn = load4(t + D / 2);
+    load_pairs(rotation + 8 * (lane % (D / 16)), t.c);
+    load_pairs(rotation + D / 2 + 8 * (lane % (D / 16)), t.s);
   }
-  const int nq = a.q ? m.n_head : 0, nk = stores ? m.n_kv_head : 0, heads = nq + 2 * nk;
-  const int slot = pos % m.page_tokens;
-  for (int h0 = part * HEADS; h0 < heads; h0 += parts * HEADS * BATCH) {
-  Raw<T> raw[BATCH][2];                                           // a batch of heads' loads in flight at once
-#pragma unroll
-  for (int i = 0; i < BATCH; ++i) {
-    const int h = h0 + i * parts * HEADS + lane / LH;
-    if (h < heads) {
-      const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2;          // query, key, value
-      const int hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
-      const T* src = static_cast<const T*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
-                     row * (kind == 0 ? a.ldq : kind == 1 ? a.ldk : a.ldv) + (long long)hh * D + 4 * l;
-      raw[i][0] = *reinterpret_cast<const Raw<T>*>(src);
-      raw[i][1] = *reinterpret_cast<const Raw<T>*>(src + D / 2);
-    }
+  const int nq = a.q ? a.m.n_head : 0, nk = a.k ? a.m.n_kv_head : 0;
+  const int gq = (nq + HEADS - 1) / HEADS, gk = (nk + HEADS - 1) / HEADS;
+  const int fk = (part + parts - gq % parts) % parts, fv = (fk + parts - gk % parts) % parts;
+  put_heads<T, D, FORMAT, QUERY>(a, t, q, a.q_gain, nq, part, parts, 0, row, lane);
+  put_heads<T, D, FORMAT, KEY>(a, t, k, a.k_gain, nk, fk, parts, at, row, lane);
+  put_heads<T, D, FORMAT, VALUE>(a, t, v, nullptr, nk, fv, parts, at, row, lane);
+}
+
+// few rows: a row's heads over `parts` warps, straight from global memory
+template <typename T, int D, int FORMAT>
+__global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__ AppendArgs a, int parts) {
+  const int lane = threadIdx.x & 31;
+  const int w = blockIdx.x * WARPS + (threadIdx.x >> 5), row = w / parts;
+  if (row >= a.rows) return;
+  const Place p = place_of(a, row);
+  if (p.turn < 0) return;
+  const long long at = (long long)p.page * a.m.n_kv_head * a.m.page_tokens + p.slot;
+  put_row<T, D, FORMAT>(a, static_cast<const T*>(a.q) + row * a.ldq, static_cast<const T*>(a.k) + row * a.ldk,
+                        static_cast<const T*>(a.v) + row * a.ldv, a.rotation + (long long)p.turn * D, w % parts, parts, at, row,
+                        lane);
+}
+
+// many rows: a warp takes `each` rows behind one another.  Their places are looked up together, a
+// lane each, and their data arrive in the warp's ring of STAGES rows by bulk copies, so that neither
+// chain of loads is waited out once a row.
+template <typename T, int D, int FORMAT>
+__global__ void __launch_bounds__(RING_THREADS, RING_BLOCKS) append_ring_kernel(const __grid_constant__ AppendArgs a, int each) {
+  extern __shared__ __align__(128) uint8_t ring[];
+  __shared__ __align__(8) uint64_t full[RING_WARPS][STAGES];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int first = (blockIdx.x * RING_WARPS + warp) * each, count = min(each, a.rows - first);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < RING_WARPS * STAGES; ++i) tc::mbar_init1(&full[0][i], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-#pragma unroll
-  for (int i = 0; i < BATCH; ++i) {
-    if (h0 + i * parts * HEADS >= heads) break;                   // the same for the whole warp
-    const int h = h0 + i * parts * HEADS + lane / LH;
-    const bool on = h < heads;
-    const int kind = h < nq ? 0 : h < nq + nk ? 1 : 2;
-    const int hh = kind == 0 ? h : kind == 1 ? h - nq : h - nq - nk;
-    float4 x = {}, y = {};
-    if (on) x = values(raw[i][0]), y = values(raw[i][1]);
-    const float* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
-    float ss = dot4(x) + dot4(y);
-#pragma unroll
-    for (int o = LH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    if (gain) {
-      const float f = 1.0f / sqrtf(ss * (1.0f / D) + a.eps);
-      const float4 g = load4(gain + 4 * l), e = load4(gain + D / 2 + 4 * l);
-      x = make_float4(x.x * f * g.x, x.y * f * g.y, x.z * f * g.z, x.w * f * g.w);
-      y = make_float4(y.x * f * e.x, y.y * f * e.y, y.z * f * e.z, y.w * f * e.w);
+  __syncthreads();
+  const int qb = a.q ? a.m.n_head * D * (int)sizeof(T) : 0, kb = a.k ? a.m.n_kv_head * D * (int)sizeof(T) : 0;
+  const int rb = a.rotation ? D * 4 : 0, bytes = qb + 2 * kb + rb;
+  uint8_t* const mine = ring + warp * STAGES * bytes;
+  const auto copy_data = [&](int i) {
+    if (i >= count || lane != 0) return;
+    const long long row = first + i;
+    uint8_t* dst = mine + i % STAGES * bytes;
+    uint64_t* bar = &full[warp][i % STAGES];
+    if (qb) bulk_load(dst, static_cast<const T*>(a.q) + row * a.ldq, qb, bar);
+    if (kb) bulk_load(dst + qb, static_cast<const T*>(a.k) + row * a.ldk, kb, bar);
+    if (kb) bulk_load(dst + qb + kb, static_cast<const T*>(a.v) + row * a.ldv, kb, bar);
+  };
+  for (int i = 0; i < STAGES; ++i) copy_data(i);    // on their way while the places are looked up
+  const Place place = place_of(a, lane < count ? first + lane : a.rows);
+  const auto copy_rotation = [&](int i) {           // and the stage's count of bytes
+    const int turn = __shfl_sync(0xffffffffu, place.turn, i & 31);
+    if (i >= count || lane != 0) return;
+    uint64_t* bar = &full[warp][i % STAGES];
+    const int r = turn < 0 ? 0 : rb;                // a row that is not touched has none
+    tc::mbar_expect_tx(bar, qb + 2 * kb + r);
+    if (r) bulk_load(mine + i % STAGES * bytes + qb + 2 * kb, a.rotation + (long long)turn * D, r, bar);
+  };
+  for (int i = 0; i < STAGES; ++i) copy_rotation(i);
+  bool ok = true;
+  for (int i = 0; i < count && ok; ++i) {
+    const int stage = i % STAGES, turn = __shfl_sync(0xffffffffu, place.turn, i);
+    const int page = __shfl_sync(0xffffffffu, place.page, i), slot = __shfl_sync(0xffffffffu, place.slot, i);
+    ok = __all_sync(0xffffffffu, arrived(&full[warp][stage], (i / STAGES) & 1));
+    if (ok && turn >= 0) {
+      const uint8_t* src = mine + stage * bytes;
+      put_row<T, D, FORMAT>(a, reinterpret_cast<const T*>(src), reinterpret_cast<const T*>(src + qb),
+                            reinterpret_cast<const T*>(src + qb + kb), reinterpret_cast<const float*>(src + qb + 2 * kb), 0, 1,
+                            (long long)page * a.m.n_kv_head * a.m.page_tokens + slot, first + i, lane);
     }
-    if (a.rotation && kind != 2) {
-      const float4 u = x;
-      x = make_float4(x.x * c.x - y.x * sn.x, x.y * c.y - y.y * sn.y, x.z * c.z - y.z * sn.z, x.w * c.w - y.w * sn.w);
-      y = make_float4(y.x * c.x + u.x * sn.x, y.y * c.y + u.y * sn.y, y.z * c.z + u.z * sn.z, y.w * c.w + u.w * sn.w);
-    }
-    uint32_t byte = 0;
-    if constexpr (FORMAT == EVO_CACHE_E4M3) {
-      uint32_t b = 0;
-      b = amax_bits(amax_bits(amax_bits(amax_bits(b, x.x), x.y), x.z), x.w);
-      b = amax_bits(amax_bits(amax_bits(amax_bits(b, y.x), y.y), y.z), y.w);
-      byte = scale_byte(group_umax<LH>(b));
-    }
-    if (!on) continue;
-    if (kind == 0) {
-      T* dst = static_cast<T*>(a.q_out) + row * a.ldo + (long long)hh * D + 4 * l;
-      store4(dst, x);
-      store4(dst + D / 2, y);
-      continue;
-    }
-    const long long at = ((long long)page * m.n_kv_head + hh) * m.page_tokens + slot;
-    if constexpr (FORMAT == EVO_CACHE_E4M3) {
-      uint8_t* dst = static_cast<uint8_t*>(kind == 1 ? m.k_pages : m.v_pages) + at * D + 4 * l;
-      *reinterpret_cast<uint32_t*>(dst) = quantise4(x, byte);
-      *reinterpret_cast<uint32_t*>(dst + D / 2) = quantise4(y, byte);
-      if (l == 0) (kind == 1 ? m.k_scales : m.v_scales)[at] = (uint8_t)byte;
-    } else {
-      T* dst = static_cast<T*>(kind == 1 ? m.k_pages : m.v_pages) + at * D + 4 * l;
-      store4(dst, x);
-      store4(dst + D / 2, y);
-    }
+    __syncwarp();                                   // every lane has read the stage
+    if (ok) copy_data(i + STAGES), copy_rotation(i + STAGES);
   }
+  if (__syncthreads_or(!ok)) {                      // a copy did not arrive: those in flight land before the block ends
+    if (threadIdx.x == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
+    const long long t0 = clock64();
+    while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);
   }
 }
 
-template <typename T, int D>
-cudaError_t launch_as(const AppendArgs& a, int parts, cudaStream_t st) {
-  const long long warps = (long long)a.rows * parts;
-  const unsigned grid = (unsigned)((warps + WARPS - 1) / WARPS);
-  if (a.m.format == EVO_CACHE_E4M3)
-    append_kernel<T, D, EVO_CACHE_E4M3><<<grid, THREADS, 0, st>>>(a, parts);
-  else
-    append_kernel<T, D, EVO_CACHE_F32><<<grid, THREADS, 0, st>>>(a, parts);   // the activations' own type
+template <typename T, int D, int FORMAT>
+cudaError_t launch_as(const AppendArgs& a, cudaStream_t st) {
+  const int row = ((a.q ? a.m.n_head : 0) + (a.k ? 2 * a.m.n_kv_head : 0)) * D * (int)sizeof(T) + (a.rotation ? 4 * D : 0);
+  const int smem = RING_WARPS * STAGES * row, blocks = std::min(RING_BLOCKS, 220 * 1024 / std::max(smem, 1));
+  const int warps = 152 * RING_WARPS * blocks;      // resident at once
+  if (blocks >= 2 && a.rows >= 2 * warps) {
+    const auto k = append_ring_kernel<T, D, FORMAT>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const int each = std::min(32, (a.rows + warps - 1) / warps);
+    const int need = (a.rows + each - 1) / each;
+    k<<<(need + RING_WARPS - 1) / RING_WARPS, RING_THREADS, smem, st>>>(a, each);
+    return cudaGetLastError();
+  }
+  const int at_once = 512 / D;
+  const int most = (a.q ? (a.m.n_head + at_once - 1) / at_once : 0) + (a.k ? 2 * ((a.m.n_kv_head + at_once - 1) / at_once) : 0);
+  // a row's heads over as many warps as keep the GPU's 152 x 32 busy
+  const int parts = (int)std::max(1ll, std::min((long long)most, 152ll * 32 / a.rows));
+  const long long warps_needed = (long long)a.rows * parts;
+  append_kernel<T, D, FORMAT><<<(unsigned)((warps_needed + WARPS - 1) / WARPS), THREADS, 0, st>>>(a, parts);
   return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_type(const AppendArgs& a, cudaStream_t st) {
+  const bool d64 = a.m.head_dim == 64;              // EVO_CACHE_F32 stands for the rows' own type
+  if (a.m.format == EVO_CACHE_E4M3) return d64 ? launch_as<T, 64, EVO_CACHE_E4M3>(a, st) : launch_as<T, 128, EVO_CACHE_E4M3>(a, st);
+  return d64 ? launch_as<T, 64, EVO_CACHE_F32>(a, st) : launch_as<T, 128, EVO_CACHE_F32>(a, st);
 }
 
 }  // namespace
 
 cudaError_t launch_append(const AppendArgs& a, cudaStream_t st) {
-  const int D = a.m.head_dim, at_once = 256 / D;
-  const int heads = (a.q ? a.m.n_head : 0) + (a.k ? 2 * a.m.n_kv_head : 0);
-  const int most = (heads + at_once - 1) / at_once;
-  // few rows: a row's heads over as many warps as keep the GPU's 152 x 32 warps busy
-  const int parts = (int)std::max(1ll, std::min((long long)most, 152ll * 32 / a.rows));
-  if (a.m.dtype == EVO_DTYPE_F32) return D == 64 ? launch_as<float, 64>(a, parts, st) : launch_as<float, 128>(a, parts, st);
-  return D == 64 ? launch_as<__nv_bfloat16, 64>(a, parts, st) : launch_as<__nv_bfloat16, 128>(a, parts, st);
+  return a.m.dtype == EVO_DTYPE_F32 ? launch_type<float>(a, st) : launch_type<__nv_bfloat16>(a, st);
 }
 
 }  // namespace evo

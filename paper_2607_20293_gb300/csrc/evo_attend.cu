@@ -7,9 +7,12 @@
 // (a row that sees none is zero).  A memory split over several blocks leaves each
 // piece's maximum, sum and unnormalised values, which a second kernel joins.
 //
-// fp32 kernel: a block of 256 threads takes BM = 16 RM rows and 64 keys at a
-// time; the thread at (ty, tx) of a 16 x 16 grid computes RM rows x 4 keys of the
-// scores and RM rows x D/16 columns of the output, all products in fp32.
+// fp32 kernel: a block of 128 threads takes 8 RM rows and 64 keys at a time; the
+// thread at (ty, tx) of an 8 x 16 grid computes RM rows x 4 keys of the scores and RM
+// rows x D/16 columns of the output.  All products are fp32 (packed in pairs: half the
+// issue slots), so that the multiply-add units bound it with many rows; with few rows
+// the blocks of a SM hide one another's loads.  There is no tensor-core form of it:
+// three tf32 products for one of fp32 are 170 multiply-adds a cycle and SM, against 128.
 #include <algorithm>
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -22,11 +25,11 @@
 namespace evo {
 namespace {
 
-constexpr int BN = 64, THREADS = 256;
+constexpr int BN = 64, THREADS = 128, JOIN_THREADS = 256;
 
 template <int D, int RM>
 struct Smem {
-  static constexpr int BM = 16 * RM;
+  static constexpr int BM = 8 * RM;
   float q[BM][D];
   float k[BN][D + 4];           // rows 4 banks apart: 8 rows' float4 in a phase do not collide
   float v[BN][D];
@@ -45,8 +48,14 @@ __device__ __forceinline__ float4 memory4(const void* pages, const uint8_t* scal
   }
 }
 
-__device__ __forceinline__ float dot4(float4 a, float4 b, float c) {
-  return fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, c))));
+// exact products and sums of pairs, subnormals kept
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
+      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
 }
 
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
@@ -65,13 +74,16 @@ template <int D, int FORMAT, int RM>
 __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
   extern __shared__ __align__(16) uint8_t raw[];
   Smem<D, RM>& sm = *reinterpret_cast<Smem<D, RM>*>(raw);
-  constexpr int BM = 16 * RM, DC = D / 16;
+  constexpr int BM = 8 * RM, DC = D / 64;          // a thread's columns: 4 tx + 64 c .. + 3
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
   const Tile t = tile_of_block(a);
   const int rows = t.count * a.group, r0 = t.tile * BM;
   if (r0 >= rows) return;
   const int last = min(r0 + BM, rows) - 1;
-  const Range all = piece_of(a, t, seen_by_tile(a, t, r0 / a.group, last / a.group), BN);
+  const Range first_row = seen_by(a, t, r0 / a.group), last_row = seen_by(a, t, last / a.group);
+  const Range all = piece_of(a, t, {first_row.lo, last_row.hi}, BN);
+  const int whole_lo = max(last_row.lo, all.lo), whole_hi = min(first_row.hi, all.hi);
+  const int shift = 31 - __clz(a.m.page_tokens);
 
   for (int i = tid; i < BM * D / 4; i += THREADS) {
     const int r = i / (D / 4), d = i % (D / 4) * 4, R = r0 + r;
@@ -82,25 +94,29 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
     *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
   }
   Range seen[RM];
-  float mx[RM], sum[RM], o[RM][DC];
+  float mx[RM], sum[RM];
+  float2 o[RM][DC][2];
 #pragma unroll
   for (int i = 0; i < RM; ++i) {
     const int R = r0 + ty * RM + i;
     seen[i] = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
+    seen[i] = {max(seen[i].lo, all.lo), min(seen[i].hi, all.hi)};
     mx[i] = -INFINITY;
     sum[i] = 0.f;
 #pragma unroll
-    for (int c = 0; c < DC; ++c) o[i][c] = 0.f;
+    for (int c = 0; c < DC; ++c) o[i][c][0] = o[i][c][1] = make_float2(0.f, 0.f);
   }
   for (int k0 = all.lo / BN * BN; k0 < all.hi; k0 += BN) {
+    const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
     __syncthreads();
+#pragma unroll 4
     for (int i = tid; i < BN * D / 4; i += THREADS) {
       const int r = i / (D / 4), d = i % (D / 4) * 4, key = k0 + r;
       float4 k = {}, v = {};
       if (key >= all.lo && key < all.hi) {
-        const int page = seq_page(a.m, t.n, key / a.m.page_tokens);
+        const int page = seq_page(a.m, t.n, key >> shift);
         const long long at =
-            ((long long)page * a.m.n_kv_head + t.kv_head) * a.m.page_tokens + key % a.m.page_tokens;
+            ((long long)page * a.m.n_kv_head + t.kv_head) * a.m.page_tokens + (key & (a.m.page_tokens - 1));
         k = memory4<FORMAT>(a.m.k_pages, a.m.k_scales, at, D, d);
         v = memory4<FORMAT>(a.m.v_pages, a.m.v_scales, at, D, d);
       }
@@ -108,26 +124,31 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
       *reinterpret_cast<float4*>(&sm.v[r][d]) = v;
     }
     __syncthreads();
-    float s[RM][4] = {};
+    float2 s2[RM][4] = {};                         // sums over the even and the odd dimensions
+#pragma unroll 4
     for (int d = 0; d < D; d += 4) {
-      float4 q[RM];
+      float4 k[4];
 #pragma unroll
-      for (int i = 0; i < RM; ++i) q[i] = *reinterpret_cast<const float4*>(&sm.q[ty * RM + i][d]);
+      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float4 k = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+      for (int i = 0; i < RM; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(&sm.q[ty * RM + i][d]);
 #pragma unroll
-        for (int i = 0; i < RM; ++i) s[i][j] = dot4(q[i], k, s[i][j]);
+        for (int j = 0; j < 4; ++j) {
+          s2[i][j] = fma_pair(make_float2(q.x, q.y), make_float2(k[j].x, k[j].y), s2[i][j]);
+          s2[i][j] = fma_pair(make_float2(q.z, q.w), make_float2(k[j].z, k[j].w), s2[i][j]);
+        }
       }
     }
 #pragma unroll
     for (int i = 0; i < RM; ++i) {
-      float top = -INFINITY;
+      float s[4], top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int key = k0 + tx + 16 * j;
-        s[i][j] = key >= max(seen[i].lo, all.lo) && key < min(seen[i].hi, all.hi) ? s[i][j] * a.scale_log2 : -INFINITY;
-        top = fmaxf(top, s[i][j]);
+        s[j] = (s2[i][j].x + s2[i][j].y) * a.scale_log2;
+        if (!whole && (key < seen[i].lo || key >= seen[i].hi)) s[j] = -INFINITY;
+        top = fmaxf(top, s[j]);
       }
 #pragma unroll
       for (int w = 8; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
@@ -137,54 +158,78 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
       float add = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p = exp2f(s[i][j] - base);
+        const float p = exp2f(s[j] - base);
         add += p;
         sm.p[ty * RM + i][tx + 16 * j] = p;
       }
+      sum[i] = sum[i] * keep + add;                // this thread's keys; joined at the end
 #pragma unroll
-      for (int w = 8; w > 0; w >>= 1) add += __shfl_xor_sync(0xffffffffu, add, w);
-      sum[i] = sum[i] * keep + add;
+      for (int c = 0; c < DC; ++c)
 #pragma unroll
-      for (int c = 0; c < DC; ++c) o[i][c] *= keep;
+        for (int h = 0; h < 2; ++h) o[i][c][h] = make_float2(o[i][c][h].x * keep, o[i][c][h].y * keep);
     }
     __syncwarp();               // a row's weights come from its own half warp
-    for (int j = 0; j < BN; ++j) {
+    if (whole) {
+#pragma unroll 2
+      for (int j = 0; j < BN; j += 4) {
+        float4 v[4][DC];
 #pragma unroll
-      for (int i = 0; i < RM; ++i) {
-        const float p = sm.p[ty * RM + i][j];
-        // a key that the row does not see adds nothing, whatever its value holds
-        if (p != 0.f) {
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int c = 0; c < DC; ++c) o[i][c] = fmaf(p, sm.v[j][tx + 16 * c], o[i][c]);
+          for (int c = 0; c < DC; ++c) v[e][c] = *reinterpret_cast<const float4*>(&sm.v[j + e][4 * tx + 64 * c]);
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+          const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[ty * RM + i][j]);
+          const float p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int c = 0; c < DC; ++c) {
+              o[i][c][0] = fma_pair(make_float2(p[e], p[e]), make_float2(v[e][c].x, v[e][c].y), o[i][c][0]);
+              o[i][c][1] = fma_pair(make_float2(p[e], p[e]), make_float2(v[e][c].z, v[e][c].w), o[i][c][1]);
+            }
         }
       }
+    } else {
+      // some row does not see the whole block: what it does not see adds nothing, whatever it holds
+      for (int j = 0; j < BN; ++j)
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+          const float p = sm.p[ty * RM + i][j];
+          if (p != 0.f)
+#pragma unroll
+            for (int c = 0; c < DC; ++c) {
+              const float4 v = *reinterpret_cast<const float4*>(&sm.v[j][4 * tx + 64 * c]);
+              o[i][c][0] = fma_pair(make_float2(p, p), make_float2(v.x, v.y), o[i][c][0]);
+              o[i][c][1] = fma_pair(make_float2(p, p), make_float2(v.z, v.w), o[i][c][1]);
+            }
+        }
     }
     __syncwarp();
   }
 #pragma unroll
   for (int i = 0; i < RM; ++i) {
+#pragma unroll
+    for (int w = 8; w > 0; w >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], w);
     const int R = r0 + ty * RM + i;
     if (R >= rows) continue;
     const int row = t.first + R / a.group, head = t.kv_head * a.group + R % a.group;
-    if (a.splits == 1) {
-      const float f = sum[i] == 0.f ? 0.f : 1.f / sum[i];
-      float* dst = static_cast<float*>(a.out) + row * a.ldo + (long long)head * D;
+    const float f = a.splits > 1 ? 1.f : sum[i] == 0.f ? 0.f : 1.f / sum[i];
+    const long long at = part_index(a, t.split, row, head);
+    float* dst = a.splits > 1 ? a.part + at * D : static_cast<float*>(a.out) + row * a.ldo + (long long)head * D;
 #pragma unroll
-      for (int c = 0; c < DC; ++c) dst[tx + 16 * c] = o[i][c] * f;
-    } else {
-      const long long at = part_index(a, t.split, row, head);
-#pragma unroll
-      for (int c = 0; c < DC; ++c) a.part[at * D + tx + 16 * c] = o[i][c];
-      if (tx == 0) a.ml[at] = make_float2(mx[i], sum[i]);
-    }
+    for (int c = 0; c < DC; ++c)
+      *reinterpret_cast<float4*>(dst + 4 * tx + 64 * c) =
+          make_float4(o[i][c][0].x * f, o[i][c][0].y * f, o[i][c][1].x * f, o[i][c][1].y * f);
+    if (a.splits > 1 && tx == 0) a.ml[at] = make_float2(mx[i], sum[i]);
   }
 }
 
 // joins the pieces: D / 4 lanes a (row, head), or several such groups that share its
 // pieces (groups > 1: few outputs of many pieces would else wait out one load after the other)
 template <typename T, int D>
-__global__ void __launch_bounds__(THREADS) join_kernel(const __grid_constant__ AttendArgs a, int groups) {
-  constexpr int LANES = D / 4, AT_ONCE = THREADS / LANES, BATCH = 4;
+__global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ AttendArgs a, int groups) {
+  constexpr int LANES = D / 4, AT_ONCE = JOIN_THREADS / LANES, BATCH = 4;
   __shared__ float4 os[AT_ONCE][LANES];
   __shared__ float2 mls[AT_ONCE];
   const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES, d = lane * 4, group = slot % groups;
@@ -239,23 +284,27 @@ cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-template <int D>
-cudaError_t launch_f32(const AttendArgs& a, bool wide, cudaStream_t st) {
+template <int D, int RM>
+cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
   const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
-  const bool e4m3 = a.m.format == EVO_CACHE_E4M3;
-  if (wide) return e4m3 ? launch_tiles<D, EVO_CACHE_E4M3, 4>(a, grid, st) : launch_tiles<D, EVO_CACHE_F32, 4>(a, grid, st);
-  return e4m3 ? launch_tiles<D, EVO_CACHE_E4M3, 1>(a, grid, st) : launch_tiles<D, EVO_CACHE_F32, 1>(a, grid, st);
+  return a.m.format == EVO_CACHE_E4M3 ? launch_tiles<D, EVO_CACHE_E4M3, RM>(a, grid, st)
+                                      : launch_tiles<D, EVO_CACHE_F32, RM>(a, grid, st);
+}
+
+template <int D>
+cudaError_t launch_f32(const AttendArgs& a, int tile_rows, cudaStream_t st) {
+  return tile_rows == 16 ? launch_f32<D, 2>(a, st) : tile_rows == 32 ? launch_f32<D, 4>(a, st) : launch_f32<D, 8>(a, st);
 }
 
 template <typename T, int D>
 cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
-  constexpr int AT_ONCE = THREADS / (D / 4);
+  constexpr int AT_ONCE = JOIN_THREADS / (D / 4);
   const long long outputs = (long long)a.rows * a.m.n_head;
   int groups = 1;                                  // 16 pieces a group, while the GPU has threads to spare
   while (groups < AT_ONCE && groups * 16 < a.splits && outputs * groups < 152 * 8 * AT_ONCE) groups *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = (unsigned)((outputs * groups + AT_ONCE - 1) / AT_ONCE);
-  cfg.blockDim = THREADS;
+  cfg.blockDim = JOIN_THREADS;
   cfg.stream = st;
   cudaLaunchAttribute at[1];                       // the launch overlaps the pieces' end; the kernel waits for it
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -273,11 +322,11 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   const bool f32 = m.dtype == EVO_DTYPE_F32;
   const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && all > 32;
   p.kernel = f32 ? ATTEND_F32 : tiles ? ATTEND_TILES : ATTEND_ROWS;
-  p.tile_rows = f32 ? (all <= 16 ? 16 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  p.tile_rows = f32 ? (all <= 16 ? 16 : all <= 32 ? 32 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   const long long most = std::max(1, max_len / (tiles ? 512 : f32 ? 64 : 256));
-  const long long target = f32 ? 304 : tiles ? 152 : blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
+  const long long target = f32 ? 152 * 4 : tiles ? 152 : blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
   p.splits = (int)std::max(1ll, std::min({most, tiles ? target / blocks : (target + blocks / 2) / blocks, 64ll}));
   p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
   return p;
@@ -291,7 +340,7 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
   const bool d64 = a.m.head_dim == 64;
   cudaError_t e = cudaSuccess;
   if (p.kernel == ATTEND_F32)
-    e = d64 ? launch_f32<64>(a, p.tile_rows == 64, st) : launch_f32<128>(a, p.tile_rows == 64, st);
+    e = d64 ? launch_f32<64>(a, p.tile_rows, st) : launch_f32<128>(a, p.tile_rows, st);
   else if (p.kernel == ATTEND_ROWS)
     e = launch_attend_rows(a, p.tile_rows, st);
   else

@@ -65,7 +65,7 @@ evo_status cache_args(int32_t U, int32_t N, int32_t H, int32_t E, const float* x
   if (*per > (1ll << 33) || (N > 0 && *per > (1ll << 33) / N) || N * (*per / 8) > INT_MAX - 1024) return EVO_ERR_SHAPE;
   if (N == 0 || H == 0) return EVO_OK;
   if ((U > 0 && (!codes || !scales)) || (x == nullptr) != (y == nullptr)) return EVO_ERR_ARG;
-  if (!aligned(codes, 8) || !aligned(x, 16) || !aligned(y, 16)) return EVO_ERR_ARG;
+  if (!aligned(codes, 16) || !aligned(x, 16) || !aligned(y, 16)) return EVO_ERR_ARG;
   if (x && x != y && overlap(x, y, (size_t)N * *per * sizeof(float))) return EVO_ERR_ARG;
   return EVO_OK;
 }
