@@ -27,26 +27,24 @@ namespace {
 
 constexpr int BN = 64, THREADS = 128, JOIN_THREADS = 256;
 
-template <int D, int RM>
+template <int D, int RM, int NBUF>
 struct Smem {
   static constexpr int BM = 8 * RM;
   float q[BM][D];
-  float k[BN][D + 4];           // rows 4 banks apart: 8 rows' float4 in a phase do not collide
-  float v[BN][D];
+  float k[NBUF][BN][D + 4];     // rows 4 banks apart: 8 rows' float4 in a phase do not collide
+  float v[NBUF][BN][D];
   float p[BM][BN + 4];
 };
 
-// 4 values of a key's or value's row in the memory's format
-template <int FORMAT>
-__device__ __forceinline__ float4 memory4(const void* pages, const uint8_t* scales, long long at, int D, int d) {
-  if constexpr (FORMAT == EVO_CACHE_E4M3) {
-    const float4 c = codes4(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(pages) + at * D + d));
-    const float f = scale_value(scales[at]);
-    return make_float4(c.x * f, c.y * f, c.z * f, c.w * f);
-  } else {
-    return *reinterpret_cast<const float4*>(static_cast<const float*>(pages) + at * D + d);
-  }
+__device__ __forceinline__ void copy16(float* dst, const float* src, bool on) {   // zeros where it is off
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+               "r"(on ? 16 : 0)
+               : "memory");
 }
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+template <int FORMAT, int RM>
+constexpr int BUFFERS = FORMAT != EVO_CACHE_E4M3 && RM <= 2 ? 2 : 1;
 
 // exact products and sums of pairs, subnormals kept
 __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
@@ -72,8 +70,14 @@ __device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 m
 
 template <int D, int FORMAT, int RM>
 __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
+  // few rows: the next 64 keys and values are on their way while these are used, fp32 pages by
+  // asynchronous copies to a second buffer, codes in registers.  Many rows: the products take
+  // longer than the loads, which the SM's other blocks hide
+  constexpr bool CODES = FORMAT == EVO_CACHE_E4M3, AHEAD = RM <= 2;
+  constexpr int NBUF = BUFFERS<FORMAT, RM>;
   extern __shared__ __align__(16) uint8_t raw[];
-  Smem<D, RM>& sm = *reinterpret_cast<Smem<D, RM>*>(raw);
+  using S = Smem<D, RM, NBUF>;
+  S& sm = *reinterpret_cast<S*>(raw);
   constexpr int BM = 8 * RM, DC = D / 64;          // a thread's columns: 4 tx + 64 c .. + 3
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
   const Tile t = tile_of_block(a);
@@ -106,30 +110,79 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
 #pragma unroll
     for (int c = 0; c < DC; ++c) o[i][c][0] = o[i][c][1] = make_float2(0.f, 0.f);
   }
-  for (int k0 = all.lo / BN * BN; k0 < all.hi; k0 += BN) {
-    const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
-    __syncthreads();
-#pragma unroll 4
-    for (int i = tid; i < BN * D / 4; i += THREADS) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4, key = k0 + r;
-      float4 k = {}, v = {};
-      if (key >= all.lo && key < all.hi) {
-        const int page = seq_page(a.m, t.n, key >> shift);
-        const long long at =
-            ((long long)page * a.m.n_kv_head + t.kv_head) * a.m.page_tokens + (key & (a.m.page_tokens - 1));
-        k = memory4<FORMAT>(a.m.k_pages, a.m.k_scales, at, D, d);
-        v = memory4<FORMAT>(a.m.v_pages, a.m.v_scales, at, D, d);
+  // row of the pool that holds a key, or -1 outside the piece
+  const auto row_of = [&](int key) -> long long {
+    if (key < all.lo || key >= all.hi) return -1;
+    return ((long long)seq_page(a.m, t.n, key >> shift) * a.m.n_kv_head + t.kv_head) * a.m.page_tokens +
+           (key & (a.m.page_tokens - 1));
+  };
+  constexpr int CV = CODES ? BN * D / 16 / THREADS : 1;      // 16-code vectors a thread brings, keys and values each
+  uint4 kc[CV], vc[CV];
+  uint32_t kscale[CV], vscale[CV];
+  const auto bring = [&](int k0, int buf) {
+    if constexpr (CODES) {
+#pragma unroll
+      for (int i = 0; i < CV; ++i) {
+        const int v = tid + i * THREADS, r = v / (D / 16), d = v % (D / 16) * 16;
+        const long long at = row_of(k0 + r);
+        kc[i] = vc[i] = make_uint4(0, 0, 0, 0);
+        kscale[i] = vscale[i] = 1;
+        if (at >= 0) {
+          kc[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.m.k_pages) + at * D + d);
+          vc[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.m.v_pages) + at * D + d);
+          kscale[i] = a.m.k_scales[at];
+          vscale[i] = a.m.v_scales[at];
+        }
       }
-      *reinterpret_cast<float4*>(&sm.k[r][d]) = k;
-      *reinterpret_cast<float4*>(&sm.v[r][d]) = v;
+    } else {
+#pragma unroll 4
+      for (int i = tid; i < BN * D / 4; i += THREADS) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        const long long at = row_of(k0 + r);
+        copy16(&sm.k[buf][r][d], static_cast<const float*>(a.m.k_pages) + max(at, 0ll) * D + d, at >= 0);
+        copy16(&sm.v[buf][r][d], static_cast<const float*>(a.m.v_pages) + max(at, 0ll) * D + d, at >= 0);
+      }
     }
-    __syncthreads();
+  };
+  const auto unpack = [&] {                        // the codes in registers to shared memory
+    if constexpr (CODES) {
+#pragma unroll
+      for (int i = 0; i < CV; ++i) {
+        const int v = tid + i * THREADS, r = v / (D / 16), d = v % (D / 16) * 16;
+        const float kf = scale_value(kscale[i]), vf = scale_value(vscale[i]);
+        const uint32_t kw[4] = {kc[i].x, kc[i].y, kc[i].z, kc[i].w}, vw[4] = {vc[i].x, vc[i].y, vc[i].z, vc[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 k = codes4(kw[e]), x = codes4(vw[e]);
+          *reinterpret_cast<float4*>(&sm.k[0][r][d + 4 * e]) = make_float4(k.x * kf, k.y * kf, k.z * kf, k.w * kf);
+          *reinterpret_cast<float4*>(&sm.v[0][r][d + 4 * e]) = make_float4(x.x * vf, x.y * vf, x.z * vf, x.w * vf);
+        }
+      }
+    }
+  };
+  int buf = 0;
+  const int start = all.lo / BN * BN;
+  if (AHEAD && start < all.hi) bring(start, 0);
+  for (int k0 = start; k0 < all.hi; k0 += BN, buf = NBUF == 2 ? buf ^ 1 : 0) {
+    const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
+    if constexpr (NBUF == 2) {
+      copies_done();
+      __syncthreads();                             // this buffer is there, the other one is free
+      if (k0 + BN < all.hi) bring(k0 + BN, buf ^ 1);
+    } else {
+      __syncthreads();
+      if (!AHEAD) bring(k0, 0);
+      if constexpr (CODES) unpack();
+      else copies_done();
+      __syncthreads();
+      if (AHEAD && k0 + BN < all.hi) bring(k0 + BN, 0);
+    }
     float2 s2[RM][4] = {};                         // sums over the even and the odd dimensions
 #pragma unroll 4
     for (int d = 0; d < D; d += 4) {
       float4 k[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[buf][tx + 16 * j][d]);
 #pragma unroll
       for (int i = 0; i < RM; ++i) {
         const float4 q = *reinterpret_cast<const float4*>(&sm.q[ty * RM + i][d]);
@@ -176,7 +229,7 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int c = 0; c < DC; ++c) v[e][c] = *reinterpret_cast<const float4*>(&sm.v[j + e][4 * tx + 64 * c]);
+          for (int c = 0; c < DC; ++c) v[e][c] = *reinterpret_cast<const float4*>(&sm.v[buf][j + e][4 * tx + 64 * c]);
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
           const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[ty * RM + i][j]);
@@ -199,7 +252,7 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
           if (p != 0.f)
 #pragma unroll
             for (int c = 0; c < DC; ++c) {
-              const float4 v = *reinterpret_cast<const float4*>(&sm.v[j][4 * tx + 64 * c]);
+              const float4 v = *reinterpret_cast<const float4*>(&sm.v[buf][j][4 * tx + 64 * c]);
               o[i][c][0] = fma_pair(make_float2(p, p), make_float2(v.x, v.y), o[i][c][0]);
               o[i][c][1] = fma_pair(make_float2(p, p), make_float2(v.z, v.w), o[i][c][1]);
             }
@@ -278,9 +331,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
 template <int D, int FORMAT, int RM>
 cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
   const auto k = attend_kernel<D, FORMAT, RM>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Smem<D, RM>));
+  constexpr int smem = (int)sizeof(Smem<D, RM, BUFFERS<FORMAT, RM>>);
+  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  k<<<grid, THREADS, sizeof(Smem<D, RM>), st>>>(a);
+  k<<<grid, THREADS, smem, st>>>(a);
   return cudaGetLastError();
 }
 
@@ -293,7 +347,7 @@ cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
 
 template <int D>
 cudaError_t launch_f32(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  return tile_rows == 16 ? launch_f32<D, 2>(a, st) : tile_rows == 32 ? launch_f32<D, 4>(a, st) : launch_f32<D, 8>(a, st);
+  return tile_rows == 8 ? launch_f32<D, 1>(a, st) : tile_rows == 16 ? launch_f32<D, 2>(a, st) : tile_rows == 32 ? launch_f32<D, 4>(a, st) : launch_f32<D, 8>(a, st);
 }
 
 template <typename T, int D>
@@ -322,7 +376,7 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   const bool f32 = m.dtype == EVO_DTYPE_F32;
   const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && all > 32;
   p.kernel = f32 ? ATTEND_F32 : tiles ? ATTEND_TILES : ATTEND_ROWS;
-  p.tile_rows = f32 ? (all <= 16 ? 16 : all <= 32 ? 32 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  p.tile_rows = f32 ? (all <= 8 ? 8 : all <= 16 ? 16 : all <= 32 ? 32 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   const long long most = std::max(1, max_len / (tiles ? 512 : f32 ? 64 : 256));
