@@ -27,12 +27,12 @@ namespace {
 
 constexpr int BN = 64, THREADS = 128, JOIN_THREADS = 256;
 
-template <int D, int RM, int NBUF>
+template <int D, int RM>
 struct Smem {
   static constexpr int BM = 8 * RM;
   float q[BM][D];
-  float k[NBUF][BN][D + 4];     // rows 4 banks apart: 8 rows' float4 in a phase do not collide
-  float v[NBUF][BN][D];
+  float k[BN][D + 4];           // rows 4 banks apart: 8 rows' float4 in a phase do not collide
+  float v[BN][D];
   float p[BM][BN + 4];
 };
 
@@ -42,9 +42,6 @@ __device__ __forceinline__ void copy16(float* dst, const float* src, bool on) { 
                : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-template <int FORMAT, int RM>
-constexpr int BUFFERS = FORMAT != EVO_CACHE_E4M3 && RM <= 2 ? 2 : 1;
 
 // exact products and sums of pairs, subnormals kept
 __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
@@ -69,14 +66,10 @@ __device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 m
 }
 
 template <int D, int FORMAT, int RM>
-__global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__ AttendArgs a) {
-  // few rows: the next 64 keys and values are on their way while these are used, fp32 pages by
-  // asynchronous copies to a second buffer, codes in registers.  Many rows: the products take
-  // longer than the loads, which the SM's other blocks hide
-  constexpr bool CODES = FORMAT == EVO_CACHE_E4M3, AHEAD = RM <= 2;
-  constexpr int NBUF = BUFFERS<FORMAT, RM>;
+__global__ void __launch_bounds__(THREADS, D == 64 ? 3 : 2) attend_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr bool CODES = FORMAT == EVO_CACHE_E4M3;
   extern __shared__ __align__(16) uint8_t raw[];
-  using S = Smem<D, RM, NBUF>;
+  using S = Smem<D, RM>;
   S& sm = *reinterpret_cast<S*>(raw);
   constexpr int BM = 8 * RM, DC = D / 64;          // a thread's columns: 4 tx + 64 c .. + 3
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
@@ -119,7 +112,7 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
   constexpr int CV = CODES ? BN * D / 16 / THREADS : 1;      // 16-code vectors a thread brings, keys and values each
   uint4 kc[CV], vc[CV];
   uint32_t kscale[CV], vscale[CV];
-  const auto bring = [&](int k0, int buf) {
+  const auto bring = [&](int k0) {
     if constexpr (CODES) {
 #pragma unroll
       for (int i = 0; i < CV; ++i) {
@@ -139,8 +132,8 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
       for (int i = tid; i < BN * D / 4; i += THREADS) {
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         const long long at = row_of(k0 + r);
-        copy16(&sm.k[buf][r][d], static_cast<const float*>(a.m.k_pages) + max(at, 0ll) * D + d, at >= 0);
-        copy16(&sm.v[buf][r][d], static_cast<const float*>(a.m.v_pages) + max(at, 0ll) * D + d, at >= 0);
+        copy16(&sm.k[r][d], static_cast<const float*>(a.m.k_pages) + max(at, 0ll) * D + d, at >= 0);
+        copy16(&sm.v[r][d], static_cast<const float*>(a.m.v_pages) + max(at, 0ll) * D + d, at >= 0);
       }
     }
   };
@@ -154,35 +147,25 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float4 k = codes4(kw[e]), x = codes4(vw[e]);
-          *reinterpret_cast<float4*>(&sm.k[0][r][d + 4 * e]) = make_float4(k.x * kf, k.y * kf, k.z * kf, k.w * kf);
-          *reinterpret_cast<float4*>(&sm.v[0][r][d + 4 * e]) = make_float4(x.x * vf, x.y * vf, x.z * vf, x.w * vf);
+          *reinterpret_cast<float4*>(&sm.k[r][d + 4 * e]) = make_float4(k.x * kf, k.y * kf, k.z * kf, k.w * kf);
+          *reinterpret_cast<float4*>(&sm.v[r][d + 4 * e]) = make_float4(x.x * vf, x.y * vf, x.z * vf, x.w * vf);
         }
       }
     }
   };
-  int buf = 0;
-  const int start = all.lo / BN * BN;
-  if (AHEAD && start < all.hi) bring(start, 0);
-  for (int k0 = start; k0 < all.hi; k0 += BN, buf = NBUF == 2 ? buf ^ 1 : 0) {
+  for (int k0 = all.lo / BN * BN; k0 < all.hi; k0 += BN) {
     const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
-    if constexpr (NBUF == 2) {
-      copies_done();
-      __syncthreads();                             // this buffer is there, the other one is free
-      if (k0 + BN < all.hi) bring(k0 + BN, buf ^ 1);
-    } else {
-      __syncthreads();
-      if (!AHEAD) bring(k0, 0);
-      if constexpr (CODES) unpack();
-      else copies_done();
-      __syncthreads();
-      if (AHEAD && k0 + BN < all.hi) bring(k0 + BN, 0);
-    }
+    __syncthreads();
+    bring(k0);
+    if constexpr (CODES) unpack();
+    else copies_done();
+    __syncthreads();
     float2 s2[RM][4] = {};                         // sums over the even and the odd dimensions
 #pragma unroll 4
     for (int d = 0; d < D; d += 4) {
       float4 k[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[buf][tx + 16 * j][d]);
+      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
 #pragma unroll
       for (int i = 0; i < RM; ++i) {
         const float4 q = *reinterpret_cast<const float4*>(&sm.q[ty * RM + i][d]);
@@ -229,7 +212,7 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int c = 0; c < DC; ++c) v[e][c] = *reinterpret_cast<const float4*>(&sm.v[buf][j + e][4 * tx + 64 * c]);
+          for (int c = 0; c < DC; ++c) v[e][c] = *reinterpret_cast<const float4*>(&sm.v[j + e][4 * tx + 64 * c]);
 #pragma unroll
         for (int i = 0; i < RM; ++i) {
           const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[ty * RM + i][j]);
@@ -252,7 +235,7 @@ __global__ void __launch_bounds__(THREADS) attend_kernel(const __grid_constant__
           if (p != 0.f)
 #pragma unroll
             for (int c = 0; c < DC; ++c) {
-              const float4 v = *reinterpret_cast<const float4*>(&sm.v[buf][j][4 * tx + 64 * c]);
+              const float4 v = *reinterpret_cast<const float4*>(&sm.v[j][4 * tx + 64 * c]);
               o[i][c][0] = fma_pair(make_float2(p, p), make_float2(v.x, v.y), o[i][c][0]);
               o[i][c][1] = fma_pair(make_float2(p, p), make_float2(v.z, v.w), o[i][c][1]);
             }
@@ -331,7 +314,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
 template <int D, int FORMAT, int RM>
 cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
   const auto k = attend_kernel<D, FORMAT, RM>;
-  constexpr int smem = (int)sizeof(Smem<D, RM, BUFFERS<FORMAT, RM>>);
+  constexpr int smem = (int)sizeof(Smem<D, RM>);
   const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   k<<<grid, THREADS, smem, st>>>(a);
@@ -343,11 +326,6 @@ cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
   const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
   return a.m.format == EVO_CACHE_E4M3 ? launch_tiles<D, EVO_CACHE_E4M3, RM>(a, grid, st)
                                       : launch_tiles<D, EVO_CACHE_F32, RM>(a, grid, st);
-}
-
-template <int D>
-cudaError_t launch_f32(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  return tile_rows == 8 ? launch_f32<D, 1>(a, st) : tile_rows == 16 ? launch_f32<D, 2>(a, st) : tile_rows == 32 ? launch_f32<D, 4>(a, st) : launch_f32<D, 8>(a, st);
 }
 
 template <typename T, int D>
@@ -375,8 +353,8 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
   const bool f32 = m.dtype == EVO_DTYPE_F32;
   const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && all > 32;
-  p.kernel = f32 ? ATTEND_F32 : tiles ? ATTEND_TILES : ATTEND_ROWS;
-  p.tile_rows = f32 ? (all <= 8 ? 8 : all <= 16 ? 16 : all <= 32 ? 32 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  p.kernel = f32 ? (all <= 16 ? ATTEND_F32_ROWS : ATTEND_F32) : tiles ? ATTEND_TILES : ATTEND_ROWS;
+  p.tile_rows = f32 ? (all == 1 ? 1 : all <= 4 ? 4 : all <= 16 ? 16 : all <= 32 || m.head_dim == 128 ? 32 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   const long long most = std::max(1, max_len / (tiles ? 512 : f32 ? 64 : 256));
@@ -394,7 +372,10 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
   const bool d64 = a.m.head_dim == 64;
   cudaError_t e = cudaSuccess;
   if (p.kernel == ATTEND_F32)
-    e = d64 ? launch_f32<64>(a, p.tile_rows, st) : launch_f32<128>(a, p.tile_rows, st);
+    e = p.tile_rows == 32 ? d64 ? launch_f32<64, 4>(a, st) : launch_f32<128, 4>(a, st)
+                          : d64 ? launch_f32<64, 8>(a, st) : launch_f32<128, 8>(a, st);
+  else if (p.kernel == ATTEND_F32_ROWS)
+    e = launch_attend_f32_rows(a, p.tile_rows, st);
   else if (p.kernel == ATTEND_ROWS)
     e = launch_attend_rows(a, p.tile_rows, st);
   else

@@ -25,13 +25,16 @@ bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_
   }();
   if (!encode) return false;
   const bool codes = m.format == EVO_CACHE_E4M3;
-  const cuuint64_t row = (cuuint64_t)m.head_dim * (codes ? 1 : 2);
+  const cuuint32_t item = codes ? 1 : m.format == EVO_CACHE_BF16 ? 2 : 4;
+  const cuuint64_t row = (cuuint64_t)m.head_dim * item;
   const cuuint64_t dims[2] = {(cuuint64_t)m.head_dim, (cuuint64_t)m.n_pages * m.n_kv_head * m.page_tokens};
   const cuuint64_t strides[1] = {row};
   const cuuint32_t width = (cuuint32_t)(row < 128 ? row : 128);
-  const cuuint32_t box[2] = {codes ? width : width / 2, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-  return encode(map, codes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pages),
-                dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint32_t box[2] = {width / item, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  const CUtensorMapDataType type = codes       ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : item == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                               : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+  return encode(map, type, 2, const_cast<void*>(pages), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

@@ -48,7 +48,7 @@ struct AttendArgs {
   float2* ml;                     // [splits][rows][n_head]: its maximum (base 2) and sum
 };
 // which kernel takes a call, and how it is cut up
-enum AttendKernel { ATTEND_F32, ATTEND_ROWS, ATTEND_TILES };
+enum AttendKernel { ATTEND_F32, ATTEND_F32_ROWS, ATTEND_ROWS, ATTEND_TILES };
 struct AttendPlan {
   AttendKernel kernel;
   int tile_rows, tiles, splits;
@@ -56,6 +56,7 @@ struct AttendPlan {
 };
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len);
 cudaError_t launch_attend_rows(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_attend_rows.cu
+cudaError_t launch_attend_f32_rows(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_attend_f32.cu
 cudaError_t launch_attend_tiles(const AttendArgs& a, cudaStream_t st);                // evo_attend_tiles.cu
 cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st);
 
