@@ -53,9 +53,6 @@ __device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
   return d;
 }
 
-__device__ __forceinline__ void put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
 // (top, sum, o) joined with another piece's
 __device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 ml, float4 p) {
   const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
@@ -271,13 +268,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
   const int slot = threadIdx.x / LANES, lane = threadIdx.x % LANES, d = lane * 4, group = slot % groups;
   const long long i = (long long)blockIdx.x * (AT_ONCE / groups) + slot / groups;
   const int row = (int)(i / a.m.n_head), head = (int)(i % a.m.n_head);
+  const int parts = a.splits / a.cluster;
   tc::pdl_wait();
   bool on = row < a.rows;
   if (on && a.m.starts) on = row >= a.m.starts[0] && row < a.m.starts[a.m.n_seq];
   float top = -INFINITY, sum = 0.f;
   float4 o = {};
   if (on)
-    for (int s0 = group; s0 < a.splits; s0 += groups * BATCH) {
+    for (int s0 = group; s0 < parts; s0 += groups * BATCH) {
       float2 ml[BATCH];
       float4 p[BATCH];
 #pragma unroll
@@ -285,7 +283,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
         const int s = s0 + j * groups;
         ml[j] = make_float2(-INFINITY, 0.f);
         p[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (s < a.splits) {
+        if (s < parts) {
           const long long at = part_index(a, s, row, head);
           ml[j] = a.ml[at];
           p[j] = *reinterpret_cast<const float4*>(a.part + at * D + d);
@@ -303,12 +301,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
     on = on && group == 0;
   }
   if (!on) return;
-  const float f = sum == 0.f ? 0.f : 1.f / sum;
-  T* dst = static_cast<T*>(a.out) + row * a.ldo + (long long)head * D + d;
-  put(dst, o.x * f);
-  put(dst + 1, o.y * f);
-  put(dst + 2, o.z * f);
-  put(dst + 3, o.w * f);
+  store_out(static_cast<T*>(a.out) + row * a.ldo + (long long)head * D + d, o, sum == 0.f ? 0.f : 1.f / sum);
 }
 
 template <int D, int FORMAT, int RM>
@@ -333,7 +326,7 @@ cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   constexpr int AT_ONCE = JOIN_THREADS / (D / 4);
   const long long outputs = (long long)a.rows * a.m.n_head;
   int groups = 1;                                  // 16 pieces a group, while the GPU has threads to spare
-  while (groups < AT_ONCE && groups * 16 < a.splits && outputs * groups < 152 * 8 * AT_ONCE) groups *= 2;
+  while (groups < AT_ONCE && groups * 16 < a.splits / a.cluster && outputs * groups < 152 * 8 * AT_ONCE) groups *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = (unsigned)((outputs * groups + AT_ONCE - 1) / AT_ONCE);
   cfg.blockDim = JOIN_THREADS;
@@ -351,24 +344,44 @@ cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) {
   AttendPlan p;
   const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
-  const bool f32 = m.dtype == EVO_DTYPE_F32;
-  const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && all > 32;
-  p.kernel = f32 ? (all <= 16 ? ATTEND_F32_ROWS : ATTEND_F32) : tiles ? ATTEND_TILES : ATTEND_ROWS;
-  p.tile_rows = f32 ? (all == 1 ? 1 : all <= 4 ? 4 : all <= 16 ? 16 : all <= 32 || m.head_dim == 128 ? 32 : 64) : tiles ? 256 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  const bool f32 = m.dtype == EVO_DTYPE_F32, few = all <= (f32 ? 16 : 32);
+  const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && !few;
+  p.kernel = f32 ? (few ? ATTEND_F32_ROWS : ATTEND_F32) : tiles ? ATTEND_TILES : ATTEND_ROWS;
+  p.tile_rows = f32     ? (all == 1 ? 1 : all <= 4 || few && (long long)m.n_seq * m.n_kv_head < 152 ? 4 : few ? 16 : all <= 32 || m.head_dim == 128 ? 32 : 64)
+                : tiles ? 256
+                        : (all <= 8 ? 8 : all <= 16 ? 16 : 32);
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
-  const long long most = std::max(1, max_len / (tiles ? 512 : f32 ? 64 : 256));
-  const long long target = f32 ? 152 * 4 : tiles ? 152 : blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
-  p.splits = (int)std::max(1ll, std::min({most, tiles ? target / blocks : (target + blocks / 2) / blocks, 64ll}));
-  p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
+  p.cluster = 1;
+  if (p.kernel == ATTEND_ROWS || p.kernel == ATTEND_F32_ROWS) {
+    // Pieces: enough blocks to fill the GPU, and with plenty of work several waves of them, so
+    // that sequences of different lengths even out; tiles of 32 rows pay 10 us a wave of further
+    // blocks (32 rows of 64 sequences: 99 us in one piece, 104 in two).  Up to 8 pieces of few
+    // items are joined by a cluster, without a second kernel (3 x 16 rows over 333 fp32 keys: 8.3
+    // us against 10.3); more, or those of many items, by a kernel (a cluster's blocks wait for
+    // one another: 64 ragged sequences 147 us against 134).
+    const long long most = std::max(1, max_len / (f32 ? 64 : 128));
+    const long long target = blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
+    const long long want = std::max(1ll, std::min({most, (target + blocks / 2) / blocks, 64ll}));
+    p.cluster = blocks < 456 && want <= 8 ? (int)want : 1;
+    p.splits = (int)want;
+  } else {
+    const long long most = std::max(1, max_len / (tiles ? 512 : 64));
+    const long long target = tiles ? 152 : 152 * 4;
+    p.splits = (int)std::max(1ll, std::min({most, target / blocks, 64ll}));
+  }
+  const int parts = p.splits / p.cluster;
+  p.scratch = parts == 1 ? 0 : (size_t)parts * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
   return p;
 }
 
 cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st) {
   a.tiles = p.tiles;
   a.splits = p.splits;
+  a.cluster = p.cluster;
+  const int parts = p.splits / p.cluster;
   a.part = static_cast<float*>(scratch);
-  a.ml = reinterpret_cast<float2*>(a.part + (size_t)p.splits * a.rows * a.m.n_head * a.m.head_dim);
+  a.ml = reinterpret_cast<float2*>(a.part + (size_t)parts * a.rows * a.m.n_head * a.m.head_dim);
   const bool d64 = a.m.head_dim == 64;
   cudaError_t e = cudaSuccess;
   if (p.kernel == ATTEND_F32)
@@ -380,7 +393,7 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
     e = launch_attend_rows(a, p.tile_rows, st);
   else
     e = launch_attend_tiles(a, st);
-  if (e != cudaSuccess || a.splits == 1) return e;
+  if (e != cudaSuccess || parts == 1) return e;
   if (a.m.dtype == EVO_DTYPE_F32) return d64 ? launch_join<float, 64>(a, st) : launch_join<float, 128>(a, st);
   return d64 ? launch_join<__nv_bfloat16, 64>(a, st) : launch_join<__nv_bfloat16, 128>(a, st);
 }

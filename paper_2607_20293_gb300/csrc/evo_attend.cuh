@@ -7,6 +7,8 @@
 // piece of the keys that any of them sees.
 #pragma once
 
+#include <cuda_bf16.h>
+
 #include "evo_memory.h"
 
 namespace evo {
@@ -55,9 +57,99 @@ __device__ __forceinline__ Range piece_of(const AttendArgs& a, const Tile& t, Ra
   return {max(r.lo, (lo + t.split * each) * step), min(r.hi, (lo + (t.split + 1) * each) * step)};
 }
 
-// index of (row of the call, query head) in the partial results of a piece
-__device__ __forceinline__ long long part_index(const AttendArgs& a, int split, int row, int head) {
-  return ((long long)split * a.rows + row) * a.m.n_head + head;
+// index of (row of the call, query head) in the partial results of a cluster's pieces
+__device__ __forceinline__ long long part_index(const AttendArgs& a, int part, int row, int head) {
+  return ((long long)part * a.rows + row) * a.m.n_head + head;
+}
+
+__device__ __forceinline__ void cluster_arrive_wait() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of this block's shared memory at p in the block of another rank of the cluster
+__device__ __forceinline__ uint32_t in_rank(const void* p, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float2 remote_f2(uint32_t p) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(p));
+  return v;
+}
+__device__ __forceinline__ float4 remote_f4(uint32_t p) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(p));
+  return v;
+}
+
+__device__ __forceinline__ void store_out(float* p, float4 v, float f) {
+  *reinterpret_cast<float4*>(p) = make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+}
+__device__ __forceinline__ void store_out(__nv_bfloat16* p, float4 v, float f) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x * f, v.y * f), b = __floats2bfloat162_rn(v.z * f, v.w * f);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// The end of a block of few rows: 4 values d .. d + 3 of the sums of row R of the tile, its maximum
+// m and sum l go to the output, or to the partial results where a join kernel follows.
+template <typename T, int D>
+__device__ __forceinline__ void put_result(const AttendArgs& a, const Tile& t, int R, int d, float4 x, float m, float l) {
+  const int row = t.first + R / a.group, head = t.kv_head * a.group + R % a.group;
+  if (a.splits == a.cluster) {
+    store_out(static_cast<T*>(a.out) + row * a.ldo + (long long)head * D + d, x, l == 0.f ? 0.f : 1.f / l);
+  } else {
+    const long long at = part_index(a, t.split / a.cluster, row, head);
+    *reinterpret_cast<float4*>(a.part + at * D + d) = x;
+    if (d == 0) a.ml[at] = make_float2(m, l);
+  }
+}
+
+// Joins the pieces of a cluster's blocks through their shared memory: `sums` [ROWS][ld] and `ml`
+// [ROWS] hold each block's; every block finishes its share of the values.  All threads of all
+// blocks of the cluster call it.
+template <typename T, int D, int ROWS, int THREADS>
+__device__ __forceinline__ void join_cluster(const AttendArgs& a, const Tile& t, const float* sums, int ld, const float2* ml, int r0,
+                                             int rows) {
+  cluster_arrive_wait();
+  const int rank = t.split % a.cluster;
+  for (int i = rank * THREADS + threadIdx.x; i < ROWS * D / 4; i += a.cluster * THREADS) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4, R = r0 + r;
+    if (R >= rows) break;
+    float m = -INFINITY, l = 0.f;
+    for (int c = 0; c < a.cluster; ++c) m = fmaxf(m, remote_f2(in_rank(ml + r, c)).x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float4 x = {};
+#pragma unroll 4
+    for (int c = 0; c < a.cluster; ++c) {
+      const float2 o = remote_f2(in_rank(ml + r, c));
+      const float4 y = remote_f4(in_rank(sums + r * ld + d, c));
+      const float f = exp2f(o.x - ref);
+      l = fmaf(o.y, f, l);
+      x = make_float4(fmaf(y.x, f, x.x), fmaf(y.y, f, x.y), fmaf(y.z, f, x.z), fmaf(y.w, f, x.w));
+    }
+    put_result<T, D>(a, t, R, d, x, m, l);
+  }
+  cluster_arrive_wait();                           // no block ends while another reads its shared memory
+}
+
+// launches a block a piece, the pieces of a cluster as one
+template <typename... K, typename... A>
+cudaError_t launch_pieces(void (*kernel)(K...), const AttendArgs& a, int threads, int smem, cudaStream_t st, const A&... args) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess && a.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
+  cfg.blockDim = threads;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = a.cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = a.cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, a, args...);
 }
 
 }  // namespace evo

@@ -121,6 +121,7 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t full[WARPS][STAGES];
   __shared__ float2 stat[WARPS][R];                // the warps' maxima and sums
+  __shared__ float2 block_ml[R];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   const uint32_t ring = tc::su32(mem) + warp * C::RING, psm = tc::su32(mem) + WARPS * C::RING + warp * C::P;
@@ -299,7 +300,6 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
     if (tid == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
     const long long t0 = clock64();
     while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);   // those in flight land before the block ends
-    return;
   }
   // the warps' sums, each in its own part of the ring
   float* const mine = reinterpret_cast<float*>(mem + warp * C::RING);
@@ -329,27 +329,23 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
       l = fmaf(ml.y, f, l);
       x = make_float4(fmaf(y.x, f, x.x), fmaf(y.y, f, x.y), fmaf(y.z, f, x.z), fmaf(y.w, f, x.w));
     }
-    const int row = t.first + q / a.group, head = t.kv_head * a.group + q % a.group;
-    const float f = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-    const long long at = part_index(a, t.split, row, head);
-    float* dst = a.splits > 1 ? a.part + at * D : static_cast<float*>(a.out) + row * a.ldo + (long long)head * D;
-    *reinterpret_cast<float4*>(dst + d) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
-    if (a.splits > 1 && d == 0) a.ml[at] = make_float2(m, l);
+    if (a.cluster == 1) {
+      put_result<float, D>(a, t, q, d, x, m, l);
+    } else {                                       // in place of the first warp's
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(mem) + r * D + d) = x;
+      if (d == 0) block_ml[r] = make_float2(m, l);
+    }
   }
+  if (a.cluster > 1) join_cluster<float, D, R, THREADS>(a, t, reinterpret_cast<const float*>(mem), D, block_ml, r0, rows);
 }
 
 template <int D, bool E4M3, int R>
 cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
   using C = Cfg<D, E4M3, R>;
-  const auto k = f32_rows_kernel<D, E4M3, R>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-  if (e != cudaSuccess) return e;
   CUtensorMap km, vm;
   const int box = std::min(a.m.page_tokens, RUN);
   if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
-  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
-  k<<<grid, C::THREADS, C::SMEM, st>>>(a, km, vm);
-  return cudaGetLastError();
+  return launch_pieces(f32_rows_kernel<D, E4M3, R>, a, C::THREADS, C::SMEM, st, km, vm);
 }
 
 template <int R>

@@ -56,6 +56,7 @@ namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
+constexpr float SLACK = 7.f;                       // and, with its value's scale, pass the row's reference for those: 2^15 in all
 constexpr float NO_NUMBER = __builtin_nanf("");
 
 template <int D, bool E4M3, int NR>
@@ -71,7 +72,8 @@ struct Cfg {
   static constexpr int STAGES = STAGE > 4096 ? 3 : 4;
   static constexpr int JOIN = 8 * NR * (D + 4) * 4;
   static constexpr int RING = (STAGES * STAGE > JOIN ? STAGES * STAGE : JOIN + 1023) / 1024 * 1024;   // a warp's bytes
-  static constexpr bool QS = NR == 4 && D == 128;  // queries stay in shared memory: their fragments take 64 registers
+  static constexpr bool QS = NR == 4;              // queries stay in shared memory: their fragments take 32 or 64 registers
+  static constexpr int BLOCKS = NR == 4 ? (D == 64 ? 3 : 2) : 1;   // blocks a SM that the registers leave room for
   static constexpr int QB = QS ? NR * (D / 16) * 256 : 0;
   static constexpr int SCALES = E4M3 ? WARPS * STAGES * 2 * RUN : 0;
   static constexpr int SMEM = 1024 + WARPS * RING + QB + SCALES;
@@ -162,7 +164,7 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w, bool* bad) {
 }
 
 template <int D, bool E4M3, int NR>
-__global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ AttendArgs a,
+__global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel(const __grid_constant__ AttendArgs a,
                                                        const __grid_constant__ CUtensorMap kmap,
                                                        const __grid_constant__ CUtensorMap vmap) {
   using C = Cfg<D, E4M3, NR>;
@@ -171,6 +173,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
   __shared__ __align__(8) uint64_t full[WARPS][STAGES];
   __shared__ float2 stat[WARPS][ROWS];                       // the warps' maxima and sums
   __shared__ float vmax[E4M3 ? WARPS : 1][ROWS];
+  __shared__ float2 block_ml[ROWS];
   __shared__ int poison;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
@@ -237,7 +240,12 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
     for (int i = 0; i < D / 32; ++i)
       u[i] = R < rows ? *reinterpret_cast<const uint4*>(src + (E4M3 ? 64 * (i / 2) + 16 * c + 8 * (i % 2) : 32 * i + 8 * c))
                       : make_uint4(0, 0, 0, 0);
-    float f = a.scale_log2;
+    // the softmax works with a positive factor: the scale's sign goes to the queries
+    float f = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u, keep = a.scale_log2 == 0.f ? 0u : ~0u;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      u[i] = make_uint4((u[i].x ^ flip) & keep, (u[i].y ^ flip) & keep, (u[i].z ^ flip) & keep, (u[i].w ^ flip) & keep);
     if constexpr (E4M3) {
       uint32_t top = 0;
 #pragma unroll
@@ -261,6 +269,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
           w[j] = pack(__uint_as_float(w[j] << 16) * s2, __uint_as_float(w[j] & 0xffff0000u) * s2, true);
       }
     }
+    f = fmaxf(f, 1.1754944e-38f);                            // (a factor that is flushed to zero would make a masked score none)
     rf[nr][0] = __shfl_sync(0xffffffffu, f, 8 * c);
     rf[nr][1] = __shfl_sync(0xffffffffu, f, 8 * c + 4);
 #pragma unroll
@@ -277,7 +286,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
   }
   if constexpr (C::QS) __syncthreads();
 
-  float o[NR][DT][4], sum[NR][2], top[NR][2], vtop[NR][2];   // o: dimensions g, g + 8 x rows 2 c, 2 c + 1 of a tile
+  float o[NR][DT][4], sum[NR][2], top[NR][2], vtop[NR][2], limit[NR][2];   // o: dimensions g, g + 8 x rows 2 c, 2 c + 1 of a tile
 #pragma unroll
   for (int nr = 0; nr < NR; ++nr) {
 #pragma unroll
@@ -285,7 +294,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[nr][j][i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) sum[nr][e] = 0.f, top[nr][e] = vtop[nr][e] = -INFINITY;
+    for (int e = 0; e < 2; ++e) sum[nr][e] = 0.f, top[nr][e] = vtop[nr][e] = limit[nr][e] = -INFINITY;
   }
 
   int stage = 0;
@@ -344,31 +353,32 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
         }
       }
     }
-    // base-2 scores; a value's scale as an exponent
+    // a key's scale; a value's as an exponent
     float vs[NB][2];
     bool odd = k0 < whole_lo || k0 + RUN > whole_hi;         // some row does not see the whole run
+    float vs_top = 0.f;                                      // the largest value scale of the run
+    if constexpr (E4M3) {
+      const uint32_t kb = lane < RUN ? lds8(sc + lane) : 0, vb = lane < RUN ? lds8(sc + RUN + lane) : 0;
+      const uint32_t top_byte = __reduce_max_sync(0xffffffffu, max(kb == SCALE_NAN ? SCALE_NAN : 0u, vb));
+      vs_top = __uint_as_float(0x4b000000u | top_byte) - 8388735.f;
+      odd |= top_byte == SCALE_NAN;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float ks = 1.f;
-        if constexpr (E4M3) {
+        for (int i = 0; i < 2; ++i) {
           const uint32_t kb = lds8(sc + 16 * b + 8 * i + g), vb = lds8(sc + RUN + 16 * b + 8 * i + g);
-          ks = __uint_as_float(kb << 23);
-          vs[b][i] = __uint_as_float(0x4b000000u | vb) - 8388735.f;   // vb - 127
+          float ks = __uint_as_float(kb << 23);
+          vs[b][i] = __uint_as_float(0x4b000000u | vb) - 8388735.f;      // vb - 127
           // a key or value that is no number makes the key's scores none: the rows that see it,
           // and no other, then hold NaN
-          if (kb == SCALE_NAN || vb == SCALE_NAN) odd = true, ks = NO_NUMBER, vs[b][i] = 0.f;
-        }
+          if (odd && (kb == SCALE_NAN || vb == SCALE_NAN)) ks = NO_NUMBER, vs[b][i] = 0.f;
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) {
-          float2 x = make_float2(s[nr][b][2 * i], s[nr][b][2 * i + 1]);
-          if constexpr (E4M3) x = mul2(x, make_float2(ks, ks));
-          x = mul2(x, make_float2(rf[nr][0], rf[nr][1]));
-          s[nr][b][2 * i] = x.x, s[nr][b][2 * i + 1] = x.y;
+          for (int nr = 0; nr < NR; ++nr) {
+            const float2 x = mul2(make_float2(s[nr][b][2 * i], s[nr][b][2 * i + 1]), make_float2(ks, ks));
+            s[nr][b][2 * i] = x.x, s[nr][b][2 * i + 1] = x.y;
+          }
         }
-      }
-    odd = __any_sync(0xffffffffu, odd);
+    }
     if (odd) {
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr)
@@ -386,45 +396,47 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
             }
         }
     }
+    // does a score pass its row's reference by 2^LAZY?  (limits are held in units of the product.)
+    // 8-bit pages: or could a weight times its value's scale pass what fp16 holds, 2^(LAZY + SLACK)
     bool raise = false;
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float m = -INFINITY, mv = -INFINITY;
+        float m = fmaxf(s[nr][0][e], s[nr][0][2 + e]);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            m = fmaxf(m, s[nr][b][2 * i + e]);
-            if constexpr (E4M3) mv = fmaxf(mv, s[nr][b][2 * i + e] + vs[b][i]);
-          }
-        raise |= m > top[nr][e] + LAZY;
-        if constexpr (E4M3) raise |= mv > vtop[nr][e] + LAZY;
+        for (int b = 1; b < NB; ++b) m = fmaxf(m, fmaxf(s[nr][b][e], s[nr][b][2 + e]));
+        raise |= m > limit[nr][e];
+        if constexpr (E4M3) raise |= top[nr][e] + vs_top > vtop[nr][e] + SLACK;
       }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float m = top[nr][e], mv = vtop[nr][e];
+          float m = -INFINITY, mv = -INFINITY;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              m = fmaxf(m, s[nr][b][2 * i + e]);
-              if constexpr (E4M3) mv = fmaxf(mv, s[nr][b][2 * i + e] + vs[b][i]);
+              const float x = s[nr][b][2 * i + e] * rf[nr][e];
+              m = fmaxf(m, x);
+              if constexpr (E4M3) mv = fmaxf(mv, x + vs[b][i]);
             }
 #pragma unroll
           for (int x = 4; x < 32; x *= 2) {
             m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
             if constexpr (E4M3) mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
           }
-          if constexpr (!E4M3) mv = m;
+          m = fmaxf(m, top[nr][e]);
+          // the values' reference: the row's own largest weight times scale so far, raised no further
+          // than this run's weights need, so that no outlier of negligible weight pushes the others out
+          mv = E4M3 ? fmaxf(mv, vtop[nr][e]) : m;
           const float f = ex2_approx(top[nr][e] - (m == -INFINITY ? 0.f : m));
           const float fv = E4M3 ? ex2_approx(vtop[nr][e] - (mv == -INFINITY ? 0.f : mv)) : f;
           top[nr][e] = m;
           vtop[nr][e] = mv;
+          limit[nr][e] = (m + LAZY) / rf[nr][e];
           sum[nr][e] *= f;
 #pragma unroll
           for (int j = 0; j < DT; ++j) o[nr][j][e] *= fv, o[nr][j][2 + e] *= fv;
@@ -434,18 +446,25 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
     uint32_t p[NR][NB][2];
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr) {
-      const float m0 = top[nr][0] == -INFINITY ? 0.f : top[nr][0], m1 = top[nr][1] == -INFINITY ? 0.f : top[nr][1];
-      const float v0 = vtop[nr][0] == -INFINITY ? 0.f : vtop[nr][0], v1 = vtop[nr][1] == -INFINITY ? 0.f : vtop[nr][1];
+      const float2 r2 = make_float2(rf[nr][0], rf[nr][1]);
+      const float2 m2 = make_float2(top[nr][0] == -INFINITY ? 0.f : -top[nr][0], top[nr][1] == -INFINITY ? 0.f : -top[nr][1]);
+      const float2 v2 = make_float2(vtop[nr][0] == -INFINITY ? 0.f : -vtop[nr][0], vtop[nr][1] == -INFINITY ? 0.f : -vtop[nr][1]);
+      float2 l2 = make_float2(sum[nr][0], sum[nr][1]);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float x0 = s[nr][b][2 * i], x1 = s[nr][b][2 * i + 1];
-          float w0 = ex2_approx(x0 - m0), w1 = ex2_approx(x1 - m1);
-          sum[nr][0] += w0, sum[nr][1] += w1;
-          if constexpr (E4M3) w0 = ex2_approx(x0 + (vs[b][i] - v0)), w1 = ex2_approx(x1 + (vs[b][i] - v1));
-          p[nr][b][i] = transposed(pack(w0, w1, E4M3));
+          const float2 x = make_float2(s[nr][b][2 * i], s[nr][b][2 * i + 1]);
+          float2 w = fma2(x, r2, m2);
+          w = make_float2(ex2_approx(w.x), ex2_approx(w.y));
+          l2 = add2(l2, w);
+          if constexpr (E4M3) {
+            w = fma2(x, r2, add2(make_float2(vs[b][i], vs[b][i]), v2));
+            w = make_float2(ex2_approx(w.x), ex2_approx(w.y));
+          }
+          p[nr][b][i] = transposed(pack(w.x, w.y, E4M3));
         }
+      sum[nr][0] = l2.x, sum[nr][1] = l2.y;
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -506,7 +525,6 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
     if (tid == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
     const long long t0 = clock64();
     while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);   // those in flight land before the block ends
-    return;
   }
 
   // this warp's sums to its part of the ring: [row][dimension]; tile j holds, in its rows g and
@@ -568,31 +586,23 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ A
         if (!isfinite(y[3])) x.w += y[3];
       }
     }
-    const int row = t.first + R / a.group, head = t.kv_head * a.group + R % a.group;
-    if (a.splits == 1) {
-      const float f = l == 0.f ? 0.f : 1.f / l;
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.out) + row * a.ldo + (long long)head * D + d;
-      *reinterpret_cast<uint2*>(dst) = make_uint2(pack(x.x * f, x.y * f, false), pack(x.z * f, x.w * f, false));
-    } else {
-      const long long at = part_index(a, t.split, row, head);
-      *reinterpret_cast<float4*>(a.part + at * D + d) = x;
-      if (d == 0) a.ml[at] = make_float2(m, l);
+    if (a.cluster == 1) {
+      put_result<__nv_bfloat16, D>(a, t, R, d, x, m, l);
+    } else {                                                 // in place of the first warp's
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(mem) + r * LD + d) = x;
+      if (d == 0) block_ml[r] = make_float2(m, l);
     }
   }
+  if (a.cluster > 1) join_cluster<__nv_bfloat16, D, ROWS, THREADS>(a, t, reinterpret_cast<const float*>(mem), LD, block_ml, r0, rows);
 }
 
 template <int D, bool E4M3, int NR>
 cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
   using C = Cfg<D, E4M3, NR>;
-  const auto k = rows_kernel<D, E4M3, NR>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-  if (e != cudaSuccess) return e;
   CUtensorMap km, vm;
   const int box = std::min(a.m.page_tokens, C::RUN);
   if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
-  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
-  k<<<grid, THREADS, C::SMEM, st>>>(a, km, vm);
-  return cudaGetLastError();
+  return launch_pieces(rows_kernel<D, E4M3, NR>, a, THREADS, C::SMEM, st, km, vm);
 }
 
 template <int NR>

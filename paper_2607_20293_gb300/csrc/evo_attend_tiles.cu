@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // queries to shared memory, a row a thread; the softmax works with a positive scale
-  const float sc = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+  const float sc = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f);
   if (warp < 8 && (pair || warp < 4)) {
     const int r = tid % BM, R = r0 + tid;
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;

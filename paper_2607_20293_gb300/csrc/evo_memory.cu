@@ -116,7 +116,7 @@ evo_status attend_sizes(const evo_memory* m, int32_t rows, int32_t max_new, int3
   if (!m->starts && max_new < rows / m->n_seq) return EVO_ERR_ARG;
   if (max_len > m->max_pages * m->page_tokens) return EVO_ERR_ARG;
   // blocks of the launch: the row tiles of every sequence and head, a piece each
-  if (((long long)max_new * m->n_head / 16 + m->n_kv_head) * m->n_seq > INT_MAX / 64) return EVO_ERR_SHAPE;
+  if (((long long)max_new * m->n_head / 16 + m->n_kv_head) * m->n_seq > INT_MAX / 128) return EVO_ERR_SHAPE;
   return EVO_OK;
 }
 

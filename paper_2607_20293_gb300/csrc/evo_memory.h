@@ -44,14 +44,15 @@ struct AttendArgs {
   int causal, window;
   int tiles;                      // row tiles of a (sequence, key/value head): max_new * group rows
   int splits;                     // pieces of the memory that a tile's blocks share
-  float* part;                    // [splits][rows][n_head][head_dim]: unnormalised sums of a piece
-  float2* ml;                     // [splits][rows][n_head]: its maximum (base 2) and sum
+  int cluster;                    // pieces that the blocks of a cluster join among themselves; divides splits
+  float* part;                    // [splits / cluster][rows][n_head][head_dim]: unnormalised sums of a cluster's pieces
+  float2* ml;                     // [splits / cluster][rows][n_head]: their maximum (base 2) and sum
 };
 // which kernel takes a call, and how it is cut up
 enum AttendKernel { ATTEND_F32, ATTEND_F32_ROWS, ATTEND_ROWS, ATTEND_TILES };
 struct AttendPlan {
   AttendKernel kernel;
-  int tile_rows, tiles, splits;
+  int tile_rows, tiles, splits, cluster;
   size_t scratch;
 };
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len);
