@@ -26,6 +26,11 @@ namespace evo {
 namespace {
 
 constexpr int BN = 64, THREADS = 128, JOIN_THREADS = 256;
+// from this many rows a key/value head on, 8-bit pages are written out as bf16 pages for the tcgen05
+// kernel (16 sequences of 8,192 keys of 64, us with / without: 64 rows 131 / 129, 96 rows 131 / 152,
+// 256 rows 165 / 362; of 128: 237 / 196, 238 / 331, 267 / 693), while they fit this many bytes
+constexpr int EXPAND_ROWS = 65;
+constexpr long long EXPAND_MOST = 4ll << 30;
 
 template <int D, int RM>
 struct Smem {
@@ -314,6 +319,37 @@ cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+// 8-bit pages of every sequence as bf16 pages n * cols + i (i < cols: what max_len tokens fill),
+// keys and values: a power of two times a code is exact in bf16.  16 codes a thread.
+template <int D>
+__global__ void __launch_bounds__(JOIN_THREADS) expand_kernel(const __grid_constant__ evo_memory m, int cols, int max_len, __nv_bfloat16* k,
+                                                              __nv_bfloat16* v, int* table) {
+  const int page = blockIdx.x, n = page / cols, i = page % cols;
+  if (threadIdx.x == 0 && blockIdx.y == 0) table[page] = page;
+  if ((long long)i * m.page_tokens >= seq_len(m, n, max_len)) return;
+  const long long head_rows = (long long)m.n_kv_head * m.page_tokens, from = seq_page(m, n, i) * head_rows, to = page * head_rows;
+  const uint8_t* codes = static_cast<const uint8_t*>(blockIdx.y ? m.v_pages : m.k_pages);
+  const uint8_t* scales = blockIdx.y ? m.v_scales : m.k_scales;
+  __nv_bfloat16* out = blockIdx.y ? v : k;
+  for (int x = threadIdx.x; x < head_rows * (D / 16); x += JOIN_THREADS) {
+    const int r = x / (D / 16), d = x % (D / 16) * 16;
+    const uint4 c = *reinterpret_cast<const uint4*>(codes + (from + r) * D + d);
+    const float f = scale_value(scales[from + r]);
+    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    uint32_t h[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 y = codes4(w[e]);
+      const __nv_bfloat162 a = __floats2bfloat162_rn(y.x * f, y.y * f), b = __floats2bfloat162_rn(y.z * f, y.w * f);
+      h[2 * e] = *reinterpret_cast<const uint32_t*>(&a);
+      h[2 * e + 1] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    uint4* dst = reinterpret_cast<uint4*>(out + (to + r) * D + d);
+    dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
+    dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
+  }
+}
+
 template <int D, int RM>
 cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
   const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
@@ -345,7 +381,13 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   AttendPlan p;
   const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
   const bool f32 = m.dtype == EVO_DTYPE_F32, few = all <= (f32 ? 16 : 32);
-  const bool tiles = !f32 && m.format == EVO_CACHE_BF16 && !few;
+  // Many rows: 8-bit pages are written out as bf16 pages once, so that the tensor cores read them
+  // as they lie
+  const long long cols = (max_len + m.page_tokens - 1) / m.page_tokens;
+  const long long expanded = 4ll * m.n_seq * cols * m.n_kv_head * m.page_tokens * m.head_dim;
+  const bool expand = !f32 && m.format == EVO_CACHE_E4M3 && all >= EXPAND_ROWS && expanded <= EXPAND_MOST && cols > 0;
+  const bool tiles = !f32 && !few && (m.format == EVO_CACHE_BF16 || expand);
+  p.expand = expand ? (int)cols : 0;
   p.kernel = f32 ? (few ? ATTEND_F32_ROWS : ATTEND_F32) : tiles ? ATTEND_TILES : ATTEND_ROWS;
   p.tile_rows = f32     ? (all == 1 ? 1 : all <= 4 || few && (long long)m.n_seq * m.n_kv_head < 152 ? 4 : few ? 16 : all <= 32 || m.head_dim == 128 ? 32 : 64)
                 : tiles ? 256
@@ -372,6 +414,7 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   }
   const int parts = p.splits / p.cluster;
   p.scratch = parts == 1 ? 0 : (size_t)parts * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
+  if (expand) p.scratch = (p.scratch + 15) / 16 * 16 + expanded + 4ll * m.n_seq * cols;
   return p;
 }
 
@@ -384,6 +427,25 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
   a.ml = reinterpret_cast<float2*>(a.part + (size_t)parts * a.rows * a.m.n_head * a.m.head_dim);
   const bool d64 = a.m.head_dim == 64;
   cudaError_t e = cudaSuccess;
+  if (p.expand) {
+    const size_t joined = parts == 1 ? 0 : (size_t)parts * a.rows * a.m.n_head * ((size_t)a.m.head_dim + 2) * sizeof(float);
+    const size_t values = (size_t)a.m.n_seq * p.expand * a.m.n_kv_head * a.m.page_tokens * a.m.head_dim;
+    __nv_bfloat16* k = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(scratch) + (joined + 15) / 16 * 16);
+    int* table = reinterpret_cast<int*>(k + 2 * values);
+    const dim3 grid(a.m.n_seq * p.expand, 2);
+    if (d64)
+      expand_kernel<64><<<grid, JOIN_THREADS, 0, st>>>(a.m, p.expand, a.max_len, k, k + values, table);
+    else
+      expand_kernel<128><<<grid, JOIN_THREADS, 0, st>>>(a.m, p.expand, a.max_len, k, k + values, table);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    a.m.format = EVO_CACHE_BF16;
+    a.m.k_pages = k;
+    a.m.v_pages = k + values;
+    a.m.k_scales = a.m.v_scales = nullptr;
+    a.m.table = table;
+    a.m.max_pages = p.expand;
+    a.m.n_pages = a.m.n_seq * p.expand;
+  }
   if (p.kernel == ATTEND_F32)
     e = p.tile_rows == 32 ? d64 ? launch_f32<64, 4>(a, st) : launch_f32<128, 4>(a, st)
                           : d64 ? launch_f32<64, 8>(a, st) : launch_f32<128, 8>(a, st);

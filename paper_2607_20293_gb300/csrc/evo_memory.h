@@ -48,11 +48,12 @@ struct AttendArgs {
   float* part;                    // [splits / cluster][rows][n_head][head_dim]: unnormalised sums of a cluster's pieces
   float2* ml;                     // [splits / cluster][rows][n_head]: their maximum (base 2) and sum
 };
-// which kernel takes a call, and how it is cut up
+// which kernel takes a call, and how it is cut up.  expand: 8-bit pages are first written out as
+// bf16 pages of their own in the scratch, `expand` of them a sequence (0: no)
 enum AttendKernel { ATTEND_F32, ATTEND_F32_ROWS, ATTEND_ROWS, ATTEND_TILES };
 struct AttendPlan {
   AttendKernel kernel;
-  int tile_rows, tiles, splits, cluster;
+  int tile_rows, tiles, splits, cluster, expand;
   size_t scratch;
 };
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len);
