@@ -4,28 +4,30 @@
 // With 128 rows and more a key is used often enough that the tensor cores bound
 // the call: 4 D operations a (row, key), 628 cycles for 128 rows x 128 keys of 64 at
 // the measured bf16 rate, against 512 cycles for their 16,384 exponentials (32 a
-// cycle and SM) and about 400 issue slots a scheduler for the rest of the softmax.
-// All three have to run at once, so a block keeps two streams of tiles in flight:
-// while the softmax of one stream runs, the tensor cores work for the other.
+// cycle and SM) and about 600 issue cycles a scheduler for the rest of the softmax.
+// All three have to run at once.  A block keeps two streams of tiles in flight, and of
+// each stream the scores of two blocks of 64 keys: while the softmax works on one, the
+// tensor cores have the other and the output of the one before.
 //   * more than 128 rows: the streams are two tiles of 128 rows over the same keys;
 //   * else: both are the same rows, over the even and the odd blocks of keys, and
 //     are joined at the end.
+// Blocks of 128 keys, one of a stream at a time, leave the softmax waiting for the
+// tensor cores and back (2,048 rows over 16,384 keys: 99 us against FIGURE).
 // Roles: warps 0-3 and 4-7 are the softmax of streams A and B, a thread a row (the
 // thread-per-lane layout of tensor memory: no reduction over lanes anywhere); warp 8
-// issues the MMAs; warp 9 brings keys and values, 128 at a time, by tiled bulk
-// copies of whole pages (or 128 tokens of one) into a ring.
+// issues the MMAs; warp 9 brings keys and values, 64 at a time, by tiled bulk copies
+// into a ring.
 //
 //   S = Q K^T      both operands from shared memory, 128-byte swizzle, fp32 in TMEM
 //   P = 2^(S - m)  read from TMEM, written back to it as bf16 over S
 //   O += P V       P from TMEM, V as it lies in its page (rows of keys: the operand
 //                  whose contiguous index is N)
-// The order of issue (PV of a block, then S of the next block of the same stream)
-// keeps the write over S behind the read of P: the tensor pipe executes a block's
-// MMAs in order.
+// The scores two blocks on go into the buffer that P came from, once the product
+// that reads P is done.
 //
-// The running maximum is lazy: O is rescaled (a pass over TMEM) only when a row's
-// maximum grows by more than 2^8; weights are at most 2^8 and bf16 holds them with the
-// same relative rounding, 2^-8 at most of each.
+// The running maximum is lazy: O is rescaled (a pass over TMEM, behind the product
+// before) only when a row's maximum grows by more than 2^8; weights are at most 2^8
+// and bf16 holds them with the same relative rounding, 2^-8 at most of each.
 //
 // Masks are looked at only in blocks that some row does not see whole.  There, the
 // values of keys outside the piece are set to zero in shared memory, and entries
@@ -42,25 +44,27 @@
 namespace evo {
 namespace {
 
-constexpr int BM = 128, BN = 128;
+constexpr int BM = 128;
 constexpr int THREADS = 384;                       // warps 10 and 11 only complete the third warpgroup
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
-constexpr int BLOCK64 = BN * 128;                  // bytes of 128 rows of 64 bf16
+constexpr int Q64 = BM * 128;                      // bytes of 64 columns of 128 queries
 
 template <int D>
 struct Cfg {
-  static constexpr int TILE = BN * D * 2;          // bytes of 128 rows
-  static constexpr int SLOTS = D == 64 ? 8 : 5;
+  static constexpr int BN = D == 64 ? 128 : 64;    // keys of a block: what 512 columns of tensor memory hold of S, P and O twice
+  static constexpr int QTILE = BM * D * 2, TILE = BN * D * 2, K64 = BN * 128;   // bytes: 128 queries, BN keys or values, 64 columns of them
+  static constexpr int SLOTS = D == 64 ? 8 : 10;
   static constexpr int LD = D + 4;                 // floats of a row where the streams are joined
-  static constexpr int SMEM = 1024 + 2 * TILE + SLOTS * TILE;
+  static constexpr int SMEM = 1024 + 2 * QTILE + SLOTS * TILE;
   static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BM >> 4) << 24);
   static constexpr uint32_t IDESC_S = IDESC | ((uint32_t)(BN >> 3) << 17);
   static constexpr uint32_t IDESC_O = IDESC | (1u << 16) | ((uint32_t)(D >> 3) << 17);   // B's contiguous index is N
-  static constexpr int S_COL = 0, O_COL = 256;     // TMEM columns: S of stream x at 128 x, O at 256 + D x
+  // TMEM columns of stream x: S at BN x, P (bf16, two a column) at P_COL + BN / 2 x, O at O_COL + D x
+  static constexpr int P_COL = 2 * BN, O_COL = 512 - 2 * D;
 };
 
 struct Shared {
-  uint64_t full[8], empty[8], s_full[2], p_full[2], o_full[2];
+  uint64_t full[10], empty[10], s_full[2], s_free[2], p_full[2], o_full[2];
   uint32_t tmem;
   int dead, poison;
   float2 ml[BM];                                   // stream B's maximum and sum where the streams are joined
@@ -103,7 +107,7 @@ __device__ __forceinline__ void tmem_wait_ld(float (&v)[N]) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// registers of a warpgroup: 8 softmax warps of 232 and 4 of 40 are the 12 warps of 168 of the launch
+// registers of a warpgroup: 8 softmax warps of 216 and 4 of 72 are the 12 warps of 168 of the launch
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -111,9 +115,9 @@ __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec
 __device__ __forceinline__ void bar_softmax() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
 // descriptor of V as the operand whose contiguous index is N: 64 dimensions by 8 keys
-// a swizzled kilobyte, the next 8 keys behind it, the next 64 dimensions BLOCK64 on
-__device__ __forceinline__ uint64_t v_desc(uint32_t saddr) {
-  return (tc::sw128_desc(saddr) & ~(0x3fffull << 16)) | (uint64_t)(BLOCK64 >> 4) << 16;
+// a swizzled kilobyte, the next 8 keys behind it, the next 64 dimensions k64 bytes on
+__device__ __forceinline__ uint64_t v_desc(uint32_t saddr, int k64) {
+  return (tc::sw128_desc(saddr) & ~(0x3fffull << 16)) | (uint64_t)(k64 >> 4) << 16;
 }
 
 // a bounded wait; false once any wait of the block was in vain
@@ -128,6 +132,24 @@ __device__ __forceinline__ bool wait_for(Shared& sh, uint64_t* bar, uint32_t par
   return false;
 }
 
+// the same behind a first test that failed, for the issuing warp
+__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) {
+  const long long t0 = clock64();
+  while (!tc::block_dead(dead)) {
+    if (tc::mbar_test(bar, parity)) return;
+    if (clock64() - t0 > WAIT_CYCLES_DEFAULT) asm volatile("st.volatile.shared::cta.b32 [%0], 1;" ::"r"(dead) : "memory");
+  }
+}
+__device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ float2 exp2_of(float2 x) { return make_float2(ex2_approx(x.x), ex2_approx(x.y)); }
 __device__ __forceinline__ uint32_t pack(float2 x) {
   uint32_t r;
@@ -140,30 +162,31 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
                                                            const __grid_constant__ CUtensorMap kmap,
                                                            const __grid_constant__ CUtensorMap vmap) {
   using C = Cfg<D>;
-  constexpr int SLOTS = C::SLOTS;
+  constexpr int SLOTS = C::SLOTS, BN = C::BN, K64 = C::K64;
   extern __shared__ uint8_t raw[];
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
-  uint8_t* const ring = mem + 2 * C::TILE;
+  uint8_t* const ring = mem + 2 * C::QTILE;
   const Tile t = tile_of_block(a);
   const int rows = t.count * a.group, r0 = t.tile * 2 * BM;
   if (r0 >= rows) return;
   const bool pair = r0 + BM < rows;                // two tiles of rows; else one, its keys over both streams
-  const int ahead = pair ? 1 : 2;                  // blocks of keys whose scores are asked for before the first output
+  const int ahead = pair ? 2 : 4;                  // blocks of keys whose scores are asked for before the first output
   const int last = min(r0 + 2 * BM, rows) - 1;
   const Range first_row = seen_by(a, t, r0 / a.group), last_row = seen_by(a, t, last / a.group);
   const Range all = piece_of(a, t, {first_row.lo, last_row.hi}, BN);
   const int whole_lo = max(last_row.lo, all.lo), whole_hi = min(first_row.hi, all.hi);
   const int key0 = all.lo / BN * BN, n = max(0, (all.hi - key0 + BN - 1) / BN);
-  // operands in the order in which they are used: K 0 .. ahead - 1, then V i, K i + ahead
+  // operands in the ring: K 0 .. ahead - 1, then V i, K i + ahead
   const auto v_index = [&](int i) { return min(n, i + ahead) + i; };
 
   if (warp == 0) tc::tmem_alloc(&sh.tmem, 512);
   if (tid == 32) {
-    for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], 1);
+    for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], pair ? 2 : 1);
     for (int x = 0; x < 2; ++x) {
       tc::mbar_init1(&sh.s_full[x], 1);
+      tc::mbar_init1(&sh.s_free[x], BM);
       tc::mbar_init1(&sh.p_full[x], BM);
       tc::mbar_init1(&sh.o_full[x], 1);
     }
@@ -182,7 +205,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     for (int j = 0; j < D / 8; ++j) {
       uint4 u = R < rows && a.scale_log2 != 0.f ? src[j] : make_uint4(0, 0, 0, 0);
       u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
-      *reinterpret_cast<uint4*>(mem + (warp / 4) * C::TILE + (j / 8) * BLOCK64 + r * 128 + ((j % 8 ^ (r & 7)) << 4)) = u;
+      *reinterpret_cast<uint4*>(mem + (warp / 4) * C::QTILE + (j / 8) * Q64 + r * 128 + ((j % 8 ^ (r & 7)) << 4)) = u;
     }
     tc::fence_async_smem();
   }
@@ -192,11 +215,11 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
   const uint32_t tmem = sh.tmem;
 
   if (warp >= 8) {
-  fewer_registers<40>();
+  fewer_registers<72>();
   if (warp == 9) {
     // ------------------------------------------------------------ copies
-    const int box = a.m.page_tokens, shift = 31 - __clz(box);
-    const long long head_row = (long long)t.kv_head * box, page_rows = (long long)a.m.n_kv_head * box;
+    const int page_tokens = a.m.page_tokens, box = min(page_tokens, BN), shift = 31 - __clz(page_tokens);
+    const int head_row = t.kv_head * page_tokens, page_rows = a.m.n_kv_head * page_tokens;
     int index = 0;
     const auto bring = [&](const CUtensorMap* map, int i) {
       const int slot = index % SLOTS, use = index / SLOTS;
@@ -211,8 +234,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       if (on)
 #pragma unroll
         for (int x = 0; x < D / 64; ++x)
-          tc::tma_load_2d(ring + slot * C::TILE + x * BLOCK64 + lane * box * 128, map, x * 64,
-                          (int)(page * page_rows + head_row), &sh.full[slot]);
+          tc::tma_load_2d(ring + slot * C::TILE + x * K64 + lane * box * 128, map, x * 64,
+                          page * page_rows + head_row + (key & (page_tokens - 1)), &sh.full[slot]);
       __syncwarp();
     };
     for (int i = 0; i < min(ahead, n); ++i) bring(&kmap, i);
@@ -220,68 +243,71 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       bring(&vmap, i);
       if (i + ahead < n) bring(&kmap, i + ahead);
     }
-  } else if (warp == 8) {
-    // ------------------------------------------------------------ MMAs
-    const uint32_t q0 = tc::su32(mem), ring0 = tc::su32(ring);
-    const auto k_index = [&](int i) { return i < ahead ? i : 2 * i - ahead + 1; };
-    bool ok = true;
-    // S of stream x from the keys of block i; the last stream that reads them frees their slot
-    const auto scores = [&](int x, int i, bool release) {
-      const int index = k_index(i), slot = index % SLOTS;
-      ok = ok && wait_for(sh, &sh.full[slot], (index / SLOTS) & 1);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
-      tc::tc_fence_after();
-      if (tc::elect_one()) {
-        const uint64_t qd = tc::sw128_desc(q0 + (pair ? x : 0) * C::TILE), kd = tc::sw128_desc(ring0 + slot * C::TILE);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          tc::mma_f16(tmem + C::S_COL + 128 * x, qd + (k / 4) * (BLOCK64 >> 4) + (k % 4) * 2,
-                      kd + (k / 4) * (BLOCK64 >> 4) + (k % 4) * 2, C::IDESC_S, k > 0);
-        tc::mma_commit(&sh.s_full[x]);
-        if (release) tc::mma_commit(&sh.empty[slot]);
-      }
-      __syncwarp();
+  } else if (warp == 8 || warp == 10) {
+    // ------------------------------------------------------------ MMAs of a stream
+    // Uniform over the warp and known to the compiler to be (a shuffle's result is), one elected
+    // lane issuing: descriptors then stay in uniform registers.
+    const uint32_t x = __shfl_sync(0xffffffffu, warp == 8 ? 0 : 1, 0);
+    const int blocks = __shfl_sync(0xffffffffu, n, 0), two = __shfl_sync(0xffffffffu, (int)pair, 0);
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t kdesc = tc::sw128_desc(0), vdesc = v_desc(0, K64);
+    const uint32_t khi = (uint32_t)(kdesc >> 32), klo = (uint32_t)kdesc, vhi = (uint32_t)(vdesc >> 32), vlo = (uint32_t)vdesc;
+    const uint32_t qd = klo + (tc::su32(mem) >> 4) + (two ? x : 0) * (C::QTILE >> 4), r0d = tc::su32(ring) >> 4;
+    const uint32_t full = tc::su32(sh.full), empty = tc::su32(sh.empty), dead = tc::su32(&sh.dead);
+    const uint32_t s_full = tc::su32(&sh.s_full[x]), s_free = tc::su32(&sh.s_free[x]), p_full = tc::su32(&sh.p_full[x]),
+                   o_full = tc::su32(&sh.o_full[x]);
+    const uint32_t lead = two ? 2 : 4;
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (!tc::mbar_test(bar, parity)) wait_slow(bar, parity, dead);
     };
-    // O += P V of block i, the it-th of stream x
-    const auto output = [&](int x, int i, int it, bool release, bool final) {
-      const int index = v_index(i), slot = index % SLOTS;
-      ok = ok && wait_for(sh, &sh.p_full[x], it & 1) && wait_for(sh, &sh.full[slot], (index / SLOTS) & 1);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) return;
+    // S of block i
+    const auto scores = [&](uint32_t i) {
+      const uint32_t index = i < lead ? i : 2 * i - lead + 1, slot = index % SLOTS;
+      wait(full + 8 * slot, (index / SLOTS) & 1);
       tc::tc_fence_after();
+      const uint32_t kd = klo + r0d + slot * (C::TILE >> 4);
       if (tc::elect_one()) {
-        const uint64_t vd = v_desc(ring0 + slot * C::TILE);
 #pragma unroll
-        for (int k = 0; k < BN / 16; ++k)
-          mma_tmem_a(tmem + C::O_COL + D * x, tmem + C::S_COL + 128 * x + 8 * k, vd + k * (2048 >> 4), C::IDESC_O,
-                     it > 0 || k > 0);
-        if (release) tc::mma_commit(&sh.empty[slot]);
-        if (final) tc::mma_commit(&sh.o_full[x]);
+        for (uint32_t k = 0; k < D / 16; ++k)
+          tc::mma_f16(tm + BN * x, desc64(qd + (k / 4) * (Q64 >> 4) + (k % 4) * 2, khi),
+                      desc64(kd + (k / 4) * (K64 >> 4) + (k % 4) * 2, khi), C::IDESC_S, k);
+        commit(s_full);
+        commit(empty + 8 * slot);
       }
-      __syncwarp();
     };
-    if (pair) {
-      if (n > 0) scores(0, 0, false), scores(1, 0, true);
-      for (int i = 0; i < n; ++i)
-        for (int x = 0; x < 2; ++x) {
-          output(x, i, i, x == 1, i == n - 1);
-          if (i + 1 < n) scores(x, i + 1, x == 1);
-        }
-    } else {
-      for (int i = 0; i < min(2, n); ++i) scores(i, i, true);
-      for (int i = 0; i < n; ++i) {
-        output(i & 1, i, i >> 1, true, i + 2 >= n);
-        if (i + 2 < n) scores(i & 1, i + 2, true);
+    // O += P V of block i
+    const auto output = [&](uint32_t i, uint32_t accumulate) {
+      const uint32_t index = min((uint32_t)blocks, i + lead) + i, slot = index % SLOTS;
+      wait(full + 8 * slot, (index / SLOTS) & 1);
+      tc::tc_fence_after();
+      const uint32_t vd = vlo + r0d + slot * (C::TILE >> 4);
+      if (tc::elect_one()) {
+#pragma unroll
+        for (uint32_t k = 0; k < BN / 16; ++k)
+          mma_tmem_a(tm + C::O_COL + D * x, tm + C::P_COL + BN / 2 * x + 8 * k, desc64(vd + k * (2048 >> 4), vhi), C::IDESC_O,
+                     accumulate | k);
+        commit(empty + 8 * slot);
+        commit(o_full);
       }
+    };
+    const int from = two ? 0 : x, by = two ? 1 : 2;
+    if (from < blocks) scores(from);
+    for (int it = 0; from + by * it < blocks; ++it) {
+      if (from + by * (it + 1) < blocks) {
+        wait(s_free, it & 1);                      // the softmax has this block's scores in registers
+        scores(from + by * (it + 1));
+      }
+      wait(p_full, it & 1);
+      output(from + by * it, it);
+      if (__any_sync(0xffffffffu, tc::block_dead(dead))) break;
     }
   }
   } else {
-    more_registers<232>();
+    more_registers<216>();
     // ------------------------------------------------------------ softmax: stream x, a row a thread
     const int x = warp / 4, r = tid % BM, R = r0 + (pair ? tid : r);
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    const uint32_t s_at = tmem + C::S_COL + 128 * x + lanes, o_at = tmem + C::O_COL + D * x + lanes;
+    const uint32_t s_at = tmem + BN * x + lanes, p_at = tmem + C::P_COL + BN / 2 * x + lanes, o_at = tmem + C::O_COL + D * x + lanes;
     Range see = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
     see = {max(see.lo, all.lo), min(see.hi, all.hi)};
     const int from = pair ? 0 : x, by = pair ? 1 : 2;
@@ -295,24 +321,29 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       tc::tc_fence_after();
       float v[BN];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) tmem_ld32_async(s_at + 32 * j, v + 32 * j);
+      for (int j = 0; j < BN / 32; ++j) tmem_ld32_async(s_at + 32 * j, v + 32 * j);
       tmem_wait_ld(v);
+      tc::tc_fence_before();
+      tc::mbar_arrive1(&sh.s_free[x]);
       const int k0 = key0 + i * BN;
       const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
       if (!whole) {
         const int lo = see.lo - k0, hi = see.hi - k0;
 #pragma unroll
         for (int j = 0; j < BN; ++j) v[j] = j >= lo && j < hi ? v[j] : -INFINITY;
-        if (!pair || x == 0) {
-          // this block's values, cleaned before the product may read them
+        {
+          // this block's values, cleaned before the product may read them (two streams that share
+          // them both do it, each for its own product: they write the same)
           const int index = v_index(i), slot = index % SLOTS;
           ok = __all_sync(0xffffffffu, wait_for(sh, &sh.full[slot], (index / SLOTS) & 1));
           if (!ok) break;
-          const bool drop = k0 + r < all.lo || k0 + r >= all.hi;
+          const int vr = r % BN, part = r / BN;    // a value a thread, or its columns' half
+          const bool drop = k0 + vr < all.lo || k0 + vr >= all.hi;
           bool bad = false;
 #pragma unroll
-          for (int j = 0; j < D / 8; ++j) {
-            uint4* p = reinterpret_cast<uint4*>(ring + slot * C::TILE + (j / 8) * BLOCK64 + r * 128 + ((j % 8 ^ (r & 7)) << 4));
+          for (int jj = 0; jj < D * BN / 1024; ++jj) {
+            const int j = part * (D * BN / 1024) + jj;
+            uint4* p = reinterpret_cast<uint4*>(ring + slot * C::TILE + (j / 8) * K64 + vr * 128 + ((j % 8 ^ (vr & 7)) << 4));
             uint4 u = *p;
             uint32_t* w = reinterpret_cast<uint32_t*>(&u);
             bool changed = drop;
@@ -330,14 +361,19 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
           tc::fence_async_smem();
         }
       }
-      float mx[8];                                 // chains of their own: the latency of one is 128 steps
+      float mx[4];                                 // chains of their own
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mx[j] = fmaxf(v[j], v[8 + j]);
+      for (int j = 0; j < 4; ++j) mx[j] = v[j];
 #pragma unroll
-      for (int j = 16; j < BN; j += 16)
+      for (int j = 4; j + 8 <= BN; j += 8)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx[e] = fmaxf(mx[e], fmaxf(v[j + e], v[j + 8 + e]));
-      const float m = sc * fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), fmaxf(fmaxf(mx[4], mx[5]), fmaxf(mx[6], mx[7])));
+        for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], v[j + e], v[j + 4 + e]);
+      const float m = sc * fmaxf(max3(mx[0], mx[1], max3(v[BN - 4], v[BN - 3], v[BN - 2])), max3(mx[2], mx[3], v[BN - 1]));
+      if (it > 0) {                                // the product before this block has read its weights
+        ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], (it - 1) & 1));
+        if (!ok) break;
+        tc::tc_fence_after();
+      }
       const bool raise = m > top + LAZY;
       if (__any_sync(0xffffffffu, raise)) {
         const float now = raise ? m : top;
@@ -345,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         top = now;
 #pragma unroll
         for (int j = 0; j < 4; ++j) sums[j] = make_float2(sums[j].x * f, sums[j].y * f);
-        if (it > 0) {                              // the products before this block are done: s_full came behind them
+        if (it > 0) {
 #pragma unroll
           for (int j = 0; j < D / 32; ++j) {
             float o[32];
@@ -360,7 +396,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       const float ref = top == -INFINITY ? 0.f : -top;
       const float2 sc2 = make_float2(sc, sc), ref2 = make_float2(ref, ref);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < BN / 64; ++h) {
         uint32_t p[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
@@ -368,14 +404,14 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
           sums[j % 4] = add2(sums[j % 4], w);
           p[j] = pack(w);
         }
-        tmem_st32(s_at + 32 * h, p);
+        tmem_st32(p_at + 32 * h, p);
       }
       tmem_wait_st();
       tc::tc_fence_before();
       tc::mbar_arrive1(&sh.p_full[x]);
     }
     float l = ((sums[0].x + sums[0].y) + (sums[1].x + sums[1].y)) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
-    if (ok && it > 0) ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], 0));
+    if (ok && it > 0) ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], (it - 1) & 1));
     tc::tc_fence_after();
     bool mine = R < rows, scaled = false;
     float fa = 1.f, fb = 0.f;
@@ -481,7 +517,7 @@ cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
   const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   if (e != cudaSuccess) return e;
   CUtensorMap km, vm;
-  const int box = a.m.page_tokens;
+  const int box = std::min(a.m.page_tokens, C::BN);
   if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
   const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
   k<<<grid, THREADS, C::SMEM, st>>>(a, km, vm);
