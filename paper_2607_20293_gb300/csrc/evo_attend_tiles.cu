@@ -123,7 +123,7 @@ __device__ __forceinline__ uint64_t v_desc(uint32_t saddr, int k64) {
 // a bounded wait; false once any wait of the block was in vain
 __device__ __forceinline__ bool wait_for(Shared& sh, uint64_t* bar, uint32_t parity) {
   const uint32_t b = tc::su32(bar), dead = tc::su32(&sh.dead);
-  if (tc::mbar_test(b, parity)) return !tc::block_dead(dead);
+  if (tc::mbar_test(b, parity)) return true;
   const long long t0 = clock64();
   while (!tc::block_dead(dead)) {
     if (tc::mbar_test(b, parity)) return true;
@@ -186,8 +186,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], pair ? 2 : 1);
     for (int x = 0; x < 2; ++x) {
       tc::mbar_init1(&sh.s_full[x], 1);
-      tc::mbar_init1(&sh.s_free[x], BM);
-      tc::mbar_init1(&sh.p_full[x], BM);
+      tc::mbar_init1(&sh.s_free[x], 4);        // a warp each
+      tc::mbar_init1(&sh.p_full[x], 4);
       tc::mbar_init1(&sh.o_full[x], 1);
     }
     sh.dead = sh.poison = 0;
@@ -324,7 +324,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       for (int j = 0; j < BN / 32; ++j) tmem_ld32_async(s_at + 32 * j, v + 32 * j);
       tmem_wait_ld(v);
       tc::tc_fence_before();
-      tc::mbar_arrive1(&sh.s_free[x]);
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive1(&sh.s_free[x]);
       const int k0 = key0 + i * BN;
       const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
       if (!whole) {
@@ -408,7 +409,8 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
       }
       tmem_wait_st();
       tc::tc_fence_before();
-      tc::mbar_arrive1(&sh.p_full[x]);
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive1(&sh.p_full[x]);
     }
     float l = ((sums[0].x + sums[0].y) + (sums[1].x + sums[1].y)) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
     if (ok && it > 0) ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], (it - 1) & 1));
