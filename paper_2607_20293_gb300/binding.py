@@ -372,36 +372,41 @@ CACHE_FORMATS = {"fp32": 0, "bf16": 1, "e4m3": 2}
 UNIT_GROUP = 32          # values of a unit's cache that share a scale
 
 
-_torch = None
+# The small calls below take as long as their checks: names of torch and of the library are looked
+# up once, and every tensor is looked at once.
+_torch = _F32 = _BF16 = _U8 = _I32 = _raw_stream = _current_device = None
 
 
 def _load_torch():
-    global _torch
+    global _torch, _F32, _BF16, _U8, _I32, _raw_stream, _current_device
     import torch
+    _F32, _BF16, _U8, _I32 = torch.float32, torch.bfloat16, torch.uint8, torch.int32
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None)
+    load()
     _torch = torch
     return torch
 
 
-def _misfit(t, what: str, dtype, shape, device) -> ValueError:
+def _misfit(t, what: str, dtype, shape, index) -> ValueError:
     return ValueError(f"{what}: {t.dtype} {tuple(t.shape)} on {t.device}, contiguous: {t.is_contiguous()}; expected a "
-                      f"contiguous {dtype} {tuple(shape)} on {device}")
+                      f"contiguous {dtype} {tuple(shape)} on device {index}")
 
 
-def _need(t, what: str, dtype, shape, device):
+def _need(t, what: str, dtype, shape, index):
     """Address of a contiguous tensor of this type and shape on this device, or ValueError."""
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise _misfit(t, what, dtype, shape, device)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise _misfit(t, what, dtype, shape, index)
     return t.data_ptr()
 
 
-def _launch_stream(device, stream):
+def _launch_stream(index: int, stream):
     """The stream's handle (None: the current one); the tensors' device has to be the current one,
     because the library launches there."""
-    index = device.index
-    if device.type != "cuda" or index != _torch.cuda.current_device():
-        raise ValueError(f"tensors are on {device}, the call runs on the current CUDA device")
+    if index < 0 or index != _current_device():
+        raise ValueError(f"tensors are on device {index}, the call runs on the current CUDA device")
     if stream is None:
-        return _torch._C._cuda_getCurrentRawStream(index)
+        return _raw_stream(index)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -411,23 +416,25 @@ def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
     refresh [N] (uint8) is not zero, or all.  Returns y = x + r for those samples
     and x for the others (in `out`, which may be x), or None without x."""
     torch = _torch or _load_torch()
-    dev, dtype, u8, shape = r.device, r.dtype, torch.uint8, r.shape
-    st = _launch_stream(dev, stream)
-    if dtype is not torch.float32 and dtype is not torch.bfloat16:
-        raise _misfit(r, "r", "float32 or bfloat16", shape, dev)
+    index, dtype, shape = r.get_device(), r.dtype, r.shape
+    st = _launch_stream(index, stream)
+    if dtype is not _F32 and dtype is not _BF16:
+        raise _misfit(r, "r", "float32 or bfloat16", shape, index)
     N, H, E = shape
     xp = yp = None
     if x is not None:
-        xp = _need(x, "x", torch.float32, shape, dev)
+        xp = _need(x, "x", _F32, shape, index)
         if out is None:
             out = torch.empty_like(x)
-        yp = _need(out, "out", torch.float32, shape, dev)
+            yp = out.data_ptr()
+        else:
+            yp = _need(out, "out", _F32, shape, index)
     elif out is not None:
         raise ValueError("out without x")
-    rc = load().evo_cache_write(_need(r, "r", dtype, shape, dev), 0 if dtype is torch.float32 else 1,
-                                None if refresh is None else _need(refresh, "refresh", u8, (N,), dev), N, H, E, xp, yp,
-                                _need(codes, "codes", u8, shape, dev),
-                                _need(scales, "scales", u8, (N, H, E // UNIT_GROUP), dev), st)
+    rc = _lib.evo_cache_write(_need(r, "r", dtype, shape, index), 0 if dtype is _F32 else 1,
+                              None if refresh is None else _need(refresh, "refresh", _U8, (N,), index), N, H, E, xp, yp,
+                              _need(codes, "codes", _U8, shape, index),
+                              _need(scales, "scales", _U8, (N, H, E // UNIT_GROUP), index), st)
     if rc:
         _check(rc, "evo_cache_write")
     return out
@@ -438,16 +445,19 @@ def cache_add(codes, scales, x, reuse=None, out=None, stream=None):
     (codes [U][N][H][E], scales [U][N][H][E/32]) where reuse [U][N] is not zero, or
     of all; in `out` (which may be x) or a new tensor."""
     torch = _torch or _load_torch()
-    dev, u8, shape = x.device, torch.uint8, x.shape
-    st = _launch_stream(dev, stream)
+    index, shape = x.get_device(), x.shape
+    st = _launch_stream(index, stream)
     N, H, E = shape
     U = codes.shape[0]
+    xp = _need(x, "x", _F32, shape, index)
     if out is None:
         out = torch.empty_like(x)
-    rc = load().evo_cache_add(_need(codes, "codes", u8, (U, N, H, E), dev),
-                              _need(scales, "scales", u8, (U, N, H, E // UNIT_GROUP), dev),
-                              None if reuse is None else _need(reuse, "reuse", u8, (U, N), dev), U, N, H, E,
-                              _need(x, "x", torch.float32, shape, dev), _need(out, "out", torch.float32, shape, dev), st)
+        yp = out.data_ptr()
+    else:
+        yp = _need(out, "out", _F32, shape, index)
+    rc = _lib.evo_cache_add(_need(codes, "codes", _U8, (U, N, H, E), index),
+                            _need(scales, "scales", _U8, (U, N, H, E // UNIT_GROUP), index),
+                            None if reuse is None else _need(reuse, "reuse", _U8, (U, N), index), U, N, H, E, xp, yp, st)
     if rc:
         _check(rc, "evo_cache_add")
     return out
@@ -471,14 +481,14 @@ class Memory:
 
     def __init__(self, k_pages, v_pages, table, lens, n_head: int, k_scales=None, v_scales=None, starts=None,
                  status=None, dtype: str = "bf16"):
-        torch = _torch or _load_torch()
-        self._lib = load()
-        dev = self.device = k_pages.device
+        _torch or _load_torch()
+        self.device, dev = k_pages.device, k_pages.get_device()
+        self.index = dev
         e4m3 = k_pages.dtype.itemsize == 1
-        self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16
+        self.dtype = _F32 if dtype == "fp32" else _BF16
         n_pages, n_kv, page, dim = k_pages.shape
         n_seq, cols = table.shape
-        kind, shape, u8, i32 = torch.uint8 if e4m3 else self.dtype, k_pages.shape, torch.uint8, torch.int32
+        kind, shape, u8, i32 = _U8 if e4m3 else self.dtype, k_pages.shape, _U8, _I32
         if e4m3 != (k_scales is not None) or e4m3 != (v_scales is not None):
             raise ValueError("scales belong to pages of 8-bit codes")
         v = MemoryView(DTYPES[dtype], CACHE_FORMATS["e4m3" if e4m3 else dtype], n_head, n_kv, dim, page, n_pages, cols,
@@ -503,7 +513,7 @@ class Memory:
         """(address, elements between rows) of [rows][heads][head_dim], heads of a row contiguous."""
         dim = self.head_dim
         ld, between, within = t.stride() if t.dim() == 3 else (0, 0, 0)
-        if (t.dtype is not self.dtype or t.device != self.device or t.shape != (rows, heads, dim) or within != 1
+        if (t.dtype is not self.dtype or t.get_device() != self.index or t.shape != (rows, heads, dim) or within != 1
                 or (between != dim and heads > 1)):
             raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; expected {self.dtype} "
                              f"({rows}, {heads}, {dim}) on {self.device}, the heads of a row contiguous")
@@ -514,9 +524,8 @@ class Memory:
         """evo_memory_append: keys and values [rows][n_kv_head][head_dim] to their pages, and the
         normed and rotated queries [rows][n_head][head_dim] (in `out`, which may be q, or a new
         tensor).  q may be None (returns None), or k and v.  max_new is not needed here."""
-        torch = _torch or _load_torch()
-        dev, dim = self.device, self.head_dim
-        st = _launch_stream(dev, stream)
+        index, dim = self.index, self.head_dim
+        st = _launch_stream(index, stream)
         if q is None and k is None:
             raise ValueError("neither queries nor keys")
         if (k is None) != (v is None):
@@ -525,24 +534,26 @@ class Memory:
         qp = kp = vp = op = gq = gk = rot = at0 = None
         ldq = ldk = ldv = ldo = n_pos = 0
         if q is not None:
-            qp, ldq = self._rows(q, "q", rows, self.n_head)
+            heads = self.n_head
+            qp, ldq = self._rows(q, "q", rows, heads)
             if out is None:
-                out = torch.empty((rows, self.n_head, dim), dtype=self.dtype, device=dev)
-            op, ldo = self._rows(out, "out", rows, self.n_head)
+                out = _torch.empty((rows, heads, dim), dtype=self.dtype, device=self.device)
+                op, ldo = out.data_ptr(), heads * dim
+            else:
+                op, ldo = self._rows(out, "out", rows, heads)
         if k is not None:
             kp, ldk = self._rows(k, "k", rows, self.n_kv_head)
             vp, ldv = self._rows(v, "v", rows, self.n_kv_head)
         if q_gain is not None:
-            gq = _need(q_gain, "q_gain", torch.float32, (dim,), dev)
+            gq = _need(q_gain, "q_gain", _F32, (dim,), index)
         if k_gain is not None:
-            gk = _need(k_gain, "k_gain", torch.float32, (dim,), dev)
+            gk = _need(k_gain, "k_gain", _F32, (dim,), index)
         if rotation is not None:
             n_pos = rotation.shape[0]
-            rot = _need(rotation, "rotation", torch.float32, (n_pos, dim), dev)
+            rot = _need(rotation, "rotation", _F32, (n_pos, dim), index)
         if pos0 is not None:
-            at0 = _need(pos0, "pos0", torch.int32, (self.n_seq,), dev)
-        rc = self._lib.evo_memory_append(self._ref, qp, kp, vp, ldq, ldk, ldv, rows, gq, gk, eps, rot, n_pos, at0, op,
-                                         ldo, st)
+            at0 = _need(pos0, "pos0", _I32, (self.n_seq,), index)
+        rc = _lib.evo_memory_append(self._ref, qp, kp, vp, ldq, ldk, ldv, rows, gq, gk, eps, rot, n_pos, at0, op, ldo, st)
         if rc:
             _check(rc, "evo_memory_append")
         return out if q is not None else None
@@ -553,14 +564,15 @@ class Memory:
         a new tensor (rows of no sequence are left as they are: unset in a new tensor).  scale
         None: head_dim ** -0.5.  max_new, max_len: bounds on the chunks and memories (None: the
         rows, or their equal share, and what the table can hold)."""
-        torch = _torch or _load_torch()
-        dev, heads, dim = self.device, self.n_head, self.head_dim
-        st = _launch_stream(dev, stream)
+        heads, dim = self.n_head, self.head_dim
+        st = _launch_stream(self.index, stream)
         rows = q.shape[0]
         qp, ldq = self._rows(q, "q", rows, heads)
         if out is None:
-            out = torch.empty((rows, heads, dim), dtype=self.dtype, device=dev)
-        op, ldo = self._rows(out, "out", rows, heads)
+            out = _torch.empty((rows, heads, dim), dtype=self.dtype, device=self.device)
+            op, ldo = out.data_ptr(), heads * dim
+        else:
+            op, ldo = self._rows(out, "out", rows, heads)
         if rows == 0:
             return out
         if max_new is None:
@@ -569,15 +581,15 @@ class Memory:
             max_len = self.max_len
         nb = self._scratch.get((rows, max_new, max_len))
         if nb is None:
-            nb = self._scratch[rows, max_new, max_len] = self._lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
+            nb = self._scratch[rows, max_new, max_len] = _lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
         sp = None
         if nb:
-            scratch = torch.empty(nb, dtype=torch.uint8, device=dev)
+            scratch = _torch.empty(nb, dtype=_U8, device=self.device)
             sp = scratch.data_ptr()
             if stream is not None:                  # not reused before that stream's work is done
-                scratch.record_stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
-        rc = self._lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, dim ** -0.5 if scale is None else scale,
-                                         causal, window, op, ldo, sp, st)
+                scratch.record_stream(_torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+        rc = _lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, dim ** -0.5 if scale is None else scale,
+                                    causal, window, op, ldo, sp, st)
         if rc:
             _check(rc, "evo_memory_attend")
         return out

@@ -25,9 +25,12 @@
 // The scores two blocks on go into the buffer that P came from, once the product
 // that reads P is done.
 //
-// The running maximum is lazy: O is rescaled (a pass over TMEM, behind the product
-// before) only when a row's maximum grows by more than 2^8; weights are at most 2^8
-// and bf16 holds them with the same relative rounding, 2^-8 at most of each.
+// There is no running maximum: a row's reference is the maximum of its first block,
+// and every further block's weights are summed before they are handed on.  Only where
+// a sum passes 2^16 is a new maximum taken, O rescaled (a pass over TMEM, behind the
+// product before) and the block done again: the common block reads no maximum (a fifth
+// of the softmax's instructions, which bound it).  Weights are at most 2^16, and bf16
+// holds them with the same relative rounding, 2^-8 at most of each.
 //
 // Masks are looked at only in blocks that some row does not see whole.  There, the
 // values of keys outside the piece are set to zero in shared memory, and entries
@@ -46,7 +49,7 @@ namespace {
 
 constexpr int BM = 128;
 constexpr int THREADS = 384;                       // warps 10 and 11 only complete the third warpgroup
-constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
+constexpr float LAZY = 8.f;                        // log2 of how far a block's maximum passes a reference that stays
 constexpr int Q64 = BM * 128;                      // bytes of 64 columns of 128 queries
 
 template <int D>
@@ -145,11 +148,6 @@ __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 __device__ __forceinline__ float2 exp2_of(float2 x) { return make_float2(ex2_approx(x.x), ex2_approx(x.y)); }
 __device__ __forceinline__ uint32_t pack(float2 x) {
   uint32_t r;
@@ -312,7 +310,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
     see = {max(see.lo, all.lo), min(see.hi, all.hi)};
     const int from = pair ? 0 : x, by = pair ? 1 : 2;
     float top = -INFINITY;
-    float2 sums[4] = {};
+    float l = 0.f;
     bool ok = true;
     int it = 0;
     for (int i = from; i < n; i += by, ++it) {
@@ -362,57 +360,62 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
           tc::fence_async_smem();
         }
       }
-      float mx[4];                                 // chains of their own
-#pragma unroll
-      for (int j = 0; j < 4; ++j) mx[j] = v[j];
-#pragma unroll
-      for (int j = 4; j + 8 <= BN; j += 8)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx[e] = max3(mx[e], v[j + e], v[j + 4 + e]);
-      const float m = sc * fmaxf(max3(mx[0], mx[1], max3(v[BN - 4], v[BN - 3], v[BN - 2])), max3(mx[2], mx[3], v[BN - 1]));
       if (it > 0) {                                // the product before this block has read its weights
         ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], (it - 1) & 1));
         if (!ok) break;
         tc::tc_fence_after();
       }
-      const bool raise = m > top + LAZY;
-      if (__any_sync(0xffffffffu, raise)) {
-        const float now = raise ? m : top;
-        const float f = ex2_approx(top - (now == -INFINITY ? 0.f : now));
-        top = now;
+      // a row's reference is the maximum of the block where it was set.  The others are taken on
+      // trust: a block whose weights sum to more than 2^16 sets it anew and is done again
+      const float2 sc2 = make_float2(sc, sc);
+      for (bool set = __any_sync(0xffffffffu, top == -INFINITY);;) {
+        if (set) {
+          float m = v[0];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sums[j] = make_float2(sums[j].x * f, sums[j].y * f);
-        if (it > 0) {
+          for (int j = 1; j < BN; ++j) m = fmaxf(m, v[j]);
+          m *= sc;
+          const float now = m > top + LAZY ? m : top;
+          const float f = ex2_approx(top - (now == -INFINITY ? 0.f : now));
+          top = now;
+          l *= f;
+          if (it > 0) {
+#pragma unroll 1
+            for (int j = 0; j < D / 32; ++j) {
+              float o[32];
+              tmem_ld32_async(o_at + 32 * j, o);
+              tmem_wait_ld(o);
 #pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            float o[32];
-            tmem_ld32_async(o_at + 32 * j, o);
-            tmem_wait_ld(o);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] *= f;
-            tmem_st32(o_at + 32 * j, reinterpret_cast<const uint32_t*>(o));
+              for (int e = 0; e < 32; ++e) o[e] *= f;
+              tmem_st32(o_at + 32 * j, reinterpret_cast<const uint32_t*>(o));
+            }
           }
         }
-      }
-      const float ref = top == -INFINITY ? 0.f : -top;
-      const float2 sc2 = make_float2(sc, sc), ref2 = make_float2(ref, ref);
+        const float ref = top == -INFINITY ? 0.f : -top;
+        const float2 ref2 = make_float2(ref, ref);
+        float2 sums[4] = {};                       // chains of their own
 #pragma unroll
-      for (int h = 0; h < BN / 64; ++h) {
-        uint32_t p[32];
+        for (int h = 0; h < BN / 64; ++h) {
+          uint32_t p[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float2 w = exp2_of(fma2(make_float2(v[64 * h + 2 * j], v[64 * h + 2 * j + 1]), sc2, ref2));
-          sums[j % 4] = add2(sums[j % 4], w);
-          p[j] = pack(w);
+          for (int j = 0; j < 32; ++j) {
+            const float2 w = exp2_of(fma2(make_float2(v[64 * h + 2 * j], v[64 * h + 2 * j + 1]), sc2, ref2));
+            sums[j % 4] = add2(sums[j % 4], w);
+            p[j] = pack(w);
+          }
+          tmem_st32(p_at + 32 * h, p);
         }
-        tmem_st32(p_at + 32 * h, p);
+        const float2 all4 = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
+        set = __any_sync(0xffffffffu, all4.x + all4.y > 65536.f);
+        if (!set) {
+          l += all4.x + all4.y;
+          break;
+        }
       }
       tmem_wait_st();
       tc::tc_fence_before();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive1(&sh.p_full[x]);
     }
-    float l = ((sums[0].x + sums[0].y) + (sums[1].x + sums[1].y)) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
     if (ok && it > 0) ok = __all_sync(0xffffffffu, wait_for(sh, &sh.o_full[x], (it - 1) & 1));
     tc::tc_fence_after();
     bool mine = R < rows, scaled = false;
