@@ -26,9 +26,9 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include "evo_mem_ptx.cuh"
 #include "evo_memory.h"
 #include "evo_quant.cuh"
-#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
@@ -68,36 +68,6 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float2 (&v)[4]) {
   }
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-// packed arithmetic that keeps subnormals
-__device__ __forceinline__ float2 mul_pair(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 ra, rb, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n"
-      " mul.rn.f32x2 rd, ra, rb;\n mov.b64 {%0, %1}, rd;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
-      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
-
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(tc::su32(dst)),
-               "l"(src), "r"(bytes), "r"(tc::su32(bar))
-               : "memory");
-}
-// a bounded wait: false if the copies did not arrive
-__device__ __forceinline__ bool arrived(uint64_t* bar, uint32_t parity) {
-  for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
-    if (tc::mbar_test(tc::su32(bar), parity)) return true;
-  return false;
-}
-
 enum { QUERY, KEY, VALUE };
 
 // 8 + 8 values of a head (columns 8 l and D/2 + 8 l): norm, rotation and store
@@ -294,8 +264,7 @@ __global__ void __launch_bounds__(RING_THREADS, RING_BLOCKS) append_ring_kernel(
   const auto copy_data = [&](int i) {
     if (i >= count || lane != 0) return;
     const long long row = first + i;
-    uint8_t* dst = mine + i % STAGES * bytes;
-    uint64_t* bar = &full[warp][i % STAGES];
+    const uint32_t dst = tc::su32(mine + i % STAGES * bytes), bar = tc::su32(&full[warp][i % STAGES]);
     if (qb) bulk_load(dst, static_cast<const T*>(a.q) + row * a.ldq, qb, bar);
     if (kb) bulk_load(dst + qb, static_cast<const T*>(a.k) + row * a.ldk, kb, bar);
     if (kb) bulk_load(dst + qb + kb, static_cast<const T*>(a.v) + row * a.ldv, kb, bar);
@@ -308,14 +277,14 @@ __global__ void __launch_bounds__(RING_THREADS, RING_BLOCKS) append_ring_kernel(
     uint64_t* bar = &full[warp][i % STAGES];
     const int r = turn < 0 ? 0 : rb;                // a row that is not touched has none
     tc::mbar_expect_tx(bar, qb + 2 * kb + r);
-    if (r) bulk_load(mine + i % STAGES * bytes + qb + 2 * kb, a.rotation + (long long)turn * D, r, bar);
+    if (r) bulk_load(tc::su32(mine + i % STAGES * bytes + qb + 2 * kb), a.rotation + (long long)turn * D, r, tc::su32(bar));
   };
   for (int i = 0; i < STAGES; ++i) copy_rotation(i);
   bool ok = true;
   for (int i = 0; i < count && ok; ++i) {
     const int stage = i % STAGES, turn = __shfl_sync(0xffffffffu, place.turn, i);
     const int page = __shfl_sync(0xffffffffu, place.page, i), slot = __shfl_sync(0xffffffffu, place.slot, i);
-    ok = __all_sync(0xffffffffu, arrived(&full[warp][stage], (i / STAGES) & 1));
+    ok = __all_sync(0xffffffffu, wait_full(tc::su32(&full[warp][stage]), (i / STAGES) & 1));
     if (ok && turn >= 0) {
       const uint8_t* src = mine + stage * bytes;
       put_row<T, D, FORMAT>(a, reinterpret_cast<const T*>(src), reinterpret_cast<const T*>(src + qb),
@@ -325,11 +294,7 @@ __global__ void __launch_bounds__(RING_THREADS, RING_BLOCKS) append_ring_kernel(
     __syncwarp();                                   // every lane has read the stage
     if (ok) copy_data(i + STAGES), copy_rotation(i + STAGES);
   }
-  if (__syncthreads_or(!ok)) {                      // a copy did not arrive: those in flight land before the block ends
-    if (threadIdx.x == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
-    const long long t0 = clock64();
-    while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);
-  }
+  if (__syncthreads_or(!ok)) settle(a.m.status);    // a copy did not arrive
 }
 
 template <typename T, int D, int FORMAT>

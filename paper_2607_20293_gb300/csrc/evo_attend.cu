@@ -1,5 +1,11 @@
-// Attention over a paged memory: the fp32 kernel, the join of split memories
-// and the choice among the kernels.
+// Attention over a paged memory: the fp32 kernel for many rows, the expansion of
+// 8-bit pages, the join of split memories and the choice among the kernels:
+//
+//   rows a key/value head    bf16 rows                          fp32 rows
+//   up to 32 (fp32: 16)      evo_attend_rows.cu (mma.sync)      evo_attend_f32.cu
+//   more                     evo_attend_tiles.cu (tcgen05);     attend_kernel
+//                            8-bit pages from 65 rows on
+// (8-bit pages of 33 to 64 rows: two tiles of evo_attend_rows.cu).
 //
 //   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(s_j - max s),  s_j = scale log2(e) <q, k_j>
 //
@@ -10,8 +16,8 @@
 // fp32 kernel: a block of 128 threads takes 8 RM rows and 64 keys at a time; the
 // thread at (ty, tx) of an 8 x 16 grid computes RM rows x 4 keys of the scores and RM
 // rows x D/16 columns of the output.  All products are fp32 (packed in pairs: half the
-// issue slots), so that the multiply-add units bound it with many rows; with few rows
-// the blocks of a SM hide one another's loads.  There is no tensor-core form of it:
+// issue slots); the multiply-add units bound it: 1,024 rows over 4,096 keys of 64, 8
+// heads, 251 us = 34 TFLOP/s, registers leaving 12 warps a SM to hide their latency.  There is no tensor-core form of it:
 // three tf32 products for one of fp32 are 170 multiply-adds a cycle and SM, against 128.
 #include <algorithm>
 #include <cstdint>
@@ -19,8 +25,8 @@
 #include <cuda_runtime.h>
 
 #include "evo_attend.cuh"
+#include "evo_mem_ptx.cuh"
 #include "evo_quant.cuh"
-#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
@@ -47,16 +53,6 @@ __device__ __forceinline__ void copy16(float* dst, const float* src, bool on) { 
                : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-// exact products and sums of pairs, subnormals kept
-__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
-      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
 
 // (top, sum, o) joined with another piece's
 __device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 ml, float4 p) {
@@ -309,16 +305,6 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
   store_out(static_cast<T*>(a.out) + row * a.ldo + (long long)head * D + d, o, sum == 0.f ? 0.f : 1.f / sum);
 }
 
-template <int D, int FORMAT, int RM>
-cudaError_t launch_tiles(const AttendArgs& a, unsigned grid, cudaStream_t st) {
-  const auto k = attend_kernel<D, FORMAT, RM>;
-  constexpr int smem = (int)sizeof(Smem<D, RM>);
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  k<<<grid, THREADS, smem, st>>>(a);
-  return cudaGetLastError();
-}
-
 // 8-bit pages of every sequence as bf16 pages n * cols + i (i < cols: what max_len tokens fill),
 // keys and values: a power of two times a code is exact in bf16.  16 codes a thread.
 template <int D>
@@ -350,11 +336,15 @@ __global__ void __launch_bounds__(JOIN_THREADS) expand_kernel(const __grid_const
   }
 }
 
+template <int D, int FORMAT, int RM>
+cudaError_t launch_f32_as(const AttendArgs& a, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  return launch_pieces(attend_kernel<D, FORMAT, RM>, a, THREADS, (int)sizeof(Smem<D, RM>), done, st);
+}
+
 template <int D, int RM>
 cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
-  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
-  return a.m.format == EVO_CACHE_E4M3 ? launch_tiles<D, EVO_CACHE_E4M3, RM>(a, grid, st)
-                                      : launch_tiles<D, EVO_CACHE_F32, RM>(a, grid, st);
+  return a.m.format == EVO_CACHE_E4M3 ? launch_f32_as<D, EVO_CACHE_E4M3, RM>(a, st) : launch_f32_as<D, EVO_CACHE_F32, RM>(a, st);
 }
 
 template <typename T, int D>
@@ -389,9 +379,14 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   const bool tiles = !f32 && !few && (m.format == EVO_CACHE_BF16 || expand);
   p.expand = expand ? (int)cols : 0;
   p.kernel = f32 ? (few ? ATTEND_F32_ROWS : ATTEND_F32) : tiles ? ATTEND_TILES : ATTEND_ROWS;
-  p.tile_rows = f32     ? (all == 1 ? 1 : all <= 4 || few && (long long)m.n_seq * m.n_kv_head < 152 ? 4 : few ? 16 : all <= 32 || m.head_dim == 128 ? 32 : 64)
-                : tiles ? 256
-                        : (all <= 8 ? 8 : all <= 16 ? 16 : 32);
+  if (tiles)
+    p.tile_rows = 256;
+  else if (!f32)
+    p.tile_rows = all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  else if (few)   // 4 rows a tile while that fills the GPU sooner (3 x 16 rows over 333 keys: 8.3 us against 12.4 with 16)
+    p.tile_rows = all == 1 ? 1 : all <= 4 || (long long)m.n_seq * m.n_kv_head < 152 ? 4 : 16;
+  else            // 64 rows of 128 leave one block a SM
+    p.tile_rows = all <= 32 || m.head_dim == 128 ? 32 : 64;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   p.cluster = 1;

@@ -7,6 +7,7 @@
 // piece of the keys that any of them sees.
 #pragma once
 
+#include <atomic>
 #include <cuda_bf16.h>
 
 #include "evo_memory.h"
@@ -132,11 +133,22 @@ __device__ __forceinline__ void join_cluster(const AttendArgs& a, const Tile& t,
   cluster_arrive_wait();                           // no block ends while another reads its shared memory
 }
 
+// lets a kernel have this much dynamic shared memory; `done`: a bit for each device where it has it
+template <typename K>
+cudaError_t allow_smem(K kernel, int smem, std::atomic<uint64_t>& done) {
+  int dev;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1))) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
+
 // launches a block a piece, the pieces of a cluster as one
 template <typename... K, typename... A>
-cudaError_t launch_pieces(void (*kernel)(K...), const AttendArgs& a, int threads, int smem, cudaStream_t st, const A&... args) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess && a.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+cudaError_t launch_pieces(void (*kernel)(K...), const AttendArgs& a, int threads, int smem, std::atomic<uint64_t>& done,
+                          cudaStream_t st, const A&... args) {
+  const cudaError_t e = allow_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);

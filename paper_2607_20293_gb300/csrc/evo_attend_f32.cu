@@ -21,8 +21,8 @@
 #include <cuda_runtime.h>
 
 #include "evo_attend.cuh"
+#include "evo_mem_ptx.cuh"
 #include "evo_quant.cuh"
-#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
@@ -43,74 +43,6 @@ struct Cfg {
   static constexpr int SCALES = E4M3 ? STAGES * 2 * RUN : 0;
   static constexpr int SMEM = 1024 + WARPS * (RING + P + SCALES) + R * D * 4;
 };
-
-__device__ __forceinline__ float4 lds_f4(uint32_t p) {
-  float4 v;
-  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ float2 lds_f2(uint32_t p) {
-  float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ uint4 lds_u4(uint32_t p) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds_u32(uint32_t p) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds_u16(uint32_t p) {
-  uint16_t v;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds_u8(uint32_t p) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ void sts_f4(uint32_t p, float4 v) {
-  asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
-}
-__device__ __forceinline__ void sts_f1(uint32_t p, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(p), "f"(v) : "memory"); }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
-__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
-          "r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-// a bounded wait: false if the copies did not arrive
-__device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
-  for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
-    if (tc::mbar_test(bar, parity)) return true;
-  return false;
-}
-// byte offset of 16-byte chunk `chunk` of key r in a tile (boxes of at most 128 bytes, one behind the other)
-template <int ROW>
-__device__ __forceinline__ int chunk_at(int r, int chunk) {
-  if constexpr (ROW == 64) return r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4);
-  return (chunk >> 3) * (RUN * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
-}
-// a * b + c of pairs, subnormals kept
-__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n .reg .b64 ra, rb, rc, rd;\n mov.b64 ra, {%2, %3};\n mov.b64 rb, {%4, %5};\n mov.b64 rc, {%6, %7};\n"
-      " fma.rn.f32x2 rd, ra, rb, rc;\n mov.b64 {%0, %1}, rd;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
 
 template <int D, bool E4M3, int R>
 __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(const __grid_constant__ AttendArgs a,
@@ -207,10 +139,10 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
     for (int ch = 0; ch < C::ROW / 16; ++ch) {
       float4 k[E4M3 ? 4 : 1];
       if constexpr (E4M3) {
-        const uint4 u = lds_u4(kt + chunk_at<C::ROW>(lane, ch));
+        const uint4 u = lds128(kt + chunk_at<C::ROW, RUN>(lane, ch));
         k[0] = codes4(u.x), k[1] = codes4(u.y), k[2] = codes4(u.z), k[3] = codes4(u.w);
       } else {
-        k[0] = lds_f4(kt + chunk_at<C::ROW>(lane, ch));
+        k[0] = lds_f4(kt + chunk_at<C::ROW, RUN>(lane, ch));
       }
 #pragma unroll
       for (int e = 0; e < (E4M3 ? 4 : 1); ++e)
@@ -222,7 +154,7 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
         }
     }
     float ks = a.scale_log2, vs = 1.f;
-    if constexpr (E4M3) ks *= scale_value(lds_u8(sc + lane)), vs = scale_value(lds_u8(sc + RUN + lane));
+    if constexpr (E4M3) ks *= scale_value(lds8(sc + lane)), vs = scale_value(lds8(sc + RUN + lane));
     float s[R];
     bool raise = false;
 #pragma unroll
@@ -265,14 +197,14 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
         const int r = j + e;
         if constexpr (E4M3) {                      // 2 or 4 codes of the row
           const int b = lane * 2 * PD;
-          const uint32_t at = vt + chunk_at<C::ROW>(r, b / 16) + b % 16;
-          const float4 x = codes4(PD == 1 ? lds_u16(at) : lds_u32(at));
+          const uint32_t at = vt + chunk_at<C::ROW, RUN>(r, b / 16) + b % 16;
+          const float4 x = codes4(PD == 1 ? lds16(at) : lds32(at));
           v[e][0] = make_float2(x.x, x.y);
           if constexpr (PD == 2) v[e][1] = make_float2(x.z, x.w);
         } else if constexpr (PD == 1) {
-          v[e][0] = lds_f2(vt + chunk_at<C::ROW>(r, lane / 2) + 8 * (lane % 2));
+          v[e][0] = lds_f2(vt + chunk_at<C::ROW, RUN>(r, lane / 2) + 8 * (lane % 2));
         } else {
-          const float4 x = lds_f4(vt + chunk_at<C::ROW>(r, lane));
+          const float4 x = lds_f4(vt + chunk_at<C::ROW, RUN>(r, lane));
           v[e][0] = make_float2(x.x, x.y);
           v[e][1] = make_float2(x.z, x.w);
         }
@@ -296,11 +228,8 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
     }
     if (++stage == STAGES) stage = 0, phase ^= 1;
   }
-  if (__syncthreads_or(dead)) {                    // a copy did not arrive: nothing more is asked for
-    if (tid == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
-    const long long t0 = clock64();
-    while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);   // those in flight land before the block ends
-  }
+  if (__syncthreads_or(dead)) settle(a.m.status);  // a copy did not arrive: nothing more was asked for
+
   // the warps' sums, each in its own part of the ring
   float* const mine = reinterpret_cast<float*>(mem + warp * C::RING);
 #pragma unroll
@@ -345,7 +274,8 @@ cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
   CUtensorMap km, vm;
   const int box = std::min(a.m.page_tokens, RUN);
   if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
-  return launch_pieces(f32_rows_kernel<D, E4M3, R>, a, C::THREADS, C::SMEM, st, km, vm);
+  static std::atomic<uint64_t> done{0};
+  return launch_pieces(f32_rows_kernel<D, E4M3, R>, a, C::THREADS, C::SMEM, done, st, km, vm);
 }
 
 template <int R>

@@ -48,8 +48,8 @@
 #include <cuda_runtime.h>
 
 #include "evo_attend.cuh"
+#include "evo_mem_ptx.cuh"
 #include "evo_quant.cuh"
-#include "evo_tc.cuh"
 
 namespace evo {
 namespace {
@@ -114,47 +114,6 @@ __device__ __forceinline__ uint32_t pack(float a, float b, bool half) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
   return r;
 }
-__device__ __forceinline__ uint4 lds128(uint32_t p) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t p) {
-  uint2 v;
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t lds8(uint32_t p) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p));
-  return v;
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
-__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::
-          "r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-// a bounded wait: false if the copies did not arrive
-__device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
-  for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
-    if (tc::mbar_test(bar, parity)) return true;
-  return false;
-}
-
-// byte offset of 16-byte chunk `chunk` of row r in a tile of ROWS rows (boxes of at most 128 bytes, one behind the other)
-template <int ROW, int ROWS>
-__device__ __forceinline__ int chunk_at(int r, int chunk) {
-  if constexpr (ROW == 64) return r * 64 + ((chunk ^ ((r >> 1) & 3)) << 4);
-  return (chunk >> 3) * (ROWS * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4);
-}
-
 __device__ __forceinline__ uint32_t finite_halves(uint32_t w, bool* bad) {
   uint32_t keep = 0xffffffffu;
   if ((w & 0x7f80u) == 0x7f80u) keep &= 0xffff0000u;
@@ -521,11 +480,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
     __syncwarp();                                            // every lane has read the stage
     if (++stage == STAGES) stage = 0, phase ^= 1;
   }
-  if (__syncthreads_or(dead)) {                              // a copy did not arrive: nothing more is asked for
-    if (tid == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
-    const long long t0 = clock64();
-    while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);   // those in flight land before the block ends
-  }
+  if (__syncthreads_or(dead)) settle(a.m.status);            // a copy did not arrive: nothing more was asked for
 
   // this warp's sums to its part of the ring: [row][dimension]; tile j holds, in its rows g and
   // g + 8, dimensions D/8 g + 2 j and the next (8-bit), 64 (j / 4) + 8 g + 2 (j % 4) and the next (bf16)
@@ -602,7 +557,8 @@ cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
   CUtensorMap km, vm;
   const int box = std::min(a.m.page_tokens, C::RUN);
   if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
-  return launch_pieces(rows_kernel<D, E4M3, NR>, a, THREADS, C::SMEM, st, km, vm);
+  static std::atomic<uint64_t> done{0};
+  return launch_pieces(rows_kernel<D, E4M3, NR>, a, THREADS, C::SMEM, done, st, km, vm);
 }
 
 template <int NR>

@@ -6,24 +6,27 @@
 // the measured bf16 rate, against 512 cycles for their 16,384 exponentials (32 a
 // cycle and SM) and about 600 issue cycles a scheduler for the rest of the softmax.
 // All three have to run at once.  A block keeps two streams of tiles in flight, and of
-// each stream the scores of two blocks of 64 keys: while the softmax works on one, the
-// tensor cores have the other and the output of the one before.
+// each stream the next scores start as soon as the softmax has loaded these to registers:
 //   * more than 128 rows: the streams are two tiles of 128 rows over the same keys;
 //   * else: both are the same rows, over the even and the odd blocks of keys, and
 //     are joined at the end.
-// Blocks of 128 keys, one of a stream at a time, leave the softmax waiting for the
-// tensor cores and back (2,048 rows over 16,384 keys: 99 us against FIGURE).
 // Roles: warps 0-3 and 4-7 are the softmax of streams A and B, a thread a row (the
-// thread-per-lane layout of tensor memory: no reduction over lanes anywhere); warp 8
-// issues the MMAs; warp 9 brings keys and values, 64 at a time, by tiled bulk copies
-// into a ring.
+// thread-per-lane layout of tensor memory: no reduction over lanes anywhere); warps 8
+// and 10 issue a stream's MMAs each, so that neither waits for the other's weights; warp
+// 9 brings keys and values, a block of BN at a time, by tiled bulk copies into a ring.
 //
 //   S = Q K^T      both operands from shared memory, 128-byte swizzle, fp32 in TMEM
-//   P = 2^(S - m)  read from TMEM, written back to it as bf16 over S
+//   P = 2^(S - m)  read from TMEM, written back to it as bf16, beside S
 //   O += P V       P from TMEM, V as it lies in its page (rows of keys: the operand
 //                  whose contiguous index is N)
-// The scores two blocks on go into the buffer that P came from, once the product
-// that reads P is done.
+// BN is what 512 columns of tensor memory hold of S, P and O of two streams: 128 keys
+// of 64, 64 keys of 128.  Measured (2,048 rows over 16,384 keys of 64, 8 heads / four
+// causal chunks of 1,000 tokens over 8,000, heads of 128): 86 us = 0.80 PFLOP/s / 137 us =
+// 0.86; weights over the scores, so that the next ones wait for the product, 99 / 147; one
+// issuing warp that takes both streams in turn 114 / 150.  What bounds it now is the
+// softmax's issue: its two warps a scheduler are 85 % of the special-function unit while
+// both are at their exponentials, and wait side by side when they are not (alternating them
+// by a barrier, or a polynomial for some of the exponentials, measured slower).
 //
 // There is no running maximum: a row's reference is the maximum of its first block,
 // and every further block's weights are summed before they are handed on.  Only where
@@ -42,7 +45,7 @@
 #include <cuda_runtime.h>
 
 #include "evo_attend.cuh"
-#include "evo_tc.cuh"
+#include "evo_mem_ptx.cuh"
 
 namespace evo {
 namespace {
@@ -507,9 +510,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
   __syncthreads();
   tc::tc_fence_after();
   if (sh.dead) {                                   // a wait was in vain: what is in flight lands before memory is given back
-    if (tid == 0 && a.m.status) *a.m.status = EVO_ERR_TIMEOUT;
-    const long long t0 = clock64();
-    while (clock64() - t0 < SETTLE_CYCLES) __nanosleep(1000);
+    settle(a.m.status);
     __syncthreads();
   }
   if (warp == 0) tc::tmem_dealloc(tmem, 512);
@@ -518,15 +519,11 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
 template <int D>
 cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
   using C = Cfg<D>;
-  const auto k = tiles_kernel<D>;
-  const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-  if (e != cudaSuccess) return e;
   CUtensorMap km, vm;
   const int box = std::min(a.m.page_tokens, C::BN);
   if (!page_map(&km, a.m, a.m.k_pages, box) || !page_map(&vm, a.m, a.m.v_pages, box)) return cudaErrorInvalidValue;
-  const unsigned grid = (unsigned)((long long)a.m.n_seq * a.m.n_kv_head * a.tiles * a.splits);
-  k<<<grid, THREADS, C::SMEM, st>>>(a, km, vm);
-  return cudaGetLastError();
+  static std::atomic<uint64_t> done{0};
+  return launch_pieces(tiles_kernel<D>, a, THREADS, C::SMEM, done, st, km, vm);
 }
 
 }  // namespace
