@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, R>::THREADS) f32_rows_kernel(cons
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   const uint32_t ring = tc::su32(mem) + warp * C::RING, psm = tc::su32(mem) + WARPS * C::RING + warp * C::P;
   const uint32_t qsm = tc::su32(mem) + WARPS * (C::RING + C::P), ssm = qsm + R * D * 4 + warp * C::SCALES;
+  if (tid == 0) fetch_map(&kmap), fetch_map(&vmap);
   const Tile t = tile_of_block(a);
   const int rows = t.count * a.group, r0 = t.tile * R;
   if (r0 >= rows) return;

@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
   const uint32_t ring = tc::su32(mem) + warp * C::RING;
   const uint32_t qsm = tc::su32(mem) + WARPS * C::RING;
   const uint32_t ssm = qsm + C::QB + warp * (STAGES * 2 * RUN);
+  if (tid == 0) fetch_map(&kmap), fetch_map(&vmap);
   const Tile t = tile_of_block(a);
   const int rows = t.count * a.group, r0 = t.tile * ROWS;
   if (r0 >= rows) return;

@@ -169,6 +169,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   uint8_t* const ring = mem + 2 * C::QTILE;
+  if (tid == 0) fetch_map(&kmap), fetch_map(&vmap);
   const Tile t = tile_of_block(a);
   const int rows = t.count * a.group, r0 = t.tile * 2 * BM;
   if (r0 >= rows) return;

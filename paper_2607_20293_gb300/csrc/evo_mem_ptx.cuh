@@ -60,6 +60,10 @@ __device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, 
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
       : "memory");
 }
+// a tensor map on its way to the copy unit while the first coordinates are looked up
+__device__ __forceinline__ void fetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
 // a bounded wait: false if the copies did not arrive
 __device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
   for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
