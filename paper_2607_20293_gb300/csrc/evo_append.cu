@@ -304,7 +304,8 @@ cudaError_t launch_as(const AppendArgs& a, cudaStream_t st) {
   const int warps = 152 * RING_WARPS * blocks;      // resident at once
   if (blocks >= 2 && a.rows >= 2 * warps) {
     const auto k = append_ring_kernel<T, D, FORMAT>;
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static std::atomic<uint64_t> done{0};           // the most that a call takes: calls of other sizes may launch meanwhile
+    const cudaError_t e = allow_smem(k, 110 * 1024, done);
     if (e != cudaSuccess) return e;
     const int each = std::min(32, (a.rows + warps - 1) / warps);
     const int need = (a.rows + each - 1) / each;

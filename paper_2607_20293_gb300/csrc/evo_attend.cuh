@@ -7,7 +7,6 @@
 // piece of the keys that any of them sees.
 #pragma once
 
-#include <atomic>
 #include <cuda_bf16.h>
 
 #include "evo_memory.h"
@@ -131,17 +130,6 @@ __device__ __forceinline__ void join_cluster(const AttendArgs& a, const Tile& t,
     put_result<T, D>(a, t, R, d, x, m, l);
   }
   cluster_arrive_wait();                           // no block ends while another reads its shared memory
-}
-
-// lets a kernel have this much dynamic shared memory; `done`: a bit for each device where it has it
-template <typename K>
-cudaError_t allow_smem(K kernel, int smem, std::atomic<uint64_t>& done) {
-  int dev;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1))) return e;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
-  return e;
 }
 
 // launches a block a piece, the pieces of a cluster as one

@@ -2,6 +2,7 @@
 // arguments of their kernels and the host functions that launch them.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -65,6 +66,17 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
 // tensor map of a pool of pages: its rows (a token of a head each) in boxes of
 // box_rows rows x 128 bytes (64 where a row has no more), swizzled by the box's width
 bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows);
+
+// lets a kernel have this much dynamic shared memory; `done`: a bit for each device where it has it
+template <typename K>
+cudaError_t allow_smem(K kernel, int smem, std::atomic<uint64_t>& done) {
+  int dev;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1))) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
 
 // ---------------------------------------------------------------- device helpers
 

@@ -547,6 +547,35 @@ def test_captured_replayed_and_repeated(torch, B, dtype, fmt, m, length):
     w.check_attend(outs[0], q=q)
 
 
+def test_appends_of_two_host_threads(torch, B):
+    """Long chunks of different widths appended from two threads at once, each on its own stream."""
+    import threading
+    jobs = []
+    for hq, hk, D in ((8, 2, 128), (2, 1, 128)):
+        w = World(torch, [6400] * 2, [6400] * 2, hq, hk, D, 128, "bf16", "bf16", seed=hq, stale=None)
+        mem, st = w.device(B), torch.cuda.Stream()
+        args = [t.cuda() for t in (w.q, w.k, w.v)]
+        want = mem.append(*args)
+        jobs.append((mem, st, args, want, []))
+    torch.cuda.synchronize()
+
+    def run(mem, st, args, want, got):
+        try:
+            with torch.cuda.stream(st):
+                for _ in range(200):
+                    got[:] = [mem.append(*args)]
+        except Exception as e:                                     # noqa: BLE001
+            got[:] = [e]
+    threads = [threading.Thread(target=run, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for _, _, _, want, got in jobs:
+        assert torch.is_tensor(got[0]) and torch.equal(got[0], want), got[0]
+
+
 def test_a_stream_given_by_the_caller(torch, B):
     w = World(torch, [3000], [1], 4, 2, 64, 64, "bf16", "e4m3")
     mem = w.device(B, starts=False)
