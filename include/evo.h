@@ -344,12 +344,12 @@ enum { EVO_CACHE_F32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_E4M3 = 2 };
 typedef struct evo_memory {
   int32_t dtype;            /* EVO_DTYPE_* of the rows */
   int32_t format;           /* EVO_CACHE_* of the pages: E4M3, or the one that matches dtype */
-  int32_t n_head;           /* query heads, a multiple of n_kv_head */
+  int32_t n_head;           /* query heads, a multiple of n_kv_head, at most 1024 */
   int32_t n_kv_head;        /* key/value heads; query head h reads key/value head h * n_kv_head / n_head */
   int32_t head_dim;         /* 64 or 128 */
   int32_t page_tokens;      /* 16, 32, 64 or 128 */
-  int32_t n_pages;          /* pages of the pool */
-  int32_t max_pages;        /* columns of the table; max_pages * page_tokens < 2^31 */
+  int32_t n_pages;          /* pages of the pool; n_pages * n_kv_head * page_tokens < 2^31 */
+  int32_t max_pages;        /* columns of the table; max_pages * page_tokens at most 2^30 */
   int32_t n_seq;
   int32_t pad_;
   void *k_pages, *v_pages;  /* device [n_pages][n_kv_head][page_tokens][head_dim], start on 16 bytes */

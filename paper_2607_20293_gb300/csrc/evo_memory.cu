@@ -83,7 +83,8 @@ evo_status memory_ok(const evo_memory* m) {
   if (m->head_dim != 64 && m->head_dim != 128) return EVO_ERR_SHAPE;
   if (m->n_head % m->n_kv_head || m->n_head > 1024) return EVO_ERR_SHAPE;
   if (m->page_tokens != 16 && m->page_tokens != 32 && m->page_tokens != 64 && m->page_tokens != 128) return EVO_ERR_SHAPE;
-  if (m->max_pages > INT_MAX / m->page_tokens) return EVO_ERR_SHAPE;
+  // 2^30 tokens: the kernels look runs ahead in 32 bits
+  if (m->max_pages > (1 << 30) / m->page_tokens) return EVO_ERR_SHAPE;
   if ((long long)m->n_pages * m->n_kv_head * m->page_tokens > INT_MAX) return EVO_ERR_SHAPE;
   if (!m->k_pages || !m->v_pages || !m->table || !m->lens) return EVO_ERR_ARG;
   if (!aligned(m->k_pages, 16) || !aligned(m->v_pages, 16)) return EVO_ERR_ARG;

@@ -43,7 +43,7 @@ BAD_VIEWS = [
     (dict(head_dim=96), "SHAPE"), (dict(n_head=7), "SHAPE"), (dict(n_head=0), "ARG"), (dict(n_kv_head=-1), "ARG"),
     (dict(n_head=2048, n_kv_head=1), "SHAPE"), (dict(page_tokens=8), "SHAPE"), (dict(page_tokens=48), "SHAPE"),
     (dict(page_tokens=256), "SHAPE"), (dict(n_pages=0), "ARG"), (dict(max_pages=0), "ARG"),
-    (dict(max_pages=1 << 27), "SHAPE"), (dict(n_pages=1 << 27), "SHAPE"), (dict(n_seq=-1), "ARG"),
+    (dict(max_pages=1 << 27), "SHAPE"), (dict(max_pages=(1 << 26) + 1), "SHAPE"), (dict(n_pages=1 << 27), "SHAPE"), (dict(n_seq=-1), "ARG"),
     (dict(k_pages=None), "ARG"), (dict(v_pages=P + 8), "ARG"), (dict(k_scales=None), "ARG"), (dict(table=None), "ARG"),
     (dict(lens=None), "ARG"), (dict(format=1), "ARG"),
 ]
@@ -96,6 +96,12 @@ def test_a_split_memory_needs_scratch(B):
     assert nb > 0 and nb % 4 == 0
     assert attend(B, m, rows=3, max_new=1, max_len=65536, scratch=None) == B.ERR_ARG
     assert attend(B, m, rows=3, max_new=1, max_len=65536, scratch=P + 4) == B.ERR_ARG
+
+
+def test_a_memory_of_the_most_tokens_is_planned(B):
+    m = view(B, max_pages=1 << 26)
+    assert B.load().evo_memory_scratch_bytes(ctypes.byref(m), 3, 1, 1 << 30) > 0
+    assert attend(B, m, rows=3, max_new=1, max_len=1 << 30, scratch=None) == B.ERR_ARG
 
 
 def test_calls_without_rows_do_nothing(B):
