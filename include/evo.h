@@ -372,13 +372,14 @@ evo_status evo_rotation_table(int32_t n_pos, int32_t head_dim, double base, floa
  *   q, k, v  device [rows][heads][head_dim], ld* elements between rows (so that they
  *            may be column ranges of one projection).  q NULL: only keys and values
  *            are appended; k and v NULL: only queries are made
- *   q_out    device [rows][n_head][head_dim], ldo between rows; may be q
+ *   q_out    device [rows][n_head][head_dim], ldo between rows; may be q (with ldo =
+ *            ldq), and otherwise shares no byte with q, k or v (EVO_ERR_ARG)
  *   q_gain, k_gain  device [head_dim] fp32 or NULL (no norm)
  *   rotation device [n_pos][head_dim] fp32 (evo_rotation_table) or NULL
  *   pos0     device [n_seq] or NULL (zero): position of a memory's token 0, so that a
  *            memory whose oldest pages were dropped keeps its positions
  * Buffers start on 16 bytes and row strides are multiples of 16 bytes, at least
- * a row (EVO_ERR_ARG).  Two rows of a call must not be the same token of the same
+ * a row and below 2^31 elements (EVO_ERR_ARG).  Two rows of a call must not be the same token of the same
  * page (sequences that share their last page are not appended to in one call).
  * Asynchronous on the stream. */
 evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k, const void* v, int64_t ldq,
@@ -393,7 +394,8 @@ evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k
  * of those.  A row that sees no key is zero; what a masked token holds (a NaN,
  * too) reaches no row that does not see it.
  *   q, out  device [rows][n_head][head_dim], ldq / ldo elements between rows; start
- *           on 16 bytes, strides multiples of 16 bytes.  They must not overlap
+ *           on 16 bytes, strides multiples of 16 bytes.  They share no byte
+ *           (EVO_ERR_ARG; column ranges of one buffer may interleave)
  *   max_new, max_len  at least the largest chunk and memory of the call: they size the
  *           launch, nothing else depends on them
  *   scratch device, evo_memory_scratch_bytes(mem, rows, max_new, max_len) bytes,

@@ -97,7 +97,20 @@ evo_status memory_ok(const evo_memory* m) {
 // rows of `heads` heads, ld elements apart
 bool rows_ok(const evo_memory* m, const void* p, int64_t ld, int heads) {
   const int item = m->dtype == EVO_DTYPE_F32 ? 4 : 2;
-  return aligned(p, 16) && ld >= (int64_t)heads * m->head_dim && ld * item % 16 == 0;
+  return aligned(p, 16) && ld >= (int64_t)heads * m->head_dim && ld <= INT_MAX && ld * item % 16 == 0;
+}
+
+// do `rows` rows of a_heads heads, lda elements apart, at a share a byte with those at b?  (Column
+// ranges of one buffer interleave without doing so.)
+bool rows_overlap(const evo_memory* m, const void* a, int64_t lda, int a_heads, const void* b, int64_t ldb, int b_heads,
+                  int32_t rows) {
+  const uint64_t item = m->dtype == EVO_DTYPE_F32 ? 4 : 2, wide_a = a_heads * m->head_dim * item, wide_b = b_heads * m->head_dim * item;
+  const uint64_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const uint64_t end_a = x + (rows - 1) * lda * item + wide_a, end_b = y + (rows - 1) * ldb * item + wide_b;
+  if (end_a <= y || end_b <= x) return false;
+  if (lda != ldb) return true;
+  const uint64_t step = lda * item, at = x <= y ? (y - x) % step : (step - (x - y) % step) % step;   // b's column, a's being 0
+  return at < wide_a || at + wide_b > step;
 }
 
 // rows of a call: none, or chunks that the sequences can have
@@ -172,6 +185,11 @@ evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k
   if (rows == 0 || (!q && !k)) return EVO_OK;
   if (q && (!rows_ok(mem, q, ldq, mem->n_head) || !rows_ok(mem, q_out, ldo, mem->n_head))) return EVO_ERR_ARG;
   if (k && (!rows_ok(mem, k, ldk, mem->n_kv_head) || !rows_ok(mem, v, ldv, mem->n_kv_head))) return EVO_ERR_ARG;
+  // queries may be overwritten in place (a warp reads what it writes), nothing else that the call reads
+  if (q && (q_out != q || ldo != ldq) && rows_overlap(mem, q_out, ldo, mem->n_head, q, ldq, mem->n_head, rows)) return EVO_ERR_ARG;
+  if (q && k && (rows_overlap(mem, q_out, ldo, mem->n_head, k, ldk, mem->n_kv_head, rows) ||
+                 rows_overlap(mem, q_out, ldo, mem->n_head, v, ldv, mem->n_kv_head, rows)))
+    return EVO_ERR_ARG;
   if (!aligned(rotation, 16) || !aligned(q_gain, 16) || !aligned(k_gain, 16)) return EVO_ERR_ARG;
   const AppendArgs a{*mem, q, k, v, q_out, ldq, ldk, ldv, ldo, rows, q_gain, k_gain, eps, rotation, n_pos, pos0};
   EVO_CUDA(launch_append(a, reinterpret_cast<cudaStream_t>(stream)));
@@ -193,6 +211,7 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
   if (s != EVO_OK) return s;
   if (!q || !out || !std::isfinite(scale) || (causal != 0 && causal != 1) || window < 0) return EVO_ERR_ARG;
   if (!rows_ok(mem, q, ldq, mem->n_head) || !rows_ok(mem, out, ldo, mem->n_head)) return EVO_ERR_ARG;
+  if (rows_overlap(mem, q, ldq, mem->n_head, out, ldo, mem->n_head, rows)) return EVO_ERR_ARG;
   const AttendPlan p = plan_attend(*mem, rows, max_new, max_len);
   if (p.scratch && (!scratch || !aligned(scratch, 16))) return EVO_ERR_ARG;
   AttendArgs a{};

@@ -547,6 +547,26 @@ def test_captured_replayed_and_repeated(torch, B, dtype, fmt, m, length):
     w.check_attend(outs[0], q=q)
 
 
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+def test_queries_in_place_and_outputs_beside_them(torch, B, dtype, fmt):
+    """One buffer of rows holds queries, keys, values and outputs: queries are turned in place, outputs interleave."""
+    hq, hk, D = 8, 2, 64
+    w = World(torch, [300, 40], [70, 3], hq, hk, D, 32, dtype, fmt, seed=5)
+    a, b = w.device(B), World(torch, [300, 40], [70, 3], hq, hk, D, 32, dtype, fmt, seed=5)
+    rot = torch.from_numpy(B.rotation_table(300, D)).cuda()
+    want = a.append(w.q.cuda(), w.k.cuda(), w.v.cuda(), rotation=rot)
+    out = a.attend(want, max_new=70)
+    wide = torch.cat([w.q, w.k, w.v, torch.zeros_like(w.q)], 1).cuda()
+    q, k, v, o = wide[:, :hq], wide[:, hq:hq + hk], wide[:, hq + hk:hq + 2 * hk], wide[:, hq + 2 * hk:]
+    mem = b.device(B)
+    mem.append(q, k, v, rotation=rot, out=q)
+    mem.attend(q, max_new=70, out=o)
+    assert torch.equal(q, want) and torch.equal(o, out)
+    assert torch.equal(k.cpu(), w.k) and torch.equal(v.cpu(), w.v)
+    with pytest.raises(B.EvoError):
+        mem.attend(q, max_new=70, out=q)
+
+
 def test_appends_of_two_host_threads(torch, B):
     """Long chunks of different widths appended from two threads at once, each on its own stream."""
     import threading

@@ -25,13 +25,13 @@ def view(B, **over):
     return m
 
 
-def append(B, m, q=P, k=P, v=P, ldq=512, ldk=128, ldv=128, rows=6, eps=1e-6, rotation=None, n_pos=0, pos0=None, out=P,
+def append(B, m, q=P, k=3 * P, v=4 * P, ldq=512, ldk=128, ldv=128, rows=6, eps=1e-6, rotation=None, n_pos=0, pos0=None, out=P,
            ldo=512, gain=None):
     return B.load().evo_memory_append(ctypes.byref(m), q, k, v, ldq, ldk, ldv, rows, gain, gain, eps, rotation, n_pos,
                                       pos0, out, ldo, None)
 
 
-def attend(B, m, q=P, ldq=512, rows=6, max_new=6, max_len=64, scale=0.125, causal=1, window=0, out=P, ldo=512,
+def attend(B, m, q=P, ldq=512, rows=6, max_new=6, max_len=64, scale=0.125, causal=1, window=0, out=2 * P, ldo=512,
            scratch=P):
     return B.load().evo_memory_attend(ctypes.byref(m), q, ldq, rows, max_new, max_len, scale, causal, window, out, ldo,
                                       scratch, None)
@@ -81,6 +81,18 @@ def test_append_arguments(B, over, code):
     (dict(causal=2), "ARG"), (dict(window=-1), "ARG"), (dict(rows=1 << 28, max_new=1), "SHAPE")])
 def test_attend_arguments(B, over, code):
     assert attend(B, view(B), **over) == getattr(B, "ERR_" + code)
+
+
+def test_outputs_that_overlap_what_is_read(B):
+    """8 query heads of 64 bf16 are 1,024 bytes, 2 key heads 256; 6 rows."""
+    m = view(B)
+    for over in (dict(), dict(out=P + 16), dict(out=P + 5 * 1024), dict(out=P - 5 * 1024), dict(ldq=1024, ldo=1024, out=P + 1008),
+                 dict(ldq=1024, ldo=1024, out=P - 1008), dict(ldq=520, ldo=512, out=P + 1024), dict(ldq=1024, out=P + 1024)):
+        assert attend(B, m, **(dict(out=P) | over)) == B.ERR_ARG, over
+    far = dict(k=P + 20480, v=P + 40960)
+    for over in (dict(out=P + 1024), dict(out=P - 1024), dict(out=P, ldo=520), dict(out=P + 20480), dict(out=P + 40960 - 6 * 1024 + 16),
+                 dict(ldq=768, ldk=768, ldv=768, k=P + 1024, v=P + 1280, out=P + 16, ldo=768)):
+        assert append(B, m, **(far | over)) == B.ERR_ARG, over
 
 
 def test_equal_chunks_have_to_divide(B):
