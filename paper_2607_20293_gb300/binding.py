@@ -410,12 +410,21 @@ def _launch_stream(index: int, stream):
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+def _new(shape, dtype, device, stream):
+    """A tensor from the pool of the stream that the call runs on: one of another stream's pool may
+    still be in use there."""
+    if stream is None:
+        return _torch.empty(shape, dtype=dtype, device=device)
+    with _torch.cuda.stream(_torch.cuda.ExternalStream(stream, device) if isinstance(stream, int) else stream):
+        return _torch.empty(shape, dtype=dtype, device=device)
+
+
 def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
     """evo_cache_write: the residual r [N][H][E] (fp32 or bf16) to the unit's 8-bit
     cache (codes [N][H][E], scales [N][H][E/32], uint8) for the samples whose
     refresh [N] (uint8) is not zero, or all.  Returns y = x + r for those samples
     and x for the others (in `out`, which may be x), or None without x."""
-    torch = _torch or _load_torch()
+    _torch or _load_torch()
     index, dtype, shape = r.get_device(), r.dtype, r.shape
     st = _launch_stream(index, stream)
     if dtype is not _F32 and dtype is not _BF16:
@@ -425,7 +434,7 @@ def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
     if x is not None:
         xp = _need(x, "x", _F32, shape, index)
         if out is None:
-            out = torch.empty_like(x)
+            out = _new(shape, _F32, x.device, stream)
             yp = out.data_ptr()
         else:
             yp = _need(out, "out", _F32, shape, index)
@@ -444,14 +453,14 @@ def cache_add(codes, scales, x, reuse=None, out=None, stream=None):
     """evo_cache_add: x [N][H][E] (fp32) plus the cached values of a run of units
     (codes [U][N][H][E], scales [U][N][H][E/32]) where reuse [U][N] is not zero, or
     of all; in `out` (which may be x) or a new tensor."""
-    torch = _torch or _load_torch()
+    _torch or _load_torch()
     index, shape = x.get_device(), x.shape
     st = _launch_stream(index, stream)
     N, H, E = shape
     U = codes.shape[0]
     xp = _need(x, "x", _F32, shape, index)
     if out is None:
-        out = torch.empty_like(x)
+        out = _new(shape, _F32, x.device, stream)
         yp = out.data_ptr()
     else:
         yp = _need(out, "out", _F32, shape, index)
@@ -537,7 +546,7 @@ class Memory:
             heads = self.n_head
             qp, ldq = self._rows(q, "q", rows, heads)
             if out is None:
-                out = _torch.empty((rows, heads, dim), dtype=self.dtype, device=self.device)
+                out = _new((rows, heads, dim), self.dtype, self.device, stream)
                 op, ldo = out.data_ptr(), heads * dim
             else:
                 op, ldo = self._rows(out, "out", rows, heads)
@@ -569,7 +578,7 @@ class Memory:
         rows = q.shape[0]
         qp, ldq = self._rows(q, "q", rows, heads)
         if out is None:
-            out = _torch.empty((rows, heads, dim), dtype=self.dtype, device=self.device)
+            out = _new((rows, heads, dim), self.dtype, self.device, stream)
             op, ldo = out.data_ptr(), heads * dim
         else:
             op, ldo = self._rows(out, "out", rows, heads)
@@ -581,13 +590,13 @@ class Memory:
             max_len = self.max_len
         nb = self._scratch.get((rows, max_new, max_len))
         if nb is None:
+            if len(self._scratch) >= 1024:          # max_len may grow with every token
+                self._scratch.clear()
             nb = self._scratch[rows, max_new, max_len] = _lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
         sp = None
         if nb:
-            scratch = _torch.empty(nb, dtype=_U8, device=self.device)
+            scratch = _new(nb, _U8, self.device, stream)   # back in that pool once this returns, for later work of the stream
             sp = scratch.data_ptr()
-            if stream is not None:                  # not reused before that stream's work is done
-                scratch.record_stream(_torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
         rc = _lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, dim ** -0.5 if scale is None else scale,
                                     causal, window, op, ldo, sp, st)
         if rc:

@@ -607,6 +607,41 @@ def test_a_stream_given_by_the_caller(torch, B):
         w.check_attend(got)
 
 
+def test_a_call_on_another_stream_takes_nothing_from_the_current_ones_pool(torch, B):
+    """Memory that pending work of the current stream may still use is neither output nor workspace of
+    a call on another stream, and the call's own is not handed out on the current stream."""
+    w = World(torch, [9000], [1], 4, 2, 64, 64, "bf16", "e4m3")
+    mem, q, other = w.device(B, starts=False), w.q.cuda(), torch.cuda.Stream()
+    nb = B.load().evo_memory_scratch_bytes(mem._ref, 1, 1, mem.max_len)
+    assert nb > 1 << 12
+    torch.cuda.synchronize()
+    for st in (other, other.cuda_stream):
+        gone = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (512, nb, nb, 512, 512)]
+        old = {t.data_ptr() for t in gone}
+        del gone
+        out = mem.attend(q, stream=st)
+        assert out.data_ptr() not in old
+        for n in (512, nb, nb, 512, 512):                          # nothing of this is the call's workspace
+            torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+        torch.cuda.synchronize()
+        w.check_attend(out)
+    x, y = torch.zeros(2, 2, 64, device="cuda"), torch.zeros(2, 2, 64, device="cuda").data_ptr()
+    codes, scales = torch.zeros(1, 2, 2, 64, dtype=torch.uint8, device="cuda"), torch.ones(1, 2, 2, 2, dtype=torch.uint8, device="cuda")
+    assert B.cache_add(codes, scales, x, stream=other).data_ptr() != y
+    assert B.cache_write(x, codes[0], scales[0], x, stream=other).data_ptr() != y
+    assert mem.append(q, None, None, stream=other).shape == q.shape
+    torch.cuda.synchronize()
+
+
+def test_sizes_of_a_growing_memory_are_forgotten(torch, B):
+    w = World(torch, [3], [1], 4, 2, 64, 16, "bf16", "bf16", max_pages=100)
+    mem, q = w.device(B, starts=False), w.q.cuda()
+    for n in range(3, 1600):
+        mem.attend(q, max_len=n)
+    assert len(mem._scratch) <= 1024
+    w.check_attend(mem.attend(q))
+
+
 def test_binding_refuses(torch, B):
     w = World(torch, [30], [4], 4, 2, 64, 16, "bf16", "bf16")
     mem = w.device(B)
