@@ -342,14 +342,13 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
           if (!ok) break;
           const int vr = r % BN, part = r / BN;    // a value a thread, or its columns' half
           const bool drop = k0 + vr < all.lo || k0 + vr >= all.hi;
-          bool bad = false;
 #pragma unroll
           for (int jj = 0; jj < D * BN / 1024; ++jj) {
             const int j = part * (D * BN / 1024) + jj;
             uint4* p = reinterpret_cast<uint4*>(ring + slot * C::TILE + (j / 8) * K64 + vr * 128 + ((j % 8 ^ (vr & 7)) << 4));
             uint4 u = *p;
             uint32_t* w = reinterpret_cast<uint32_t*>(&u);
-            bool changed = drop;
+            bool changed = drop, bad = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               uint32_t keep = 0xffffffffu;
@@ -358,9 +357,12 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
               if (keep != 0xffffffffu) changed = true, bad |= !drop;
               w[e] = drop ? 0u : w[e] & keep;
             }
+            if (bad) {                             // before the value goes: the other stream may find it clean already
+              *reinterpret_cast<volatile int*>(&sh.poison) = 1;
+              __threadfence_block();
+            }
             if (changed) *p = u;
           }
-          if (bad) sh.poison = 1;
           tc::fence_async_smem();
         }
       }
