@@ -13,12 +13,16 @@
 // (a row that sees none is zero).  A memory split over several blocks leaves each
 // piece's maximum, sum and unnormalised values, which a second kernel joins.
 //
-// fp32 kernel: a block of 128 threads takes 8 RM rows and 64 keys at a time; the
-// thread at (ty, tx) of an 8 x 16 grid computes RM rows x 4 keys of the scores and RM
-// rows x D/16 columns of the output.  All products are fp32 (packed in pairs: half the
-// issue slots); the multiply-add units bound it: 1,024 rows over 4,096 keys of 64, 8
-// heads, 251 us = 34 TFLOP/s, registers leaving 12 warps a SM to hide their latency.  There is no tensor-core form of it:
-// three tf32 products for one of fp32 are 170 multiply-adds a cycle and SM, against 128.
+// fp32 kernel: a warp takes 16 rows, a block 64 (or 32), and 64 keys at a time.  fp32 multiply-adds
+// bounded its first form (a register tile a thread: 1,024 rows over 4,096 keys of 64, 8 heads,
+// 255 us = 34 TFLOP/s, of keys of 128 541 us).  So a number is split into two of 11 bits and a product
+// taken as three of tf32, off by 2^-19 of itself at most (2 x 2^-21 for what the parts leave out, 2^-22
+// for the product of the low parts): mma.sync has 512 of these multiply-adds a cycle and SM, 170 of
+// the fp32 ones, against 85 to 110 of the plain ones: 178 us = 48 TFLOP/s and 352 us.  Codes are exact
+// in 11 bits and take two products.  What bounds it now is issue: a warp's 384 products of a block of keys
+// (42 % of the tensor pipe's time) stand beside some 2,000 other instructions, half of them the
+// split of keys and values, which do not overlap much with them.  Tiles of 32 rows a warp split half as
+// often, but spill (194 us where 16 rows took 203).
 #include <algorithm>
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -31,28 +35,66 @@
 namespace evo {
 namespace {
 
-constexpr int BN = 64, THREADS = 128, JOIN_THREADS = 256;
+constexpr int BN = 64, JOIN_THREADS = 256;
 // from this many rows a key/value head on, 8-bit pages are written out as bf16 pages for the tcgen05
 // kernel (16 sequences of 8,192 keys of 64, us with / without: 64 rows 131 / 129, 96 rows 131 / 152,
 // 256 rows 165 / 362; of 128: 237 / 196, 238 / 331, 267 / 693), while they fit this many bytes
 constexpr int EXPAND_ROWS = 65;
 constexpr long long EXPAND_MOST = 4ll << 30;
 
-template <int D, int RM>
+template <int D, int WARPS>
 struct Smem {
-  static constexpr int BM = 8 * RM;
-  float q[BM][D];
-  float k[BN][D + 4];           // rows 4 banks apart: 8 rows' float4 in a phase do not collide
-  float v[BN][D];
-  float p[BM][BN + 4];
+  static constexpr int BM = 16 * WARPS;
+  float q[BM * D], k[BN * D], v[BN * D];
+  int row[2][BN];               // rows of the pool that hold the keys of this block and the next, or -1
 };
+// where 4 floats d .. d + 3 of row r lie, so that the 8 lanes of a phase meet 8 different chunks of 128
+// bytes: 2 rows x 4 chunks of queries and keys, 4 pairs of rows x 2 chunks of values
+template <int D>
+__device__ __forceinline__ int key_at(int r, int d) { return r * D + (d ^ (r & 1) << 4); }
+template <int D>
+__device__ __forceinline__ int value_at(int r, int d) { return r * D + (d ^ (r >> 1 & 3) << 3); }
 
 __device__ __forceinline__ void copy16(float* dst, const float* src, bool on) {   // zeros where it is off
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
                "r"(on ? 16 : 0)
                : "memory");
 }
-__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }   // all but the last N groups
+
+// x as two numbers of 11 bits: hi, x rounded to nearest, and lo, what is left of it, cut off:
+// hi + lo = x (1 + e), |e| <= 2^-21.  In integers: a conversion has an eighth of their rate
+struct Split { uint32_t hi, lo; };
+__device__ __forceinline__ Split split(float x) {
+  Split s;
+  s.hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  s.lo = __float_as_uint(x - __uint_as_float(s.hi)) & 0xffffe000u;
+  return s;
+}
+__device__ __forceinline__ void mma8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// four tiles d += a b of fp32 numbers, so that a product does not wait for the one before it on its
+// tile; CODES: b is exact in 11 bits
+template <bool CODES>
+__device__ __forceinline__ void mma_split(float (&d0)[4], float (&d1)[4], float (&d2)[4], float (&d3)[4], const uint32_t (&ah)[4],
+                                          const uint32_t (&al)[4], float4 b0, float4 b1) {
+  const float x[4] = {b0.x, b0.y, b0.z, b0.w}, y[4] = {b1.x, b1.y, b1.z, b1.w};
+  uint32_t xh[4], xl[4], yh[4], yl[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const Split u = split(x[i]), w = split(y[i]);
+    xh[i] = CODES ? __float_as_uint(x[i]) : u.hi, xl[i] = u.lo;
+    yh[i] = CODES ? __float_as_uint(y[i]) : w.hi, yl[i] = w.lo;
+  }
+  if constexpr (!CODES) mma8(d0, ah, xl[0], yl[0]), mma8(d1, ah, xl[1], yl[1]), mma8(d2, ah, xl[2], yl[2]), mma8(d3, ah, xl[3], yl[3]);
+  mma8(d0, al, xh[0], yh[0]), mma8(d1, al, xh[1], yh[1]), mma8(d2, al, xh[2], yh[2]), mma8(d3, al, xh[3], yh[3]);
+  mma8(d0, ah, xh[0], yh[0]), mma8(d1, ah, xh[1], yh[1]), mma8(d2, ah, xh[2], yh[2]), mma8(d3, ah, xh[3], yh[3]);
+}
 
 // (top, sum, o) joined with another piece's
 __device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 ml, float4 p) {
@@ -63,14 +105,66 @@ __device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 m
   o = make_float4(o.x * f + p.x * g, o.y * f + p.y * g, o.z * f + p.z * g, o.w * f + p.w * g);
 }
 
-template <int D, int FORMAT, int RM>
-__global__ void __launch_bounds__(THREADS, D == 64 ? 3 : 2) attend_kernel(const __grid_constant__ AttendArgs a) {
+// A row whose sums are not finite, once more with plain fp32 products (an infinity's low part is no
+// number, so that infinities that a row sees, and NaN in tokens that it does not see, spoil the split
+// form).  A warp takes the row: a lane a key, then a lane D / 32 dimensions.
+template <int D, int FORMAT>
+__device__ __noinline__ void row_again(const AttendArgs& a, const Tile& t, const float* q, int r, Range see, float& top, float& sum,
+                                       float (&o)[D / 32]) {
   constexpr bool CODES = FORMAT == EVO_CACHE_E4M3;
+  const int lane = threadIdx.x & 31, page_tokens = a.m.page_tokens;
+  top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
+  for (int k0 = see.lo; k0 < see.hi; k0 += 32) {
+    const int key = min(k0 + lane, see.hi - 1);
+    const long long at =
+        ((long long)seq_page(a.m, t.n, key / page_tokens) * a.m.n_kv_head + t.kv_head) * page_tokens + key % page_tokens;
+    float s = 0.f;
+    for (int d = 0; d < D; d += 4) {
+      float4 k;
+      if constexpr (CODES) k = codes4(*reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(a.m.k_pages) + at * D + d));
+      else k = *reinterpret_cast<const float4*>(static_cast<const float*>(a.m.k_pages) + at * D + d);
+      const float4 x = *reinterpret_cast<const float4*>(q + key_at<D>(r, d));
+      s = fmaf(x.x, k.x, fmaf(x.y, k.y, fmaf(x.z, k.z, fmaf(x.w, k.w, s))));
+    }
+    if constexpr (CODES) s *= scale_value(a.m.k_scales[at]);
+    s = k0 + lane < see.hi ? s * a.scale_log2 : -INFINITY;
+    float m = s;
+#pragma unroll
+    for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    m = fmaxf(m, top);
+    const float base = m == -INFINITY ? 0.f : m, keep = exp2f(top - base), p = exp2f(s - base);
+    top = m;
+    sum = sum * keep + p;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] *= keep;
+    for (int j = 0; j < min(32, see.hi - k0); ++j) {
+      const float w = __shfl_sync(0xffffffffu, p, j);
+      const long long from = __shfl_sync(0xffffffffu, at, j);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        float v;
+        if constexpr (CODES)
+          v = codes4(static_cast<const uint8_t*>(a.m.v_pages)[from * D + lane + 32 * i]).x * scale_value(a.m.v_scales[from]);
+        else
+          v = static_cast<const float*>(a.m.v_pages)[from * D + lane + 32 * i];
+        o[i] = fmaf(w, v, o[i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+}
+
+template <int D, int FORMAT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 4 : 2) * (4 / WARPS)) attend_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr bool CODES = FORMAT == EVO_CACHE_E4M3;
+  constexpr int THREADS = 32 * WARPS, BM = 16 * WARPS, NT = BN / 8, DT = D / 8;
   extern __shared__ __align__(16) uint8_t raw[];
-  using S = Smem<D, RM>;
+  using S = Smem<D, WARPS>;
   S& sm = *reinterpret_cast<S*>(raw);
-  constexpr int BM = 8 * RM, DC = D / 64;          // a thread's columns: 4 tx + 64 c .. + 3
-  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
   const Tile t = tile_of_block(a);
   const int rows = t.count * a.group, r0 = t.tile * BM;
   if (r0 >= rows) return;
@@ -80,182 +174,203 @@ __global__ void __launch_bounds__(THREADS, D == 64 ? 3 : 2) attend_kernel(const 
   const int whole_lo = max(last_row.lo, all.lo), whole_hi = min(first_row.hi, all.hi);
   const int shift = 31 - __clz(a.m.page_tokens);
 
+  const auto look_up = [&](int k0) {               // the pool's rows for 64 keys from k0 on, a thread each
+    if (tid >= BN) return;
+    const int key = k0 + tid;
+    int row = -1;
+    if (key >= all.lo && key < all.hi)
+      row = (seq_page(a.m, t.n, key >> shift) * a.m.n_kv_head + t.kv_head) * a.m.page_tokens + (key & (a.m.page_tokens - 1));
+    sm.row[k0 / BN & 1][tid] = row;
+  };
+  // 64 keys or values from k0 on (zeros outside the piece): fp32 on their way, a group of copies;
+  // 8-bit ones as numbers
+  const auto bring = [&](int k0, const void* pages, const uint8_t* scales, float* tile, auto place) {
+    const int* row = sm.row[k0 / BN & 1];
+    if constexpr (CODES) {
+#pragma unroll 4
+      for (int i = tid; i < BN * D / 16; i += THREADS) {
+        const int r = i / (D / 16), d = i % (D / 16) * 16, at = row[r];
+        uint4 u = make_uint4(0, 0, 0, 0);
+        float f = 0.f;
+        if (at >= 0) u = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(pages) + (long long)at * D + d), f = scale_value(scales[at]);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 x = codes4(w[e]);
+          *reinterpret_cast<float4*>(tile + place(r, d + 4 * e)) = make_float4(x.x * f, x.y * f, x.z * f, x.w * f);
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int i = tid; i < BN * D / 4; i += THREADS) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4, at = row[r];
+        copy16(tile + place(r, d), static_cast<const float*>(pages) + (long long)max(at, 0) * D + d, at >= 0);
+      }
+      copies_close();
+    }
+  };
+  const auto bring_k = [&](int k0) { bring(k0, a.m.k_pages, a.m.k_scales, sm.k, key_at<D>); };
+  const auto bring_v = [&](int k0) { bring(k0, a.m.v_pages, a.m.v_scales, sm.v, value_at<D>); };
+  int k0 = all.lo / BN * BN;
+  look_up(k0);
+  __syncthreads();
+  if (k0 < all.hi) bring_k(k0), bring_v(k0);
+
   for (int i = tid; i < BM * D / 4; i += THREADS) {
     const int r = i / (D / 4), d = i % (D / 4) * 4, R = r0 + r;
     float4 x = {};
     if (R < rows)
       x = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (t.first + R / a.group) * a.ldq +
                                            (long long)(t.kv_head * a.group + R % a.group) * D + d);
-    *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
+    *reinterpret_cast<float4*>(&sm.q[key_at<D>(r, d)]) = x;
   }
-  Range seen[RM];
-  float mx[RM], sum[RM];
-  float2 o[RM][DC][2];
+  Range seen[2];                                   // rows g and g + 8 of the warp's 16
+  float mx[2], sum[2], o[DT][4];
 #pragma unroll
-  for (int i = 0; i < RM; ++i) {
-    const int R = r0 + ty * RM + i;
-    seen[i] = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
-    seen[i] = {max(seen[i].lo, all.lo), min(seen[i].hi, all.hi)};
-    mx[i] = -INFINITY;
-    sum[i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < DC; ++c) o[i][c][0] = o[i][c][1] = make_float2(0.f, 0.f);
+  for (int e = 0; e < 2; ++e) {
+    const int R = r0 + 16 * warp + g + 8 * e;
+    seen[e] = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
+    seen[e] = {max(seen[e].lo, all.lo), min(seen[e].hi, all.hi)};
+    mx[e] = -INFINITY;
+    sum[e] = 0.f;
   }
-  // row of the pool that holds a key, or -1 outside the piece
-  const auto row_of = [&](int key) -> long long {
-    if (key < all.lo || key >= all.hi) return -1;
-    return ((long long)seq_page(a.m, t.n, key >> shift) * a.m.n_kv_head + t.kv_head) * a.m.page_tokens +
-           (key & (a.m.page_tokens - 1));
-  };
-  constexpr int CV = CODES ? BN * D / 16 / THREADS : 1;      // 16-code vectors a thread brings, keys and values each
-  uint4 kc[CV], vc[CV];
-  uint32_t kscale[CV], vscale[CV];
-  const auto bring = [&](int k0) {
-    if constexpr (CODES) {
 #pragma unroll
-      for (int i = 0; i < CV; ++i) {
-        const int v = tid + i * THREADS, r = v / (D / 16), d = v % (D / 16) * 16;
-        const long long at = row_of(k0 + r);
-        kc[i] = vc[i] = make_uint4(0, 0, 0, 0);
-        kscale[i] = vscale[i] = 1;
-        if (at >= 0) {
-          kc[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.m.k_pages) + at * D + d);
-          vc[i] = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.m.v_pages) + at * D + d);
-          kscale[i] = a.m.k_scales[at];
-          vscale[i] = a.m.v_scales[at];
-        }
-      }
-    } else {
-#pragma unroll 4
-      for (int i = tid; i < BN * D / 4; i += THREADS) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        const long long at = row_of(k0 + r);
-        copy16(&sm.k[r][d], static_cast<const float*>(a.m.k_pages) + max(at, 0ll) * D + d, at >= 0);
-        copy16(&sm.v[r][d], static_cast<const float*>(a.m.v_pages) + max(at, 0ll) * D + d, at >= 0);
-      }
-    }
-  };
-  const auto unpack = [&] {                        // the codes in registers to shared memory
-    if constexpr (CODES) {
+  for (int j = 0; j < DT; ++j)
 #pragma unroll
-      for (int i = 0; i < CV; ++i) {
-        const int v = tid + i * THREADS, r = v / (D / 16), d = v % (D / 16) * 16;
-        const float kf = scale_value(kscale[i]), vf = scale_value(vscale[i]);
-        const uint32_t kw[4] = {kc[i].x, kc[i].y, kc[i].z, kc[i].w}, vw[4] = {vc[i].x, vc[i].y, vc[i].z, vc[i].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 k = codes4(kw[e]), x = codes4(vw[e]);
-          *reinterpret_cast<float4*>(&sm.k[r][d + 4 * e]) = make_float4(k.x * kf, k.y * kf, k.z * kf, k.w * kf);
-          *reinterpret_cast<float4*>(&sm.v[r][d + 4 * e]) = make_float4(x.x * vf, x.y * vf, x.z * vf, x.w * vf);
-        }
-      }
-    }
-  };
-  for (int k0 = all.lo / BN * BN; k0 < all.hi; k0 += BN) {
-    const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi;
+    for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+
+  const bool busy = r0 + 16 * warp < rows;         // a warp without rows only copies
+  for (; k0 < all.hi; k0 += BN) {
+    const bool whole = k0 >= whole_lo && k0 + BN <= whole_hi, more = k0 + BN < all.hi;
+    if (more) look_up(k0 + BN);
+    copies_wait<1>();                              // the keys (their copies are older than the values')
     __syncthreads();
-    bring(k0);
-    if constexpr (CODES) unpack();
-    else copies_done();
-    __syncthreads();
-    float2 s2[RM][4] = {};                         // sums over the even and the odd dimensions
-#pragma unroll 4
-    for (int d = 0; d < D; d += 4) {
-      float4 k[4];
+    // s[n]: keys 8 n + 2 c, 8 n + 2 c + 1 of rows g (0, 1) and g + 8 (2, 3).  A contraction's index may be
+    // permuted at will: a lane's four dimensions 16 h + 4 c .. + 3 are its places c, c + 4 of two steps
+    float s[NT][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][d]);
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < RM; ++i) {
-        const float4 q = *reinterpret_cast<const float4*>(&sm.q[ty * RM + i][d]);
+      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll 1
+    for (int h = busy ? 0 : D / 16; h < D / 16; ++h) {
+      const float4 x = *reinterpret_cast<const float4*>(&sm.q[key_at<D>(16 * warp + g, 16 * h + 4 * c)]);
+      const float4 y = *reinterpret_cast<const float4*>(&sm.q[key_at<D>(16 * warp + g + 8, 16 * h + 4 * c)]);
+      const Split q[2][4] = {{split(x.x), split(y.x), split(x.y), split(y.y)}, {split(x.z), split(y.z), split(x.w), split(y.w)}};
+      const uint32_t ah[2][4] = {{q[0][0].hi, q[0][1].hi, q[0][2].hi, q[0][3].hi}, {q[1][0].hi, q[1][1].hi, q[1][2].hi, q[1][3].hi}};
+      const uint32_t al[2][4] = {{q[0][0].lo, q[0][1].lo, q[0][2].lo, q[0][3].lo}, {q[1][0].lo, q[1][1].lo, q[1][2].lo, q[1][3].lo}};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          s2[i][j] = fma_pair(make_float2(q.x, q.y), make_float2(k[j].x, k[j].y), s2[i][j]);
-          s2[i][j] = fma_pair(make_float2(q.z, q.w), make_float2(k[j].z, k[j].w), s2[i][j]);
-        }
+      for (int n = 0; n < NT; n += 4) {
+        float4 k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = *reinterpret_cast<const float4*>(&sm.k[key_at<D>(8 * (n + i) + g, 16 * h + 4 * c)]);
+        mma_split<CODES>(s[n], s[n + 1], s[n + 2], s[n + 3], ah[0], al[0], make_float4(k[0].x, k[1].x, k[2].x, k[3].x),
+                         make_float4(k[0].y, k[1].y, k[2].y, k[3].y));
+        mma_split<CODES>(s[n], s[n + 1], s[n + 2], s[n + 3], ah[1], al[1], make_float4(k[0].z, k[1].z, k[2].z, k[3].z),
+                         make_float4(k[0].w, k[1].w, k[2].w, k[3].w));
       }
     }
+    __syncthreads();                               // every warp has read the keys
+    if (more) bring_k(k0 + BN);
+    else copies_close();                           // an empty group, so that the count of groups stays
+    if (busy)
 #pragma unroll
-    for (int i = 0; i < RM; ++i) {
-      float s[4], top = -INFINITY;
+    for (int e = 0; e < 2; ++e) {
+      float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = k0 + tx + 16 * j;
-        s[j] = (s2[i][j].x + s2[i][j].y) * a.scale_log2;
-        if (!whole && (key < seen[i].lo || key >= seen[i].hi)) s[j] = -INFINITY;
-        top = fmaxf(top, s[j]);
-      }
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int w = 8; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-      const float now = fmaxf(mx[i], top), base = now == -INFINITY ? 0.f : now;
-      const float keep = exp2f(mx[i] - base);
-      mx[i] = now;
+        for (int i = 0; i < 2; ++i) {
+          float& x = s[n][2 * e + i];
+          x *= a.scale_log2;
+          const int key = k0 + 8 * n + 2 * c + i;
+          if (!whole && (key < seen[e].lo || key >= seen[e].hi)) x = -INFINITY;
+          top = fmaxf(top, x);
+        }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const float now = fmaxf(mx[e], top), base = now == -INFINITY ? 0.f : now;
+      const float keep = ex2_approx(mx[e] - base);
+      mx[e] = now;
       float add = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = exp2f(s[j] - base);
-        add += p;
-        sm.p[ty * RM + i][tx + 16 * j] = p;
-      }
-      sum[i] = sum[i] * keep + add;                // this thread's keys; joined at the end
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int c = 0; c < DC; ++c)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) o[i][c][h] = make_float2(o[i][c][h].x * keep, o[i][c][h].y * keep);
-    }
-    __syncwarp();               // a row's weights come from its own half warp
-    if (whole) {
-#pragma unroll 2
-      for (int j = 0; j < BN; j += 4) {
-        float4 v[4][DC];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int c = 0; c < DC; ++c) v[e][c] = *reinterpret_cast<const float4*>(&sm.v[j + e][4 * tx + 64 * c]);
-#pragma unroll
-        for (int i = 0; i < RM; ++i) {
-          const float4 p4 = *reinterpret_cast<const float4*>(&sm.p[ty * RM + i][j]);
-          const float p[4] = {p4.x, p4.y, p4.z, p4.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int c = 0; c < DC; ++c) {
-              o[i][c][0] = fma_pair(make_float2(p[e], p[e]), make_float2(v[e][c].x, v[e][c].y), o[i][c][0]);
-              o[i][c][1] = fma_pair(make_float2(p[e], p[e]), make_float2(v[e][c].z, v[e][c].w), o[i][c][1]);
-            }
+        for (int i = 0; i < 2; ++i) {
+          float& x = s[n][2 * e + i];
+          x = ex2_approx(x - base);
+          add += x;
         }
-      }
-    } else {
-      // some row does not see the whole block: what it does not see adds nothing, whatever it holds
-      for (int j = 0; j < BN; ++j)
+      sum[e] = sum[e] * keep + add;                // this lane's keys; joined at the end
 #pragma unroll
-        for (int i = 0; i < RM; ++i) {
-          const float p = sm.p[ty * RM + i][j];
-          if (p != 0.f)
-#pragma unroll
-            for (int c = 0; c < DC; ++c) {
-              const float4 v = *reinterpret_cast<const float4*>(&sm.v[j][4 * tx + 64 * c]);
-              o[i][c][0] = fma_pair(make_float2(p, p), make_float2(v.x, v.y), o[i][c][0]);
-              o[i][c][1] = fma_pair(make_float2(p, p), make_float2(v.z, v.w), o[i][c][1]);
-            }
-        }
+      for (int j = 0; j < DT; ++j) o[j][2 * e] *= keep, o[j][2 * e + 1] *= keep;
     }
-    __syncwarp();
+    copies_wait<1>();                              // the values
+    __syncthreads();
+    // weights enter as they left the scores: keys 2 c, 2 c + 1 of 8 are places c, c + 4.  Tile 4 x + y of o
+    // holds dimensions 32 x + 8 c + y (0, 2) and 32 x + 8 c + 4 + y (1, 3) of rows g and g + 8
+    if (busy)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const Split p[4] = {split(s[n][0]), split(s[n][2]), split(s[n][1]), split(s[n][3])};
+      const uint32_t ah[4] = {p[0].hi, p[1].hi, p[2].hi, p[3].hi}, al[4] = {p[0].lo, p[1].lo, p[2].lo, p[3].lo};
+#pragma unroll
+      for (int x = 0; x < D / 32; ++x) {
+        const float4 u = *reinterpret_cast<const float4*>(&sm.v[value_at<D>(8 * n + 2 * c, 32 * x + 4 * g)]);
+        const float4 w = *reinterpret_cast<const float4*>(&sm.v[value_at<D>(8 * n + 2 * c + 1, 32 * x + 4 * g)]);
+        mma_split<CODES>(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3], ah, al, u, w);
+      }
+    }
+    __syncthreads();                               // every warp has read the values
+    if (more) bring_v(k0 + BN);
   }
 #pragma unroll
-  for (int i = 0; i < RM; ++i) {
-#pragma unroll
-    for (int w = 8; w > 0; w >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], w);
-    const int R = r0 + ty * RM + i;
-    if (R >= rows) continue;
+  for (int e = 0; e < 2; ++e) {
+    sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 1);
+    sum[e] += __shfl_xor_sync(0xffffffffu, sum[e], 2);
+  }
+  const auto place = [&](int R, long long& at) {   // where a row's sums go
     const int row = t.first + R / a.group, head = t.kv_head * a.group + R % a.group;
-    const float f = a.splits > 1 ? 1.f : sum[i] == 0.f ? 0.f : 1.f / sum[i];
-    const long long at = part_index(a, t.split, row, head);
-    float* dst = a.splits > 1 ? a.part + at * D : static_cast<float*>(a.out) + row * a.ldo + (long long)head * D;
+    at = part_index(a, t.split, row, head);
+    return a.splits > 1 ? a.part + at * D : static_cast<float*>(a.out) + row * a.ldo + (long long)head * D;
+  };
+  uint32_t again = 0;                              // the warp's rows whose sums are not finite, a bit each
 #pragma unroll
-    for (int c = 0; c < DC; ++c)
-      *reinterpret_cast<float4*>(dst + 4 * tx + 64 * c) =
-          make_float4(o[i][c][0].x * f, o[i][c][0].y * f, o[i][c][1].x * f, o[i][c][1].y * f);
-    if (a.splits > 1 && tx == 0) a.ml[at] = make_float2(mx[i], sum[i]);
+  for (int e = 0; e < 2; ++e) {
+    float bad = sum[e] * 0.f;                      // NaN if the sum or a value is not finite
+#pragma unroll
+    for (int j = 0; j < DT; ++j) bad += o[j][2 * e] * 0.f + o[j][2 * e + 1] * 0.f;
+    const uint32_t lanes = __ballot_sync(0xffffffffu, bad != 0.f && r0 + 16 * warp + g + 8 * e < rows);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) again |= (lanes >> (4 * i) & 15u ? 1u : 0u) << (8 * e + i);
+  }
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int R = r0 + 16 * warp + g + 8 * e;
+    if (R >= rows || (again >> (8 * e + g) & 1)) continue;
+    const float f = a.splits > 1 ? 1.f : sum[e] == 0.f ? 0.f : 1.f / sum[e];
+    long long at;
+    float* dst = place(R, at);
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        *reinterpret_cast<float4*>(dst + 32 * x + 8 * c + 4 * i) =
+            make_float4(o[4 * x][2 * e + i] * f, o[4 * x + 1][2 * e + i] * f, o[4 * x + 2][2 * e + i] * f, o[4 * x + 3][2 * e + i] * f);
+    if (a.splits > 1 && c == 0) a.ml[at] = make_float2(mx[e], sum[e]);
+  }
+  for (; again; again &= again - 1) {
+    const int r = 16 * warp + __ffs(again) - 1, R = r0 + r;
+    Range see = seen_by(a, t, R / a.group);
+    see = {max(see.lo, all.lo), min(see.hi, all.hi)};
+    float top, l, x[D / 32];
+    row_again<D, FORMAT>(a, t, sm.q, r, see, top, l, x);
+    const float f = a.splits > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
+    long long at;
+    float* dst = place(R, at);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) dst[lane + 32 * i] = x[i] * f;
+    if (a.splits > 1 && lane == 0) a.ml[at] = make_float2(top, l);
   }
 }
 
@@ -336,15 +451,15 @@ __global__ void __launch_bounds__(JOIN_THREADS) expand_kernel(const __grid_const
   }
 }
 
-template <int D, int FORMAT, int RM>
+template <int D, int FORMAT, int WARPS>
 cudaError_t launch_f32_as(const AttendArgs& a, cudaStream_t st) {
   static std::atomic<uint64_t> done{0};
-  return launch_pieces(attend_kernel<D, FORMAT, RM>, a, THREADS, (int)sizeof(Smem<D, RM>), done, st);
+  return launch_pieces(attend_kernel<D, FORMAT, WARPS>, a, 32 * WARPS, (int)sizeof(Smem<D, WARPS>), done, st);
 }
 
-template <int D, int RM>
+template <int D, int WARPS>
 cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
-  return a.m.format == EVO_CACHE_E4M3 ? launch_f32_as<D, EVO_CACHE_E4M3, RM>(a, st) : launch_f32_as<D, EVO_CACHE_F32, RM>(a, st);
+  return a.m.format == EVO_CACHE_E4M3 ? launch_f32_as<D, EVO_CACHE_E4M3, WARPS>(a, st) : launch_f32_as<D, EVO_CACHE_F32, WARPS>(a, st);
 }
 
 template <typename T, int D>
@@ -385,8 +500,11 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
     p.tile_rows = all <= 8 ? 8 : all <= 16 ? 16 : 32;
   else if (few)   // 4 rows a tile while that fills the GPU sooner (3 x 16 rows over 333 keys: 8.3 us against 12.4 with 16)
     p.tile_rows = all == 1 ? 1 : all <= 4 || (long long)m.n_seq * m.n_kv_head < 152 ? 4 : 16;
-  else            // 64 rows of 128 leave one block a SM
-    p.tile_rows = all <= 32 || m.head_dim == 128 ? 32 : 64;
+  else
+    // 64 rows a block, of which up to 32 idle; blocks of 32 where the idle ones' shared memory keeps others out
+    // (64 x 32 fp32 rows over 4,000 keys of 128: 928 us against 1,284; of 64, or 8-bit ones: slower, 2 x 32
+    // rows over 500 keys 28.8 against 24.7)
+    p.tile_rows = all <= 32 && m.head_dim == 128 && m.format == EVO_CACHE_F32 && (long long)m.n_seq * m.n_kv_head >= 152 ? 32 : 64;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   p.cluster = 1;
@@ -442,8 +560,7 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
     a.m.n_pages = a.m.n_seq * p.expand;
   }
   if (p.kernel == ATTEND_F32)
-    e = p.tile_rows == 32 ? d64 ? launch_f32<64, 4>(a, st) : launch_f32<128, 4>(a, st)
-                          : d64 ? launch_f32<64, 8>(a, st) : launch_f32<128, 8>(a, st);
+    e = p.tile_rows == 32 ? launch_f32_as<128, EVO_CACHE_F32, 2>(a, st) : d64 ? launch_f32<64, 4>(a, st) : launch_f32<128, 4>(a, st);
   else if (p.kernel == ATTEND_F32_ROWS)
     e = launch_attend_f32_rows(a, p.tile_rows, st);
   else if (p.kernel == ATTEND_ROWS)

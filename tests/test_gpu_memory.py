@@ -547,6 +547,24 @@ def test_captured_replayed_and_repeated(torch, B, dtype, fmt, m, length):
     w.check_attend(outs[0], q=q)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 20, 40, 200])
+def test_a_key_at_minus_infinity_is_no_key(torch, B, dtype, D, m):
+    """A key whose scores are all minus infinity has no weight: the others' attention is what is left."""
+    w = World(torch, [333], [m], 2, 2, D, 32, dtype, dtype, seed=m)
+    k, v = w.dense(0)
+    tok = 100
+    w.pages[0][int(w.table[0, tok // 32]), :, tok % 32, 3] = -float("inf")
+    w.q[:, :, 3] = w.q[:, :, 3].abs() + 0.5
+    mem = w.device(B)
+    got = mem.attend(w.q.cuda(), causal=False, max_new=m).double().cpu().numpy()
+    out, size, dots = M.attend(w.q.double().numpy(), np.delete(k, tok, 0), np.delete(v, tok, 0), 2, D ** -0.5, False, 0)
+    half = 2.0 ** -8 if dtype == "bf16" else U
+    weight = 2 * (D + 8) * U * dots + 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+    assert (np.abs(got - out) <= half * np.abs(out) + (1 + half) * (weight + 333 * U) * size + 1e-37).all()
+
+
 @pytest.mark.parametrize("dtype,fmt", FORMATS)
 def test_queries_in_place_and_outputs_beside_them(torch, B, dtype, fmt):
     """One buffer of rows holds queries, keys, values and outputs: queries are turned in place, outputs interleave."""
