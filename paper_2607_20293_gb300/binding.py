@@ -434,7 +434,7 @@ def cache_write(r, codes, scales, x=None, refresh=None, out=None, stream=None):
     if x is not None:
         xp = _need(x, "x", _F32, shape, index)
         if out is None:
-            out = _new(shape, _F32, x.device, stream)
+            out = _torch.empty_like(x) if stream is None else _new(shape, _F32, x.device, stream)
             yp = out.data_ptr()
         else:
             yp = _need(out, "out", _F32, shape, index)
@@ -460,7 +460,7 @@ def cache_add(codes, scales, x, reuse=None, out=None, stream=None):
     U = codes.shape[0]
     xp = _need(x, "x", _F32, shape, index)
     if out is None:
-        out = _new(shape, _F32, x.device, stream)
+        out = _torch.empty_like(x) if stream is None else _new(shape, _F32, x.device, stream)
         yp = out.data_ptr()
     else:
         yp = _need(out, "out", _F32, shape, index)
@@ -528,6 +528,15 @@ class Memory:
                              f"({rows}, {heads}, {dim}) on {self.device}, the heads of a row contiguous")
         return t.data_ptr(), ld if rows > 1 else heads * dim
 
+    def _like(self, q, ldq: int, rows: int, stream):
+        """A contiguous tensor for q's rows, its address and the elements between its rows."""
+        row = self.n_head * self.head_dim
+        if stream is None and ldq == row:
+            out = _torch.empty_like(q)
+        else:
+            out = _new((rows, self.n_head, self.head_dim), self.dtype, self.device, stream)
+        return out, out.data_ptr(), row
+
     def append(self, q, k, v, q_gain=None, k_gain=None, eps: float = 1e-6, rotation=None, pos0=None, out=None,
                max_new=None, stream=None):
         """evo_memory_append: keys and values [rows][n_kv_head][head_dim] to their pages, and the
@@ -546,8 +555,7 @@ class Memory:
             heads = self.n_head
             qp, ldq = self._rows(q, "q", rows, heads)
             if out is None:
-                out = _new((rows, heads, dim), self.dtype, self.device, stream)
-                op, ldo = out.data_ptr(), heads * dim
+                out, op, ldo = self._like(q, ldq, rows, stream)
             else:
                 op, ldo = self._rows(out, "out", rows, heads)
         if k is not None:
@@ -578,8 +586,7 @@ class Memory:
         rows = q.shape[0]
         qp, ldq = self._rows(q, "q", rows, heads)
         if out is None:
-            out = _new((rows, heads, dim), self.dtype, self.device, stream)
-            op, ldo = out.data_ptr(), heads * dim
+            out, op, ldo = self._like(q, ldq, rows, stream)
         else:
             op, ldo = self._rows(out, "out", rows, heads)
         if rows == 0:
