@@ -20,7 +20,7 @@
 // for the product of the low parts): mma.sync has 512 of these multiply-adds a cycle and SM, 170 of
 // the fp32 ones, against 85 to 110 of the plain ones: 178 us = 48 TFLOP/s and 352 us.  Codes are exact
 // in 11 bits and take two products.  What bounds it now is issue: a warp's 384 products of a block of keys
-// (42 % of the tensor pipe's time) stand beside some 2,000 other instructions, half of them the
+// (48 % of the tensor pipe's time) stand beside some 1,900 other instructions, half of them the
 // split of keys and values, which do not overlap much with them.  Tiles of 32 rows a warp split half as
 // often, but spill (194 us where 16 rows took 203).
 #include <algorithm>
