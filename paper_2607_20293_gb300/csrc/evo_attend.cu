@@ -509,17 +509,30 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   p.cluster = 1;
   if (p.kernel == ATTEND_ROWS || p.kernel == ATTEND_F32_ROWS) {
-    // Pieces: enough blocks to fill the GPU, and with plenty of work several waves of them, so
-    // that sequences of different lengths even out; tiles of 32 rows pay 10 us a wave of further
-    // blocks (32 rows of 64 sequences: 99 us in one piece, 104 in two).  Up to 8 pieces of few
-    // items are joined by a cluster, without a second kernel (3 x 16 rows over 333 fp32 keys: 8.3
-    // us against 10.3); more, or those of many items, by a kernel (a cluster's blocks wait for
-    // one another: 64 ragged sequences 147 us against 134).
-    const long long most = std::max(1, max_len / (f32 ? 64 : 128));
-    const long long target = blocks < 456 || p.tile_rows == 32 ? 456 : 1824;
-    const long long want = std::max(1ll, std::min({most, (target + blocks / 2) / blocks, 64ll}));
-    p.cluster = blocks < 456 && want <= 8 ? (int)want : 1;
-    p.splits = (int)want;
+    // Pieces of few items: as many as are resident at once, joined by the blocks of a cluster of up to 8
+    // without a second kernel.  Of the 2, 3 or 6 blocks that a SM holds, whole clusters of up to 5 find at
+    // least 288, 432 or 860 places, of up to 8 at least 264, 400 or 800; one cluster more is a wave of its own (56
+    // items over 16,000 8-bit keys: 38 us in 6 pieces, 49 in 8; 65 over 12,000: 27 in 6, 39 in 7).
+    // Long memories of fewer items take several clusters an item, whose results a kernel joins (8 items
+    // over 16,389 keys: 26.7 us in 8 pieces, 16.5 in 40, and 20 in 57 without clusters; over 4,096 keys
+    // 10.4 in 8, 12.4 in 24).
+    const bool codes = m.format == EVO_CACHE_E4M3, wide = m.head_dim == 128;
+    const int a_sm = f32 ? (p.tile_rows == 16 ? 2 : codes && !wide ? 6 : 3) : wide && (!codes || p.tile_rows == 32) ? 2 : 3;
+    const long long places5 = a_sm == 2 ? 288 : a_sm == 3 ? 432 : 860, places8 = a_sm == 2 ? 264 : a_sm == 3 ? 400 : 800;
+    if (2 * blocks <= places5) {
+      const long long most = std::max(1, max_len / (f32 ? 64 : 128));
+      p.cluster = (int)std::min({8ll, std::max(std::min(5ll, places5 / blocks), places8 / blocks), most});
+      const long long more = p.cluster == 8 ? std::min({8ll, places8 / (8 * blocks), max_len / 2048ll}) : 1;
+      p.splits = p.cluster * (int)std::max(1ll, more);
+    } else {
+      // More: several waves, so that sequences of different lengths even out (240 items over 16,000 keys:
+      // 157 us in one piece, 116 in 7; 64 ragged sequences 134 us, in clusters 147), of pieces that are
+      // worth the kernel that joins them (over 2,000 keys 26 us in one, 33 in 7).  Tiles of 32 rows pay
+      // 10 us a wave of further blocks (64 sequences: 99 us in one piece, 104 in two; 45: 314 and 285).
+      const long long most = std::max(1, max_len / 1024);
+      const long long want = p.tile_rows == 32 ? 900 / blocks : (1824 + blocks / 2) / blocks;
+      p.splits = (int)std::max(1ll, std::min({most, want, 64ll}));
+    }
   } else {
     const long long most = std::max(1, max_len / (tiles ? 512 : 64));
     const long long target = tiles ? 152 : 152 * 4;
