@@ -18,12 +18,13 @@
 // 255 us = 34 TFLOP/s, of keys of 128 541 us).  So a number is split into two of 11 bits and a product
 // taken as three of tf32, off by 2^-19 of itself at most (2 x 2^-21 for what the parts leave out, 2^-22
 // for the product of the low parts): mma.sync has 512 of these multiply-adds a cycle and SM, 170 of
-// the fp32 ones, against 85 to 110 of the plain ones: 178 us = 48 TFLOP/s and 352 us.  Codes are exact
+// the fp32 ones, against 85 to 110 of the plain ones: 160 us = 54 TFLOP/s and 322 us.  Codes are exact
 // in 11 bits and take two products.  What bounds it now is issue: a warp's 384 products of a block of keys
 // (48 % of the tensor pipe's time) stand beside some 1,900 other instructions, half of them the
 // split of keys and values, which do not overlap much with them.  Tiles of 32 rows a warp split half as
 // often, but spill (194 us where 16 rows took 203).
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -480,6 +481,29 @@ cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, join_kernel<T, D>, a, groups);
 }
 
+// Pieces of an item for the kernels of many rows: as many as leave the fullest SM least to do, in keys: its
+// blocks times (a piece's keys, and what a block costs beside them).
+//   tcgen05: a block a SM; 450 keys, or 1,100 where the pieces are joined, which are of 512 keys at least
+//     (100 items of 256 rows over 16,000 keys of 64: 148 us in one piece, 122 in 3, 143 in 4; over 4,000 49, 56, 68)
+//   fp32: blocks of 64 keys and 100 beside them, and an SM with few blocks is slower at them (256 items of
+//     64 rows over 8,000 keys of 64: 667 us in 2 pieces, which fill the places, 563 in 7; 96 over 700: 39
+//     us in 3, 48 in 6).  Up to 32 rows leave half the warps without any: as many blocks as there are places
+//     (96 items of 20 rows over 2,000 keys: 55 us in 6 pieces, 62 in 4), of 128 keys at least (8 items over 700: 17 us in 6, 19 in 10)
+int pieces_of(bool tiles, long long blocks, long long rows, int max_len) {
+  const bool half = !tiles && rows <= 32;
+  const int most = std::min(64, std::max(1, max_len / (tiles ? 512 : half ? 128 : 64)));
+  if (half) return (int)std::max(1ll, std::min((long long)most, 152 * 4 / blocks));
+  int best = 1;
+  double least = 1e300;
+  for (int s = 1; s <= most; ++s) {
+    const double each = (double)((blocks * s + 151) / 152), keys = (double)max_len / s;
+    const double cost = tiles ? each * (keys + (s == 1 ? 450 : 1100))
+                              : each * (64 * std::ceil(keys / 64) + 100) * (each == 1 ? 1.5 : each == 2 ? 1.07 : each == 3 ? 1.06 : 1);
+    if (cost < least) least = cost, best = s;
+  }
+  return best;
+}
+
 }  // namespace
 
 AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) {
@@ -534,9 +558,7 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
       p.splits = (int)std::max(1ll, std::min({most, want, 64ll}));
     }
   } else {
-    const long long most = std::max(1, max_len / (tiles ? 512 : 64));
-    const long long target = tiles ? 152 : 152 * 4;
-    p.splits = (int)std::max(1ll, std::min({most, target / blocks, 64ll}));
+    p.splits = pieces_of(tiles, blocks, all, max_len);
   }
   const int parts = p.splits / p.cluster;
   p.scratch = parts == 1 ? 0 : (size_t)parts * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);

@@ -566,6 +566,45 @@ def test_a_key_at_minus_infinity_is_no_key(torch, B, dtype, D, m):
 
 
 @pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("m", [1, 20, 50, 130])
+def test_rows_before_and_behind_the_sequences_stay(torch, B, dtype, fmt, m):
+    """Starts begin behind the first rows, chunks may be empty, the table names far more pages than are used."""
+    news = [m, 0, 3, m]
+    w = World(torch, [m + 40, 17, 5, m], news, 4, 2, 64, 16, dtype, fmt, seed=m, max_pages=600)
+    mem = w.device(B)
+    front, back = 5, 4
+    rows = front + sum(news) + back
+    starts = (w.starts + front).to(torch.int32).cuda()
+    pad = lambda t: torch.cat([torch.full((front,) + t.shape[1:], float("nan")).to(t), t,  # noqa: E731
+                               torch.full((back,) + t.shape[1:], float("nan")).to(t)]).cuda()
+    q, k, v = pad(w.q), pad(w.k), pad(w.v)
+    mem = B.Memory(w.dpages[0], w.dpages[1], w.dtable, w.dlens, 4, k_scales=w.dscales[0], v_scales=w.dscales[1], starts=starts,
+                   status=w.status, dtype=dtype)
+    out = torch.full((rows, 4, 64), 7.0).to(w.t).cuda()
+    got = mem.append(q, k, v, out=out)
+    inner = slice(front, front + sum(news))
+    assert torch.equal(got[inner], q[inner])
+    assert (got[:front] == 7).all() and (got[rows - back:] == 7).all()
+    out = torch.full((rows, 4, 64), 7.0).to(w.t).cuda()
+    mem.attend(q, max_new=max(news), out=out)
+    assert (out[:front] == 7).all() and (out[rows - back:] == 7).all() and int(w.status) == 0
+    w.check_attend(out[inner], pages=w.dpages, scales=w.dscales)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "e4m3"), ("fp32", "fp32")])
+def test_thousands_of_sequences(torch, B, dtype, fmt):
+    g = np.random.default_rng(3)
+    lens = g.integers(1, 40, 2500).tolist()
+    w = World(torch, lens, [1] * 2500, 2, 1, 64, 16, dtype, fmt, seed=3)
+    mem = w.device(B)
+    got = mem.attend(w.q.cuda(), max_new=1, max_len=40)
+    assert int(w.status) == 0
+    w.check_attend(got)
+    mem.append(None, w.k.cuda(), w.v.cuda())
+    w.check_attend(mem.attend(w.q.cuda(), max_new=1), pages=w.dpages, scales=w.dscales)
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
 def test_queries_in_place_and_outputs_beside_them(torch, B, dtype, fmt):
     """One buffer of rows holds queries, keys, values and outputs: queries are turned in place, outputs interleave."""
     hq, hk, D = 8, 2, 64
