@@ -18,11 +18,13 @@
 // 255 us = 34 TFLOP/s, of keys of 128 541 us).  So a number is split into two of 11 bits and a product
 // taken as three of tf32, off by 2^-19 of itself at most (2 x 2^-21 for what the parts leave out, 2^-22
 // for the product of the low parts): mma.sync has 512 of these multiply-adds a cycle and SM, 170 of
-// the fp32 ones, against 85 to 110 of the plain ones: 160 us = 54 TFLOP/s and 322 us.  Codes are exact
-// in 11 bits and take two products.  What bounds it now is issue: a warp's 384 products of a block of keys
-// (48 % of the tensor pipe's time) stand beside some 1,900 other instructions, half of them the
-// split of keys and values, which do not overlap much with them.  Tiles of 32 rows a warp split half as
-// often, but spill (194 us where 16 rows took 203).
+// the fp32 ones, against 85 to 110 of the plain ones: 170 us = 50 TFLOP/s and 338 us.  The matrix unit cuts
+// its sums off, so products of high and of low parts have sums of their own, and those of 32 keys are added
+// to the output in fp32: over 2,302 keys the result is off by 3.8e-7 of its norm (all in one sum, which takes
+// 6 % less time, 2.3e-6; PyTorch's fp32 products 9e-7).  Codes are exact in 11 bits and take two products.  What bounds
+// it now is issue: a warp's 384 products of a block of keys (51 % of the tensor pipe's time) stand beside some
+// 2,100 other instructions, half of them the split of keys and values, which do not overlap much with them.
+// Tiles of 32 rows a warp split half as often, but spill (194 us where 16 rows took 203).
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -79,11 +81,12 @@ __device__ __forceinline__ void mma8(float (&d)[4], const uint32_t (&a)[4], uint
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// four tiles d += a b of fp32 numbers, so that a product does not wait for the one before it on its
-// tile; CODES: b is exact in 11 bits
+// four tiles (d + r)[i] += a b_i of fp32 numbers: the products of the high parts to d, those with a low
+// part to r, for the matrix unit cuts its sums off and loses half a step of d with each; CODES: b is exact in
+// 11 bits.  A product does not wait for the one before it on its tile
 template <bool CODES>
-__device__ __forceinline__ void mma_split(float (&d0)[4], float (&d1)[4], float (&d2)[4], float (&d3)[4], const uint32_t (&ah)[4],
-                                          const uint32_t (&al)[4], float4 b0, float4 b1) {
+__device__ __forceinline__ void mma_split(float (*d)[4], float (*r)[4], const uint32_t (&ah)[4], const uint32_t (&al)[4], float4 b0,
+                                          float4 b1) {
   const float x[4] = {b0.x, b0.y, b0.z, b0.w}, y[4] = {b1.x, b1.y, b1.z, b1.w};
   uint32_t xh[4], xl[4], yh[4], yl[4];
 #pragma unroll
@@ -92,9 +95,13 @@ __device__ __forceinline__ void mma_split(float (&d0)[4], float (&d1)[4], float 
     xh[i] = CODES ? __float_as_uint(x[i]) : u.hi, xl[i] = u.lo;
     yh[i] = CODES ? __float_as_uint(y[i]) : w.hi, yl[i] = w.lo;
   }
-  if constexpr (!CODES) mma8(d0, ah, xl[0], yl[0]), mma8(d1, ah, xl[1], yl[1]), mma8(d2, ah, xl[2], yl[2]), mma8(d3, ah, xl[3], yl[3]);
-  mma8(d0, al, xh[0], yh[0]), mma8(d1, al, xh[1], yh[1]), mma8(d2, al, xh[2], yh[2]), mma8(d3, al, xh[3], yh[3]);
-  mma8(d0, ah, xh[0], yh[0]), mma8(d1, ah, xh[1], yh[1]), mma8(d2, ah, xh[2], yh[2]), mma8(d3, ah, xh[3], yh[3]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) mma8(d[i], ah, xh[i], yh[i]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) mma8(r[i], al, xh[i], yh[i]);
+  if constexpr (!CODES)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mma8(r[i], ah, xl[i], yl[i]);
 }
 
 // (top, sum, o) joined with another piece's
@@ -159,7 +166,7 @@ __device__ __noinline__ void row_again(const AttendArgs& a, const Tile& t, const
 }
 
 template <int D, int FORMAT, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 4 : 2) * (4 / WARPS)) attend_kernel(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 3 : 2) * (4 / WARPS)) attend_kernel(const __grid_constant__ AttendArgs a) {
   constexpr bool CODES = FORMAT == EVO_CACHE_E4M3;
   constexpr int THREADS = 32 * WARPS, BM = 16 * WARPS, NT = BN / 8, DT = D / 8;
   extern __shared__ __align__(16) uint8_t raw[];
@@ -248,11 +255,11 @@ __global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 4 : 2) * (4 / WARPS)) a
     __syncthreads();
     // s[n]: keys 8 n + 2 c, 8 n + 2 c + 1 of rows g (0, 1) and g + 8 (2, 3).  A contraction's index may be
     // permuted at will: a lane's four dimensions 16 h + 4 c .. + 3 are its places c, c + 4 of two steps
-    float s[NT][4];
+    float s[NT][4], low[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[n][e] = low[n][e] = 0.f;
 #pragma unroll 1
     for (int h = busy ? 0 : D / 16; h < D / 16; ++h) {
       const float4 x = *reinterpret_cast<const float4*>(&sm.q[key_at<D>(16 * warp + g, 16 * h + 4 * c)]);
@@ -265,9 +272,9 @@ __global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 4 : 2) * (4 / WARPS)) a
         float4 k[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[i] = *reinterpret_cast<const float4*>(&sm.k[key_at<D>(8 * (n + i) + g, 16 * h + 4 * c)]);
-        mma_split<CODES>(s[n], s[n + 1], s[n + 2], s[n + 3], ah[0], al[0], make_float4(k[0].x, k[1].x, k[2].x, k[3].x),
+        mma_split<CODES>(s + n, low + n, ah[0], al[0], make_float4(k[0].x, k[1].x, k[2].x, k[3].x),
                          make_float4(k[0].y, k[1].y, k[2].y, k[3].y));
-        mma_split<CODES>(s[n], s[n + 1], s[n + 2], s[n + 3], ah[1], al[1], make_float4(k[0].z, k[1].z, k[2].z, k[3].z),
+        mma_split<CODES>(s + n, low + n, ah[1], al[1], make_float4(k[0].z, k[1].z, k[2].z, k[3].z),
                          make_float4(k[0].w, k[1].w, k[2].w, k[3].w));
       }
     }
@@ -283,7 +290,7 @@ __global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 4 : 2) * (4 / WARPS)) a
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           float& x = s[n][2 * e + i];
-          x *= a.scale_log2;
+          x = (x + low[n][2 * e + i]) * a.scale_log2;
           const int key = k0 + 8 * n + 2 * c + i;
           if (!whole && (key < seen[e].lo || key >= seen[e].hi)) x = -INFINITY;
           top = fmaxf(top, x);
@@ -310,16 +317,35 @@ __global__ void __launch_bounds__(32 * WARPS, (D == 64 ? 4 : 2) * (4 / WARPS)) a
     __syncthreads();
     // weights enter as they left the scores: keys 2 c, 2 c + 1 of 8 are places c, c + 4.  Tile 4 x + y of o
     // holds dimensions 32 x + 8 c + y (0, 2) and 32 x + 8 c + 4 + y (1, 3) of rows g and g + 8
+    // The sums of 32 keys are added to o in fp32 (sums over a long memory in the matrix unit would fall behind by a
+    // half step each: 6e-6 of the values over 16,000 keys)
     if (busy)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const Split p[4] = {split(s[n][0]), split(s[n][2]), split(s[n][1]), split(s[n][3])};
-      const uint32_t ah[4] = {p[0].hi, p[1].hi, p[2].hi, p[3].hi}, al[4] = {p[0].lo, p[1].lo, p[2].lo, p[3].lo};
+    for (int half = 0; half < 2; ++half) {
+      uint32_t ph[NT / 2][4], pl[NT / 2][4];
+#pragma unroll
+      for (int n = 0; n < NT / 2; ++n) {
+        const float(&w)[4] = s[half * (NT / 2) + n];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const Split u = split(w[e % 2 * 2 + e / 2]);
+          ph[n][e] = u.hi, pl[n][e] = u.lo;
+        }
+      }
 #pragma unroll
       for (int x = 0; x < D / 32; ++x) {
-        const float4 u = *reinterpret_cast<const float4*>(&sm.v[value_at<D>(8 * n + 2 * c, 32 * x + 4 * g)]);
-        const float4 w = *reinterpret_cast<const float4*>(&sm.v[value_at<D>(8 * n + 2 * c + 1, 32 * x + 4 * g)]);
-        mma_split<CODES>(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3], ah, al, u, w);
+        float d[4][4] = {}, r[4][4] = {};
+#pragma unroll
+        for (int n = 0; n < NT / 2; ++n) {
+          const int key = 8 * (half * (NT / 2) + n) + 2 * c;
+          const float4 u = *reinterpret_cast<const float4*>(&sm.v[value_at<D>(key, 32 * x + 4 * g)]);
+          const float4 w = *reinterpret_cast<const float4*>(&sm.v[value_at<D>(key + 1, 32 * x + 4 * g)]);
+          mma_split<CODES>(d, r, ph[n], pl[n], u, w);
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[4 * x + y][e] += d[y][e] + r[y][e];
       }
     }
     __syncthreads();                               // every warp has read the values
@@ -525,10 +551,10 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
   else if (few)   // 4 rows a tile while that fills the GPU sooner (3 x 16 rows over 333 keys: 8.3 us against 12.4 with 16)
     p.tile_rows = all == 1 ? 1 : all <= 4 || (long long)m.n_seq * m.n_kv_head < 152 ? 4 : 16;
   else
-    // 64 rows a block, of which up to 32 idle; blocks of 32 where the idle ones' shared memory keeps others out
-    // (64 x 32 fp32 rows over 4,000 keys of 128: 928 us against 1,284; of 64, or 8-bit ones: slower, 2 x 32
-    // rows over 500 keys 28.8 against 24.7)
-    p.tile_rows = all <= 32 && m.head_dim == 128 && m.format == EVO_CACHE_F32 && (long long)m.n_seq * m.n_kv_head >= 152 ? 32 : 64;
+    // 64 rows a block, of which up to 32 idle; blocks of 32 where there are items enough to fill the GPU with them
+    // (64 x 32 rows over 4,000 keys of 64: 404 us against 581; of 128: 928 against 1,284, but 8-bit ones 1,658
+    // against 1,234; 2 x 32 rows over 500 keys of 128: 28.8 against 24.7)
+    p.tile_rows = all <= 32 && (m.head_dim == 64 || m.format == EVO_CACHE_F32) && (long long)m.n_seq * m.n_kv_head >= 152 ? 32 : 64;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   p.cluster = 1;
@@ -595,7 +621,8 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
     a.m.n_pages = a.m.n_seq * p.expand;
   }
   if (p.kernel == ATTEND_F32)
-    e = p.tile_rows == 32 ? launch_f32_as<128, EVO_CACHE_F32, 2>(a, st) : d64 ? launch_f32<64, 4>(a, st) : launch_f32<128, 4>(a, st);
+    e = p.tile_rows == 32 ? d64 ? launch_f32<64, 2>(a, st) : launch_f32_as<128, EVO_CACHE_F32, 2>(a, st)
+        : d64 ? launch_f32<64, 4>(a, st) : launch_f32<128, 4>(a, st);
   else if (p.kernel == ATTEND_F32_ROWS)
     e = launch_attend_f32_rows(a, p.tile_rows, st);
   else if (p.kernel == ATTEND_ROWS)
