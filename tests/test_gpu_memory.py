@@ -591,6 +591,22 @@ def test_rows_before_and_behind_the_sequences_stay(torch, B, dtype, fmt, m):
     w.check_attend(out[inner], pages=w.dpages, scales=w.dscales)
 
 
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_sequences_of_short_chunks(torch, B, dtype, fmt, D):
+    """80 sequences of two key heads: chunks of up to 24 tokens, of which some see nothing, one is empty."""
+    g = np.random.default_rng(D)
+    news = g.integers(1, 25, 80).tolist()
+    news[7], news[8] = 0, 24
+    lens = (np.array(news) + g.integers(-5, 200, 80)).clip(0).tolist()
+    w = World(torch, lens, news, 2, 2, D, 32, dtype, fmt, seed=D)
+    mem = w.device(B)
+    q = w.q.cuda()
+    w.check_attend(mem.attend(q, max_new=24))
+    w.check_attend(mem.attend(q, causal=False, window=50, max_new=24), causal=False, window=50)
+    assert int(w.status) == 0
+
+
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "e4m3"), ("fp32", "fp32")])
 def test_thousands_of_sequences(torch, B, dtype, fmt):
     g = np.random.default_rng(3)
