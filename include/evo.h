@@ -339,7 +339,8 @@ evo_status evo_cache_add(const uint8_t* codes, const uint8_t* scales, const uint
  * rows or max_new, and a rotation position outside the table make EVO_ERR_CORRUPT in
  * *status (device memory, zeroed by the caller; NULL: not reported).  Nothing out
  * of bounds is read or written for them; evo_memory_append stores no such token
- * and leaves its q_out row, and evo_memory_attend's rows of such a sequence are unspecified. */
+ * and leaves its q_out row, and evo_memory_attend's rows of such a sequence are unspecified.  A wait for copies or
+ * matrix units that ran out makes EVO_ERR_TIMEOUT there: the call's results are unspecified. */
 enum { EVO_CACHE_F32 = 0, EVO_CACHE_BF16 = 1, EVO_CACHE_E4M3 = 2 };
 typedef struct evo_memory {
   int32_t dtype;            /* EVO_DTYPE_* of the rows */
@@ -407,8 +408,7 @@ evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k
  * 2^(s - max) are rounded to 16 bits (off by at most 2^-8 of each) before their
  * product with the values; with more than 16 fp32 rows a key/value head a product
  * of two numbers is off by at most 2^-19 of itself (three tf32 products).
- * Deterministic; asynchronous on the stream.  A wait in a kernel that ran out puts
- * EVO_ERR_TIMEOUT in *status. */
+ * Deterministic; asynchronous on the stream. */
 size_t evo_memory_scratch_bytes(const evo_memory* mem, int32_t rows, int32_t max_new, int32_t max_len);
 evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
                              int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,

@@ -36,7 +36,7 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int RING_WARPS = 4, RING_THREADS = 32 * RING_WARPS;
 constexpr int STAGES = 1;                           // rows a warp holds: 20 warps a SM with one each are ahead of 16 with two (30.1 us)
-constexpr int RING_BLOCKS = 5;                      // blocks a SM
+constexpr int RING_BLOCKS = 5;                      // blocks a SM (6, which spill: 32.1 us)
 constexpr int BATCH = 2;                            // head groups whose loads a warp has in flight
 
 // eight values of a row as they are in memory, and as four pairs of fp32
