@@ -399,6 +399,19 @@ def test_attend_scores_of_every_size(torch, B, dtype, fmt):
     w.check_attend(mem.attend(w.q.cuda(), max_new=70))
 
 
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("m", [1, 12, 20, 45, 200])
+def test_attend_scales(torch, B, dtype, fmt, m):
+    """A scale of zero (the mean of the values), negative, tiny and large ones, at both head widths."""
+    for D in (64, 128):
+        w = World(torch, [m + 150, m // 2], [m, m], 4, 2, D, 16, dtype, fmt, seed=m + D)
+        mem = w.device(B)
+        q = w.q.cuda()
+        for scale in (0.0, -0.125, 1e-30, 2.0):
+            w.check_attend(mem.attend(q, scale=scale, max_new=m), scale=scale)
+        w.check_attend(mem.attend(q, scale=-0.1, causal=False, window=33, max_new=m), scale=-0.1, causal=False, window=33)
+
+
 def test_sequences_share_pages_and_strided_rows(torch, B):
     w = World(torch, [100, 100, 90], [8, 8, 8], 4, 2, 64, 16, "bf16", "e4m3")
     w.table[1] = w.table[0]
