@@ -21,8 +21,8 @@
 //                  whose contiguous index is N)
 // BN is what 512 columns of tensor memory hold of S, P and O of two streams: 128 keys
 // of 64, 64 keys of 128.  Measured (2,048 rows over 16,384 keys of 64, 8 heads / four
-// causal chunks of 1,000 tokens over 8,000, heads of 128): 86 us = 0.80 PFLOP/s / 137 us =
-// 0.86; weights over the scores, so that the next ones wait for the product, 99 / 147; one
+// causal chunks of 1,000 tokens over 8,000, heads of 128): 87 us = 0.79 PFLOP/s / 135 us =
+// 0.88; weights over the scores, so that the next ones wait for the product, 99 / 147; one
 // issuing warp that takes both streams in turn 114 / 150.  What bounds it now is the
 // softmax's issue: its two warps a scheduler are 85 % of the special-function unit while
 // both are at their exponentials, and wait side by side when they are not (alternating them
@@ -31,7 +31,7 @@
 // There is no running maximum: a row's reference is the maximum of its first block,
 // and every further block's weights are summed before they are handed on.  Only where
 // a sum passes 2^16 is a new maximum taken, O rescaled (a pass over TMEM, behind the
-// product before) and the block done again: the common block reads no maximum (a fifth
+// product before) and the block done again, once: the common block reads no maximum (a fifth
 // of the softmax's instructions, which bound it).  Weights are at most 2^16, and bf16
 // holds them with the same relative rounding, 2^-8 at most of each.
 //
@@ -372,15 +372,15 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         tc::tc_fence_after();
       }
       // a row's reference is the maximum of the block where it was set.  The others are taken on
-      // trust: a block whose weights sum to more than 2^16 sets it anew and is done again
-      const float2 sc2 = make_float2(sc, sc);
-      for (bool set = __any_sync(0xffffffffu, top == -INFINITY);;) {
+      // trust: a block whose weights sum to more than 2^16 sets it anew and is done again, once
+      float s1 = sc;                               // factor that the scores in v still lack
+      for (bool set = __any_sync(0xffffffffu, top == -INFINITY), again = true;; again = false) {
         if (set) {
           float m = v[0];
 #pragma unroll
           for (int j = 1; j < BN; ++j) m = fmaxf(m, v[j]);
-          m *= sc;
-          const float now = m > top + LAZY ? m : top;
+          m = __fmul_rn(m, s1);
+          const float now = m - top > LAZY ? m : top;   // (top + LAZY may round to more than LAZY above top)
           const float f = ex2_approx(top - (now == -INFINITY ? 0.f : now));
           top = now;
           l *= f;
@@ -397,7 +397,15 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
           }
         }
         const float ref = top == -INFINITY ? 0.f : -top;
-        const float2 ref2 = make_float2(ref, ref);
+        // The reference is a rounded product, the fused ones below are not: past 2^24 they differ by more
+        // than a step of the exponent, and the largest weight would not be 1.  Where a row of the warp is
+        // that far, scores are rounded first, as the reference was
+        if (__any_sync(0xffffffffu, fabsf(ref) >= 16777216.f)) {
+#pragma unroll
+          for (int j = 0; j < BN; ++j) v[j] = __fmul_rn(v[j], s1);
+          s1 = 1.f;
+        }
+        const float2 sc2 = make_float2(s1, s1), ref2 = make_float2(ref, ref);
         float2 sums[4] = {};                       // chains of their own
 #pragma unroll
         for (int h = 0; h < BN / 64; ++h) {
@@ -412,7 +420,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
         }
         const float2 all4 = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
         set = __any_sync(0xffffffffu, all4.x + all4.y > 65536.f);
-        if (!set) {
+        if (!set || !again) {
           l += all4.x + all4.y;
           break;
         }

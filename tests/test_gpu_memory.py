@@ -744,3 +744,46 @@ def test_binding_refuses(torch, B):
         with pytest.raises(ValueError):
             mem.append(**(dict(q=q, k=k, v=v) | bad))
     assert mem.attend(q[:0]).shape == (0, 4, 64)
+
+
+# ---------------------------------------------------------------- scores past what fp32 resolves
+
+def whole_numbers(torch, w, q_unit, k_unit):
+    """Queries of -1, 0, 1 and keys of -3 .. 3, times a power of two: every score is exact in fp32, and two scores
+    are equal or a unit apart."""
+    g = torch.Generator().manual_seed(77)
+    w.q = (torch.randint(-1, 2, w.q.shape, generator=g).float() * q_unit).to(w.t)
+    k = torch.randint(-3, 4, w.pages[0].shape, generator=g).float() * k_unit
+    k[..., 0] = 3 * k_unit
+    if w.fmt == "e4m3":
+        c, s = M.quantise(k.numpy().astype(np.float64))
+        assert np.array_equal(M.dequantise(c, s), k.double().numpy())
+        w.pages[0], w.scales[0] = torch.from_numpy(c.copy()), torch.from_numpy(s.copy())
+    else:
+        w.pages[0] = k.to(w.t)
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [40, 150])
+def test_attend_scores_of_any_finite_size(torch, B, dtype, fmt, D, m):
+    """Scores from 2^18 to 2^125: weights are equal for the keys with the largest score and zero for all others, so that
+    the score's own rounding moves nothing, and what is left of the tolerance is that of the weights and the sums."""
+    w = World(torch, [m + 300, m // 2 + 40], [m, m], 4, 2, D, 16, dtype, fmt, seed=m + D, stale="none")
+    for q_unit, k_unit, scales in ((1.0, 1.0, (2.0 ** 12, 2.0 ** 21, -2.0 ** 26, 2.0 ** 60, 2.0 ** 118)),
+                                   (2.0 ** 30, 2.0 ** 40, (2.0 ** -8, -2.0 ** -40))):
+        whole_numbers(torch, w, q_unit, k_unit)
+        mem = w.device(B)
+        q = w.q.cuda()
+        for scale in scales:
+            for causal, window in ((True, 0), (False, 90)):
+                got = mem.attend(q, scale=scale, causal=causal, window=window, max_new=m).double().cpu().numpy()
+                for n in range(2):
+                    k, v = w.dense(n)
+                    a, b = int(w.starts[n]), int(w.starts[n + 1])
+                    out, size, _ = M.attend(w.q[a:b].double().numpy(), k, v, 2, scale, causal, window)
+                    half = 2.0 ** -8 if dtype == "bf16" else U
+                    weight = 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+                    tol = half * np.abs(out) + (1 + half) * (weight + w.lens[n] * U) * size + 1e-37
+                    assert (np.abs(got[a:b] - out) <= tol).all(), (scale, causal, n)
+        assert int(w.status) == 0
