@@ -30,13 +30,17 @@
 // the row's reference by 2^8, so the common run has one vote instead of
 // reductions over lanes and a pass over the accumulators.  Weights are then at
 // most 2^8, which the 16-bit operand holds with the same relative rounding.
+// The reference m is subtracted from the product, and the difference multiplied by
+// the row's factor: equal scores have equal weights at any size.  (A fused product minus a
+// rounded reference leaves the largest weight at 2^(rounding error): past fp16 from scores of 2^24.)
 //
 // 8-bit pages: codes become fp16 exactly (one conversion for two).  A key's scale
 // multiplies its row of S^T in fp32; queries are brought to fp16 by an exact power of
 // two per row.  A value's scale 2^k is added to the exponent of its weights,
-// 2^(s + k - m'), with a reference m' of its own, so that the fp16 operand stays in
+// 2^(s - m + k - m'), with an offset m' of its own, so that the fp16 operand stays in
 // range for any mixture of scales; the sum of weights uses 2^(s - m).  The weights'
-// rounding is fp16's (2^-11 of each) there, bf16's (2^-8) with bf16 pages.
+// rounding is fp16's there: 2^-11 of each, or 2^-25 absolute for those that are, with
+// their value's scale, below 2^-14 of the row's largest; bf16's (2^-8) with bf16 pages.
 //
 // Masks are looked at only in runs that some row does not see whole.  There, keys
 // outside the piece give zero values, and a value that is not finite is taken out
@@ -246,7 +250,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
   }
   if constexpr (C::QS) __syncthreads();
 
-  float o[NR][DT][4], sum[NR][2], top[NR][2], vtop[NR][2], limit[NR][2];   // o: dimensions g, g + 8 x rows 2 c, 2 c + 1 of a tile
+  // o: dimensions g, g + 8 x rows 2 c, 2 c + 1 of a tile; top: the row's reference, in units of the product;
+  // voff: what its values' sums stand in beside it, as an exponent (+infinity: it has seen no key)
+  float o[NR][DT][4], sum[NR][2], top[NR][2], voff[NR][2];
 #pragma unroll
   for (int nr = 0; nr < NR; ++nr) {
 #pragma unroll
@@ -254,7 +260,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[nr][j][i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) sum[nr][e] = 0.f, top[nr][e] = vtop[nr][e] = limit[nr][e] = -INFINITY;
+    for (int e = 0; e < 2; ++e) sum[nr][e] = 0.f, top[nr][e] = -INFINITY, voff[nr][e] = INFINITY;
   }
 
   int stage = 0;
@@ -356,7 +362,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
             }
         }
     }
-    // does a score pass its row's reference by 2^LAZY?  (limits are held in units of the product.)
+    // does a score pass its row's reference by 2^LAZY?  The reference is subtracted before the factor is
+    // multiplied in, here as for the weights, so that the largest weight is 1 at any size of the scores.
     // 8-bit pages: or could a weight times its value's scale pass what fp16 holds, 2^(LAZY + SLACK)
     bool raise = false;
 #pragma unroll
@@ -366,37 +373,41 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
         float m = fmaxf(s[nr][0][e], s[nr][0][2 + e]);
 #pragma unroll
         for (int b = 1; b < NB; ++b) m = fmaxf(m, fmaxf(s[nr][b][e], s[nr][b][2 + e]));
-        raise |= m > limit[nr][e];
-        if constexpr (E4M3) raise |= top[nr][e] + vs_top > vtop[nr][e] + SLACK;
+        raise |= (m - top[nr][e]) * rf[nr][e] > LAZY;
+        if constexpr (E4M3) raise |= vs_top > voff[nr][e] + SLACK;
       }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float m = -INFINITY, mv = -INFINITY;
+          float m = s[nr][0][e];
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float x = s[nr][b][2 * i + e] * rf[nr][e];
-              m = fmaxf(m, x);
-              if constexpr (E4M3) mv = fmaxf(mv, x + vs[b][i]);
-            }
+            for (int i = 0; i < 2; ++i) m = fmaxf(m, s[nr][b][2 * i + e]);
 #pragma unroll
-          for (int x = 4; x < 32; x *= 2) {
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-            if constexpr (E4M3) mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
-          }
+          for (int x = 4; x < 32; x *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
           m = fmaxf(m, top[nr][e]);
-          // the values' reference: the row's own largest weight times scale so far, raised no further
-          // than this run's weights need, so that no outlier of negligible weight pushes the others out
-          mv = E4M3 ? fmaxf(mv, vtop[nr][e]) : m;
-          const float f = ex2_approx(top[nr][e] - (m == -INFINITY ? 0.f : m));
-          const float fv = E4M3 ? ex2_approx(vtop[nr][e] - (mv == -INFINITY ? 0.f : mv)) : f;
+          const float base = m == -INFINITY ? 0.f : m, down = (top[nr][e] - base) * rf[nr][e];
+          const float f = ex2_approx(down);
+          float fv = f;
+          if constexpr (E4M3) {
+            // the values' reference: the row's own largest weight times scale so far, raised no further
+            // than this run's weights need, so that no outlier of negligible weight pushes the others out
+            float mv = -INFINITY;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) mv = fmaxf(mv, (s[nr][b][2 * i + e] - base) * rf[nr][e] + vs[b][i]);
+#pragma unroll
+            for (int x = 4; x < 32; x *= 2) mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, x));
+            const float old = top[nr][e] == -INFINITY ? -INFINITY : voff[nr][e] + down;
+            mv = fmaxf(mv, old);
+            fv = ex2_approx(old - (mv == -INFINITY ? 0.f : mv));
+            voff[nr][e] = m == -INFINITY ? INFINITY : mv;
+          }
           top[nr][e] = m;
-          vtop[nr][e] = mv;
-          limit[nr][e] = (m + LAZY) / rf[nr][e];
           sum[nr][e] *= f;
 #pragma unroll
           for (int j = 0; j < DT; ++j) o[nr][j][e] *= fv, o[nr][j][2 + e] *= fv;
@@ -408,14 +419,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
     for (int nr = 0; nr < NR; ++nr) {
       const float2 r2 = make_float2(rf[nr][0], rf[nr][1]);
       const float2 m2 = make_float2(top[nr][0] == -INFINITY ? 0.f : -top[nr][0], top[nr][1] == -INFINITY ? 0.f : -top[nr][1]);
-      const float2 v2 = make_float2(vtop[nr][0] == -INFINITY ? 0.f : -vtop[nr][0], vtop[nr][1] == -INFINITY ? 0.f : -vtop[nr][1]);
+      const float2 v2 = make_float2(-voff[nr][0], -voff[nr][1]);
       float2 l2 = make_float2(sum[nr][0], sum[nr][1]);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float2 x = make_float2(s[nr][b][2 * i], s[nr][b][2 * i + 1]);
-          float2 w = fma2(x, r2, m2);
+          const float2 x = add2(make_float2(s[nr][b][2 * i], s[nr][b][2 * i + 1]), m2);
+          float2 w = mul2(x, r2);
           w = make_float2(ex2_approx(w.x), ex2_approx(w.y));
           l2 = add2(l2, w);
           if constexpr (E4M3) {
@@ -500,8 +511,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
         *reinterpret_cast<float2*>(mine + r * LD + d) = make_float2(o[nr][j][e], o[nr][j][2 + e]);
       }
       if (g == 0) {
-        stat[warp][r] = make_float2(top[nr][e], l);
-        if constexpr (E4M3) vmax[warp][r] = vtop[nr][e];
+        stat[warp][r] = make_float2(top[nr][e] * rf[nr][e], l);
+        if constexpr (E4M3) vmax[warp][r] = voff[nr][e];
       }
     }
   __syncthreads();
@@ -519,8 +530,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
       const float2 ml = stat[w][r];
       const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(mem + w * C::RING) + r * LD + d);
       const float f = ex2_approx(ml.x - ref);
-      // 8-bit pages: the sums stand in units of 2^m'
-      const float fv = E4M3 ? (ml.x == -INFINITY ? 0.f : ex2_approx(vmax[E4M3 ? w : 0][r] - ref)) : f;
+      // 8-bit pages: the sums stand in units of 2^(m + m')
+      const float fv = E4M3 ? (ml.x == -INFINITY ? 0.f : ex2_approx(vmax[E4M3 ? w : 0][r] + (ml.x - ref))) : f;
       l = fmaf(ml.y, f, l);
       x = make_float4(fmaf(y.x, fv, x.x), fmaf(y.y, fv, x.y), fmaf(y.z, fv, x.z), fmaf(y.w, fv, x.w));
     }

@@ -765,7 +765,7 @@ def whole_numbers(torch, w, q_unit, k_unit):
 
 @pytest.mark.parametrize("dtype,fmt", FORMATS)
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("m", [40, 150])
+@pytest.mark.parametrize("m", [1, 3, 8, 14, 30, 40, 150])
 def test_attend_scores_of_any_finite_size(torch, B, dtype, fmt, D, m):
     """Scores from 2^18 to 2^125: weights are equal for the keys with the largest score and zero for all others, so that
     the score's own rounding moves nothing, and what is left of the tolerance is that of the weights and the sums."""
