@@ -394,6 +394,7 @@ evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k
  * m sees tokens up to its own, lens[n] - m + j.  window > 0: only the last `window`
  * of those.  A row that sees no key is zero; what a masked token holds (a NaN,
  * too) reaches no row that does not see it.
+ *   scale   finite, and so is scale * log2(e) in fp32 (EVO_ERR_ARG)
  *   q, out  device [rows][n_head][head_dim], ldq / ldo elements between rows; start
  *           on 16 bytes, strides multiples of 16 bytes.  They share no byte
  *           (EVO_ERR_ARG; column ranges of one buffer may interleave)

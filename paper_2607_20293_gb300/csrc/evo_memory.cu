@@ -209,7 +209,8 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
   if (rows == 0) return EVO_OK;
   s = attend_sizes(mem, rows, max_new, max_len);
   if (s != EVO_OK) return s;
-  if (!q || !out || !std::isfinite(scale) || (causal != 0 && causal != 1) || window < 0) return EVO_ERR_ARG;
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if (!q || !out || !std::isfinite(scale_log2) || (causal != 0 && causal != 1) || window < 0) return EVO_ERR_ARG;
   if (!rows_ok(mem, q, ldq, mem->n_head) || !rows_ok(mem, out, ldo, mem->n_head)) return EVO_ERR_ARG;
   if (rows_overlap(mem, q, ldq, mem->n_head, out, ldo, mem->n_head, rows)) return EVO_ERR_ARG;
   const AttendPlan p = plan_attend(*mem, rows, max_new, max_len);
@@ -224,7 +225,7 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
   a.max_new = max_new;
   a.max_len = max_len;
   a.group = mem->n_head / mem->n_kv_head;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale_log2;
   a.causal = causal;
   a.window = window;
   EVO_CUDA(launch_attend(a, p, scratch, reinterpret_cast<cudaStream_t>(stream)));

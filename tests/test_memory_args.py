@@ -83,6 +83,11 @@ def test_attend_arguments(B, over, code):
     assert attend(B, view(B), **over) == getattr(B, "ERR_" + code)
 
 
+@pytest.mark.parametrize("scale", [2.4e38, -3e38, float("-inf")])
+def test_a_scale_whose_base_2_form_is_infinite(B, scale):
+    assert attend(B, view(B), scale=scale) == B.ERR_ARG
+
+
 def test_outputs_that_overlap_what_is_read(B):
     """8 query heads of 64 bf16 are 1,024 bytes, 2 key heads 256; 6 rows."""
     m = view(B)
