@@ -448,13 +448,18 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
 }
 
 // 8-bit pages of every sequence as bf16 pages n * cols + i (i < cols: what max_len tokens fill),
-// keys and values: a power of two times a code is exact in bf16.  16 codes a thread.
+// keys and values: a power of two times a code is exact in bf16.  16 codes a thread.  Pages that no row
+// sees are left out: their entries may name nothing (pages that left the window and were dropped).
 template <int D>
-__global__ void __launch_bounds__(JOIN_THREADS) expand_kernel(const __grid_constant__ evo_memory m, int cols, int max_len, __nv_bfloat16* k,
+__global__ void __launch_bounds__(JOIN_THREADS) expand_kernel(const __grid_constant__ AttendArgs a, int cols, __nv_bfloat16* k,
                                                               __nv_bfloat16* v, int* table) {
+  const evo_memory& m = a.m;
   const int page = blockIdx.x, n = page / cols, i = page % cols;
   if (threadIdx.x == 0 && blockIdx.y == 0) table[page] = page;
-  if ((long long)i * m.page_tokens >= seq_len(m, n, max_len)) return;
+  const SeqRows s = seq_rows(m, n, a.rows, a.max_new);
+  const Tile t{n, 0, 0, 0, s.first, s.count, seq_len(m, n, a.max_len)};
+  const long long at = (long long)i * m.page_tokens;
+  if (s.count == 0 || at >= t.len || at + m.page_tokens <= seen_by(a, t, 0).lo) return;
   const long long head_rows = (long long)m.n_kv_head * m.page_tokens, from = seq_page(m, n, i) * head_rows, to = page * head_rows;
   const uint8_t* codes = static_cast<const uint8_t*>(blockIdx.y ? m.v_pages : m.k_pages);
   const uint8_t* scales = blockIdx.y ? m.v_scales : m.k_scales;
@@ -608,9 +613,9 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
     int* table = reinterpret_cast<int*>(k + 2 * values);
     const dim3 grid(a.m.n_seq * p.expand, 2);
     if (d64)
-      expand_kernel<64><<<grid, JOIN_THREADS, 0, st>>>(a.m, p.expand, a.max_len, k, k + values, table);
+      expand_kernel<64><<<grid, JOIN_THREADS, 0, st>>>(a, p.expand, k, k + values, table);
     else
-      expand_kernel<128><<<grid, JOIN_THREADS, 0, st>>>(a.m, p.expand, a.max_len, k, k + values, table);
+      expand_kernel<128><<<grid, JOIN_THREADS, 0, st>>>(a, p.expand, k, k + values, table);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     a.m.format = EVO_CACHE_BF16;
     a.m.k_pages = k;

@@ -787,3 +787,22 @@ def test_attend_scores_of_any_finite_size(torch, B, dtype, fmt, D, m):
                     tol = half * np.abs(out) + (1 + half) * (weight + w.lens[n] * U) * size + 1e-37
                     assert (np.abs(got[a:b] - out) <= tol).all(), (scale, causal, n)
         assert int(w.status) == 0
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 20, 40, 150, 300])
+def test_pages_that_left_the_window(torch, B, dtype, fmt, D, m):
+    """A memory whose oldest pages were dropped: their entries name no page, and no row of the call sees them."""
+    window, lens, news = 100, [m + 700, m + 31, 450, 60], [m, m, 0, min(m, 60)]
+    w = World(torch, lens, news, 4, 2, D, 16, dtype, fmt, seed=m + D)
+    for causal in (True, False):
+        mem = w.device(B)
+        table = w.table.clone()
+        for n, (ln, new) in enumerate(zip(lens, news)):
+            first = max(0, ln - window - (new - 1 if causal else 0)) if new else ln
+            table[n, :first // 16] = -1 - n
+        w.dtable.copy_(table)
+        got = mem.attend(w.q.cuda(), causal=causal, window=window, max_new=m)
+        assert int(w.status) == 0
+        w.check_attend(got, causal=causal, window=window)
