@@ -537,7 +537,7 @@ int pieces_of(bool tiles, long long blocks, long long rows, int max_len) {
 
 }  // namespace
 
-AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) {
+AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window) {
   AttendPlan p;
   const long long all = (long long)max_new * (m.n_head / m.n_kv_head);
   const bool f32 = m.dtype == EVO_DTYPE_F32, few = all <= (f32 ? 16 : 32);
@@ -561,6 +561,11 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
     // against 1,234; 2 x 32 rows over 500 keys of 128: 28.8 against 24.7)
     p.tile_rows = all <= 32 && (m.head_dim == 64 || m.format == EVO_CACHE_F32) && (long long)m.n_seq * m.n_kv_head >= 152 ? 32 : 64;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
+  // keys that a tile's rows see: a window's, and one more a token behind the first where it moves with the rows.
+  // Pieces by these, by all 16,000 keys: one token, window 256, 5.3 and 9.4 us; by all 8,192: 64 tokens, window 512,
+  // 18.8 and 27.1 (4 x 256 rows, window 1,024 of 16,000, which is two pieces: 26.1 and 23.7)
+  const int group = m.n_head / m.n_kv_head, moves = causal ? std::min(max_new, p.tile_rows / group + 1) : 0;
+  const int keys = window ? (int)std::min<long long>(max_len, (long long)window + moves) : max_len;
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
   p.cluster = 1;
   if (p.kernel == ATTEND_ROWS || p.kernel == ATTEND_F32_ROWS) {
@@ -575,21 +580,21 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len) 
     const int a_sm = f32 ? (p.tile_rows == 16 ? 2 : codes && !wide ? 6 : 3) : wide && (!codes || p.tile_rows == 32) ? 2 : 3;
     const long long places5 = a_sm == 2 ? 288 : a_sm == 3 ? 432 : 860, places8 = a_sm == 2 ? 264 : a_sm == 3 ? 400 : 800;
     if (2 * blocks <= places5) {
-      const long long most = std::max(1, max_len / (f32 ? 64 : 128));
+      const long long most = std::max(1, keys / (f32 ? 64 : 128));
       p.cluster = (int)std::min({8ll, std::max(std::min(5ll, places5 / blocks), places8 / blocks), most});
-      const long long more = p.cluster == 8 ? std::min({8ll, places8 / (8 * blocks), max_len / 2048ll}) : 1;
+      const long long more = p.cluster == 8 ? std::min({8ll, places8 / (8 * blocks), keys / 2048ll}) : 1;
       p.splits = p.cluster * (int)std::max(1ll, more);
     } else {
       // More: several waves, so that sequences of different lengths even out (240 items over 16,000 keys:
       // 157 us in one piece, 116 in 7; 64 ragged sequences 134 us, in clusters 147), of pieces that are
       // worth the kernel that joins them (over 2,000 keys 26 us in one, 33 in 7).  Tiles of 32 rows pay
       // 10 us a wave of further blocks (64 sequences: 99 us in one piece, 104 in two; 45: 314 and 285).
-      const long long most = std::max(1, max_len / 1024);
+      const long long most = std::max(1, keys / 1024);
       const long long want = p.tile_rows == 32 ? 900 / blocks : (1824 + blocks / 2) / blocks;
       p.splits = (int)std::max(1ll, std::min({most, want, 64ll}));
     }
   } else {
-    p.splits = pieces_of(tiles, blocks, all, max_len);
+    p.splits = pieces_of(tiles, blocks, all, keys);
   }
   const int parts = p.splits / p.cluster;
   p.scratch = parts == 1 ? 0 : (size_t)parts * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);

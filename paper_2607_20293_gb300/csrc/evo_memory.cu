@@ -198,7 +198,7 @@ evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k
 
 size_t evo_memory_scratch_bytes(const evo_memory* mem, int32_t rows, int32_t max_new, int32_t max_len) {
   if (memory_ok(mem) != EVO_OK || attend_sizes(mem, rows, max_new, max_len) != EVO_OK) return 0;
-  return plan_attend(*mem, rows, max_new, max_len).scratch;
+  return plan_attend(*mem, rows, max_new, max_len, 0, 0).scratch;
 }
 
 evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
@@ -213,7 +213,12 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
   if (!q || !out || !std::isfinite(scale_log2) || (causal != 0 && causal != 1) || window < 0) return EVO_ERR_ARG;
   if (!rows_ok(mem, q, ldq, mem->n_head) || !rows_ok(mem, out, ldo, mem->n_head)) return EVO_ERR_ARG;
   if (rows_overlap(mem, q, ldq, mem->n_head, out, ldo, mem->n_head, rows)) return EVO_ERR_ARG;
-  const AttendPlan p = plan_attend(*mem, rows, max_new, max_len);
+  // pieces by what a window leaves to see, in the workspace that a call without one has
+  AttendPlan p = plan_attend(*mem, rows, max_new, max_len, 0, 0);
+  if (window) {
+    const AttendPlan w = plan_attend(*mem, rows, max_new, max_len, causal, window);
+    if (w.scratch <= p.scratch) p = w;
+  }
   if (p.scratch && (!scratch || !aligned(scratch, 16))) return EVO_ERR_ARG;
   AttendArgs a{};
   a.m = *mem;

@@ -57,7 +57,7 @@ struct AttendPlan {
   int tile_rows, tiles, splits, cluster, expand;
   size_t scratch;
 };
-AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len);
+AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window);
 cudaError_t launch_attend_rows(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_attend_rows.cu
 cudaError_t launch_attend_f32_rows(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_attend_f32.cu
 cudaError_t launch_attend_tiles(const AttendArgs& a, cudaStream_t st);                // evo_attend_tiles.cu

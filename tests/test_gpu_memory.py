@@ -806,3 +806,22 @@ def test_pages_that_left_the_window(torch, B, dtype, fmt, D, m):
         got = mem.attend(w.q.cuda(), causal=causal, window=window, max_new=m)
         assert int(w.status) == 0
         w.check_attend(got, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("m,length", [(1, 9000), (6, 9000), (30, 3000), (100, 2000), (400, 1200)])
+def test_windows_of_every_size_fit_the_workspace(torch, B, dtype, fmt, m, length):
+    """A call stays in the bytes that its sizes ask for, whatever window cuts its pieces."""
+    import ctypes
+    w = World(torch, [length, length - 700], [m, m], 4, 2, 64, 16, dtype, fmt, seed=m)
+    mem = w.device(B)
+    q, out = w.q.cuda(), torch.empty(2 * m, 4, 64, dtype=w.t, device="cuda")
+    nb = B.load().evo_memory_scratch_bytes(mem._ref, 2 * m, m, length)
+    scratch = torch.full((nb + (8 << 20),), 85, dtype=torch.uint8, device="cuda")
+    for causal, window in ((1, 0), (1, 1), (1, 17), (0, 300), (1, 1025), (0, 2500), (1, length), (0, 2 ** 31 - 1)):
+        scratch.fill_(85)
+        rc = B.load().evo_memory_attend(mem._ref, q.data_ptr(), 256, 2 * m, m, length, 0.125, causal, window, out.data_ptr(), 256,
+                                        scratch.data_ptr(), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+        assert rc == B.OK
+        assert (scratch[nb:] == 85).all() and int(w.status) == 0
+        w.check_attend(out, causal=bool(causal), window=window)
