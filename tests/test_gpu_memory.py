@@ -825,3 +825,140 @@ def test_windows_of_every_size_fit_the_workspace(torch, B, dtype, fmt, m, length
         assert rc == B.OK
         assert (scratch[nb:] == 85).all() and int(w.status) == 0
         w.check_attend(out, causal=bool(causal), window=window)
+
+
+# ---------------------------------------------------------------- append of thousands of rows (the kernel with a ring of rows)
+
+def check_append_of_many(w, q_out, q_gain, k_gain, eps, base, pos0):
+    """As check_append, all rows at once."""
+    torch = w.torch
+    n = np.repeat(np.arange(len(w.news)), w.news)
+    at = np.concatenate([np.arange(ln - m, ln) for ln, m in zip(w.lens, w.news)])
+    pos = at + np.asarray(pos0)[n]
+    page, slot = w.table.numpy()[n, at // w.page], at % w.page
+    half, rows = 2.0 ** -8 if w.dtype == "bf16" else U, len(n)
+
+    def want(x, gain):
+        y = M.normed_and_turned(x.double().numpy()[:rows], gain, eps, pos, base)
+        a = np.hypot(*np.split(y, 2, -1))
+        return y, 32 * U * np.concatenate([a, a], -1) + 1e-37
+    y, tol = want(w.q, q_gain)
+    assert (np.abs(q_out.double().cpu().numpy()[:rows] - y) <= tol + half * (np.abs(y) + tol)).all()
+    y, tol = want(w.k, k_gain)
+    v = w.v.double().numpy()[:rows]
+    touched = torch.zeros(w.pages[0].shape[:3], dtype=torch.bool)
+    touched[page, :, slot] = True
+    for i, (e, t) in enumerate(((y, tol), (v, 0.0))):
+        got = w.dpages[i].cpu()
+        mine = got[page, :, slot]
+        if w.fmt == "e4m3":
+            s = w.dscales[i].cpu()
+            c, k = mine.numpy(), s[page, :, slot].numpy().astype(np.float64)[..., None] - 127
+            if i == 1:                                             # no arithmetic before the rounding: bit for bit
+                wc, ws = M.quantise(e)
+                assert np.array_equal(c, wc) and np.array_equal(k[..., 0] + 127, ws)
+            amax = np.abs(e).max(-1, keepdims=True)
+            assert (amax <= 448 * 2.0 ** k * (1 + 1e-4)).all() and ((amax > 448 * 2.0 ** (k - 1) * (1 - 1e-4)) | (k == -126)).all()
+            mine = M.dequantise(c, (k[..., 0] + 127).astype(np.uint8))
+            t = t + np.maximum(2.0 ** -4 * (np.abs(e) + t), 2.0 ** (k - 10))
+            assert torch.equal(s[~touched], w.scales[i][~touched])
+        else:
+            mine = mine.double().numpy()
+            t = t + half * (np.abs(e) + t) if i == 0 else 0.0
+        assert (np.abs(mine - e) <= t).all(), i
+        same = (got.view(torch.uint8) == w.pages[i].view(torch.uint8)).flatten(3).all(-1)
+        assert same[~touched].all()
+
+
+def many_rows(torch, hq, hk, D, dtype, fmt, page, seed, each=700):
+    """Ragged chunks, 6,300 rows or more: first chunks of a memory, an empty one, one of a single token."""
+    g = np.random.default_rng(seed)
+    news = g.integers(each // 2, each + 400, 9).tolist() + [0, 1]
+    while sum(news) < 6300:
+        news.append(int(g.integers(1, each)))
+    lens = [m + int(g.integers(0, 300)) for m in news]
+    lens[0], lens[-1] = news[0], news[-1]
+    return World(torch, lens, news, hq, hk, D, page, dtype, fmt, seed=seed, stale="none", spare_rows=3)
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("hq,hk,D,page", [(2, 1, 64, 16), (3, 3, 64, 128), (5, 1, 128, 32), (16, 4, 128, 64)])
+def test_append_of_thousands_of_rows(torch, B, dtype, fmt, hq, hk, D, page):
+    w = many_rows(torch, hq, hk, D, dtype, fmt, page, seed=hq + D)
+    mem = w.device(B)
+    g = torch.Generator().manual_seed(1)
+    qg, kg = 1 + 0.3 * torch.randn(D, generator=g), 1 + 0.3 * torch.randn(D, generator=g)
+    pos0 = (torch.arange(len(w.news)) * 97 % 4000).to(torch.int32)
+    rot = torch.from_numpy(B.rotation_table(5600, D, 1e4)).cuda()
+    out = torch.full((w.rows, hq, D), 7.0, dtype=w.t, device="cuda")
+    q = mem.append(w.q.cuda(), w.k.cuda(), w.v.cuda(), qg.cuda(), kg.cuda(), 1e-6, rot, pos0=pos0.cuda(), out=out)
+    assert q is out and (out[-3:] == 7).all() and int(w.status) == 0     # rows behind the last sequence
+    check_append_of_many(w, q, qg.double().numpy(), kg.double().numpy(), 1e-6, 1e4, pos0.numpy())
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "e4m3"), ("fp32", "fp32")])
+def test_append_of_a_hundred_thousand_rows(torch, B, dtype, fmt):
+    """More rows than all warps hold 32 of: blocks that start when others have ended."""
+    g = np.random.default_rng(4)
+    news = g.integers(1, 260, 800).tolist()
+    assert sum(news) > 2 * 152 * 4 * 5 * 16 + 1000
+    w = World(torch, [m + int(x) for m, x in zip(news, g.integers(0, 50, 800))], news, 1, 1, 64, 16, dtype, fmt, seed=4, stale="none")
+    mem = w.device(B)
+    rot = torch.from_numpy(B.rotation_table(320, 64, 1e4)).cuda()
+    q = mem.append(w.q.cuda(), w.k.cuda(), w.v.cuda(), rotation=rot)
+    assert int(w.status) == 0
+    check_append_of_many(w, q, None, None, 0, 1e4, np.zeros(800, int))
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("parts", ["all", "queries", "keys"])
+@pytest.mark.parametrize("extras", [True, False])
+def test_thousands_of_rows_are_those_of_small_calls(torch, B, dtype, fmt, parts, extras):
+    """Rows of a fused projection, queries in place, bit for bit what calls of a sequence each leave; entries that name
+    nothing, lengths past the table and rows outside the sequences are not touched."""
+    hq, hk, D, page = 4, 2, 128, 32
+    a, b = (many_rows(torch, hq, hk, D, dtype, fmt, page, seed=12) for _ in range(2))
+    g = torch.Generator().manual_seed(2)
+    gain = (1 + 0.3 * torch.randn(D, generator=g)).cuda() if extras else None
+    rot = torch.from_numpy(B.rotation_table(1500, D, 1e4)).cuda() if extras else None
+    pos0 = (torch.arange(len(a.news)) * 13 % 50).to(torch.int32).cuda() if extras else None
+    front, back = 5, 3
+    rows = front + a.rows + back
+    fused = torch.cat([a.q.flatten(1), a.k.flatten(1), a.v.flatten(1), torch.zeros(a.rows, 8, dtype=a.t)], 1)
+    fused = torch.cat([fused[:front], fused, fused[:back]]).cuda()
+    two = fused.clone()
+    states = []
+    for w, buf in ((a, fused), (b, two)):
+        w.table[2, (w.lens[2] - w.news[2] // 2) // page] = 10 ** 7       # a bad entry inside the chunk
+        w.table[4, :] = -3
+        w.device(B)
+        w.dlens[5] = w.table.shape[1] * page + 40                       # the chunk's end is past the table
+        cols = [buf[:, i:j].unflatten(1, (-1, D)) for i, j in ((0, hq * D), (hq * D, (hq + hk) * D), ((hq + hk) * D, (hq + 2 * hk) * D))]
+        states.append(cols)
+    starts = (a.starts + front).to(torch.int32).cuda()
+
+    def call(w, cols, at, seqs, starts):
+        mem = B.Memory(w.dpages[0], w.dpages[1], w.dtable[seqs].contiguous(), w.dlens[seqs].contiguous(), hq, k_scales=w.dscales[0],
+                       v_scales=w.dscales[1], starts=starts, status=w.status, dtype=dtype)
+        q, k, v = (x[at] for x in cols)
+        p0 = None if pos0 is None else pos0[seqs].contiguous()
+        if parts == "keys":
+            mem.append(None, k, v, k_gain=gain, rotation=rot, pos0=p0)
+        elif parts == "queries":
+            mem.append(q, None, None, q_gain=gain, rotation=rot, pos0=p0, out=q)
+        else:
+            mem.append(q, k, v, gain, gain, rotation=rot, pos0=p0, out=q)
+    call(a, states[0], slice(0, rows), slice(0, len(a.news)), starts)
+    assert int(a.status) == B.ERR_CORRUPT
+    for n, m in enumerate(b.news):
+        first = front + int(b.starts[n])
+        if m:
+            call(b, states[1], slice(first, first + m), slice(n, n + 1), torch.tensor([0, m], dtype=torch.int32).cuda())
+    assert int(b.status) == B.ERR_CORRUPT
+    assert torch.equal(fused, two)
+    raw = torch.cat([a.q.flatten(1), a.k.flatten(1), a.v.flatten(1), torch.zeros(a.rows, 8, dtype=a.t)], 1)
+    assert torch.equal(fused[:front].cpu(), raw[:front]) and torch.equal(fused[rows - back - 3:rows - back].cpu(), raw[-3:])
+    for x, y, z in zip(a.dpages + a.dscales, b.dpages + b.dscales, a.pages + a.scales):
+        if x is not None:
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+            assert (parts == "queries") == torch.equal(x.cpu().view(torch.uint8), z.view(torch.uint8))
