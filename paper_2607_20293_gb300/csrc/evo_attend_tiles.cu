@@ -128,24 +128,12 @@ __device__ __forceinline__ uint64_t v_desc(uint32_t saddr, int k64) {
 
 // a bounded wait; false once any wait of the block was in vain
 __device__ __forceinline__ bool wait_for(Shared& sh, uint64_t* bar, uint32_t parity) {
-  const uint32_t b = tc::su32(bar), dead = tc::su32(&sh.dead);
-  if (tc::mbar_test(b, parity)) return true;
-  const long long t0 = clock64();
-  while (!tc::block_dead(dead)) {
-    if (tc::mbar_test(b, parity)) return true;
-    if (clock64() - t0 > WAIT_CYCLES_DEFAULT) asm volatile("st.volatile.shared::cta.b32 [%0], 1;" ::"r"(dead) : "memory");
-  }
-  return false;
+  const uint32_t b = tc::su32(bar);
+  return tc::mbar_test(b, parity) || wait_live(b, parity, tc::su32(&sh.dead));
 }
 
 // the same behind a first test that failed, for the issuing warp
-__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) {
-  const long long t0 = clock64();
-  while (!tc::block_dead(dead)) {
-    if (tc::mbar_test(bar, parity)) return;
-    if (clock64() - t0 > WAIT_CYCLES_DEFAULT) asm volatile("st.volatile.shared::cta.b32 [%0], 1;" ::"r"(dead) : "memory");
-  }
-}
+__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) { wait_live(bar, parity, dead); }
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");

@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "evo_ptx.cuh"
+#include "evo_mem_ptx.cuh"
 #include "evo_tc.cuh"
 #include "evo_shapes.h"
 
@@ -461,9 +462,10 @@ cudaError_t launch_obs_cond(const float* w, const int* wo_dev, const int* wo, co
 // that nothing arrives at, through the same bounded-wait helper the loop kernel
 // (helper 0) or the tensor-core kernels (helper 1) use.  No cluster, no copy and
 // no tensor memory are involved, so giving up leaves nothing in flight.  Helper 1
-// runs both of theirs, the GEMMs' and the tile kernel's, and the latter once more
-// with a limit of 10^9 cycles, which has to find the block given up and return at
-// once; the timeout is recorded if all of them ended as they should.
+// runs all of theirs, the GEMMs', the tile kernel's and the two of the paged memory's
+// kernels, and those that end a block's later waits once more with a limit of 10^9
+// cycles, which have to find the block given up and return at once; the timeout is
+// recorded if all of them ended as they should.
 __global__ void wait_probe_kernel(int helper, long long limit, int* status) {
   __shared__ uint64_t bar;
   if (threadIdx.x == 0) {
@@ -487,8 +489,14 @@ __global__ void wait_probe_kernel(int helper, long long limit, int* status) {
       const long long t0 = clock64();
       tc::mbar_wait_live(smem_u32(&bar), 0u, &rec[2], 1000000000ll, smem_u32(&dead));
       const bool at_once = clock64() - t0 < 100000000ll;
+      __shared__ int dead_memory;
+      dead_memory = 0;
+      const uint32_t b = smem_u32(&bar), dm = smem_u32(&dead_memory);
+      bool memory = !wait_full(b, 0u, (int)limit) && !wait_live(b, 0u, dm, limit) && tc::block_dead(dm);
+      const long long t1 = clock64();
+      memory = memory && !wait_live(b, 0u, dm, 1000000000ll) && clock64() - t1 < 100000000ll;
       if (atomicOr(&rec[0], 0) == ST_TIMEOUT && atomicOr(&rec[1], 0) == ST_TIMEOUT && atomicOr(&rec[2], 0) == 0 &&
-          given_up && at_once)
+          given_up && at_once && memory)
         atomicOr(status, ST_TIMEOUT);
     }
   }

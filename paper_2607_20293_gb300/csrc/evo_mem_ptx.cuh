@@ -64,10 +64,22 @@ __device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, 
 __device__ __forceinline__ void fetch_map(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
-// a bounded wait: false if the copies did not arrive
-__device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity) {
-  for (long long i = 0; i < WAIT_POLLS_DEFAULT; ++i)
+// a bounded wait: false if the copies did not arrive within `limit` tests.  A test that fails suspends its
+// warp for 3.8 us (measured on a barrier that nothing arrives at): about 2 s.  A clock in place of the count
+// takes registers that the kernels do not have (64 x 32 rows over 8-bit pages of 64: 94 us against 91)
+__device__ __forceinline__ bool wait_full(uint32_t bar, uint32_t parity, int limit = 1 << 19) {
+  for (int i = 0; i < limit; ++i)
     if (tc::mbar_test(bar, parity)) return true;
+  return false;
+}
+// the same behind a first test that failed, over as soon as any wait of the block was in vain: `dead`
+// is a word of shared memory, zero at the start
+__device__ __forceinline__ bool wait_live(uint32_t bar, uint32_t parity, uint32_t dead, long long limit = WAIT_CYCLES_DEFAULT) {
+  const long long t0 = clock64();
+  while (!tc::block_dead(dead)) {
+    if (tc::mbar_test(bar, parity)) return true;
+    if (clock64() - t0 > limit) asm volatile("st.volatile.shared::cta.b32 [%0], 1;" ::"r"(dead) : "memory");
+  }
   return false;
 }
 // what a block does in which a wait was in vain, after its last one: it reports, and lets the

@@ -60,3 +60,14 @@ def test_wait_probe_rejects_unbounded_limits(torch, B):
             ev.test_wait_timeout(helper, limit)
         assert e.value.code == B.ERR_ARG
     assert ev.status() == B.OK
+
+
+def test_wait_probe_at_its_largest_limit(torch, B):
+    """Every helper gives up there too, within seconds."""
+    import time
+    cfg = synth.config("tiny")
+    ev = B.Evo(cfg, synth.make_weights(cfg, 0), 1)
+    t = time.perf_counter()
+    ev.test_wait_timeout(1, 10 ** 5)
+    assert ev.status() == B.ERR_TIMEOUT
+    assert time.perf_counter() - t < 20
