@@ -486,6 +486,8 @@ class Memory:
                       e4m3 codes with k_scales, v_scales [n_pages][n_kv_head][page_tokens]
     table [n_seq][max_pages], lens [n_seq], starts [n_seq + 1] or None (equal chunks),
     status [1] or None: int32.  The tensors are kept; their contents may change between calls.
+    Calls report what they cannot read or place, and waits that ran out, in status; None: in
+    a word of the memory's own.  status() reads it.
     """
 
     def __init__(self, k_pages, v_pages, table, lens, n_head: int, k_scales=None, v_scales=None, starts=None,
@@ -510,13 +512,25 @@ class Memory:
         v.table = _need(table, "table", i32, (n_seq, cols), dev)
         v.lens = _need(lens, "lens", i32, (n_seq,), dev)
         v.starts = None if starts is None else _need(starts, "starts", i32, (n_seq + 1,), dev)
-        v.status = None if status is None else _need(status, "status", i32, (1,), dev)
+        if status is None:
+            status = _torch.zeros(1, dtype=i32, device=self.device)
+        v.status = _need(status, "status", i32, (1,), dev)
         self.view, self._ref = v, ctypes.byref(v)
         self.n_head, self.n_kv_head, self.head_dim, self.n_seq = n_head, n_kv, dim, n_seq
         self.max_len = cols * page
         self.uniform = starts is None
         self._scratch = {}                          # bytes of scratch by (rows, max_new, max_len)
         self.tensors = (k_pages, v_pages, table, lens, k_scales, v_scales, starts, status)
+
+    def status(self) -> int:
+        """What calls have reported since it was last read: OK, ERR_CORRUPT (an entry, length, start or
+        position out of its bounds) or ERR_TIMEOUT.  Waits for the device's work, and clears it."""
+        if self.device.type == "cuda":
+            _torch.cuda.synchronize(self.device)
+        code = int(self.tensors[-1])
+        if code:
+            self.tensors[-1].zero_()
+        return code
 
     def _rows(self, t, what: str, rows: int, heads: int):
         """(address, elements between rows) of [rows][heads][head_dim], heads of a row contiguous."""

@@ -962,3 +962,24 @@ def test_thousands_of_rows_are_those_of_small_calls(torch, B, dtype, fmt, parts,
         if x is not None:
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
             assert (parts == "queries") == torch.equal(x.cpu().view(torch.uint8), z.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("m", [1, 20, 70, 300])
+def test_a_memory_without_a_status_word_reports_too(torch, B, dtype, fmt, m):
+    w = World(torch, [m + 90, m], [m, m], 2, 1, 64, 16, dtype, fmt, seed=m, stale="none")
+    w.device(B)
+    mem = B.Memory(w.dpages[0], w.dpages[1], w.dtable, w.dlens, 2, k_scales=w.dscales[0], v_scales=w.dscales[1], dtype=dtype)
+    q, k, v = w.q.cuda(), w.k.cuda(), w.v.cuda()
+    w.check_attend(mem.attend(q))
+    assert mem.status() == B.OK
+    w.dtable[1, 0] = w.pages[0].shape[0]
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    for call in (lambda: mem.attend(q), lambda: mem.append(q, k, v), lambda: mem.attend(q, stream=other)):
+        call()
+        assert mem.status() == B.ERR_CORRUPT
+        assert mem.status() == B.OK                                # read and cleared
+    w.dtable.copy_(w.table)
+    mem.attend(q)
+    assert mem.status() == B.OK

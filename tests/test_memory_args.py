@@ -176,3 +176,15 @@ def test_binding_checks_tensors(B):
             m._rows(bad, "q", 6, 4)
     fused = torch.zeros(6, 8 * 64, dtype=torch.bfloat16)
     assert m._rows(fused[:, 128:384].unflatten(1, (4, 64)), "q", 6, 4) == (fused.data_ptr() + 256, 512)
+
+
+def test_a_memory_has_a_status_word(B):
+    torch = pytest.importorskip("torch")
+    pages = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    table, lens, word = torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    m = B.Memory(pages, pages, table, lens, 4)
+    assert m.view.status and m.status() == B.OK
+    m = B.Memory(pages, pages, table, lens, 4, status=word)
+    assert m.view.status == word.data_ptr()
+    word.fill_(B.ERR_CORRUPT)
+    assert m.status() == B.ERR_CORRUPT and int(word) == 0 and m.status() == B.OK
