@@ -609,6 +609,8 @@ class Memory:
             max_new = rows // max(1, self.n_seq) if self.uniform else rows
         if max_len is None:
             max_len = self.max_len
+        if (window | max_new | max_len) >> 31:      # the library's numbers have 32 bits: the nearest that it takes or refuses
+            window, max_new, max_len = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (window, max_new, max_len))
         nb = self._scratch.get((rows, max_new, max_len))
         if nb is None:
             if len(self._scratch) >= 1024:          # max_len may grow with every token

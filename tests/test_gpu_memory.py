@@ -964,6 +964,18 @@ def test_thousands_of_rows_are_those_of_small_calls(torch, B, dtype, fmt, parts,
             assert (parts == "queries") == torch.equal(x.cpu().view(torch.uint8), z.view(torch.uint8))
 
 
+def test_numbers_past_32_bits(torch, B):
+    """A window longer than any memory hides nothing; sizes that no table has are refused."""
+    w = World(torch, [300], [4], 4, 2, 64, 16, "bf16", "bf16")
+    mem, q = w.device(B), w.q.cuda()
+    for window in (2 ** 31, 2 ** 32 + 5, 2 ** 40):
+        w.check_attend(mem.attend(q, window=window))
+    for bad in (dict(max_len=2 ** 32 + 300), dict(max_new=2 ** 32 + 4), dict(window=-2 ** 32 + 7)):
+        with pytest.raises(B.EvoError) as e:
+            mem.attend(q, **bad)
+        assert e.value.code == B.ERR_ARG
+
+
 @pytest.mark.parametrize("dtype,fmt", FORMATS)
 @pytest.mark.parametrize("m", [1, 20, 70, 300])
 def test_a_memory_without_a_status_word_reports_too(torch, B, dtype, fmt, m):
