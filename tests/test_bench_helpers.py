@@ -30,3 +30,19 @@ def test_recorded_traffic_matches_the_current_sources():
         else:
             assert got is None
     assert bench.recorded_traffic("no such workload") is None
+
+
+def test_hash_covers_what_a_denoising_call_reaches(tmp_path):
+    src = os.path.join(os.path.dirname(__file__), "..", "paper_2607_20293_gb300", "csrc")
+    for f in os.listdir(src):
+        (tmp_path / f).write_text(open(os.path.join(src, f)).read())
+    sha = bench.kernel_source_hash(str(tmp_path))
+    assert sha == bench.kernel_source_hash()
+    for f, counts in (("evo_attend.cu", False), ("evo_attend_tiles.cu", False), ("evo_quant.cuh", False), ("evo_memory.cu", False),
+                      ("evo_cache.cu", False), ("evo_append.cu", False), ("evo_tc.cuh", True), ("evo_api.cu", True), ("evo_wide.cu", True)):
+        before = (tmp_path / f).read_text()
+        (tmp_path / f).write_text(before + "\nint more;\n")
+        assert (bench.kernel_source_hash(str(tmp_path)) != sha) == counts, f
+        (tmp_path / f).write_text(before)
+    (tmp_path / "evo_new.cu").write_text("int more;\n")            # a file that nothing is known of counts
+    assert bench.kernel_source_hash(str(tmp_path)) != sha
