@@ -529,7 +529,8 @@ class Memory:
             _torch.cuda.synchronize(self.device)
         code = int(self.tensors[-1])
         if code:
-            self.tensors[-1].zero_()
+            with _torch.inference_mode():           # the word may have been made under it
+                self.tensors[-1].zero_()
         return code
 
     def _rows(self, t, what: str, rows: int, heads: int):

@@ -188,3 +188,12 @@ def test_a_memory_has_a_status_word(B):
     assert m.view.status == word.data_ptr()
     word.fill_(B.ERR_CORRUPT)
     assert m.status() == B.ERR_CORRUPT and int(word) == 0 and m.status() == B.OK
+
+
+def test_status_of_a_memory_made_under_inference_mode(B):
+    torch = pytest.importorskip("torch")
+    with torch.inference_mode():
+        pages = torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+        m = B.Memory(pages, pages, torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), 4)
+        m.tensors[-1].fill_(B.ERR_TIMEOUT)
+    assert m.status() == B.ERR_TIMEOUT and m.status() == B.OK
