@@ -54,9 +54,10 @@ namespace {
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
-bool overlap(const void* a, const void* b, size_t bytes) {
+// do a_bytes at a and b_bytes at b share any?
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + bytes && y < x + bytes;
+  return x < y + b_bytes && y < x + a_bytes;
 }
 
 // what evo_cache_write and evo_cache_add check alike; *per = values of a sample
@@ -69,7 +70,12 @@ evo_status cache_args(int32_t U, int32_t N, int32_t H, int32_t E, const float* x
   if (N == 0 || H == 0) return EVO_OK;
   if ((U > 0 && (!codes || !scales)) || (x == nullptr) != (y == nullptr)) return EVO_ERR_ARG;
   if (!aligned(codes, 16) || !aligned(x, 16) || !aligned(y, 16)) return EVO_ERR_ARG;
-  if (x && x != y && overlap(x, y, (size_t)N * *per * sizeof(float))) return EVO_ERR_ARG;
+  const size_t values = (size_t)N * *per, held = (size_t)U * values;
+  if (x && x != y && overlap(x, 4 * values, y, 4 * values)) return EVO_ERR_ARG;
+  if (U > 0 && (overlap(codes, held, scales, held / UNIT_GROUP) ||
+                (x && (overlap(x, 4 * values, codes, held) || overlap(x, 4 * values, scales, held / UNIT_GROUP) ||
+                       overlap(y, 4 * values, codes, held) || overlap(y, 4 * values, scales, held / UNIT_GROUP)))))
+    return EVO_ERR_ARG;
   return EVO_OK;
 }
 
@@ -145,6 +151,11 @@ evo_status evo_cache_write(const void* r, int32_t dtype, const uint8_t* refresh,
   const evo_status s = cache_args(1, N, H, E, x, y, codes, scales, &per);
   if (s != EVO_OK || N == 0 || H == 0) return s;
   if (!r || !aligned(r, 16)) return EVO_ERR_ARG;
+  // the stream may take the place of an fp32 residual (a thread reads what it writes), nothing else that is read
+  const size_t values = (size_t)N * per, bytes = values * (dtype == EVO_DTYPE_F32 ? 4 : 2);
+  if (overlap(r, bytes, codes, values) || overlap(r, bytes, scales, values / UNIT_GROUP) ||
+      (y && !(y == r && dtype == EVO_DTYPE_F32) && overlap(r, bytes, y, 4 * values)))
+    return EVO_ERR_ARG;
   EVO_CUDA(launch_cache_write(r, dtype, refresh, N, per, x, y, codes, scales, reinterpret_cast<cudaStream_t>(stream)));
   return EVO_OK;
 }

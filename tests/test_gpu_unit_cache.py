@@ -187,3 +187,18 @@ def test_binding_refuses_other_layouts(torch, B):
     assert e.value.code == B.ERR_SHAPE
     with pytest.raises(ValueError):
         B.cache_add(codes[None], scales[None], x[:2])
+
+
+def test_the_stream_takes_the_residuals_place(torch, B):
+    r, x, gate, codes, scales = make(torch, 6, 8, 128, "fp32", 8)
+    rd, c, s = r.cuda(), codes.cuda(), scales.cuda()
+    assert B.cache_write(rd, c, s, x.cuda(), gate.cuda(), out=rd) is rd
+    want = np.where((gate.numpy() != 0)[:, None, None], x.numpy() + r.numpy(), x.numpy())
+    wc, ws = codes.numpy().copy(), scales.numpy().copy()
+    M.cache_write(r.double().numpy(), x.numpy(), gate.numpy(), wc, ws)
+    assert np.array_equal(rd.cpu().numpy(), want)
+    assert np.array_equal(c.cpu().numpy(), wc) and np.array_equal(s.cpu().numpy(), ws)
+    flat = torch.zeros(6 * 8 * 128 + 64, device="cuda")
+    with pytest.raises(B.EvoError) as e:
+        B.cache_write(flat[:-64].view(6, 8, 128), c, s, x.cuda(), out=flat[64:].view(6, 8, 128))
+    assert e.value.code == B.ERR_ARG

@@ -197,3 +197,25 @@ def test_status_of_a_memory_made_under_inference_mode(B):
         m = B.Memory(pages, pages, torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), 4)
         m.tensors[-1].fill_(B.ERR_TIMEOUT)
     assert m.status() == B.ERR_TIMEOUT and m.status() == B.OK
+
+
+def test_unit_cache_buffers_that_overlap(B):
+    """2 samples of 4 x 64: 512 values, 2,048 bytes of fp32, 512 of codes, 16 of scales; two units of them in the sum."""
+    lib = B.load()
+    at = dict(r=P, x=2 * P, y=3 * P, codes=4 * P, scales=5 * P)
+
+    def write(dtype=0, **over):
+        b = at | over
+        return lib.evo_cache_write(b["r"], dtype, None, 2, 4, 64, b["x"], b["y"], b["codes"], b["scales"], None)
+
+    def add(**over):
+        b = at | over
+        return lib.evo_cache_add(b["codes"], b["scales"], None, 2, 2, 4, 64, b["x"], b["y"], None)
+
+    for over in (dict(y=P + 16), dict(y=P - 2032), dict(y=P, dtype=1), dict(codes=P + 2032), dict(codes=P - 496), dict(scales=P + 2047),
+                 dict(scales=P - 15), dict(codes=2 * P), dict(codes=3 * P + 16), dict(scales=3 * P), dict(scales=4 * P + 511),
+                 dict(scales=4 * P - 15), dict(x=2 * P, y=2 * P + 16), dict(r=P, y=P + 1008, dtype=1)):
+        assert write(**over) == B.ERR_ARG, over
+    for over in (dict(codes=2 * P), dict(codes=3 * P - 1008), dict(scales=2 * P + 2040), dict(scales=3 * P - 31), dict(scales=4 * P + 1023),
+                 dict(y=4 * P + 1008), dict(x=5 * P + 16, y=5 * P + 16)):
+        assert add(**over) == B.ERR_ARG, over
