@@ -92,7 +92,7 @@ evo_status memory_ok(const evo_memory* m) {
   // 2^30 tokens: the kernels look runs ahead in 32 bits
   if (m->max_pages > (1 << 30) / m->page_tokens) return EVO_ERR_SHAPE;
   if ((long long)m->n_pages * m->n_kv_head * m->page_tokens > INT_MAX) return EVO_ERR_SHAPE;
-  if (!m->k_pages || !m->v_pages || !m->table || !m->lens) return EVO_ERR_ARG;
+  if (!m->k_pages || !m->v_pages || (m->n_seq > 0 && (!m->table || !m->lens))) return EVO_ERR_ARG;
   if (!aligned(m->k_pages, 16) || !aligned(m->v_pages, 16)) return EVO_ERR_ARG;
   const bool scales = m->format == EVO_CACHE_E4M3;
   if ((m->k_scales != nullptr) != scales || (m->v_scales != nullptr) != scales) return EVO_ERR_ARG;

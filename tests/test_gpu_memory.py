@@ -995,3 +995,78 @@ def test_a_memory_without_a_status_word_reports_too(torch, B, dtype, fmt, m):
     w.dtable.copy_(w.table)
     mem.attend(q)
     assert mem.status() == B.OK
+
+
+# ---------------------------------------------------------------- calls at the edge of what is documented
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+def test_empty_memories_and_calls(torch, B, dtype, fmt):
+    w = World(torch, [0, 0], [3, 3], 4, 2, 64, 16, dtype, fmt)
+    mem = w.device(B)
+    for m, news in ((3, [3, 3]), (60, [60, 60]), (300, [300, 300])):
+        q = torch.randn(sum(news), 4, 64).to(w.t).cuda()
+        starts = torch.tensor([0, m, 2 * m], dtype=torch.int32).cuda()
+        mem = B.Memory(w.dpages[0], w.dpages[1], w.dtable, w.dlens, 4, k_scales=w.dscales[0], v_scales=w.dscales[1], starts=starts, dtype=dtype)
+        for causal, window in ((False, 0), (True, 0), (True, 5)):
+            assert (mem.attend(q, causal=causal, window=window, max_new=m, max_len=0) == 0).all()
+            assert (mem.attend(q, causal=causal, window=window, max_new=m) == 0).all()
+        assert mem.status() == B.OK
+    empty = torch.empty(0, 4, 64, dtype=w.t, device="cuda")
+    none = torch.zeros(0, 1, dtype=torch.int32, device="cuda")
+    mem = B.Memory(w.dpages[0], w.dpages[1], none, none[:, 0].contiguous(), 4, k_scales=w.dscales[0], v_scales=w.dscales[1], dtype=dtype)
+    assert mem.attend(empty).shape == empty.shape
+    assert mem.append(empty, empty[:, :2], empty[:, :2]).shape == empty.shape
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("hq,hk,D", [(256, 1, 64), (130, 2, 128), (1024, 1024, 64), (1024, 8, 64)])
+def test_many_heads(torch, B, dtype, fmt, hq, hk, D):
+    """One token's query heads fill several tiles; as many heads as a call may have."""
+    w = World(torch, [77, 3], [2, 1], hq, hk, D, 16, dtype, fmt, seed=hq)
+    mem = w.device(B)
+    w.check_attend(mem.attend(w.q.cuda(), max_new=2))
+    w.check_attend(mem.attend(w.q.cuda(), max_new=2, causal=False, window=20), causal=False, window=20)
+    q = mem.append(w.q.cuda(), w.k.cuda(), w.v.cuda())
+    assert torch.equal(q.cpu(), w.q) and mem.status() == B.OK
+    check_append(w, mem, q, None, None, 0, None)
+
+
+def test_streams_by_every_name(torch, B):
+    w = World(torch, [9000], [1], 4, 2, 64, 64, "bf16", "e4m3")
+    mem, q = w.device(B, starts=False), w.q.cuda()
+    torch.cuda.synchronize()
+    want = mem.attend(q)
+    for st in (0, torch.cuda.default_stream(), torch.cuda.current_stream(), torch.cuda.current_stream().cuda_stream, torch.cuda.Stream()):
+        got, turned = mem.attend(q, stream=st), mem.append(q, None, None, stream=st)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(turned, q)
+
+
+def test_one_memory_read_by_two_host_threads(torch, B):
+    """Calls of different sizes on one memory at once, each thread on its stream: workspaces are a call's own."""
+    import threading
+    w = World(torch, [6000, 5000], [40, 40], 4, 2, 64, 64, "bf16", "e4m3")
+    mem = w.device(B)
+    q = w.q.cuda()
+    calls = [dict(max_new=40), dict(max_new=41, window=900), dict(max_new=44, causal=False), dict(max_new=80, max_len=6016)]
+    want = [mem.attend(q, **c) for c in calls]
+    torch.cuda.synchronize()
+    bad = []
+
+    def run(first):
+        st = torch.cuda.Stream()
+        try:
+            with torch.cuda.stream(st):
+                for i in range(100):
+                    c = (first + i) % len(calls)
+                    if not torch.equal(mem.attend(q, **calls[c]), want[c]):
+                        bad.append(c)
+        except Exception as e:                                     # noqa: BLE001
+            bad.append(e)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not bad and int(w.status) == 0

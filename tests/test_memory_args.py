@@ -219,3 +219,9 @@ def test_unit_cache_buffers_that_overlap(B):
     for over in (dict(codes=2 * P), dict(codes=3 * P - 1008), dict(scales=2 * P + 2040), dict(scales=3 * P - 31), dict(scales=4 * P + 1023),
                  dict(y=4 * P + 1008), dict(x=5 * P + 16, y=5 * P + 16)):
         assert add(**over) == B.ERR_ARG, over
+
+
+def test_a_memory_of_no_sequences_needs_no_table(B):
+    m = view(B, n_seq=0, table=None, lens=None, starts=None)
+    assert append(B, m, rows=0) == B.OK and attend(B, m, rows=0) == B.OK
+    assert append(B, m) == B.ERR_ARG and attend(B, m) == B.ERR_ARG
