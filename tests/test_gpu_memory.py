@@ -1070,3 +1070,50 @@ def test_one_memory_read_by_two_host_threads(torch, B):
         t.join()
     torch.cuda.synchronize()
     assert not bad and int(w.status) == 0
+
+
+@pytest.mark.parametrize("dtype,fmt", FORMATS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [2, 7, 15, 30, 60, 200])
+def test_queries_that_are_not_numbers(torch, B, dtype, fmt, D, m):
+    """A NaN query gives NaN in its own row and head, and no other row knows of it."""
+    w = World(torch, [m + 200, m], [m, m], 2, 2, D, 16, dtype, fmt, seed=m)
+    w.q[0, 0, 5] = float("nan")
+    w.q[m + 1, 1] = float("nan")
+    mem = w.device(B)
+    for window in (0, 50):
+        got = mem.attend(w.q.cuda(), max_new=m, window=window).clone()
+        assert got[0, 0].isnan().all() and got[m + 1, 1].isnan().all()
+        sane = w.q.clone()
+        sane[0, 0], sane[m + 1, 1] = 0, 0
+        got[0, 0], got[m + 1, 1] = (mem.attend(sane.cuda(), max_new=m, window=window)[i] for i in ((0, 0), (m + 1, 1)))
+        w.check_attend(got, q=sane, window=window)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("m", [1, 6, 14, 30, 200])
+@pytest.mark.parametrize("size", [2.0 ** 8, 2.0 ** 14, 2.0 ** 30])
+def test_one_large_value_beside_small_ones(torch, B, D, m, size):
+    """8-bit pages, one token with a single large value: the others' columns are off by the weights' rounding, and by
+    2^-25 of the largest weight times scale a key where the weights are fp16 (a code is at most 448)."""
+    w = World(torch, [m + 250, m], [m, m], 2, 2, D, 16, "bf16", "e4m3", seed=m)
+    page, slot = int(w.table[0, 0]), 3
+    v = torch.zeros(2, D, dtype=torch.float64)
+    v[:, 7] = size
+    c, s = M.quantise(v.numpy())
+    w.pages[1][page, :, slot], w.scales[1][page, :, slot] = torch.from_numpy(c), torch.from_numpy(s)
+    mem = w.device(B)
+    got = mem.attend(w.q.cuda(), causal=False, max_new=m).double().cpu().numpy()
+    for n in range(2):
+        k, v = w.dense(n)
+        a, b = int(w.starts[n]), int(w.starts[n + 1])
+        q = w.q[a:b].double().numpy()
+        out, mean, dots = M.attend(q, k, v, 2, D ** -0.5, False, 0)
+        p = np.exp(np.einsum("mhd,khd->mhk", q, k) * D ** -0.5)
+        p /= p.sum(-1, keepdims=True)
+        at = w.table[n, :-(-w.lens[n] // 16)].long()
+        scales = 2.0 ** (w.scales[1][at].double().numpy() - 127).transpose(0, 2, 1).reshape(-1, 2)[:w.lens[n]]
+        most = (p * scales.T[None]).max(-1)[..., None]
+        tol = 2.0 ** -8 * np.abs(out) + (1 + 2.0 ** -8) * ((2 * (D + 8) * U * dots + 2.0 ** -20 + 2.0 ** -8 + w.lens[n] * U) * mean
+                                                           + 2.0 ** -25 * 448 * w.lens[n] * most)
+        assert (np.abs(got[a:b] - out) <= tol).all(), n
