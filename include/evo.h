@@ -401,17 +401,20 @@ evo_status evo_memory_append(const evo_memory* mem, const void* q, const void* k
  *           on 16 bytes, strides multiples of 16 bytes.  They share no byte
  *           (EVO_ERR_ARG; column ranges of one buffer may interleave)
  *   max_new, max_len  at least the largest chunk and memory of the call (max_new 1 ..
- *           rows, max_len at most max_pages * page_tokens): they size the launch,
- *           nothing else depends on them
+ *           rows, max_len at most max_pages * page_tokens): they size the launch, and
+ *           with it the order of the sums, nothing else
  *   scratch device, evo_memory_scratch_bytes(mem, rows, max_new, max_len) bytes (0: none
  *           is needed, or the arguments are refused), 16-byte aligned, caller-owned;
  *           need not be cleared.  Calls that overlap on
  *           the GPU need their own
  * Scores, softmax statistics and sums are fp32.  With bf16 rows the weights
- * 2^(s - max) are rounded to 16 bits (off by at most 2^-8 of each) before their
- * product with the values; with more than 16 fp32 rows a key/value head a product
- * of two numbers is off by at most 2^-19 of itself (three tf32 products).
- * Deterministic; asynchronous on the stream. */
+ * 2^(s - max) are rounded to 16 bits before their product with the values: to bf16
+ * with bf16 pages (2^-8 of each), and with 8-bit pages from 65 rows (tokens times query
+ * heads that share a key/value head, counted by max_new) on, as far as 4 GiB of workspace
+ * hold the pages as bf16; with fewer rows to fp16, where a weight times its value's
+ * scale is off by 2^-11 of itself, or by 2^-25 of the row's largest such product below
+ * 2^-14 of it.  With more than 16 fp32 rows a product of two numbers is off by at most
+ * 2^-19 of itself (three tf32 products).  Deterministic; asynchronous on the stream. */
 size_t evo_memory_scratch_bytes(const evo_memory* mem, int32_t rows, int32_t max_new, int32_t max_len);
 evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
                              int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,

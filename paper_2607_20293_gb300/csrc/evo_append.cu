@@ -14,12 +14,14 @@
 // the rotation needs no exchange, and the norm and the largest magnitude are
 // shuffles over those lanes.
 //
-// The work is bound by DRAM for long chunks and by the chain starts -> length ->
-// table -> page for single tokens.  Calls of few rows spread a row's heads over
-// several warps (64 tokens of 24 heads of 64: 6.2 us).  Calls of many rows copy whole
-// rows to shared memory by bulk copies, issued before the chain is walked, and walk it
-// for all rows of a warp at once: 11,700 rows of 24 heads of 128 take 29.0 us (4.75
-// TB/s), against 32.7 with loads to registers and one chain a row.
+// Single tokens are bound by the chain starts -> length -> table -> page.  Calls of few
+// rows spread a row's heads over several warps (64 tokens of 24 heads of 64: 6.2 us).
+// Calls of many rows copy whole rows to shared memory by bulk copies, issued before the
+// chain is walked, and walk it for all rows of a warp at once: 11,700 rows of 24 heads of
+// 128 take 29.1 us (4.7 TB/s, 70 % of the copy rate), against 32.7 with loads to registers
+// and one chain a row.  What bounds them is latency: a warp has one row at a time, so that
+// nothing of its own is on the way while it computes and stores, and the warps take
+// their four rows in step (half of the issue slots are empty, and DRAM has room).
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>
@@ -36,7 +38,9 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int RING_WARPS = 4, RING_THREADS = 32 * RING_WARPS;
 constexpr int STAGES = 1;                           // rows a warp holds: 20 warps a SM with one each are ahead of 16 with two (30.1 us)
-constexpr int RING_BLOCKS = 5;                      // blocks a SM (6, which spill: 32.1 us)
+// blocks a SM (6: 32.1 us).  Their 96 registers a thread hold bf16 rows over 8-bit pages; with bf16 pages 8 bytes
+// a thread are spilled, with fp32 rows 56
+constexpr int RING_BLOCKS = 5;
 constexpr int BATCH = 2;                            // head groups whose loads a warp has in flight
 
 // eight values of a row as they are in memory, and as four pairs of fp32

@@ -40,8 +40,8 @@ namespace {
 
 constexpr int BN = 64, JOIN_THREADS = 256;
 // from this many rows a key/value head on, 8-bit pages are written out as bf16 pages for the tcgen05
-// kernel (16 sequences of 8,192 keys of 64, us with / without: 64 rows 131 / 129, 96 rows 131 / 152,
-// 256 rows 165 / 362; of 128: 237 / 196, 238 / 331, 267 / 693), while they fit this many bytes
+// kernel (16 sequences of 8,192 keys of 64, us with / without: 64 rows 123 / 103, 96 rows 123 / 144,
+// 256 rows 148 / 331; of 128: 239 / 191, 240 / 272, 251 / 638), while they fit this many bytes
 constexpr int EXPAND_ROWS = 65;
 constexpr long long EXPAND_MOST = 4ll << 30;
 
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
 }
 
 // 8-bit pages of every sequence as bf16 pages n * cols + i (i < cols: what max_len tokens fill),
-// keys and values: a power of two times a code is exact in bf16.  16 codes a thread.  Pages that no row
+// keys and values: a power of two times a code is exact in bf16 (but for steps below 2^-133).  16 codes a thread.  Pages that no row
 // sees are left out: their entries may name nothing (pages that left the window and were dropped).
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS) expand_kernel(const __grid_constant__ AttendArgs a, int cols, __nv_bfloat16* k,
@@ -504,7 +504,9 @@ cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   cfg.gridDim = (unsigned)((outputs * groups + AT_ONCE - 1) / AT_ONCE);
   cfg.blockDim = JOIN_THREADS;
   cfg.stream = st;
-  cudaLaunchAttribute at[1];                       // the launch overlaps the pieces' end; the kernel waits for it
+  // The join may start once every block of the pieces has ended, before what they wrote is visible to all, and
+  // waits for that; none of them lets it start sooner
+  cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
@@ -588,7 +590,8 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len, 
       // More: several waves, so that sequences of different lengths even out (240 items over 16,000 keys:
       // 157 us in one piece, 116 in 7; 64 ragged sequences 134 us, in clusters 147), of pieces that are
       // worth the kernel that joins them (over 2,000 keys 26 us in one, 33 in 7).  Tiles of 32 rows pay
-      // 10 us a wave of further blocks (64 sequences: 99 us in one piece, 104 in two; 45: 314 and 285).
+      // 10 us a wave of further blocks (64 ragged sequences to 4,099 keys: 90.4 us in one piece, 93.2 in two, though
+      // 114 and 107 where all have 4,096; 45 of 16,000: 255 and 235).
       const long long most = std::max(1, keys / 1024);
       const long long want = p.tile_rows == 32 ? 900 / blocks : (1824 + blocks / 2) / blocks;
       p.splits = (int)std::max(1ll, std::min({most, want, 64ll}));

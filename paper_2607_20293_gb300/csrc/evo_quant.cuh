@@ -5,7 +5,8 @@
 // k + 127; a code is x * 2^-k rounded to nearest even.  Scaling by a power of
 // two is exact, so a stored value is off by the one rounding of the code (half
 // a step: 2^-4 of the value, or 2^-10 * 2^k among the subnormal codes), the
-// same on every path, and a value that is read back is exact in bf16 as well.
+// same on every path, and a value that is read back is exact in bf16 as well (its
+// subnormals have steps of 2^-133; codes of the two smallest scales go to 2^-135).
 // A group that holds a NaN or an infinity gets scale byte 255 and reads back
 // as NaN.
 #pragma once
