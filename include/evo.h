@@ -308,10 +308,10 @@ evo_status evo_guided_schedules(const float* d, int32_t U, int32_t T, int32_t K,
  *   codes   device [U][N][H][E], scales device [U][N][H][E/32]
  *   reuse   device [U][N] uint8 or NULL
  * E is a multiple of 32, N * H * E at most 2^33.  N = 0 or H = 0 launches nothing;
- * U = 0 copies x.  x and y are the same buffer or do not overlap, so are y and an
- * fp32 r; no other two of the buffers share a byte; r, x, y and codes start on 16
- * bytes (EVO_ERR_ARG otherwise).  Asynchronous on
- * the stream; every buffer belongs to the current device. */
+ * U = 0 copies x.  y may be x, or an fp32 r; apart from that none of y, codes and scales
+ * shares a byte with another of r, x, y, codes and scales.  r, x, y and codes start on 16
+ * bytes (EVO_ERR_ARG otherwise).  Asynchronous on the stream; every buffer belongs to the
+ * current device. */
 evo_status evo_cache_write(const void* r, int32_t dtype, const uint8_t* refresh, int32_t N, int32_t H, int32_t E,
                            const float* x, float* y, uint8_t* codes, uint8_t* scales, void* stream);
 evo_status evo_cache_add(const uint8_t* codes, const uint8_t* scales, const uint8_t* reuse, int32_t U, int32_t N,
