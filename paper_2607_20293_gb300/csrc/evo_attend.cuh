@@ -63,6 +63,7 @@ __device__ __forceinline__ long long part_index(const AttendArgs& a, int part, i
 }
 
 __device__ __forceinline__ void cluster_arrive_wait() {
+  __syncwarp();                                    // the barrier wants whole warps; lanes left the loop before at their own times
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // the address of this block's shared memory at p in the block of another rank of the cluster

@@ -467,6 +467,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, E4M3, NR>::BLOCKS) rows_kernel
             }
           }
           if (!E4M3 && bad) poison = 1;
+          __syncwarp();                                      // the products are a whole warp's
         }
         if constexpr (E4M3) {
 #pragma unroll

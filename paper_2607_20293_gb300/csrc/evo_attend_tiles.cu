@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
   // operands in the ring: K 0 .. ahead - 1, then V i, K i + ahead
   const auto v_index = [&](int i) { return min(n, i + ahead) + i; };
 
+  __syncwarp();                                    // a whole warp's instruction, behind one lane's prefetches
   if (warp == 0) tc::tmem_alloc(&sh.tmem, 512);
   if (tid == 32) {
     for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], pair ? 2 : 1);
@@ -458,6 +459,7 @@ __global__ void __launch_bounds__(THREADS, 1) tiles_kernel(const __grid_constant
 #pragma unroll 1
       for (int j = 0; j < D / 32; ++j) {
         float o[32];
+        __syncwarp();                              // lanes leave the turn before at their own times
         if (x == 0 || pair) {                      // (a warp's collective load: whole warps of stream B are out)
           if (it > 0) {
             tmem_ld32_async(o_at + 32 * j, o);
