@@ -565,7 +565,7 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len, 
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   // keys that a tile's rows see: a window's, and one more a token behind the first where it moves with the rows.
   // Pieces by these, by all 16,000 keys: one token, window 256, 5.3 and 9.4 us; by all 8,192: 64 tokens, window 512,
-  // 18.8 and 27.1 (4 x 256 rows, window 1,024 of 16,000, which is two pieces: 26.1 and 23.7)
+  // 18.8 and 27.1
   const int group = m.n_head / m.n_kv_head, moves = causal ? std::min(max_new, p.tile_rows / group + 1) : 0;
   const int keys = window ? (int)std::min<long long>(max_len, (long long)window + moves) : max_len;
   const long long blocks = (long long)m.n_seq * m.n_kv_head * p.tiles;
@@ -597,7 +597,11 @@ AttendPlan plan_attend(const evo_memory& m, int rows, int max_new, int max_len, 
       p.splits = (int)std::max(1ll, std::min({most, want, 64ll}));
     }
   } else {
-    p.splits = pieces_of(tiles, blocks, all, keys);
+    // A window: the tcgen05 kernel's pieces as without one, but of 256 keys at least (4 x 256 rows of 16,000 keys of
+    // 64, window 1,024: 20.0 us, 27.3 in one piece; 64 rows, window 128: 9.1 us, 15.8 in pieces of the whole memory's
+    // number); the fp32 kernel's by what is seen (200 rows of 4 heads, keys of 128, window 512: 26.6 us, 32.9 by that rule)
+    p.splits = tiles && window ? std::min(pieces_of(tiles, blocks, all, max_len), std::max(1, keys / 256))
+                               : pieces_of(tiles, blocks, all, keys);
   }
   const int parts = p.splits / p.cluster;
   p.scratch = parts == 1 ? 0 : (size_t)parts * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
