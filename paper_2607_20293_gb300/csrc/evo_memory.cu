@@ -224,7 +224,7 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
   if (!q || !out || !std::isfinite(scale_log2) || (causal != 0 && causal != 1) || window < 0) return EVO_ERR_ARG;
   if (!rows_ok(mem, q, ldq, mem->n_head) || !rows_ok(mem, out, ldo, mem->n_head)) return EVO_ERR_ARG;
   if (rows_overlap(mem, q, ldq, mem->n_head, out, ldo, mem->n_head, rows)) return EVO_ERR_ARG;
-  // pieces by what a window leaves to see, in the workspace that a call without one has
+  // pieces by what a window leaves to see, where they fit the workspace that a call without one has
   AttendPlan p = plan_attend(*mem, rows, max_new, max_len, 0, 0);
   if (window) {
     const AttendPlan w = plan_attend(*mem, rows, max_new, max_len, causal, window);
