@@ -420,6 +420,84 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
                              int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,
                              void* scratch, void* stream);
 
+/* Latent memory: a paged memory whose heads share one vector a token.  Token i of a sequence
+ * is a row of rank + rope values: its latent c (rank), from which every head's key
+ * and value are linear maps, and a key part k (rope) that is rotated by the token's position
+ * and that all heads share.  Against an evo_memory of n_head heads of 128 it holds
+ * (rank + 64) / (256 n_head) of the bytes.  Sequences, pages, rows, lengths and the status word are as for
+ * evo_memory.  Two ways lead to a head's attention of (q_c | q_r) over keys (W_k c | k) and values W_v c:
+ *   absorbed  the caller multiplies queries by the head's key map, q = (q_c W_k | q_r), evo_latent_attend
+ *             attends over the latents themselves, and the caller multiplies the result by W_v.  For
+ *             single tokens and short chunks: a token of the memory is read once for all heads
+ *   expanded  evo_latent_expand writes keys and values to an evo_memory, which evo_memory_attend reads.  For
+ *             long chunks: 640 operations a (row, head, token) against 4 rank + 128 */
+typedef struct evo_latent {
+  int32_t dtype;            /* EVO_DTYPE_* of rows and pages */
+  int32_t n_head;           /* query heads, at most 1024 */
+  int32_t rank;             /* 128, 256 or 512 */
+  int32_t rope;             /* 64 */
+  int32_t page_tokens;      /* 16, 32, 64 or 128 */
+  int32_t n_pages;          /* pages of the pool; n_pages * page_tokens < 2^31 */
+  int32_t max_pages;        /* columns of the table; max_pages * page_tokens at most 2^30 */
+  int32_t n_seq;
+  void* pages;              /* device [n_pages][page_tokens][rank + rope], start on 16 bytes */
+  const int32_t* table;     /* device [n_seq][max_pages] */
+  const int32_t* lens;      /* device [n_seq] */
+  const int32_t* starts;    /* device [n_seq + 1] or NULL */
+  int32_t* status;          /* device [1] or NULL */
+} evo_latent;
+
+/* Append the call's rows to their memories.  Latents get an RMS norm c / sqrt(mean(c^2) + eps) *
+ * gain where c_gain is given; key parts, and the rotated parts of every query's heads, a
+ * rotation of the pairs (i, i + 32) by their position where `rotation` is (evo_rotation_table with
+ * head_dim 64).  Latents and key parts go to their pages, queries to q_out.  fp32 inside, one rounding.
+ *   c, k     device [rows][rank] and [rows][64], ldc / ldk elements between rows (column ranges of one
+ *            projection, say).  Both NULL: only queries are made
+ *   q        device [rows][n_head][64], ldq elements between rows and hdq between heads: the last columns
+ *            of queries [n_head][nope + 64], say.  q and q_out NULL: only tokens are appended
+ *   q_out    the same with ldo and hdo (the last columns of absorbed queries [n_head][rank + 64], say); may be q
+ *            with its strides, and otherwise shares no byte with q, c or k.  Heads of one set may lie between
+ *            another's where both have the same ld; with different ones their extents have to be apart (EVO_ERR_ARG)
+ *   c_gain   device [rank] fp32 or NULL (no norm)
+ *   rotation device [n_pos][64] fp32 or NULL
+ *   pos0     device [n_seq] or NULL (zero): position of a memory's token 0
+ * Buffers start on 16 bytes, strides are multiples of 16 bytes below 2^31 elements, a row's at least what it
+ * holds (EVO_ERR_ARG); no buffer of rows meets the pages.  Two rows of a call must not be the same token of the same
+ * page.  Asynchronous on the stream. */
+evo_status evo_latent_append(const evo_latent* lat, const void* c, int64_t ldc, const void* k, int64_t ldk,
+                             const void* q, int64_t ldq, int64_t hdq, int32_t rows, const float* c_gain, float eps,
+                             const float* rotation, int32_t n_pos, const int32_t* pos0, void* q_out, int64_t ldo,
+                             int64_t hdo, void* stream);
+
+/* Attention of the call's rows over the latents:
+ *   out = softmax over the tokens i that a row sees of (scale <q, (c_i | k_i)>) times c_i
+ * causal, window, max_new, max_len and scratch are as for evo_memory_attend (evo_latent_scratch_bytes in place of
+ * evo_memory_scratch_bytes).  A row that sees no token is zero.  What a masked token holds reaches no row that does
+ * not see it.
+ *   q        device [rows][n_head][rank + 64], ldq elements between rows
+ *   out      device [rows][n_head][rank], ldo elements between rows; shares no byte with q or the pages (EVO_ERR_ARG)
+ *   scale    of the scores; finite, and so is scale * log2(e) in fp32 (EVO_ERR_ARG)
+ * Scores, softmax statistics and sums are fp32.  Deterministic; asynchronous on the stream. */
+size_t evo_latent_scratch_bytes(const evo_latent* lat, int32_t rows, int32_t max_new, int32_t max_len);
+evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
+                             int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,
+                             void* scratch, void* stream);
+
+/* Write tokens first[n] .. lens[n]-1 of every sequence n of a latent memory (lens: the latent memory's) as keys and
+ * values of an ordinary one, to the same token index through its own table:
+ *   key of head h = (w_k[h] c | k),   value of head h = w_v[h] c
+ *   w_k, w_v device [n_head][64][rank] and [n_head][128][rank] of dtype, contiguous, start on 16 bytes
+ *   first    device [n_seq] or NULL (zero)
+ *   max_new, max_len  at least the most tokens of a sequence that are written, and the longest latent memory; they
+ *            size the launch
+ *   mem      dtype of lat and its format (EVO_ERR_UNSUPPORTED otherwise), head_dim 128, n_kv_head = lat's n_head, as many
+ *            sequences; its lens and starts are not read, its pages meet no other buffer, and no two tokens of a
+ *            call are the same token of the same of its pages
+ * Sums are fp32, one rounding.  A range that is not within the memory, or a page entry outside its pool, makes
+ * EVO_ERR_CORRUPT in lat's status, and no such token is written.  Asynchronous on the stream. */
+evo_status evo_latent_expand(const evo_latent* lat, const void* w_k, const void* w_v, const int32_t* first,
+                             int32_t max_new, int32_t max_len, const evo_memory* mem, void* stream);
+
 /* Schedule search (Sec. 3.2 genetic algorithm, Sec. 3.3 redundancy-guided
  * initialisation and target-conditioned early stopping, Eq. 8 and 9).  Host
  * code; fitness comes from the caller:

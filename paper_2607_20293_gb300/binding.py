@@ -47,6 +47,12 @@ class MemoryView(ctypes.Structure):
                                                   "starts", "status")])
 
 
+class LatentView(ctypes.Structure):
+    _fields_ = ([(f, ctypes.c_int32) for f in ("dtype", "n_head", "rank", "rope", "page_tokens", "n_pages", "max_pages",
+                                               "n_seq")]
+                + [(f, ctypes.c_void_p) for f in ("pages", "table", "lens", "starts", "status")])
+
+
 class SearchResult(ctypes.Structure):
     _fields_ = [("best_fitness", ctypes.c_double), ("generations", ctypes.c_int32), ("evaluations", ctypes.c_int32),
                 ("formal_evaluations", ctypes.c_int32), ("memo_hits", ctypes.c_int32),
@@ -86,7 +92,7 @@ def load(debug: bool = False) -> ctypes.CDLL:
     lib = ctypes.CDLL(path)
     P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     cfgp = ctypes.POINTER(EvoConfig)
-    memp = ctypes.POINTER(MemoryView)
+    memp, latp = ctypes.POINTER(MemoryView), ctypes.POINTER(LatentView)
     sig = {
         "evo_weight_count": (SZ, [cfgp]),
         "evo_create": (I32, [P, SZ, cfgp, I32, ctypes.POINTER(P)]),
@@ -118,6 +124,10 @@ def load(debug: bool = False) -> ctypes.CDLL:
         "evo_memory_append": (I32, [memp, P, P, P, I64, I64, I64, I32, P, P, ctypes.c_float, P, I32, P, P, I64, P]),
         "evo_memory_scratch_bytes": (SZ, [memp, I32, I32, I32]),
         "evo_memory_attend": (I32, [memp, P, I64, I32, I32, I32, ctypes.c_float, I32, I32, P, I64, P, P]),
+        "evo_latent_append": (I32, [latp, P, I64, P, I64, P, I64, I64, I32, P, ctypes.c_float, P, I32, P, P, I64, I64, P]),
+        "evo_latent_scratch_bytes": (SZ, [latp, I32, I32, I32]),
+        "evo_latent_attend": (I32, [latp, P, I64, I32, I32, I32, ctypes.c_float, I32, I32, P, I64, P, P]),
+        "evo_latent_expand": (I32, [latp, P, P, P, I32, I32, memp, P]),
         "evo_status_string": (ctypes.c_char_p, [I32]),
     }
     for name, (res, args) in sig.items():
@@ -479,7 +489,41 @@ def rotation_table(n_pos: int, head_dim: int, base: float = 10000.0) -> np.ndarr
     return out
 
 
-class Memory:
+class _Paged:
+    """What the memories share: `tensors`, of which the last is the status word, and sizes of attention calls."""
+
+    def status(self) -> int:
+        """What calls have reported since it was last read: OK, ERR_CORRUPT (an entry, length, start or
+        position out of its bounds) or ERR_TIMEOUT.  Waits for the device's work, and clears it."""
+        if self.device.type == "cuda":
+            _torch.cuda.synchronize(self.device)
+        code = int(self.tensors[-1])
+        if code:
+            with _torch.inference_mode():           # the word may have been made under it
+                self.tensors[-1].zero_()
+        return code
+
+    def _sizes(self, rows: int, max_new, max_len, window: int):
+        """(max_new, max_len, window) of a call; None: what the rows and the table can hold."""
+        if max_new is None:
+            max_new = rows // max(1, self.n_seq) if self.uniform else rows
+        if max_len is None:
+            max_len = self.max_len
+        if (window | max_new | max_len) >> 31:      # the library's numbers have 32 bits: the nearest that it takes or refuses
+            window, max_new, max_len = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (window, max_new, max_len))
+        return max_new, max_len, window
+
+    def _workspace(self, bytes_of, rows: int, max_new: int, max_len: int, stream):
+        """A tensor for the call's scratch, or None; bytes_of: the library's function that says how much."""
+        nb = self._scratch.get((rows, max_new, max_len))
+        if nb is None:
+            if len(self._scratch) >= 1024:          # max_len may grow with every token
+                self._scratch.clear()
+            nb = self._scratch[rows, max_new, max_len] = bytes_of(self._ref, rows, max_new, max_len)
+        return _new(nb, _U8, self.device, stream) if nb else None   # back in that pool once the call returns, for later work of the stream
+
+
+class Memory(_Paged):
     """A paged memory (evo_memory) over caller-owned CUDA tensors.
 
     k_pages, v_pages  [n_pages][n_kv_head][page_tokens][head_dim]: of `dtype`, or uint8
@@ -521,17 +565,6 @@ class Memory:
         self.uniform = starts is None
         self._scratch = {}                          # bytes of scratch by (rows, max_new, max_len)
         self.tensors = (k_pages, v_pages, table, lens, k_scales, v_scales, starts, status)
-
-    def status(self) -> int:
-        """What calls have reported since it was last read: OK, ERR_CORRUPT (an entry, length, start or
-        position out of its bounds) or ERR_TIMEOUT.  Waits for the device's work, and clears it."""
-        if self.device.type == "cuda":
-            _torch.cuda.synchronize(self.device)
-        code = int(self.tensors[-1])
-        if code:
-            with _torch.inference_mode():           # the word may have been made under it
-                self.tensors[-1].zero_()
-        return code
 
     def _rows(self, t, what: str, rows: int, heads: int):
         """(address, elements between rows) of [rows][heads][head_dim], heads of a row contiguous."""
@@ -606,26 +639,147 @@ class Memory:
             op, ldo = self._rows(out, "out", rows, heads)
         if rows == 0:
             return out
-        if max_new is None:
-            max_new = rows // max(1, self.n_seq) if self.uniform else rows
-        if max_len is None:
-            max_len = self.max_len
-        if (window | max_new | max_len) >> 31:      # the library's numbers have 32 bits: the nearest that it takes or refuses
-            window, max_new, max_len = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (window, max_new, max_len))
-        nb = self._scratch.get((rows, max_new, max_len))
-        if nb is None:
-            if len(self._scratch) >= 1024:          # max_len may grow with every token
-                self._scratch.clear()
-            nb = self._scratch[rows, max_new, max_len] = _lib.evo_memory_scratch_bytes(self._ref, rows, max_new, max_len)
-        sp = None
-        if nb:
-            scratch = _new(nb, _U8, self.device, stream)   # back in that pool once this returns, for later work of the stream
-            sp = scratch.data_ptr()
+        max_new, max_len, window = self._sizes(rows, max_new, max_len, window)
+        scratch = self._workspace(_lib.evo_memory_scratch_bytes, rows, max_new, max_len, stream)
+        sp = None if scratch is None else scratch.data_ptr()
         rc = _lib.evo_memory_attend(self._ref, qp, ldq, rows, max_new, max_len, dim ** -0.5 if scale is None else scale,
                                     causal, window, op, ldo, sp, st)
         if rc:
             _check(rc, "evo_memory_attend")
         return out
+
+
+LATENT_ROPE, LATENT_KEY, LATENT_VALUE = 64, 64, 128    # rotated values of a token; widths that evo_latent_expand writes
+
+
+class LatentMemory(_Paged):
+    """A latent memory (evo_latent) over caller-owned CUDA tensors.
+
+    pages [n_pages][page_tokens][rank + 64]: float32 or bfloat16, the type of the rows too
+    table [n_seq][max_pages], lens [n_seq], starts [n_seq + 1] or None (equal chunks),
+    status [1] or None: int32.  Kept and reported to as in Memory.
+    """
+
+    def __init__(self, pages, table, lens, n_head: int, starts=None, status=None):
+        _torch or _load_torch()
+        self.device, dev = pages.device, pages.get_device()
+        self.index, self.dtype = dev, pages.dtype
+        if self.dtype is not _F32 and self.dtype is not _BF16:
+            raise _misfit(pages, "pages", "float32 or bfloat16", pages.shape, dev)
+        n_pages, page, wide = pages.shape
+        n_seq, cols = table.shape
+        rank, i32 = wide - LATENT_ROPE, _I32
+        v = LatentView(0 if self.dtype is _F32 else 1, n_head, rank, LATENT_ROPE, page, n_pages, cols, n_seq)
+        v.pages = _need(pages, "pages", self.dtype, pages.shape, dev)
+        v.table = _need(table, "table", i32, (n_seq, cols), dev)
+        v.lens = _need(lens, "lens", i32, (n_seq,), dev)
+        v.starts = None if starts is None else _need(starts, "starts", i32, (n_seq + 1,), dev)
+        if status is None:
+            status = _torch.zeros(1, dtype=i32, device=self.device)
+        v.status = _need(status, "status", i32, (1,), dev)
+        self.view, self._ref = v, ctypes.byref(v)
+        self.n_head, self.rank, self.n_seq = n_head, rank, n_seq
+        self.max_len = cols * page
+        self.uniform = starts is None
+        self._scratch = {}                          # bytes of scratch by (rows, max_new, max_len)
+        self.tensors = (pages, table, lens, starts, status)
+
+    def _parts(self, t, what: str, shape):
+        """(address, elements between rows, and between heads) of [rows][width] or [rows][heads][width]."""
+        if t.dtype is not self.dtype or t.get_device() != self.index or t.shape != shape or t.stride(-1) != 1:
+            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; expected {self.dtype} "
+                             f"{shape} on {self.device}, the last dimension contiguous")
+        heads, width = (shape[1] if len(shape) == 3 else 1), shape[-1]
+        hd = t.stride(1) if heads > 1 else width
+        ld = t.stride(0) if shape[0] > 1 else max(0, heads - 1) * hd + width
+        return t.data_ptr(), ld, hd
+
+    def _heads(self, t, what: str, rows: int, width: int):
+        """(address, elements between rows) of [rows][n_head][width], the heads of a row contiguous."""
+        p, ld, hd = self._parts(t, what, (rows, self.n_head, width))
+        if hd != width:
+            raise ValueError(f"{what}: strides {t.stride()}; expected the heads of a row contiguous")
+        return p, ld
+
+    def append(self, c, k, q=None, c_gain=None, eps: float = 1e-6, rotation=None, pos0=None, out=None, stream=None):
+        """evo_latent_append: latents c [rows][rank] (normed where c_gain is given) and rotated key parts k
+        [rows][64] to their pages, and the rotated parts q [rows][n_head][64] of the queries to `out` (which may
+        be q, or the last columns of the absorbed queries) or a new tensor.  q may be None (returns None), or c
+        and k.  Rows and heads may be strided."""
+        index = self.index
+        st = _launch_stream(index, stream)
+        if q is None and c is None:
+            raise ValueError("neither queries nor latents")
+        if (c is None) != (k is None):
+            raise ValueError("latents and key parts come together")
+        if out is not None and q is None:
+            raise ValueError("out without q")
+        rows = (c if q is None else q).shape[0]
+        cp = kp = qp = op = gain = rot = at0 = None
+        ldc = ldk = ldq = hdq = ldo = hdo = n_pos = 0
+        if c is not None:
+            cp, ldc, _ = self._parts(c, "c", (rows, self.rank))
+            kp, ldk, _ = self._parts(k, "k", (rows, LATENT_ROPE))
+        if q is not None:
+            shape = (rows, self.n_head, LATENT_ROPE)
+            qp, ldq, hdq = self._parts(q, "q", shape)
+            if out is None:
+                out = _new(shape, self.dtype, self.device, stream)
+            op, ldo, hdo = self._parts(out, "out", shape)
+        if c_gain is not None:
+            gain = _need(c_gain, "c_gain", _F32, (self.rank,), index)
+        if rotation is not None:
+            n_pos = rotation.shape[0]
+            rot = _need(rotation, "rotation", _F32, (n_pos, LATENT_ROPE), index)
+        if pos0 is not None:
+            at0 = _need(pos0, "pos0", _I32, (self.n_seq,), index)
+        rc = _lib.evo_latent_append(self._ref, cp, ldc, kp, ldk, qp, ldq, hdq, rows, gain, eps, rot, n_pos, at0, op, ldo, hdo, st)
+        if rc:
+            _check(rc, "evo_latent_append")
+        return out
+
+    def attend(self, q, scale: float, causal: bool = True, window: int = 0, max_new=None, max_len=None, out=None,
+               stream=None):
+        """evo_latent_attend: attention of absorbed queries q [rows][n_head][rank + 64] over the latents, [rows][n_head][rank]
+        in `out` or a new tensor (rows of no sequence are left as they are: unset in a new tensor).  scale: of
+        the scores, head_dim ** -0.5 of the heads that the queries were absorbed from.  max_new, max_len: bounds on the
+        chunks and memories (None: the rows, or their equal share, and what the table can hold)."""
+        st = _launch_stream(self.index, stream)
+        rows = q.shape[0]
+        qp, ldq = self._heads(q, "q", rows, self.rank + LATENT_ROPE)
+        if out is None:
+            out = _new((rows, self.n_head, self.rank), self.dtype, self.device, stream)
+        op, ldo = self._heads(out, "out", rows, self.rank)
+        if rows == 0:
+            return out
+        max_new, max_len, window = self._sizes(rows, max_new, max_len, window)
+        scratch = self._workspace(_lib.evo_latent_scratch_bytes, rows, max_new, max_len, stream)
+        rc = _lib.evo_latent_attend(self._ref, qp, ldq, rows, max_new, max_len, scale, causal, window, op, ldo,
+                                    None if scratch is None else scratch.data_ptr(), st)
+        if rc:
+            _check(rc, "evo_latent_attend")
+        return out
+
+    def expand(self, w_k, w_v, memory: Memory, first=None, max_new=None, max_len=None, stream=None):
+        """evo_latent_expand: tokens first[n] .. lens[n]-1 (first [n_seq] int32, None: all) as keys (w_k[h] c | k) and values
+        w_v[h] c of `memory`, a Memory of n_head key/value heads of 128, by w_k [n_head][64][rank] and w_v
+        [n_head][128][rank].  max_new, max_len: bounds on the tokens written and held (None: what the table can hold)."""
+        index, heads = self.index, self.n_head
+        st = _launch_stream(index, stream)
+        if max_len is None:
+            max_len = self.max_len
+        if max_new is None:
+            max_new = max_len
+        if (max_new | max_len) >> 31:
+            max_new, max_len = (max(-1, min(int(x), 2 ** 31 - 1)) for x in (max_new, max_len))
+        if memory.index != index:
+            raise ValueError(f"memory is on device {memory.index}, the latents on {index}")
+        rc = _lib.evo_latent_expand(self._ref, _need(w_k, "w_k", self.dtype, (heads, LATENT_KEY, self.rank), index),
+                                    _need(w_v, "w_v", self.dtype, (heads, LATENT_VALUE, self.rank), index),
+                                    None if first is None else _need(first, "first", _I32, (self.n_seq,), index),
+                                    max_new, max_len, memory._ref, st)
+        if rc:
+            _check(rc, "evo_latent_expand")
 
 
 def search(n_units: int, n_steps: int, budget: int, quick, formal=None, d_map=None, block_wise: bool = False,

@@ -24,13 +24,13 @@
 // their four rows in step (half of the issue slots are empty, and DRAM has room).
 #include <algorithm>
 #include <cstdint>
-#include <type_traits>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include "evo_mem_ptx.cuh"
 #include "evo_memory.h"
 #include "evo_quant.cuh"
+#include "evo_rows.cuh"
 
 namespace evo {
 namespace {
@@ -43,35 +43,6 @@ constexpr int STAGES = 1;                           // rows a warp holds: 20 war
 constexpr int RING_BLOCKS = 5;
 constexpr int BATCH = 2;                            // head groups whose loads a warp has in flight
 
-// eight values of a row as they are in memory, and as four pairs of fp32
-template <typename T>
-struct Raw {
-  uint4 u[sizeof(T) / 2];
-};
-__device__ __forceinline__ void values(const Raw<float>& r, float2 (&v)[4]) {
-  v[0] = make_float2(__uint_as_float(r.u[0].x), __uint_as_float(r.u[0].y));
-  v[1] = make_float2(__uint_as_float(r.u[0].z), __uint_as_float(r.u[0].w));
-  v[2] = make_float2(__uint_as_float(r.u[1].x), __uint_as_float(r.u[1].y));
-  v[3] = make_float2(__uint_as_float(r.u[1].z), __uint_as_float(r.u[1].w));
-}
-__device__ __forceinline__ void values(const Raw<__nv_bfloat16>& r, float2 (&v)[4]) {
-  const uint32_t w[4] = {r.u[0].x, r.u[0].y, r.u[0].z, r.u[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-}
-__device__ __forceinline__ void store8(float* p, const float2 (&v)[4]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float2 (&v)[4]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[i].x, v[i].y);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
 enum { QUERY, KEY, VALUE };
 
 // 8 + 8 values of a head (columns 8 l and D/2 + 8 l): norm, rotation and store
@@ -79,12 +50,6 @@ struct Lane {
   float2 c[4], s[4];              // cosines and sines of the row
   float2 g0[4], g1[4];            // gain
 };
-__device__ __forceinline__ void load_pairs(const float* p, float2 (&v)[4]) {
-  Raw<float> r;
-  r.u[0] = reinterpret_cast<const uint4*>(p)[0];
-  r.u[1] = reinterpret_cast<const uint4*>(p)[1];
-  values(r, v);
-}
 
 template <typename T, int D, int FORMAT, int KIND>
 __device__ __forceinline__ void put_head(const AppendArgs& a, const Lane& t, const Raw<T>& r0, const Raw<T>& r1, bool norm,
@@ -168,51 +133,6 @@ __device__ __forceinline__ void put_heads(const AppendArgs& a, Lane& t, const T*
       put_head<T, D, FORMAT, KIND>(a, t, r[i][0], r[i][1], norm, turn, h < n, at0 + (long long)h * a.m.page_tokens, row, h, l);
     }
   }
-}
-
-// where a row belongs
-struct Place {
-  int turn;                       // position for the rotation, or -1: the row is not touched
-  int page, slot;
-};
-
-// the place of this lane's row; reports what it cannot place
-__device__ __forceinline__ Place place_of(const AppendArgs& a, int row) {
-  const evo_memory& m = a.m;
-  Place p{-1, 0, 0};
-  if (row >= a.rows) return p;
-  int n;
-  if (m.starts) {
-    if (row < m.starts[0] || row >= m.starts[m.n_seq]) return p;  // behind the last sequence
-    int lo = 0, hi = m.n_seq;                                     // starts[lo] <= row < starts[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (m.starts[mid] <= row) lo = mid;
-      else hi = mid;
-    }
-    n = lo;
-  } else {
-    n = row / (a.rows / m.n_seq);
-  }
-  const SeqRows s = seq_rows(m, n, a.rows, a.rows);
-  if (row < s.first || row >= s.first + s.count) return p;        // malformed starts
-  const int pos = m.lens[n] - s.count + (row - s.first);
-  const int turn = a.rotation ? pos + (a.pos0 ? a.pos0[n] : 0) : 0;
-  const int pi = pos >> (31 - __clz(m.page_tokens));
-  if (pos < 0 || pi >= m.max_pages || turn < 0 || (a.rotation && turn >= a.n_pos)) {
-    memory_fault(m);
-    return p;
-  }
-  if (a.k) {
-    p.page = m.table[(long long)n * m.max_pages + pi];
-    if ((unsigned)p.page >= (unsigned)m.n_pages) {
-      memory_fault(m);
-      return p;
-    }
-  }
-  p.turn = turn;
-  p.slot = pos & (m.page_tokens - 1);
-  return p;
 }
 
 // a row's heads, from wherever its queries, keys and values lie: groups of HEADS heads of one

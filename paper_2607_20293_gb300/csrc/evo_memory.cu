@@ -1,5 +1,5 @@
-// Entry points of the 8-bit unit caches and the paged memory (include/evo.h):
-// argument checks on the host, then the launch.
+// Entry points of the 8-bit unit caches, the paged memory and the latent memory
+// (include/evo.h): argument checks on the host, then the launch.
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -140,6 +140,77 @@ evo_status attend_sizes(const evo_memory* m, int32_t rows, int32_t max_new, int3
   return EVO_OK;
 }
 
+int item_of(int32_t dtype) { return dtype == EVO_DTYPE_F32 ? 4 : 2; }
+
+// the latent memory as the paged memory whose arguments its kernels take: one key/value head, whose
+// head_dim values are the first of a page's rows
+evo_status latent_ok(const evo_latent* l, evo_memory* m) {
+  if (!l) return EVO_ERR_ARG;
+  if (l->dtype != EVO_DTYPE_F32 && l->dtype != EVO_DTYPE_BF16) return EVO_ERR_ARG;
+  if (l->n_head <= 0 || l->n_pages <= 0 || l->max_pages <= 0 || l->n_seq < 0) return EVO_ERR_ARG;
+  if ((l->rank != 128 && l->rank != 256 && l->rank != 512) || l->rope != LATENT_ROPE || l->n_head > 1024) return EVO_ERR_SHAPE;
+  if (l->page_tokens != 16 && l->page_tokens != 32 && l->page_tokens != 64 && l->page_tokens != 128) return EVO_ERR_SHAPE;
+  if (l->max_pages > (1 << 30) / l->page_tokens || (long long)l->n_pages * l->page_tokens > INT_MAX) return EVO_ERR_SHAPE;
+  if (!l->pages || !aligned(l->pages, 16) || (l->n_seq > 0 && (!l->table || !l->lens))) return EVO_ERR_ARG;
+  *m = evo_memory{};
+  m->dtype = l->dtype;
+  m->format = l->dtype == EVO_DTYPE_F32 ? EVO_CACHE_F32 : EVO_CACHE_BF16;
+  m->n_head = l->n_head;
+  m->n_kv_head = 1;
+  m->head_dim = l->rank;
+  m->page_tokens = l->page_tokens;
+  m->n_pages = l->n_pages;
+  m->max_pages = l->max_pages;
+  m->n_seq = l->n_seq;
+  m->k_pages = m->v_pages = l->pages;
+  m->table = l->table;
+  m->lens = l->lens;
+  m->starts = l->starts;
+  m->status = l->status;
+  return EVO_OK;
+}
+size_t latent_pool(const evo_latent* l) {
+  return (size_t)l->n_pages * l->page_tokens * (l->rank + l->rope) * item_of(l->dtype);
+}
+
+// `rows` x `heads` blocks of `width` values: ld elements between rows, hd between a row's blocks
+struct Blocks {
+  const void* p;
+  int64_t ld, hd;
+  int64_t rows, heads, width;
+  int item;
+  // (with one row or head its stride is not used)
+  int64_t span() const { return ((rows - 1) * ld + (heads - 1) * hd + width) * item; }
+};
+bool blocks_ok(const Blocks& b) {
+  if (!b.p || !aligned(b.p, 16)) return false;
+  if (b.heads > 1 && (b.hd < b.width || b.hd > INT_MAX || b.hd * b.item % 16)) return false;
+  return b.ld >= (b.heads - 1) * (b.heads > 1 ? b.hd : 0) + b.width && b.ld <= INT_MAX && b.ld * b.item % 16 == 0;
+}
+// do two sets of blocks share a byte?  With one stride of rows, blocks of one set may lie between the other's;
+// with two, sets whose extents meet count as sharing
+bool blocks_overlap(const Blocks& a, const Blocks& b) {
+  if (!overlap(a.p, a.span(), b.p, b.span())) return false;
+  if (a.ld != b.ld) return true;
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)), step = a.ld * a.item;
+  const auto meet = [&](int64_t at) {                       // a block of b's first row at this distance from one of a's
+    const int64_t wa = a.width * a.item, wb = b.width * b.item;
+    int64_t r = at / step - 2;
+    for (int i = 0; i < 5; ++i, ++r) {                      // r rows of a further on (b's row 0 .. rows - 1 less a's)
+      const int64_t x = at - r * step;
+      if (-r > b.rows - 1 || r > a.rows - 1) continue;
+      if (x < wa && -x < wb) return true;
+    }
+    return false;
+  };
+  for (int64_t i = 0; i < a.heads; ++i) {
+    if (a.hd == b.hd && i > 0) break;                       // differences of heads, below
+    for (int64_t j = a.hd == b.hd ? 1 - a.heads : 0; j < b.heads; ++j)
+      if (meet(d + j * b.hd * b.item - i * a.hd * a.item)) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -245,6 +316,105 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
   a.causal = causal;
   a.window = window;
   EVO_CUDA(launch_attend(a, p, scratch, reinterpret_cast<cudaStream_t>(stream)));
+  return EVO_OK;
+}
+
+evo_status evo_latent_append(const evo_latent* lat, const void* c, int64_t ldc, const void* k, int64_t ldk, const void* q,
+                             int64_t ldq, int64_t hdq, int32_t rows, const float* c_gain, float eps, const float* rotation,
+                             int32_t n_pos, const int32_t* pos0, void* q_out, int64_t ldo, int64_t hdo, void* stream) {
+  evo_memory m;
+  evo_status s = latent_ok(lat, &m);
+  if (s == EVO_OK) s = chunks_ok(&m, rows);
+  if (s != EVO_OK) return s;
+  if ((c == nullptr) != (k == nullptr) || (q == nullptr) != (q_out == nullptr) || !(eps >= 0.f)) return EVO_ERR_ARG;
+  if (rotation ? n_pos <= 0 : pos0 != nullptr) return EVO_ERR_ARG;
+  if (rows == 0 || (!q && !c)) return EVO_OK;
+  const int item = item_of(lat->dtype);
+  const Blocks in{q, ldq, hdq, rows, lat->n_head, LATENT_ROPE, item}, out{q_out, ldo, hdo, rows, lat->n_head, LATENT_ROPE, item};
+  const Blocks cb{c, ldc, 0, rows, 1, lat->rank, item}, kb{k, ldk, 0, rows, 1, LATENT_ROPE, item};
+  if (q && (!blocks_ok(in) || !blocks_ok(out))) return EVO_ERR_ARG;
+  if (c && (!blocks_ok(cb) || !blocks_ok(kb))) return EVO_ERR_ARG;
+  // queries may be overwritten in place (a thread reads what it writes), nothing else that the call reads
+  if (q && (q_out != q || ldo != ldq || (hdo != hdq && lat->n_head > 1)) && blocks_overlap(out, in)) return EVO_ERR_ARG;
+  if (q && c && (blocks_overlap(out, cb) || blocks_overlap(out, kb))) return EVO_ERR_ARG;
+  const size_t pool = latent_pool(lat);
+  if (q && overlap(lat->pages, pool, q_out, out.span())) return EVO_ERR_ARG;
+  if (c && (overlap(lat->pages, pool, c, cb.span()) || overlap(lat->pages, pool, k, kb.span()) ||
+            (q && overlap(lat->pages, pool, q, in.span()))))
+    return EVO_ERR_ARG;
+  if (!aligned(rotation, 16) || !aligned(c_gain, 16)) return EVO_ERR_ARG;
+  const LatentAppendArgs a{m, c, k, q, q_out, ldc, ldk, ldq, hdq, ldo, hdo, rows, c_gain, eps, rotation, n_pos, pos0};
+  EVO_CUDA(launch_latent_append(a, reinterpret_cast<cudaStream_t>(stream)));
+  return EVO_OK;
+}
+
+size_t evo_latent_scratch_bytes(const evo_latent* lat, int32_t rows, int32_t max_new, int32_t max_len) {
+  evo_memory m;
+  if (latent_ok(lat, &m) != EVO_OK || attend_sizes(&m, rows, max_new, max_len) != EVO_OK) return 0;
+  return plan_latent(m, rows, max_new, max_len, 0, 0).scratch;
+}
+
+evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
+                             int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,
+                             void* scratch, void* stream) {
+  evo_memory m;
+  evo_status s = latent_ok(lat, &m);
+  if (s != EVO_OK) return s;
+  if (rows == 0) return EVO_OK;
+  s = attend_sizes(&m, rows, max_new, max_len);
+  if (s != EVO_OK) return s;
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if (!std::isfinite(scale_log2) || (causal != 0 && causal != 1) || window < 0) return EVO_ERR_ARG;
+  const int item = item_of(lat->dtype);
+  const Blocks in{q, ldq, 0, rows, 1, (int64_t)lat->n_head * (lat->rank + lat->rope), item};
+  const Blocks to{out, ldo, 0, rows, 1, (int64_t)lat->n_head * lat->rank, item};
+  if (!blocks_ok(in) || !blocks_ok(to) || blocks_overlap(in, to)) return EVO_ERR_ARG;
+  if (overlap(lat->pages, latent_pool(lat), out, to.span())) return EVO_ERR_ARG;
+  // pieces by what a window leaves to see, where they fit the workspace that a call without one has
+  LatentPlan p = plan_latent(m, rows, max_new, max_len, 0, 0);
+  if (window) {
+    const LatentPlan w = plan_latent(m, rows, max_new, max_len, causal, window);
+    if (w.scratch <= p.scratch) p = w;
+  }
+  if (p.scratch && (!scratch || !aligned(scratch, 16))) return EVO_ERR_ARG;
+  AttendArgs a{};
+  a.m = m;
+  a.q = q;
+  a.out = out;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.rows = rows;
+  a.max_new = max_new;
+  a.max_len = max_len;
+  a.group = m.n_head;
+  a.scale_log2 = scale_log2;
+  a.causal = causal;
+  a.window = window;
+  EVO_CUDA(launch_latent_attend(a, p, scratch, reinterpret_cast<cudaStream_t>(stream)));
+  return EVO_OK;
+}
+
+evo_status evo_latent_expand(const evo_latent* lat, const void* w_k, const void* w_v, const int32_t* first,
+                             int32_t max_new, int32_t max_len, const evo_memory* mem, void* stream) {
+  evo_memory m;
+  evo_status s = latent_ok(lat, &m);
+  if (s == EVO_OK) s = memory_ok(mem);
+  if (s != EVO_OK) return s;
+  if (mem->dtype != lat->dtype || mem->format == EVO_CACHE_E4M3) return EVO_ERR_UNSUPPORTED;
+  if (mem->head_dim != LATENT_KEY + LATENT_ROPE || mem->n_kv_head != lat->n_head || mem->n_seq != lat->n_seq) return EVO_ERR_SHAPE;
+  if (max_new < 0 || max_len < 0 || max_new > max_len || max_len > m.max_pages * m.page_tokens) return EVO_ERR_ARG;
+  if (!w_k || !w_v || !aligned(w_k, 16) || !aligned(w_v, 16)) return EVO_ERR_ARG;
+  // blocks of the launch
+  if (m.n_seq > 0 && ((long long)max_new / 64 + 1) * m.n_head > INT_MAX / m.n_seq) return EVO_ERR_SHAPE;
+  const size_t item = item_of(lat->dtype), heads = lat->n_head;
+  const size_t to = (size_t)mem->n_pages * mem->page_tokens * heads * mem->head_dim * item, pool = latent_pool(lat);
+  const size_t wk = heads * LATENT_KEY * lat->rank * item, wv = heads * LATENT_VALUE * lat->rank * item;
+  if (overlap(mem->k_pages, to, mem->v_pages, to)) return EVO_ERR_ARG;
+  for (const void* p : {mem->k_pages, mem->v_pages})
+    if (overlap(p, to, lat->pages, pool) || overlap(p, to, w_k, wk) || overlap(p, to, w_v, wv)) return EVO_ERR_ARG;
+  if (m.n_seq == 0 || max_new == 0) return EVO_OK;
+  const LatentExpandArgs a{m, *mem, w_k, w_v, first, max_new, max_len};
+  EVO_CUDA(launch_latent_expand(a, reinterpret_cast<cudaStream_t>(stream)));
   return EVO_OK;
 }
 

@@ -1,5 +1,5 @@
-// Internal declarations of the 8-bit unit caches and the paged memory:
-// arguments of their kernels and the host functions that launch them.
+// Internal declarations of the 8-bit unit caches, the paged memory and the latent
+// memory: arguments of their kernels and the host functions that launch them.
 #pragma once
 
 #include <atomic>
@@ -62,6 +62,39 @@ cudaError_t launch_attend_rows(const AttendArgs& a, int tile_rows, cudaStream_t 
 cudaError_t launch_attend_f32_rows(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_attend_f32.cu
 cudaError_t launch_attend_tiles(const AttendArgs& a, cudaStream_t st);                // evo_attend_tiles.cu
 cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st);
+
+// joins the pieces of a call's rows from a.part and a.ml (evo_attend.cu); head_dim 64 to 512
+cudaError_t launch_join(const AttendArgs& a, cudaStream_t st);
+
+// The latent memory.  Its calls run on the paged memory's arguments: one key/value head whose keys are a
+// page's rows of rank + LATENT_ROPE values and whose values are the first head_dim = rank of them.
+constexpr int LATENT_ROPE = 64, LATENT_KEY = 64, LATENT_VALUE = 128;
+struct LatentAppendArgs {
+  evo_memory m;                   // k_pages: the latent pages
+  const void *c, *k, *q;          // c and k null: only queries; q null: only tokens
+  void* q_out;
+  long long ldc, ldk, ldq, hdq, ldo, hdo;   // elements between rows, and between a row's heads
+  int rows;
+  const float* c_gain;            // [rank] or null: no norm
+  float eps;
+  const float* rotation;          // [n_pos][LATENT_ROPE] or null
+  int n_pos;
+  const int* pos0;
+};
+cudaError_t launch_latent_append(const LatentAppendArgs& a, cudaStream_t st);   // evo_latent.cu
+struct LatentPlan {
+  int tile_rows, tiles, splits, cluster;
+  size_t scratch;
+};
+LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window);   // evo_latent.cu
+cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
+struct LatentExpandArgs {
+  evo_memory m, to;               // the latent memory, and the one that its tokens are written to
+  const void *w_k, *w_v;          // [n_head][LATENT_KEY][rank], [n_head][LATENT_VALUE][rank]
+  const int* first;               // [n_seq] or null: the first token of each that is written
+  int max_new, max_len;
+};
+cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st);   // evo_latent_expand.cu
 
 // tensor map of a pool of pages: its rows (a token of a head each) in boxes of
 // box_rows rows x 128 bytes (64 where a row has no more), swizzled by the box's width
