@@ -162,37 +162,19 @@ constexpr int AT_ONCE = 4;                         // tokens that a warp takes a
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
 constexpr float MASKED = -1.f;                     // in place of the weight of a token that a row does not see
 
-template <typename T, int RANK, int KW, int RW>
+template <int RANK, int KW, int RW>
 struct Cfg {
   static constexpr int THREADS = 32 * (KW * RW + 1), ROWS = R * RW;
-  static constexpr int ROW = (RANK + LATENT_ROPE) * (int)sizeof(T), BYTES = STAGE * ROW;
+  static constexpr int ROW = (RANK + LATENT_ROPE) * 4, BYTES = STAGE * ROW;
   static constexpr int LD = RANK + 4;
   static constexpr int JOIN = KW * ROWS * LD * 4;
   static constexpr int STAGES = 108 * 1024 / BYTES > 8 ? 8 : 108 * 1024 / BYTES;
   static constexpr int SMEM = STAGES * BYTES > JOIN ? STAGES * BYTES : JOIN;
 };
 
-// 4 values at p (16-byte or 8-byte aligned) as pairs
-__device__ __forceinline__ void lds4(uint32_t p, float2& a, float2& b, float) {
-  const float4 v = lds_f4(p);
-  a = make_float2(v.x, v.y), b = make_float2(v.z, v.w);
-}
-__device__ __forceinline__ void lds4(uint32_t p, float2& a, float2& b, __nv_bfloat16) {
-  const uint2 v = lds64(p);
-  a = make_float2(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u));
-  b = make_float2(__uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-}
-__device__ __forceinline__ float2 lds2(uint32_t p, float) { return lds_f2(p); }
-__device__ __forceinline__ float2 lds2(uint32_t p, __nv_bfloat16) {
-  const uint32_t v = lds32(p);
-  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-}
-__device__ __forceinline__ float one(float x) { return x; }
-__device__ __forceinline__ float one(__nv_bfloat16 x) { return __bfloat162float(x); }
-
-template <typename T, int RANK, int KW, int RW>
-__global__ void __launch_bounds__(Cfg<T, RANK, KW, RW>::THREADS) latent_rows_kernel(const __grid_constant__ AttendArgs a) {
-  using C = Cfg<T, RANK, KW, RW>;
+template <int RANK, int KW, int RW>
+__global__ void __launch_bounds__(Cfg<RANK, KW, RW>::THREADS) latent_rows_kernel(const __grid_constant__ AttendArgs a) {
+  using C = Cfg<RANK, KW, RW>;
   constexpr int N4 = RANK / 128, PAIRS = 2 * N4 + 1;         // float2 of a lane: its share of the latent, then of the key part
   extern __shared__ __align__(128) uint8_t ring[];
   __shared__ __align__(8) uint64_t full[8], empty[8];
@@ -245,11 +227,11 @@ __global__ void __launch_bounds__(Cfg<T, RANK, KW, RW>::THREADS) latent_rows_ker
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int Q = r0 + R * rw + r;
-      const T* src = static_cast<const T*>(a.q) + (long long)(t.first + Q / a.group) * a.ldq + (long long)(Q % a.group) * (RANK + LATENT_ROPE);
+      const float* src = static_cast<const float*>(a.q) + (long long)(t.first + Q / a.group) * a.ldq + (long long)(Q % a.group) * (RANK + LATENT_ROPE);
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) {
         const int d = i < 2 * N4 ? 128 * (i / 2) + 4 * lane + 2 * (i % 2) : RANK + 2 * lane;
-        q[r][i] = Q < rows ? make_float2(one(src[d]), one(src[d + 1])) : make_float2(0.f, 0.f);
+        q[r][i] = Q < rows ? *reinterpret_cast<const float2*>(src + d) : make_float2(0.f, 0.f);
       }
     }
     const float f = a.scale_log2;
@@ -267,9 +249,11 @@ __global__ void __launch_bounds__(Cfg<T, RANK, KW, RW>::THREADS) latent_rows_ker
         for (int k = 0; k < AT_ONCE; ++k) {
           const uint32_t p = base + (g * AT_ONCE + k) * C::ROW;
 #pragma unroll
-          for (int j = 0; j < N4; ++j)
-            lds4(p + (128 * j + 4 * lane) * (int)sizeof(T), x[k][2 * j], x[k][2 * j + 1], T());
-          x[k][2 * N4] = lds2(p + (RANK + 2 * lane) * (int)sizeof(T), T());
+          for (int j = 0; j < N4; ++j) {
+            const float4 y = lds_f4(p + (128 * j + 4 * lane) * 4);
+            x[k][2 * j] = make_float2(y.x, y.y), x[k][2 * j + 1] = make_float2(y.z, y.w);
+          }
+          x[k][2 * N4] = lds_f2(p + (RANK + 2 * lane) * 4);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
             float2 s = mul_pair(x[k][0], q[r][0]);
@@ -360,33 +344,32 @@ __global__ void __launch_bounds__(Cfg<T, RANK, KW, RW>::THREADS) latent_rows_ker
       x = make_float4(fmaf(y.x, fw, x.x), fmaf(y.y, fw, x.y), fmaf(y.z, fw, x.z), fmaf(y.w, fw, x.w));
     }
     if (a.cluster == 1) {
-      put_result<T, RANK>(a, t, r0 + r, d, x, m, l);
+      put_result<float, RANK>(a, t, r0 + r, d, x, m, l);
     } else {                                                 // in place of the first warp's
       *reinterpret_cast<float4*>(sums + r * C::LD + d) = x;
       if (d == 0) block_ml[r] = make_float2(m, l);
     }
   }
-  if (a.cluster > 1) join_cluster<T, RANK, C::ROWS, C::THREADS>(a, t, sums, C::LD, block_ml, r0, rows);
+  if (a.cluster > 1) join_cluster<float, RANK, C::ROWS, C::THREADS>(a, t, sums, C::LD, block_ml, r0, rows);
 }
 
-template <typename T, int RANK, int KW, int RW>
+template <int RANK, int KW, int RW>
 cudaError_t launch_rows_as(const AttendArgs& a, cudaStream_t st) {
-  using C = Cfg<T, RANK, KW, RW>;
+  using C = Cfg<RANK, KW, RW>;
   static std::atomic<uint64_t> done{0};
-  return launch_pieces(latent_rows_kernel<T, RANK, KW, RW>, a, C::THREADS, C::SMEM, done, st);
+  return launch_pieces(latent_rows_kernel<RANK, KW, RW>, a, C::THREADS, C::SMEM, done, st);
 }
-template <typename T, int RANK>
+template <int RANK>
 cudaError_t launch_rows_of(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  return tile_rows == 4    ? launch_rows_as<T, RANK, 4, 1>(a, st)
-         : tile_rows == 8  ? launch_rows_as<T, RANK, 4, 2>(a, st)
-         : tile_rows == 16 ? launch_rows_as<T, RANK, 2, 4>(a, st)
-                           : launch_rows_as<T, RANK, 1, 8>(a, st);
+  return tile_rows == 4    ? launch_rows_as<RANK, 4, 1>(a, st)
+         : tile_rows == 8  ? launch_rows_as<RANK, 4, 2>(a, st)
+         : tile_rows == 16 ? launch_rows_as<RANK, 2, 4>(a, st)
+                           : launch_rows_as<RANK, 1, 8>(a, st);
 }
-template <typename T>
-cudaError_t launch_rows_type(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  return a.m.head_dim == 128   ? launch_rows_of<T, 128>(a, tile_rows, st)
-         : a.m.head_dim == 256 ? launch_rows_of<T, 256>(a, tile_rows, st)
-                               : launch_rows_of<T, 512>(a, tile_rows, st);
+cudaError_t launch_rows(const AttendArgs& a, int tile_rows, cudaStream_t st) {
+  return a.m.head_dim == 128   ? launch_rows_of<128>(a, tile_rows, st)
+         : a.m.head_dim == 256 ? launch_rows_of<256>(a, tile_rows, st)
+                               : launch_rows_of<512>(a, tile_rows, st);
 }
 
 }  // namespace
@@ -398,13 +381,26 @@ cudaError_t launch_latent_append(const LatentAppendArgs& a, cudaStream_t st) {
 LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window) {
   LatentPlan p;
   const long long all = (long long)max_new * m.n_head;
-  p.tile_rows = all <= 4 ? 4 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  const bool f32 = m.dtype == EVO_DTYPE_F32;
+  if (f32)
+    p.tile_rows = all <= 4 ? 4 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  else
+    p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : all <= 64 ? 64 : 128;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const int moves = causal ? std::min(max_new, p.tile_rows / m.n_head + 1) : 0;
   const int keys = window ? (int)std::min<long long>(max_len, (long long)window + moves) : max_len;
   const long long blocks = (long long)m.n_seq * p.tiles;
   p.cluster = 1;
-  p.splits = (int)std::max(1ll, std::min({(long long)keys / 64, 304 / blocks, 64ll}));
+  if (f32) {
+    p.splits = (int)std::max(1ll, std::min({(long long)keys / 64, 304 / blocks, 64ll}));
+  } else {
+    p.splits = 1;
+    double least = 1e300;
+    for (int s = 1; s <= std::min(128, std::max(1, keys / 128)); ++s) {
+      const double each = (double)((blocks * s + 151) / 152), cost = each * ((keys + s - 1) / s + (s == 1 ? 400 : 800));
+      if (cost < least) least = cost, p.splits = s;
+    }
+  }
   p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
   return p;
 }
@@ -416,8 +412,7 @@ cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scrat
   const int parts = p.splits / p.cluster;
   a.part = static_cast<float*>(scratch);
   a.ml = reinterpret_cast<float2*>(a.part + (size_t)parts * a.rows * a.m.n_head * a.m.head_dim);
-  const cudaError_t e = a.m.dtype == EVO_DTYPE_F32 ? launch_rows_type<float>(a, p.tile_rows, st)
-                                                   : launch_rows_type<__nv_bfloat16>(a, p.tile_rows, st);
+  const cudaError_t e = a.m.dtype == EVO_DTYPE_F32 ? launch_rows(a, p.tile_rows, st) : launch_latent_tiles(a, p.tile_rows, st);
   return e != cudaSuccess || parts == 1 ? e : launch_join(a, st);
 }
 

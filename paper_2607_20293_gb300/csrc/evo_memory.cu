@@ -11,7 +11,9 @@ using namespace evo;
 
 namespace evo {
 
-bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows) {
+namespace {
+// tensor map of `rows` rows of `row` values, in boxes of box_rows x 128 bytes (64 where a row has no more)
+bool rows_map(CUtensorMap* map, int32_t format, const void* rows_at, cuuint64_t row, cuuint64_t rows, int box_rows) {
   using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -24,19 +26,26 @@ bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_
     return reinterpret_cast<Encode>(p);
   }();
   if (!encode) return false;
-  const bool codes = m.format == EVO_CACHE_E4M3;
-  const cuuint32_t item = codes ? 1 : m.format == EVO_CACHE_BF16 ? 2 : 4;
-  const cuuint64_t row = (cuuint64_t)m.head_dim * item;
-  const cuuint64_t dims[2] = {(cuuint64_t)m.head_dim, (cuuint64_t)m.n_pages * m.n_kv_head * m.page_tokens};
-  const cuuint64_t strides[1] = {row};
-  const cuuint32_t width = (cuuint32_t)(row < 128 ? row : 128);
+  const bool codes = format == EVO_CACHE_E4M3;
+  const cuuint32_t item = codes ? 1 : format == EVO_CACHE_BF16 ? 2 : 4;
+  const cuuint64_t dims[2] = {row, rows};
+  const cuuint64_t strides[1] = {row * item};
+  const cuuint32_t width = (cuuint32_t)(row * item < 128 ? row * item : 128);
   const cuuint32_t box[2] = {width / item, (cuuint32_t)box_rows}, steps[2] = {1, 1};
   const CUtensorMapDataType type = codes       ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                    : item == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
-  return encode(map, type, 2, const_cast<void*>(pages), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return encode(map, type, 2, const_cast<void*>(rows_at), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 width == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+}  // namespace
+
+bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows) {
+  return rows_map(map, m.format, pages, m.head_dim, (cuuint64_t)m.n_pages * m.n_kv_head * m.page_tokens, box_rows);
+}
+bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows) {
+  return rows_map(map, m.format, m.k_pages, m.head_dim + LATENT_ROPE, (cuuint64_t)m.n_pages * m.page_tokens, box_rows);
 }
 
 }  // namespace evo

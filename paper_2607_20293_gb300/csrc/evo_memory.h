@@ -88,6 +88,7 @@ struct LatentPlan {
 };
 LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window);   // evo_latent.cu
 cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
+cudaError_t launch_latent_tiles(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_latent_tiles.cu
 struct LatentExpandArgs {
   evo_memory m, to;               // the latent memory, and the one that its tokens are written to
   const void *w_k, *w_v;          // [n_head][LATENT_KEY][rank], [n_head][LATENT_VALUE][rank]
@@ -99,6 +100,8 @@ cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st);   
 // tensor map of a pool of pages: its rows (a token of a head each) in boxes of
 // box_rows rows x 128 bytes (64 where a row has no more), swizzled by the box's width
 bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows);
+// the same of a latent memory's pages, a row a token
+bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows);
 
 // lets a kernel have this much dynamic shared memory; `done`: a bit for each device where it has it
 template <typename K>
