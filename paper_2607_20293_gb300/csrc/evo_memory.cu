@@ -48,6 +48,10 @@ bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows) {
   return rows_map(map, m.format, m.k_pages, m.head_dim + LATENT_ROPE, (cuuint64_t)m.n_pages * m.page_tokens, box_rows);
 }
 
+bool map_of(CUtensorMap* map, const void* p, long long rows, int width, int box_rows) {
+  return rows_map(map, EVO_CACHE_BF16, p, width, rows, box_rows);
+}
+
 }  // namespace evo
 
 namespace {
@@ -414,7 +418,7 @@ evo_status evo_latent_expand(const evo_latent* lat, const void* w_k, const void*
   if (max_new < 0 || max_len < 0 || max_new > max_len || max_len > m.max_pages * m.page_tokens) return EVO_ERR_ARG;
   if (!w_k || !w_v || !aligned(w_k, 16) || !aligned(w_v, 16)) return EVO_ERR_ARG;
   // blocks of the launch
-  if (m.n_seq > 0 && ((long long)max_new / 64 + 1) * m.n_head > INT_MAX / m.n_seq) return EVO_ERR_SHAPE;
+  if (m.n_seq > 0 && ((long long)max_new / 64 + 2) * m.n_head > INT_MAX / 2 / m.n_seq) return EVO_ERR_SHAPE;
   const size_t item = item_of(lat->dtype), heads = lat->n_head;
   const size_t to = (size_t)mem->n_pages * mem->page_tokens * heads * mem->head_dim * item, pool = latent_pool(lat);
   const size_t wk = heads * LATENT_KEY * lat->rank * item, wv = heads * LATENT_VALUE * lat->rank * item;
