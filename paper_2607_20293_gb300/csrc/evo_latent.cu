@@ -379,28 +379,19 @@ cudaError_t launch_latent_append(const LatentAppendArgs& a, cudaStream_t st) {
 }
 
 LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window) {
-  LatentPlan p;
+  LatentPlan p{};
   const long long all = (long long)max_new * m.n_head;
-  const bool f32 = m.dtype == EVO_DTYPE_F32;
-  if (f32)
-    p.tile_rows = all <= 4 ? 4 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
-  else
-    p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : all <= 64 ? 64 : 128;
-  p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
-  const int moves = causal ? std::min(max_new, p.tile_rows / m.n_head + 1) : 0;
+  const int moves = causal ? std::min(max_new, 128 / m.n_head + 1) : 0;
   const int keys = window ? (int)std::min<long long>(max_len, (long long)window + moves) : max_len;
-  const long long blocks = (long long)m.n_seq * p.tiles;
   p.cluster = 1;
-  if (f32) {
-    p.splits = (int)std::max(1ll, std::min({(long long)keys / 64, 304 / blocks, 64ll}));
-  } else {
-    p.splits = 1;
-    double least = 1e300;
-    for (int s = 1; s <= std::min(128, std::max(1, keys / 128)); ++s) {
-      const double each = (double)((blocks * s + 151) / 152), cost = each * ((keys + s - 1) / s + (s == 1 ? 400 : 800));
-      if (cost < least) least = cost, p.splits = s;
-    }
+  if (m.dtype != EVO_DTYPE_F32) {
+    plan_latent_tiles(p, m, all, keys);
+    return p;
   }
+  p.tile_rows = all <= 4 ? 4 : all <= 8 ? 8 : all <= 16 ? 16 : 32;
+  p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
+  const long long blocks = (long long)m.n_seq * p.tiles;
+  p.splits = (int)std::max(1ll, std::min({(long long)keys / 64, 304 / blocks, 64ll}));
   p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
   return p;
 }
@@ -409,10 +400,11 @@ cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scrat
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.cluster = p.cluster;
+  if (a.m.dtype != EVO_DTYPE_F32) return launch_latent_tiles(a, p, scratch, st);
   const int parts = p.splits / p.cluster;
   a.part = static_cast<float*>(scratch);
   a.ml = reinterpret_cast<float2*>(a.part + (size_t)parts * a.rows * a.m.n_head * a.m.head_dim);
-  const cudaError_t e = a.m.dtype == EVO_DTYPE_F32 ? launch_rows(a, p.tile_rows, st) : launch_latent_tiles(a, p.tile_rows, st);
+  const cudaError_t e = launch_rows(a, p.tile_rows, st);
   return e != cudaSuccess || parts == 1 ? e : launch_join(a, st);
 }
 

@@ -167,29 +167,38 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
     __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(value ? a.to.v_pages : a.to.k_pages);
     const bool whole = reinterpret_cast<uintptr_t>(out) % 32 == 0;
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    int i = 0;
-    for (int pair = first; pair < pairs; pair += groups) {
-      int2 range;
-      const int t0 = tile_of(pair, range), n = pair % a.m.n_seq;
-      if (t0 >= range.y) continue;
-      const int t = t0 + tid % TM;
-      __nv_bfloat16* dst = nullptr;
+    // a thread's token: its row in either pool.  Looked up a tile ahead
+    struct Token { long long from, to; };
+    const auto next_of = [&](int pair, Token& token) {
+      for (; pair < pairs; pair += groups) {
+        int2 range;
+        const int t0 = tile_of(pair, range), n = pair % a.m.n_seq, t = t0 + tid % TM;
+        if (t0 >= range.y) continue;
+        token = Token{-1, -1};
+        if (t >= range.x && t < range.y) {
+          const int p = page_or_none(a.m, a.m.status, n, t / a.m.page_tokens), q = page_or_none(a.to, a.m.status, n, t / a.to.page_tokens);
+          if (p >= 0 && q >= 0)
+            token = Token{(long long)p * a.m.page_tokens + t % a.m.page_tokens, ((long long)q * H + h) * a.to.page_tokens + t % a.to.page_tokens};
+        }
+        break;
+      }
+      return pair;
+    };
+    Token token;
+    int pair = next_of(first, token);
+    for (int i = 0; pair < pairs; ++i) {
+      __nv_bfloat16* const dst = token.to >= 0 ? out + token.to * 128 : nullptr;
       uint32_t turned[4][8];                                 // the rotated half of a key
-      if (t >= range.x && t < range.y) {
-        const int p = page_or_none(a.m, a.m.status, n, t / a.m.page_tokens), q = page_or_none(a.to, a.m.status, n, t / a.to.page_tokens);
-        if (p >= 0 && q >= 0) {
-          dst = out + (((long long)q * H + h) * a.to.page_tokens + t % a.to.page_tokens) * 128;
-          const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.m.k_pages) +
-                                                            ((long long)p * a.m.page_tokens + t % a.m.page_tokens) * (RANK + LATENT_ROPE) + RANK);
-          if (!value)
+      if (dst && !value) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.m.k_pages) + token.from * (RANK + LATENT_ROPE) + RANK);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const uint4 u = src[j];
-              uint32_t* w = &turned[j / 2][4 * (j % 2)];
-              w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-            }
+        for (int j = 0; j < 8; ++j) {
+          const uint4 u = src[j];
+          uint32_t* w = &turned[j / 2][4 * (j % 2)];
+          w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
         }
       }
+      pair = next_of(pair + groups, token);
       wait_for(&sh.acc_full[i & 1], (i / 2) & 1, &sh.dead);
       __syncwarp();
       tc::tc_fence_after();
@@ -216,7 +225,6 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
       if (dst && !value)
 #pragma unroll
         for (int j = 0; j < 4; ++j) put16(dst + LATENT_KEY + 16 * j, turned[j], whole);
-      ++i;
     }
   }
   tc::tc_fence_before();

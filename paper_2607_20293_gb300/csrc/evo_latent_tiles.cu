@@ -7,21 +7,28 @@
 // cost an eighth of what 128 do, and the output of 512 dimensions takes 4 N columns of tensor memory:
 //   S^T = X Q^T   tokens x rows, X = (c | k) as it lies in its page
 //   O^T += C^T P^T  dimensions x rows, C^T by the transposing form of the same tiles
-// A block takes N = 16 to 128 rows (tokens of the chunk times heads) and one piece of the memory, 128
-// tokens at a time.  Warp 9 brings them by tiled bulk copies into a ring of slots of 128 dimensions
-// (and one of key parts); warp 8 issues the products; warps 0-7 are the softmax: a thread has a token
-// (its lane of tensor memory) and half of the rows, and writes the weights P^T, which are summed
-// over the lanes only at the end.
+// An item is N = 16 to 128 rows (tokens of a chunk times heads) of one sequence, and is taken 128
+// tokens of memory at a time. The last warp brings these by tiled bulk copies into a ring of slots of 128
+// dimensions (and one of key parts); the one before it issues the products; the others are the
+// softmax: a thread has a token (its lane of tensor memory) and 8 to 32 of the rows, and writes the weights
+// P^T, which are summed over the lanes only at the end of an item.
+//
+// Blocks stay resident, one a SM.  Where items do not fill them evenly, the tiles of all items are counted
+// (every block does so, by itself) and each block takes an equal run of them, so that sequences of different
+// lengths end at the same time; the runs' first and last items are shared with other blocks, leave
+// their sums in the workspace and are joined by a second kernel.  The copies run ahead into the next item
+// while the softmax still writes this one's output.
 //
 // The running maximum is lazy: a row's reference is raised only when a score passes it by 2^8, so that
 // the common tile has one vote in place of reductions over the lanes.  The reference m is subtracted from the
 // product, and the difference multiplied by the factor: equal scores have equal weights at any size.
 // Weights are rounded to bf16 for their product, 2^-8 of each at most.
 //
-// Masks are looked at only in tiles that some row does not see whole.  There, tokens outside the piece
-// are set to zero in shared memory; so is one with a value that is not finite (0 * NaN would reach
+// Masks are looked at only in tiles that some row does not see whole.  There, tokens outside the item's
+// range are set to zero in shared memory; so is one with a value that is not finite (0 * NaN would reach
 // rows that do not see it), whose score is then NaN for the rows that see it.
 #include <algorithm>
+#include <climits>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -33,9 +40,10 @@ namespace evo {
 namespace {
 
 constexpr int BK = 128;                            // tokens of a tile
-constexpr int SOFTMAX = 256, THREADS = SOFTMAX + 64;
+constexpr int SMS = 152, MOST_ITEMS = 2048;        // items that a block counts
 constexpr int SLOT = BK * 256, HALF = BK * 128;    // bytes of 128 and of 64 dimensions of a tile
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
+constexpr float NONE = -3.402823466e38f;           // the reference of a row that has seen nothing
 
 template <int RANK, int N>
 struct Cfg {
@@ -50,21 +58,46 @@ struct Cfg {
   static constexpr int SMEM = 1024 + Q + P + SLOTS * SLOT + PARTS * HALF;
   static constexpr int S_COL = PER * N, COLS = S_COL + 2 * N;     // tensor memory: O, then two buffers of S
   static constexpr int ALLOC = COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
-  static constexpr int HC = N / 2;                 // rows of a softmax thread
-  static constexpr int LD = RANK + 4;              // floats of a row where sums are handed over
+  static constexpr int WARPS = N >= 64 ? 16 : 8, SOFTMAX = 32 * WARPS, THREADS = SOFTMAX + 64;
+  static constexpr int WEIGHTS16 = 16 * (N >= 64 ? 128 : 2 * N);  // bytes of 16 tokens' weights
+  static constexpr int HC = N / (WARPS / 4);       // rows of a softmax thread
   static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(BK >> 4) << 24);
   static constexpr uint32_t IDESC_O = IDESC | (1u << 15) | (1u << 16);   // contiguous indexes: dimensions, rows
-  static_assert(SLOTS >= PER && SLOTS <= 6 && N * LD * 4 <= SMEM - 1024 && COLS <= 512, "");
+  static_assert(SLOTS >= PER && SLOTS <= 6 && COLS <= 512, "");
+};
+
+// An item's rows and the tokens that they see
+struct Item {
+  Tile t;
+  int rows, r0, last;             // rows of the sequence; the item's are r0 .. last
+  Range first_row, last_row, all;
+  int tile0, tiles;               // tiles of 128 tokens that some row sees
+  // (an item without any is written as zeros, and counts as a tile)
+  __device__ __forceinline__ int cost() const { return r0 >= rows ? 0 : max(1, tiles); }
+};
+// what the softmax's warps have to know of one item, or of what this block has of it
+struct Segment {
+  Item x;
+  int more, n, key0, slot, whole; // more: there is one.  n tiles from token key0 on; slot: of its sums, unless it is whole here
+  bool alike;                     // every row sees the same tokens
 };
 
 template <int N>
 struct Shared {
-  uint64_t full[6], empty[6], part_full[6], part_empty[6], s_full[2], p_full, o_full;
-  __align__(16) float2 ref[N];                     // what is subtracted from a row's scores, and the score that raises it
+  uint64_t full[6], empty[6], part_full[6], part_empty[6], s_full[2], p_full, o_full, q_full;
+  __align__(16) float ref[N];                      // what is subtracted from a row's scores
   int top[N];                                      // a new maximum (ordered as integers), then the factor of what was summed
   uint32_t bad[4];
   uint32_t tmem;
-  int dead;
+  int dead, item, skip;                            // the first item's number, and the tiles of it that others take
+  long long tiles, warp_tiles[18];                 // tiles that the block takes; sums of the warps' items
+  Segment seg[2];
+  Item begin;                                      // the block's first item
+};
+
+struct Run {
+  int items, split;                                // split: blocks take equal runs of tiles; else whole items, every gridDim-th
+  int4* meta;                                      // of each block, where an item goes on from it to others: its piece's slot, the last block, the item
 };
 
 // ---------------------------------------------------------------- PTX wrappers
@@ -105,13 +138,15 @@ __device__ __forceinline__ void tmem_store8(uint32_t taddr, const float* v) {
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
 }
-__device__ __forceinline__ void bar_softmax() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+template <int THREADS>
+__device__ __forceinline__ void bar_softmax() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+template <int THREADS>
 __device__ __forceinline__ bool bar_softmax_or(bool x) {
   uint32_t r;
   asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+      "{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}\n"
       : "=r"(r)
-      : "r"((uint32_t)x)
+      : "r"((uint32_t)x), "n"(THREADS)
       : "memory");
   return r != 0;
 }
@@ -119,6 +154,13 @@ __device__ __forceinline__ bool bar_softmax_or(bool x) {
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* dead) {
   const uint32_t b = tc::su32(bar);
   return tc::mbar_test(b, parity) || wait_live(b, parity, tc::su32(dead));
+}
+
+// the same behind a first test that failed, for the issuing warp
+__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) { wait_live(bar, parity, dead); }
+__device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 // operands whose contiguous index is not the contraction's: 64 dimensions by 8 tokens a swizzled
@@ -147,11 +189,71 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float unordered(int b) { return __int_as_float(b >= 0 ? b : b ^ 0x7fffffff); }
 
+template <int N>
+__device__ __forceinline__ Item item_of(const AttendArgs& a, int i) {
+  Item x;
+  x.t = {};
+  x.t.n = i / a.tiles;
+  const SeqRows s = seq_rows(a.m, x.t.n, a.rows, a.max_new);
+  x.t.first = s.first;
+  x.t.count = s.count;
+  x.t.len = seq_len(a.m, x.t.n, a.max_len);
+  x.rows = s.count * a.group;
+  x.r0 = i % a.tiles * N;
+  x.last = min(x.r0 + N, x.rows) - 1;
+  x.first_row = seen_by(a, x.t, x.r0 / a.group);
+  x.last_row = seen_by(a, x.t, max(x.last, 0) / a.group);
+  x.all = {x.first_row.lo, x.last_row.hi};
+  x.tile0 = x.all.lo / BK;
+  x.tiles = x.r0 >= x.rows || x.all.hi <= x.all.lo ? 0 : (x.all.hi + BK - 1) / BK - x.tile0;
+  return x;
+}
+
+// The block's items one after the other, the same for every role
+template <int N>
+struct Walk {
+  const AttendArgs& a;
+  const Run& run;
+  const Item& begin;
+  int item, skip;
+  long long left;
+  bool fresh = true;
+  // this segment: tiles from .. from + n - 1 of item x
+  Item x;
+  int index, from, n, segments = 0, filled = 0;   // filled: segments with tiles so far
+  int after;                                       // tiles of the item that later blocks have
+
+  template <typename S>
+  __device__ __forceinline__ Walk(const AttendArgs& a, const Run& run, const S& sh)
+      : a(a), run(run), begin(sh.begin), item(sh.item), skip(sh.skip), left(sh.tiles) {}
+  __device__ __forceinline__ bool next() {
+    for (; item < run.items && left > 0; item += run.split ? 1 : gridDim.x, skip = 0) {
+      x = fresh ? begin : item_of<N>(a, item);
+      fresh = false;
+      const int cost = x.cost();
+      if (cost == 0) continue;
+      index = item;
+      from = skip;
+      const int take = (int)min((long long)(cost - skip), left);
+      n = x.tiles == 0 ? 0 : take;
+      after = cost - from - take;
+      left -= take;
+      item += run.split ? 1 : gridDim.x;
+      skip = 0;
+      ++segments;
+      filled += n > 0;
+      return true;
+    }
+    return false;
+  }
+  __device__ __forceinline__ int key0() const { return (x.tile0 + from) * BK; }
+};
+
 template <int RANK, int N>
-__global__ void __launch_bounds__(THREADS, 1) latent_tiles_kernel(const __grid_constant__ AttendArgs a,
-                                                                  const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
+    latent_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ Run run) {
   using C = Cfg<RANK, N>;
-  constexpr int PER = C::PER, HC = C::HC, SLOTS = C::SLOTS, PARTS = C::PARTS;
+  constexpr int PER = C::PER, HC = C::HC, SLOTS = C::SLOTS, PARTS = C::PARTS, SOFTMAX = C::SOFTMAX, THREADS = C::THREADS;
   extern __shared__ uint8_t raw[];
   __shared__ Shared<N> sh;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -160,292 +262,412 @@ __global__ void __launch_bounds__(THREADS, 1) latent_tiles_kernel(const __grid_c
   uint8_t* const ring = weights + C::P;
   uint8_t* const parts = ring + SLOTS * SLOT;
   if (tid == 0) fetch_map(&map);
-  const Tile t = tile_of_block(a);
-  const int rows = t.count * a.group, r0 = t.tile * N;
-  if (r0 >= rows) return;
-  const int last = min(r0 + N, rows) - 1;
-  const Range first_row = seen_by(a, t, r0 / a.group), last_row = seen_by(a, t, last / a.group);
-  const Range all = piece_of(a, t, {first_row.lo, last_row.hi}, BK);
-  const int whole_lo = max(last_row.lo, all.lo), whole_hi = min(first_row.hi, all.hi);
-  const bool alike = first_row.lo == last_row.lo && first_row.hi == last_row.hi;   // every row sees the same tokens
-  const int key0 = all.lo / BK * BK, n = max(0, (all.hi - key0 + BK - 1) / BK);
-
   __syncwarp();                                    // a whole warp's instruction, behind one lane's prefetch
   if (warp == 0) tc::tmem_alloc(&sh.tmem, C::ALLOC);
   if (tid == 32) {
     for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], 1);
     for (int i = 0; i < PARTS; ++i) tc::mbar_init1(&sh.part_full[i], 1), tc::mbar_init1(&sh.part_empty[i], 1);
     tc::mbar_init1(&sh.s_full[0], 1), tc::mbar_init1(&sh.s_full[1], 1);
-    tc::mbar_init1(&sh.p_full, SOFTMAX / 32);      // a warp each
+    tc::mbar_init1(&sh.p_full, C::WARPS);          // a warp each
+    tc::mbar_init1(&sh.q_full, C::WARPS);
     tc::mbar_init1(&sh.o_full, 1);
     sh.dead = 0;
+    sh.item = run.split ? run.items : blockIdx.x;
+    sh.skip = 0;
+    sh.tiles = run.split ? 0 : 1ll << 62;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (tid >= 64 && tid < 64 + N) sh.ref[tid - 64] = make_float2(0.f, -INFINITY);
-  // queries to shared memory; the softmax works with a positive factor
-  const float f = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f);
-  {
-    constexpr int PIECES = (RANK + LATENT_ROPE) / 8;
-    const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
-    for (int i = tid; i < N * PIECES; i += THREADS) {
-      const int r = i / PIECES, j = i % PIECES, R = r0 + r;
-      uint4 u = make_uint4(0, 0, 0, 0);
-      if (R < rows && a.scale_log2 != 0.f)
-        u = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (long long)(t.first + R / a.group) * a.ldq +
-                                           (long long)(R % a.group) * (RANK + LATENT_ROPE))[j];
-      u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
-      *reinterpret_cast<uint4*>(mem + (j / 8) * (N * 128) + r * 128 + ((j % 8 ^ (r & 7)) << 4)) = u;
+  if (tid < N) sh.ref[tid] = NONE;
+  long long total = 0;
+  if (!run.split) {
+    if (tid == 0) sh.begin = item_of<N>(a, blockIdx.x);
+  } else {
+    // every thread counts the tiles of a few items; the block's run is the blockIdx-th of gridDim equal ones
+    const int each = (run.items + THREADS - 1) / THREADS, i0 = tid * each, i1 = min(i0 + each, run.items);
+    Item x;
+    if (i0 < i1) x = item_of<N>(a, i0);
+    const long long one = i0 < i1 ? x.cost() : 0;
+    long long mine = one;
+    for (int i = i0 + 1; i < i1; ++i) mine += item_of<N>(a, i).cost();
+    long long before = mine;                       // inclusive sum over the lanes
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const long long y = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += y;
     }
-    tc::fence_async_smem();
+    if (lane == 31) sh.warp_tiles[warp] = before;
+    __syncthreads();
+    before -= mine;
+    for (int w = 0; w < THREADS / 32; ++w) {
+      if (w < warp) before += sh.warp_tiles[w];
+      total += sh.warp_tiles[w];
+    }
+    const long long lo = blockIdx.x * total / gridDim.x, hi = (blockIdx.x + 1) * total / gridDim.x;
+    if (lo >= before && lo < before + mine) {      // the run begins in one of this thread's items
+      int i = i0;
+      for (long long cost = one; lo >= before + cost; cost = x.cost()) before += cost, x = item_of<N>(a, ++i);
+      sh.begin = x;
+      sh.item = i;
+      sh.skip = (int)(lo - before);
+      sh.tiles = hi - lo;
+    }
   }
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
+  Walk<N> walk(a, run, sh);
+  int g = 0;                                       // tiles so far
 
-  if (warp == 9) {
+  if (warp == C::WARPS + 1) {
     // ------------------------------------------------------------ copies
     const int page_tokens = a.m.page_tokens, box = min(page_tokens, BK), shift = 31 - __clz(page_tokens);
-    for (int i = 0; i < n; ++i) {
-      const int key = key0 + i * BK + lane * box;
-      const bool on = lane * box < BK && key + box > all.lo && key < all.hi;
-      const int page = on ? seq_page(a.m, t.n, key >> shift) : 0;
-      const int at = page * page_tokens + (key & (page_tokens - 1)), copies = __popc(__ballot_sync(0xffffffffu, on));
-      const auto bring = [&](uint8_t* to, uint64_t* full, uint64_t* empty, int use, int column, int halves) {
-        if (!__all_sync(0xffffffffu, use == 0 || wait_for(empty, (use - 1) & 1, &sh.dead))) return;
-        if (lane == 0) tc::mbar_expect_tx(full, copies * box * 128 * halves);
-        __syncwarp();
-        if (on)
-          for (int x = 0; x < halves; ++x)
-            tile_load(tc::su32(to) + x * HALF + lane * box * 128, &map, column + 64 * x, at, tc::su32(full));
-        __syncwarp();
+    while (walk.next()) {
+      const Range all = walk.x.all;
+      const auto page_of = [&](int i) {              // -1: no token of the item is there
+        const int key = walk.key0() + i * BK + lane * box;
+        return i < walk.n && lane * box < BK && key + box > all.lo && key < all.hi ? seq_page(a.m, walk.x.t.n, key >> shift) : -1;
       };
-      for (int j = 0; j < PER; ++j) {
-        const int index = i * PER + j, slot = index % SLOTS;
-        bring(ring + slot * SLOT, &sh.full[slot], &sh.empty[slot], index / SLOTS, 128 * j, 2);
+      int ahead = page_of(0);
+      for (int i = 0; i < walk.n; ++i, ++g) {
+        const int page = ahead;
+        ahead = page_of(i + 1);
+        const bool on = page >= 0;
+        const int at = page * page_tokens + ((walk.key0() + i * BK + lane * box) & (page_tokens - 1));
+        const int copies = __popc(__ballot_sync(0xffffffffu, on));
+        const auto bring = [&](uint8_t* to, uint64_t* full, uint64_t* empty, int use, int column, int halves) {
+          if (!__all_sync(0xffffffffu, use == 0 || wait_for(empty, (use - 1) & 1, &sh.dead))) return;
+          if (lane == 0) tc::mbar_expect_tx(full, copies * box * 128 * halves);
+          __syncwarp();
+          if (on)
+            for (int x = 0; x < halves; ++x)
+              tile_load(tc::su32(to) + x * HALF + lane * box * 128, &map, column + 64 * x, at, tc::su32(full));
+          __syncwarp();
+        };
+        for (int j = 0; j < PER; ++j) {
+          const int index = g * PER + j, slot = index % SLOTS;
+          bring(ring + slot * SLOT, &sh.full[slot], &sh.empty[slot], index / SLOTS, 128 * j, 2);
+        }
+        bring(parts + g % PARTS * HALF, &sh.part_full[g % PARTS], &sh.part_empty[g % PARTS], g / PARTS, RANK, 1);
       }
-      bring(parts + i % PARTS * HALF, &sh.part_full[i % PARTS], &sh.part_empty[i % PARTS], i / PARTS, RANK, 1);
     }
-  } else if (warp == 8) {
+  } else if (warp == C::WARPS) {
     // ------------------------------------------------------------ products
-    const uint32_t q = tc::su32(mem), w = tc::su32(weights);
+    // Uniform over the warp and known to the compiler to be (a shuffle's result is), one elected lane issuing:
+    // descriptors then stay in uniform registers, and an instruction costs an addition or two.
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t rows_desc = tc::sw128_desc(0), turned_desc = latent_desc(0), w_desc = weight_desc<N>(0);
+    const uint32_t hi = (uint32_t)(rows_desc >> 32), whi = (uint32_t)(w_desc >> 32), at = tc::su32(ring) >> 4;
+    const uint32_t xr = (uint32_t)rows_desc + at, xt = (uint32_t)turned_desc + at, q = (uint32_t)rows_desc + (tc::su32(mem) >> 4),
+                   kp = (uint32_t)rows_desc + (tc::su32(parts) >> 4), w = (uint32_t)w_desc + (tc::su32(weights) >> 4);
+    const uint32_t full = tc::su32(sh.full), empty = tc::su32(sh.empty), part_full = tc::su32(sh.part_full),
+                   part_empty = tc::su32(sh.part_empty), dead_word = tc::su32(&sh.dead);
+    uint32_t s_slot = 0, s_phase = 0, s_part = 0, s_part_phase = 0, o_slot = 0;
+    const auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (!tc::mbar_test(bar, parity)) wait_slow(bar, parity, dead_word);
+    };
     const auto scores = [&](int i) {
-      const uint32_t d = tmem + C::S_COL + (i & 1) * N;
+      const uint32_t d = tm + C::S_COL + (i & 1) * N;
+#pragma unroll
       for (int j = 0; j < PER; ++j) {
-        const int index = i * PER + j, slot = index % SLOTS;
-        wait_for(&sh.full[slot], (index / SLOTS) & 1, &sh.dead);
+        wait(full + 8 * s_slot, s_phase);
         tc::tc_fence_after();
-        const uint32_t x = tc::su32(ring + slot * SLOT);
+        const uint32_t x = xr + s_slot * (SLOT >> 4);
         if (tc::elect_one())
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            tc::mma_f16(d, tc::sw128_desc(x + (k / 4) * HALF + (k % 4) * 32),
-                        tc::sw128_desc(q + (2 * j + k / 4) * (N * 128) + (k % 4) * 32), C::IDESC, j | k);
-        __syncwarp();
+            tc::mma_f16(d, desc64(x + (k / 4) * (HALF >> 4) + (k % 4) * 2, hi), desc64(q + (2 * j + k / 4) * (N * 128 >> 4) + (k % 4) * 2, hi),
+                        C::IDESC, j | k);
+        if (++s_slot == SLOTS) s_slot = 0, s_phase ^= 1;
       }
-      wait_for(&sh.part_full[i % PARTS], (i / PARTS) & 1, &sh.dead);
+      wait(part_full + 8 * s_part, s_part_phase);
       tc::tc_fence_after();
-      const uint32_t x = tc::su32(parts + i % PARTS * HALF);
+      const uint32_t x = kp + s_part * (HALF >> 4);
       if (tc::elect_one()) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          tc::mma_f16(d, tc::sw128_desc(x + k * 32), tc::sw128_desc(q + 2 * PER * (N * 128) + k * 32), C::IDESC, 1);
-        tc::mma_commit(&sh.s_full[i & 1]);
-        tc::mma_commit(&sh.part_empty[i % PARTS]);
+          tc::mma_f16(d, desc64(x + k * 2, hi), desc64(q + 2 * PER * (N * 128 >> 4) + k * 2, hi), C::IDESC, 1);
+        commit(tc::su32(&sh.s_full[i & 1]));
+        commit(part_empty + 8 * s_part);
       }
-      __syncwarp();
+      if (++s_part == PARTS) s_part = 0, s_part_phase ^= 1;
     };
-    const auto output = [&](int i) {
-      if (tc::elect_one())
-        for (int j = 0; j < PER; ++j) {
-          const int slot = (i * PER + j) % SLOTS;
-          const uint32_t x = tc::su32(ring + slot * SLOT);
+    const auto output = [&](uint32_t accumulate) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const uint32_t x = xt + o_slot * (SLOT >> 4);
+        if (tc::elect_one()) {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            tc::mma_f16(tmem + j * N, latent_desc(x + k * 2048), weight_desc<N>(w + k * (N >= 64 ? 2048 : N * 32)), C::IDESC_O, i | k);
-          tc::mma_commit(&sh.empty[slot]);
-          if (j == PER - 1) tc::mma_commit(&sh.o_full);
+            tc::mma_f16(tm + j * N, desc64(x + k * (2048 >> 4), hi), desc64(w + k * (C::WEIGHTS16 >> 4), whi), C::IDESC_O, k ? 1 : accumulate);
+          commit(empty + 8 * o_slot);
+          if (j == PER - 1) commit(tc::su32(&sh.o_full));
         }
-      __syncwarp();
+        if (++o_slot == SLOTS) o_slot = 0;
+      }
     };
-    if (n > 0) scores(0);
-    for (int i = 0; i < n; ++i) {
-      if (C::AHEAD && i + 1 < n) scores(i + 1);
-      wait_for(&sh.p_full, i & 1, &sh.dead);
+    bool dead = false;
+    while (!dead && walk.next()) {
+      if (walk.n == 0) continue;
+      const int n = __shfl_sync(0xffffffffu, walk.n, 0);
+      wait(tc::su32(&sh.q_full), (walk.filled - 1) & 1);
       tc::tc_fence_after();
-      if (__any_sync(0xffffffffu, tc::block_dead(tc::su32(&sh.dead)))) break;
-      output(i);
-      if (!C::AHEAD && i + 1 < n) scores(i + 1);
+      scores(g);
+      for (int i = 0; i < n; ++i, ++g) {
+        if (C::AHEAD && i + 1 < n) scores(g + 1);
+        wait(tc::su32(&sh.p_full), g & 1);
+        tc::tc_fence_after();
+        dead = __any_sync(0xffffffffu, tc::block_dead(dead_word));
+        if (dead) break;
+        output(i);
+        if (!C::AHEAD && i + 1 < n) scores(g + 1);
+      }
     }
   } else {
     // ------------------------------------------------------------ softmax: a token and rows c0 .. c0 + HC - 1 a thread
     // A wait that is in vain ends no turn: the barriers of the softmax want all of its warps.
-    const int k = tid % BK, c0 = warp / 4 * HC;
+    const int k = tid % BK, part = warp / 4, c0 = part * HC;
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    float sum[HC];
-#pragma unroll
-    for (int j = 0; j < HC; ++j) sum[j] = 0.f;
-    for (int i = 0; i < n; ++i) {
-      wait_for(&sh.s_full[i & 1], (i >> 1) & 1, &sh.dead);
+    // the softmax works with a positive factor: the scale's sign goes to the queries
+    const float f = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f), far = fminf(LAZY / f, 1e38f);
+    const auto load_queries = [&](const Item& x) {
+      constexpr int PIECES = (RANK + LATENT_ROPE) / 8;
+      const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll 4
+      for (int i = tid; i < N * PIECES; i += SOFTMAX) {
+        const int r = i / PIECES, j = i % PIECES, R = x.r0 + r;
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (R < x.rows && a.scale_log2 != 0.f)
+          u = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (long long)(x.t.first + R / a.group) * a.ldq +
+                                             (long long)(R % a.group) * (RANK + LATENT_ROPE))[j];
+        u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
+        *reinterpret_cast<uint4*>(mem + (j / 8) * (N * 128) + r * 128 + ((j % 8 ^ (r & 7)) << 4)) = u;
+      }
+      tc::fence_async_smem();
       __syncwarp();
-      tc::tc_fence_after();
-      float v[HC];
-      tmem_load(tmem + C::S_COL + (i & 1) * N + c0 + lanes, v);
-      const int key = key0 + i * BK + k;
-      if (key0 + i * BK < whole_lo || key0 + (i + 1) * BK > whole_hi) {
-        const bool out = key < all.lo || key >= all.hi;
-        // this thread's half of the token's latent
-        bool bad = false;
-        for (int j = 0; j < PER; ++j) {
-          const int index = i * PER + j, slot = index % SLOTS;
-          wait_for(&sh.full[slot], (index / SLOTS) & 1, &sh.dead);
-          uint4* p = reinterpret_cast<uint4*>(ring + slot * SLOT + warp / 4 * HALF + k * 128);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (out) {
-              p[e] = make_uint4(0, 0, 0, 0);
-            } else if (!alike) {
-              const uint4 u = p[e];
-              const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-              for (int y = 0; y < 4; ++y) bad |= (x[y] & 0x7f80u) == 0x7f80u || (x[y] & 0x7f800000u) == 0x7f800000u;
+      if (lane == 0) tc::mbar_arrive1(&sh.q_full);
+    };
+    // the first warp looks the next item up for all of them
+    bool shares = false;
+    const auto advance = [&](Segment& q) {
+      bar_softmax<SOFTMAX>();                        // nobody is at the item before any more
+      if (warp == 0) {
+        const bool more = walk.next();
+        if (lane == 0) {
+          q.more = more;
+          if (more) {
+            const Item& x = walk.x;
+            q.x = x;
+            q.n = walk.n;
+            q.key0 = walk.key0();
+            q.slot = 2 * blockIdx.x + (walk.segments > 1 ? 1 : 0);   // of an item that other blocks share: the run's first or last
+            q.whole = walk.from == 0 && walk.after == 0;
+            q.alike = x.first_row.lo == x.last_row.lo && x.first_row.hi == x.last_row.hi;
+            if (walk.from == 0 && walk.after > 0) {  // it goes on to the block that has the last of its tiles
+              const long long end = (blockIdx.x + 1) * total / gridDim.x + walk.after;
+              run.meta[blockIdx.x] = make_int4(q.slot, (int)((end * gridDim.x - 1) / total), walk.index, (int)total);
+              shares = true;
             }
           }
         }
-        if (alike) {
+      }
+      bar_softmax<SOFTMAX>();
+      if (q.more && q.n > 0) load_queries(q.x);
+    };
+    float sum[HC];
+    advance(sh.seg[0]);
+    for (int s = 0; sh.seg[s].more; s ^= 1) {
+      const Segment& q = sh.seg[s];
+      const Item& x = q.x;
+      const Tile& t = x.t;
+      const int n = q.n, key0 = q.key0;
 #pragma unroll
-          for (int j = 0; j < HC; ++j) v[j] = out ? -INFINITY : v[j];
-        } else {
-          if (tid < 4) sh.bad[tid] = 0;
-          bar_softmax();
-          if (bad) atomicOr(&sh.bad[k / 32], 1u << (k % 32));
-          bar_softmax();
-          bad = sh.bad[k / 32] >> (k % 32) & 1;
-          if (bad)
-            for (int j = 0; j < PER; ++j) {
-              uint4* p = reinterpret_cast<uint4*>(ring + (i * PER + j) % SLOTS * SLOT + warp / 4 * HALF + k * 128);
-              for (int e = 0; e < 8; ++e) p[e] = make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < HC; ++j) sum[j] = 0.f;
+      for (int i = 0; i < n; ++i, ++g) {
+        wait_for(&sh.s_full[g & 1], (g >> 1) & 1, &sh.dead);
+        __syncwarp();
+        tc::tc_fence_after();
+        float v[HC];
+        const uint32_t scores = tmem + C::S_COL + (g & 1) * N + c0 + lanes;
+        tmem_load(scores, v);
+        const int key = key0 + i * BK + k;
+        if (key0 + i * BK < x.last_row.lo || key0 + (i + 1) * BK > x.first_row.hi) {
+          const bool alike = q.alike, out = key < x.all.lo || key >= x.all.hi;
+          // this thread's share of the token's latent: 64 of each 128 dimensions of every second slot, or of all
+          constexpr int SHARES = C::WARPS / 8;
+          bool bad = false;
+          for (int j = part / 2 % SHARES; j < PER; j += SHARES) {
+            const int index = g * PER + j, slot = index % SLOTS;
+            wait_for(&sh.full[slot], (index / SLOTS) & 1, &sh.dead);
+            uint4* p = reinterpret_cast<uint4*>(ring + slot * SLOT + part % 2 * HALF + k * 128);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (out) {
+                p[e] = make_uint4(0, 0, 0, 0);
+              } else if (!alike) {
+                const uint4 u = p[e];
+                const uint32_t y[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int z = 0; z < 4; ++z) bad |= (y[z] & 0x7f80u) == 0x7f80u || (y[z] & 0x7f800000u) == 0x7f800000u;
+              }
             }
-#pragma unroll
-          for (int j = 0; j < HC; ++j) {
-            const Range see = seen_by(a, t, min(r0 + c0 + j, last) / a.group);
-            if (bad) v[j] = __builtin_nanf("");
-            if (out || key < see.lo || key >= see.hi) v[j] = -INFINITY;
           }
-        }
-        tc::fence_async_smem();
-      }
-      bool raise = false;
+          if (alike) {
 #pragma unroll
-      for (int j = 0; j < HC; j += 2) {
-        const float4 r = *reinterpret_cast<const float4*>(&sh.ref[c0 + j]);
-        raise |= v[j] > r.y || v[j + 1] > r.w;
-      }
-      bool waited = i == 0;
-      if (bar_softmax_or(raise)) {
-        if (tid < N) sh.top[tid] = ordered(-INFINITY);
-        bar_softmax();
+            for (int j = 0; j < HC; ++j) v[j] = out ? -INFINITY : v[j];
+          } else {
+            if (tid < 4) sh.bad[tid] = 0;
+            bar_softmax<SOFTMAX>();
+            if (bad) atomicOr(&sh.bad[k / 32], 1u << (k % 32));
+            bar_softmax<SOFTMAX>();
+            bad = sh.bad[k / 32] >> (k % 32) & 1;
+            if (bad)
+              for (int j = part / 2 % SHARES; j < PER; j += SHARES) {
+                uint4* p = reinterpret_cast<uint4*>(ring + (g * PER + j) % SLOTS * SLOT + part % 2 * HALF + k * 128);
+                for (int e = 0; e < 8; ++e) p[e] = make_uint4(0, 0, 0, 0);
+              }
 #pragma unroll
-        for (int j0 = 0; j0 < HC; j0 += 32) {
-          int mine = 0;
-#pragma unroll
-          for (int j = 0; j < (HC < 32 ? HC : 32); ++j) {
-            const int m = __reduce_max_sync(0xffffffffu, ordered(v[j0 + j]));
-            if (lane == j) mine = m;
+            for (int j = 0; j < HC; ++j) {
+              const Range see = seen_by(a, t, min(x.r0 + c0 + j, x.last) / a.group);
+              if (bad) v[j] = __builtin_nanf("");
+              if (out || key < see.lo || key >= see.hi) v[j] = -INFINITY;
+            }
           }
-          if (lane < HC) atomicMax(&sh.top[c0 + j0 + lane], mine);
-        }
-        bar_softmax();
-        if (tid < N) {
-          const float2 r = sh.ref[tid];
-          const float old = r.y == -INFINITY ? -INFINITY : r.x, m = fmaxf(old, unordered(sh.top[tid]));
-          sh.top[tid] = __float_as_int(old == -INFINITY ? 1.f : ex2_approx((old - m) * f));
-          if (m != -INFINITY) sh.ref[tid] = make_float2(m, m + LAZY / f);
-        }
-        bar_softmax();
-#pragma unroll
-        for (int j = 0; j < HC; ++j) sum[j] *= __int_as_float(sh.top[c0 + j]);
-        if (i > 0) {
-          wait_for(&sh.o_full, (i - 1) & 1, &sh.dead);
-          waited = true;
-          __syncwarp();
-          tc::tc_fence_after();
-#pragma unroll 1
-          for (int j = 0; j < PER * HC; j += 8) {
-            const int col = c0 + j % HC;
-            const uint32_t at = tmem + j / HC * N + col + lanes;
-            float o[8];
-            tmem_load(at, o);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] *= __int_as_float(sh.top[col + e]);
-            tmem_store8(at, o);
-          }
+          tc::fence_async_smem();
+          for (int j = 0; j < HC; j += 8) tmem_store8(scores + j, v + j);   // where a new reference looks for them
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         }
-      }
-      uint32_t p[HC / 2];
+        // scores less their references; a row that has seen nothing is far below any score
+        const auto less = [&] {
+          float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < HC; j += 2) {
-        const float4 r = *reinterpret_cast<const float4*>(&sh.ref[c0 + j]);
-        const float2 x = mul2(add2(make_float2(v[j], v[j + 1]), make_float2(-r.x, -r.z)), make_float2(f, f));
-        const float2 e = make_float2(ex2_approx(x.x), ex2_approx(x.y)), s = add2(make_float2(sum[j], sum[j + 1]), e);
-        sum[j] = s.x, sum[j + 1] = s.y;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[j / 2]) : "f"(e.y), "f"(e.x));
-      }
-      if (!waited) wait_for(&sh.o_full, (i - 1) & 1, &sh.dead);   // the product before has read its weights
+          for (int j = 0; j < HC; j += 4) {
+            const float4 r = *reinterpret_cast<const float4*>(&sh.ref[c0 + j]);
+            const float2 d = add2(make_float2(v[j], v[j + 1]), make_float2(-r.x, -r.y));
+            const float2 e = add2(make_float2(v[j + 2], v[j + 3]), make_float2(-r.z, -r.w));
+            v[j] = d.x, v[j + 1] = d.y, v[j + 2] = e.x, v[j + 3] = e.y;
+            top = fmaxf(fmaxf(top, fmaxf(d.x, d.y)), fmaxf(e.x, e.y));
+          }
+          return top;
+        };
+        const bool raise = less() > far;
+        bool waited = i == 0;
+        if (bar_softmax_or<SOFTMAX>(raise)) {
+          if (tid < N) sh.top[tid] = ordered(-INFINITY);
+          tmem_load(scores, v);
+          bar_softmax<SOFTMAX>();
+          int mine = 0;
 #pragma unroll
-      for (int j = 0; j < HC / 8; ++j)
-        *reinterpret_cast<uint4*>(weights + weight_at<N>(k, c0 / 8 + j)) = make_uint4(p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]);
-      tc::fence_async_smem();
-      tc::tc_fence_before();
+          for (int j = 0; j < HC; ++j) {
+            const int m = __reduce_max_sync(0xffffffffu, ordered(v[j]));
+            if (lane == j) mine = m;
+          }
+          if (lane < HC) atomicMax(&sh.top[c0 + lane], mine);
+          bar_softmax<SOFTMAX>();
+          if (tid < N) {
+            const float old = sh.ref[tid], m = fmaxf(old, unordered(sh.top[tid]));
+            sh.top[tid] = __float_as_int(old == NONE ? 1.f : ex2_approx((old - m) * f));
+            sh.ref[tid] = m;
+          }
+          bar_softmax<SOFTMAX>();
+#pragma unroll
+          for (int j = 0; j < HC; ++j) sum[j] *= __int_as_float(sh.top[c0 + j]);
+          if (i > 0) {
+            wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
+            waited = true;
+            __syncwarp();
+            tc::tc_fence_after();
+#pragma unroll 1
+            for (int j = 0; j < PER * HC; j += 8) {
+              const int col = c0 + j % HC;
+              const uint32_t at = tmem + j / HC * N + col + lanes;
+              float o[8];
+              tmem_load(at, o);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] *= __int_as_float(sh.top[col + e]);
+              tmem_store8(at, o);
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          }
+          less();
+        }
+        uint32_t p[HC / 2];
+#pragma unroll
+        for (int j = 0; j < HC / 2; ++j) {
+          const float2 y = mul2(make_float2(v[2 * j], v[2 * j + 1]), make_float2(f, f));
+          const float2 e = make_float2(ex2_approx(y.x), ex2_approx(y.y)), s = add2(make_float2(sum[2 * j], sum[2 * j + 1]), e);
+          sum[2 * j] = s.x, sum[2 * j + 1] = s.y;
+          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[j]) : "f"(e.y), "f"(e.x));
+        }
+        if (!waited) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);   // the product before has read its weights
+#pragma unroll
+        for (int j = 0; j < HC / 8; ++j)
+          *reinterpret_cast<uint4*>(weights + weight_at<N>(k, c0 / 8 + j)) = make_uint4(p[4 * j], p[4 * j + 1], p[4 * j + 2], p[4 * j + 3]);
+        tc::fence_async_smem();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive1(&sh.p_full);
+      }
+      // the next item's queries take the place of these, whose scores are all there
+      advance(sh.seg[s ^ 1]);
+      if (n > 0) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive1(&sh.p_full);
-    }
-    if (n > 0) wait_for(&sh.o_full, (n - 1) & 1, &sh.dead);
-    __syncwarp();
-    tc::tc_fence_after();
-    // sums of the weights over the lanes: each step halves the rows that a lane holds
-    constexpr int B = HC < 32 ? HC : 32;
-    float* const lsum = reinterpret_cast<float*>(weights);   // [4][N]
-#pragma unroll
-    for (int j0 = 0; j0 < HC; j0 += 32) {
+      tc::tc_fence_after();
+      // sums of the weights over the lanes: each step halves the rows that a lane holds
+      float* const lsum = reinterpret_cast<float*>(weights);   // [4][N]
       int m = 16;
 #pragma unroll
-      for (int h = B / 2; h > 0; h >>= 1, m >>= 1) {
+      for (int h = HC / 2; h > 0; h >>= 1, m >>= 1) {
         const bool up = lane & m;
 #pragma unroll
-        for (int j = 0; j < B / 2; ++j)
+        for (int j = 0; j < HC / 2; ++j)
           if (j < h) {
-            const float keep = up ? sum[j0 + j + h] : sum[j0 + j], give = up ? sum[j0 + j] : sum[j0 + j + h];
-            sum[j0 + j] = keep + __shfl_xor_sync(0xffffffffu, give, m);
+            const float keep = up ? sum[j + h] : sum[j], give = up ? sum[j] : sum[j + h];
+            sum[j] = keep + __shfl_xor_sync(0xffffffffu, give, m);
           }
       }
-      for (; m > 0; m >>= 1) sum[j0] += __shfl_xor_sync(0xffffffffu, sum[j0], m);
-      if (lane % (32 / B) == 0) lsum[warp % 4 * N + c0 + j0 + lane / (32 / B)] = sum[j0];
-    }
-  }
-  __syncthreads();                                 // nothing reads the queries, the ring or the weights any more
-  float* const sums = reinterpret_cast<float*>(mem);   // [N][LD]
-  float l = 0.f, m = -INFINITY;
-  if (tid < N && n > 0) {
-    const float* lsum = reinterpret_cast<const float*>(weights);
-    l = (lsum[tid] + lsum[N + tid]) + (lsum[2 * N + tid] + lsum[3 * N + tid]);
-    const float2 r = sh.ref[tid];
-    m = r.y == -INFINITY ? -INFINITY : r.x * f;
-  }
-  __syncthreads();
-  if (tid < N) sh.ref[tid] = make_float2(m, l);
-  if (warp < 8) {
-    const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    const int c0 = warp / 4 * HC;
+      for (; m > 0; m >>= 1) sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], m);
+      if (lane % (32 / HC) == 0) lsum[warp % 4 * N + c0 + lane / (32 / HC)] = sum[0];
+      bar_softmax<SOFTMAX>();
+      if (tid < N) {
+        const float l = n > 0 ? (lsum[tid] + lsum[N + tid]) + (lsum[2 * N + tid] + lsum[3 * N + tid]) : 0.f;
+        if (q.whole)
+          sh.top[tid] = __float_as_int(l == 0.f ? 0.f : 1.f / l);
+        else
+          a.ml[q.slot * N + tid] = make_float2(sh.ref[tid] == NONE ? -INFINITY : sh.ref[tid] * f, l);
+        sh.ref[tid] = NONE;
+      }
+      bar_softmax<SOFTMAX>();
+      {
+        int R = x.r0 + c0, token = R / a.group, head = R - token * a.group;
 #pragma unroll 1
-    for (int j = 0; j < PER * HC; j += 8) {
-      const int col = c0 + j % HC, d = j / HC * 128 + tid % 128;
-      float o[8] = {};
-      if (n > 0) tmem_load(tmem + j / HC * N + col + lanes, o);
+        for (int j = 0; j < HC; j += 8) {
+#pragma unroll 1
+          for (int y = 0; y < PER; ++y) {
+            const int d = y * 128 + k;
+            float o[8] = {};
+            if (n > 0) tmem_load(tmem + y * N + c0 + j + lanes, o);
+            if (q.whole) {
+              int to = token, he = head;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sums[(col + e) * C::LD + d] = o[e];
+              for (int e = 0; e < 8; ++e) {
+                if (R + e <= x.last)
+                  static_cast<__nv_bfloat16*>(a.out)[(long long)(t.first + to) * a.ldo + (long long)he * RANK + d] =
+                      __float2bfloat16_rn(o[e] * __int_as_float(sh.top[c0 + j + e]));
+                if (++he == a.group) he = 0, ++to;
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) a.part[(long long)(q.slot * N + c0 + j + e) * RANK + d] = o[e];
+            }
+          }
+          R += 8;
+          token = R / a.group;
+          head = R - token * a.group;
+        }
+      }
     }
+    if (run.split && tid == 0 && !shares) run.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
   }
   tc::tc_fence_before();
   __syncthreads();
@@ -455,42 +677,134 @@ __global__ void __launch_bounds__(THREADS, 1) latent_tiles_kernel(const __grid_c
     __syncthreads();
   }
   if (warp == 0) tc::tmem_dealloc(tmem, C::ALLOC);
-  if (a.cluster > 1) {
-    join_cluster<__nv_bfloat16, RANK, N, THREADS>(a, t, sums, C::LD, sh.ref, r0, rows);
-  } else {
-    for (int i = tid; i < N * RANK / 4; i += THREADS) {
-      const int r = i / (RANK / 4), d = i % (RANK / 4) * 4;
-      if (r0 + r >= rows) break;
-      const float2 ml = sh.ref[r];
-      put_result<__nv_bfloat16, RANK>(a, t, r0 + r, d, *reinterpret_cast<const float4*>(sums + r * C::LD + d), ml.x, ml.y);
+}
+
+// Joins the pieces of the items that blocks share, from the block that has an item's first tile: it and, of those
+// behind it up to the last, each that has tiles (its first piece).  RANK / 4 lanes a row, the rest of the block's
+// threads on further pieces.
+constexpr int JOIN_THREADS = 256;
+template <int RANK, int N>
+__global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_constant__ AttendArgs a, const int4* meta, int blocks,
+                                                                   int each) {
+  constexpr int LANES = RANK / 4, GROUPS = JOIN_THREADS / LANES;
+  __shared__ float weight[SMS];
+  __shared__ int slots[SMS];
+  __shared__ float4 os[GROUPS][LANES];
+  __shared__ int pieces;
+  const int tid = threadIdx.x, lane = tid % LANES, group = tid / LANES;
+  tc::pdl_wait();
+  const int4 m = meta[blockIdx.x];
+  if (m.x < 0) return;
+  const Item x = item_of<N>(a, m.z);
+  if (tid < 32) {                                  // the pieces' slots, in the order of the blocks
+    int n = 1;
+    if (tid == 0) slots[0] = m.x;
+    for (int b0 = blockIdx.x + 1; b0 <= m.y; b0 += 32) {
+      const long long b = b0 + tid;
+      const bool on = b <= m.y && b * m.w / blocks < (b + 1) * m.w / blocks;
+      const uint32_t all = __ballot_sync(0xffffffffu, on);
+      if (on) slots[n + __popc(all & ((1u << tid) - 1))] = 2 * (int)b;
+      n += __popc(all);
+    }
+    if (tid == 0) pieces = n;
+  }
+  for (int r = blockIdx.y * each; r < min((blockIdx.y + 1) * each, N) && x.r0 + r <= x.last; ++r) {
+    __syncthreads();
+    const int n = pieces;
+    if (tid < 32) {
+      float top = -INFINITY, sum = 0.f;
+      for (int p = tid; p < n; p += 32) top = fmaxf(top, a.ml[slots[p] * N + r].x);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float ref = top == -INFINITY ? 0.f : top;
+      for (int p = tid; p < n; p += 32) {
+        const float2 ml = a.ml[slots[p] * N + r];
+        const float w = ex2_approx(ml.x - ref);
+        weight[p] = w;
+        sum = fmaf(ml.y, w, sum);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (tid == 0) os[0][0].x = sum;
+    }
+    __syncthreads();
+    const float sum = os[0][0].x;
+    float4 o = {};
+#pragma unroll 4
+    for (int p = group; p < n; p += GROUPS) {
+      const float4 y = *reinterpret_cast<const float4*>(a.part + (long long)(slots[p] * N + r) * RANK + 4 * lane);
+      const float w = weight[p];
+      o = make_float4(fmaf(y.x, w, o.x), fmaf(y.y, w, o.y), fmaf(y.z, w, o.z), fmaf(y.w, w, o.w));
+    }
+    __syncthreads();
+    os[group][lane] = o;
+    __syncthreads();
+    if (group == 0) {
+      for (int e = 1; e < GROUPS; ++e) {
+        const float4 y = os[e][lane];
+        o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
+      }
+      const int R = x.r0 + r;
+      store_out(static_cast<__nv_bfloat16*>(a.out) + (long long)(x.t.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane,
+                o, sum == 0.f ? 0.f : 1.f / sum);
     }
   }
 }
 
 template <int RANK, int N>
-cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
+cudaError_t launch_as(const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
   using C = Cfg<RANK, N>;
   CUtensorMap map;
   if (!latent_map(&map, a.m, std::min(a.m.page_tokens, BK))) return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
-  return launch_pieces(latent_tiles_kernel<RANK, N>, a, THREADS, C::SMEM, done, st, map);
+  cudaError_t e = allow_smem(latent_tiles_kernel<RANK, N>, C::SMEM, done);
+  if (e != cudaSuccess) return e;
+  const Run run{a.m.n_seq * a.tiles, p.splits > 1, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * N)};
+  latent_tiles_kernel<RANK, N><<<p.blocks, C::THREADS, C::SMEM, st>>>(a, map, run);
+  e = cudaGetLastError();
+  if (e != cudaSuccess || !run.split) return e;
+  const int each = std::max(1, N / 16);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.blocks, (N + each - 1) / each);
+  cfg.blockDim = JOIN_THREADS;
+  cfg.stream = st;
+  // the join waits for what the pieces wrote (griddepcontrol.wait)
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, p.blocks, each);
 }
 template <int RANK>
-cudaError_t launch_of(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  if (tile_rows == 16) return launch_as<RANK, 16>(a, st);
+cudaError_t launch_of(const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
+  if (p.tile_rows == 16) return launch_as<RANK, 16>(a, p, st);
   if constexpr (RANK < 512) {
-    if (tile_rows == 64) return launch_as<RANK, 64>(a, st);
-    if (tile_rows == 128) return launch_as<RANK, 128>(a, st);
+    if (p.tile_rows == 64) return launch_as<RANK, 64>(a, p, st);
+    if (p.tile_rows == 128) return launch_as<RANK, 128>(a, p, st);
   }
-  return launch_as<RANK, 32>(a, st);
+  return launch_as<RANK, 32>(a, p, st);
 }
 
 }  // namespace
 
-cudaError_t launch_latent_tiles(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  return a.m.head_dim == 128   ? launch_of<128>(a, tile_rows, st)
-         : a.m.head_dim == 256 ? launch_of<256>(a, tile_rows, st)
-                               : launch_of<512>(a, tile_rows, st);
+// Pieces: items go to the blocks whole where that takes little longer, in tiles, than equal runs and their join
+void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int keys) {
+  p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : all <= 64 ? 64 : 128;
+  p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
+  const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + BK - 1) / BK);
+  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 8;
+  const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
+  p.splits = split ? 2 : 1;
+  p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
+  // sums, and maximum and sum of weights, of two pieces a block; where a block's last item goes on
+  p.scratch = split ? (size_t)p.blocks * (2 * p.tile_rows * ((size_t)m.head_dim + 2) * sizeof(float) + sizeof(int4)) : 0;
+}
+
+cudaError_t launch_latent_tiles(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st) {
+  a.part = static_cast<float*>(scratch);
+  a.ml = reinterpret_cast<float2*>(a.part + (size_t)2 * p.blocks * p.tile_rows * a.m.head_dim);
+  return a.m.head_dim == 128 ? launch_of<128>(a, p, st) : a.m.head_dim == 256 ? launch_of<256>(a, p, st) : launch_of<512>(a, p, st);
 }
 
 }  // namespace evo

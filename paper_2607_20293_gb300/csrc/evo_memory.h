@@ -84,11 +84,13 @@ struct LatentAppendArgs {
 cudaError_t launch_latent_append(const LatentAppendArgs& a, cudaStream_t st);   // evo_latent.cu
 struct LatentPlan {
   int tile_rows, tiles, splits, cluster;
+  int blocks;                     // bf16: of the launch; splits 2: they share items
   size_t scratch;
 };
 LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window);   // evo_latent.cu
 cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
-cudaError_t launch_latent_tiles(const AttendArgs& a, int tile_rows, cudaStream_t st);   // evo_latent_tiles.cu
+void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int keys);    // evo_latent_tiles.cu
+cudaError_t launch_latent_tiles(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
 struct LatentExpandArgs {
   evo_memory m, to;               // the latent memory, and the one that its tokens are written to
   const void *w_k, *w_v;          // [n_head][LATENT_KEY][rank], [n_head][LATENT_VALUE][rank]
