@@ -7,7 +7,7 @@
 // cost an eighth of what 128 do, and the output of 512 dimensions takes 4 N columns of tensor memory:
 //   S^T = X Q^T   tokens x rows, X = (c | k) as it lies in its page
 //   O^T += C^T P^T  dimensions x rows, C^T by the transposing form of the same tiles
-// An item is N = 16 to 128 rows (tokens of a chunk times heads) of one sequence, and is taken 128
+// An item is N = 16 to 64 rows (tokens of a chunk times heads) of one sequence, and is taken 128
 // tokens of memory at a time. The last warp brings these by tiled bulk copies into a ring of slots of 128
 // dimensions (and one of key parts); the one before it issues the products; the others are the
 // softmax: a thread has a token (its lane of tensor memory) and 8 to 32 of the rows, and writes the weights
@@ -54,7 +54,6 @@ struct Cfg {
   static constexpr int EVEN = FREE / (SLOT + HALF), MOST = (FREE - HALF) / SLOT;
   static constexpr int SLOTS = PER == 1 ? EVEN : MOST > 6 ? 6 : MOST;
   static constexpr int PARTS = PER == 1 ? EVEN : FREE - SLOTS * SLOT >= 2 * HALF ? 2 : 1;
-  static constexpr bool AHEAD = SLOTS >= 2 * PER && PARTS >= 2;   // the next scores before this output
   static constexpr int SMEM = 1024 + Q + P + SLOTS * SLOT + PARTS * HALF;
   static constexpr int S_COL = PER * N, COLS = S_COL + 2 * N;     // tensor memory: O, then two buffers of S
   static constexpr int ALLOC = COLS <= 64 ? 64 : COLS <= 128 ? 128 : COLS <= 256 ? 256 : 512;
@@ -90,14 +89,15 @@ struct Shared {
   uint32_t bad[4];
   uint32_t tmem;
   int dead, item, skip;                            // the first item's number, and the tiles of it that others take
-  long long tiles, warp_tiles[18];                 // tiles that the block takes; sums of the warps' items
+  int tiles, warp_tiles[32];                       // tiles that the block takes; sums of the warps' items
   Segment seg[2];
   Item begin;                                      // the block's first item
+  long long to[N];                                 // where a row's output begins
 };
 
 struct Run {
   int items, split;                                // split: blocks take equal runs of tiles; else whole items, every gridDim-th
-  int4* meta;                                      // of each block, where an item goes on from it to others: its piece's slot, the last block, the item
+  int4* meta;                                      // of each block from which an item goes on to others: its piece's slot (else -1), the last block, the item
 };
 
 // ---------------------------------------------------------------- PTX wrappers
@@ -156,7 +156,17 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* de
   return tc::mbar_test(b, parity) || wait_live(b, parity, tc::su32(dead));
 }
 
-// the same behind a first test that failed, for the issuing warp
+// does not suspend the warp, for the one that waits for either of two; one lane's answer for all
+__device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return __shfl_sync(0xffffffffu, ok, 0) != 0;
+}
+// a wait behind a first test that failed
 __device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) { wait_live(bar, parity, dead); }
 __device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
 __device__ __forceinline__ void commit(uint32_t bar) {
@@ -209,14 +219,20 @@ __device__ __forceinline__ Item item_of(const AttendArgs& a, int i) {
   return x;
 }
 
+// `blocks` runs of `tiles` tiles, the first ones a tile longer: where run b begins, and which has tile t
+__device__ __forceinline__ int run_from(int tiles, int blocks, int b) { return blocks ? b * (tiles / blocks) + min(b, tiles % blocks) : 0; }
+__device__ __forceinline__ int block_of(int tiles, int blocks, int t) {
+  const int each = tiles / blocks, longer = tiles % blocks * (each + 1);
+  return t < longer ? t / (each + 1) : tiles % blocks + (t - longer) / each;
+}
+
 // The block's items one after the other, the same for every role
 template <int N>
 struct Walk {
   const AttendArgs& a;
   const Run& run;
   const Item& begin;
-  int item, skip;
-  long long left;
+  int item, skip, left;
   bool fresh = true;
   // this segment: tiles from .. from + n - 1 of item x
   Item x;
@@ -234,10 +250,10 @@ struct Walk {
       if (cost == 0) continue;
       index = item;
       from = skip;
-      const int take = (int)min((long long)(cost - skip), left);
+      const int take = min(cost - skip, left);
       n = x.tiles == 0 ? 0 : take;
       after = cost - from - take;
-      left -= take;
+      if (run.split) left -= take;
       item += run.split ? 1 : gridDim.x;
       skip = 0;
       ++segments;
@@ -274,41 +290,44 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     sh.dead = 0;
     sh.item = run.split ? run.items : blockIdx.x;
     sh.skip = 0;
-    sh.tiles = run.split ? 0 : 1ll << 62;
+    sh.tiles = run.split ? 0 : INT_MAX;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid < N) sh.ref[tid] = NONE;
-  long long total = 0;
+  int total = 0;
+  int blocks = gridDim.x;                          // that take tiles
   if (!run.split) {
     if (tid == 0) sh.begin = item_of<N>(a, blockIdx.x);
   } else {
-    // every thread counts the tiles of a few items; the block's run is the blockIdx-th of gridDim equal ones
+    // every thread counts the tiles of a few items; the block's run is the blockIdx-th of `blocks` equal ones
     const int each = (run.items + THREADS - 1) / THREADS, i0 = tid * each, i1 = min(i0 + each, run.items);
     Item x;
     if (i0 < i1) x = item_of<N>(a, i0);
-    const long long one = i0 < i1 ? x.cost() : 0;
-    long long mine = one;
+    const int one = i0 < i1 ? x.cost() : 0;
+    int mine = one;
     for (int i = i0 + 1; i < i1; ++i) mine += item_of<N>(a, i).cost();
-    long long before = mine;                       // inclusive sum over the lanes
+    const auto up_to = [&](int v) {                // sum over the lanes up to this one
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const long long y = __shfl_up_sync(0xffffffffu, before, o);
-      if (lane >= o) before += y;
-    }
+      for (int o = 1; o < 32; o *= 2) {
+        const int y = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += y;
+      }
+      return v;
+    };
+    int before = up_to(mine);
     if (lane == 31) sh.warp_tiles[warp] = before;
     __syncthreads();
-    before -= mine;
-    for (int w = 0; w < THREADS / 32; ++w) {
-      if (w < warp) before += sh.warp_tiles[w];
-      total += sh.warp_tiles[w];
-    }
-    const long long lo = blockIdx.x * total / gridDim.x, hi = (blockIdx.x + 1) * total / gridDim.x;
-    if (lo >= before && lo < before + mine) {      // the run begins in one of this thread's items
+    const int warps = up_to(lane < THREADS / 32 ? sh.warp_tiles[lane] : 0);
+    total = __shfl_sync(0xffffffffu, warps, 31);
+    before += (warp ? __shfl_sync(0xffffffffu, warps, max(warp - 1, 0)) : 0) - mine;
+    blocks = min(blocks, total);
+    const int lo = run_from(total, blocks, blockIdx.x), hi = run_from(total, blocks, blockIdx.x + 1);
+    if (blockIdx.x < blocks && lo >= before && lo < before + mine) {   // the run begins in one of this thread's items
       int i = i0;
-      for (long long cost = one; lo >= before + cost; cost = x.cost()) before += cost, x = item_of<N>(a, ++i);
+      for (int cost = one; lo >= before + cost; cost = x.cost()) before += cost, x = item_of<N>(a, ++i);
       sh.begin = x;
       sh.item = i;
-      sh.skip = (int)(lo - before);
+      sh.skip = lo - before;
       sh.tiles = hi - lo;
     }
   }
@@ -362,20 +381,21 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
                    kp = (uint32_t)rows_desc + (tc::su32(parts) >> 4), w = (uint32_t)w_desc + (tc::su32(weights) >> 4);
     const uint32_t full = tc::su32(sh.full), empty = tc::su32(sh.empty), part_full = tc::su32(sh.part_full),
                    part_empty = tc::su32(sh.part_empty), dead_word = tc::su32(&sh.dead);
+    const uint32_t s_full = tc::su32(sh.s_full), p_full = tc::su32(&sh.p_full), o_full = tc::su32(&sh.o_full);
     uint32_t s_slot = 0, s_phase = 0, s_part = 0, s_part_phase = 0, o_slot = 0;
     const auto wait = [&](uint32_t bar, uint32_t parity) {
       if (!tc::mbar_test(bar, parity)) wait_slow(bar, parity, dead_word);
     };
-    const auto scores = [&](int i) {
+    const auto scores = [&](uint32_t i) {
       const uint32_t d = tm + C::S_COL + (i & 1) * N;
 #pragma unroll
-      for (int j = 0; j < PER; ++j) {
+      for (uint32_t j = 0; j < PER; ++j) {
         wait(full + 8 * s_slot, s_phase);
         tc::tc_fence_after();
         const uint32_t x = xr + s_slot * (SLOT >> 4);
         if (tc::elect_one())
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (uint32_t k = 0; k < 8; ++k)
             tc::mma_f16(d, desc64(x + (k / 4) * (HALF >> 4) + (k % 4) * 2, hi), desc64(q + (2 * j + k / 4) * (N * 128 >> 4) + (k % 4) * 2, hi),
                         C::IDESC, j | k);
         if (++s_slot == SLOTS) s_slot = 0, s_phase ^= 1;
@@ -385,9 +405,9 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
       const uint32_t x = kp + s_part * (HALF >> 4);
       if (tc::elect_one()) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (uint32_t k = 0; k < 4; ++k)
           tc::mma_f16(d, desc64(x + k * 2, hi), desc64(q + 2 * PER * (N * 128 >> 4) + k * 2, hi), C::IDESC, 1);
-        commit(tc::su32(&sh.s_full[i & 1]));
+        commit(s_full + 8 * (i & 1));
         commit(part_empty + 8 * s_part);
       }
       if (++s_part == PARTS) s_part = 0, s_part_phase ^= 1;
@@ -401,11 +421,13 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
           for (int k = 0; k < 8; ++k)
             tc::mma_f16(tm + j * N, desc64(x + k * (2048 >> 4), hi), desc64(w + k * (C::WEIGHTS16 >> 4), whi), C::IDESC_O, k ? 1 : accumulate);
           commit(empty + 8 * o_slot);
-          if (j == PER - 1) commit(tc::su32(&sh.o_full));
+          if (j == PER - 1) commit(o_full);
         }
         if (++o_slot == SLOTS) o_slot = 0;
       }
     };
+    // The next tile's scores go before this one's output where its tokens are there (its key parts come last), and
+    // else behind it: the output frees the slots that further tokens wait for
     bool dead = false;
     while (!dead && walk.next()) {
       if (walk.n == 0) continue;
@@ -414,13 +436,14 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
       tc::tc_fence_after();
       scores(g);
       for (int i = 0; i < n; ++i, ++g) {
-        if (C::AHEAD && i + 1 < n) scores(g + 1);
-        wait(tc::su32(&sh.p_full), g & 1);
+        const bool early = i + 1 < n && test(part_full + 8 * s_part, s_part_phase);
+        if (early) scores(g + 1);
+        wait(p_full, g & 1);
         tc::tc_fence_after();
         dead = __any_sync(0xffffffffu, tc::block_dead(dead_word));
         if (dead) break;
         output(i);
-        if (!C::AHEAD && i + 1 < n) scores(g + 1);
+        if (!early && i + 1 < n) scores(g + 1);
       }
     }
   } else {
@@ -428,28 +451,32 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     // A wait that is in vain ends no turn: the barriers of the softmax want all of its warps.
     const int k = tid % BK, part = warp / 4, c0 = part * HC;
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    // the softmax works with a positive factor: the scale's sign goes to the queries
+    // the softmax works with a positive factor: the scale's sign goes to the scores
     const float f = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f), far = fminf(LAZY / f, 1e38f);
-    const auto load_queries = [&](const Item& x) {
+    const float sign = a.scale_log2 < 0.f ? -1.f : a.scale_log2 == 0.f ? 0.f : 1.f;
+    // an item's queries on their way to shared memory, and there
+    const auto bring_queries = [&](const Item& x) {
       constexpr int PIECES = (RANK + LATENT_ROPE) / 8;
-      const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;
-#pragma unroll 4
+#pragma unroll 2
       for (int i = tid; i < N * PIECES; i += SOFTMAX) {
-        const int r = i / PIECES, j = i % PIECES, R = x.r0 + r;
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (R < x.rows && a.scale_log2 != 0.f)
-          u = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (long long)(x.t.first + R / a.group) * a.ldq +
-                                             (long long)(R % a.group) * (RANK + LATENT_ROPE))[j];
-        u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
-        *reinterpret_cast<uint4*>(mem + (j / 8) * (N * 128) + r * 128 + ((j % 8 ^ (r & 7)) << 4)) = u;
+        const int r = i / PIECES, j = i % PIECES, R = x.r0 + r, on = R < x.rows ? 16 : 0, token = on ? R / a.group : 0;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (long long)(x.t.first + token) * a.ldq +
+                                   (long long)(on ? R - token * a.group : 0) * (RANK + LATENT_ROPE) + 8 * j;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                         tc::su32(mem + (j / 8) * (N * 128) + r * 128 + ((j % 8 ^ (r & 7)) << 4))),
+                     "l"(src), "r"(on)
+                     : "memory");
       }
+    };
+    const auto queries_there = [&] {
+      asm volatile("cp.async.wait_all;" ::: "memory");
       tc::fence_async_smem();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive1(&sh.q_full);
     };
     // the first warp looks the next item up for all of them
     bool shares = false;
-    const auto advance = [&](Segment& q) {
+    const auto look_up = [&](Segment& q) {
       bar_softmax<SOFTMAX>();                        // nobody is at the item before any more
       if (warp == 0) {
         const bool more = walk.next();
@@ -464,20 +491,23 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
             q.whole = walk.from == 0 && walk.after == 0;
             q.alike = x.first_row.lo == x.last_row.lo && x.first_row.hi == x.last_row.hi;
             if (walk.from == 0 && walk.after > 0) {  // it goes on to the block that has the last of its tiles
-              const long long end = (blockIdx.x + 1) * total / gridDim.x + walk.after;
-              run.meta[blockIdx.x] = make_int4(q.slot, (int)((end * gridDim.x - 1) / total), walk.index, (int)total);
+              const int end = run_from(total, blocks, blockIdx.x + 1) + walk.after;
+              run.meta[blockIdx.x] = make_int4(q.slot, block_of(total, blocks, end - 1), walk.index, 0);
               shares = true;
             }
           }
         }
       }
       bar_softmax<SOFTMAX>();
-      if (q.more && q.n > 0) load_queries(q.x);
     };
     float sum[HC];
-    advance(sh.seg[0]);
+    look_up(sh.seg[0]);
+    if (sh.seg[0].more && sh.seg[0].n > 0) bring_queries(sh.seg[0].x);
     for (int s = 0; sh.seg[s].more; s ^= 1) {
       const Segment& q = sh.seg[s];
+      const Segment& after = sh.seg[s ^ 1];
+      if (q.n > 0) queries_there();
+      look_up(sh.seg[s ^ 1]);
       const Item& x = q.x;
       const Tile& t = x.t;
       const int n = q.n, key0 = q.key0;
@@ -490,6 +520,9 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         float v[HC];
         const uint32_t scores = tmem + C::S_COL + (g & 1) * N + c0 + lanes;
         tmem_load(scores, v);
+        if (sign != 1.f)
+#pragma unroll
+          for (int j = 0; j < HC; ++j) v[j] *= sign;
         const int key = key0 + i * BK + k;
         if (key0 + i * BK < x.last_row.lo || key0 + (i + 1) * BK > x.first_row.hi) {
           const bool alike = q.alike, out = key < x.all.lo || key >= x.all.hi;
@@ -503,9 +536,9 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               if (out) {
-                p[e] = make_uint4(0, 0, 0, 0);
+                p[e ^ (k & 7)] = make_uint4(0, 0, 0, 0);
               } else if (!alike) {
-                const uint4 u = p[e];
+                const uint4 u = p[e ^ (k & 7)];
                 const uint32_t y[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
                 for (int z = 0; z < 4; ++z) bad |= (y[z] & 0x7f80u) == 0x7f80u || (y[z] & 0x7f800000u) == 0x7f800000u;
@@ -534,6 +567,8 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
             }
           }
           tc::fence_async_smem();
+        }
+        if (sign != 1.f || key0 + i * BK < x.last_row.lo || key0 + (i + 1) * BK > x.first_row.hi) {
           for (int j = 0; j < HC; j += 8) tmem_store8(scores + j, v + j);   // where a new reference looks for them
           asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         }
@@ -609,7 +644,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         if (lane == 0) tc::mbar_arrive1(&sh.p_full);
       }
       // the next item's queries take the place of these, whose scores are all there
-      advance(sh.seg[s ^ 1]);
+      if (after.more && after.n > 0) bring_queries(after.x);
       if (n > 0) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
       __syncwarp();
       tc::tc_fence_after();
@@ -636,34 +671,29 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         else
           a.ml[q.slot * N + tid] = make_float2(sh.ref[tid] == NONE ? -INFINITY : sh.ref[tid] * f, l);
         sh.ref[tid] = NONE;
+        const int R = min(x.r0 + tid, x.last), token = R / a.group;
+        sh.to[tid] = q.whole ? (long long)(t.first + token) * a.ldo + (long long)(R - token * a.group) * RANK : (long long)(q.slot * N + tid) * RANK;
       }
       bar_softmax<SOFTMAX>();
-      {
-        int R = x.r0 + c0, token = R / a.group, head = R - token * a.group;
+      const int rows = min(HC, x.last - x.r0 - c0 + 1);
 #pragma unroll 1
-        for (int j = 0; j < HC; j += 8) {
-#pragma unroll 1
-          for (int y = 0; y < PER; ++y) {
-            const int d = y * 128 + k;
-            float o[8] = {};
-            if (n > 0) tmem_load(tmem + y * N + c0 + j + lanes, o);
-            if (q.whole) {
-              int to = token, he = head;
+      for (int y = 0; y < PER; ++y) {
+        const int d = y * 128 + k;
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                if (R + e <= x.last)
-                  static_cast<__nv_bfloat16*>(a.out)[(long long)(t.first + to) * a.ldo + (long long)he * RANK + d] =
-                      __float2bfloat16_rn(o[e] * __int_as_float(sh.top[c0 + j + e]));
-                if (++he == a.group) he = 0, ++to;
-              }
-            } else {
+        for (int j0 = 0; j0 < HC; j0 += 16) {
+          constexpr int E = HC < 16 ? HC : 16;
+          float o[E];
 #pragma unroll
-              for (int e = 0; e < 8; ++e) a.part[(long long)(q.slot * N + c0 + j + e) * RANK + d] = o[e];
+          for (int e = 0; e < E; ++e) o[e] = 0.f;
+          if (n > 0) tmem_load(tmem + y * N + c0 + j0 + lanes, o);
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (j0 + e < rows) {
+              if (q.whole)
+                static_cast<__nv_bfloat16*>(a.out)[sh.to[c0 + j0 + e] + d] = __float2bfloat16_rn(o[e] * __int_as_float(sh.top[c0 + j0 + e]));
+              else
+                a.part[sh.to[c0 + j0 + e] + d] = o[e];
             }
-          }
-          R += 8;
-          token = R / a.group;
-          head = R - token * a.group;
         }
       }
     }
@@ -679,76 +709,53 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
   if (warp == 0) tc::tmem_dealloc(tmem, C::ALLOC);
 }
 
-// Joins the pieces of the items that blocks share, from the block that has an item's first tile: it and, of those
-// behind it up to the last, each that has tiles (its first piece).  RANK / 4 lanes a row, the rest of the block's
-// threads on further pieces.
-constexpr int JOIN_THREADS = 256;
+// Joins the pieces of the items that blocks share, from the block that has an item's first tile: its piece, and the
+// first of each block behind it up to the last.  RANK / 4 lanes a row, or several such groups that share its pieces
+// (groups > 1: few rows of many pieces would else wait out one load after the other).
+constexpr int JOIN_THREADS = 512, JOIN_BATCH = 4;
 template <int RANK, int N>
-__global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_constant__ AttendArgs a, const int4* meta, int blocks,
-                                                                   int each) {
-  constexpr int LANES = RANK / 4, GROUPS = JOIN_THREADS / LANES;
-  __shared__ float weight[SMS];
-  __shared__ int slots[SMS];
-  __shared__ float4 os[GROUPS][LANES];
-  __shared__ int pieces;
-  const int tid = threadIdx.x, lane = tid % LANES, group = tid / LANES;
+__global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_constant__ AttendArgs a, const int4* meta, int groups) {
+  constexpr int LANES = RANK / 4, AT_ONCE = JOIN_THREADS / LANES;
+  __shared__ float4 os[AT_ONCE][LANES];
+  __shared__ float2 mls[AT_ONCE];
+  const int at = threadIdx.x / LANES, lane = threadIdx.x % LANES, group = at % groups, r = blockIdx.y * (AT_ONCE / groups) + at / groups;
   tc::pdl_wait();
   const int4 m = meta[blockIdx.x];
   if (m.x < 0) return;
-  const Item x = item_of<N>(a, m.z);
-  if (tid < 32) {                                  // the pieces' slots, in the order of the blocks
-    int n = 1;
-    if (tid == 0) slots[0] = m.x;
-    for (int b0 = blockIdx.x + 1; b0 <= m.y; b0 += 32) {
-      const long long b = b0 + tid;
-      const bool on = b <= m.y && b * m.w / blocks < (b + 1) * m.w / blocks;
-      const uint32_t all = __ballot_sync(0xffffffffu, on);
-      if (on) slots[n + __popc(all & ((1u << tid) - 1))] = 2 * (int)b;
-      n += __popc(all);
-    }
-    if (tid == 0) pieces = n;
-  }
-  for (int r = blockIdx.y * each; r < min((blockIdx.y + 1) * each, N) && x.r0 + r <= x.last; ++r) {
-    __syncthreads();
-    const int n = pieces;
-    if (tid < 32) {
-      float top = -INFINITY, sum = 0.f;
-      for (int p = tid; p < n; p += 32) top = fmaxf(top, a.ml[slots[p] * N + r].x);
+  const int n = m.z / a.tiles;
+  const SeqRows s = seq_rows(a.m, n, a.rows, a.max_new);
+  const int R = m.z % a.tiles * N + r, pieces = m.y - blockIdx.x + 1;
+  const bool on = r < N && R < s.count * a.group;
+  float top = -INFINITY, sum = 0.f;
+  float4 o = {};
+  if (on)
+    for (int p0 = group; p0 < pieces; p0 += groups * JOIN_BATCH) {
+      float2 ml[JOIN_BATCH];
+      float4 y[JOIN_BATCH];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float ref = top == -INFINITY ? 0.f : top;
-      for (int p = tid; p < n; p += 32) {
-        const float2 ml = a.ml[slots[p] * N + r];
-        const float w = ex2_approx(ml.x - ref);
-        weight[p] = w;
-        sum = fmaf(ml.y, w, sum);
+      for (int j = 0; j < JOIN_BATCH; ++j) {
+        const int p = p0 + j * groups;
+        ml[j] = make_float2(-INFINITY, 0.f);
+        y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p < pieces) {
+          const long long row = (long long)(p == 0 ? m.x : 2 * (blockIdx.x + p)) * N + r;
+          ml[j] = a.ml[row];
+          y[j] = *reinterpret_cast<const float4*>(a.part + row * RANK + 4 * lane);
+        }
       }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      if (tid == 0) os[0][0].x = sum;
+      for (int j = 0; j < JOIN_BATCH; ++j) join(top, sum, o, ml[j], y[j]);
     }
+  if (groups > 1) {
+    os[at][lane] = o;
+    if (lane == 0) mls[at] = make_float2(top, sum);
     __syncthreads();
-    const float sum = os[0][0].x;
-    float4 o = {};
-#pragma unroll 4
-    for (int p = group; p < n; p += GROUPS) {
-      const float4 y = *reinterpret_cast<const float4*>(a.part + (long long)(slots[p] * N + r) * RANK + 4 * lane);
-      const float w = weight[p];
-      o = make_float4(fmaf(y.x, w, o.x), fmaf(y.y, w, o.y), fmaf(y.z, w, o.z), fmaf(y.w, w, o.w));
-    }
-    __syncthreads();
-    os[group][lane] = o;
-    __syncthreads();
-    if (group == 0) {
-      for (int e = 1; e < GROUPS; ++e) {
-        const float4 y = os[e][lane];
-        o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
-      }
-      const int R = x.r0 + r;
-      store_out(static_cast<__nv_bfloat16*>(a.out) + (long long)(x.t.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane,
-                o, sum == 0.f ? 0.f : 1.f / sum);
-    }
+    if (!on || group != 0) return;
+    for (int e = 1; e < groups; ++e) join(top, sum, o, mls[at + e], os[at + e][lane]);
   }
+  if (!on) return;
+  store_out(static_cast<__nv_bfloat16*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane, o,
+            sum == 0.f ? 0.f : 1.f / sum);
 }
 
 template <int RANK, int N>
@@ -763,9 +770,11 @@ cudaError_t launch_as(const AttendArgs& a, const LatentPlan& p, cudaStream_t st)
   latent_tiles_kernel<RANK, N><<<p.blocks, C::THREADS, C::SMEM, st>>>(a, map, run);
   e = cudaGetLastError();
   if (e != cudaSuccess || !run.split) return e;
-  const int each = std::max(1, N / 16);
+  constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
+  int groups = 1;
+  while (groups < AT_ONCE && groups * JOIN_BATCH * run.items < p.blocks) groups *= 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.blocks, (N + each - 1) / each);
+  cfg.gridDim = dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE);
   cfg.blockDim = JOIN_THREADS;
   cfg.stream = st;
   // the join waits for what the pieces wrote (griddepcontrol.wait)
@@ -774,15 +783,13 @@ cudaError_t launch_as(const AttendArgs& a, const LatentPlan& p, cudaStream_t st)
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, p.blocks, each);
+  return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, groups);
 }
 template <int RANK>
 cudaError_t launch_of(const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
   if (p.tile_rows == 16) return launch_as<RANK, 16>(a, p, st);
-  if constexpr (RANK < 512) {
+  if constexpr (RANK < 512)
     if (p.tile_rows == 64) return launch_as<RANK, 64>(a, p, st);
-    if (p.tile_rows == 128) return launch_as<RANK, 128>(a, p, st);
-  }
   return launch_as<RANK, 32>(a, p, st);
 }
 
@@ -790,10 +797,10 @@ cudaError_t launch_of(const AttendArgs& a, const LatentPlan& p, cudaStream_t st)
 
 // Pieces: items go to the blocks whole where that takes little longer, in tiles, than equal runs and their join
 void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int keys) {
-  p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : all <= 64 ? 64 : 128;
+  p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : 64;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + BK - 1) / BK);
-  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 8;
+  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 6;
   const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
   p.splits = split ? 2 : 1;
   p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
