@@ -426,8 +426,8 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         if (++o_slot == SLOTS) o_slot = 0;
       }
     };
-    // The next tile's scores go before this one's output where its tokens are there (its key parts come last), and
-    // else behind it: the output frees the slots that further tokens wait for
+    // The next tile's scores go before this one's output where its tokens are there (its key parts come last) before
+    // the weights are, and else behind it: the output frees the slots that further tokens wait for
     bool dead = false;
     while (!dead && walk.next()) {
       if (walk.n == 0) continue;
@@ -436,14 +436,18 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
       tc::tc_fence_after();
       scores(g);
       for (int i = 0; i < n; ++i, ++g) {
-        const bool early = i + 1 < n && test(part_full + 8 * s_part, s_part_phase);
-        if (early) scores(g + 1);
+        bool early = i + 1 >= n;
+        for (const long long since = clock64(); !early && !test(p_full, g & 1);) {
+          early = test(part_full + 8 * s_part, s_part_phase);
+          if (early) scores(g + 1);
+          else if (clock64() - since > WAIT_CYCLES_DEFAULT) break;   // (the wait below reports it)
+        }
         wait(p_full, g & 1);
         tc::tc_fence_after();
         dead = __any_sync(0xffffffffu, tc::block_dead(dead_word));
         if (dead) break;
         output(i);
-        if (!early && i + 1 < n) scores(g + 1);
+        if (!early) scores(g + 1);
       }
     }
   } else {
@@ -672,28 +676,35 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
           a.ml[q.slot * N + tid] = make_float2(sh.ref[tid] == NONE ? -INFINITY : sh.ref[tid] * f, l);
         sh.ref[tid] = NONE;
         const int R = min(x.r0 + tid, x.last), token = R / a.group;
-        sh.to[tid] = q.whole ? (long long)(t.first + token) * a.ldo + (long long)(R - token * a.group) * RANK : (long long)(q.slot * N + tid) * RANK;
+        sh.to[tid] = (long long)(t.first + token) * a.ldo + (long long)(R - token * a.group) * RANK;
       }
       bar_softmax<SOFTMAX>();
+      // (what is read of shared memory is read before the stores: they might write it, for all that the compiler knows)
       const int rows = min(HC, x.last - x.r0 - c0 + 1);
+      const bool whole = q.whole;
+      float* const part = a.part + (long long)(q.slot * N + c0) * RANK + k;
 #pragma unroll 1
       for (int y = 0; y < PER; ++y) {
-        const int d = y * 128 + k;
+        float o[HC];
 #pragma unroll
-        for (int j0 = 0; j0 < HC; j0 += 16) {
-          constexpr int E = HC < 16 ? HC : 16;
-          float o[E];
+        for (int e = 0; e < HC; ++e) o[e] = 0.f;
+        if (n > 0) tmem_load(tmem + y * N + c0 + lanes, o);
+        if (!whole) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) o[e] = 0.f;
-          if (n > 0) tmem_load(tmem + y * N + c0 + j0 + lanes, o);
+          for (int e = 0; e < HC; ++e)
+            if (e < rows) part[e * RANK + y * 128] = o[e];
+        } else {
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (j0 + e < rows) {
-              if (q.whole)
-                static_cast<__nv_bfloat16*>(a.out)[sh.to[c0 + j0 + e] + d] = __float2bfloat16_rn(o[e] * __int_as_float(sh.top[c0 + j0 + e]));
-              else
-                a.part[sh.to[c0 + j0 + e] + d] = o[e];
-            }
+          for (int e0 = 0; e0 < HC; e0 += 8) {
+            __nv_bfloat16* to[8];
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              to[e] = static_cast<__nv_bfloat16*>(a.out) + sh.to[c0 + e0 + e] + y * 128 + k, f[e] = __int_as_float(sh.top[c0 + e0 + e]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (e0 + e < rows) *to[e] = __float2bfloat16_rn(o[e0 + e] * f[e]);
+          }
         }
       }
     }
