@@ -104,6 +104,15 @@ __device__ __forceinline__ void mma_split(float (*d)[4], float (*r)[4], const ui
     for (int i = 0; i < 4; ++i) mma8(r[i], ah, xl[i], yl[i]);
 }
 
+// (top, sum, o) joined with another piece's
+__device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 ml, float4 p) {
+  const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
+  const float f = exp2f(top - base), g = exp2f(ml.x - base);
+  top = now;
+  sum = sum * f + ml.y * g;
+  o = make_float4(o.x * f + p.x * g, o.y * f + p.y * g, o.z * f + p.z * g, o.w * f + p.w * g);
+}
+
 // A row whose sums are not finite, once more with plain fp32 products (an infinity's low part is no
 // number, so that infinities that a row sees, and NaN in tokens that it does not see, spoil the split
 // form).  A warp takes the row: a lane a key, then a lane D / 32 dimensions.

@@ -133,15 +133,6 @@ __device__ __forceinline__ void join_cluster(const AttendArgs& a, const Tile& t,
   cluster_arrive_wait();                           // no block ends while another reads its shared memory
 }
 
-// (top, sum, o) joined with another piece's
-__device__ __forceinline__ void join(float& top, float& sum, float4& o, float2 ml, float4 p) {
-  const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
-  const float f = exp2f(top - base), g = exp2f(ml.x - base);
-  top = now;
-  sum = sum * f + ml.y * g;
-  o = make_float4(o.x * f + p.x * g, o.y * f + p.y * g, o.z * f + p.z * g, o.w * f + p.w * g);
-}
-
 // launches a block a piece, the pieces of a cluster as one
 template <typename... K, typename... A>
 cudaError_t launch_pieces(void (*kernel)(K...), const AttendArgs& a, int threads, int smem, std::atomic<uint64_t>& done,

@@ -294,6 +294,8 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid < N) sh.ref[tid] = NONE;
+  tc::pdl_wait();                                  // what earlier kernels wrote is there
+  if (run.split) tc::pdl_trigger();                // the join may take its places, and waits there
   int total = 0;
   int blocks = gridDim.x;                          // that take tiles
   if (!run.split) {
@@ -340,18 +342,20 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
 
   if (warp == C::WARPS + 1) {
     // ------------------------------------------------------------ copies
-    const int page_tokens = a.m.page_tokens, box = min(page_tokens, BK), shift = 31 - __clz(page_tokens);
+    const int page_tokens = a.m.page_tokens, box = min(page_tokens, BK), shift = 31 - __clz(page_tokens), log_boxes = 7 - shift;   // 1 << log_boxes boxes a tile
     while (walk.next()) {
       const Range all = walk.x.all;
-      const auto page_of = [&](int i) {              // -1: no token of the item is there
-        const int key = walk.key0() + i * BK + lane * box;
-        return i < walk.n && lane * box < BK && key + box > all.lo && key < all.hi ? seq_page(a.m, walk.x.t.n, key >> shift) : -1;
+      // pages are looked up for 32 boxes of consecutive tiles at once, a lane each (-1: it holds no token of the item)
+      const auto pages_from = [&](int i) {
+        const int tile = i + (lane >> log_boxes), key = walk.key0() + i * BK + lane * box;
+        return tile < walk.n && key + box > all.lo && key < all.hi ? seq_page(a.m, walk.x.t.n, key >> shift) : -1;
       };
-      int ahead = page_of(0);
+      int batch = pages_from(0);
       for (int i = 0; i < walk.n; ++i, ++g) {
-        const int page = ahead;
-        ahead = page_of(i + 1);
-        const bool on = page >= 0;
+        const int at_lane = (i << log_boxes) & 31;
+        if (at_lane == 0 && i > 0) batch = pages_from(i);
+        const int page = __shfl_sync(0xffffffffu, batch, (at_lane + lane) & 31);
+        const bool on = lane >> log_boxes == 0 && page >= 0;
         const int at = page * page_tokens + ((walk.key0() + i * BK + lane * box) & (page_tokens - 1));
         const int copies = __popc(__ballot_sync(0xffffffffu, on));
         const auto bring = [&](uint8_t* to, uint64_t* full, uint64_t* empty, int use, int column, int halves) {
@@ -722,49 +726,60 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
 
 // Joins the pieces of the items that blocks share, from the block that has an item's first tile: its piece, and the
 // first of each block behind it up to the last.  RANK / 4 lanes a row, or several such groups that share its pieces
-// (groups > 1: few rows of many pieces would else wait out one load after the other).
-constexpr int JOIN_THREADS = 512, JOIN_BATCH = 4;
+// (few rows of many pieces would else wait out one load after the other).
+constexpr int JOIN_THREADS = 512;
 template <int RANK, int N>
 __global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_constant__ AttendArgs a, const int4* meta, int groups) {
   constexpr int LANES = RANK / 4, AT_ONCE = JOIN_THREADS / LANES;
+  __shared__ float weight[AT_ONCE][SMS];           // of a row's pieces
+  __shared__ float total[AT_ONCE];
   __shared__ float4 os[AT_ONCE][LANES];
-  __shared__ float2 mls[AT_ONCE];
-  const int at = threadIdx.x / LANES, lane = threadIdx.x % LANES, group = at % groups, r = blockIdx.y * (AT_ONCE / groups) + at / groups;
+  const int at = threadIdx.x / LANES, lane = threadIdx.x % LANES, group = at % groups, row = at / groups;
+  const int r = blockIdx.y * (AT_ONCE / groups) + row;
   tc::pdl_wait();
   const int4 m = meta[blockIdx.x];
   if (m.x < 0) return;
-  const int n = m.z / a.tiles;
+  const int n = m.z / a.tiles, pieces = m.y - blockIdx.x + 1;
   const SeqRows s = seq_rows(a.m, n, a.rows, a.max_new);
-  const int R = m.z % a.tiles * N + r, pieces = m.y - blockIdx.x + 1;
+  const int R = m.z % a.tiles * N + r;
   const bool on = r < N && R < s.count * a.group;
-  float top = -INFINITY, sum = 0.f;
-  float4 o = {};
-  if (on)
-    for (int p0 = group; p0 < pieces; p0 += groups * JOIN_BATCH) {
-      float2 ml[JOIN_BATCH];
-      float4 y[JOIN_BATCH];
+  const auto place = [&](int p) { return (long long)(p == 0 ? m.x : 2 * (blockIdx.x + p)) * N + r; };
+  if (on && group == 0 && lane < 32) {             // a warp a row: its pieces' weights
+    float top = -INFINITY, sum = 0.f;
+    for (int p = lane; p < pieces; p += 32) top = fmaxf(top, a.ml[place(p)].x);
 #pragma unroll
-      for (int j = 0; j < JOIN_BATCH; ++j) {
-        const int p = p0 + j * groups;
-        ml[j] = make_float2(-INFINITY, 0.f);
-        y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p < pieces) {
-          const long long row = (long long)(p == 0 ? m.x : 2 * (blockIdx.x + p)) * N + r;
-          ml[j] = a.ml[row];
-          y[j] = *reinterpret_cast<const float4*>(a.part + row * RANK + 4 * lane);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < JOIN_BATCH; ++j) join(top, sum, o, ml[j], y[j]);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int p = lane; p < pieces; p += 32) {
+      const float2 ml = a.ml[place(p)];
+      const float w = ex2_approx(ml.x - (top == -INFINITY ? 0.f : top));
+      weight[row][p] = w;
+      sum = fmaf(ml.y, w, sum);
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) total[row] = sum;
+  }
+  __syncthreads();
+  float4 o = {};
+  if (on) {
+#pragma unroll 8
+    for (int p = group; p < pieces; p += groups) {
+      const float4 y = *reinterpret_cast<const float4*>(a.part + place(p) * RANK + 4 * lane);
+      const float w = weight[row][p];
+      o = make_float4(fmaf(y.x, w, o.x), fmaf(y.y, w, o.y), fmaf(y.z, w, o.z), fmaf(y.w, w, o.w));
+    }
+  }
   if (groups > 1) {
     os[at][lane] = o;
-    if (lane == 0) mls[at] = make_float2(top, sum);
     __syncthreads();
-    if (!on || group != 0) return;
-    for (int e = 1; e < groups; ++e) join(top, sum, o, mls[at + e], os[at + e][lane]);
+    if (group == 0)
+      for (int e = 1; e < groups; ++e) {
+        const float4 y = os[at + e][lane];
+        o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
+      }
   }
-  if (!on) return;
+  if (!on || group != 0) return;
+  const float sum = total[row];
   store_out(static_cast<__nv_bfloat16*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane, o,
             sum == 0.f ? 0.f : 1.f / sum);
 }
@@ -778,22 +793,25 @@ cudaError_t launch_as(const AttendArgs& a, const LatentPlan& p, cudaStream_t st)
   cudaError_t e = allow_smem(latent_tiles_kernel<RANK, N>, C::SMEM, done);
   if (e != cudaSuccess) return e;
   const Run run{a.m.n_seq * a.tiles, p.splits > 1, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * N)};
-  latent_tiles_kernel<RANK, N><<<p.blocks, C::THREADS, C::SMEM, st>>>(a, map, run);
-  e = cudaGetLastError();
-  if (e != cudaSuccess || !run.split) return e;
-  constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
-  int groups = 1;
-  while (groups < AT_ONCE && groups * JOIN_BATCH * run.items < p.blocks) groups *= 2;
+  // both kernels wait for the ones before them themselves (griddepcontrol.wait)
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE);
-  cfg.blockDim = JOIN_THREADS;
-  cfg.stream = st;
-  // the join waits for what the pieces wrote (griddepcontrol.wait)
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
+  cfg.stream = st;
+  cfg.gridDim = p.blocks;
+  cfg.blockDim = C::THREADS;
+  cfg.dynamicSmemBytes = C::SMEM;
+  e = cudaLaunchKernelEx(&cfg, latent_tiles_kernel<RANK, N>, a, map, run);
+  if (e != cudaSuccess || !run.split) return e;
+  constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
+  int groups = 1;
+  while (groups < AT_ONCE && groups * 8 * run.items < p.blocks) groups *= 2;
+  cfg.gridDim = dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE);
+  cfg.blockDim = JOIN_THREADS;
+  cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, groups);
 }
 template <int RANK>
@@ -811,7 +829,7 @@ void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int ke
   p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : 64;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + BK - 1) / BK);
-  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 6;
+  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 3;
   const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
   p.splits = split ? 2 : 1;
   p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
