@@ -684,22 +684,28 @@ class LatentMemory(_Paged):
         self._scratch = {}                          # bytes of scratch by (rows, max_new, max_len)
         self.tensors = (pages, table, lens, starts, status)
 
+    def _misfit(self, t, what: str, shape, inner: str) -> ValueError:
+        return ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; expected {self.dtype} "
+                          f"{shape} on {self.device}, {inner} contiguous")
+
     def _parts(self, t, what: str, shape):
         """(address, elements between rows, and between heads) of [rows][width] or [rows][heads][width]."""
-        if t.dtype is not self.dtype or t.get_device() != self.index or t.shape != shape or t.stride(-1) != 1:
-            raise ValueError(f"{what}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; expected {self.dtype} "
-                             f"{shape} on {self.device}, the last dimension contiguous")
-        heads, width = (shape[1] if len(shape) == 3 else 1), shape[-1]
-        hd = t.stride(1) if heads > 1 else width
-        ld = t.stride(0) if shape[0] > 1 else max(0, heads - 1) * hd + width
-        return t.data_ptr(), ld, hd
+        s = t.stride()
+        if t.dtype is not self.dtype or t.get_device() != self.index or t.shape != shape or s[-1] != 1:
+            raise self._misfit(t, what, shape, "the last dimension")
+        if len(s) == 2:
+            return t.data_ptr(), s[0] if shape[0] > 1 else shape[1], shape[1]
+        rows, heads, width = shape
+        hd = s[1] if heads > 1 else width
+        return t.data_ptr(), s[0] if rows > 1 else (heads - 1) * hd + width, hd
 
-    def _heads(self, t, what: str, rows: int, width: int):
+    def _heads(self, t, what: str, shape):
         """(address, elements between rows) of [rows][n_head][width], the heads of a row contiguous."""
-        p, ld, hd = self._parts(t, what, (rows, self.n_head, width))
-        if hd != width:
-            raise ValueError(f"{what}: strides {t.stride()}; expected the heads of a row contiguous")
-        return p, ld
+        s, (rows, heads, width) = t.stride(), shape
+        if (t.dtype is not self.dtype or t.get_device() != self.index or t.shape != shape or s[2] != 1
+                or (s[1] != width and heads > 1)):
+            raise self._misfit(t, what, shape, "the heads of a row")
+        return t.data_ptr(), s[0] if rows > 1 else heads * width
 
     def append(self, c, k, q=None, c_gain=None, eps: float = 1e-6, rotation=None, pos0=None, out=None, stream=None):
         """evo_latent_append: latents c [rows][rank] (normed where c_gain is given) and rotated key parts k
@@ -721,11 +727,14 @@ class LatentMemory(_Paged):
             cp, ldc, _ = self._parts(c, "c", (rows, self.rank))
             kp, ldk, _ = self._parts(k, "k", (rows, LATENT_ROPE))
         if q is not None:
-            shape = (rows, self.n_head, LATENT_ROPE)
+            heads = self.n_head
+            shape = (rows, heads, LATENT_ROPE)
             qp, ldq, hdq = self._parts(q, "q", shape)
             if out is None:
                 out = _new(shape, self.dtype, self.device, stream)
-            op, ldo, hdo = self._parts(out, "out", shape)
+                op, ldo, hdo = out.data_ptr(), heads * LATENT_ROPE, LATENT_ROPE
+            else:
+                op, ldo, hdo = self._parts(out, "out", shape)
         if c_gain is not None:
             gain = _need(c_gain, "c_gain", _F32, (self.rank,), index)
         if rotation is not None:
@@ -746,10 +755,13 @@ class LatentMemory(_Paged):
         chunks and memories (None: the rows, or their equal share, and what the table can hold)."""
         st = _launch_stream(self.index, stream)
         rows = q.shape[0]
-        qp, ldq = self._heads(q, "q", rows, self.rank + LATENT_ROPE)
+        heads, rank = self.n_head, self.rank
+        qp, ldq = self._heads(q, "q", (rows, heads, rank + LATENT_ROPE))
         if out is None:
-            out = _new((rows, self.n_head, self.rank), self.dtype, self.device, stream)
-        op, ldo = self._heads(out, "out", rows, self.rank)
+            out = _new((rows, heads, rank), self.dtype, self.device, stream)
+            op, ldo = out.data_ptr(), heads * rank
+        else:
+            op, ldo = self._heads(out, "out", (rows, heads, rank))
         if rows == 0:
             return out
         max_new, max_len, window = self._sizes(rows, max_new, max_len, window)

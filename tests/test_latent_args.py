@@ -157,12 +157,12 @@ def test_binding_checks_tensors(B):
             B.LatentMemory(**(dict(pages=pages, table=table, lens=lens, n_head=4) | bad))
     wide = torch.zeros(6, 4, 200, dtype=torch.bfloat16)
     assert m._parts(wide[..., 136:], "q", (6, 4, 64)) == (wide.data_ptr() + 272, 800, 200)
-    assert m._heads(torch.zeros(6, 4, 192, dtype=torch.bfloat16), "q", 6, 192)[1] == 768
+    assert m._heads(torch.zeros(6, 4, 192, dtype=torch.bfloat16), "q", (6, 4, 192))[1] == 768
     for bad in (wide, wide[:5, :, :64], wide[:, :3, :64], wide[..., :64].float(), wide.transpose(1, 2)[:, :64], wide[0]):
         with pytest.raises(ValueError):
             m._parts(bad, "q", (6, 4, 64))
     with pytest.raises(ValueError):
-        m._heads(wide[..., :192], "q", 6, 192)
+        m._heads(wide[..., :192], "q", (6, 4, 192))
 
 
 def test_status_word(B):
