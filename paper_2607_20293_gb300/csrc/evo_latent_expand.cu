@@ -4,10 +4,13 @@
 // written to the token's page of the other memory.
 //
 // bf16, on tcgen05: a block has one head's 192 products (its maps stay in shared memory: 48 to 192 KB) and takes
-// tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  Warp 9 brings them, warp
-// 8 issues the products into one of two accumulators, warps 0-7 empty the other: a thread has a token and
-// either its key or its value, and writes whole 32-byte sectors of them.  The output is 512 bytes a
-// (token, head) against 2 rank that are read, mostly from L2: what bounds the kernel is the writes.
+// tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  Warp 9 looks tiles and
+// pages up, for all, and brings the latents, warp 8 issues the products into one of two accumulators, warps
+// 0-7 empty the other: four warps the keys, four the values.  The output is 512 bytes a (token, head) against 2 rank
+// that are read, mostly from L2, so the writes bound the kernel, and have to leave as whole lines: accumulators are read
+// 16 tokens by 256 bits, four lanes a token, and the maps' rows stand in shared memory in the order that gives
+// each of these lanes 8 products of its own in a row (a token a lane and 32 bytes a store were 32 lines an
+// instruction: 101 us for 20,500 tokens of 16 heads).
 //
 // fp32: a block takes 64 tokens and the 192 products of a head, 16 of the rank at a time through shared
 // memory; a thread has 8 tokens x 6 products in packed pairs of tokens.
@@ -54,8 +57,14 @@ struct Cfg {
   static constexpr int SMEM = 1024 + W + STAGES * STAGE;
   static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
 };
+constexpr int INFOS = 4;                           // tiles that are looked up ahead
+struct Info {
+  int n, t0, lo, hi;              // sequence; the tile's tokens t0 .. t0 + 127, of which lo .. hi - 1 are written; n < 0: no more
+  int from[8], to[8];             // pages of its tokens in either memory, -1: outside the pool
+};
 struct Shared {
-  uint64_t full[8], empty[8], w_full, acc_full[2], acc_empty[2];
+  uint64_t full[8], empty[8], w_full, acc_full[2], acc_empty[2], info_full[INFOS], info_empty[INFOS];
+  Info info[INFOS];
   uint32_t tmem;
   int dead;
 };
@@ -64,34 +73,41 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* de
   const uint32_t b = tc::su32(bar);
   return tc::mbar_test(b, parity) || wait_live(b, parity, tc::su32(dead));
 }
-// 16 values as bf16 to a 32-byte sector, or to two halves of 16 where rows start on these
-__device__ __forceinline__ void put16(__nv_bfloat16* p, const uint32_t (&w)[8], bool whole) {
-  if (whole) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-  } else {
-    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-  }
+// 32 columns of 16 lanes: of column 8 k + 2 c + e, lane (g, c) gets that of TMEM lane g in v[4 k + e] and of g + 8 in v[4 k + 2 + e]
+__device__ __forceinline__ void tmem_ld16x32(uint32_t taddr, float (&v)[16]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
 }
+__device__ __forceinline__ uint32_t pair_of(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// the product (0 .. 63 of the key, 64 .. of the value) that stands in column p of the accumulator: a lane's 8 in a row
+__device__ __forceinline__ int product_of(int p) { return p & ~31 | (p & 6) << 2 | (p & 24) >> 2 | (p & 1); }
 
 template <int RANK>
 __global__ void __launch_bounds__(TILE_THREADS, 1)
-    latent_expand_tiles_kernel(const __grid_constant__ LatentExpandArgs a, const __grid_constant__ CUtensorMap xmap,
-                               const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, int pairs,
-                               int groups) {
+    latent_expand_tiles_kernel(const __grid_constant__ LatentExpandArgs a, const __grid_constant__ CUtensorMap map, int pairs, int groups) {
   using C = Cfg<RANK>;
   extern __shared__ uint8_t raw[];
   __shared__ Shared sh;
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, H = a.to.n_kv_head, h = blockIdx.x % H, first = blockIdx.x / H;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, H = a.to.n_kv_head, h = blockIdx.x % H;
   uint8_t* const maps = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   uint8_t* const ring = maps + C::W;
+  if (tid == 0) fetch_map(&map);
+  __syncwarp();                                              // a whole warp's instruction, behind one lane's prefetch
   if (warp == 0) tc::tmem_alloc(&sh.tmem, 512);
   if (tid == 32) {
     for (int i = 0; i < C::STAGES; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], 1);
-    tc::mbar_init1(&sh.w_full, 1);
-    for (int i = 0; i < 2; ++i) tc::mbar_init1(&sh.acc_full[i], 1), tc::mbar_init1(&sh.acc_empty[i], 8);   // a warp each
+    tc::mbar_init1(&sh.w_full, 9);                           // a warp each
+    for (int i = 0; i < 2; ++i) tc::mbar_init1(&sh.acc_full[i], 1), tc::mbar_init1(&sh.acc_empty[i], 8);
+    for (int i = 0; i < INFOS; ++i) tc::mbar_init1(&sh.info_full[i], 1), tc::mbar_init1(&sh.info_empty[i], 9);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -99,132 +115,148 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  // The block's tiles: of pairs (tile, sequence), sequences first, every groups-th.  Tiles start at multiples of 128
-  // tokens, so that pages fit them
-  const auto tile_of = [&](int pair, int2& range) {
-    const int n = pair % a.m.n_seq;
-    range = token_range(a, n);
-    return range.x / TM * TM + pair / a.m.n_seq * TM;
-  };
+  tc::pdl_wait();                                            // what earlier kernels wrote is there
 
   if (warp == 9) {
-    // ------------------------------------------------------------ copies
-    if (lane == 0) {
-      tc::mbar_expect_tx(&sh.w_full, C::W);
-      for (int c = 0; c < C::CHUNKS; ++c) {
-        tile_load(tc::su32(maps + c * CHUNK), &kmap, 64 * c, h * LATENT_KEY, tc::su32(&sh.w_full));
-        tile_load(tc::su32(maps + c * CHUNK + LATENT_KEY * 128), &vmap, 64 * c, h * LATENT_VALUE, tc::su32(&sh.w_full));
-      }
-    }
-    __syncwarp();
-    const int page_tokens = a.m.page_tokens, box = min(page_tokens, TM);
-    int index = 0;
-    for (int pair = first; pair < pairs; pair += groups) {
-      int2 range;
-      const int t0 = tile_of(pair, range);
-      if (t0 >= range.y) continue;
-      const int t = t0 + lane * box;
-      int page = lane * box < TM && t + box > range.x && t < range.y ? page_or_none(a.m, a.m.status, pair % a.m.n_seq, t / page_tokens) : -1;
-      const int copies = __popc(__ballot_sync(0xffffffffu, page >= 0));
+    // ------------------------------------------------------------ tiles, pages and copies
+    // The block's tiles: of pairs (tile, sequence), sequences first, every groups-th.  Tiles start at multiples of 128
+    // tokens, so that pages fit them
+    const int page_tokens = a.m.page_tokens, to_tokens = a.to.page_tokens, box = min(page_tokens, TM);
+    int index = 0, i = 0;
+    for (int pair = blockIdx.x / H;; pair += groups) {
+      const bool more = pair < pairs;
+      const int n = more ? pair % a.m.n_seq : -1;
+      int2 range = make_int2(0, 0);
+      if (more) range = token_range(a, n);
+      const int t0 = range.x / TM * TM + (more ? pair / a.m.n_seq * TM : 0);
+      if (more && t0 >= range.y) continue;
+      Info& info = sh.info[i % INFOS];
+      if (i >= INFOS && !__all_sync(0xffffffffu, wait_for(&sh.info_empty[i % INFOS], (i / INFOS - 1) & 1, &sh.dead))) break;
+      // lanes 0 .. 7: the latents' pages; 8 .. 15: the other memory's
+      const int l = lane % 8, size = lane < 8 ? page_tokens : to_tokens, t = t0 + l * size;
+      int page = -1;
+      if (more && lane < 16 && l * size < TM && t + size > range.x && t < range.y)
+        page = page_or_none(lane < 8 ? a.m : a.to, a.m.status, n, t / size);
+      if (lane < 8) info.from[l] = page;
+      else if (lane < 16) info.to[l] = page;
+      if (lane == 0) info.n = n, info.t0 = t0, info.lo = range.x, info.hi = range.y;
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive1(&sh.info_full[i % INFOS]);
+      if (!more) break;
+      ++i;
+      const bool on = lane < 8 && page >= 0;
+      const int copies = __popc(__ballot_sync(0xffffffffu, on));
       for (int c = 0; c < C::CHUNKS; ++c, ++index) {
         const int slot = index % C::STAGES, use = index / C::STAGES;
         if (!__all_sync(0xffffffffu, use == 0 || wait_for(&sh.empty[slot], (use - 1) & 1, &sh.dead))) continue;
         if (lane == 0) tc::mbar_expect_tx(&sh.full[slot], copies * box * 128);
         __syncwarp();
-        if (page >= 0)
-          tile_load(tc::su32(ring + slot * STAGE + lane * box * 128), &xmap, 64 * c, page * page_tokens + t % page_tokens,
+        if (on)
+          tile_load(tc::su32(ring + slot * STAGE + lane * box * 128), &map, 64 * c, page * page_tokens + t % page_tokens,
                     tc::su32(&sh.full[slot]));
         __syncwarp();
       }
     }
-  } else if (warp == 8) {
-    // ------------------------------------------------------------ products
-    wait_for(&sh.w_full, 0, &sh.dead);
-    int index = 0, i = 0;
-    for (int pair = first; pair < pairs; pair += groups) {
-      int2 range;
-      if (tile_of(pair, range) >= range.y) continue;
-      if (i >= 2) wait_for(&sh.acc_empty[i & 1], (i / 2 - 1) & 1, &sh.dead);
-      for (int c = 0; c < C::CHUNKS; ++c, ++index) {
-        const int slot = index % C::STAGES;
-        wait_for(&sh.full[slot], (index / C::STAGES) & 1, &sh.dead);
-        tc::tc_fence_after();
-        if (!tc::block_dead(tc::su32(&sh.dead)) && tc::elect_one()) {
-          const uint32_t x = tc::su32(ring + slot * STAGE), w = tc::su32(maps + c * CHUNK);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            tc::mma_f16(tmem + 256 * (i & 1), tc::sw128_desc(x + 32 * k), tc::sw128_desc(w + 32 * k), C::IDESC, c | k);
-          tc::mma_commit(&sh.empty[slot]);
-          if (c == C::CHUNKS - 1) tc::mma_commit(&sh.acc_full[i & 1]);
-        }
-        __syncwarp();
-      }
-      ++i;
-    }
   } else {
-    // ------------------------------------------------------------ a token a thread: its key (warps 0-3) or its value
-    const bool value = warp >= 4;
-    __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(value ? a.to.v_pages : a.to.k_pages);
-    const bool whole = reinterpret_cast<uintptr_t>(out) % 32 == 0;
-    const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    // a thread's token: its row in either pool.  Looked up a tile ahead
-    struct Token { long long from, to; };
-    const auto next_of = [&](int pair, Token& token) {
-      for (; pair < pairs; pair += groups) {
-        int2 range;
-        const int t0 = tile_of(pair, range), n = pair % a.m.n_seq, t = t0 + tid % TM;
-        if (t0 >= range.y) continue;
-        token = Token{-1, -1};
-        if (t >= range.x && t < range.y) {
-          const int p = page_or_none(a.m, a.m.status, n, t / a.m.page_tokens), q = page_or_none(a.to, a.m.status, n, t / a.to.page_tokens);
-          if (p >= 0 && q >= 0)
-            token = Token{(long long)p * a.m.page_tokens + t % a.m.page_tokens, ((long long)q * H + h) * a.to.page_tokens + t % a.to.page_tokens};
-        }
-        break;
-      }
-      return pair;
+    // the head's maps, 16 bytes a copy
+    constexpr int PIECES = RANK / 8;
+#pragma unroll 4
+    for (int i = tid; i < BN * PIECES; i += TILE_THREADS - 32) {
+      const int p = i / PIECES, j = i % PIECES, o = product_of(p);
+      const __nv_bfloat16* src = (p < LATENT_KEY ? static_cast<const __nv_bfloat16*>(a.w_k) + ((long long)h * LATENT_KEY + o) * RANK
+                                                 : static_cast<const __nv_bfloat16*>(a.w_v) + ((long long)h * LATENT_VALUE + o - LATENT_KEY) * RANK) + 8 * j;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::su32(maps + j / 8 * CHUNK + p * 128 + ((j % 8 ^ (p & 7)) << 4))), "l"(src)
+                   : "memory");
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    tc::fence_async_smem();
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive1(&sh.w_full);
+    // the i-th tile's info; false: there is none, or a wait was in vain
+    const auto info_of = [&](int i, Info& info) {
+      const bool ok = __all_sync(0xffffffffu, wait_for(&sh.info_full[i % INFOS], (i / INFOS) & 1, &sh.dead));
+      if (ok) info = sh.info[i % INFOS];
+      return ok && info.n >= 0;
     };
-    Token token;
-    int pair = next_of(first, token);
-    for (int i = 0; pair < pairs; ++i) {
-      __nv_bfloat16* const dst = token.to >= 0 ? out + token.to * 128 : nullptr;
-      uint32_t turned[4][8];                                 // the rotated half of a key
-      if (dst && !value) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.m.k_pages) + token.from * (RANK + LATENT_ROPE) + RANK);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint4 u = src[j];
-          uint32_t* w = &turned[j / 2][4 * (j % 2)];
-          w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-        }
-      }
-      pair = next_of(pair + groups, token);
-      wait_for(&sh.acc_full[i & 1], (i / 2) & 1, &sh.dead);
+    const auto done_with = [&](int i) {
       __syncwarp();
-      tc::tc_fence_after();
-#pragma unroll 1
-      for (int c = 0; c < (value ? 4 : 2); ++c) {
-        float v[32];
-        __syncwarp();                                        // whole warps before a collective load
-        tc::tmem_ld32(tmem + 256 * (i & 1) + (value ? LATENT_KEY : 0) + 32 * c + lanes, v);
-        if (!dst) continue;
+      if (lane == 0) tc::mbar_arrive1(&sh.info_empty[i % INFOS]);
+    };
+    Info info;
+    if (warp == 8) {
+      // ---------------------------------------------------------- products
+      wait_for(&sh.w_full, 0, &sh.dead);
+      int index = 0;
+      for (int i = 0; info_of(i, info); ++i) {
+        done_with(i);
+        if (i >= 2) wait_for(&sh.acc_empty[i & 1], (i / 2 - 1) & 1, &sh.dead);
+        for (int c = 0; c < C::CHUNKS; ++c, ++index) {
+          const int slot = index % C::STAGES;
+          wait_for(&sh.full[slot], (index / C::STAGES) & 1, &sh.dead);
+          tc::tc_fence_after();
+          if (!__any_sync(0xffffffffu, tc::block_dead(tc::su32(&sh.dead))) && tc::elect_one()) {
+            const uint32_t x = tc::su32(ring + slot * STAGE), w = tc::su32(maps + c * CHUNK);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          uint32_t w[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * j + 2 * e], v[16 * j + 2 * e + 1]);
-            w[e] = *reinterpret_cast<const uint32_t*>(&b);
+            for (int k = 0; k < 4; ++k)
+              tc::mma_f16(tmem + 256 * (i & 1), tc::sw128_desc(x + 32 * k), tc::sw128_desc(w + 32 * k), C::IDESC, c | k);
+            tc::mma_commit(&sh.empty[slot]);
+            if (c == C::CHUNKS - 1) tc::mma_commit(&sh.acc_full[i & 1]);
           }
-          put16(dst + 32 * c + 16 * j, w, whole);
+          __syncwarp();
         }
       }
-      __syncwarp();
-      tc::tc_fence_before();
-      if (lane == 0) tc::mbar_arrive1(&sh.acc_empty[i & 1]);
-      if (dst && !value)
+    } else {
+      // ---------------------------------------------------------- keys (warps 0-3) or values of 32 tokens: lane (g, c) has
+      // tokens g, g + 8, .. and of each 32 products the 8 from 8 c on
+      const bool value = warp >= 4;
+      const int g = lane / 4, c = lane % 4, shift = 31 - __clz(a.m.page_tokens), to_shift = 31 - __clz(a.to.page_tokens);
+      __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(value ? a.to.v_pages : a.to.k_pages) + 8 * c;
+      const __nv_bfloat16* const pool = static_cast<const __nv_bfloat16*>(a.m.k_pages) + RANK + 8 * c;
+      for (int i = 0; info_of(i, info); ++i) {
+        __nv_bfloat16* dst[4];
+        uint4 turned[4][2];                                  // the rotated half of a key
 #pragma unroll
-        for (int j = 0; j < 4; ++j) put16(dst + LATENT_KEY + 16 * j, turned[j], whole);
+        for (int j = 0; j < 4; ++j) {
+          const int y = 32 * (warp % 4) + 8 * j + g, t = info.t0 + y;
+          const int from = sh.info[i % INFOS].from[y >> shift], to = sh.info[i % INFOS].to[y >> to_shift];
+          dst[j] = nullptr;
+          if (t >= info.lo && t < info.hi && from >= 0 && to >= 0) {
+            dst[j] = out + (((long long)to * H + h) * a.to.page_tokens + (t & (a.to.page_tokens - 1))) * 128;
+            if (!value) {
+              const uint4* src = reinterpret_cast<const uint4*>(pool + (((long long)from << shift) + (t & (a.m.page_tokens - 1))) * (RANK + LATENT_ROPE));
+              turned[j][0] = src[0], turned[j][1] = src[4];
+            }
+          }
+        }
+        done_with(i);
+        wait_for(&sh.acc_full[i & 1], (i / 2) & 1, &sh.dead);
+        __syncwarp();
+        tc::tc_fence_after();
+#pragma unroll 1
+        for (int x = 0; x < (value ? 4 : 2); ++x)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {                      // 16 lanes each
+            float v[16];
+            __syncwarp();                                    // whole warps before a collective load
+            tmem_ld16x32(tmem + 256 * (i & 1) + (value ? LATENT_KEY : 0) + 32 * x + ((uint32_t)(32 * (warp % 4) + 16 * y) << 16), v);
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+              if (dst[2 * y + z])
+                *reinterpret_cast<uint4*>(dst[2 * y + z] + 32 * x) =
+                    make_uint4(pair_of(v[2 * z], v[2 * z + 1]), pair_of(v[4 + 2 * z], v[5 + 2 * z]), pair_of(v[8 + 2 * z], v[9 + 2 * z]),
+                               pair_of(v[12 + 2 * z], v[13 + 2 * z]));
+          }
+        __syncwarp();
+        tc::tc_fence_before();
+        if (lane == 0) tc::mbar_arrive1(&sh.acc_empty[i & 1]);
+        if (!value)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (dst[j]) {
+              uint4* p = reinterpret_cast<uint4*>(dst[j] + LATENT_KEY);
+              p[0] = turned[j][0], p[4] = turned[j][1];
+            }
+      }
     }
   }
   tc::tc_fence_before();
@@ -240,17 +272,24 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
 template <int RANK>
 cudaError_t launch_tiles(const LatentExpandArgs& a, cudaStream_t st) {
   using C = Cfg<RANK>;
-  CUtensorMap x, k, v;
-  if (!latent_map(&x, a.m, a.m.page_tokens) || !map_of(&k, a.w_k, (long long)a.m.n_head * LATENT_KEY, RANK, LATENT_KEY) ||
-      !map_of(&v, a.w_v, (long long)a.m.n_head * LATENT_VALUE, RANK, LATENT_VALUE))
-    return cudaErrorInvalidValue;
+  CUtensorMap map;
+  if (!latent_map(&map, a.m, a.m.page_tokens)) return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = allow_smem(latent_expand_tiles_kernel<RANK>, C::SMEM, done);
   if (e != cudaSuccess) return e;
   const int pairs = a.m.n_seq * (a.max_new / TM + 2);        // a range may begin and end within a tile
   const int groups = std::max(1, std::min(pairs, 152 / a.to.n_kv_head));
-  latent_expand_tiles_kernel<RANK><<<groups * a.to.n_kv_head, TILE_THREADS, C::SMEM, st>>>(a, x, k, v, pairs, groups);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // it waits for the kernels before it itself
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  cfg.stream = st;
+  cfg.gridDim = groups * a.to.n_kv_head;
+  cfg.blockDim = TILE_THREADS;
+  cfg.dynamicSmemBytes = C::SMEM;
+  return cudaLaunchKernelEx(&cfg, latent_expand_tiles_kernel<RANK>, a, map, pairs, groups);
 }
 
 // ---------------------------------------------------------------- fp32

@@ -48,9 +48,6 @@ bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows) {
   return rows_map(map, m.format, m.k_pages, m.head_dim + LATENT_ROPE, (cuuint64_t)m.n_pages * m.page_tokens, box_rows);
 }
 
-bool map_of(CUtensorMap* map, const void* p, long long rows, int width, int box_rows) {
-  return rows_map(map, EVO_CACHE_BF16, p, width, rows, box_rows);
-}
 
 }  // namespace evo
 

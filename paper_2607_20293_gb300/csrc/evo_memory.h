@@ -106,8 +106,6 @@ cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st);   
 bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows);
 // the same of a latent memory's pages, a row a token
 bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows);
-// of bf16 rows [rows][width]
-bool map_of(CUtensorMap* map, const void* p, long long rows, int width, int box_rows);
 
 // lets a kernel have this much dynamic shared memory; `done`: a bit for each device where it has it
 template <typename K>
