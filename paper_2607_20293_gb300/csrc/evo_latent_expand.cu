@@ -6,7 +6,7 @@
 // bf16, on tcgen05: a block has one head's 192 products (its maps stay in shared memory: 48 to 192 KB) and takes
 // tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  Warp 9 looks tiles and
 // pages up, for all, and brings the latents, warp 8 issues the products into one of two accumulators, warps
-// 0-7 empty the other: four warps the keys, four the values.  The output is 512 bytes a (token, head) against 2 rank
+// 0-7 empty the other, 96 of the products each.  The output is 512 bytes a (token, head) against 2 rank
 // that are read, mostly from L2, so the writes bound the kernel, and have to leave as whole lines: accumulators are read
 // 16 tokens by 256 bits, four lanes a token, and the maps' rows stand in shared memory in the order that gives
 // each of these lanes 8 products of its own in a row (a token a lane and 32 bytes a store were 32 lines an
@@ -122,41 +122,61 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
     // The block's tiles: of pairs (tile, sequence), sequences first, every groups-th.  Tiles start at multiples of 128
     // tokens, so that pages fit them
     const int page_tokens = a.m.page_tokens, to_tokens = a.to.page_tokens, box = min(page_tokens, TM);
+    const int l = lane % 8, size = lane < 8 ? page_tokens : to_tokens;   // lanes 0 .. 7: the latents' pages; 8 .. 15: the other memory's
     int index = 0, i = 0;
-    for (int pair = blockIdx.x / H;; pair += groups) {
-      const bool more = pair < pairs;
-      const int n = more ? pair % a.m.n_seq : -1;
-      int2 range = make_int2(0, 0);
-      if (more) range = token_range(a, n);
-      const int t0 = range.x / TM * TM + (more ? pair / a.m.n_seq * TM : 0);
-      if (more && t0 >= range.y) continue;
+    const auto publish = [&](int n, int t0, int lo, int hi, int page) {
       Info& info = sh.info[i % INFOS];
-      if (i >= INFOS && !__all_sync(0xffffffffu, wait_for(&sh.info_empty[i % INFOS], (i / INFOS - 1) & 1, &sh.dead))) break;
-      // lanes 0 .. 7: the latents' pages; 8 .. 15: the other memory's
-      const int l = lane % 8, size = lane < 8 ? page_tokens : to_tokens, t = t0 + l * size;
-      int page = -1;
-      if (more && lane < 16 && l * size < TM && t + size > range.x && t < range.y)
-        page = page_or_none(lane < 8 ? a.m : a.to, a.m.status, n, t / size);
+      if (i >= INFOS && !__all_sync(0xffffffffu, wait_for(&sh.info_empty[i % INFOS], (i / INFOS - 1) & 1, &sh.dead))) return;
       if (lane < 8) info.from[l] = page;
       else if (lane < 16) info.to[l] = page;
-      if (lane == 0) info.n = n, info.t0 = t0, info.lo = range.x, info.hi = range.y;
+      if (lane == 0) info.n = n, info.t0 = t0, info.lo = lo, info.hi = hi;
       __syncwarp();
       if (lane == 0) tc::mbar_arrive1(&sh.info_full[i % INFOS]);
-      if (!more) break;
       ++i;
-      const bool on = lane < 8 && page >= 0;
-      const int copies = __popc(__ballot_sync(0xffffffffu, on));
-      for (int c = 0; c < C::CHUNKS; ++c, ++index) {
-        const int slot = index % C::STAGES, use = index / C::STAGES;
-        if (!__all_sync(0xffffffffu, use == 0 || wait_for(&sh.empty[slot], (use - 1) & 1, &sh.dead))) continue;
-        if (lane == 0) tc::mbar_expect_tx(&sh.full[slot], copies * box * 128);
-        __syncwarp();
-        if (on)
-          tile_load(tc::su32(ring + slot * STAGE + lane * box * 128), &map, 64 * c, page * page_tokens + t % page_tokens,
-                    tc::su32(&sh.full[slot]));
-        __syncwarp();
+    };
+    // a lane a tile: 32 ranges are looked up at once, and pages a tile ahead of their use
+    for (long long pair0 = blockIdx.x / H; pair0 < pairs; pair0 += 32ll * groups) {
+      const long long pair = pair0 + (long long)lane * groups;
+      int2 range = make_int2(0, 0);
+      int my_t0 = 0;
+      if (pair < pairs) {
+        range = token_range(a, (int)(pair % a.m.n_seq));
+        my_t0 = range.x / TM * TM + (int)(pair / a.m.n_seq) * TM;
+      }
+      uint32_t left = __ballot_sync(0xffffffffu, my_t0 < range.y);
+      struct Ahead { int n, t0, lo, hi, entry; bool on; } next;
+      const auto look_up = [&] {                             // the entry is looked at when the tile's turn comes
+        const int from = left ? __ffs(left) - 1 : 0;
+        next.n = (int)((pair0 + (long long)from * groups) % a.m.n_seq);
+        next.t0 = __shfl_sync(0xffffffffu, my_t0, from);
+        next.lo = __shfl_sync(0xffffffffu, range.x, from);
+        next.hi = __shfl_sync(0xffffffffu, range.y, from);
+        const int t = next.t0 + l * size;
+        next.on = left && lane < 16 && l * size < TM && t + size > next.lo && t < next.hi;
+        const evo_memory& m = lane < 8 ? a.m : a.to;
+        next.entry = next.on ? m.table[(long long)next.n * m.max_pages + t / size] : 0;
+      };
+      look_up();
+      while (left) {
+        const Ahead now = next;
+        left &= left - 1;
+        if (left) look_up();
+        int page = now.on ? now.entry : -1;
+        if (now.on && (unsigned)page >= (unsigned)(lane < 8 ? a.m.n_pages : a.to.n_pages)) page = -1, memory_fault(a.m);
+        publish(now.n, now.t0, now.lo, now.hi, page);
+        const bool on = lane < 8 && page >= 0;
+        const int copies = __popc(__ballot_sync(0xffffffffu, on)), row = page * page_tokens + ((now.t0 + l * size) & (page_tokens - 1));
+        for (int c = 0; c < C::CHUNKS; ++c, ++index) {
+          const int slot = index % C::STAGES, use = index / C::STAGES;
+          if (!__all_sync(0xffffffffu, use == 0 || wait_for(&sh.empty[slot], (use - 1) & 1, &sh.dead))) continue;
+          if (lane == 0) tc::mbar_expect_tx(&sh.full[slot], copies * box * 128);
+          __syncwarp();
+          if (on) tile_load(tc::su32(ring + slot * STAGE + lane * box * 128), &map, 64 * c, row, tc::su32(&sh.full[slot]));
+          __syncwarp();
+        }
       }
     }
+    publish(-1, 0, 0, 0, -1);
   } else {
     // the head's maps, 16 bytes a copy
     constexpr int PIECES = RANK / 8;
@@ -206,24 +226,26 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
         }
       }
     } else {
-      // ---------------------------------------------------------- keys (warps 0-3) or values of 32 tokens: lane (g, c) has
-      // tokens g, g + 8, .. and of each 32 products the 8 from 8 c on
-      const bool value = warp >= 4;
+      // ---------------------------------------------------------- 96 columns of 32 tokens: warps 0-3 the key and a quarter of
+      // the value, and the rotated half of the key; warps 4-7 the rest.  Lane (g, c) has tokens g, g + 8, .. and of
+      // each 32 products the 8 from 8 c on
+      const bool second = warp >= 4;
       const int g = lane / 4, c = lane % 4, shift = 31 - __clz(a.m.page_tokens), to_shift = 31 - __clz(a.to.page_tokens);
-      __nv_bfloat16* const out = static_cast<__nv_bfloat16*>(value ? a.to.v_pages : a.to.k_pages) + 8 * c;
+      __nv_bfloat16* const keys = static_cast<__nv_bfloat16*>(a.to.k_pages) + 8 * c;
+      __nv_bfloat16* const values = static_cast<__nv_bfloat16*>(a.to.v_pages) + 8 * c;
       const __nv_bfloat16* const pool = static_cast<const __nv_bfloat16*>(a.m.k_pages) + RANK + 8 * c;
       for (int i = 0; info_of(i, info); ++i) {
-        __nv_bfloat16* dst[4];
+        long long to[4];                                     // a token's row of either pool, -1: none
         uint4 turned[4][2];                                  // the rotated half of a key
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int y = 32 * (warp % 4) + 8 * j + g, t = info.t0 + y;
-          const int from = sh.info[i % INFOS].from[y >> shift], to = sh.info[i % INFOS].to[y >> to_shift];
-          dst[j] = nullptr;
-          if (t >= info.lo && t < info.hi && from >= 0 && to >= 0) {
-            dst[j] = out + (((long long)to * H + h) * a.to.page_tokens + (t & (a.to.page_tokens - 1))) * 128;
-            if (!value) {
-              const uint4* src = reinterpret_cast<const uint4*>(pool + (((long long)from << shift) + (t & (a.m.page_tokens - 1))) * (RANK + LATENT_ROPE));
+          const int p = sh.info[i % INFOS].from[y >> shift], q = sh.info[i % INFOS].to[y >> to_shift];
+          to[j] = -1;
+          if (t >= info.lo && t < info.hi && p >= 0 && q >= 0) {
+            to[j] = ((((long long)q * H + h) << to_shift) + (t & (a.to.page_tokens - 1))) * 128;
+            if (!second) {
+              const uint4* src = reinterpret_cast<const uint4*>(pool + (((long long)p << shift) + (t & (a.m.page_tokens - 1))) * (RANK + LATENT_ROPE));
               turned[j][0] = src[0], turned[j][1] = src[4];
             }
           }
@@ -232,28 +254,30 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
         wait_for(&sh.acc_full[i & 1], (i / 2) & 1, &sh.dead);
         __syncwarp();
         tc::tc_fence_after();
-#pragma unroll 1
-        for (int x = 0; x < (value ? 4 : 2); ++x)
+#pragma unroll
+        for (int x = 0; x < 3; ++x) {
+          __nv_bfloat16* const out = second ? values + 32 * (x + 1) : x < 2 ? keys + 32 * x : values;
 #pragma unroll
           for (int y = 0; y < 2; ++y) {                      // 16 lanes each
             float v[16];
             __syncwarp();                                    // whole warps before a collective load
-            tmem_ld16x32(tmem + 256 * (i & 1) + (value ? LATENT_KEY : 0) + 32 * x + ((uint32_t)(32 * (warp % 4) + 16 * y) << 16), v);
+            tmem_ld16x32(tmem + 256 * (i & 1) + (second ? 96 : 0) + 32 * x + ((uint32_t)(32 * (warp % 4) + 16 * y) << 16), v);
 #pragma unroll
             for (int z = 0; z < 2; ++z)
-              if (dst[2 * y + z])
-                *reinterpret_cast<uint4*>(dst[2 * y + z] + 32 * x) =
+              if (to[2 * y + z] >= 0)
+                *reinterpret_cast<uint4*>(out + to[2 * y + z]) =
                     make_uint4(pair_of(v[2 * z], v[2 * z + 1]), pair_of(v[4 + 2 * z], v[5 + 2 * z]), pair_of(v[8 + 2 * z], v[9 + 2 * z]),
                                pair_of(v[12 + 2 * z], v[13 + 2 * z]));
           }
+        }
         __syncwarp();
         tc::tc_fence_before();
         if (lane == 0) tc::mbar_arrive1(&sh.acc_empty[i & 1]);
-        if (!value)
+        if (!second)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (dst[j]) {
-              uint4* p = reinterpret_cast<uint4*>(dst[j] + LATENT_KEY);
+            if (to[j] >= 0) {
+              uint4* p = reinterpret_cast<uint4*>(keys + to[j] + LATENT_KEY);
               p[0] = turned[j][0], p[4] = turned[j][1];
             }
       }
