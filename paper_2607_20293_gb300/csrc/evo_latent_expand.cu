@@ -4,9 +4,10 @@
 // written to the token's page of the other memory.
 //
 // bf16, on tcgen05: a block has one head's 192 products (its maps stay in shared memory: 48 to 192 KB) and takes
-// tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  Warp 9 looks tiles and
-// pages up, for all, and brings the latents, warp 8 issues the products into one of two accumulators, warps
-// 0-7 empty the other, 96 of the products each.  The output is 512 bytes a (token, head) against 2 rank
+// tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  The last warp looks tiles
+// and pages up, for all, and brings the latents, the one before it issues the products into one of two accumulators,
+// and eight warps each empty one of these, so that what a warp waits for (a tile's pages, tensor memory, room for
+// its stores) is hidden by the others.  The output is 512 bytes a (token, head) against 2 rank
 // that are read, mostly from L2, so the writes bound the kernel, and have to leave as whole lines: accumulators are read
 // 16 tokens by 256 bits, four lanes a token, and the maps' rows stand in shared memory in the order that gives
 // each of these lanes 8 products of its own in a row (a token a lane and 32 bytes a store were 32 lines an
@@ -49,7 +50,7 @@ __device__ __forceinline__ void put2(float* p, float2 v) { *reinterpret_cast<flo
 
 // ---------------------------------------------------------------- bf16
 
-constexpr int TM = 128, TILE_THREADS = 320, STAGE = TM * 128, CHUNK = BN * 128;   // bytes of 64 dimensions of the tokens, of the maps
+constexpr int TM = 128, WRITERS = 16, TILE_THREADS = 32 * (WRITERS + 2), STAGE = TM * 128, CHUNK = BN * 128;   // bytes of 64 dimensions of the tokens, of the maps
 template <int RANK>
 struct Cfg {
   static constexpr int CHUNKS = RANK / 64, W = CHUNKS * CHUNK;
@@ -72,6 +73,12 @@ struct Shared {
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* dead) {
   const uint32_t b = tc::su32(bar);
   return tc::mbar_test(b, parity) || wait_live(b, parity, tc::su32(dead));
+}
+// a wait behind a first test that failed
+__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) { wait_live(bar, parity, dead); }
+__device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // 32 columns of 16 lanes: of column 8 k + 2 c + e, lane (g, c) gets that of TMEM lane g in v[4 k + e] and of g + 8 in v[4 k + 2 + e]
 __device__ __forceinline__ void tmem_ld16x32(uint32_t taddr, float (&v)[16]) {
@@ -105,9 +112,9 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
   if (warp == 0) tc::tmem_alloc(&sh.tmem, 512);
   if (tid == 32) {
     for (int i = 0; i < C::STAGES; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], 1);
-    tc::mbar_init1(&sh.w_full, 9);                           // a warp each
-    for (int i = 0; i < 2; ++i) tc::mbar_init1(&sh.acc_full[i], 1), tc::mbar_init1(&sh.acc_empty[i], 8);
-    for (int i = 0; i < INFOS; ++i) tc::mbar_init1(&sh.info_full[i], 1), tc::mbar_init1(&sh.info_empty[i], 9);
+    tc::mbar_init1(&sh.w_full, WRITERS + 1);                 // a warp each
+    for (int i = 0; i < 2; ++i) tc::mbar_init1(&sh.acc_full[i], 1), tc::mbar_init1(&sh.acc_empty[i], WRITERS / 2);
+    for (int i = 0; i < INFOS; ++i) tc::mbar_init1(&sh.info_full[i], 1), tc::mbar_init1(&sh.info_empty[i], WRITERS / 2 + 1);
     sh.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -117,7 +124,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
   const uint32_t tmem = sh.tmem;
   tc::pdl_wait();                                            // what earlier kernels wrote is there
 
-  if (warp == 9) {
+  if (warp == WRITERS + 1) {
     // ------------------------------------------------------------ tiles, pages and copies
     // The block's tiles: of pairs (tile, sequence), sequences first, every groups-th.  Tiles start at multiples of 128
     // tokens, so that pages fit them
@@ -176,6 +183,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
         }
       }
     }
+    publish(-1, 0, 0, 0, -1);                                // no more, for the writers of even and of odd tiles
     publish(-1, 0, 0, 0, -1);
   } else {
     // the head's maps, 16 bytes a copy
@@ -203,38 +211,47 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
       if (lane == 0) tc::mbar_arrive1(&sh.info_empty[i % INFOS]);
     };
     Info info;
-    if (warp == 8) {
+    if (warp == WRITERS) {
       // ---------------------------------------------------------- products
-      wait_for(&sh.w_full, 0, &sh.dead);
-      int index = 0;
+      // (uniform over the warp and known to the compiler to be: descriptors stay in uniform registers)
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), dead = tc::su32(&sh.dead), full = tc::su32(sh.full), empty = tc::su32(sh.empty);
+      const uint64_t desc = tc::sw128_desc(0);
+      const uint32_t hi = (uint32_t)(desc >> 32), x0 = (uint32_t)desc + (tc::su32(ring) >> 4), w = (uint32_t)desc + (tc::su32(maps) >> 4);
+      const auto wait = [&](uint32_t bar, uint32_t parity) {
+        if (!tc::mbar_test(bar, parity)) wait_slow(bar, parity, dead);
+      };
+      wait(tc::su32(&sh.w_full), 0);
+      uint32_t slot = 0, phase = 0;
       for (int i = 0; info_of(i, info); ++i) {
         done_with(i);
-        if (i >= 2) wait_for(&sh.acc_empty[i & 1], (i / 2 - 1) & 1, &sh.dead);
-        for (int c = 0; c < C::CHUNKS; ++c, ++index) {
-          const int slot = index % C::STAGES;
-          wait_for(&sh.full[slot], (index / C::STAGES) & 1, &sh.dead);
-          tc::tc_fence_after();
-          if (!__any_sync(0xffffffffu, tc::block_dead(tc::su32(&sh.dead))) && tc::elect_one()) {
-            const uint32_t x = tc::su32(ring + slot * STAGE), w = tc::su32(maps + c * CHUNK);
+        if (i >= 2) wait(tc::su32(&sh.acc_empty[i & 1]), (i / 2 - 1) & 1);
+        if (__any_sync(0xffffffffu, tc::block_dead(dead))) break;
+        const uint32_t d = tm + 256 * (i & 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              tc::mma_f16(tmem + 256 * (i & 1), tc::sw128_desc(x + 32 * k), tc::sw128_desc(w + 32 * k), C::IDESC, c | k);
-            tc::mma_commit(&sh.empty[slot]);
-            if (c == C::CHUNKS - 1) tc::mma_commit(&sh.acc_full[i & 1]);
+        for (uint32_t c = 0; c < C::CHUNKS; ++c) {
+          wait(full + 8 * slot, phase);
+          tc::tc_fence_after();
+          const uint32_t x = x0 + slot * (STAGE >> 4);
+          if (tc::elect_one()) {
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k)
+              tc::mma_f16(d, desc64(x + 2 * k, hi), desc64(w + c * (CHUNK >> 4) + 2 * k, hi), C::IDESC, c | k);
+            commit(empty + 8 * slot);
+            if (c == C::CHUNKS - 1) commit(tc::su32(&sh.acc_full[i & 1]));
           }
-          __syncwarp();
+          if (++slot == C::STAGES) slot = 0, phase ^= 1;
         }
       }
     } else {
       // ---------------------------------------------------------- 96 columns of 32 tokens: warps 0-3 the key and a quarter of
-      // the value, and the rotated half of the key; warps 4-7 the rest.  Lane (g, c) has tokens g, g + 8, .. and of
-      // each 32 products the 8 from 8 c on
-      const bool second = warp >= 4;
+      // the value, and the rotated half of the key; warps 4-7 the rest; warps 8-15 the same of every second tile.
+      // Lane (g, c) has tokens g, g + 8, .. and of each 32 products the 8 from 8 c on
+      const bool second = warp / 4 % 2;
       const int g = lane / 4, c = lane % 4, shift = 31 - __clz(a.m.page_tokens), to_shift = 31 - __clz(a.to.page_tokens);
       __nv_bfloat16* const keys = static_cast<__nv_bfloat16*>(a.to.k_pages) + 8 * c;
       __nv_bfloat16* const values = static_cast<__nv_bfloat16*>(a.to.v_pages) + 8 * c;
       const __nv_bfloat16* const pool = static_cast<const __nv_bfloat16*>(a.m.k_pages) + RANK + 8 * c;
-      for (int i = 0; info_of(i, info); ++i) {
+      for (int i = warp / 8; info_of(i, info); i += 2) {
         long long to[4];                                     // a token's row of either pool, -1: none
         uint4 turned[4][2];                                  // the rotated half of a key
 #pragma unroll
