@@ -21,7 +21,7 @@ OUT_DEBUG = os.path.join(HERE, "libevo_debug.so")
 BUILD = os.path.join(ROOT, "_build")
 SOURCES = ["evo_api.cu", "evo_job.cu", "evo_loop_s01.cu", "evo_loop_s23.cu", "evo_loop_s45.cu", "evo_loop_f32.cu", "evo_wide.cu", "evo_tile.cu", "evo_redundancy.cu", "evo_search.cpp",
            "evo_cache.cu", "evo_append.cu", "evo_attend.cu", "evo_attend_f32.cu", "evo_attend_rows.cu", "evo_attend_tiles.cu",
-           "evo_latent.cu", "evo_latent_f32.cu", "evo_latent_tiles.cu", "evo_latent_expand.cu", "evo_memory.cu"]
+           "evo_latent.cu", "evo_latent_f32.cu", "evo_latent_tiles.cu", "evo_latent_wide.cu", "evo_latent_expand.cu", "evo_memory.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2", "-Xcompiler", "-ffp-contract=off",
          "-I", os.path.join(ROOT, "include")]

@@ -91,6 +91,7 @@ LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, 
 cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
 void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int keys);    // evo_latent_tiles.cu
 cudaError_t launch_latent_tiles(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
+cudaError_t launch_latent_wide(const AttendArgs& a, const LatentPlan& p, cudaStream_t st);   // 128 rows: evo_latent_wide.cu
 int latent_f32_rows(int rank, long long all, int n_seq);   // rows of a tile of fp32 rows, evo_latent_f32.cu
 cudaError_t launch_latent_f32(const AttendArgs& a, int tile_rows, cudaStream_t st);
 struct LatentExpandArgs {
