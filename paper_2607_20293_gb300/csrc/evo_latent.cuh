@@ -43,6 +43,7 @@ struct Segment {
 
 struct Run {
   int items, split;                                // split: blocks take equal runs of tiles; else whole items, every gridDim-th
+  int flat;                                        // queries lie row behind row: an item's come by tiled copies
   int4* meta;                                      // of each block from which an item goes on to others: its piece's slot (else -1), the last block, the item
 };
 
@@ -292,6 +293,40 @@ __device__ __forceinline__ void bring_tiles(const AttendArgs& a, W& walk, const 
   }
 }
 
+// An item's queries to shared memory, 64 of their dimensions behind one another, 128-byte swizzle.  Flat ones are one
+// lane's tiled copies (rows behind the sequence's are others', and nobody's result), others all threads' asynchronous ones,
+// which queries_there waits for.
+template <int RANK, int N, int SOFTMAX>
+__device__ __forceinline__ void bring_queries(const AttendArgs& a, const Run& run, const CUtensorMap& map, const Item& x, uint8_t* mem, Roles& sh) {
+  const int tid = threadIdx.x;
+  if (run.flat) {
+    if (tid == 0) {
+      tc::mbar_expect_tx(&sh.q_full, N * (RANK + LATENT_ROPE) * 2);
+      const int row = x.t.first * a.group + x.r0;
+      for (int c = 0; c < (RANK + LATENT_ROPE) / 64; ++c) tile_load(tc::su32(mem + c * (N * 128)), &map, 64 * c, row, tc::su32(&sh.q_full));
+    }
+    return;
+  }
+  constexpr int PIECES = (RANK + LATENT_ROPE) / 8;
+#pragma unroll 2
+  for (int i = tid; i < N * PIECES; i += SOFTMAX) {
+    const int r = i / PIECES, j = i % PIECES, R = x.r0 + r, on = R < x.rows ? 16 : 0, token = on ? R / a.group : 0;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (long long)(x.t.first + token) * a.ldq +
+                               (long long)(on ? R - token * a.group : 0) * (RANK + LATENT_ROPE) + 8 * j;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                     tc::su32(mem + (j / 8) * (N * 128) + r * 128 + ((j % 8 ^ (r & 7)) << 4))),
+                 "l"(src), "r"(on)
+                 : "memory");
+  }
+}
+__device__ __forceinline__ void queries_there(const Run& run, Roles& sh) {
+  if (run.flat) return;
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  tc::fence_async_smem();
+  __syncwarp();
+  if (threadIdx.x % 32 == 0) tc::mbar_arrive1(&sh.q_full);
+}
+
 // the block's next item, by the first warp of the softmax for all; shares: an item goes on to further blocks
 template <typename W>
 __device__ __forceinline__ void fill_segment(const AttendArgs& a, const Run& run, const Share& share, W& walk, Segment& q, bool& shares) {
@@ -373,16 +408,55 @@ __global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_
             sum == 0.f ? 0.f : 1.f / sum);
 }
 
+// The same for items of 128 rows, whose pieces are [dimension][row]: a thread a row and 8 dimensions
+template <int RANK>
+__global__ void __launch_bounds__(256) latent_join_wide_kernel(const __grid_constant__ AttendArgs a, const int4* meta) {
+  const int r = threadIdx.x % 128, d = (blockIdx.y * 2 + threadIdx.x / 128) * 8;
+  tc::pdl_wait();
+  const int4 m = meta[blockIdx.x];
+  if (m.x < 0) return;
+  const int n = m.z / a.tiles, pieces = m.y - blockIdx.x + 1;
+  const SeqRows s = seq_rows(a.m, n, a.rows, a.max_new);
+  const int R = m.z % a.tiles * 128 + r;
+  if (R >= s.count * a.group) return;
+  const auto slot = [&](int p) { return (long long)(p == 0 ? m.x : 2 * (blockIdx.x + p)); };
+  float top = -INFINITY, sum = 0.f;
+  for (int p = 0; p < pieces; ++p) top = fmaxf(top, a.ml[slot(p) * 128 + r].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float o[8] = {};
+#pragma unroll 2
+  for (int p = 0; p < pieces; ++p) {
+    const float2 ml = a.ml[slot(p) * 128 + r];
+    const float* part = a.part + (slot(p) * RANK + d) * 128 + r;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = part[e * 128];
+    const float f = ex2_approx(ml.x - ref);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(y[e], f, o[e]);
+  }
+  const float norm = sum == 0.f ? 0.f : 1.f / sum;
+  uint32_t v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[e]) : "f"(o[2 * e + 1] * norm), "f"(o[2 * e] * norm));
+  *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + d) =
+      make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 // launches the kernel of items of N rows, and the join of those that blocks share; both wait for the kernels before
 // them themselves (griddepcontrol.wait)
 template <int RANK, int N, typename K>
 cudaError_t launch_items(K kernel, int threads, int smem, const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
-  CUtensorMap map;
+  CUtensorMap map, queries;
+  const bool flat = a.ldq == (long long)a.m.n_head * (RANK + LATENT_ROPE);
   if (!latent_map(&map, a.m, a.m.page_tokens)) return cudaErrorInvalidValue;
+  queries = map;
+  if (flat && !query_map(&queries, a, N)) return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
   cudaError_t e = allow_smem(kernel, smem, done);
   if (e != cudaSuccess) return e;
-  const Run run{a.m.n_seq * a.tiles, p.splits > 1, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * N)};
+  const Run run{a.m.n_seq * a.tiles, p.splits > 1, flat, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * N)};
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -393,15 +467,21 @@ cudaError_t launch_items(K kernel, int threads, int smem, const AttendArgs& a, c
   cfg.gridDim = p.blocks;
   cfg.blockDim = threads;
   cfg.dynamicSmemBytes = smem;
-  e = cudaLaunchKernelEx(&cfg, kernel, a, map, run);
+  e = cudaLaunchKernelEx(&cfg, kernel, a, map, queries, run);
   if (e != cudaSuccess || !run.split) return e;
-  constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
-  int groups = 1;
-  while (groups < AT_ONCE && groups * 8 * run.items < p.blocks) groups *= 2;
-  cfg.gridDim = dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE);
-  cfg.blockDim = JOIN_THREADS;
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, groups);
+  if constexpr (N == 128) {
+    cfg.gridDim = dim3(p.blocks, RANK / 16);
+    cfg.blockDim = 256;
+    return cudaLaunchKernelEx(&cfg, latent_join_wide_kernel<RANK>, a, (const int4*)run.meta);
+  } else {
+    constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
+    int groups = 1;
+    while (groups < AT_ONCE && groups * 8 * run.items < p.blocks) groups *= 2;
+    cfg.gridDim = dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE);
+    cfg.blockDim = JOIN_THREADS;
+    return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, groups);
+  }
 }
 
 }  // namespace evo

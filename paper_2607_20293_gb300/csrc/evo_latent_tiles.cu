@@ -78,7 +78,8 @@ __device__ __forceinline__ int weight_at(int k, int i) {
 }
 template <int RANK, int N>
 __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
-    latent_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ Run run) {
+    latent_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
+                        const __grid_constant__ CUtensorMap queries, const __grid_constant__ Run run) {
   using C = Cfg<RANK, N>;
   constexpr int PER = C::PER, HC = C::HC, SLOTS = C::SLOTS, PARTS = C::PARTS, SOFTMAX = C::SOFTMAX, THREADS = C::THREADS;
   extern __shared__ uint8_t raw[];
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
   uint8_t* const weights = mem + C::Q;
   uint8_t* const ring = weights + C::P;
   uint8_t* const parts = ring + SLOTS * SLOT;
-  if (tid == 0) fetch_map(&map);
+  if (tid == 0) fetch_map(&map), fetch_map(&queries);
   __syncwarp();                                    // a whole warp's instruction, behind one lane's prefetch
   if (warp == 0) tc::tmem_alloc(&sh.tmem, C::ALLOC);
   if (tid == 32) {
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     for (int i = 0; i < PARTS; ++i) tc::mbar_init1(&sh.part_full[i], 1), tc::mbar_init1(&sh.part_empty[i], 1);
     tc::mbar_init1(&sh.s_full[0], 1), tc::mbar_init1(&sh.s_full[1], 1);
     tc::mbar_init1(&sh.p_full, C::WARPS);          // a warp each
-    tc::mbar_init1(&sh.q_full, C::WARPS);
+    tc::mbar_init1(&sh.q_full, run.flat ? 1 : C::WARPS);
     tc::mbar_init1(&sh.o_full, 1);
     sh.dead = 0;
     sh.item = run.split ? run.items : blockIdx.x;
@@ -206,26 +207,6 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     // the softmax works with a positive factor: the scale's sign goes to the scores
     const float f = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f), far = fminf(LAZY / f, 1e38f);
     const float sign = a.scale_log2 < 0.f ? -1.f : a.scale_log2 == 0.f ? 0.f : 1.f;
-    // an item's queries on their way to shared memory, and there
-    const auto bring_queries = [&](const Item& x) {
-      constexpr int PIECES = (RANK + LATENT_ROPE) / 8;
-#pragma unroll 2
-      for (int i = tid; i < N * PIECES; i += SOFTMAX) {
-        const int r = i / PIECES, j = i % PIECES, R = x.r0 + r, on = R < x.rows ? 16 : 0, token = on ? R / a.group : 0;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + (long long)(x.t.first + token) * a.ldq +
-                                   (long long)(on ? R - token * a.group : 0) * (RANK + LATENT_ROPE) + 8 * j;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                         tc::su32(mem + (j / 8) * (N * 128) + r * 128 + ((j % 8 ^ (r & 7)) << 4))),
-                     "l"(src), "r"(on)
-                     : "memory");
-      }
-    };
-    const auto queries_there = [&] {
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      tc::fence_async_smem();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive1(&sh.q_full);
-    };
     // the first warp looks the next item up for all of them
     bool shares = false;
     const auto look_up = [&](Segment& q) {
@@ -235,11 +216,11 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     };
     float sum[HC];
     look_up(sh.seg[0]);
-    if (sh.seg[0].more && sh.seg[0].n > 0) bring_queries(sh.seg[0].x);
+    if (sh.seg[0].more && sh.seg[0].n > 0) bring_queries<RANK, N, SOFTMAX>(a, run, queries, sh.seg[0].x, mem, sh);
     for (int s = 0; sh.seg[s].more; s ^= 1) {
       const Segment& q = sh.seg[s];
       const Segment& after = sh.seg[s ^ 1];
-      if (q.n > 0) queries_there();
+      if (q.n > 0) queries_there(run, sh);
       look_up(sh.seg[s ^ 1]);
       const Item& x = q.x;
       const Tile& t = x.t;
@@ -377,7 +358,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         if (lane == 0) tc::mbar_arrive1(&sh.p_full);
       }
       // the next item's queries take the place of these, whose scores are all there
-      if (after.more && after.n > 0) bring_queries(after.x);
+      if (after.more && after.n > 0) bring_queries<RANK, N, SOFTMAX>(a, run, queries, after.x, mem, sh);
       if (n > 0) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
       __syncwarp();
       tc::tc_fence_after();
@@ -468,7 +449,7 @@ void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int ke
   p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : all <= 64 ? 64 : 128;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + BK - 1) / BK);
-  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + (p.tile_rows <= 32 ? 3 : p.tile_rows == 64 ? 5 : 9);
+  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + (p.tile_rows <= 32 ? 3 : p.tile_rows == 64 ? 5 : 6);
   const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
   p.splits = split ? 2 : 1;
   p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);

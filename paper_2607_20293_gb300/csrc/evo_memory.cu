@@ -44,6 +44,9 @@ bool rows_map(CUtensorMap* map, int32_t format, const void* rows_at, cuuint64_t 
 bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows) {
   return rows_map(map, m.format, pages, m.head_dim, (cuuint64_t)m.n_pages * m.n_kv_head * m.page_tokens, box_rows);
 }
+bool query_map(CUtensorMap* map, const AttendArgs& a, int box_rows) {
+  return rows_map(map, EVO_CACHE_BF16, a.q, a.m.head_dim + LATENT_ROPE, (cuuint64_t)a.rows * a.m.n_head, box_rows);
+}
 bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows) {
   return rows_map(map, m.format, m.k_pages, m.head_dim + LATENT_ROPE, (cuuint64_t)m.n_pages * m.page_tokens, box_rows);
 }

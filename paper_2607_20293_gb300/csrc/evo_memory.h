@@ -107,6 +107,8 @@ cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st);   
 bool page_map(CUtensorMap* map, const evo_memory& m, const void* pages, int box_rows);
 // the same of a latent memory's pages, a row a token
 bool latent_map(CUtensorMap* map, const evo_memory& m, int box_rows);
+// of a call's bf16 queries whose rows lie behind one another, a row a (token, head)
+bool query_map(CUtensorMap* map, const AttendArgs& a, int box_rows);
 
 // lets a kernel have this much dynamic shared memory; `done`: a bit for each device where it has it
 template <typename K>
