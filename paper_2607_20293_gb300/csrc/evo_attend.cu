@@ -495,7 +495,7 @@ cudaError_t launch_f32(const AttendArgs& a, cudaStream_t st) {
 }
 
 template <typename T, int D>
-cudaError_t launch_join_as(const AttendArgs& a, cudaStream_t st) {
+cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
   constexpr int AT_ONCE = JOIN_THREADS / (D / 4);
   const long long outputs = (long long)a.rows * a.m.n_head;
   int groups = 1;                                  // 16 pieces a group, while the GPU has threads to spare
@@ -647,17 +647,8 @@ cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cud
   else
     e = launch_attend_tiles(a, st);
   if (e != cudaSuccess || parts == 1) return e;
-  return launch_join(a, st);
-}
-
-cudaError_t launch_join(const AttendArgs& a, cudaStream_t st) {
-  const bool f32 = a.m.dtype == EVO_DTYPE_F32;
-  switch (a.m.head_dim) {
-    case 64: return f32 ? launch_join_as<float, 64>(a, st) : launch_join_as<__nv_bfloat16, 64>(a, st);
-    case 128: return f32 ? launch_join_as<float, 128>(a, st) : launch_join_as<__nv_bfloat16, 128>(a, st);
-    case 256: return f32 ? launch_join_as<float, 256>(a, st) : launch_join_as<__nv_bfloat16, 256>(a, st);
-    default: return f32 ? launch_join_as<float, 512>(a, st) : launch_join_as<__nv_bfloat16, 512>(a, st);
-  }
+  if (a.m.dtype == EVO_DTYPE_F32) return d64 ? launch_join<float, 64>(a, st) : launch_join<float, 128>(a, st);
+  return d64 ? launch_join<__nv_bfloat16, 64>(a, st) : launch_join<__nv_bfloat16, 128>(a, st);
 }
 
 }  // namespace evo

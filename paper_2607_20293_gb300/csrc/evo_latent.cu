@@ -9,6 +9,7 @@
 // and key part, or some of its queries: 4 lanes a head, each the 8 values at 8 l and the 8 at 32 + 8 l,
 // so that the rotation needs no exchange.
 #include <algorithm>
+#include <climits>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -153,34 +154,30 @@ LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, 
   const long long all = (long long)max_new * m.n_head;
   const int moves = causal ? std::min(max_new, 128 / m.n_head + 1) : 0;
   const int keys = window ? (int)std::min<long long>(max_len, (long long)window + moves) : max_len;
-  p.cluster = 1;
-  if (m.dtype != EVO_DTYPE_F32) {
-    plan_latent_tiles(p, m, all, keys);
-    return p;
-  }
-  p.tile_rows = latent_f32_rows(m.head_dim, all, m.n_seq);
+  p.tile_rows = m.dtype == EVO_DTYPE_F32 ? latent_f32_rows(m.head_dim, all, m.n_seq)
+                : all <= 16              ? 16
+                : all <= 32 || m.head_dim == 512 ? 32
+                : all <= 64              ? 64
+                                         : 128;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
-  const long long blocks = (long long)m.n_seq * p.tiles;
-  p.splits = 1;
-  double least = 1e300;
-  for (int s = 1; s <= std::min(152, std::max(1, keys / 64)); ++s) {
-    const double each = (double)((blocks * s + 151) / 152), cost = each * ((keys + s - 1) / s + (s == 1 ? 200 : 350));
-    if (cost < least) least = cost, p.splits = s;
-  }
-  p.scratch = p.splits == 1 ? 0 : (size_t)p.splits * rows * m.n_head * ((size_t)m.head_dim + 2) * sizeof(float);
+  // Items go to the blocks whole where that takes little longer, in tiles of 128 tokens, than equal runs, their
+  // pieces and the join of these
+  constexpr int SMS = 152, MOST_ITEMS = 2048;      // items that a block counts
+  const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + 127) / 128);
+  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + (p.tile_rows <= 32 ? 3 : p.tile_rows == 64 ? 5 : 6);
+  const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
+  p.splits = split ? 2 : 1;
+  p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
+  // sums, and maximum and sum of weights, of two pieces a block; where a block's last item goes on
+  p.scratch = split ? (size_t)p.blocks * (2 * p.tile_rows * ((size_t)m.head_dim + 2) * sizeof(float) + sizeof(int4)) : 0;
   return p;
 }
 
 cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st) {
   a.tiles = p.tiles;
-  a.splits = p.splits;
-  a.cluster = p.cluster;
-  if (a.m.dtype != EVO_DTYPE_F32) return launch_latent_tiles(a, p, scratch, st);
-  const int parts = p.splits / p.cluster;
   a.part = static_cast<float*>(scratch);
-  a.ml = reinterpret_cast<float2*>(a.part + (size_t)parts * a.rows * a.m.n_head * a.m.head_dim);
-  const cudaError_t e = launch_latent_f32(a, p.tile_rows, st);
-  return e != cudaSuccess || parts == 1 ? e : launch_join(a, st);
+  a.ml = reinterpret_cast<float2*>(a.part + (size_t)2 * p.blocks * p.tile_rows * a.m.head_dim);
+  return a.m.dtype == EVO_DTYPE_F32 ? launch_latent_f32(a, p, st) : p.tile_rows == 128 ? launch_latent_wide(a, p, st) : launch_latent_tiles(a, p, st);
 }
 
 }  // namespace evo

@@ -20,7 +20,7 @@
 namespace evo {
 
 constexpr int BK = 128;                            // tokens of a tile
-constexpr int SMS = 152, MOST_ITEMS = 2048;        // items that a block counts
+constexpr int SMS = 152;
 constexpr int SLOT = BK * 256, HALF = BK * 128;    // bytes of 128 and of 64 dimensions of a tile
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
 constexpr float NONE = -3.402823466e38f;           // the reference of a row that has seen nothing
@@ -352,7 +352,7 @@ __device__ __forceinline__ void fill_segment(const AttendArgs& a, const Run& run
 // first of each block behind it up to the last.  RANK / 4 lanes a row, or several such groups that share its pieces
 // (few rows of many pieces would else wait out one load after the other).
 constexpr int JOIN_THREADS = 512;
-template <int RANK, int N>
+template <typename T, int RANK, int N>
 __global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_constant__ AttendArgs a, const int4* meta, int groups) {
   constexpr int LANES = RANK / 4, AT_ONCE = JOIN_THREADS / LANES;
   __shared__ float weight[AT_ONCE][SMS];           // of a row's pieces
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_
   }
   if (!on || group != 0) return;
   const float sum = total[row];
-  store_out(static_cast<__nv_bfloat16*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane, o,
+  store_out(static_cast<T*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane, o,
             sum == 0.f ? 0.f : 1.f / sum);
 }
 
@@ -444,44 +444,54 @@ __global__ void __launch_bounds__(256) latent_join_wide_kernel(const __grid_cons
       make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-// launches the kernel of items of N rows, and the join of those that blocks share; both wait for the kernels before
-// them themselves (griddepcontrol.wait)
-template <int RANK, int N, typename K>
-cudaError_t launch_items(K kernel, int threads, int smem, const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
-  CUtensorMap map, queries;
-  const bool flat = a.ldq == (long long)a.m.n_head * (RANK + LATENT_ROPE);
-  if (!latent_map(&map, a.m, a.m.page_tokens)) return cudaErrorInvalidValue;
-  queries = map;
-  if (flat && !query_map(&queries, a, N)) return cudaErrorInvalidValue;
-  static std::atomic<uint64_t> done{0};
-  cudaError_t e = allow_smem(kernel, smem, done);
-  if (e != cudaSuccess) return e;
-  const Run run{a.m.n_seq * a.tiles, p.splits > 1, flat, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * N)};
+// a launch whose kernel waits for the ones before it itself (griddepcontrol.wait)
+struct Launch {
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  cfg.stream = st;
-  cfg.gridDim = p.blocks;
-  cfg.blockDim = threads;
-  cfg.dynamicSmemBytes = smem;
-  e = cudaLaunchKernelEx(&cfg, kernel, a, map, queries, run);
-  if (e != cudaSuccess || !run.split) return e;
-  cfg.dynamicSmemBytes = 0;
+  Launch(dim3 grid, int threads, int smem, cudaStream_t st) {
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    cfg.stream = st;
+    cfg.gridDim = grid;
+    cfg.blockDim = threads;
+    cfg.dynamicSmemBytes = smem;
+  }
+};
+inline Run run_of_plan(const AttendArgs& a, const LatentPlan& p, int rows) {
+  return Run{a.m.n_seq * a.tiles, p.splits > 1, 0, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * rows)};
+}
+
+template <typename T, int RANK, int N>
+cudaError_t launch_join_of(const AttendArgs& a, const LatentPlan& p, const Run& run, cudaStream_t st) {
   if constexpr (N == 128) {
-    cfg.gridDim = dim3(p.blocks, RANK / 16);
-    cfg.blockDim = 256;
-    return cudaLaunchKernelEx(&cfg, latent_join_wide_kernel<RANK>, a, (const int4*)run.meta);
+    Launch launch(dim3(p.blocks, RANK / 16), 256, 0, st);
+    return cudaLaunchKernelEx(&launch.cfg, latent_join_wide_kernel<RANK>, a, (const int4*)run.meta);
   } else {
     constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
     int groups = 1;
     while (groups < AT_ONCE && groups * 8 * run.items < p.blocks) groups *= 2;
-    cfg.gridDim = dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE);
-    cfg.blockDim = JOIN_THREADS;
-    return cudaLaunchKernelEx(&cfg, latent_join_kernel<RANK, N>, a, (const int4*)run.meta, groups);
+    Launch launch(dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE), JOIN_THREADS, 0, st);
+    return cudaLaunchKernelEx(&launch.cfg, latent_join_kernel<T, RANK, N>, a, (const int4*)run.meta, groups);
   }
+}
+
+// launches the bf16 kernel of items of N rows, and the join of those that blocks share
+template <int RANK, int N, typename K>
+cudaError_t launch_items(K kernel, int threads, int smem, const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
+  CUtensorMap map, queries;
+  Run run = run_of_plan(a, p, N);
+  run.flat = a.ldq == (long long)a.m.n_head * (RANK + LATENT_ROPE);
+  if (!latent_map(&map, a.m, a.m.page_tokens)) return cudaErrorInvalidValue;
+  queries = map;
+  if (run.flat && !query_map(&queries, a, N)) return cudaErrorInvalidValue;
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = allow_smem(kernel, smem, done);
+  if (e != cudaSuccess) return e;
+  Launch launch(p.blocks, threads, smem, st);
+  e = cudaLaunchKernelEx(&launch.cfg, kernel, a, map, queries, run);
+  return e != cudaSuccess || !run.split ? e : launch_join_of<__nv_bfloat16, RANK, N>(a, p, run, st);
 }
 
 }  // namespace evo

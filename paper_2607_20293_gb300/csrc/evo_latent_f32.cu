@@ -5,7 +5,7 @@
 // As in the bf16 kernel both products have the memory as their first operand,
 //   S^T = X Q^T (tokens x rows),   O^T += C^T P^T (dimensions x rows)
 // so that the split of a token's values, three instructions each, serves all rows. A block is 8 warps (rank 512: 5) on
-// one tile of 8 NR rows and one piece of the memory.  A warp takes every eighth run of 16 tokens by itself, which
+// an item of 8 NR rows, or its run's part of one (evo_latent.cuh).  A warp takes every eighth run of 16 tokens by itself, which
 // arrives in its own one or two slots by tiled bulk copies, so that no barrier of the block is met until the end:
 // while one warp waits for its run the others compute.  Every warp keeps its own maximum
 // (lazy: rescaled only when a score passes it by 2^8) and sums, joined through shared memory.
@@ -24,15 +24,14 @@
 #include <algorithm>
 #include <cstdint>
 #include <cuda_runtime.h>
+#include <new>
 
-#include "evo_attend.cuh"
-#include "evo_mem_ptx.cuh"
+#include "evo_latent.cuh"
 
 namespace evo {
 namespace {
 
 constexpr int RUN = 16;                            // tokens of a run: a page holds whole ones
-constexpr float LAZY = 8.f;
 
 template <int RANK, int NR>
 struct Cfg {
@@ -60,262 +59,309 @@ __device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo) {
 __device__ __forceinline__ bool odd_number(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
 template <int RANK, int NR>
-__global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1) latent_f32_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
+    latent_f32_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ Run run) {
   using C = Cfg<RANK, NR>;
   constexpr int WARPS = C::WARPS, THREADS = C::THREADS, SLOTS = C::SLOTS, STEPS = C::DIMS / 16, BOXES = RANK / 32;   // boxes of 32 dimensions of the latent
   extern __shared__ uint8_t raw[];
+  __shared__ Roles sh;
   __shared__ __align__(8) uint64_t full[WARPS][SLOTS];
   __shared__ float2 stat[WARPS][C::ROWS];
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   const uint32_t ring = tc::su32(mem), queries = ring + C::RING;
-  if (tid == 0) fetch_map(&map);
-  const Tile t = tile_of_block(a);
-  const int rows = t.count * a.group, r0 = t.tile * C::ROWS;
-  if (r0 >= rows) return;
-  const int last = min(r0 + C::ROWS, rows) - 1;
-  const Range first_row = seen_by(a, t, r0 / a.group), last_row = seen_by(a, t, last / a.group);
-  const Range all = piece_of(a, t, {first_row.lo, last_row.hi}, RUN);
-  const int whole_lo = max(last_row.lo, all.lo), whole_hi = min(first_row.hi, all.hi);
-  const int from = all.lo / RUN * RUN, n = max(0, (all.hi - from + RUN - 1) / RUN);
   if (tid == 0) {
+    fetch_map(&map);
     for (int i = 0; i < WARPS * SLOTS; ++i) tc::mbar_init1(&full[0][i], 1);
+    sh.item = run.split ? run.items : blockIdx.x;
+    sh.skip = 0;
+    sh.tiles = run.split ? 0 : INT_MAX;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  __syncwarp();
+  tc::pdl_wait();                                            // what earlier kernels wrote is there
+  if (run.split) tc::pdl_trigger();                          // the join may take its places, and waits there
+  const Share share = count_tiles<C::ROWS, THREADS>(a, run, sh);
   __syncthreads();
+  __shared__ __align__(8) uint8_t walk_at[sizeof(Walk<C::ROWS>)];   // one thread's: registers are short
+  Walk<C::ROWS>* const walk = reinterpret_cast<Walk<C::ROWS>*>(walk_at);
+  if (tid == 0) new (walk) Walk<C::ROWS>(a, run, sh);
+  bool shares = false, dead = false;
+  int asked = 0;                                             // runs of this warp before this item's
   const int shift = 31 - __clz(a.m.page_tokens);
-  // the j-th run of this warp is run i of the piece; only this warp asks for it, waits for it and reads it
-  const auto run_of = [&](int j) { return warp + j * WARPS; };
-  const auto page_of = [&](int j) { return run_of(j) < n ? seq_page(a.m, t.n, (from + run_of(j) * RUN) >> shift) : 0; };
-  const uint32_t mine = ring + warp * (SLOTS * C::BYTES);
-  const auto ask = [&](int j, int page) {          // to its slot, a lane a box
-    if (run_of(j) >= n) return;
-    uint64_t* bar = &full[warp][j % SLOTS];
-    if (lane == 0) tc::mbar_expect_tx(bar, C::BYTES);
-    __syncwarp();
-    if (lane < C::BOXES)
-      tile_load(mine + j % SLOTS * C::BYTES + lane * (RUN * 128), &map, 32 * lane,
-                (page << shift) + ((from + run_of(j) * RUN) & (a.m.page_tokens - 1)), tc::su32(bar));
-  };
+  while (true) {
+    if (tid == 0) fill_segment(a, run, share, *walk, sh.seg[0], shares);
+    __syncthreads();
+    const Segment& seg = sh.seg[0];
+    if (!seg.more) break;
+    const Tile& t = seg.x.t;
+    const int rows = seg.x.rows, r0 = seg.x.r0;
+    // this block's piece of the tokens, and of these the ones that every row sees
+    const Range all = {max(seg.x.all.lo, seg.key0), seg.n == 0 ? 0 : min(seg.x.all.hi, seg.key0 + seg.n * BK)};
+    const int whole_lo = max(seg.x.last_row.lo, all.lo), whole_hi = min(seg.x.first_row.hi, all.hi);
+    const int from = all.lo / RUN * RUN, n = max(0, (all.hi - from + RUN - 1) / RUN);
+    // the j-th run of this warp is run i of the piece; only this warp asks for it, waits for it and reads it
+    const auto run_of = [&](int j) { return warp + j * WARPS; };
+    const auto page_of = [&](int j) { return run_of(j) < n ? seq_page(a.m, t.n, (from + run_of(j) * RUN) >> shift) : 0; };
+    const uint32_t mine = ring + warp * (SLOTS * C::BYTES);
+    const auto ask = [&](int j, int page) {          // to its slot, a lane a box
+      if (run_of(j) >= n) return;
+      const int slot = (asked + j) % SLOTS;
+      uint64_t* bar = &full[warp][slot];
+      if (lane == 0) tc::mbar_expect_tx(bar, C::BYTES);
+      __syncwarp();
+      if (lane < C::BOXES)
+        tile_load(mine + slot * C::BYTES + lane * (RUN * 128), &map, 32 * lane,
+                  (page << shift) + ((from + run_of(j) * RUN) & (a.m.page_tokens - 1)), tc::su32(bar));
+    };
 #pragma unroll
-  for (int j = 0; j < SLOTS; ++j) ask(j, page_of(j));
-  int ahead = page_of(SLOTS);
-  // queries: the fragments of a step pair, high parts and low parts
+    for (int j = 0; j < SLOTS; ++j) ask(j, page_of(j));
+    int ahead = page_of(SLOTS);
+    // queries: the fragments of a step pair, high parts and low parts
 #pragma unroll 4
-  for (int i = tid; i < STEPS * NR * 32; i += THREADS) {
-    const int l = i % 32, nr = i / 32 % NR, h = i / 32 / NR, R = r0 + 8 * nr + l / 4;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (R < rows)
-      x = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (long long)(t.first + R / a.group) * a.ldq +
-                                           (long long)(R % a.group) * C::DIMS + 16 * h + 4 * (l % 4));
-    uint4 hi, lo;
-    split(x.x, hi.x, lo.x), split(x.y, hi.y, lo.y), split(x.z, hi.z, lo.z), split(x.w, hi.w, lo.w);
-    uint4* dst = reinterpret_cast<uint4*>(mem + C::RING + (h * NR + nr) * 1024 + l * 16);
-    dst[0] = hi;
-    dst[32] = lo;
-  }
-  __syncthreads();
-
-  float o[NR][2 * BOXES][4], sum[NR][2], top[NR][2];         // o: tile 2 b + j; rows 2 c, 2 c + 1
-#pragma unroll
-  for (int nr = 0; nr < NR; ++nr) {
-#pragma unroll
-    for (int j = 0; j < 2 * BOXES; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[nr][j][e] = 0.f;
-    sum[nr][0] = sum[nr][1] = 0.f;
-    top[nr][0] = top[nr][1] = -INFINITY;
-  }
-  const int tg = g / 2 + 4 * (g % 2);                        // the token of the scores' row g; row g + 8: 8 further
-  const float f = a.scale_log2;
-  bool dead = false;
-  for (int j = 0; run_of(j) < n; ++j) {
-    const uint32_t x = mine + j % SLOTS * C::BYTES;
-    if (!__all_sync(0xffffffffu, wait_full(tc::su32(&full[warp][j % SLOTS]), (j / SLOTS) & 1))) {
-      dead = true;
-      break;
+    for (int i = tid; i < STEPS * NR * 32; i += THREADS) {
+      const int l = i % 32, nr = i / 32 % NR, h = i / 32 / NR, R = r0 + 8 * nr + l / 4;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (R < rows)
+        x = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (long long)(t.first + R / a.group) * a.ldq +
+                                             (long long)(R % a.group) * C::DIMS + 16 * h + 4 * (l % 4));
+      uint4 hi, lo;
+      split(x.x, hi.x, lo.x), split(x.y, hi.y, lo.y), split(x.z, hi.z, lo.z), split(x.w, hi.w, lo.w);
+      uint4* dst = reinterpret_cast<uint4*>(mem + C::RING + (h * NR + nr) * 1024 + l * 16);
+      dst[0] = hi;
+      dst[32] = lo;
     }
-    const int k0 = from + run_of(j) * RUN;
-    const bool odd = k0 < whole_lo || k0 + RUN > whole_hi;
-    float s[NR][4];
-    uint32_t drop = 0;                                       // tokens whose values count as zero
-    {
-      float hh[NR][4][4] = {}, rest[NR][4] = {};
-      bool bad0 = false, bad1 = false;
+    __syncthreads();
+
+    float o[NR][2 * BOXES][4], sum[NR][2], top[NR][2];         // o: tile 2 b + j; rows 2 c, 2 c + 1
 #pragma unroll
-      for (int h = 0; h < STEPS; ++h) {
-        const float4 x0 = lds_f4(x + h / 2 * (RUN * 128) + tg * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
-        const float4 x1 = lds_f4(x + h / 2 * (RUN * 128) + (8 + tg) * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
-        if (odd && h < RANK / 16) {
-          bad0 |= odd_number(x0.x) || odd_number(x0.y) || odd_number(x0.z) || odd_number(x0.w);
-          bad1 |= odd_number(x1.x) || odd_number(x1.y) || odd_number(x1.z) || odd_number(x1.w);
-        }
-        uint32_t hi[2][4], lo[2][4];
-        split(x0.x, hi[0][0], lo[0][0]), split(x1.x, hi[0][1], lo[0][1]), split(x0.y, hi[0][2], lo[0][2]), split(x1.y, hi[0][3], lo[0][3]);
-        split(x0.z, hi[1][0], lo[1][0]), split(x1.z, hi[1][1], lo[1][1]), split(x0.w, hi[1][2], lo[1][2]), split(x1.w, hi[1][3], lo[1][3]);
+    for (int nr = 0; nr < NR; ++nr) {
 #pragma unroll
-        for (int nr = 0; nr < NR; ++nr) {
-          const uint4 qh = lds128(queries + (h * NR + nr) * 1024 + lane * 16), ql = lds128(queries + (h * NR + nr) * 1024 + 512 + lane * 16);
-          mma8(hh[nr][2 * h % 4], hi[0], qh.x, qh.y);
-          mma8(hh[nr][(2 * h + 1) % 4], hi[1], qh.z, qh.w);
-          mma8(rest[nr], lo[0], qh.x, qh.y);
-          mma8(rest[nr], hi[0], ql.x, ql.y);
-          mma8(rest[nr], lo[1], qh.z, qh.w);
-          mma8(rest[nr], hi[1], ql.z, ql.w);
-        }
+      for (int j = 0; j < 2 * BOXES; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nr][j][e] = 0.f;
+      sum[nr][0] = sum[nr][1] = 0.f;
+      top[nr][0] = top[nr][1] = -INFINITY;
+    }
+    const int tg = g / 2 + 4 * (g % 2);                        // the token of the scores' row g; row g + 8: 8 further
+    const float f = a.scale_log2;
+    int j = 0;
+    for (; run_of(j) < n; ++j) {
+      const int slot = (asked + j) % SLOTS;
+      const uint32_t x = mine + slot * C::BYTES;
+      if (!__all_sync(0xffffffffu, wait_full(tc::su32(&full[warp][slot]), ((asked + j) / SLOTS) & 1))) {
+        dead = true;
+        break;
       }
+      const int k0 = from + run_of(j) * RUN;
+      const bool odd = k0 < whole_lo || k0 + RUN > whole_hi;
+      float s[NR][4];
+      uint32_t drop = 0;                                       // tokens whose values count as zero
+      {
+        constexpr int RESTS = NR == 1 ? 4 : 1;                 // sums of the other products: chains of their own, where registers are left
+        float hh[NR][4][4] = {}, rest[NR][RESTS][4] = {};
+        bool bad0 = false, bad1 = false;
 #pragma unroll
-      for (int nr = 0; nr < NR; ++nr)
+        for (int h = 0; h < STEPS; ++h) {
+          const float4 x0 = lds_f4(x + h / 2 * (RUN * 128) + tg * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
+          const float4 x1 = lds_f4(x + h / 2 * (RUN * 128) + (8 + tg) * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
+          if (odd && h < RANK / 16) {
+            bad0 |= odd_number(x0.x) || odd_number(x0.y) || odd_number(x0.z) || odd_number(x0.w);
+            bad1 |= odd_number(x1.x) || odd_number(x1.y) || odd_number(x1.z) || odd_number(x1.w);
+          }
+          uint32_t hi[2][4], lo[2][4];
+          split(x0.x, hi[0][0], lo[0][0]), split(x1.x, hi[0][1], lo[0][1]), split(x0.y, hi[0][2], lo[0][2]), split(x1.y, hi[0][3], lo[0][3]);
+          split(x0.z, hi[1][0], lo[1][0]), split(x1.z, hi[1][1], lo[1][1]), split(x0.w, hi[1][2], lo[1][2]), split(x1.w, hi[1][3], lo[1][3]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[nr][e] = (((hh[nr][0][e] + hh[nr][1][e]) + (hh[nr][2][e] + hh[nr][3][e])) + rest[nr][e]) * f;
-      if (odd) {
-        const int k1 = k0 + tg, k2 = k1 + 8;
-        const bool out0 = k1 < all.lo || k1 >= all.hi, out1 = k2 < all.lo || k2 >= all.hi;
-        // bit 4 g + c of a ballot: a quarter of token t(g)
-        uint32_t b0 = __ballot_sync(0xffffffffu, bad0 || out0), b1 = __ballot_sync(0xffffffffu, bad1 || out1);
-#pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          const uint32_t at = 0xfu << (4 * y), to = 1u << (y / 2 + 4 * (y % 2));
-          if (b0 & at) drop |= to;
-          if (b1 & at) drop |= to << 8;
+          for (int nr = 0; nr < NR; ++nr) {
+            const uint4 qh = lds128(queries + (h * NR + nr) * 1024 + lane * 16), ql = lds128(queries + (h * NR + nr) * 1024 + 512 + lane * 16);
+            mma8(hh[nr][2 * h % 4], hi[0], qh.x, qh.y);
+            mma8(hh[nr][(2 * h + 1) % 4], hi[1], qh.z, qh.w);
+            mma8(rest[nr][0], lo[0], qh.x, qh.y);
+            mma8(rest[nr][1 % RESTS], hi[0], ql.x, ql.y);
+            mma8(rest[nr][2 % RESTS], lo[1], qh.z, qh.w);
+            mma8(rest[nr][3 % RESTS], hi[1], ql.z, ql.w);
+          }
         }
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int R = r0 + 8 * nr + 2 * c + e;
-            const Range see = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
-            const int lo = max(see.lo, all.lo), hi = min(see.hi, all.hi);
-            if (drop >> tg & 1) s[nr][e] = __builtin_nanf("");
-            if (drop >> (tg + 8) & 1) s[nr][2 + e] = __builtin_nanf("");
-            if (k1 < lo || k1 >= hi) s[nr][e] = -INFINITY;
-            if (k2 < lo || k2 >= hi) s[nr][2 + e] = -INFINITY;
+          for (int e = 0; e < 4; ++e) {
+            float low = rest[nr][0][e];
+#pragma unroll
+            for (int y = 1; y < RESTS; ++y) low += rest[nr][y][e];
+            s[nr][e] = (((hh[nr][0][e] + hh[nr][1][e]) + (hh[nr][2][e] + hh[nr][3][e])) + low) * f;
           }
-      }
-    }
-    bool raise = false;
+        if (odd) {
+          const int k1 = k0 + tg, k2 = k1 + 8;
+          const bool out0 = k1 < all.lo || k1 >= all.hi, out1 = k2 < all.lo || k2 >= all.hi;
+          // bit 4 g + c of a ballot: a quarter of token t(g)
+          uint32_t b0 = __ballot_sync(0xffffffffu, bad0 || out0), b1 = __ballot_sync(0xffffffffu, bad1 || out1);
 #pragma unroll
-    for (int nr = 0; nr < NR; ++nr)
+          for (int y = 0; y < 8; ++y) {
+            const uint32_t at = 0xfu << (4 * y), to = 1u << (y / 2 + 4 * (y % 2));
+            if (b0 & at) drop |= to;
+            if (b1 & at) drop |= to << 8;
+          }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float m = fmaxf(s[nr][e], s[nr][2 + e]);
-        raise |= m > top[nr][e] + LAZY || (top[nr][e] == -INFINITY && m > -INFINITY);
+          for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int R = r0 + 8 * nr + 2 * c + e;
+              const Range see = R < rows ? seen_by(a, t, R / a.group) : Range{0, 0};
+              const int lo = max(see.lo, all.lo), hi = min(see.hi, all.hi);
+              if (drop >> tg & 1) s[nr][e] = __builtin_nanf("");
+              if (drop >> (tg + 8) & 1) s[nr][2 + e] = __builtin_nanf("");
+              if (k1 < lo || k1 >= hi) s[nr][e] = -INFINITY;
+              if (k2 < lo || k2 >= hi) s[nr][2 + e] = -INFINITY;
+            }
+        }
       }
-    if (__any_sync(0xffffffffu, raise)) {
+      bool raise = false;
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float m = fmaxf(s[nr][e], s[nr][2 + e]);
-#pragma unroll
-          for (int y = 4; y < 32; y *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, y));
-          m = fmaxf(m, top[nr][e]);
-          const float down = m == -INFINITY ? 1.f : ex2_approx(top[nr][e] - m);
-          top[nr][e] = m;
-          sum[nr][e] *= down;
-#pragma unroll
-          for (int j = 0; j < 2 * BOXES; ++j) o[nr][j][e] *= down, o[nr][j][2 + e] *= down;
+          const float m = fmaxf(s[nr][e], s[nr][2 + e]);
+          raise |= m > top[nr][e] + LAZY || (top[nr][e] == -INFINITY && m > -INFINITY);
         }
-    }
-    // weights, and the output's second operand: steps z, tokens 8 z + 2 c and the next, row g
-    uint32_t ph[NR][2][2], pl[NR][2][2];
-#pragma unroll
-    for (int nr = 0; nr < NR; ++nr) {
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float m = top[nr][e % 2];
-        p[e] = ex2_approx(s[nr][e] - (m == -INFINITY ? 0.f : m));
-        sum[nr][e % 2] += p[e];
-      }
-#pragma unroll
-      for (int z = 0; z < 2; ++z)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int token = 2 * c + b, src = ((token & 3) * 2 + token / 4) * 4 + g / 2;
-          const float y0 = __shfl_sync(0xffffffffu, p[2 * z], src), y1 = __shfl_sync(0xffffffffu, p[2 * z + 1], src);
-          split(g % 2 ? y1 : y0, ph[nr][z][b], pl[nr][z][b]);
-        }
-    }
-#pragma unroll
-    for (int b = 0; b < BOXES; ++b) {
-      float y[NR][2][4] = {};
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int k1 = 8 * z + 2 * c;
-        float4 x0 = lds_f4(x + b * (RUN * 128) + k1 * 128 + ((g ^ (2 * c)) << 4));
-        float4 x1 = lds_f4(x + b * (RUN * 128) + (k1 + 1) * 128 + ((g ^ (2 * c + 1)) << 4));
-        if (odd) {
-          if (drop >> k1 & 1) x0 = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (drop >> (k1 + 1) & 1) x1 = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        uint32_t hi[2][4], lo[2][4];
-        split(x0.x, hi[0][0], lo[0][0]), split(x0.y, hi[0][1], lo[0][1]), split(x1.x, hi[0][2], lo[0][2]), split(x1.y, hi[0][3], lo[0][3]);
-        split(x0.z, hi[1][0], lo[1][0]), split(x0.w, hi[1][1], lo[1][1]), split(x1.z, hi[1][2], lo[1][2]), split(x1.w, hi[1][3], lo[1][3]);
+      if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
         for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            mma8(y[nr][j], hi[j], ph[nr][z][0], ph[nr][z][1]);
-            mma8(y[nr][j], lo[j], ph[nr][z][0], ph[nr][z][1]);
-            mma8(y[nr][j], hi[j], pl[nr][z][0], pl[nr][z][1]);
+          for (int e = 0; e < 2; ++e) {
+            float m = fmaxf(s[nr][e], s[nr][2 + e]);
+#pragma unroll
+            for (int y = 4; y < 32; y *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, y));
+            m = fmaxf(m, top[nr][e]);
+            const float down = m == -INFINITY ? 1.f : ex2_approx(top[nr][e] - m);
+            top[nr][e] = m;
+            sum[nr][e] *= down;
+#pragma unroll
+            for (int j = 0; j < 2 * BOXES; ++j) o[nr][j][e] *= down, o[nr][j][2 + e] *= down;
+          }
+      }
+      // weights, and the output's second operand: steps z, tokens 8 z + 2 c and the next, row g
+      uint32_t ph[NR][2][2], pl[NR][2][2];
+#pragma unroll
+      for (int nr = 0; nr < NR; ++nr) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float m = top[nr][e % 2];
+          p[e] = ex2_approx(s[nr][e] - (m == -INFINITY ? 0.f : m));
+          sum[nr][e % 2] += p[e];
+        }
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const int token = 2 * c + b, src = ((token & 3) * 2 + token / 4) * 4 + g / 2;
+            const float y0 = __shfl_sync(0xffffffffu, p[2 * z], src), y1 = __shfl_sync(0xffffffffu, p[2 * z + 1], src);
+            split(g % 2 ? y1 : y0, ph[nr][z][b], pl[nr][z][b]);
           }
       }
 #pragma unroll
-      for (int nr = 0; nr < NR; ++nr)
+      for (int b = 0; b < BOXES; ++b) {
+        float y[NR][2][4] = {};
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int z = 0; z < 2; ++z) {
+          const int k1 = 8 * z + 2 * c;
+          float4 x0 = lds_f4(x + b * (RUN * 128) + k1 * 128 + ((g ^ (2 * c)) << 4));
+          float4 x1 = lds_f4(x + b * (RUN * 128) + (k1 + 1) * 128 + ((g ^ (2 * c + 1)) << 4));
+          if (odd) {
+            if (drop >> k1 & 1) x0 = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (drop >> (k1 + 1) & 1) x1 = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          uint32_t hi[2][4], lo[2][4];
+          split(x0.x, hi[0][0], lo[0][0]), split(x0.y, hi[0][1], lo[0][1]), split(x1.x, hi[0][2], lo[0][2]), split(x1.y, hi[0][3], lo[0][3]);
+          split(x0.z, hi[1][0], lo[1][0]), split(x0.w, hi[1][1], lo[1][1]), split(x1.z, hi[1][2], lo[1][2]), split(x1.w, hi[1][3], lo[1][3]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[nr][2 * b + j][e] += y[nr][j][e];
+          for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              mma8(y[nr][j], hi[j], ph[nr][z][0], ph[nr][z][1]);
+              mma8(y[nr][j], lo[j], ph[nr][z][0], ph[nr][z][1]);
+              mma8(y[nr][j], hi[j], pl[nr][z][0], pl[nr][z][1]);
+            }
+        }
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[nr][2 * b + j][e] += y[nr][j][e];
+      }
+      __syncwarp();                                            // every lane has read the slot
+      ask(j + SLOTS, ahead);
+      ahead = page_of(j + 1 + SLOTS);
     }
-    __syncwarp();                                            // every lane has read the slot
-    ask(j + SLOTS, ahead);
-    ahead = page_of(j + 1 + SLOTS);
+    asked += j;
+    dead = __syncthreads_or(dead);
+    if (dead) {                                                // a copy did not arrive
+      settle(a.m.status);
+      break;
+    }
+    float* const sums = reinterpret_cast<float*>(mem);         // [WARPS][ROWS][LD], in place of the ring
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float l = sum[nr][e];
+#pragma unroll
+        for (int y = 4; y < 32; y *= 2) l += __shfl_xor_sync(0xffffffffu, l, y);
+        const int r = 8 * nr + 2 * c + e;
+        if (g == 0) stat[warp][r] = make_float2(top[nr][e], l);
+#pragma unroll
+        for (int b = 0; b < BOXES; ++b)
+          *reinterpret_cast<float4*>(sums + (warp * C::ROWS + r) * C::LD + 32 * b + 4 * g) =
+              make_float4(o[nr][2 * b][e], o[nr][2 * b][2 + e], o[nr][2 * b + 1][e], o[nr][2 * b + 1][2 + e]);
+      }
+    __syncthreads();
+    for (int i = tid; i < C::ROWS * RANK / 4; i += THREADS) {
+      const int r = i / (RANK / 4), d = i % (RANK / 4) * 4;
+      if (r0 + r >= rows) break;
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) m = fmaxf(m, stat[w][r].x);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float4 v = {};
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float2 ml = stat[w][r];
+        const float4 y = *reinterpret_cast<const float4*>(sums + (w * C::ROWS + r) * C::LD + d);
+        const float fw = ex2_approx(ml.x - ref);
+        l = fmaf(ml.y, fw, l);
+        v = make_float4(fmaf(y.x, fw, v.x), fmaf(y.y, fw, v.y), fmaf(y.z, fw, v.z), fmaf(y.w, fw, v.w));
+      }
+      if (seg.whole) {
+        const int R = r0 + r;
+        store_out(static_cast<float*>(a.out) + (long long)(t.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + d, v,
+                  l == 0.f ? 0.f : 1.f / l);
+      } else {
+        const long long at = (long long)seg.slot * C::ROWS + r;
+        *reinterpret_cast<float4*>(a.part + at * RANK + d) = v;
+        if (d == 0) a.ml[at] = make_float2(m, l);
+      }
+    }
+    tc::fence_async_smem();                                    // before further copies take the place of the sums
+    __syncthreads();
   }
-  if (__syncthreads_or(dead)) settle(a.m.status);            // a copy did not arrive
-  float* const sums = reinterpret_cast<float*>(mem);         // [WARPS][ROWS][LD], in place of the ring
-#pragma unroll
-  for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float l = sum[nr][e];
-#pragma unroll
-      for (int y = 4; y < 32; y *= 2) l += __shfl_xor_sync(0xffffffffu, l, y);
-      const int r = 8 * nr + 2 * c + e;
-      if (g == 0) stat[warp][r] = make_float2(top[nr][e], l);
-#pragma unroll
-      for (int b = 0; b < BOXES; ++b)
-        *reinterpret_cast<float4*>(sums + (warp * C::ROWS + r) * C::LD + 32 * b + 4 * g) =
-            make_float4(o[nr][2 * b][e], o[nr][2 * b][2 + e], o[nr][2 * b + 1][e], o[nr][2 * b + 1][2 + e]);
-    }
-  __syncthreads();
-  for (int i = tid; i < C::ROWS * RANK / 4; i += THREADS) {
-    const int r = i / (RANK / 4), d = i % (RANK / 4) * 4;
-    if (r0 + r >= rows) break;
-    float m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) m = fmaxf(m, stat[w][r].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float4 v = {};
-#pragma unroll
-    for (int w = 0; w < WARPS; ++w) {
-      const float2 ml = stat[w][r];
-      const float4 y = *reinterpret_cast<const float4*>(sums + (w * C::ROWS + r) * C::LD + d);
-      const float fw = ex2_approx(ml.x - ref);
-      l = fmaf(ml.y, fw, l);
-      v = make_float4(fmaf(y.x, fw, v.x), fmaf(y.y, fw, v.y), fmaf(y.z, fw, v.z), fmaf(y.w, fw, v.w));
-    }
-    put_result<float, RANK>(a, t, r0 + r, d, v, m, l);
-  }
+  if (run.split && tid == 0 && !shares) run.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
 }
 
 template <int RANK, int NR>
-cudaError_t launch_as(const AttendArgs& a, cudaStream_t st) {
+cudaError_t launch_as(const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
   using C = Cfg<RANK, NR>;
   CUtensorMap map;
   if (!latent_map(&map, a.m, RUN)) return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
-  return launch_pieces(latent_f32_kernel<RANK, NR>, a, C::THREADS, C::SMEM, done, st, map);
+  cudaError_t e = allow_smem(latent_f32_kernel<RANK, NR>, C::SMEM, done);
+  if (e != cudaSuccess) return e;
+  const Run run = run_of_plan(a, p, C::ROWS);
+  Launch launch(p.blocks, C::THREADS, C::SMEM, st);
+  e = cudaLaunchKernelEx(&launch.cfg, latent_f32_kernel<RANK, NR>, a, map, run);
+  return e != cudaSuccess || !run.split ? e : launch_join_of<float, RANK, C::ROWS>(a, p, run, st);
 }
 
 }  // namespace
@@ -327,10 +373,10 @@ int latent_f32_rows(int rank, long long all, int n_seq) {
   return rows;
 }
 
-cudaError_t launch_latent_f32(const AttendArgs& a, int tile_rows, cudaStream_t st) {
-  if (a.m.head_dim == 512) return launch_as<512, 1>(a, st);
-  if (a.m.head_dim == 256) return tile_rows == 8 ? launch_as<256, 1>(a, st) : launch_as<256, 2>(a, st);
-  return tile_rows == 8 ? launch_as<128, 1>(a, st) : tile_rows == 16 ? launch_as<128, 2>(a, st) : launch_as<128, 4>(a, st);
+cudaError_t launch_latent_f32(const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
+  if (a.m.head_dim == 512) return launch_as<512, 1>(a, p, st);
+  if (a.m.head_dim == 256) return p.tile_rows == 8 ? launch_as<256, 1>(a, p, st) : launch_as<256, 2>(a, p, st);
+  return p.tile_rows == 8 ? launch_as<128, 1>(a, p, st) : p.tile_rows == 16 ? launch_as<128, 2>(a, p, st) : launch_as<128, 4>(a, p, st);
 }
 
 }  // namespace evo

@@ -444,23 +444,7 @@ cudaError_t launch_of(const AttendArgs& a, const LatentPlan& p, cudaStream_t st)
 
 }  // namespace
 
-// Pieces: items go to the blocks whole where that takes little longer, in tiles, than equal runs and their join
-void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int keys) {
-  p.tile_rows = all <= 16 ? 16 : all <= 32 || m.head_dim == 512 ? 32 : all <= 64 ? 64 : 128;
-  p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
-  const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + BK - 1) / BK);
-  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + (p.tile_rows <= 32 ? 3 : p.tile_rows == 64 ? 5 : 6);
-  const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
-  p.splits = split ? 2 : 1;
-  p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
-  // sums, and maximum and sum of weights, of two pieces a block; where a block's last item goes on
-  p.scratch = split ? (size_t)p.blocks * (2 * p.tile_rows * ((size_t)m.head_dim + 2) * sizeof(float) + sizeof(int4)) : 0;
-}
-
-cudaError_t launch_latent_tiles(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st) {
-  a.part = static_cast<float*>(scratch);
-  a.ml = reinterpret_cast<float2*>(a.part + (size_t)2 * p.blocks * p.tile_rows * a.m.head_dim);
-  if (p.tile_rows == 128) return launch_latent_wide(a, p, st);
+cudaError_t launch_latent_tiles(const AttendArgs& a, const LatentPlan& p, cudaStream_t st) {
   return a.m.head_dim == 128 ? launch_of<128>(a, p, st) : a.m.head_dim == 256 ? launch_of<256>(a, p, st) : launch_of<512>(a, p, st);
 }
 

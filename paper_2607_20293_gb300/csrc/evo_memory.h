@@ -63,9 +63,6 @@ cudaError_t launch_attend_f32_rows(const AttendArgs& a, int tile_rows, cudaStrea
 cudaError_t launch_attend_tiles(const AttendArgs& a, cudaStream_t st);                // evo_attend_tiles.cu
 cudaError_t launch_attend(AttendArgs& a, const AttendPlan& p, void* scratch, cudaStream_t st);
 
-// joins the pieces of a call's rows from a.part and a.ml (evo_attend.cu); head_dim 64 to 512
-cudaError_t launch_join(const AttendArgs& a, cudaStream_t st);
-
 // The latent memory.  Its calls run on the paged memory's arguments: one key/value head whose keys are a
 // page's rows of rank + LATENT_ROPE values and whose values are the first head_dim = rank of them.
 constexpr int LATENT_ROPE = 64, LATENT_KEY = 64, LATENT_VALUE = 128;
@@ -83,17 +80,16 @@ struct LatentAppendArgs {
 };
 cudaError_t launch_latent_append(const LatentAppendArgs& a, cudaStream_t st);   // evo_latent.cu
 struct LatentPlan {
-  int tile_rows, tiles, splits, cluster;
-  int blocks;                     // bf16: of the launch; splits 2: they share items
+  int tile_rows, tiles;           // rows of an item, items of a sequence
+  int splits, blocks;             // 2: the launch's blocks share items
   size_t scratch;
 };
 LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, int causal, int window);   // evo_latent.cu
 cudaError_t launch_latent_attend(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
-void plan_latent_tiles(LatentPlan& p, const evo_memory& m, long long all, int keys);    // evo_latent_tiles.cu
-cudaError_t launch_latent_tiles(AttendArgs& a, const LatentPlan& p, void* scratch, cudaStream_t st);
-cudaError_t launch_latent_wide(const AttendArgs& a, const LatentPlan& p, cudaStream_t st);   // 128 rows: evo_latent_wide.cu
-int latent_f32_rows(int rank, long long all, int n_seq);   // rows of a tile of fp32 rows, evo_latent_f32.cu
-cudaError_t launch_latent_f32(const AttendArgs& a, int tile_rows, cudaStream_t st);
+cudaError_t launch_latent_tiles(const AttendArgs& a, const LatentPlan& p, cudaStream_t st);  // up to 64 bf16 rows an item: evo_latent_tiles.cu
+cudaError_t launch_latent_wide(const AttendArgs& a, const LatentPlan& p, cudaStream_t st);   // 128: evo_latent_wide.cu
+int latent_f32_rows(int rank, long long all, int n_seq);   // rows of an item of fp32 rows, evo_latent_f32.cu
+cudaError_t launch_latent_f32(const AttendArgs& a, const LatentPlan& p, cudaStream_t st);
 struct LatentExpandArgs {
   evo_memory m, to;               // the latent memory, and the one that its tokens are written to
   const void *w_k, *w_v;          // [n_head][LATENT_KEY][rank], [n_head][LATENT_VALUE][rank]
