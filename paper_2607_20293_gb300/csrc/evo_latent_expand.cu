@@ -13,20 +13,22 @@
 // each of these lanes 8 products of its own in a row (a token a lane and 32 bytes a store were 32 lines an
 // instruction: 101 us for 20,500 tokens of 16 heads).
 //
-// fp32: a block takes 64 tokens and the 192 products of a head, 16 of the rank at a time through shared
-// memory; a thread has 8 tokens x 6 products in packed pairs of tokens.
+// fp32, on mma.sync: a number is split into two of 11 bits and a product taken as three of tf32 (evo_latent_f32.cu).
+// A block has 64 tokens and a head, a warp 32 of these and 48 of its 192 products; rows of 32 dimensions of both
+// arrive in a ring by asynchronous copies.  The matrix unit cuts its sums off: those of 32 dimensions are added in
+// fp32.  Rows stand in shared memory in the order that gives the lanes of a 16-byte load different banks, and each
+// lane four products in a row of its tokens.
 #include <algorithm>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
-#include "evo_mem_ptx.cuh"
-#include "evo_rows.cuh"
+#include "evo_latent.cuh"
 
 namespace evo {
 namespace {
 
-constexpr int THREADS = 256, BM = 64, BN = LATENT_KEY + LATENT_VALUE, BK = 16;
+constexpr int THREADS = 256, BM = 64, BN = LATENT_KEY + LATENT_VALUE;   // fp32: threads and tokens of a block; products of a head
 
 // tokens of sequence n that are written: [lo, hi); what does not fit the call reports itself and gives none
 __device__ __forceinline__ int2 token_range(const LatentExpandArgs& a, int n) {
@@ -44,9 +46,6 @@ __device__ __forceinline__ int page_or_none(const evo_memory& m, int32_t* status
   if (status) *status = EVO_ERR_CORRUPT;
   return -1;
 }
-
-__device__ __forceinline__ float4 four(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ void put2(float* p, float2 v) { *reinterpret_cast<float2*>(p) = v; }
 
 // ---------------------------------------------------------------- bf16
 
@@ -70,16 +69,6 @@ struct Shared {
   int dead;
 };
 
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* dead) {
-  const uint32_t b = tc::su32(bar);
-  return tc::mbar_test(b, parity) || wait_live(b, parity, tc::su32(dead));
-}
-// a wait behind a first test that failed
-__device__ __noinline__ void wait_slow(uint32_t bar, uint32_t parity, uint32_t dead) { wait_live(bar, parity, dead); }
-__device__ __forceinline__ uint64_t desc64(uint32_t lo, uint32_t hi) { return ((uint64_t)hi << 32) | lo; }
-__device__ __forceinline__ void commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
 // 32 columns of 16 lanes: of column 8 k + 2 c + e, lane (g, c) gets that of TMEM lane g in v[4 k + e] and of g + 8 in v[4 k + 2 + e]
 __device__ __forceinline__ void tmem_ld16x32(uint32_t taddr, float (&v)[16]) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
@@ -320,26 +309,37 @@ cudaError_t launch_tiles(const LatentExpandArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int pairs = a.m.n_seq * (a.max_new / TM + 2);        // a range may begin and end within a tile
   const int groups = std::max(1, std::min(pairs, 152 / a.to.n_kv_head));
-  cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // it waits for the kernels before it itself
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  cfg.stream = st;
-  cfg.gridDim = groups * a.to.n_kv_head;
-  cfg.blockDim = TILE_THREADS;
-  cfg.dynamicSmemBytes = C::SMEM;
-  return cudaLaunchKernelEx(&cfg, latent_expand_tiles_kernel<RANK>, a, map, pairs, groups);
+  Launch launch(groups * a.to.n_kv_head, TILE_THREADS, C::SMEM, st);
+  return cudaLaunchKernelEx(&launch.cfg, latent_expand_tiles_kernel<RANK>, a, map, pairs, groups);
 }
 
 // ---------------------------------------------------------------- fp32
 
-__global__ void __launch_bounds__(THREADS) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
-  __shared__ __align__(16) float as[BK][BM], bs[BK][BN];
+constexpr int F32_STAGES = 4, F32_STAGE = (BM + BN) * 128, F32_SMEM = 1024 + F32_STAGES * F32_STAGE;   // 32 dimensions of a block's rows
+
+__device__ __forceinline__ void mma8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the 11 leading bits of x, rounded, and what they leave
+__device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo) {
+  hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  lo = __float_as_uint(x - __uint_as_float(hi));
+}
+// the place of row n of 8 of a fragment: those that the 8 lanes of a load's phase have are 4 rows apart
+__device__ __forceinline__ int place8(int n) { return n / 2 + 4 * (n % 2); }
+// the place of product p of 16: column 2 c + e of tile t is 4 c + 2 t + e
+__device__ __forceinline__ int place16(int p) { return 8 * (p / 2 % 2) + place8(p / 4 * 2 + p % 2); }
+
+__global__ void __launch_bounds__(THREADS, 1) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
+  extern __shared__ uint8_t raw[];
   __shared__ long long from_row[BM], to_row[BM];             // rows of the pools; -1: none
   const int tid = threadIdx.x, H = a.to.n_kv_head, rank = a.m.head_dim;
   const int h = blockIdx.x % H, tile = blockIdx.x / H % tiles, n = blockIdx.x / H / tiles;
+  uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
+  tc::pdl_wait();                                            // what earlier kernels wrote is there
   const int2 range = token_range(a, n);
   const int t0 = range.x + tile * BM;
   if (t0 >= range.y) return;
@@ -357,63 +357,94 @@ __global__ void __launch_bounds__(THREADS) latent_expand_kernel(const __grid_con
     to_row[tid] = to;
   }
   __syncthreads();
-  const float* pool = static_cast<const float*>(a.m.k_pages);
-  const int row = rank + LATENT_ROPE;
-  // loads: a token's 4 values, and those of 3 products
-  const int am = tid % BM, ak = tid / BM * 4;
-  const float* asrc = from_row[am] >= 0 ? pool + from_row[am] * row + ak : nullptr;
-  const float* bsrc[3];
+  const float* const pool = static_cast<const float*>(a.m.k_pages);
+  float* const keys = static_cast<float*>(a.to.k_pages);
+  float* const values = static_cast<float*>(a.to.v_pages);
+  const int row = rank + LATENT_ROPE, chunks = rank / 32;
+  // copies: 16 bytes of 2 tokens and 6 products a thread and chunk (tokens that are not there: zeros)
+  const int piece = tid % 8, y0 = tid / 8;
+  const float* src[8];
+  uint32_t dst[8];
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int o = am + 64 * i;
-    bsrc[i] = (o < LATENT_KEY ? static_cast<const float*>(a.w_k) + ((long long)h * LATENT_KEY + o) * rank
-                              : static_cast<const float*>(a.w_v) + ((long long)h * LATENT_VALUE + o - LATENT_KEY) * rank) + ak;
+  for (int i = 0; i < 8; ++i) {
+    const int y = y0 + 32 * (i < 2 ? i : i - 2), at = i < 2 ? (y & ~7) + place8(y & 7) : BM + (y & ~15) + place16(y & 15);
+    src[i] = i < 2 ? pool + max(from_row[y], 0ll) * row
+                   : (y < LATENT_KEY ? static_cast<const float*>(a.w_k) + ((long long)h * LATENT_KEY + y) * rank
+                                     : static_cast<const float*>(a.w_v) + ((long long)h * LATENT_VALUE + y - LATENT_KEY) * rank);
+    src[i] += 4 * piece;
+    dst[i] = tc::su32(mem) + at * 128 + ((piece ^ (at & 7)) << 4);
   }
-  float2 acc[4][6] = {};                                     // tokens 8 w + 2 i and the next x products 2 l + 64 j and the next
-  const int lane = tid % 32, w = tid / 32;
-  float4 av = asrc ? four(asrc) : make_float4(0.f, 0.f, 0.f, 0.f), bv[3];
+  const bool none[2] = {from_row[y0] < 0, from_row[y0 + 32] < 0};
+  const auto bring = [&](int k) {
+    if (k < chunks)
 #pragma unroll
-  for (int i = 0; i < 3; ++i) bv[i] = four(bsrc[i]);
-  for (int k0 = 0; k0 < rank; k0 += BK) {
-    as[ak][am] = av.x, as[ak + 1][am] = av.y, as[ak + 2][am] = av.z, as[ak + 3][am] = av.w;
+      for (int i = 0; i < 8; ++i)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst[i] + k % F32_STAGES * F32_STAGE), "l"(src[i] + 32 * k),
+                     "r"(i < 2 && none[i & 1] ? 0 : 16)
+                     : "memory");
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-      bs[ak][am + 64 * i] = bv[i].x, bs[ak + 1][am + 64 * i] = bv[i].y, bs[ak + 2][am + 64 * i] = bv[i].z, bs[ak + 3][am + 64 * i] = bv[i].w;
-    __syncthreads();
-    if (k0 + BK < rank) {
-      if (asrc) av = four(asrc + k0 + BK);
+  for (int k = 0; k < F32_STAGES - 1; ++k) bring(k);
+  for (int i = tid; i < BM * 16; i += THREADS) {             // the rotated half of the keys
+    const int y = i / 16, e = i % 16 * 4;
+    if (to_row[y] >= 0) *reinterpret_cast<float4*>(keys + to_row[y] * 128 + LATENT_KEY + e) = *reinterpret_cast<const float4*>(pool + from_row[y] * row + rank + e);
+  }
+  const int warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4, wm = warp % 2, wn = warp / 2;
+  const int at = place8(g);
+  float sum[2][6][4] = {};                                   // tokens 32 wm + 16 i x columns 8 j of the warp's 48
+  for (int k = 0; k < chunks; ++k) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(F32_STAGES - 2) : "memory");
+    __syncthreads();                                         // the chunk is there for all, and the one before is read
+    bring(k + F32_STAGES - 1);
+    const uint32_t x = tc::su32(mem) + k % F32_STAGES * F32_STAGE, w = x + (BM + 48 * wn) * 128;
+    float part[2][6][4] = {};
 #pragma unroll
-      for (int i = 0; i < 3; ++i) bv[i] = four(bsrc[i] + k0 + BK);
-    }
+    for (int u = 0; u < 2; ++u) {                            // 16 dimensions: two steps, 4 of them in a lane
+      uint32_t hi[2][2][4], lo[2][2][4];
 #pragma unroll
-    for (int k = 0; k < BK; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(&as[k][8 * w]), y = *reinterpret_cast<const float4*>(&as[k][8 * w + 4]);
-      const float2 t2[4] = {make_float2(x.x, x.y), make_float2(x.z, x.w), make_float2(y.x, y.y), make_float2(y.z, y.w)};
+      for (int i = 0; i < 2; ++i) {
+        const float4 p = lds_f4(x + (32 * wm + 16 * i + at) * 128 + (((4 * u + c) ^ at) << 4));
+        const float4 q = lds_f4(x + (32 * wm + 16 * i + 8 + at) * 128 + (((4 * u + c) ^ at) << 4));
+        split(p.x, hi[i][0][0], lo[i][0][0]), split(q.x, hi[i][0][1], lo[i][0][1]), split(p.y, hi[i][0][2], lo[i][0][2]), split(q.y, hi[i][0][3], lo[i][0][3]);
+        split(p.z, hi[i][1][0], lo[i][1][0]), split(q.z, hi[i][1][1], lo[i][1][1]), split(p.w, hi[i][1][2], lo[i][1][2]), split(q.w, hi[i][1][3], lo[i][1][3]);
+      }
 #pragma unroll
-      for (int j = 0; j < 3; ++j) {
-        const float2 b = *reinterpret_cast<const float2*>(&bs[k][2 * lane + 64 * j]);
+      for (int j = 0; j < 6; ++j) {
+        const float4 p = lds_f4(w + (8 * j + at) * 128 + (((4 * u + c) ^ at) << 4));
+        uint4 bh, bl;
+        split(p.x, bh.x, bl.x), split(p.y, bh.y, bl.y), split(p.z, bh.z, bl.z), split(p.w, bh.w, bl.w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[i][2 * j] = fma_pair(t2[i], make_float2(b.x, b.x), acc[i][2 * j]);
-          acc[i][2 * j + 1] = fma_pair(t2[i], make_float2(b.y, b.y), acc[i][2 * j + 1]);
+        for (int i = 0; i < 2; ++i) {
+          mma8(part[i][j], hi[i][0], bh.x, bh.y);
+          mma8(part[i][j], hi[i][1], bh.z, bh.w);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma8(part[i][j], lo[i][0], bh.x, bh.y);
+          mma8(part[i][j], lo[i][1], bh.z, bh.w);
+          mma8(part[i][j], hi[i][0], bl.x, bl.y);
+          mma8(part[i][j], hi[i][1], bl.z, bl.w);
         }
       }
     }
-    __syncthreads();
-  }
-  float* const kp = static_cast<float*>(a.to.k_pages);
-  float* const vp = static_cast<float*>(a.to.v_pages);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const long long to = to_row[8 * w + i], from = from_row[8 * w + i];
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 6; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[i][j][e] += part[i][j][e];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {                              // token 32 wm + 8 i + g: of each two tiles four products
+    const long long to = to_row[32 * wm + 8 * i + g];
     if (to < 0) continue;
-    const auto at = [&](int j) {
-      return i % 2 ? make_float2(acc[i / 2][2 * j].y, acc[i / 2][2 * j + 1].y) : make_float2(acc[i / 2][2 * j].x, acc[i / 2][2 * j + 1].x);
-    };
-    put2(kp + to * 128 + 2 * lane, at(0));
-    put2(vp + to * 128 + 2 * lane, at(1));
-    put2(vp + to * 128 + 64 + 2 * lane, at(2));
-    put2(kp + to * 128 + 64 + 2 * lane, *reinterpret_cast<const float2*>(pool + from * row + rank + 2 * lane));
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      const int o = 48 * wn + 16 * j + 4 * c, b = 2 * (i % 2);
+      const float4 v = make_float4(sum[i / 2][2 * j][b], sum[i / 2][2 * j][b + 1], sum[i / 2][2 * j + 1][b], sum[i / 2][2 * j + 1][b + 1]);
+      *reinterpret_cast<float4*>(o < LATENT_KEY ? keys + to * 128 + o : values + to * 128 + o - LATENT_KEY) = v;
+    }
   }
 }
 
@@ -423,8 +454,11 @@ cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st) {
   if (a.m.dtype == EVO_DTYPE_BF16)
     return a.m.head_dim == 128 ? launch_tiles<128>(a, st) : a.m.head_dim == 256 ? launch_tiles<256>(a, st) : launch_tiles<512>(a, st);
   const int tiles = (a.max_new + BM - 1) / BM;
-  latent_expand_kernel<<<(unsigned)((long long)a.m.n_seq * tiles * a.to.n_kv_head), THREADS, 0, st>>>(a, tiles);
-  return cudaGetLastError();
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(latent_expand_kernel, F32_SMEM, done);
+  if (e != cudaSuccess) return e;
+  Launch launch((unsigned)((long long)a.m.n_seq * tiles * a.to.n_kv_head), THREADS, F32_SMEM, st);
+  return cudaLaunchKernelEx(&launch.cfg, latent_expand_kernel, a, tiles);
 }
 
 }  // namespace evo
