@@ -36,6 +36,7 @@ constexpr int RUN = 16;                            // tokens of a run: a page ho
 template <int RANK, int NR>
 struct Cfg {
   static constexpr int DIMS = RANK + LATENT_ROPE, ROWS = 8 * NR, BOXES = DIMS / 32;
+  static constexpr int UNROLL = RANK == 512 ? 12 : DIMS / 16;   // all of the steps of rank 512 were more code than the instructions' cache holds
   static constexpr int BYTES = RUN * DIMS * 4, Q = DIMS / 16 * NR * 1024;   // a run; the queries' fragments, high and low
   static constexpr int ROOM = (225 * 1024 - 1024 - Q) / BYTES, WARPS = ROOM > 8 ? 8 : ROOM, THREADS = 32 * WARPS;
   static constexpr int SLOTS = ROOM / WARPS > 2 ? 2 : ROOM / WARPS;   // of each warp
@@ -85,15 +86,14 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
   __syncthreads();
   __shared__ __align__(8) uint8_t walk_at[sizeof(Walk<C::ROWS>)];   // one thread's: registers are short
   Walk<C::ROWS>* const walk = reinterpret_cast<Walk<C::ROWS>*>(walk_at);
-  if (tid == 0) new (walk) Walk<C::ROWS>(a, run, sh);
   bool shares = false, dead = false;
+  if (tid == 0) new (walk) Walk<C::ROWS>(a, run, sh);
+  if (tid == 0) fill_segment(a, run, share, *walk, sh.seg[0], shares);
+  __syncthreads();
   int asked = 0;                                             // runs of this warp before this item's
   const int shift = 31 - __clz(a.m.page_tokens);
-  while (true) {
-    if (tid == 0) fill_segment(a, run, share, *walk, sh.seg[0], shares);
-    __syncthreads();
-    const Segment& seg = sh.seg[0];
-    if (!seg.more) break;
+  for (int item = 0; sh.seg[item & 1].more; ++item) {
+    const Segment& seg = sh.seg[item & 1];
     const Tile& t = seg.x.t;
     const int rows = seg.x.rows, r0 = seg.x.r0;
     // this block's piece of the tokens, and of these the ones that every row sees
@@ -117,19 +117,21 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
     for (int j = 0; j < SLOTS; ++j) ask(j, page_of(j));
     int ahead = page_of(SLOTS);
+    if (tid == 0) fill_segment(a, run, share, *walk, sh.seg[(item + 1) & 1], shares);   // while copies are under way
     // queries: the fragments of a step pair, high parts and low parts
+#pragma unroll
+    for (int nr = 0; nr < NR; ++nr) {
+      const int R = r0 + 8 * nr + g;
+      const float* const src = static_cast<const float*>(a.q) + (long long)(t.first + R / a.group) * a.ldq + (long long)(R % a.group) * C::DIMS + 4 * c;
 #pragma unroll 4
-    for (int i = tid; i < STEPS * NR * 32; i += THREADS) {
-      const int l = i % 32, nr = i / 32 % NR, h = i / 32 / NR, R = r0 + 8 * nr + l / 4;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (R < rows)
-        x = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + (long long)(t.first + R / a.group) * a.ldq +
-                                             (long long)(R % a.group) * C::DIMS + 16 * h + 4 * (l % 4));
-      uint4 hi, lo;
-      split(x.x, hi.x, lo.x), split(x.y, hi.y, lo.y), split(x.z, hi.z, lo.z), split(x.w, hi.w, lo.w);
-      uint4* dst = reinterpret_cast<uint4*>(mem + C::RING + (h * NR + nr) * 1024 + l * 16);
-      dst[0] = hi;
-      dst[32] = lo;
+      for (int h = warp; h < STEPS; h += WARPS) {
+        const float4 x = R < rows ? *reinterpret_cast<const float4*>(src + 16 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
+        uint4 hi, lo;
+        split(x.x, hi.x, lo.x), split(x.y, hi.y, lo.y), split(x.z, hi.z, lo.z), split(x.w, hi.w, lo.w);
+        uint4* dst = reinterpret_cast<uint4*>(mem + C::RING + (h * NR + nr) * 1024 + lane * 16);
+        dst[0] = hi;
+        dst[32] = lo;
+      }
     }
     __syncthreads();
 
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
         constexpr int RESTS = NR == 1 ? 4 : 1;                 // sums of the other products: chains of their own, where registers are left
         float hh[NR][4][4] = {}, rest[NR][RESTS][4] = {};
         bool bad0 = false, bad1 = false;
-#pragma unroll
+#pragma unroll(C::UNROLL)
         for (int h = 0; h < STEPS; ++h) {
           const float4 x0 = lds_f4(x + h / 2 * (RUN * 128) + tg * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
           const float4 x1 = lds_f4(x + h / 2 * (RUN * 128) + (8 + tg) * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
@@ -303,31 +305,35 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
       break;
     }
     float* const sums = reinterpret_cast<float*>(mem);         // [WARPS][ROWS][LD], in place of the ring
+    const int warps = min(n, WARPS);                           // those that had a run
+    if (warp < warps)
 #pragma unroll
-    for (int nr = 0; nr < NR; ++nr)
+      for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float l = sum[nr][e];
+        for (int e = 0; e < 2; ++e) {
+          float l = sum[nr][e];
 #pragma unroll
-        for (int y = 4; y < 32; y *= 2) l += __shfl_xor_sync(0xffffffffu, l, y);
-        const int r = 8 * nr + 2 * c + e;
-        if (g == 0) stat[warp][r] = make_float2(top[nr][e], l);
+          for (int y = 4; y < 32; y *= 2) l += __shfl_xor_sync(0xffffffffu, l, y);
+          const int r = 8 * nr + 2 * c + e;
+          if (g == 0) stat[warp][r] = make_float2(top[nr][e], l);
 #pragma unroll
-        for (int b = 0; b < BOXES; ++b)
-          *reinterpret_cast<float4*>(sums + (warp * C::ROWS + r) * C::LD + 32 * b + 4 * g) =
-              make_float4(o[nr][2 * b][e], o[nr][2 * b][2 + e], o[nr][2 * b + 1][e], o[nr][2 * b + 1][2 + e]);
-      }
+          for (int b = 0; b < BOXES; ++b)
+            *reinterpret_cast<float4*>(sums + (warp * C::ROWS + r) * C::LD + 32 * b + 4 * g) =
+                make_float4(o[nr][2 * b][e], o[nr][2 * b][2 + e], o[nr][2 * b + 1][e], o[nr][2 * b + 1][2 + e]);
+        }
     __syncthreads();
     for (int i = tid; i < C::ROWS * RANK / 4; i += THREADS) {
       const int r = i / (RANK / 4), d = i % (RANK / 4) * 4;
       if (r0 + r >= rows) break;
       float m = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) m = fmaxf(m, stat[w][r].x);
+      for (int w = 0; w < WARPS; ++w)
+        if (w < warps) m = fmaxf(m, stat[w][r].x);
       const float ref = m == -INFINITY ? 0.f : m;
       float4 v = {};
 #pragma unroll
       for (int w = 0; w < WARPS; ++w) {
+        if (w >= warps) break;
         const float2 ml = stat[w][r];
         const float4 y = *reinterpret_cast<const float4*>(sums + (w * C::ROWS + r) * C::LD + d);
         const float fw = ex2_approx(ml.x - ref);
