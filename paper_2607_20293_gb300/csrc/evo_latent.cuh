@@ -191,7 +191,10 @@ struct Walk {
       x = fresh ? begin : item_of<N>(a, item);
       fresh = false;
       const int cost = x.cost();
-      if (cost == 0) continue;
+      if (cost == 0) {                             // behind the sequence's rows: so are the others up to the next sequence's
+        if (!run.split) item += (((x.t.n + 1) * a.tiles - item + (int)gridDim.x - 1) / (int)gridDim.x - 1) * (int)gridDim.x;
+        continue;
+      }
       index = item;
       from = skip;
       const int take = min(cost - skip, left);

@@ -355,6 +355,62 @@ def test_attend_strided_rows_and_bounds(torch, B, dtype):
     assert torch.equal(exact, mem.attend(q, w.scale, max_new=9, max_len=260))
 
 
+@pytest.mark.parametrize("dtype,rank", [("bf16", 128), ("bf16", 512), ("fp32", 256)])
+def test_attend_chunks_far_below_their_bound(torch, B, dtype, rank):
+    """max_new left to the number of rows: most of the launch's items are behind their sequences' rows."""
+    news = [0, 1, 260, 0, 2] + [1] * 30 + [37]
+    w = World(torch, [n + 7 * i % 140 for i, n in enumerate(news)], news, 64, rank, 16, dtype, seed=5)
+    mem = w.device(B)
+    w.check_attend(mem.attend(w.q.cuda(), w.scale))
+    assert int(w.status) == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attend_more_items_than_a_block_counts(torch, B, dtype):
+    w = World(torch, [1 + (n * 37) % 200 for n in range(2100)], [1] * 2100, 3, 128, 32, dtype, seed=6)
+    w.check_attend(w.device(B, starts=False).attend(w.q.cuda(), w.scale))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("H", [129, 1000, 1024])
+def test_attend_many_heads(torch, B, dtype, rank, H):
+    w = World(torch, [170, 1, 300], [1, 1, 2], H, rank, 64, dtype, seed=H)
+    mem = w.device(B)
+    w.check_attend(mem.attend(w.q.cuda(), w.scale, max_new=2))
+    w.check_attend(mem.attend(w.q.cuda(), w.scale, max_new=2, window=33), window=33)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("strided", [False, True])
+@pytest.mark.parametrize("window", [0, 60])
+def test_attend_chunks_what_masked_tokens_hold(torch, B, dtype, rank, strided, window):
+    """As above, with chunks of many rows, several items a sequence, and rows behind the last sequence that are no numbers."""
+    m, length, H = 60, 700, 6
+    w = World(torch, [length, length], [m, m], H, rank, 32, dtype, seed=3, spare_rows=30)
+    w.q[2 * m:] = float("nan")
+    for at, column in ((length - 20, 3), (length - 9, rank + 5)):          # rows 40 and 51 are the first that see them
+        w.pages[int(w.table[0, at // 32]), at % 32, column] = float("nan")
+    mem, q = w.device(B), w.q.cuda()
+    buf = torch.full((w.rows, H * (2 * rank + ROPE) + 32), 7.0, dtype=w.t, device="cuda")
+    out = buf[:, H * (rank + ROPE) + 16:-16].unflatten(1, (H, rank))
+    if strided:
+        buf[:, :H * (rank + ROPE)].copy_(q.flatten(1))
+        q = buf[:, :H * (rank + ROPE)].unflatten(1, (H, rank + ROPE))
+    mem.attend(q, w.scale, window=window, max_new=m, out=out)
+    assert (buf[:, H * (rank + ROPE):H * (rank + ROPE) + 16] == 7).all() and (buf[:, -16:] == 7).all() and (out[2 * m:] == 7).all()
+    got = out.double().cpu().numpy()
+    for n in range(2):
+        x, rows = w.dense(n), 40 if n == 0 else m
+        x[np.isnan(x)] = 0
+        want, size, dots = L.attend(w.q[n * m:(n + 1) * m].double().numpy(), x, rank, w.scale, True, window)
+        weight = 2 * (rank + 72) * U * dots + 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+        tol = half(dtype) * np.abs(want) + (1 + half(dtype)) * (weight + length * U) * size + 1e-37
+        assert (np.abs(got[n * m:(n + 1) * m] - want) <= tol)[:rows].all()
+    assert not np.isfinite(got[40:m, :, 3]).any() and not np.isfinite(got[51:m]).any()
+
+
 def test_attend_reports_bad_entries(torch, B):
     for dtype in DTYPES:
         w = World(torch, [40, 40, 40], [1, 1, 1], 4, 128, 16, dtype, max_pages=4, stale=False)
@@ -447,6 +503,18 @@ def test_expand_long_memories(torch, B, dtype):
     e = Expanded(w, B, 128)
     mem.expand(e.w_k.cuda(), e.w_v.cuda(), e.mem)
     e.check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+def test_expand_few_tokens_of_many_sequences(torch, B, dtype, rank):
+    w = World(torch, [(n * 31) % 90 for n in range(170)], [1] * 170, 5, rank, 16, dtype, seed=8)
+    mem = w.device(B)
+    e = Expanded(w, B, 32)
+    first = torch.tensor([max(0, ln - n % 4) for n, ln in enumerate(w.lens)], dtype=torch.int32)
+    mem.expand(e.w_k.cuda(), e.w_v.cuda(), e.mem, first=first.cuda(), max_new=3)
+    e.check(first)
+    assert mem.status() == B.OK
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -552,6 +620,35 @@ def test_calls_in_a_graph_follow_the_lengths(torch, B):
         got = [w.dense(n, w.dpages)[-1, :256] for n in range(2)]
         assert np.array_equal(np.stack(got), c.double().cpu().numpy())
     assert mem.status() == B.OK
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 40])
+def test_two_graphs_of_split_memories(torch, B, dtype, m):
+    """Two captured calls on streams of their own, replayed at once and in turn, over lengths that change in between."""
+    worlds = [World(torch, [4000, 130, 900], [m] * 3, 4, 128, 64, dtype, seed=20 + i, stale=False) for i in range(2)]
+    mems = [w.device(B, starts=False) for w in worlds]
+    qs, outs, graphs = [w.q.cuda() for w in worlds], [None, None], [torch.cuda.CUDAGraph() for _ in range(2)]
+    for mem, q, w in zip(mems, qs, worlds):
+        mem.attend(q, w.scale)
+    torch.cuda.synchronize()
+    for i in range(2):
+        with torch.cuda.graph(graphs[i]):
+            outs[i] = mems[i].attend(qs[i], worlds[i].scale)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for lens in ([4000, 130, 900], [130, 100, 41], [60, 60, 60]):
+        for w in worlds:
+            w.lens = lens
+            w.dlens.copy_(torch.tensor(lens, dtype=torch.int32))
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for s, g in zip(streams, graphs):
+                with torch.cuda.stream(s):
+                    g.replay()
+        torch.cuda.synchronize()
+        for w, out, mem in zip(worlds, outs, mems):
+            w.check_attend(out)
+            assert mem.status() == B.OK
 
 
 def test_streams_and_threads(torch, B):
