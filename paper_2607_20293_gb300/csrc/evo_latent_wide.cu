@@ -272,6 +272,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           return top;
         };
         // (the weights go over the scores of both threads of a row: behind this barrier everybody has his)
+        bool waited = i + 1 < n || i == 0;
         if (bar_softmax_or<SOFTMAX>(less() > far)) {
           if (tid < ROWS) sh.top[tid] = ordered(-INFINITY);
           tmem_load(scores, v);
@@ -286,6 +287,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           l *= down;
           if (i > 0) {
             wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
+            waited = true;
             __syncwarp();
             tc::tc_fence_after();
             if (__any_sync(0xffffffffu, down != 1.f))
@@ -315,6 +317,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         l += all4.x + all4.y;
         tmem_store32(buffer + 32 * half, p);
         tmem_wait_st();
+        // The last output is waited for below.  A parity tells two phases apart, and so the output before has to be done
+        // when that wait begins: the scores that came say so only of the one before that
+        if (!waited) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
         tc::tc_fence_before();
         __syncwarp();
         if (lane == 0) tc::mbar_arrive1(&sh.p_full);

@@ -270,6 +270,20 @@ def test_attend_long(torch, B, dtype, rank, H, m, length):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("H", [1, 3])
+def test_attend_again_and_again(torch, B, dtype, rank, H):
+    """Chunks of one item and of several over memories of some tiles, whole and in pieces: every call gives the same."""
+    news = [187, 156, 0, 125, 94, 180, 149, 118, 187, 33]
+    w = World(torch, [2295 - 97 * n if n % 3 else 187 + n for n in range(len(news))], news, H, rank, 64, dtype, seed=rank)
+    mem, q = w.device(B), w.q.cuda()
+    want = mem.attend(q, w.scale, max_new=187)
+    w.check_attend(want)
+    for _ in range(50):
+        assert torch.equal(mem.attend(q, w.scale, max_new=187), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
 @pytest.mark.parametrize("N", [3, 40, 400])
 def test_attend_many_sequences(torch, B, dtype, rank, N):
     w = World(torch, [1 + (n * 97) % 260 for n in range(N)], [1] * N, 4, rank, 32, dtype, seed=N)
