@@ -8,6 +8,7 @@
 // with other blocks, leave their sums in the workspace and are joined by a second kernel.
 #pragma once
 
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <cstdint>
@@ -44,7 +45,8 @@ struct Segment {
 struct Run {
   int items, split;                                // split: blocks take equal runs of tiles; else whole items, every gridDim-th
   int flat;                                        // queries lie row behind row: an item's come by tiled copies
-  int4* meta;                                      // of each block from which an item goes on to others: its piece's slot (else -1), the last block, the item
+  int by_item;                                     // there are fewer items than blocks: meta is by the item, else by the block that has an item's first tile
+  int4* meta;                                      // of an item that goes on to other blocks: its piece's slot (else -1), the first block, the last, the item
 };
 
 // shared memory of the roles
@@ -346,104 +348,135 @@ __device__ __forceinline__ void fill_segment(const AttendArgs& a, const Run& run
   q.alike = x.first_row.lo == x.last_row.lo && x.first_row.hi == x.last_row.hi;
   if (walk.from == 0 && walk.after > 0) {          // it goes on to the block that has the last of its tiles
     const int end = run_from(share.total, share.blocks, blockIdx.x + 1) + walk.after;
-    run.meta[blockIdx.x] = make_int4(q.slot, block_of(share.total, share.blocks, end - 1), walk.index, 0);
+    run.meta[run.by_item ? walk.index : blockIdx.x] = make_int4(q.slot, blockIdx.x, block_of(share.total, share.blocks, end - 1), walk.index);
     shares = true;
+  } else if (run.by_item && walk.from == 0) {
+    run.meta[walk.index] = make_int4(-1, 0, 0, 0);
   }
 }
 
-// Joins the pieces of the items that blocks share, from the block that has an item's first tile: its piece, and the
-// first of each block behind it up to the last.  RANK / 4 lanes a row, or several such groups that share its pieces
-// (few rows of many pieces would else wait out one load after the other).
+// Joins the pieces of the items that blocks share: that of the block which has an item's first tile, and the first one of each
+// block behind it up to the last.
+struct Pieces {
+  int slot, first, n;             // n: 0, nothing to join
+  SeqRows s;
+  int r0;                         // of the item, in its sequence's rows
+  __device__ __forceinline__ long long at(int p) const { return p == 0 ? slot : 2 * (first + p); }
+};
+template <int N>
+__device__ __forceinline__ Pieces pieces_of(const AttendArgs& a, const Run& run) {
+  tc::pdl_trigger();
+  tc::pdl_wait();
+  Pieces x;
+  int item = blockIdx.x;
+  const int4 m = run.meta[blockIdx.x];
+  if (run.by_item) {                               // its rows are looked up beside its entry, not behind it
+    x.s = seq_rows(a.m, item / a.tiles, a.rows, a.max_new);
+    x.r0 = item % a.tiles * N;
+  }
+  // (an item without rows is nobody's, and has no entry)
+  x.n = (run.by_item && x.r0 >= x.s.count * a.group) || m.x < 0 ? 0 : m.z - m.y + 1;
+  x.slot = m.x, x.first = m.y;
+  if (x.n > 0 && !run.by_item) {
+    item = m.w;
+    x.s = seq_rows(a.m, item / a.tiles, a.rows, a.max_new);
+    x.r0 = item % a.tiles * N;
+  }
+  return x;
+}
+// a row's o and sum, with maximum top, and C further pieces of it
+template <int C, int D>
+__device__ __forceinline__ void join_pieces(float& top, float& sum, float (&o)[D], const float2 (&ml)[C], const float (&y)[C][D]) {
+  float m = top;
+#pragma unroll
+  for (int i = 0; i < C; ++i) m = fmaxf(m, ml[i].x);
+  const float ref = m == -INFINITY ? 0.f : m, f = ex2_approx(top - ref);
+  top = m;
+  sum *= f;
+#pragma unroll
+  for (int e = 0; e < D; ++e) o[e] *= f;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const float g = ex2_approx(ml[i].x - ref);
+    sum = fmaf(ml[i].y, g, sum);
+#pragma unroll
+    for (int e = 0; e < D; ++e) o[e] = fmaf(y[i][e], g, o[e]);
+  }
+}
+
+// RANK / 4 lanes a row, or several such groups that share its pieces.  The loads of several pieces, sums and statistics, are
+// under way at once: a load's time is what bounds this kernel.
 constexpr int JOIN_THREADS = 512;
 template <typename T, int RANK, int N>
-__global__ void __launch_bounds__(JOIN_THREADS) latent_join_kernel(const __grid_constant__ AttendArgs a, const int4* meta, int groups) {
+__global__ void __launch_bounds__(JOIN_THREADS, 1) latent_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Run run, int groups) {
   constexpr int LANES = RANK / 4, AT_ONCE = JOIN_THREADS / LANES;
-  __shared__ float weight[AT_ONCE][SMS];           // of a row's pieces
-  __shared__ float total[AT_ONCE];
+  __shared__ float2 stat[AT_ONCE];
   __shared__ float4 os[AT_ONCE][LANES];
   const int at = threadIdx.x / LANES, lane = threadIdx.x % LANES, group = at % groups, row = at / groups;
   const int r = blockIdx.y * (AT_ONCE / groups) + row;
-  tc::pdl_wait();
-  const int4 m = meta[blockIdx.x];
-  if (m.x < 0) return;
-  const int n = m.z / a.tiles, pieces = m.y - blockIdx.x + 1;
-  const SeqRows s = seq_rows(a.m, n, a.rows, a.max_new);
-  const int R = m.z % a.tiles * N + r;
-  const bool on = r < N && R < s.count * a.group;
-  const auto place = [&](int p) { return (long long)(p == 0 ? m.x : 2 * (blockIdx.x + p)) * N + r; };
-  if (on && group == 0 && lane < 32) {             // a warp a row: its pieces' weights
-    float top = -INFINITY, sum = 0.f;
-    for (int p = lane; p < pieces; p += 32) top = fmaxf(top, a.ml[place(p)].x);
+  const Pieces x = pieces_of<N>(a, run);
+  if (x.n == 0) return;
+  const int R = x.r0 + r;
+  const bool on = r < N && R < x.s.count * a.group;
+  float top = -INFINITY, sum = 0.f, o[4] = {};
+  if (on)
+    for (int p0 = group; p0 < x.n; p0 += 8 * groups) {
+      float2 ml[8];
+      float y[8][4];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    for (int p = lane; p < pieces; p += 32) {
-      const float2 ml = a.ml[place(p)];
-      const float w = ex2_approx(ml.x - (top == -INFINITY ? 0.f : top));
-      weight[row][p] = w;
-      sum = fmaf(ml.y, w, sum);
+      for (int i = 0; i < 8; ++i) {
+        const int p = p0 + i * groups;
+        const long long at = x.at(p) * N + r;
+        const bool there = p < x.n;
+        ml[i] = there ? a.ml[at] : make_float2(-INFINITY, 0.f);
+        const float4 v = there ? *reinterpret_cast<const float4*>(a.part + at * RANK + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+        y[i][0] = v.x, y[i][1] = v.y, y[i][2] = v.z, y[i][3] = v.w;
+      }
+      join_pieces(top, sum, o, ml, y);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) total[row] = sum;
-  }
-  __syncthreads();
-  float4 o = {};
-  if (on) {
-#pragma unroll 8
-    for (int p = group; p < pieces; p += groups) {
-      const float4 y = *reinterpret_cast<const float4*>(a.part + place(p) * RANK + 4 * lane);
-      const float w = weight[row][p];
-      o = make_float4(fmaf(y.x, w, o.x), fmaf(y.y, w, o.y), fmaf(y.z, w, o.z), fmaf(y.w, w, o.w));
-    }
-  }
   if (groups > 1) {
-    os[at][lane] = o;
+    os[at][lane] = make_float4(o[0], o[1], o[2], o[3]);
+    if (lane == 0) stat[at] = make_float2(top, sum);
     __syncthreads();
-    if (group == 0)
+    if (on && group == 0)
       for (int e = 1; e < groups; ++e) {
-        const float4 y = os[at + e][lane];
-        o = make_float4(o.x + y.x, o.y + y.y, o.z + y.z, o.w + y.w);
+        const float4 v = os[at + e][lane];
+        const float2 ml[1] = {stat[at + e]};
+        const float y[1][4] = {{v.x, v.y, v.z, v.w}};
+        join_pieces(top, sum, o, ml, y);
       }
   }
   if (!on || group != 0) return;
-  const float sum = total[row];
-  store_out(static_cast<T*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane, o,
-            sum == 0.f ? 0.f : 1.f / sum);
+  store_out(static_cast<T*>(a.out) + (long long)(x.s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + 4 * lane,
+            make_float4(o[0], o[1], o[2], o[3]), sum == 0.f ? 0.f : 1.f / sum);
 }
 
 // The same for items of 128 rows, whose pieces are [dimension][row]: a thread a row and 8 dimensions
 template <int RANK>
-__global__ void __launch_bounds__(256) latent_join_wide_kernel(const __grid_constant__ AttendArgs a, const int4* meta) {
+__global__ void __launch_bounds__(256) latent_join_wide_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Run run) {
   const int r = threadIdx.x % 128, d = (blockIdx.y * 2 + threadIdx.x / 128) * 8;
-  tc::pdl_wait();
-  const int4 m = meta[blockIdx.x];
-  if (m.x < 0) return;
-  const int n = m.z / a.tiles, pieces = m.y - blockIdx.x + 1;
-  const SeqRows s = seq_rows(a.m, n, a.rows, a.max_new);
-  const int R = m.z % a.tiles * 128 + r;
-  if (R >= s.count * a.group) return;
-  const auto slot = [&](int p) { return (long long)(p == 0 ? m.x : 2 * (blockIdx.x + p)); };
-  float top = -INFINITY, sum = 0.f;
-  for (int p = 0; p < pieces; ++p) top = fmaxf(top, a.ml[slot(p) * 128 + r].x);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float o[8] = {};
-#pragma unroll 2
-  for (int p = 0; p < pieces; ++p) {
-    const float2 ml = a.ml[slot(p) * 128 + r];
-    const float* part = a.part + (slot(p) * RANK + d) * 128 + r;
-    float y[8];
+  const Pieces x = pieces_of<128>(a, run);
+  const int R = x.n == 0 ? 0 : x.r0 + r;
+  if (x.n == 0 || R >= x.s.count * a.group) return;
+  float top = -INFINITY, sum = 0.f, o[8] = {};
+  for (int p0 = 0; p0 < x.n; p0 += 4) {
+    float2 ml[4];
+    float y[4][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = part[e * 128];
-    const float f = ex2_approx(ml.x - ref);
-    sum = fmaf(ml.y, f, sum);
+    for (int i = 0; i < 4; ++i) {
+      const bool there = p0 + i < x.n;
+      ml[i] = there ? a.ml[x.at(p0 + i) * 128 + r] : make_float2(-INFINITY, 0.f);
+      const float* part = a.part + (x.at(p0 + i) * RANK + d) * 128 + r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = fmaf(y[e], f, o[e]);
+      for (int e = 0; e < 8; ++e) y[i][e] = there ? part[e * 128] : 0.f;
+    }
+    join_pieces(top, sum, o, ml, y);
   }
   const float norm = sum == 0.f ? 0.f : 1.f / sum;
   uint32_t v[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[e]) : "f"(o[2 * e + 1] * norm), "f"(o[2 * e] * norm));
-  *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + (long long)(s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + d) =
+  *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + (long long)(x.s.first + R / a.group) * a.ldo + (long long)(R % a.group) * RANK + d) =
       make_uint4(v[0], v[1], v[2], v[3]);
 }
 
@@ -463,20 +496,22 @@ struct Launch {
   }
 };
 inline Run run_of_plan(const AttendArgs& a, const LatentPlan& p, int rows) {
-  return Run{a.m.n_seq * a.tiles, p.splits > 1, 0, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * rows)};
+  const int items = a.m.n_seq * a.tiles;
+  return Run{items, p.splits > 1, 0, items < p.blocks, reinterpret_cast<int4*>(a.ml + 2 * p.blocks * rows)};
 }
 
 template <typename T, int RANK, int N>
 cudaError_t launch_join_of(const AttendArgs& a, const LatentPlan& p, const Run& run, cudaStream_t st) {
+  const int entries = std::min(run.items, p.blocks);
   if constexpr (N == 128) {
-    Launch launch(dim3(p.blocks, RANK / 16), 256, 0, st);
-    return cudaLaunchKernelEx(&launch.cfg, latent_join_wide_kernel<RANK>, a, (const int4*)run.meta);
+    Launch launch(dim3(entries, RANK / 16), 256, 0, st);
+    return cudaLaunchKernelEx(&launch.cfg, latent_join_wide_kernel<RANK>, a, run);
   } else {
     constexpr int AT_ONCE = JOIN_THREADS / (RANK / 4);
     int groups = 1;
     while (groups < AT_ONCE && groups * 8 * run.items < p.blocks) groups *= 2;
-    Launch launch(dim3(p.blocks, (N * groups + AT_ONCE - 1) / AT_ONCE), JOIN_THREADS, 0, st);
-    return cudaLaunchKernelEx(&launch.cfg, latent_join_kernel<T, RANK, N>, a, (const int4*)run.meta, groups);
+    Launch launch(dim3(entries, (N * groups + AT_ONCE - 1) / AT_ONCE), JOIN_THREADS, 0, st);
+    return cudaLaunchKernelEx(&launch.cfg, latent_join_kernel<T, RANK, N>, a, run, groups);
   }
 }
 

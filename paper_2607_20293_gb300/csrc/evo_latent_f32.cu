@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
   }
   __syncwarp();
   tc::pdl_wait();                                            // what earlier kernels wrote is there
-  if (run.split) tc::pdl_trigger();                          // the join may take its places, and waits there
+  tc::pdl_trigger();                               // the next kernel may take the places that become free, and waits there
   const Share share = count_tiles<C::ROWS, THREADS>(a, run, sh);
   __syncthreads();
   __shared__ __align__(8) uint8_t walk_at[sizeof(Walk<C::ROWS>)];   // one thread's: registers are short
@@ -302,6 +302,8 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     dead = __syncthreads_or(dead);
     if (dead) {                                                // a copy did not arrive
       settle(a.m.status);
+      if (tid == 0)                                            // (the join looks at every item's entry)
+        while (sh.seg[(item + 1) & 1].more) fill_segment(a, run, share, *walk, sh.seg[(item + 1) & 1], shares);
       break;
     }
     float* const sums = reinterpret_cast<float*>(mem);         // [WARPS][ROWS][LD], in place of the ring
@@ -353,7 +355,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     tc::fence_async_smem();                                    // before further copies take the place of the sums
     __syncthreads();
   }
-  if (run.split && tid == 0 && !shares) run.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if (run.split && !run.by_item && tid == 0 && !shares) run.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
 }
 
 template <int RANK, int NR>

@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tc::pdl_wait();                                  // what earlier kernels wrote is there
-  if (run.split) tc::pdl_trigger();                // the join may take its places, and waits there
+  tc::pdl_trigger();                               // the next kernel may take the places that become free, and waits there
   const Share share = count_tiles<N, THREADS>(a, run, sh);
   tc::tc_fence_before();
   __syncthreads();
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (after.more && after.n > 0) bring_queries<RANK, N, SOFTMAX>(a, run, queries, after.x, mem, sh);
     }
-    if (run.split && tid == 0 && !shares) run.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (run.split && !run.by_item && tid == 0 && !shares) run.meta[blockIdx.x] = make_int4(-1, 0, 0, 0);
   }
   tc::tc_fence_before();
   __syncthreads();
