@@ -161,10 +161,13 @@ LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, 
                                          : 128;
   p.tiles = (int)((all + p.tile_rows - 1) / p.tile_rows);
   // Items go to the blocks whole where that takes little longer, in tiles of 128 tokens, than equal runs, their
-  // pieces and the join of these
+  // pieces, the join of these, and the caller's time for its launch and the workspace (5 us).  4 / 60 items of 4 tiles,
+  // whole against in runs: 10.3 to 9.2 / 10.8 to 13.1 us (bf16, rank 256, 32 rows), 13.6 to 9.4 / 14.0 to 12.5 (fp32, rank
+  // 128); of 12 tiles: 20.9 to 9.6 / 24.0 to 22.9 and 30.8 to 9.9 / 33.6 to 26.3
   constexpr int SMS = 152, MOST_ITEMS = 2048;      // items that a block counts
+  const int join = m.dtype == EVO_DTYPE_F32 ? (m.head_dim == 512 ? 1 : m.head_dim == 256 ? 2 : 3) : p.tile_rows == 128 ? 3 : m.head_dim == 512 ? 4 : 5;
   const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + 127) / 128);
-  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + (p.tile_rows <= 32 ? 3 : p.tile_rows == 64 ? 5 : 6);
+  const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 2 + join;
   const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
   p.splits = split ? 2 : 1;
   p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
