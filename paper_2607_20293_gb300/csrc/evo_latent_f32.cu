@@ -36,12 +36,13 @@ constexpr int RUN = 16;                            // tokens of a run: a page ho
 template <int RANK, int NR>
 struct Cfg {
   static constexpr int DIMS = RANK + LATENT_ROPE, ROWS = 8 * NR, BOXES = DIMS / 32;
-  static constexpr int UNROLL = RANK == 512 ? 12 : DIMS / 16;   // all of the steps of rank 512 were more code than the instructions' cache holds
+  static constexpr int SHARE = RANK == 512 || (RANK == 256 && NR == 1) ? 2 : 1;   // warps that share a run
   static constexpr int BYTES = RUN * DIMS * 4, Q = DIMS / 16 * NR * 1024;   // a run; the queries' fragments, high and low
-  static constexpr int ROOM = (225 * 1024 - 1024 - Q) / BYTES, WARPS = ROOM > 8 ? 8 : ROOM, THREADS = 32 * WARPS;
-  static constexpr int SLOTS = ROOM / WARPS > 2 ? 2 : ROOM / WARPS;   // of each warp
-  static constexpr int LD = RANK + 4, JOIN = WARPS * ROWS * LD * 4;
-  static constexpr int RING = WARPS * SLOTS * BYTES > JOIN ? WARPS * SLOTS * BYTES : JOIN;
+  static constexpr int ROOM = (225 * 1024 - 1024 - Q - (SHARE == 2 ? 8192 * NR : 0)) / BYTES, TEAMS = ROOM > 8 ? 8 : ROOM, WARPS = TEAMS * SHARE, THREADS = 32 * WARPS;
+  static constexpr int HALF = SHARE == 2 ? WARPS * NR * 32 : 1;
+  static constexpr int SLOTS = ROOM / TEAMS > 2 ? 2 : ROOM / TEAMS;   // of each team
+  static constexpr int LD = RANK + 4, JOIN = TEAMS * ROWS * LD * 4;
+  static constexpr int RING = TEAMS * SLOTS * BYTES > JOIN ? TEAMS * SLOTS * BYTES : JOIN;
   static constexpr int SMEM = 1024 + Q + RING;
   static_assert(SMEM <= 225 * 1024, "");
 };
@@ -59,21 +60,34 @@ __device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo) {
 }
 __device__ __forceinline__ bool odd_number(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
+__device__ __forceinline__ void bar_team(int team) { asm volatile("bar.sync %0, 64;" ::"r"(team + 1) : "memory"); }
+// of a ballot whose bit 4 g + c is a quarter of token t(g): the tokens
+__device__ __forceinline__ uint32_t quarters(uint32_t b) {
+  uint32_t x = 0;
+#pragma unroll
+  for (int y = 0; y < 8; ++y)
+    if (b & 0xfu << (4 * y)) x |= 1u << (y / 2 + 4 * (y % 2));
+  return x;
+}
+
 template <int RANK, int NR>
 __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     latent_f32_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, const __grid_constant__ Run run) {
   using C = Cfg<RANK, NR>;
-  constexpr int WARPS = C::WARPS, THREADS = C::THREADS, SLOTS = C::SLOTS, STEPS = C::DIMS / 16, BOXES = RANK / 32;   // boxes of 32 dimensions of the latent
+  constexpr int WARPS = C::WARPS, TEAMS = C::TEAMS, SHARE = C::SHARE, THREADS = C::THREADS, SLOTS = C::SLOTS;
+  constexpr int STEPS = C::DIMS / 16, MINE = STEPS / SHARE, BOXES = RANK / 32 / SHARE;   // steps of 16 dimensions, and those and the boxes of 32 dimensions of the latent that a warp has
   extern __shared__ uint8_t raw[];
   __shared__ Roles sh;
-  __shared__ __align__(8) uint64_t full[WARPS][SLOTS];
-  __shared__ float2 stat[WARPS][C::ROWS];
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
+  __shared__ __align__(8) uint64_t full[TEAMS][SLOTS];
+  __shared__ float2 stat[TEAMS][C::ROWS];
+  __shared__ float4 half[C::HALF];                          // the warps' parts of their teams' scores
+  __shared__ uint32_t half_bad[WARPS];
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4, team = warp / SHARE, part = warp % SHARE;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   const uint32_t ring = tc::su32(mem), queries = ring + C::RING;
   if (tid == 0) {
     fetch_map(&map);
-    for (int i = 0; i < WARPS * SLOTS; ++i) tc::mbar_init1(&full[0][i], 1);
+    for (int i = 0; i < TEAMS * SLOTS; ++i) tc::mbar_init1(&full[0][i], 1);
     sh.item = run.split ? run.items : blockIdx.x;
     sh.skip = 0;
     sh.tiles = run.split ? 0 : INT_MAX;
@@ -100,14 +114,14 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     const Range all = {max(seg.x.all.lo, seg.key0), seg.n == 0 ? 0 : min(seg.x.all.hi, seg.key0 + seg.n * BK)};
     const int whole_lo = max(seg.x.last_row.lo, all.lo), whole_hi = min(seg.x.first_row.hi, all.hi);
     const int from = all.lo / RUN * RUN, n = max(0, (all.hi - from + RUN - 1) / RUN);
-    // the j-th run of this warp is run i of the piece; only this warp asks for it, waits for it and reads it
-    const auto run_of = [&](int j) { return warp + j * WARPS; };
-    const auto page_of = [&](int j) { return run_of(j) < n ? seq_page(a.m, t.n, (from + run_of(j) * RUN) >> shift) : 0; };
-    const uint32_t mine = ring + warp * (SLOTS * C::BYTES);
+    // the j-th run of this team is run i of the piece; only it waits for it and reads it, and its first warp asks for it
+    const auto run_of = [&](int j) { return team + j * TEAMS; };
+    const auto page_of = [&](int j) { return part == 0 && run_of(j) < n ? seq_page(a.m, t.n, (from + run_of(j) * RUN) >> shift) : 0; };
+    const uint32_t mine = ring + team * (SLOTS * C::BYTES);
     const auto ask = [&](int j, int page) {          // to its slot, a lane a box
-      if (run_of(j) >= n) return;
+      if (part != 0 || run_of(j) >= n) return;
       const int slot = (asked + j) % SLOTS;
-      uint64_t* bar = &full[warp][slot];
+      uint64_t* bar = &full[team][slot];
       if (lane == 0) tc::mbar_expect_tx(bar, C::BYTES);
       __syncwarp();
       if (lane < C::BOXES)
@@ -151,7 +165,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     for (; run_of(j) < n; ++j) {
       const int slot = (asked + j) % SLOTS;
       const uint32_t x = mine + slot * C::BYTES;
-      if (!__all_sync(0xffffffffu, wait_full(tc::su32(&full[warp][slot]), ((asked + j) / SLOTS) & 1))) {
+      if (!__all_sync(0xffffffffu, wait_full(tc::su32(&full[team][slot]), ((asked + j) / SLOTS) & 1))) {
         dead = true;
         break;
       }
@@ -163,8 +177,9 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
         constexpr int RESTS = NR == 1 ? 4 : 1;                 // sums of the other products: chains of their own, where registers are left
         float hh[NR][4][4] = {}, rest[NR][RESTS][4] = {};
         bool bad0 = false, bad1 = false;
-#pragma unroll(C::UNROLL)
-        for (int h = 0; h < STEPS; ++h) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+          const int h = part * MINE + i;
           const float4 x0 = lds_f4(x + h / 2 * (RUN * 128) + tg * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
           const float4 x1 = lds_f4(x + h / 2 * (RUN * 128) + (8 + tg) * 128 + (((4 * (h % 2) + c) ^ tg) << 4));
           if (odd && h < RANK / 16) {
@@ -177,8 +192,8 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr) {
             const uint4 qh = lds128(queries + (h * NR + nr) * 1024 + lane * 16), ql = lds128(queries + (h * NR + nr) * 1024 + 512 + lane * 16);
-            mma8(hh[nr][2 * h % 4], hi[0], qh.x, qh.y);
-            mma8(hh[nr][(2 * h + 1) % 4], hi[1], qh.z, qh.w);
+            mma8(hh[nr][2 * i % 4], hi[0], qh.x, qh.y);
+            mma8(hh[nr][(2 * i + 1) % 4], hi[1], qh.z, qh.w);
             mma8(rest[nr][0], lo[0], qh.x, qh.y);
             mma8(rest[nr][1 % RESTS], hi[0], ql.x, ql.y);
             mma8(rest[nr][2 % RESTS], lo[1], qh.z, qh.w);
@@ -192,19 +207,32 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
             float low = rest[nr][0][e];
 #pragma unroll
             for (int y = 1; y < RESTS; ++y) low += rest[nr][y][e];
-            s[nr][e] = (((hh[nr][0][e] + hh[nr][1][e]) + (hh[nr][2][e] + hh[nr][3][e])) + low) * f;
+            s[nr][e] = ((hh[nr][0][e] + hh[nr][1][e]) + (hh[nr][2][e] + hh[nr][3][e])) + low;
           }
+        if constexpr (SHARE == 2) {                            // the other warp's part of the scores, and of what is no number
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) half[(warp * NR + nr) * 32 + lane] = make_float4(s[nr][0], s[nr][1], s[nr][2], s[nr][3]);
+          const uint32_t bad = odd ? __ballot_sync(0xffffffffu, bad0) : 0, bad8 = odd ? __ballot_sync(0xffffffffu, bad1) : 0;
+          if (odd && lane == 0) half_bad[warp] = quarters(bad) | quarters(bad8) << 8;
+          bar_team(team);
+#pragma unroll
+          for (int nr = 0; nr < NR; ++nr) {
+            const float4 y = half[((warp ^ 1) * NR + nr) * 32 + lane];
+            s[nr][0] += y.x, s[nr][1] += y.y, s[nr][2] += y.z, s[nr][3] += y.w;
+          }
+          if (odd) drop = quarters(bad) | quarters(bad8) << 8 | half_bad[warp ^ 1];
+        } else if (odd) {
+          drop = quarters(__ballot_sync(0xffffffffu, bad0)) | quarters(__ballot_sync(0xffffffffu, bad1)) << 8;
+        }
+#pragma unroll
+        for (int nr = 0; nr < NR; ++nr)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[nr][e] *= f;
         if (odd) {
           const int k1 = k0 + tg, k2 = k1 + 8;
-          const bool out0 = k1 < all.lo || k1 >= all.hi, out1 = k2 < all.lo || k2 >= all.hi;
-          // bit 4 g + c of a ballot: a quarter of token t(g)
-          uint32_t b0 = __ballot_sync(0xffffffffu, bad0 || out0), b1 = __ballot_sync(0xffffffffu, bad1 || out1);
 #pragma unroll
-          for (int y = 0; y < 8; ++y) {
-            const uint32_t at = 0xfu << (4 * y), to = 1u << (y / 2 + 4 * (y % 2));
-            if (b0 & at) drop |= to;
-            if (b1 & at) drop |= to << 8;
-          }
+          for (int y = 0; y < RUN; ++y)
+            if (k0 + y < all.lo || k0 + y >= all.hi) drop |= 1u << y;
 #pragma unroll
           for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
@@ -269,8 +297,8 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
           const int k1 = 8 * z + 2 * c;
-          float4 x0 = lds_f4(x + b * (RUN * 128) + k1 * 128 + ((g ^ (2 * c)) << 4));
-          float4 x1 = lds_f4(x + b * (RUN * 128) + (k1 + 1) * 128 + ((g ^ (2 * c + 1)) << 4));
+          float4 x0 = lds_f4(x + (part * BOXES + b) * (RUN * 128) + k1 * 128 + ((g ^ (2 * c)) << 4));
+          float4 x1 = lds_f4(x + (part * BOXES + b) * (RUN * 128) + (k1 + 1) * 128 + ((g ^ (2 * c + 1)) << 4));
           if (odd) {
             if (drop >> k1 & 1) x0 = make_float4(0.f, 0.f, 0.f, 0.f);
             if (drop >> (k1 + 1) & 1) x1 = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -294,7 +322,8 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[nr][2 * b + j][e] += y[nr][j][e];
       }
-      __syncwarp();                                            // every lane has read the slot
+      if constexpr (SHARE == 2) bar_team(team);                // everybody has read the slot
+      __syncwarp();
       ask(j + SLOTS, ahead);
       ahead = page_of(j + 1 + SLOTS);
     }
@@ -307,8 +336,8 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
       break;
     }
     float* const sums = reinterpret_cast<float*>(mem);         // [WARPS][ROWS][LD], in place of the ring
-    const int warps = min(n, WARPS);                           // those that had a run
-    if (warp < warps)
+    const int teams = min(n, TEAMS);                           // those that had a run
+    if (team < teams)
 #pragma unroll
       for (int nr = 0; nr < NR; ++nr)
 #pragma unroll
@@ -317,10 +346,10 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
           for (int y = 4; y < 32; y *= 2) l += __shfl_xor_sync(0xffffffffu, l, y);
           const int r = 8 * nr + 2 * c + e;
-          if (g == 0) stat[warp][r] = make_float2(top[nr][e], l);
+          if (g == 0 && part == 0) stat[team][r] = make_float2(top[nr][e], l);
 #pragma unroll
           for (int b = 0; b < BOXES; ++b)
-            *reinterpret_cast<float4*>(sums + (warp * C::ROWS + r) * C::LD + 32 * b + 4 * g) =
+            *reinterpret_cast<float4*>(sums + (team * C::ROWS + r) * C::LD + 32 * (part * BOXES + b) + 4 * g) =
                 make_float4(o[nr][2 * b][e], o[nr][2 * b][2 + e], o[nr][2 * b + 1][e], o[nr][2 * b + 1][2 + e]);
         }
     __syncthreads();
@@ -329,13 +358,13 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
       if (r0 + r >= rows) break;
       float m = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w)
-        if (w < warps) m = fmaxf(m, stat[w][r].x);
+      for (int w = 0; w < TEAMS; ++w)
+        if (w < teams) m = fmaxf(m, stat[w][r].x);
       const float ref = m == -INFINITY ? 0.f : m;
       float4 v = {};
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        if (w >= warps) break;
+      for (int w = 0; w < TEAMS; ++w) {
+        if (w >= teams) break;
         const float2 ml = stat[w][r];
         const float4 y = *reinterpret_cast<const float4*>(sums + (w * C::ROWS + r) * C::LD + d);
         const float fw = ex2_approx(ml.x - ref);
