@@ -14,8 +14,8 @@
 // instruction: 101 us for 20,500 tokens of 16 heads).
 //
 // fp32, on mma.sync: a number is split into two of 11 bits and a product taken as three of tf32 (evo_latent_f32.cu).
-// A block has 64 tokens and a head, a warp 32 of these and 48 of its 192 products; rows of 32 dimensions of both
-// arrive in a ring by asynchronous copies.  The matrix unit cuts its sums off: those of 32 dimensions are added in
+// A block has 64 tokens (16 where no sequence has more) and a head, a warp 32 (16) of these and 48 of its 192 products; rows
+// of 32 dimensions of both arrive in a ring by asynchronous copies.  The matrix unit cuts its sums off: those of 32 dimensions are added in
 // fp32.  Rows stand in shared memory in the order that gives the lanes of a 16-byte load different banks, and each
 // lane four products in a row of its tokens.
 #include <algorithm>
@@ -28,7 +28,7 @@
 namespace evo {
 namespace {
 
-constexpr int THREADS = 256, BM = 64, BN = LATENT_KEY + LATENT_VALUE;   // fp32: threads and tokens of a block; products of a head
+constexpr int BN = LATENT_KEY + LATENT_VALUE;        // products of a head
 
 // tokens of sequence n that are written: [lo, hi); what does not fit the call reports itself and gives none
 __device__ __forceinline__ int2 token_range(const LatentExpandArgs& a, int n) {
@@ -316,7 +316,13 @@ cudaError_t launch_tiles(const LatentExpandArgs& a, cudaStream_t st) {
 
 // ---------------------------------------------------------------- fp32
 
-constexpr int F32_STAGES = 4, F32_STAGE = (BM + BN) * 128, F32_SMEM = 1024 + F32_STAGES * F32_STAGE;   // 32 dimensions of a block's rows
+// tokens of a block, of which a warp has 16 MT; a stage is 32 dimensions of the block's rows
+template <int BM>
+struct F32Cfg {
+  static constexpr int MT = BM == 64 ? 2 : 1, WARPS_M = BM / (16 * MT), THREADS = 128 * WARPS_M;
+  static constexpr int STAGES = 4, STAGE = (BM + BN) * 128, SMEM = 1024 + STAGES * STAGE;
+  static constexpr int COPIES = (BM + BN) * 8 / THREADS, TOKENS = BM * 8 / THREADS;   // 16 bytes each, of a thread; those of tokens
+};
 
 __device__ __forceinline__ void mma8(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -334,7 +340,10 @@ __device__ __forceinline__ int place8(int n) { return n / 2 + 4 * (n % 2); }
 // the place of product p of 16: column 2 c + e of tile t is 4 c + 2 t + e
 __device__ __forceinline__ int place16(int p) { return 8 * (p / 2 % 2) + place8(p / 4 * 2 + p % 2); }
 
-__global__ void __launch_bounds__(THREADS, 1) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
+template <int BM>
+__global__ void __launch_bounds__(F32Cfg<BM>::THREADS, BM == 64 ? 1 : 2) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
+  using C = F32Cfg<BM>;
+  constexpr int THREADS = C::THREADS, MT = C::MT, COPIES = C::COPIES, TOKENS = C::TOKENS;
   extern __shared__ uint8_t raw[];
   __shared__ long long from_row[BM], to_row[BM];             // rows of the pools; -1: none
   const int tid = threadIdx.x, H = a.to.n_kv_head, rank = a.m.head_dim;
@@ -363,51 +372,52 @@ __global__ void __launch_bounds__(THREADS, 1) latent_expand_kernel(const __grid_
   float* const keys = static_cast<float*>(a.to.k_pages);
   float* const values = static_cast<float*>(a.to.v_pages);
   const int row = rank + LATENT_ROPE, chunks = rank / 32;
-  // copies: 16 bytes of 2 tokens and 6 products a thread and chunk (tokens that are not there: zeros)
+  // copies: a thread has 16 bytes of its tokens and products in every chunk (tokens that are not there: zeros)
   const int piece = tid % 8, y0 = tid / 8;
-  const float* src[8];
-  uint32_t dst[8];
+  const float* src[COPIES];
+  uint32_t dst[COPIES];
+  bool none[TOKENS];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int y = y0 + 32 * (i < 2 ? i : i - 2), at = i < 2 ? (y & ~7) + place8(y & 7) : BM + (y & ~15) + place16(y & 15);
-    src[i] = i < 2 ? pool + max(from_row[y], 0ll) * row
-                   : (y < LATENT_KEY ? static_cast<const float*>(a.w_k) + ((long long)h * LATENT_KEY + y) * rank
-                                     : static_cast<const float*>(a.w_v) + ((long long)h * LATENT_VALUE + y - LATENT_KEY) * rank);
+  for (int i = 0; i < COPIES; ++i) {
+    const int y = y0 + THREADS / 8 * (i < TOKENS ? i : i - TOKENS), at = i < TOKENS ? (y & ~7) + place8(y & 7) : BM + (y & ~15) + place16(y & 15);
+    src[i] = i < TOKENS ? pool + max(from_row[y], 0ll) * row
+                        : (y < LATENT_KEY ? static_cast<const float*>(a.w_k) + ((long long)h * LATENT_KEY + y) * rank
+                                          : static_cast<const float*>(a.w_v) + ((long long)h * LATENT_VALUE + y - LATENT_KEY) * rank);
     src[i] += 4 * piece;
     dst[i] = tc::su32(mem) + at * 128 + ((piece ^ (at & 7)) << 4);
+    if (i < TOKENS) none[i] = from_row[y] < 0;
   }
-  const bool none[2] = {from_row[y0] < 0, from_row[y0 + 32] < 0};
   const auto bring = [&](int k) {
     if (k < chunks)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst[i] + k % F32_STAGES * F32_STAGE), "l"(src[i] + 32 * k),
-                     "r"(i < 2 && none[i & 1] ? 0 : 16)
+      for (int i = 0; i < COPIES; ++i)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst[i] + k % C::STAGES * C::STAGE), "l"(src[i] + 32 * k),
+                     "r"(i < TOKENS && none[i < TOKENS ? i : 0] ? 0 : 16)
                      : "memory");
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
-  for (int k = 0; k < F32_STAGES - 1; ++k) bring(k);
+  for (int k = 0; k < C::STAGES - 1; ++k) bring(k);
   for (int i = tid; i < BM * 16; i += THREADS) {             // the rotated half of the keys
     const int y = i / 16, e = i % 16 * 4;
     if (to_row[y] >= 0) *reinterpret_cast<float4*>(keys + to_row[y] * 128 + LATENT_KEY + e) = *reinterpret_cast<const float4*>(pool + from_row[y] * row + rank + e);
   }
-  const int warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4, wm = warp % 2, wn = warp / 2;
+  const int warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4, wm = warp % C::WARPS_M, wn = warp / C::WARPS_M;
   const int at = place8(g);
-  float sum[2][6][4] = {};                                   // tokens 32 wm + 16 i x columns 8 j of the warp's 48
+  float sum[MT][6][4] = {};                                  // tokens 16 (MT wm + i) x columns 8 j of the warp's 48
   for (int k = 0; k < chunks; ++k) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(F32_STAGES - 2) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
     __syncthreads();                                         // the chunk is there for all, and the one before is read
-    bring(k + F32_STAGES - 1);
-    const uint32_t x = tc::su32(mem) + k % F32_STAGES * F32_STAGE, w = x + (BM + 48 * wn) * 128;
-    float part[2][6][4] = {};
+    bring(k + C::STAGES - 1);
+    const uint32_t x = tc::su32(mem) + k % C::STAGES * C::STAGE, w = x + (BM + 48 * wn) * 128;
+    float part[MT][6][4] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u) {                            // 16 dimensions: two steps, 4 of them in a lane
-      uint32_t hi[2][2][4], lo[2][2][4];
+      uint32_t hi[MT][2][4], lo[MT][2][4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float4 p = lds_f4(x + (32 * wm + 16 * i + at) * 128 + (((4 * u + c) ^ at) << 4));
-        const float4 q = lds_f4(x + (32 * wm + 16 * i + 8 + at) * 128 + (((4 * u + c) ^ at) << 4));
+      for (int i = 0; i < MT; ++i) {
+        const float4 p = lds_f4(x + (16 * (MT * wm + i) + at) * 128 + (((4 * u + c) ^ at) << 4));
+        const float4 q = lds_f4(x + (16 * (MT * wm + i) + 8 + at) * 128 + (((4 * u + c) ^ at) << 4));
         split(p.x, hi[i][0][0], lo[i][0][0]), split(q.x, hi[i][0][1], lo[i][0][1]), split(p.y, hi[i][0][2], lo[i][0][2]), split(q.y, hi[i][0][3], lo[i][0][3]);
         split(p.z, hi[i][1][0], lo[i][1][0]), split(q.z, hi[i][1][1], lo[i][1][1]), split(p.w, hi[i][1][2], lo[i][1][2]), split(q.w, hi[i][1][3], lo[i][1][3]);
       }
@@ -417,12 +427,12 @@ __global__ void __launch_bounds__(THREADS, 1) latent_expand_kernel(const __grid_
         uint4 bh, bl;
         split(p.x, bh.x, bl.x), split(p.y, bh.y, bl.y), split(p.z, bh.z, bl.z), split(p.w, bh.w, bl.w);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < MT; ++i) {
           mma8(part[i][j], hi[i][0], bh.x, bh.y);
           mma8(part[i][j], hi[i][1], bh.z, bh.w);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < MT; ++i) {
           mma8(part[i][j], lo[i][0], bh.x, bh.y);
           mma8(part[i][j], lo[i][1], bh.z, bh.w);
           mma8(part[i][j], hi[i][0], bl.x, bl.y);
@@ -431,15 +441,15 @@ __global__ void __launch_bounds__(THREADS, 1) latent_expand_kernel(const __grid_
       }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < 6; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[i][j][e] += part[i][j][e];
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {                              // token 32 wm + 8 i + g: of each two tiles four products
-    const long long to = to_row[32 * wm + 8 * i + g];
+  for (int i = 0; i < 2 * MT; ++i) {                         // token 16 MT wm + 8 i + g: of each two tiles four products
+    const long long to = to_row[16 * MT * wm + 8 * i + g];
     if (to < 0) continue;
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
@@ -450,17 +460,22 @@ __global__ void __launch_bounds__(THREADS, 1) latent_expand_kernel(const __grid_
   }
 }
 
+template <int BM>
+cudaError_t launch_f32(const LatentExpandArgs& a, cudaStream_t st) {
+  using C = F32Cfg<BM>;
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = allow_smem(latent_expand_kernel<BM>, C::SMEM, done);
+  if (e != cudaSuccess) return e;
+  const int tiles = (a.max_new + BM - 1) / BM;
+  Launch launch((unsigned)((long long)a.m.n_seq * tiles * a.to.n_kv_head), C::THREADS, C::SMEM, st);
+  return cudaLaunchKernelEx(&launch.cfg, latent_expand_kernel<BM>, a, tiles);
+}
+
 }  // namespace
 
 cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st) {
-  if (a.m.dtype == EVO_DTYPE_BF16)
-    return a.m.head_dim == 128 ? launch_tiles<128>(a, st) : a.m.head_dim == 256 ? launch_tiles<256>(a, st) : launch_tiles<512>(a, st);
-  const int tiles = (a.max_new + BM - 1) / BM;
-  static std::atomic<uint64_t> done{0};
-  const cudaError_t e = allow_smem(latent_expand_kernel, F32_SMEM, done);
-  if (e != cudaSuccess) return e;
-  Launch launch((unsigned)((long long)a.m.n_seq * tiles * a.to.n_kv_head), THREADS, F32_SMEM, st);
-  return cudaLaunchKernelEx(&launch.cfg, latent_expand_kernel, a, tiles);
+  if (a.m.dtype == EVO_DTYPE_F32) return a.max_new <= 16 ? launch_f32<16>(a, st) : launch_f32<64>(a, st);
+  return a.m.head_dim == 128 ? launch_tiles<128>(a, st) : a.m.head_dim == 256 ? launch_tiles<256>(a, st) : launch_tiles<512>(a, st);
 }
 
 }  // namespace evo

@@ -525,9 +525,12 @@ def test_expand_few_tokens_of_many_sequences(torch, B, dtype, rank):
     w = World(torch, [(n * 31) % 90 for n in range(170)], [1] * 170, 5, rank, 16, dtype, seed=8)
     mem = w.device(B)
     e = Expanded(w, B, 32)
-    first = torch.tensor([max(0, ln - n % 4) for n, ln in enumerate(w.lens)], dtype=torch.int32)
-    mem.expand(e.w_k.cuda(), e.w_v.cuda(), e.mem, first=first.cuda(), max_new=3)
-    e.check(first)
+    for most in (3, 16, 17):
+        for p, b in zip(e.pages, e.before):
+            p.copy_(b)
+        first = torch.tensor([max(0, ln - n % (most + 1)) for n, ln in enumerate(w.lens)], dtype=torch.int32)
+        mem.expand(e.w_k.cuda(), e.w_v.cuda(), e.mem, first=first.cuda(), max_new=most)
+        e.check(first)
     assert mem.status() == B.OK
 
 
