@@ -49,13 +49,15 @@ __device__ __forceinline__ int page_or_none(const evo_memory& m, int32_t* status
 
 // ---------------------------------------------------------------- bf16
 
-constexpr int TM = 128, WRITERS = 16, TILE_THREADS = 32 * (WRITERS + 2), STAGE = TM * 128, CHUNK = BN * 128;   // bytes of 64 dimensions of the tokens, of the maps
+constexpr int TM = 128, STAGE = TM * 128;          // tokens of a tile; bytes of 64 of their dimensions
 template <int RANK>
 struct Cfg {
-  static constexpr int CHUNKS = RANK / 64, W = CHUNKS * CHUNK;
+  static constexpr int PARTS = RANK == 512 ? 2 : 1;           // blocks that share a head's products
+  static constexpr int N = BN / PARTS, WRITERS = 16 / PARTS, THREADS = 32 * (WRITERS + 2);
+  static constexpr int CHUNKS = RANK / 64, CHUNK = N * 128, W = CHUNKS * CHUNK;   // bytes of 64 dimensions of the maps, of all
   static constexpr int ROOM = (227 * 1024 - 2048 - W) / STAGE, STAGES = ROOM > 8 ? 8 : ROOM;
   static constexpr int SMEM = 1024 + W + STAGES * STAGE;
-  static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
+  static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
 };
 constexpr int INFOS = 4;                           // tiles that are looked up ahead
 struct Info {
@@ -88,12 +90,13 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b) {
 __device__ __forceinline__ int product_of(int p) { return p & ~31 | (p & 6) << 2 | (p & 24) >> 2 | (p & 1); }
 
 template <int RANK>
-__global__ void __launch_bounds__(TILE_THREADS, 1)
+__global__ void __launch_bounds__(Cfg<RANK>::THREADS, 1)
     latent_expand_tiles_kernel(const __grid_constant__ LatentExpandArgs a, const __grid_constant__ CUtensorMap map, int pairs, int groups) {
   using C = Cfg<RANK>;
+  constexpr int PARTS = C::PARTS, WRITERS = C::WRITERS, CHUNK = C::CHUNK;
   extern __shared__ uint8_t raw[];
   __shared__ Shared sh;
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, H = a.to.n_kv_head, h = blockIdx.x % H;
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, H = a.to.n_kv_head, h = blockIdx.x / PARTS % H, half = blockIdx.x % PARTS;
   uint8_t* const maps = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   uint8_t* const ring = maps + C::W;
   if (tid == 0) fetch_map(&map);
@@ -132,7 +135,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
       ++i;
     };
     // a lane a tile: 32 ranges are looked up at once, and pages a tile ahead of their use
-    for (long long pair0 = blockIdx.x / H; pair0 < pairs; pair0 += 32ll * groups) {
+    for (long long pair0 = blockIdx.x / (PARTS * H); pair0 < pairs; pair0 += 32ll * groups) {
       const long long pair = pair0 + (long long)lane * groups;
       int2 range = make_int2(0, 0);
       int my_t0 = 0;
@@ -179,9 +182,9 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
     // the head's maps, 16 bytes a copy
     constexpr int PIECES = RANK / 8;
 #pragma unroll 4
-    for (int i = tid; i < BN * PIECES; i += TILE_THREADS - 32) {
-      const int p = i / PIECES, j = i % PIECES, o = product_of(p);
-      const __nv_bfloat16* src = (p < LATENT_KEY ? static_cast<const __nv_bfloat16*>(a.w_k) + ((long long)h * LATENT_KEY + o) * RANK
+    for (int i = tid; i < C::N * PIECES; i += C::THREADS - 32) {
+      const int p = i / PIECES, j = i % PIECES, o = product_of(half * C::N + p);
+      const __nv_bfloat16* src = (o < LATENT_KEY ? static_cast<const __nv_bfloat16*>(a.w_k) + ((long long)h * LATENT_KEY + o) * RANK
                                                  : static_cast<const __nv_bfloat16*>(a.w_v) + ((long long)h * LATENT_VALUE + o - LATENT_KEY) * RANK) + 8 * j;
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(tc::su32(maps + j / 8 * CHUNK + p * 128 + ((j % 8 ^ (p & 7)) << 4))), "l"(src)
                    : "memory");
@@ -234,14 +237,15 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
       }
     } else {
       // ---------------------------------------------------------- 96 columns of 32 tokens: warps 0-3 the key and a quarter of
-      // the value, and the rotated half of the key; warps 4-7 the rest; warps 8-15 the same of every second tile.
+      // the value, and the rotated half of the key; warps 4-7 the rest (rank 512: the other block does);
+      // the second half of the warps the same of every second tile.
       // Lane (g, c) has tokens g, g + 8, .. and of each 32 products the 8 from 8 c on
-      const bool second = warp / 4 % 2;
+      const bool second = PARTS == 1 ? warp / 4 % 2 : half;
       const int g = lane / 4, c = lane % 4, shift = 31 - __clz(a.m.page_tokens), to_shift = 31 - __clz(a.to.page_tokens);
       __nv_bfloat16* const keys = static_cast<__nv_bfloat16*>(a.to.k_pages) + 8 * c;
       __nv_bfloat16* const values = static_cast<__nv_bfloat16*>(a.to.v_pages) + 8 * c;
       const __nv_bfloat16* const pool = static_cast<const __nv_bfloat16*>(a.m.k_pages) + RANK + 8 * c;
-      for (int i = warp / 8; info_of(i, info); i += 2) {
+      for (int i = warp / (WRITERS / 2); info_of(i, info); i += 2) {
         long long to[4];                                     // a token's row of either pool, -1: none
         uint4 turned[4][2];                                  // the rotated half of a key
 #pragma unroll
@@ -268,7 +272,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1)
           for (int y = 0; y < 2; ++y) {                      // 16 lanes each
             float v[16];
             __syncwarp();                                    // whole warps before a collective load
-            tmem_ld16x32(tmem + 256 * (i & 1) + (second ? 96 : 0) + 32 * x + ((uint32_t)(32 * (warp % 4) + 16 * y) << 16), v);
+            tmem_ld16x32(tmem + 256 * (i & 1) + (PARTS == 1 && second ? 96 : 0) + 32 * x + ((uint32_t)(32 * (warp % 4) + 16 * y) << 16), v);
 #pragma unroll
             for (int z = 0; z < 2; ++z)
               if (to[2 * y + z] >= 0)
@@ -309,8 +313,8 @@ cudaError_t launch_tiles(const LatentExpandArgs& a, cudaStream_t st) {
   const cudaError_t e = allow_smem(latent_expand_tiles_kernel<RANK>, C::SMEM, done);
   if (e != cudaSuccess) return e;
   const int pairs = a.m.n_seq * (a.max_new / TM + 2);        // a range may begin and end within a tile
-  const int groups = std::max(1, std::min(pairs, 152 / a.to.n_kv_head));
-  Launch launch(groups * a.to.n_kv_head, TILE_THREADS, C::SMEM, st);
+  const int units = a.to.n_kv_head * C::PARTS, groups = std::max(1, std::min(pairs, 152 / units));
+  Launch launch(groups * units, C::THREADS, C::SMEM, st);
   return cudaLaunchKernelEx(&launch.cfg, latent_expand_tiles_kernel<RANK>, a, map, pairs, groups);
 }
 
