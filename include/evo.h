@@ -430,7 +430,7 @@ evo_status evo_memory_attend(const evo_memory* mem, const void* q, int64_t ldq, 
  *             attends over the latents themselves, and the caller multiplies the result by W_v.  For
  *             single tokens and short chunks: a token of the memory is read once for all heads
  *   expanded  evo_latent_expand writes keys and values to an evo_memory, which evo_memory_attend reads.  For
- *             long chunks: 640 operations a (row, head, token) against 4 rank + 128 */
+ *             long chunks: 512 operations a (row, head, token) against 4 rank + 128 */
 typedef struct evo_latent {
   int32_t dtype;            /* EVO_DTYPE_* of rows and pages */
   int32_t n_head;           /* query heads, at most 1024 */
@@ -473,11 +473,13 @@ evo_status evo_latent_append(const evo_latent* lat, const void* c, int64_t ldc, 
  *   out = softmax over the tokens i that a row sees of (scale <q, (c_i | k_i)>) times c_i
  * causal, window, max_new, max_len and scratch are as for evo_memory_attend (evo_latent_scratch_bytes in place of
  * evo_memory_scratch_bytes).  A row that sees no token is zero.  What a masked token holds reaches no row that does
- * not see it.
+ * not see it; a row that sees a value that is not finite has none in that dimension, and may have none at all.
  *   q        device [rows][n_head][rank + 64], ldq elements between rows
  *   out      device [rows][n_head][rank], ldo elements between rows; shares no byte with q or the pages (EVO_ERR_ARG)
  *   scale    of the scores; finite, and so is scale * log2(e) in fp32 (EVO_ERR_ARG)
- * Scores, softmax statistics and sums are fp32.  Deterministic; asynchronous on the stream. */
+ * Scores, softmax statistics and sums are fp32.  With bf16 rows the weights 2^(s - reference) are rounded to bf16 for
+ * their product with the latents (2^-8 of each; their sum is of the unrounded ones).  With fp32 rows a product of two numbers
+ * is off by at most 2^-21 of itself (three tf32 products).  Deterministic; asynchronous on the stream. */
 size_t evo_latent_scratch_bytes(const evo_latent* lat, int32_t rows, int32_t max_new, int32_t max_len);
 evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
                              int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,
@@ -493,7 +495,7 @@ evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, 
  *   mem      dtype of lat and its format (EVO_ERR_UNSUPPORTED otherwise), head_dim 128, n_kv_head = lat's n_head, as many
  *            sequences; its lens and starts are not read, its pages meet no other buffer, and no two tokens of a
  *            call are the same token of the same of its pages
- * Sums are fp32, one rounding.  A range that is not within the memory, or a page entry outside its pool, makes
+ * Sums are fp32 (with fp32 rows of products that are off by at most 2^-21 of themselves), one rounding.  A range that is not within the memory, or a page entry outside its pool, makes
  * EVO_ERR_CORRUPT in lat's status, and no such token is written.  Asynchronous on the stream. */
 evo_status evo_latent_expand(const evo_latent* lat, const void* w_k, const void* w_v, const int32_t* first,
                              int32_t max_new, int32_t max_len, const evo_memory* mem, void* stream);
