@@ -3,7 +3,8 @@
 // for every head h and token of a range, with c the token's latent and k' its rotated key part,
 // written to the token's page of the other memory.
 //
-// bf16, on tcgen05: a block has one head's 192 products (its maps stay in shared memory: 48 to 192 KB) and takes
+// bf16, on tcgen05: a block has one head's 192 products (rank 512: half of them; its maps stay in shared memory: 48 to 96
+// KB, with 192 only two copies would be on the way: 52.7 against 48.0 us for 4 x 2,000 tokens of 20 heads) and takes
 // tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  The last warp looks tiles
 // and pages up, for all, and brings the latents, the one before it issues the products into one of two accumulators,
 // and eight warps each empty one of these, so that what a warp waits for (a tile's pages, tensor memory, room for
@@ -11,13 +12,15 @@
 // that are read, mostly from L2, so the writes bound the kernel, and have to leave as whole lines: accumulators are read
 // 16 tokens by 256 bits, four lanes a token, and the maps' rows stand in shared memory in the order that gives
 // each of these lanes 8 products of its own in a row (a token a lane and 32 bytes a store were 32 lines an
-// instruction: 101 us for 20,500 tokens of 16 heads).
+// instruction: 101 us).  31,800 tokens of 16 heads, rank 256: 57 us, 4.9 TB/s of algorithmic bytes.
 //
 // fp32, on mma.sync: a number is split into two of 11 bits and a product taken as three of tf32 (evo_latent_f32.cu).
 // A block has 64 tokens (16 where no sequence has more) and a head, a warp 32 (16) of these and 48 of its 192 products; rows
-// of 32 dimensions of both arrive in a ring by asynchronous copies.  The matrix unit cuts its sums off: those of 32 dimensions are added in
-// fp32.  Rows stand in shared memory in the order that gives the lanes of a 16-byte load different banks, and each
-// lane four products in a row of its tokens.
+// of 32 dimensions of both arrive in a ring by asynchronous copies.  The matrix unit cuts its sums off: those of 32
+// dimensions are added in fp32.  Rows stand in shared memory in the order that gives the lanes of a 16-byte load different
+// banks, and each lane four products in a row of its tokens.  750 tokens of 64 heads, rank 256: 100 us (fp32
+// multiply-adds: 148), 47 TFLOP/s in three products each, half of what the matrix unit gives them; 68 x 2 tokens of 16
+// heads: 38 us (in blocks of 64 tokens 122).
 #include <algorithm>
 #include <cstdint>
 #include <cuda_bf16.h>

@@ -4,11 +4,17 @@
 //
 // As in the bf16 kernel both products have the memory as their first operand,
 //   S^T = X Q^T (tokens x rows),   O^T += C^T P^T (dimensions x rows)
-// so that the split of a token's values, three instructions each, serves all rows. A block is 8 warps (rank 512: 5) on
-// an item of 8 NR rows, or its run's part of one (evo_latent.cuh).  A warp takes every eighth run of 16 tokens by itself, which
-// arrives in its own one or two slots by tiled bulk copies, so that no barrier of the block is met until the end:
-// while one warp waits for its run the others compute.  Every warp keeps its own maximum
+// so that the split of a token's values, three instructions each, serves all rows. A block is 8 teams (rank 512: 5) of one
+// or two warps on an item of 8 NR rows, or its run's part of one (evo_latent.cuh).  A team takes every eighth (fifth) run of 16
+// tokens by itself, which arrives in its own one or two slots by tiled bulk copies, so that no barrier of the block is met
+// until the end: while one team waits for its run the others compute.  (Slots of all warps' in one ring would let one
+// be two phases ahead of another's wait, which a parity does not show.)  Every team keeps its own maximum
 // (lazy: rescaled only when a score passes it by 2^8) and sums, joined through shared memory.
+//
+// A run's chain of dependent products bounds a team: 14,700 cycles for rank 512 with one warp, whose 408 products need
+// 3,300.  Two warps of a team have half of the dimensions each and exchange their parts of the scores: 206 single tokens of
+// 2 heads over up to 689 tokens 109 -> 84 us (for rank 128 there is nothing to gain: 46.7 / 47.6).  48 single tokens of 8
+// heads over up to 2,050 of rank 256: 35 us, 2.7 TB/s.
 //
 // Fragments are read 16 bytes at a time, because a contraction's index may be permuted at will (lane (g, c) =
 // (lane / 4, lane % 4)):
