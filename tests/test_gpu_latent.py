@@ -668,6 +668,42 @@ def test_two_graphs_of_split_memories(torch, B, dtype, m):
             assert mem.status() == B.OK
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_offsets_beyond_32_bits(torch, B, dtype):
+    """Pools of more than 2^31 values: the same calls on their last pages give the same."""
+    H, rank, page = 4, 512, 128
+    w = World(torch, [300, 129, 40], [1, 60, 1], H, rank, page, dtype, seed=31, stale=False)
+    mem = w.device(B)
+    e = Expanded(w, B, page)
+    far, far_to = 2 ** 31 // (page * (rank + ROPE)) + 5, 2 ** 31 // (page * H * 128) + 5
+    pool = torch.empty(far + len(w.pages), page, rank + ROPE, dtype=w.t, device="cuda")
+    pool[far:] = w.dpages
+    keys, values = (torch.empty(far_to + len(p), H, page, 128, dtype=w.t, device="cuda") for p in e.pages)
+    for big, p in ((keys, e.pages[0]), (values, e.pages[1])):
+        big[far_to:] = p
+    assert min(pool.numel(), keys.numel()) > 2 ** 31
+    starts = w.starts.cuda()
+    large = B.LatentMemory(pool, torch.where(w.dtable >= 0, w.dtable + far, w.dtable), w.dlens, H, starts=starts)
+    to = B.Memory(keys, values, torch.where(e.dtable >= 0, e.dtable + far_to, e.dtable), w.dlens, H, starts=starts, dtype=dtype)
+    c, k, q = w.c.cuda(), w.k.cuda(), w.q.cuda()
+    for m, memory in ((mem, e.mem), (large, to)):
+        m.append(c, k)
+        m.expand(e.w_k.cuda(), e.w_v.cuda(), memory)
+    assert torch.equal(pool[far:], w.dpages)
+    assert torch.equal(keys[far_to:], e.pages[0]) and torch.equal(values[far_to:], e.pages[1])
+    assert torch.equal(large.attend(q, w.scale, max_new=60), mem.attend(q, w.scale, max_new=60))
+    w.check_attend(large.attend(q, w.scale, max_new=60), pages=w.dpages)
+    assert large.status() == B.OK
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m", [1, 33])
+def test_attend_very_long(torch, B, dtype, m):
+    w = World(torch, [150001, m], [m, m], 3, 128, 128, dtype, seed=33)
+    mem = w.device(B, starts=False)
+    w.check_attend(mem.attend(w.q.cuda(), w.scale))
+
+
 def test_streams_and_threads(torch, B):
     w = World(torch, [3000, 1700, 40], [1, 1, 1], 16, 256, 64, "bf16", seed=12)
     mem = w.device(B, starts=False)
