@@ -171,10 +171,8 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     for (; run_of(j) < n; ++j) {
       const int slot = (asked + j) % SLOTS;
       const uint32_t x = mine + slot * C::BYTES;
-      if (!__all_sync(0xffffffffu, wait_full(tc::su32(&full[team][slot]), ((asked + j) / SLOTS) & 1))) {
-        dead = true;
-        break;
-      }
+      // (after a wait in vain the turns go on, without copies: the other warp of the team is met in each)
+      if (!dead) dead = !__all_sync(0xffffffffu, wait_full(tc::su32(&full[team][slot]), ((asked + j) / SLOTS) & 1));
       const int k0 = from + run_of(j) * RUN;
       const bool odd = k0 < whole_lo || k0 + RUN > whole_hi;
       float s[NR][4];
@@ -330,7 +328,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
       }
       if constexpr (SHARE == 2) bar_team(team);                // everybody has read the slot
       __syncwarp();
-      ask(j + SLOTS, ahead);
+      if (!dead) ask(j + SLOTS, ahead);
       ahead = page_of(j + 1 + SLOTS);
     }
     asked += j;
