@@ -171,7 +171,7 @@ LatentPlan plan_latent(const evo_memory& m, int rows, int max_new, int max_len, 
   const int join = m.dtype == EVO_DTYPE_F32 ? (m.head_dim == 512 ? 1 : m.head_dim == 256 ? 2 : 3) : p.tile_rows == 128 ? 3 : m.head_dim == 512 ? 4 : 5;
   const long long items = (long long)m.n_seq * p.tiles, tiles = std::max(1, (keys + 127) / 128);
   const double whole = (double)((items + SMS - 1) / SMS) * (tiles + 2), even = (double)items * tiles / SMS + 2 + join;
-  const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 1) < INT_MAX && even < whole;
+  const bool split = items <= MOST_ITEMS && tiles > 1 && items * (tiles + 3) < INT_MAX && even < whole;
   p.splits = split ? 2 : 1;
   p.blocks = (int)std::min<long long>(SMS, split ? items * tiles : items);
   // sums, and maximum and sum of weights, of two pieces a block; where a block's last item goes on
