@@ -15,12 +15,12 @@
 // instruction: 101 us).  31,800 tokens of 16 heads, rank 256: 57 us, 4.9 TB/s of algorithmic bytes.
 //
 // fp32, on mma.sync: a number is split into two of 11 bits and a product taken as three of tf32 (evo_latent_f32.cu).
-// A block has 64 tokens (16 where no sequence has more) and a head, a warp 32 (16) of these and 48 of its 192 products; rows
-// of 32 dimensions of both arrive in a ring by asynchronous copies.  The matrix unit cuts its sums off: those of 32
-// dimensions are added in fp32.  Rows stand in shared memory in the order that gives the lanes of a 16-byte load different
-// banks, and each lane four products in a row of its tokens.  750 tokens of 64 heads, rank 256: 100 us (fp32
-// multiply-adds: 148), 47 TFLOP/s in three products each, half of what the matrix unit gives them; 68 x 2 tokens of 16
-// heads: 38 us (in blocks of 64 tokens 122).
+// A block has 32 tokens (16 where no sequence has more) and a head, a warp 48 of its 192 products; rows of 32
+// dimensions of both arrive in a ring by asynchronous copies.  Two blocks a SM, so that one computes while the other starts
+// or stores.  The matrix unit cuts its sums off: those of 32 dimensions are added in fp32.  Rows stand in shared memory in
+// the order that gives the lanes of a 16-byte load different banks, and each lane four products in a row of its tokens.
+// The matrix unit bounds it, at three products each: 750 tokens of 64 heads, rank 256, 84 us, 56 TFLOP/s (one block of 64
+// tokens a SM 100, fp32 multiply-adds 148); 68 x 2 tokens of 16 heads 38 us (in blocks of 64 tokens 122).
 #include <algorithm>
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -323,11 +323,11 @@ cudaError_t launch_tiles(const LatentExpandArgs& a, cudaStream_t st) {
 
 // ---------------------------------------------------------------- fp32
 
-// tokens of a block, of which a warp has 16 MT; a stage is 32 dimensions of the block's rows
+// BM tokens a block; a stage is 32 dimensions of its rows, of which two or three are on the way while one is used
 template <int BM>
 struct F32Cfg {
-  static constexpr int MT = BM == 64 ? 2 : 1, WARPS_M = BM / (16 * MT), THREADS = 128 * WARPS_M;
-  static constexpr int STAGES = 4, STAGE = (BM + BN) * 128, SMEM = 1024 + STAGES * STAGE;
+  static constexpr int MT = BM / 16, THREADS = 128, STAGES = BM == 16 ? 4 : 3;
+  static constexpr int STAGE = (BM + BN) * 128, SMEM = 1024 + STAGES * STAGE;
   static constexpr int COPIES = (BM + BN) * 8 / THREADS, TOKENS = BM * 8 / THREADS;   // 16 bytes each, of a thread; those of tokens
 };
 
@@ -348,7 +348,7 @@ __device__ __forceinline__ int place8(int n) { return n / 2 + 4 * (n % 2); }
 __device__ __forceinline__ int place16(int p) { return 8 * (p / 2 % 2) + place8(p / 4 * 2 + p % 2); }
 
 template <int BM>
-__global__ void __launch_bounds__(F32Cfg<BM>::THREADS, BM == 64 ? 1 : 2) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
+__global__ void __launch_bounds__(F32Cfg<BM>::THREADS, 2) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
   using C = F32Cfg<BM>;
   constexpr int THREADS = C::THREADS, MT = C::MT, COPIES = C::COPIES, TOKENS = C::TOKENS;
   extern __shared__ uint8_t raw[];
@@ -409,22 +409,22 @@ __global__ void __launch_bounds__(F32Cfg<BM>::THREADS, BM == 64 ? 1 : 2) latent_
     const int y = i / 16, e = i % 16 * 4;
     if (to_row[y] >= 0) *reinterpret_cast<float4*>(keys + to_row[y] * 128 + LATENT_KEY + e) = *reinterpret_cast<const float4*>(pool + from_row[y] * row + rank + e);
   }
-  const int warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4, wm = warp % C::WARPS_M, wn = warp / C::WARPS_M;
+  const int warp = tid / 32, lane = tid % 32, g = lane / 4, c = lane % 4;
   const int at = place8(g);
-  float sum[MT][6][4] = {};                                  // tokens 16 (MT wm + i) x columns 8 j of the warp's 48
+  float sum[MT][6][4] = {};                                  // tokens 16 i x columns 8 j of the warp's 48
   for (int k = 0; k < chunks; ++k) {
     asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 2) : "memory");
     __syncthreads();                                         // the chunk is there for all, and the one before is read
     bring(k + C::STAGES - 1);
-    const uint32_t x = tc::su32(mem) + k % C::STAGES * C::STAGE, w = x + (BM + 48 * wn) * 128;
+    const uint32_t x = tc::su32(mem) + k % C::STAGES * C::STAGE, w = x + (BM + 48 * warp) * 128;
     float part[MT][6][4] = {};
 #pragma unroll
     for (int u = 0; u < 2; ++u) {                            // 16 dimensions: two steps, 4 of them in a lane
       uint32_t hi[MT][2][4], lo[MT][2][4];
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        const float4 p = lds_f4(x + (16 * (MT * wm + i) + at) * 128 + (((4 * u + c) ^ at) << 4));
-        const float4 q = lds_f4(x + (16 * (MT * wm + i) + 8 + at) * 128 + (((4 * u + c) ^ at) << 4));
+        const float4 p = lds_f4(x + (16 * i + at) * 128 + (((4 * u + c) ^ at) << 4));
+        const float4 q = lds_f4(x + (16 * i + 8 + at) * 128 + (((4 * u + c) ^ at) << 4));
         split(p.x, hi[i][0][0], lo[i][0][0]), split(q.x, hi[i][0][1], lo[i][0][1]), split(p.y, hi[i][0][2], lo[i][0][2]), split(q.y, hi[i][0][3], lo[i][0][3]);
         split(p.z, hi[i][1][0], lo[i][1][0]), split(q.z, hi[i][1][1], lo[i][1][1]), split(p.w, hi[i][1][2], lo[i][1][2]), split(q.w, hi[i][1][3], lo[i][1][3]);
       }
@@ -455,12 +455,12 @@ __global__ void __launch_bounds__(F32Cfg<BM>::THREADS, BM == 64 ? 1 : 2) latent_
         for (int e = 0; e < 4; ++e) sum[i][j][e] += part[i][j][e];
   }
 #pragma unroll
-  for (int i = 0; i < 2 * MT; ++i) {                         // token 16 MT wm + 8 i + g: of each two tiles four products
-    const long long to = to_row[16 * MT * wm + 8 * i + g];
+  for (int i = 0; i < 2 * MT; ++i) {                         // token 8 i + g: of each two tiles four products
+    const long long to = to_row[8 * i + g];
     if (to < 0) continue;
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      const int o = 48 * wn + 16 * j + 4 * c, b = 2 * (i % 2);
+      const int o = 48 * warp + 16 * j + 4 * c, b = 2 * (i % 2);
       const float4 v = make_float4(sum[i / 2][2 * j][b], sum[i / 2][2 * j][b + 1], sum[i / 2][2 * j + 1][b], sum[i / 2][2 * j + 1][b + 1]);
       *reinterpret_cast<float4*>(o < LATENT_KEY ? keys + to * 128 + o : values + to * 128 + o - LATENT_KEY) = v;
     }
@@ -481,7 +481,7 @@ cudaError_t launch_f32(const LatentExpandArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st) {
-  if (a.m.dtype == EVO_DTYPE_F32) return a.max_new <= 16 ? launch_f32<16>(a, st) : launch_f32<64>(a, st);
+  if (a.m.dtype == EVO_DTYPE_F32) return a.max_new <= 16 ? launch_f32<16>(a, st) : launch_f32<32>(a, st);
   return a.m.head_dim == 128 ? launch_tiles<128>(a, st) : a.m.head_dim == 256 ? launch_tiles<256>(a, st) : launch_tiles<512>(a, st);
 }
 
