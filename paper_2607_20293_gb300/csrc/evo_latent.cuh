@@ -372,7 +372,6 @@ struct Pieces {
 };
 template <int N>
 __device__ __forceinline__ Pieces pieces_of(const AttendArgs& a, const Run& run) {
-  tc::pdl_trigger();
   tc::pdl_wait();
   Pieces x;
   int item = blockIdx.x;

@@ -118,7 +118,6 @@ __global__ void __launch_bounds__(Cfg<RANK>::THREADS, 1)
   tc::tc_fence_after();
   const uint32_t tmem = sh.tmem;
   tc::pdl_wait();                                            // what earlier kernels wrote is there
-  tc::pdl_trigger();
 
   if (warp == WRITERS + 1) {
     // ------------------------------------------------------------ tiles, pages and copies
@@ -357,7 +356,6 @@ __global__ void __launch_bounds__(F32Cfg<BM>::THREADS, 2) latent_expand_kernel(c
   const int h = blockIdx.x % H, tile = blockIdx.x / H % tiles, n = blockIdx.x / H / tiles;
   uint8_t* const mem = raw + ((1024u - (tc::su32(raw) & 1023u)) & 1023u);
   tc::pdl_wait();                                            // what earlier kernels wrote is there
-  tc::pdl_trigger();
   const int2 range = token_range(a, n);
   const int t0 = range.x + tile * BM;
   if (t0 >= range.y) return;

@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
   }
   __syncwarp();
   tc::pdl_wait();                                            // what earlier kernels wrote is there
-  tc::pdl_trigger();                               // the next kernel may take the places that become free, and waits there
+  if (run.split) tc::pdl_trigger();                // the join may take the places that become free, and waits there
   const Share share = count_tiles<C::ROWS, THREADS>(a, run, sh);
   __syncthreads();
   __shared__ __align__(8) uint8_t walk_at[sizeof(Walk<C::ROWS>)];   // one thread's: registers are short

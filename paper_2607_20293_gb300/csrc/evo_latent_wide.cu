@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   tc::pdl_wait();                                  // what earlier kernels wrote is there
-  tc::pdl_trigger();                               // the next kernel may take the places that become free, and waits there
+  if (run.split) tc::pdl_trigger();                // the join may take the places that become free, and waits there
   const Share share = count_tiles<N, THREADS>(a, run, sh);
   tc::tc_fence_before();
   __syncthreads();
