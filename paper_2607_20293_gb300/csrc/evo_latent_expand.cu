@@ -3,8 +3,8 @@
 // for every head h and token of a range, with c the token's latent and k' its rotated key part,
 // written to the token's page of the other memory.
 //
-// bf16, on tcgen05: a block has one head's 192 products (rank 512: half of them; its maps stay in shared memory: 48 to 96
-// KB, with 192 only two copies would be on the way: 52.7 against 48.0 us for 4 x 2,000 tokens of 20 heads) and takes
+// bf16, on tcgen05: a block has one head's 192 products (rank 512, large pages: half of them; its maps stay in
+// shared memory, 48 to 192 KB, and with 192 only two copies are on the way) and takes
 // tiles of 128 tokens, whose latents arrive 64 dimensions at a time by tiled bulk copies.  The last warp looks tiles
 // and pages up, for all, and brings the latents, the one before it issues the products into one of two accumulators,
 // and eight warps each empty one of these, so that what a warp waits for (a tile's pages, tensor memory, room for
@@ -53,9 +53,8 @@ __device__ __forceinline__ int page_or_none(const evo_memory& m, int32_t* status
 // ---------------------------------------------------------------- bf16
 
 constexpr int TM = 128, STAGE = TM * 128;          // tokens of a tile; bytes of 64 of their dimensions
-template <int RANK>
+template <int RANK, int PARTS>
 struct Cfg {
-  static constexpr int PARTS = RANK == 512 ? 2 : 1;           // blocks that share a head's products
   static constexpr int N = BN / PARTS, WRITERS = 16 / PARTS, THREADS = 32 * (WRITERS + 2);
   static constexpr int CHUNKS = RANK / 64, CHUNK = N * 128, W = CHUNKS * CHUNK;   // bytes of 64 dimensions of the maps, of all
   static constexpr int ROOM = (227 * 1024 - 2048 - W) / STAGE, STAGES = ROOM > 8 ? 8 : ROOM;
@@ -92,11 +91,11 @@ __device__ __forceinline__ uint32_t pair_of(float a, float b) {
 // the product (0 .. 63 of the key, 64 .. of the value) that stands in column p of the accumulator: a lane's 8 in a row
 __device__ __forceinline__ int product_of(int p) { return p & ~31 | (p & 6) << 2 | (p & 24) >> 2 | (p & 1); }
 
-template <int RANK>
-__global__ void __launch_bounds__(Cfg<RANK>::THREADS, 1)
+template <int RANK, int PARTS>
+__global__ void __launch_bounds__(Cfg<RANK, PARTS>::THREADS, 1)
     latent_expand_tiles_kernel(const __grid_constant__ LatentExpandArgs a, const __grid_constant__ CUtensorMap map, int pairs, int groups) {
-  using C = Cfg<RANK>;
-  constexpr int PARTS = C::PARTS, WRITERS = C::WRITERS, CHUNK = C::CHUNK;
+  using C = Cfg<RANK, PARTS>;
+  constexpr int WRITERS = C::WRITERS, CHUNK = C::CHUNK;
   extern __shared__ uint8_t raw[];
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, H = a.to.n_kv_head, h = blockIdx.x / PARTS % H, half = blockIdx.x % PARTS;
@@ -306,18 +305,18 @@ __global__ void __launch_bounds__(Cfg<RANK>::THREADS, 1)
   if (warp == 0) tc::tmem_dealloc(tmem, 512);
 }
 
-template <int RANK>
+template <int RANK, int PARTS>
 cudaError_t launch_tiles(const LatentExpandArgs& a, cudaStream_t st) {
-  using C = Cfg<RANK>;
+  using C = Cfg<RANK, PARTS>;
   CUtensorMap map;
   if (!latent_map(&map, a.m, a.m.page_tokens)) return cudaErrorInvalidValue;
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = allow_smem(latent_expand_tiles_kernel<RANK>, C::SMEM, done);
+  const cudaError_t e = allow_smem(latent_expand_tiles_kernel<RANK, PARTS>, C::SMEM, done);
   if (e != cudaSuccess) return e;
   const int pairs = a.m.n_seq * (a.max_new / TM + 2);        // a range may begin and end within a tile
-  const int units = a.to.n_kv_head * C::PARTS, groups = std::max(1, std::min(pairs, 152 / units));
+  const int units = a.to.n_kv_head * PARTS, groups = std::max(1, std::min(pairs, 152 / units));
   Launch launch(groups * units, C::THREADS, C::SMEM, st);
-  return cudaLaunchKernelEx(&launch.cfg, latent_expand_tiles_kernel<RANK>, a, map, pairs, groups);
+  return cudaLaunchKernelEx(&launch.cfg, latent_expand_tiles_kernel<RANK, PARTS>, a, map, pairs, groups);
 }
 
 // ---------------------------------------------------------------- fp32
@@ -480,7 +479,11 @@ cudaError_t launch_f32(const LatentExpandArgs& a, cudaStream_t st) {
 
 cudaError_t launch_latent_expand(const LatentExpandArgs& a, cudaStream_t st) {
   if (a.m.dtype == EVO_DTYPE_F32) return a.max_new <= 16 ? launch_f32<16>(a, st) : launch_f32<32>(a, st);
-  return a.m.head_dim == 128 ? launch_tiles<128>(a, st) : a.m.head_dim == 256 ? launch_tiles<256>(a, st) : launch_tiles<512>(a, st);
+  if (a.m.head_dim == 128) return launch_tiles<128, 1>(a, st);
+  if (a.m.head_dim == 256) return launch_tiles<256, 1>(a, st);
+  // two blocks a head bring every tile twice: not where it comes in many small copies (4 x 2,000 tokens of 20 heads, one
+  // against two: pages of 128 53.2 / 46.0 us, of 32 54.1 / 57.1, of 16 56.8 / 73.7)
+  return a.m.page_tokens >= 64 ? launch_tiles<512, 2>(a, st) : launch_tiles<512, 1>(a, st);
 }
 
 }  // namespace evo
