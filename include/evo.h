@@ -479,7 +479,8 @@ evo_status evo_latent_append(const evo_latent* lat, const void* c, int64_t ldc, 
  *   scale    of the scores; finite, and so is scale * log2(e) in fp32 (EVO_ERR_ARG)
  * Scores, softmax statistics and sums are fp32.  With bf16 rows the weights 2^(s - reference) are rounded to bf16 for
  * their product with the latents (2^-8 of each; their sum is of the unrounded ones).  With fp32 rows a product of two numbers
- * is off by at most 2^-21 of itself (three tf32 products).  Deterministic; asynchronous on the stream. */
+ * is off by at most 2^-21 of itself (three tf32 products; numbers from 2^128 - 2^116 on count as infinite).  Deterministic;
+ * asynchronous on the stream. */
 size_t evo_latent_scratch_bytes(const evo_latent* lat, int32_t rows, int32_t max_new, int32_t max_len);
 evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, int32_t rows, int32_t max_new,
                              int32_t max_len, float scale, int32_t causal, int32_t window, void* out, int64_t ldo,

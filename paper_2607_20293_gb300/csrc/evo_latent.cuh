@@ -1,11 +1,15 @@
-// What the tcgen05 kernels of attention over a latent memory share: items and the runs of tiles that
-// resident blocks take of them, the copies of tiles, and wrappers.
+// What the kernels of attention over a latent memory share: items and the runs of tiles that resident
+// blocks take of them, the join of what they leave, the copies of the tcgen05 kernels, and wrappers.
 //
 // An item is a number of rows (tokens of a chunk times heads) of one sequence with the tokens of the memory that
 // any of them sees, in tiles of 128.  Blocks stay resident, one a SM.  Where whole items would not fill
 // them evenly, the tiles of all items are counted (every block does so, by itself) and each block takes an equal run of
 // them, so that sequences of different lengths end at the same time; the first and the last item of a run are shared
 // with other blocks, leave their sums in the workspace and are joined by a second kernel.
+//
+// The join is bound by the time of a load after another: a row's sums and statistics of several pieces are read at once, and
+// there is a block only for what may be shared (one token of 16,389 in 129 pieces: 3.5 us of 11.3; 7 with a load behind
+// the other).
 #pragma once
 
 #include <algorithm>

@@ -17,7 +17,7 @@
 // next item while the softmax still writes this one's output.
 //
 // The memory's bytes bound it: 64 single tokens of 16 heads over up to 8,192 tokens of rank 512 take 85 us, 5.2 TB/s (77 %
-// of a copy's rate; the first tiles, the pieces and their join are the rest), 32 tokens of 64 heads over rank 256 41 us, 3.0 TB/s:
+// of a copy's rate; the first tiles, the pieces and their join are the rest), 32 tokens of 64 heads over rank 256 39 us, 3.2 TB/s:
 // with 64 rows two tiles fit the ring, and a tile's slots come free only behind its softmax.
 //
 // The running maximum is lazy: a row's reference is raised only when a score passes it by 2^8, so that

@@ -11,7 +11,7 @@
 // A thread of the softmax has a row and half of a tile's 128 tokens.  A tile's products take 2,304 cycles for
 // rank 256 at a library product's rate, 128 rows by 16 steps of 640 + 256 dimensions, a tile 3,570: with two in the ring
 // the next tile's copies wait for this one's output every other time.  4 chunks of up to 250 tokens of 16 heads over 4,096
-// tokens each: 69 us, 0.88 PFLOP/s; 64 chunks of 16 tokens of 8 heads over up to 2,050: 35 us, of which start, pieces and
+// tokens each: 67 us, 0.91 PFLOP/s; 64 chunks of 16 tokens of 8 heads over up to 2,050: 31 us, of which start, pieces and
 // join are two thirds.
 //
 // Items, runs, references, roundings and masks are as in evo_latent_tiles.cu.
