@@ -61,7 +61,7 @@ struct Run {
 
 // shared memory of the roles
 struct Roles {
-  uint64_t full[6], empty[6], part_full[6], part_empty[6], s_full[2], p_full, o_full, q_full;
+  uint64_t full[6], empty[6], part_full[6], part_empty[6], s_full[2], p_full[2], o_full, q_full;
   uint32_t bad[4];
   uint32_t tmem;
   int dead, item, skip;                            // the first item's number, and the tiles of it that others take

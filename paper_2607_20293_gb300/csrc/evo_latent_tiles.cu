@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], 1);
     for (int i = 0; i < PARTS; ++i) tc::mbar_init1(&sh.part_full[i], 1), tc::mbar_init1(&sh.part_empty[i], 1);
     tc::mbar_init1(&sh.s_full[0], 1), tc::mbar_init1(&sh.s_full[1], 1);
-    tc::mbar_init1(&sh.p_full, C::WARPS);          // a warp each
+    tc::mbar_init1(&sh.p_full[0], C::WARPS);          // a warp each
     tc::mbar_init1(&sh.q_full, run.flat ? 1 : C::WARPS);
     tc::mbar_init1(&sh.o_full, 1);
     sh.dead = 0;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
                    kp = (uint32_t)rows_desc + (tc::su32(parts) >> 4), w = (uint32_t)w_desc + (tc::su32(weights) >> 4);
     const uint32_t full = tc::su32(sh.full), empty = tc::su32(sh.empty), part_full = tc::su32(sh.part_full),
                    part_empty = tc::su32(sh.part_empty), dead_word = tc::su32(&sh.dead);
-    const uint32_t s_full = tc::su32(sh.s_full), p_full = tc::su32(&sh.p_full), o_full = tc::su32(&sh.o_full);
+    const uint32_t s_full = tc::su32(sh.s_full), p_full = tc::su32(sh.p_full), o_full = tc::su32(&sh.o_full);
     uint32_t s_slot = 0, s_phase = 0, s_part = 0, s_part_phase = 0, o_slot = 0;
     const auto wait = [&](uint32_t bar, uint32_t parity) {
       if (!tc::mbar_test(bar, parity)) wait_slow(bar, parity, dead_word);
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         tc::fence_async_smem();
         tc::tc_fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive1(&sh.p_full);
+        if (lane == 0) tc::mbar_arrive1(&sh.p_full[0]);
       }
       // the next item's queries take the place of these, whose scores are all there
       if (after.more && after.n > 0) bring_queries<RANK, N, SOFTMAX>(a, run, queries, after.x, mem, sh);

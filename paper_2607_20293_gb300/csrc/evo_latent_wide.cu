@@ -83,7 +83,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int i = 0; i < SLOTS; ++i) tc::mbar_init1(&sh.full[i], 1), tc::mbar_init1(&sh.empty[i], 1);
     for (int i = 0; i < PARTS; ++i) tc::mbar_init1(&sh.part_full[i], 1), tc::mbar_init1(&sh.part_empty[i], 1);
     tc::mbar_init1(&sh.s_full[0], 1), tc::mbar_init1(&sh.s_full[1], 1);
-    tc::mbar_init1(&sh.p_full, WARPS);             // a warp each
+    // a warp each; one for even and one for odd tiles: the softmax may end a tile more before a late test of the first, and
+    // two phases further on its parity would say that nothing has come
+    tc::mbar_init1(&sh.p_full[0], WARPS), tc::mbar_init1(&sh.p_full[1], WARPS);
     tc::mbar_init1(&sh.q_full, run.flat ? 1 : WARPS);
     tc::mbar_init1(&sh.o_full, 1);
     sh.dead = 0;
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                    kp = (uint32_t)rows_desc + (tc::su32(parts) >> 4);
     const uint32_t full = tc::su32(sh.full), empty = tc::su32(sh.empty), part_full = tc::su32(sh.part_full),
                    part_empty = tc::su32(sh.part_empty), dead_word = tc::su32(&sh.dead);
-    const uint32_t s_full = tc::su32(sh.s_full), p_full = tc::su32(&sh.p_full), o_full = tc::su32(&sh.o_full);
+    const uint32_t s_full = tc::su32(sh.s_full), p_full = tc::su32(sh.p_full), o_full = tc::su32(&sh.o_full);
     uint32_t s_slot = 0, s_phase = 0, s_part = 0, s_part_phase = 0, o_slot = 0;
     const auto wait = [&](uint32_t bar, uint32_t parity) {
       if (!tc::mbar_test(bar, parity)) wait_slow(bar, parity, dead_word);
@@ -166,12 +168,12 @@ __global__ void __launch_bounds__(THREADS, 1)
       scores(g);
       for (int i = 0; i < n; ++i, ++g) {
         bool early = i + 1 >= n, done = g == 0;    // done: the output before this one is
-        for (const long long since = clock64(); !early && !test(p_full, g & 1);) {
+        for (const long long since = clock64(); !early && !test(p_full + 8 * (g & 1), (g >> 1) & 1);) {
           early = test(part_full + 8 * s_part, s_part_phase) && (done || test(o_full, (g - 1) & 1));
           if (early) scores(g + 1), done = true;
           else if (clock64() - since > WAIT_CYCLES_DEFAULT) break;   // (the wait below reports it)
         }
-        wait(p_full, g & 1);
+        wait(p_full + 8 * (g & 1), (g >> 1) & 1);
         if (!done) wait(o_full, (g - 1) & 1);
         tc::tc_fence_after();
         dead = __any_sync(0xffffffffu, tc::block_dead(dead_word));
@@ -325,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!waited) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
         tc::tc_fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive1(&sh.p_full);
+        if (lane == 0) tc::mbar_arrive1(&sh.p_full[g & 1]);
       }
       // a row's sum from its two threads
       if (half == 1) sh.top[r] = __float_as_int(l);

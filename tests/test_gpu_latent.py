@@ -732,6 +732,28 @@ def test_streams_and_threads(torch, B):
         mem.attend(w.q, w.scale)                                          # host queries
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+def test_calls_of_three_streams_at_once(torch, B, dtype, rank):
+    """Chunks of several items while the GPU is shared: warps of a block lose their time to others', and wait for one another."""
+    worlds = [World(torch, [1100 - 13 * n for n in range(40)], [m] * 40, 5, rank, page, dtype, seed=50 + m, stale=False)
+              for m, page in ((32, 64), (20, 16), (3, 128))]
+    mems, qs = [w.device(B, starts=False) for w in worlds], [w.q.cuda() for w in worlds]
+    want = [m.attend(q, w.scale) for m, q, w in zip(mems, qs, worlds)]
+    worlds[0].check_attend(want[0])
+    streams = [torch.cuda.Stream() for _ in worlds]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for _ in range(20):
+            for s, m, q, w, x in zip(streams, mems, qs, worlds, want):
+                with torch.cuda.stream(s):
+                    got.append((m.attend(q, w.scale), x))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in got)
+    assert all(m.status() == B.OK for m in mems)
+
+
 def test_calls_without_rows(torch, B):
     w = World(torch, [20], [0], 4, 128, 16, "bf16")
     mem = w.device(B)
