@@ -44,8 +44,11 @@ struct Cfg {
 };
 
 struct Shared : Roles {
-  int top[ROWS];                                   // a new maximum, ordered as integers; at the end sums of weights
+  int top[ROWS];                                   // a new maximum, ordered as integers
+  float sum[ROWS];                                 // of the weights, at an item's end: a place of its own, because one thread of a row
+                                                   // may be there before the other has read the last tile's maximum
 };
+static_assert(sizeof(Shared) <= 2048, "what Cfg::FREE leaves out");
 
 __device__ __forceinline__ void mma_tmem_a(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -330,14 +333,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (lane == 0) tc::mbar_arrive1(&sh.p_full[g & 1]);
       }
       // a row's sum from its two threads
-      if (half == 1) sh.top[r] = __float_as_int(l);
+      if (half == 1) sh.sum[r] = l;
       bar_softmax<SOFTMAX>();
       if (half == 0) {
-        l += __int_as_float(sh.top[r]);
-        sh.top[r] = __float_as_int(l);
+        l += sh.sum[r];
+        sh.sum[r] = l;
       }
       bar_softmax<SOFTMAX>();
-      l = __int_as_float(sh.top[r]);
+      l = sh.sum[r];
       if (n > 0) wait_for(&sh.o_full, (g - 1) & 1, &sh.dead);
       __syncwarp();
       tc::tc_fence_after();

@@ -754,6 +754,29 @@ def test_calls_of_three_streams_at_once(torch, B, dtype, rank):
     assert all(m.status() == B.OK for m in mems)
 
 
+@pytest.mark.parametrize("rank", [128, 256])
+@pytest.mark.parametrize("m,length", [(32, 100), (32, 128), (128, 250), (24, 1500)])
+def test_items_of_a_tile_while_the_gpu_is_shared(torch, B, rank, m, length):
+    """Items and pieces of 128 rows that end with the tile in which their reference is raised: a row's two threads, held up by
+    other calls' blocks, take the same maximum before the sums of its weights are joined."""
+    worlds = [World(torch, [length + 3 * i] * 40, [m] * 40, 5, rank, 64, "bf16", seed=70 + i, stale=False) for i in range(3)]
+    mems, qs = [w.device(B, starts=False) for w in worlds], [w.q.cuda() for w in worlds]
+    want = [m.attend(q, w.scale) for m, q, w in zip(mems, qs, worlds)]
+    for w, x in zip(worlds, want):
+        w.check_attend(x)
+    streams = [torch.cuda.Stream() for _ in worlds]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for _ in range(20):
+            for s, mem, q, w, x in zip(streams, mems, qs, worlds, want):
+                with torch.cuda.stream(s):
+                    got.append((mem.attend(q, w.scale), x))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in got)
+    assert all(mem.status() == B.OK for mem in mems)
+
+
 def test_calls_without_rows(torch, B):
     w = World(torch, [20], [0], 4, 128, 16, "bf16")
     mem = w.device(B)
