@@ -25,8 +25,8 @@
 // others), and the output's products of a run are added to its sums in fp32.
 //
 // Masks are looked at only in runs that some row does not see whole.  There, the values of tokens outside the piece
-// count as zero, and so do those of a token that holds a value that is not finite, whose scores
-// are then no numbers for the rows that see it.
+// count as zero, and so do those of a token that holds a value that is not finite or whose high part
+// is not, whose scores are then no numbers for the rows that see it.
 #include <algorithm>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -64,7 +64,8 @@ __device__ __forceinline__ void split(float x, uint32_t& hi, uint32_t& lo) {
   hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
   lo = __float_as_uint(x - __uint_as_float(hi));
 }
-__device__ __forceinline__ bool odd_number(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+// is x, or what split rounds it to, not finite?  The latter from 2^128 - 2^116 on
+__device__ __forceinline__ bool odd_number(float x) { return (__float_as_uint(x) & 0x7fffffffu) >= 0x7f7ff000u; }
 
 __device__ __forceinline__ void bar_team(int team) { asm volatile("bar.sync %0, 64;" ::"r"(team + 1) : "memory"); }
 // of a ballot whose bit 4 g + c is a quarter of token t(g): the tokens
@@ -339,7 +340,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
         while (sh.seg[(item + 1) & 1].more) fill_segment(a, run, share, *walk, sh.seg[(item + 1) & 1], shares);
       break;
     }
-    float* const sums = reinterpret_cast<float*>(mem);         // [WARPS][ROWS][LD], in place of the ring
+    float* const sums = reinterpret_cast<float*>(mem);         // [TEAMS][ROWS][LD], the warps of a team having their dimensions of a row; in place of the ring
     const int teams = min(n, TEAMS);                           // those that had a run
     if (team < teams)
 #pragma unroll

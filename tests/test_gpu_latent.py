@@ -425,6 +425,32 @@ def test_attend_chunks_what_masked_tokens_hold(torch, B, dtype, rank, strided, w
     assert not np.isfinite(got[40:m, :, 3]).any() and not np.isfinite(got[51:m]).any()
 
 
+EDGE = 2.0 ** 128 - 2.0 ** 116                                            # fp32 rows: from here on a number counts as infinite
+BELOW = float(np.nextafter(np.float32(EDGE), np.float32(0)))
+MOST = {"fp32": float(np.finfo(np.float32).max), "bf16": 2.0 ** 128 - 2.0 ** 120}
+
+
+@pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("dtype,value", [("fp32", v) for v in (MOST["fp32"], -MOST["fp32"], EDGE, -EDGE, BELOW)]
+                         + [("bf16", v) for v in (MOST["bf16"], -MOST["bf16"])])
+def test_attend_masked_tokens_of_the_largest_values(torch, B, dtype, rank, value):
+    """Latents and key parts at the types' ends: what one row sees reaches no other, within an item and across them."""
+    m, length = 12, 400
+    w = World(torch, [length], [m], 4, rank, 16, dtype, seed=3)
+    for at, column in ((length - 5, 3), (length - 3, rank + 1), (length - 2, rank - 1)):   # row 7 is the first that sees one
+        w.pages[int(w.table[0, at // 16]), at % 16, column] = value
+    assert w.pages.isinf().sum() == 0
+    mem = w.device(B)
+    for window in (0, 200):
+        got = mem.attend(w.q.cuda(), w.scale, window=window).double().cpu().numpy()
+        x = w.dense(0)
+        x[length - 5:] = 0                                                 # rows 0 .. 6 do not see them
+        out, size, dots = L.attend(w.q.double().numpy()[:7], x[:length - 5], rank, w.scale, True, window)
+        weight = 2 * (rank + 72) * U * dots + 2.0 ** -20 + (2.0 ** -8 if dtype == "bf16" else 0.0)
+        tol = half(dtype) * np.abs(out) + (1 + half(dtype)) * (weight + length * U) * size + 1e-37
+        assert (np.abs(got[:7] - out) <= tol).all()
+
+
 def test_attend_reports_bad_entries(torch, B):
     for dtype in DTYPES:
         w = World(torch, [40, 40, 40], [1, 1, 1], 4, 128, 16, dtype, max_pages=4, stale=False)
