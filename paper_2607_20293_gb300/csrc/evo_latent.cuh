@@ -30,6 +30,15 @@ constexpr int SLOT = BK * 256, HALF = BK * 128;    // bytes of 128 and of 64 dim
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
 constexpr float NONE = -3.402823466e38f;           // the reference of a row that has seen nothing
 
+// The softmax works on products <q, x> themselves, which are fp32 numbers where they times the scale need not be: 2^(f (s - m)) with
+// a positive factor f, and the scale's sign in the products.  So are the maxima of pieces.
+__device__ __forceinline__ float factor_of(const AttendArgs& a) {
+  return a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f);
+}
+__device__ __forceinline__ float sign_of(const AttendArgs& a) { return a.scale_log2 < 0.f ? -1.f : a.scale_log2 == 0.f ? 0.f : 1.f; }
+// how far a product may pass its reference
+__device__ __forceinline__ float far_of(float f) { return fminf(LAZY / f, 1e38f); }
+
 // An item's beginning and end, in tiles (items of N rows): they count in a run before its tiles.  (128 rows: 34.5 -> 31.3 us
 // for 64 chunks of 16 tokens; 64 rows: 40.8 -> 39.0 for 32 tokens; fewer: 84.4 -> 86.0 with 1 for 64 tokens, whose tiles are long)
 template <int N>
@@ -394,20 +403,20 @@ __device__ __forceinline__ Pieces pieces_of(const AttendArgs& a, const Run& run)
   }
   return x;
 }
-// a row's o and sum, with maximum top, and C further pieces of it
+// a row's o and sum, with maximum top, and C further pieces of it; f: the scores' factor
 template <int C, int D>
-__device__ __forceinline__ void join_pieces(float& top, float& sum, float (&o)[D], const float2 (&ml)[C], const float (&y)[C][D]) {
+__device__ __forceinline__ void join_pieces(float f, float& top, float& sum, float (&o)[D], const float2 (&ml)[C], const float (&y)[C][D]) {
   float m = top;
 #pragma unroll
   for (int i = 0; i < C; ++i) m = fmaxf(m, ml[i].x);
-  const float ref = m == -INFINITY ? 0.f : m, f = ex2_approx(top - ref);
+  const float ref = m == -INFINITY ? 0.f : m, down = ex2_approx((top - ref) * f);
   top = m;
-  sum *= f;
+  sum *= down;
 #pragma unroll
-  for (int e = 0; e < D; ++e) o[e] *= f;
+  for (int e = 0; e < D; ++e) o[e] *= down;
 #pragma unroll
   for (int i = 0; i < C; ++i) {
-    const float g = ex2_approx(ml[i].x - ref);
+    const float g = ex2_approx((ml[i].x - ref) * f);
     sum = fmaf(ml[i].y, g, sum);
 #pragma unroll
     for (int e = 0; e < D; ++e) o[e] = fmaf(y[i][e], g, o[e]);
@@ -428,6 +437,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) latent_join_kernel(const __gr
   if (x.n == 0) return;
   const int R = x.r0 + r;
   const bool on = r < N && R < x.s.count * a.group;
+  const float f = factor_of(a);
   float top = -INFINITY, sum = 0.f, o[4] = {};
   if (on)
     for (int p0 = group; p0 < x.n; p0 += 8 * groups) {
@@ -442,7 +452,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) latent_join_kernel(const __gr
         const float4 v = there ? *reinterpret_cast<const float4*>(a.part + at * RANK + 4 * lane) : make_float4(0.f, 0.f, 0.f, 0.f);
         y[i][0] = v.x, y[i][1] = v.y, y[i][2] = v.z, y[i][3] = v.w;
       }
-      join_pieces(top, sum, o, ml, y);
+      join_pieces(f, top, sum, o, ml, y);
     }
   if (groups > 1) {
     os[at][lane] = make_float4(o[0], o[1], o[2], o[3]);
@@ -453,7 +463,7 @@ __global__ void __launch_bounds__(JOIN_THREADS, 1) latent_join_kernel(const __gr
         const float4 v = os[at + e][lane];
         const float2 ml[1] = {stat[at + e]};
         const float y[1][4] = {{v.x, v.y, v.z, v.w}};
-        join_pieces(top, sum, o, ml, y);
+        join_pieces(f, top, sum, o, ml, y);
       }
   }
   if (!on || group != 0) return;
@@ -468,6 +478,7 @@ __global__ void __launch_bounds__(256) latent_join_wide_kernel(const __grid_cons
   const Pieces x = pieces_of<128>(a, run);
   const int R = x.n == 0 ? 0 : x.r0 + r;
   if (x.n == 0 || R >= x.s.count * a.group) return;
+  const float f = factor_of(a);
   float top = -INFINITY, sum = 0.f, o[8] = {};
   for (int p0 = 0; p0 < x.n; p0 += 4) {
     float2 ml[4];
@@ -480,7 +491,7 @@ __global__ void __launch_bounds__(256) latent_join_wide_kernel(const __grid_cons
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[i][e] = there ? part[e * 128] : 0.f;
     }
-    join_pieces(top, sum, o, ml, y);
+    join_pieces(f, top, sum, o, ml, y);
   }
   const float norm = sum == 0.f ? 0.f : 1.f / sum;
   uint32_t v[4];

@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
   if (tid == 0) fill_segment(a, run, share, *walk, sh.seg[0], shares);
   __syncthreads();
   int asked = 0;                                             // runs of this warp before this item's
+  const float f = factor_of(a), far = far_of(f), sign = sign_of(a);
   const int shift = 31 - __clz(a.m.page_tokens);
   for (int item = 0; sh.seg[item & 1].more; ++item) {
     const Segment& seg = sh.seg[item & 1];
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
     for (int j = 0; j < SLOTS; ++j) ask(j, page_of(j));
     int ahead = page_of(SLOTS);
     if (tid == 0) fill_segment(a, run, share, *walk, sh.seg[(item + 1) & 1], shares);   // while copies are under way
-    // queries: the fragments of a step pair, high parts and low parts
+    // queries, which take the scale's sign: the fragments of a step pair, high parts and low parts
 #pragma unroll
     for (int nr = 0; nr < NR; ++nr) {
       const int R = r0 + 8 * nr + g;
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
       for (int h = warp; h < STEPS; h += WARPS) {
         const float4 x = R < rows ? *reinterpret_cast<const float4*>(src + 16 * h) : make_float4(0.f, 0.f, 0.f, 0.f);
         uint4 hi, lo;
-        split(x.x, hi.x, lo.x), split(x.y, hi.y, lo.y), split(x.z, hi.z, lo.z), split(x.w, hi.w, lo.w);
+        split(x.x * sign, hi.x, lo.x), split(x.y * sign, hi.y, lo.y), split(x.z * sign, hi.z, lo.z), split(x.w * sign, hi.w, lo.w);
         uint4* dst = reinterpret_cast<uint4*>(mem + C::RING + (h * NR + nr) * 1024 + lane * 16);
         dst[0] = hi;
         dst[32] = lo;
@@ -167,7 +168,6 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
       top[nr][0] = top[nr][1] = -INFINITY;
     }
     const int tg = g / 2 + 4 * (g % 2);                        // the token of the scores' row g; row g + 8: 8 further
-    const float f = a.scale_log2;
     int j = 0;
     for (; run_of(j) < n; ++j) {
       const int slot = (asked + j) % SLOTS;
@@ -229,10 +229,6 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
         } else if (odd) {
           drop = quarters(__ballot_sync(0xffffffffu, bad0)) | quarters(__ballot_sync(0xffffffffu, bad1)) << 8;
         }
-#pragma unroll
-        for (int nr = 0; nr < NR; ++nr)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[nr][e] *= f;
         if (odd) {
           const int k1 = k0 + tg, k2 = k1 + 8;
 #pragma unroll
@@ -258,7 +254,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float m = fmaxf(s[nr][e], s[nr][2 + e]);
-          raise |= m > top[nr][e] + LAZY || (top[nr][e] == -INFINITY && m > -INFINITY);
+          raise |= m > top[nr][e] + far || (top[nr][e] == -INFINITY && m > -INFINITY);
         }
       if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
@@ -269,7 +265,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
             for (int y = 4; y < 32; y *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, y));
             m = fmaxf(m, top[nr][e]);
-            const float down = m == -INFINITY ? 1.f : ex2_approx(top[nr][e] - m);
+            const float down = m == -INFINITY ? 1.f : ex2_approx((top[nr][e] - m) * f);
             top[nr][e] = m;
             sum[nr][e] *= down;
 #pragma unroll
@@ -284,7 +280,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float m = top[nr][e % 2];
-          p[e] = ex2_approx(s[nr][e] - (m == -INFINITY ? 0.f : m));
+          p[e] = ex2_approx((s[nr][e] - (m == -INFINITY ? 0.f : m)) * f);
           sum[nr][e % 2] += p[e];
         }
 #pragma unroll
@@ -372,7 +368,7 @@ __global__ void __launch_bounds__(Cfg<RANK, NR>::THREADS, 1)
         if (w >= teams) break;
         const float2 ml = stat[w][r];
         const float4 y = *reinterpret_cast<const float4*>(sums + (w * C::ROWS + r) * C::LD + d);
-        const float fw = ex2_approx(ml.x - ref);
+        const float fw = ex2_approx((ml.x - ref) * f);
         l = fmaf(ml.y, fw, l);
         v = make_float4(fmaf(y.x, fw, v.x), fmaf(y.y, fw, v.y), fmaf(y.z, fw, v.z), fmaf(y.w, fw, v.w));
       }

@@ -208,9 +208,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
     // A wait that is in vain ends no turn: the barriers of the softmax want all of its warps.
     const int k = tid % BK, part = warp / 4, c0 = part * HC;
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    // the softmax works with a positive factor: the scale's sign goes to the scores
-    const float f = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f), far = fminf(LAZY / f, 1e38f);
-    const float sign = a.scale_log2 < 0.f ? -1.f : a.scale_log2 == 0.f ? 0.f : 1.f;
+    const float f = factor_of(a), far = far_of(f), sign = sign_of(a);
     // the first warp looks the next item up for all of them
     bool shares = false;
     const auto look_up = [&](Segment& q) {
@@ -387,7 +385,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         if (q.whole)
           sh.top[tid] = __float_as_int(l == 0.f ? 0.f : 1.f / l);
         else
-          a.ml[q.slot * N + tid] = make_float2(sh.ref[tid] == NONE ? -INFINITY : sh.ref[tid] * f, l);
+          a.ml[q.slot * N + tid] = make_float2(sh.ref[tid] == NONE ? -INFINITY : sh.ref[tid], l);
         sh.ref[tid] = NONE;
         const int R = min(x.r0 + tid, x.last), token = R / a.group;
         sh.to[tid] = (long long)(t.first + token) * a.ldo + (long long)(R - token * a.group) * RANK;

@@ -190,9 +190,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     // A wait that is in vain ends no turn: the barriers of the softmax want all of its warps.
     const int r = tid % ROWS, half = tid / ROWS;
     const uint32_t lanes = (uint32_t)(32 * (warp % 4)) << 16;
-    // the softmax works with a positive factor: the scale's sign goes to the scores
-    const float f = a.scale_log2 == 0.f ? 1.f : fmaxf(fabsf(a.scale_log2), 1.1754944e-38f), far = fminf(LAZY / f, 1e38f);
-    const float sign = a.scale_log2 < 0.f ? -1.f : a.scale_log2 == 0.f ? 0.f : 1.f;
+    const float f = factor_of(a), far = far_of(f), sign = sign_of(a);
     // the first warp looks the next item up for all of them
     bool shares = false;
     const auto look_up = [&](Segment& q) {
@@ -347,7 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool whole = q.whole;
       const float norm = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
       float* const part = a.part + ((long long)q.slot * RANK + half * (RANK / 2)) * N + r;
-      if (!whole && half == 0) a.ml[(long long)q.slot * N + r] = make_float2(ref == NONE ? -INFINITY : ref * f, l);
+      if (!whole && half == 0) a.ml[(long long)q.slot * N + r] = make_float2(ref == NONE ? -INFINITY : ref, l);
 #pragma unroll 1
       for (int j = 0; j < RANK / 2; j += 32) {
         float o[32];

@@ -451,6 +451,41 @@ def test_attend_masked_tokens_of_the_largest_values(torch, B, dtype, rank, value
         assert (np.abs(got[:7] - out) <= tol).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("N,m", [(1, 1), (1, 20), (76, 1), (76, 20)])
+def test_attend_scores_beyond_fp32_once_scaled(torch, B, dtype, rank, N, m):
+    """Scores are fp32 numbers and so is the scale, their products are not: a few long memories in pieces and many whole ones.
+    The token of the largest score has all of the weight, and tokens of one score share it equally."""
+    H, length, page = 8, 3000 if N == 1 else 250, 64
+    w = World(torch, [length] * N, [m] * N, H, rank, page, dtype, seed=4, stale=False)
+    eighth = torch.arange(page) % 8 == 7
+    w.q[...] = 0
+    w.q[..., 1:rank] = 2.0 ** 100
+    q = w.q.cuda()
+
+    def attend(scale, best=None, q=q):                                     # tokens of 0.5, but one
+        w.pages[..., :rank] = 0.5
+        w.pages[..., 0] = eighth.to(w.t)
+        if best is not None:
+            for n in range(N):
+                w.pages[int(w.table[n, (length - 9) // page]), (length - 9) % page, :rank] = best
+        mem = w.device(B, starts=False)
+        got = mem.attend(q, scale, causal=False).double().cpu()
+        assert mem.status() == B.OK
+        return got
+
+    assert (attend(2.0 ** 60, 1.0) == 1).all()
+    assert (attend(-2.0 ** 60, 0.25) == 0.25).all()                        # all scores far below zero
+    assert (attend(2.0 ** 60, 0.25, -q) == 0.25).all()
+    # the mean of 0 and 1 over the tokens, whose weights are 1 each: their count is exact
+    mean = (length // 8) / length
+    for scale in (2.0 ** 60, -2.0 ** 60):
+        got = attend(scale)
+        assert (got[..., 1:] == 0.5).all()
+        assert ((got[..., 0] - mean).abs() <= (half(dtype) + 4 * U) * mean).all()   # a sum's reciprocal, a product and the result's rounding
+
+
 def test_attend_reports_bad_entries(torch, B):
     for dtype in DTYPES:
         w = World(torch, [40, 40, 40], [1, 1, 1], 4, 128, 16, dtype, max_pages=4, stale=False)
