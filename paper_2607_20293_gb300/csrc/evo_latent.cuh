@@ -28,7 +28,8 @@ constexpr int BK = 128;                            // tokens of a tile
 constexpr int SMS = 152;
 constexpr int SLOT = BK * 256, HALF = BK * 128;    // bytes of 128 and of 64 dimensions of a tile
 constexpr float LAZY = 8.f;                        // log2 of how far a weight may pass 1
-constexpr float NONE = -3.402823466e38f;           // the reference of a row that has seen nothing
+// The reference of a row that has seen nothing.  It is one like any other: scores next to it do not raise it, and have weights
+constexpr float NONE = -3.402823466e38f;
 
 // The softmax works on products <q, x> themselves, which are fp32 numbers where they times the scale need not be: 2^(f (s - m)) with
 // a positive factor f, and the scale's sign in the products.  So are the maxima of pieces.

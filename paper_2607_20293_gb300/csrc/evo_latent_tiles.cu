@@ -317,7 +317,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
           bar_softmax<SOFTMAX>();
           if (tid < N) {
             const float old = sh.ref[tid], m = fmaxf(old, unordered(sh.top[tid]));
-            sh.top[tid] = __float_as_int(old == NONE ? 1.f : ex2_approx((old - m) * f));
+            sh.top[tid] = __float_as_int(ex2_approx((old - m) * f));
             sh.ref[tid] = m;
           }
           bar_softmax<SOFTMAX>();
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(Cfg<RANK, N>::THREADS, 1)
         if (q.whole)
           sh.top[tid] = __float_as_int(l == 0.f ? 0.f : 1.f / l);
         else
-          a.ml[q.slot * N + tid] = make_float2(sh.ref[tid] == NONE ? -INFINITY : sh.ref[tid], l);
+          a.ml[q.slot * N + tid] = make_float2(sh.ref[tid], l);
         sh.ref[tid] = NONE;
         const int R = min(x.r0 + tid, x.last), token = R / a.group;
         sh.to[tid] = (long long)(t.first + token) * a.ldo + (long long)(R - token * a.group) * RANK;

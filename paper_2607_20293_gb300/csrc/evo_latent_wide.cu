@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           bar_softmax<SOFTMAX>();
           atomicMax(&sh.top[r], ordered(top));
           bar_softmax<SOFTMAX>();
-          const float m = fmaxf(ref, unordered(sh.top[r])), down = ref == NONE ? 1.f : ex2_approx((ref - m) * f);
+          const float m = fmaxf(ref, unordered(sh.top[r])), down = ex2_approx((ref - m) * f);
           ref = m;
           l *= down;
           if (i > 0) {
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool whole = q.whole;
       const float norm = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
       float* const part = a.part + ((long long)q.slot * RANK + half * (RANK / 2)) * N + r;
-      if (!whole && half == 0) a.ml[(long long)q.slot * N + r] = make_float2(ref == NONE ? -INFINITY : ref, l);
+      if (!whole && half == 0) a.ml[(long long)q.slot * N + r] = make_float2(ref, l);
 #pragma unroll 1
       for (int j = 0; j < RANK / 2; j += 32) {
         float o[32];

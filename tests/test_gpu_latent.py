@@ -486,6 +486,27 @@ def test_attend_scores_beyond_fp32_once_scaled(torch, B, dtype, rank, N, m):
         assert ((got[..., 0] - mean).abs() <= (half(dtype) + 4 * U) * mean).all()   # a sum's reciprocal, a product and the result's rounding
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("N,m", [(1, 1), (152, 1), (1, 20), (76, 20)])
+def test_attend_scores_near_the_lowest_number(torch, B, dtype, rank, N, m):
+    """The first 200 tokens have scores of -1.75 * 2^127, which a scale of 1e-37 makes -29.8 beside the others' 0."""
+    H, length, page = 8, 600, 64
+    w = World(torch, [length] * N, [m] * N, H, rank, page, dtype, seed=5, stale=False)
+    tokens = torch.zeros(w.table.shape[1] * page, rank + ROPE)
+    tokens[:200, 1], tokens[200:, 1] = 1, 2
+    tokens[:200, rank + 3] = -1.75 * 2.0 ** 63
+    for n in range(N):
+        w.pages[w.table[n].long()] = tokens.to(w.t).unflatten(0, (-1, page))
+    w.q[...] = 0
+    w.q[..., rank + 3] = 2.0 ** 64
+    mem = w.device(B, starts=False)
+    w.check_attend(mem.attend(w.q.cuda(), 1e-37, causal=False), causal=False, scale=1e-37)
+    w.check_attend(mem.attend(w.q.cuda(), 1e-37, causal=False, window=450), causal=False, scale=1e-37, window=450)
+    w.lens = [200] * N                                                     # and no others
+    w.check_attend(w.device(B, starts=False).attend(w.q.cuda(), 1e-37, causal=False), causal=False, scale=1e-37)
+
+
 def test_attend_reports_bad_entries(torch, B):
     for dtype in DTYPES:
         w = World(torch, [40, 40, 40], [1, 1, 1], 4, 128, 16, dtype, max_pages=4, stale=False)
