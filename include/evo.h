@@ -496,8 +496,9 @@ evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, 
  *   mem      dtype of lat and its format (EVO_ERR_UNSUPPORTED otherwise), head_dim 128, n_kv_head = lat's n_head, as many
  *            sequences; its lens and starts are not read, its pages meet no other buffer, and no two tokens of a
  *            call are the same token of the same of its pages
- * Sums are fp32 (with fp32 rows of products that are off by at most 2^-21 of themselves), one rounding.  A range that is not within the memory, or a page entry outside its pool, makes
- * EVO_ERR_CORRUPT in lat's status, and no such token is written.  Asynchronous on the stream. */
+ * Sums are fp32, with fp32 rows of products that are off by at most 2^-21 of themselves; one rounding.  Numbers that are
+ * not finite make what they make in the sums above.  A range that is not within the memory, or a page entry outside
+ * its pool, makes EVO_ERR_CORRUPT in lat's status, and no such token is written.  Asynchronous on the stream. */
 evo_status evo_latent_expand(const evo_latent* lat, const void* w_k, const void* w_v, const int32_t* first,
                              int32_t max_new, int32_t max_len, const evo_memory* mem, void* stream);
 

@@ -345,6 +345,14 @@ __device__ __forceinline__ int place8(int n) { return n / 2 + 4 * (n % 2); }
 // the place of product p of 16: column 2 c + e of tile t is 4 c + 2 t + e
 __device__ __forceinline__ int place16(int p) { return 8 * (p / 2 % 2) + place8(p / 4 * 2 + p % 2); }
 
+// <x, w>, whatever they hold
+__device__ __forceinline__ float plain_product(const float* x, const float* w, int n) {
+  double sum = 0.;
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) sum = fma((double)x[i], (double)w[i], sum);
+  return (float)sum;
+}
+
 template <int BM>
 __global__ void __launch_bounds__(F32Cfg<BM>::THREADS, 2) latent_expand_kernel(const __grid_constant__ LatentExpandArgs a, int tiles) {
   using C = F32Cfg<BM>;
@@ -451,6 +459,8 @@ __global__ void __launch_bounds__(F32Cfg<BM>::THREADS, 2) latent_expand_kernel(c
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[i][j][e] += part[i][j][e];
   }
+  const auto out_of = [&](long long to, int o) { return o < LATENT_KEY ? keys + to * 128 + o : values + to * 128 + o - LATENT_KEY; };
+  bool odd = false;
 #pragma unroll
   for (int i = 0; i < 2 * MT; ++i) {                         // token 8 i + g: of each two tiles four products
     const long long to = to_row[8 * i + g];
@@ -459,9 +469,26 @@ __global__ void __launch_bounds__(F32Cfg<BM>::THREADS, 2) latent_expand_kernel(c
     for (int j = 0; j < 3; ++j) {
       const int o = 48 * warp + 16 * j + 4 * c, b = 2 * (i % 2);
       const float4 v = make_float4(sum[i / 2][2 * j][b], sum[i / 2][2 * j][b + 1], sum[i / 2][2 * j + 1][b], sum[i / 2][2 * j + 1][b + 1]);
-      *reinterpret_cast<float4*>(o < LATENT_KEY ? keys + to * 128 + o : values + to * 128 + o - LATENT_KEY) = v;
+      *reinterpret_cast<float4*>(out_of(to, o)) = v;
+      odd |= !isfinite(v.x) || !isfinite(v.y) || !isfinite(v.z) || !isfinite(v.w);
     }
   }
+  // An infinite number, one from 2^128 - 2^116 on (its high part is infinite) and a NaN make parts that are no numbers, and so
+  // every sum with one of them: such sums are done again as they are written down (by the thread that stored them; never
+  // where all is finite)
+  if (odd)
+#pragma unroll 1
+    for (int i = 0; i < 6 * MT; ++i) {
+      const int y = 8 * (i / 3) + g, o = 48 * warp + 16 * (i % 3) + 4 * c;
+      if (to_row[y] < 0) continue;
+      float* const out = out_of(to_row[y], o);
+      const float* const token = pool + from_row[y] * row;
+      const float* const map = o < LATENT_KEY ? static_cast<const float*>(a.w_k) + ((long long)h * LATENT_KEY + o) * rank
+                                              : static_cast<const float*>(a.w_v) + ((long long)h * LATENT_VALUE + o - LATENT_KEY) * rank;
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e)
+        if (!isfinite(out[e])) out[e] = plain_product(token, map + (long long)e * rank, rank);
+    }
 }
 
 template <int BM>

@@ -641,6 +641,56 @@ def test_expand_reports_what_it_cannot_write(torch, B, dtype):
     assert not torch.equal(got[int(e.table[4, 2]), :, 13:], was[int(e.table[4, 2]), :, 13:])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", RANKS)
+@pytest.mark.parametrize("most", [120, 16])
+def test_expand_values_that_are_not_finite(torch, B, dtype, rank, most):
+    """Infinities, NaN and the largest numbers in latents and maps: as the definition has it, product by product."""
+    w = World(torch, [120, 40], [1, 1], 3, rank, 16, dtype, seed=21, stale=False)
+    largest = MOST[dtype]
+    special = [float("inf"), float("-inf"), float("nan"), largest, -largest, EDGE if dtype == "fp32" else largest, BELOW if dtype == "fp32" else -largest]
+    at = [119 - 2 * i for i in range(len(special))]
+    for i, v in zip(at, special):
+        w.pages[int(w.table[0, i // 16]), i % 16, rank // 2] = v
+    w.pages[int(w.table[1, 2]), 7, :2] = torch.tensor([float("inf"), float("-inf")])      # token 39: no number
+    w.pages[int(w.table[1, 2]), 6, 1] = 0.25                              # token 38
+    w.pages[:, :, 0] *= 0.125                                             # meets the largest weight: no product overflows
+    mem = w.device(B)
+    e = Expanded(w, B, 32)
+    e.w_k[:, 3, rank // 2] = 0                                            # 0 * inf, and 0 * the largest
+    e.w_v[1, 5, 0] = largest
+    e.w_v[2, 9, 1] = float("inf")
+    first = torch.tensor([max(0, ln - most) for ln in w.lens], dtype=torch.int32)
+    mem.expand(e.w_k.cuda(), e.w_v.cuda(), e.mem, first=first.cuda(), max_new=most)
+    assert mem.status() == B.OK
+    wk, wv = e.w_k.double().numpy(), e.w_v.double().numpy()
+    pages = [p.cpu() for p in e.pages]
+    found = 0
+    for n, ln in enumerate(w.lens):
+        pos = torch.arange(int(first[n]), ln)
+        where, slot = e.table[n][pos // 32].long(), pos % 32
+        x = w.dense(n)[int(first[n]):]
+        with np.errstate(invalid="ignore", over="ignore"):
+            # the sums in the order of the dimensions, so that no infinity comes from elsewhere
+            want = [np.zeros((len(x), 3, 64)), np.zeros((len(x), 3, 128))]
+            size = [np.zeros_like(y) for y in want]
+            for j in range(rank):
+                for y, s, maps in zip(want, size, (wk, wv)):
+                    y += x[:, j, None, None] * maps[None, :, :, j]
+                    s += np.abs(x[:, j, None, None] * maps[None, :, :, j])
+            for p, y, s, width in zip(pages, want, size, (64, 128)):
+                got = p.transpose(1, 2)[where, slot].double().numpy()[..., :width]
+                over = np.abs(y) > MOST[dtype] * (1 + half(dtype) / 2)     # an infinity of the type, or within a rounding of one
+                odd = ~np.isfinite(y)
+                assert np.array_equal(np.isnan(got), np.isnan(y))
+                assert np.array_equal(got[np.isinf(y)], y[np.isinf(y)])
+                fine = ~odd & ~over
+                tol = (half(dtype) * np.abs(y) + (rank + 8) * U * s) * (1 + half(dtype)) + 1e-37
+                assert (np.abs(got - y) <= tol)[fine].all()
+                found += int(odd.sum())
+    assert found > 100
+
+
 # ---------------------------------------------------------------- as they are used
 
 @pytest.mark.parametrize("dtype", DTYPES)
