@@ -491,8 +491,8 @@ evo_status evo_latent_attend(const evo_latent* lat, const void* q, int64_t ldq, 
  *   key of head h = (w_k[h] c | k),   value of head h = w_v[h] c
  *   w_k, w_v device [n_head][64][rank] and [n_head][128][rank] of dtype, contiguous, start on 16 bytes
  *   first    device [n_seq] or NULL (zero)
- *   max_new, max_len  at least the most tokens of a sequence that are written, and the longest latent memory; they
- *            size the launch
+ *   max_new, max_len  at least the most tokens of a sequence that are written, and the longest latent memory, each at most
+ *            max_pages * page_tokens; they size the launch
  *   mem      dtype of lat and its format (EVO_ERR_UNSUPPORTED otherwise), head_dim 128, n_kv_head = lat's n_head, as many
  *            sequences; its lens and starts are not read, its pages meet no other buffer, and no two tokens of a
  *            call are the same token of the same of its pages

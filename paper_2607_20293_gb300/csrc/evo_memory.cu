@@ -415,7 +415,9 @@ evo_status evo_latent_expand(const evo_latent* lat, const void* w_k, const void*
   if (s != EVO_OK) return s;
   if (mem->dtype != lat->dtype || mem->format == EVO_CACHE_E4M3) return EVO_ERR_UNSUPPORTED;
   if (mem->head_dim != LATENT_KEY + LATENT_ROPE || mem->n_kv_head != lat->n_head || mem->n_seq != lat->n_seq) return EVO_ERR_SHAPE;
-  if (max_new < 0 || max_len < 0 || max_new > max_len || max_len > m.max_pages * m.page_tokens) return EVO_ERR_ARG;
+  const int most = m.max_pages * m.page_tokens;
+  if (max_new < 0 || max_len < 0 || max_new > most || max_len > most) return EVO_ERR_ARG;
+  max_new = max_new < max_len ? max_new : max_len;            // a bound above the longest memory says no more than that
   if (!w_k || !w_v || !aligned(w_k, 16) || !aligned(w_v, 16)) return EVO_ERR_ARG;
   // blocks of the launch
   if (m.n_seq > 0 && ((long long)max_new / 64 + 2) * m.n_head > INT_MAX / 2 / m.n_seq) return EVO_ERR_SHAPE;

@@ -593,6 +593,16 @@ def test_expand_of_the_newest_tokens(torch, B, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_expand_with_a_loose_bound_on_the_new_tokens(torch, B, dtype):
+    w = World(torch, [130, 1, 0, 64], [1] * 4, 4, 128, 16, dtype, seed=7, max_pages=60)
+    mem = w.device(B)
+    e = Expanded(w, B, 64)
+    mem.expand(e.w_k.cuda(), e.w_v.cuda(), e.mem, max_new=60 * 16, max_len=130)
+    e.check()
+    assert mem.status() == B.OK
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_expand_long_memories(torch, B, dtype):
     w = World(torch, [2500, 777], [1, 1], 10, 128, 128, dtype, seed=2)
     mem = w.device(B)

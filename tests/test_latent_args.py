@@ -144,6 +144,14 @@ def test_calls_that_do_nothing(B):
     assert expand(B, view(B, **none), to_view(B, n_seq=0, table=None, lens=None)) == B.OK
 
 
+def test_expansion_bounds_are_independent(B):
+    """A bound on the written tokens may be looser than the one on the memories (nothing is launched here: no sequences)."""
+    none = dict(n_seq=0, table=None, lens=None)
+    m, to = view(B, **none, starts=None), to_view(B, **none)
+    for max_new, max_len, code in ((64, 0, B.OK), (64, 17, B.OK), (3, 64, B.OK), (65, 64, B.ERR_ARG), (64, 65, B.ERR_ARG), (-1, 3, B.ERR_ARG)):
+        assert expand(B, m, to, max_new=max_new, max_len=max_len) == code
+
+
 def test_binding_checks_tensors(B):
     torch = pytest.importorskip("torch")
     pages = torch.zeros(4, 16, 192, dtype=torch.bfloat16)
